@@ -68,6 +68,7 @@ extern "C" {
 #define GC_MAX_ELL 8      /* communication factor ell                        */
 #define GC_MAX_DELTA 32   /* chunks per worker                               */
 #define GC_MAX_REPL 32    /* copies of one chunk in the cluster (gamma_i)    */
+#define GC_MAX_COLS 32768 /* columns of the row-wise operators (dropout, layer norm) */
 
 /* ---- library ---------------------------------------------------------- */
 /* Thread-local text of the last error raised on this thread ("" if none). */
@@ -248,6 +249,66 @@ size_t gc_chunk_grads_workspace(int N, int n_c, int d, int x_dtype);
 int gc_chunk_grads(const void* X, int x_dtype, const float* y, const float* w, int N, int n_c,
                    int d, int loss, float* G, double* loss_out, void* ws, size_t ws_bytes,
                    void* stream);
+
+/* ---- dropout from a counter-based generator, with an optional residual ----
+ *   out = residual + D(x),  D(x)[r][c] = keep(r, c) ? x[r][c] 2^16 / (2^16 - t) : 0,
+ * t = round(2^16 p).  keep(r, c) is whether a 16-bit number is >= t: number c mod 8 of the eight
+ * halves (low first) of the words of Philox4x32-10 at counter (e low, e high, offset low, offset
+ * high), e = (row0 + r) ceil(cols / 8) + floor(c / 8), under the key (seed low, seed high).  The mask
+ * is a function of (seed, offset, row0 + r, c) and is never stored: the gradient of D is gc_dropout
+ * on the gradient with the same numbers, and every worker that holds a point (row0 = the first of the
+ * points it works on) draws the same mask, which a gradient code needs of the copies of a chunk.
+ * The scale is that of the p drawn, t / 2^16, so E[D(x)] = x.  A dropped element is 0 whatever x
+ * holds.  Computed in fp32, rounded once.
+ *   x, residual, out   rows x cols of `dtype` (GC_F32 or GC_BF16), rows ldx, ldr, ldo elements apart
+ *           (>= cols), any alignment; residual may be NULL.  out may be x or residual itself (same
+ *           pointer and stride), and must not overlap them in another way.
+ *   p       in [0, 1).  seed, offset: any (offset counts the draws of a program: step and place).
+ *   rows    0 .. 2^40 (0: nothing is launched).  cols 1 .. GC_MAX_COLS.
+ * No workspace.
+ */
+int gc_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype, int64_t rows,
+               int cols, double p, uint64_t seed, uint64_t offset, int64_t row0, void* out, int64_t ldo,
+               void* stream);
+
+/* ---- layer norm, after an optional residual branch with dropout --------------
+ *   h = residual + D(x)  (gc_dropout's; h = x without both),
+ *   mean = sum_c h / cols,  rstd = (sum_c (h - mean)^2 / cols + eps)^(-1/2),
+ *   y = (h - mean) rstd gamma + beta
+ * for every row, in fp32; the statistics and y are of h before it is rounded for the store.
+ *   x, residual, y, h   as in gc_dropout; residual and h may be NULL.  y may be x, and h residual or x
+ *           (same pointer and stride); y and h are not the same.
+ *   gamma, beta   cols fp32, NULL: ones, zeros.    eps >= 0.
+ *   mean, rstd    rows fp32 outputs, each nullable.
+ * No workspace.
+ */
+int gc_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype, int64_t rows,
+                  int cols, const float* gamma, const float* beta, float eps, double p, uint64_t seed,
+                  uint64_t offset, int64_t row0, void* y, int64_t ldy, void* h, int64_t ldh, float* mean,
+                  float* rstd, void* stream);
+
+/* ---- gradient of gc_layer_norm, parameters' per chunk -----------------------
+ * With dy the gradient of y and dh (NULL: zero) that which reaches h besides, n = (h - mean) rstd and
+ * a = dy gamma, for every row
+ *   dresidual = rstd (a - mean_c(a) - n mean_c(a n)) + dh      (the gradient of h, and of residual)
+ *   dx        = D(dresidual)                                   (the mask of the forward call)
+ * and for chunk i, rows [i n_c, (i + 1) n_c), un-normalised sums as in gc_chunk_grads
+ *   G[i][0 .. cols)      = sum_r dy n      (of gamma)
+ *   G[i][cols .. 2 cols) = sum_r dy        (of beta).
+ *   dy, h, dh, dx, dresidual   N n_c rows of cols, as in gc_dropout; dx may be dy or dh, dresidual dh or
+ *           dy (same pointer and stride), dx and dresidual not the same.
+ *   mean, rstd   N n_c fp32, the forward call's.    gamma as there.
+ *   G            N rows, ldg >= 2 cols elements apart, fp32: a slice of the chunk gradients of a model.
+ * dx, dresidual and G are each nullable, not all of them.  The sums are added in a fixed order.
+ * Workspace: gc_layer_norm_backward_workspace(N, n_c, cols) bytes; the size depends on the current
+ * device's number of SMs.
+ */
+size_t gc_layer_norm_backward_workspace(int N, int n_c, int cols);
+int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const float* mean,
+                           const float* rstd, const float* gamma, const void* dh, int64_t lddh, int dtype,
+                           int N, int n_c, int cols, double p, uint64_t seed, uint64_t offset,
+                           int64_t row0, void* dx, int64_t lddx, void* dresidual, int64_t lddr, float* G,
+                           int64_t ldg, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- Algorithm 1, Find-Encoding-Coeff, batched over patterns ----------
  * R      ell x m float64, the PS's Gaussian matrix (Sec. II).

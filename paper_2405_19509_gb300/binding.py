@@ -26,8 +26,8 @@ GC_CYCLIC, GC_EXPLICIT = 0, 1
 GC_F32, GC_BF16 = 0, 1
 GC_LSQ, GC_LOGISTIC = 0, 1
 
-_i, _sz, _p, _d, _f, _i64 = (ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_double,
-                             ctypes.c_float, ctypes.c_int64)
+_i, _sz, _p, _d, _f, _i64, _u64 = (ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_double,
+                                   ctypes.c_float, ctypes.c_int64, ctypes.c_uint64)
 
 
 def _sig(name, res, *args):
@@ -79,6 +79,12 @@ _sig("gc_mse_workspace", _sz, _i, _i, _i, _i, _i, _i)
 _sig("gc_mse", _i, _p, _i, _p, _i, _i, _i, _p, _i, _p, _i, _p, _p, _p, _p, _sz, _p)
 _sig("gc_sgd_step", _i, _p, _p, _i, _f, _i64, _p)
 _sig("gc_live_step", _i, _p, _p, _i, _p, _i, _i, _i, _p, _p, _i, _f, _i64, _p, _p, _p, _p)
+_sig("gc_dropout", _i, _p, _i64, _p, _i64, _i, _i64, _i, _d, _u64, _u64, _i64, _p, _i64, _p)
+_sig("gc_layer_norm", _i, _p, _i64, _p, _i64, _i, _i64, _i, _p, _p, _f, _d, _u64, _u64, _i64, _p, _i64,
+     _p, _i64, _p, _p, _p)
+_sig("gc_layer_norm_backward_workspace", _sz, _i, _i, _i)
+_sig("gc_layer_norm_backward", _i, _p, _i64, _p, _i64, _p, _p, _p, _p, _i64, _i, _i, _i, _i, _d, _u64,
+     _u64, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _sz, _p)
 
 
 class GCError(RuntimeError):
@@ -139,6 +145,34 @@ def _dev(t, dtype, name, shape=None):
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     return t.data_ptr()
+
+
+def _rows(t, dtype, name, shape):
+    """(device pointer, row stride) of a CUDA matrix whose rows may lie apart (None -> NULL, 0)."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"the elements of a row of {name} must lie next to each other")
+    if ld < shape[1] and shape[0] > 1:
+        raise ValueError(f"the rows of {name} overlap")
+    return t.data_ptr(), ld
+
+
+def _elt(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise TypeError(f"{name} must be a matrix")
+    if t.dtype is torch.bfloat16:
+        return GC_BF16
+    if t.dtype is torch.float32:
+        return GC_F32
+    raise TypeError(f"{name} must be float32 or bfloat16")
 
 
 class Workspace:
@@ -268,6 +302,84 @@ def gc_chunk_grads(X, y, w, N: int, n_c: int, loss: int, G=None, loss_out=None,
                               _dev(G, torch.float32, "G", (N, d)),
                               _dev(loss_out, torch.float64, "loss_out"), wp, wn, _stream()))
     return G
+
+
+# ---------------------------------------------------------------- dropout, layer norm
+def gc_dropout(x, p: float, seed: int, offset: int = 0, row0: int = 0, residual=None, out=None):
+    """residual + D(x) (rows x cols): D drops an element with probability p and scales the others, by
+    a mask that is a function of (seed, offset, row0 + row, column) and is never stored.  The
+    gradient of D is gc_dropout of the gradient with the same numbers.  Rows may be strided."""
+    dt = _elt(x, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    xp, ldx = _rows(x, x.dtype, "x", x.shape)
+    rp, ldr = _rows(residual, x.dtype, "residual", x.shape)
+    op, ldo = _rows(out, x.dtype, "out", x.shape)
+    _check(lib.gc_dropout(xp, ldx, rp, ldr, dt, x.shape[0], x.shape[1], p, seed, offset, row0, op, ldo,
+                          _stream()))
+    return out
+
+
+def gc_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, p: float = 0.0,
+                  seed: int = 0, offset: int = 0, row0: int = 0, y=None, h=None, mean=True, rstd=True):
+    """y = layer norm of h = residual + D(x) (gc_dropout's D; h = x without both).  Returns dict with
+    y, h (x itself where there is neither residual nor dropout and no tensor is given for it), and
+    mean, rstd (rows, float32; None where False is passed): what gc_layer_norm_backward takes."""
+    dt = _elt(x, "x")
+    rows, cols = x.shape
+    dev = x.device
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    if h is None and (residual is not None or p > 0):
+        h = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    if mean is True:
+        mean = torch.empty(rows, dtype=torch.float32, device=dev)
+    if rstd is True:
+        rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+    mean, rstd = (t if isinstance(t, torch.Tensor) else None for t in (mean, rstd))
+    xp, ldx = _rows(x, x.dtype, "x", x.shape)
+    rp, ldr = _rows(residual, x.dtype, "residual", x.shape)
+    yp, ldy = _rows(y, x.dtype, "y", x.shape)
+    hp, ldh = _rows(h, x.dtype, "h", x.shape)
+    _check(lib.gc_layer_norm(xp, ldx, rp, ldr, dt, rows, cols,
+                             _dev(gamma, torch.float32, "gamma", (cols,)),
+                             _dev(beta, torch.float32, "beta", (cols,)), eps, p, seed, offset, row0, yp,
+                             ldy, hp, ldh, _dev(mean, torch.float32, "mean", (rows,)),
+                             _dev(rstd, torch.float32, "rstd", (rows,)), _stream()))
+    return {"y": y, "h": x if h is None else h, "mean": mean, "rstd": rstd}
+
+
+def gc_layer_norm_backward(dy, h, mean, rstd, gamma, N: int, n_c: int, dh=None, p: float = 0.0,
+                           seed: int = 0, offset: int = 0, row0: int = 0, dx=True, dresidual=False,
+                           G=True, ws: Workspace | None = None):
+    """Gradient of gc_layer_norm.  Returns dict with dx (of x), dresidual (of residual) and G (N x 2 cols
+    float32: per chunk the sums for gamma, then those for beta); booleans ask for an output, tensors
+    are written into (G may be a column slice of a larger matrix of chunk gradients)."""
+    dt = _elt(dy, "dy")
+    rows, cols = dy.shape
+    if rows != N * n_c:
+        raise ValueError("dy must have N * n_c rows")
+    dev = dy.device
+
+    def out(t, shape, dtype):
+        if isinstance(t, torch.Tensor):
+            return t
+        return torch.empty(shape, dtype=dtype, device=dev) if t else None
+    dx, dresidual = out(dx, dy.shape, dy.dtype), out(dresidual, dy.shape, dy.dtype)
+    G = out(G, (N, 2 * cols), torch.float32)
+    yp, lddy = _rows(dy, dy.dtype, "dy", dy.shape)
+    hp, ldh = _rows(h, dy.dtype, "h", dy.shape)
+    ap, lddh = _rows(dh, dy.dtype, "dh", dy.shape)
+    xp, lddx = _rows(dx, dy.dtype, "dx", dy.shape)
+    rp, lddr = _rows(dresidual, dy.dtype, "dresidual", dy.shape)
+    gp, ldg = _rows(G, torch.float32, "G", (N, 2 * cols))
+    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_layer_norm_backward_workspace",
+                                        N, n_c, cols), dev)
+    _check(lib.gc_layer_norm_backward(
+        yp, lddy, hp, ldh, _dev(mean, torch.float32, "mean", (rows,)),
+        _dev(rstd, torch.float32, "rstd", (rows,)), _dev(gamma, torch.float32, "gamma", (cols,)), ap, lddh,
+        dt, N, n_c, cols, p, seed, offset, row0, xp, lddx, rp, lddr, gp, ldg, wp, wn, _stream()))
+    return {"dx": dx, "dresidual": dresidual, "G": G}
 
 
 # ---------------------------------------------------------------- Algorithm 1

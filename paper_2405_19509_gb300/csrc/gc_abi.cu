@@ -281,6 +281,94 @@ int gc_chunk_grads(const void* X, int x_dtype, const float* y, const float* w, i
                           as_stream(stream));
 }
 
+// ---------------------------------------------------------------- dropout, layer norm
+static int check_rowwise(int dtype, int64_t rows, int cols, double p, int64_t row0) {
+  if (dtype != GC_F32 && dtype != GC_BF16) return fail(GC_ERR_ARG, "dtype=%d", dtype);
+  if (rows < 0 || cols < 1) return fail(GC_ERR_SHAPE, "rows must be >= 0 and cols >= 1");
+  if (rows > (1LL << 40)) return fail(GC_ERR_SHAPE, "rows too large");
+  if (cols > GC_MAX_COLS) return fail(GC_ERR_UNSUPPORTED, "cols=%d exceeds %d", cols, GC_MAX_COLS);
+  if (!(p >= 0.0 && p < 1.0)) return fail(GC_ERR_ARG, "p=%g outside [0, 1)", p);
+  if (row0 < 0 || row0 > (1LL << 40)) return fail(GC_ERR_ARG, "row0 outside [0, 2^40]");
+  return GC_OK;
+}
+// A matrix of `rows` rows, ld elements apart (NULL when it is optional: not there).
+static int check_rows(const char* name, const void* p, int64_t ld, int64_t rows, int64_t cols, int elt,
+                      bool need) {
+  if (!p) return need ? fail(GC_ERR_ARG, "%s must be non-NULL", name) : GC_OK;
+  if (reinterpret_cast<uintptr_t>(p) % elt != 0) return fail(GC_ERR_ARG, "%s is misaligned", name);
+  if (rows > 1 && (ld < cols || ld > (1LL << 40)))
+    return fail(GC_ERR_SHAPE, "%s: row stride %lld, %lld columns", name, (long long)ld, (long long)cols);
+  return GC_OK;
+}
+
+int gc_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype, int64_t rows,
+               int cols, double p, uint64_t seed, uint64_t offset, int64_t row0, void* out, int64_t ldo,
+               void* stream) {
+  NvtxRange nvtx_("gc_dropout");
+  int rc = check_rowwise(dtype, rows, cols, p, row0);
+  if (rc) return rc;
+  if (rows == 0) return GC_OK;
+  const int e = dtype == GC_BF16 ? 2 : 4;
+  if ((rc = check_rows("x", x, ldx, rows, cols, e, true)) ||
+      (rc = check_rows("residual", residual, ldr, rows, cols, e, false)) ||
+      (rc = check_rows("out", out, ldo, rows, cols, e, true)))
+    return rc;
+  return launch_dropout(x, ldx, residual, ldr, dtype, rows, cols, DropArgs{p, seed, offset, row0}, out,
+                        ldo, as_stream(stream));
+}
+
+int gc_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype, int64_t rows,
+                  int cols, const float* gamma, const float* beta, float eps, double p, uint64_t seed,
+                  uint64_t offset, int64_t row0, void* y, int64_t ldy, void* h, int64_t ldh, float* mean,
+                  float* rstd, void* stream) {
+  NvtxRange nvtx_("gc_layer_norm");
+  int rc = check_rowwise(dtype, rows, cols, p, row0);
+  if (rc) return rc;
+  if (!(eps >= 0.f)) return fail(GC_ERR_ARG, "eps=%g must be >= 0", (double)eps);
+  if (rows == 0) return GC_OK;
+  const int e = dtype == GC_BF16 ? 2 : 4;
+  if ((rc = check_rows("x", x, ldx, rows, cols, e, true)) ||
+      (rc = check_rows("residual", residual, ldr, rows, cols, e, false)) ||
+      (rc = check_rows("y", y, ldy, rows, cols, e, true)) ||
+      (rc = check_rows("h", h, ldh, rows, cols, e, false)))
+    return rc;
+  const NormIO io{x, residual, gamma, beta, y, h, mean, rstd, ldx, ldr, ldy, ldh};
+  return launch_norm(io, dtype, rows, cols, eps, DropArgs{p, seed, offset, row0}, as_stream(stream));
+}
+
+size_t gc_layer_norm_backward_workspace(int N, int n_c, int cols) {
+  if (N < 1 || n_c < 1 || cols < 1 || cols > GC_MAX_COLS) return 0;
+  return kHeaderBytes + norm_grad_ws_bytes(N, n_c, cols);
+}
+
+int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const float* mean,
+                           const float* rstd, const float* gamma, const void* dh, int64_t lddh, int dtype,
+                           int N, int n_c, int cols, double p, uint64_t seed, uint64_t offset,
+                           int64_t row0, void* dx, int64_t lddx, void* dresidual, int64_t lddr, float* G,
+                           int64_t ldg, void* ws, size_t ws_bytes, void* stream) {
+  NvtxRange nvtx_("gc_layer_norm_backward");
+  if (N < 1 || n_c < 1) return fail(GC_ERR_SHAPE, "N, n_c must be >= 1");
+  if ((long long)N * n_c > (1LL << 31) - 1) return fail(GC_ERR_UNSUPPORTED, "N*n_c too large");
+  const int64_t rows = (int64_t)N * n_c;
+  int rc = check_rowwise(dtype, rows, cols, p, row0);
+  if (rc) return rc;
+  if (!mean || !rstd) return fail(GC_ERR_ARG, "mean and rstd must be non-NULL");
+  if (!dx && !dresidual && !G) return fail(GC_ERR_ARG, "one of dx, dresidual and G must be non-NULL");
+  const int e = dtype == GC_BF16 ? 2 : 4;
+  if ((rc = check_rows("dy", dy, lddy, rows, cols, e, true)) ||
+      (rc = check_rows("h", h, ldh, rows, cols, e, true)) ||
+      (rc = check_rows("dh", dh, lddh, rows, cols, e, false)) ||
+      (rc = check_rows("dx", dx, lddx, rows, cols, e, false)) ||
+      (rc = check_rows("dresidual", dresidual, lddr, rows, cols, e, false)) ||
+      (rc = check_rows("G", G, ldg, N, 2LL * cols, 4, false)))
+    return rc;
+  if ((rc = check_ws(ws, ws_bytes, gc_layer_norm_backward_workspace(N, n_c, cols)))) return rc;
+  Carve c(ws);
+  const NormGradIO io{dy, h, dh, mean, rstd, gamma, dx, dresidual, G, lddy, ldh, lddh, lddx, lddr, ldg};
+  return launch_norm_grad(io, dtype, N, n_c, cols, DropArgs{p, seed, offset, row0}, c,
+                          as_stream(stream));
+}
+
 // ---------------------------------------------------------------- Algorithm 1
 size_t gc_coeff_workspace(int N, int m, int delta, int ell, int npat) {
   if (check_dims(N, m, delta, ell, npat)) return 0;

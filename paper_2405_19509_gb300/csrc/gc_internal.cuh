@@ -159,6 +159,34 @@ int launch_live_step(const double* E, const double* R, int ell, const int32_t* o
                      int delta, const int32_t* psi, const float* G, int d, float lr, int64_t Ntil,
                      float* w, float* T, float* ghat, cudaStream_t s);
 
+// ---- row-wise operators (k_dropout.cu, k_norm.cu) --------------------------
+struct DropArgs {
+  double p;  // 0: nothing is dropped
+  uint64_t seed, offset;
+  int64_t row0;
+};
+int launch_dropout(const void* x, int64_t ldx, const void* res, int64_t ldr, int dtype, int64_t rows,
+                   int cols, const DropArgs& d, void* out, int64_t ldo, cudaStream_t s);
+struct NormIO {
+  const void *x, *res;
+  const float *gamma, *beta;
+  void *y, *h;
+  float *mean, *rstd;
+  int64_t ldx, ldr, ldy, ldh;
+};
+int launch_norm(const NormIO& io, int dtype, int64_t rows, int cols, float eps, const DropArgs& d,
+                cudaStream_t s);
+struct NormGradIO {
+  const void *dy, *h, *dh;
+  const float *mean, *rstd, *gamma;
+  void *dx, *dres;
+  float* G;
+  int64_t lddy, ldh, lddh, lddx, lddr, ldg;
+};
+size_t norm_grad_ws_bytes(int N, int n_c, int cols);
+int launch_norm_grad(const NormGradIO& io, int dtype, int N, int n_c, int cols, const DropArgs& d,
+                     Carve& ws, cudaStream_t s);
+
 // ---- batched decode in residual form (k_decode_resid.cu) -----------------
 // Per pattern the ordered list of decode blocks that differ from I_ell (chunk
 // index and D = Pi - I).
