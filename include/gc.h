@@ -102,6 +102,7 @@ int gc_set_wait_limit(int64_t cycles);
                                   it waits only when it has patterns to
                                   compute, see gc_set_decode_policy) */
 #define GC_STALL_BATCHED 4     /* the batched chunk-gradient GEMMs (first one) */
+#define GC_STALL_XENT 16       /* softmax cross entropy (its first pass)      */
 int gc_inject_stall(int kernels);
 
 /* Path of the batched decode (gc_decode_batch, gc_decode_apply,
@@ -309,6 +310,36 @@ int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t 
                            int N, int n_c, int cols, double p, uint64_t seed, uint64_t offset,
                            int64_t row0, void* dx, int64_t lddx, void* dresidual, int64_t lddr, float* G,
                            int64_t ldg, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- softmax cross entropy over a vocabulary, gradients per chunk ------------
+ * The output layer of a language model, multinomial logistic regression over V classes.  With
+ * z = X W^T, for every point t = 0 .. N n_c - 1
+ *   lse[t]      = log sum_v exp z[t][v]
+ *   row_loss[t] = lse[t] - z[t][y[t]]          (-log of the probability of y[t])
+ *   loss        = (1 / (N n_c)) sum_t row_loss[t]
+ * and, un-normalised as in gc_chunk_grads, with P[t][v] = exp(z[t][v] - lse[t]) - (v = y[t]),
+ *   dX[t]       = sum_v P[t][v] W[v]
+ *   G[i][v]     = sum_{t in chunk i} P[t][v] X[t]        (chunk i: points [i n_c, (i + 1) n_c)).
+ * A point whose label is negative (padding) has row_loss 0 and enters no gradient, whatever its row
+ * of X holds; its lse is that of a row of zeros.  A label >= V is treated so too, and raises GC_ERR_DATA
+ * in the status header.  Neither z nor P is kept: both are formed for a piece of the vocabulary at a
+ * time (a piece of P is at most about 2^26 values), the products on the tensor cores with fp32 sums.
+ * bf16 operands are used as they are, fp32 ones as bf16 hi + lo (2^-17); P enters G as hi + lo, and
+ * a bf16 dX in bf16.
+ *   X    N n_c rows of C values of x_dtype, ldx elements apart.    W   V rows, ldw apart, w_dtype.
+ *   y    N n_c labels, int64 (y64 != 0) or int32.
+ *   loss one device double; row_loss, lse  N n_c fp32;  dX  N n_c rows of x_dtype, lddx apart;
+ *   G    N rows of V * C fp32, ldg apart (a slice of the chunk gradients of a model): each nullable,
+ *        not all of them.  dX must not overlap X.  Any alignment; the sums have a fixed order.
+ *   Limits: C <= 2^20, V <= 2^28, N n_c < 2^31, and at most 2^29 tiles of 256 x 256.
+ * Workspace: gc_softmax_xent_workspace bytes.  w_16: whether W and its rows lie on 16-byte boundaries
+ * (bf16 rows that do are read in place; others are copied); want: 1 with dX, 2 with G, added up.
+ */
+size_t gc_softmax_xent_workspace(int N, int n_c, int C, int V, int x_dtype, int w_dtype, int w_16, int want);
+int gc_softmax_xent(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ldw, int w_dtype,
+                    const void* y, int y64, int N, int n_c, int C, int V, double* loss, float* row_loss,
+                    float* lse, void* dX, int64_t lddx, float* G, int64_t ldg, void* ws, size_t ws_bytes,
+                    void* stream);
 
 /* ---- Algorithm 1, Find-Encoding-Coeff, batched over patterns ----------
  * R      ell x m float64, the PS's Gaussian matrix (Sec. II).

@@ -85,6 +85,9 @@ _sig("gc_layer_norm", _i, _p, _i64, _p, _i64, _i, _i64, _i, _p, _p, _f, _d, _u64
 _sig("gc_layer_norm_backward_workspace", _sz, _i, _i, _i)
 _sig("gc_layer_norm_backward", _i, _p, _i64, _p, _i64, _p, _p, _p, _p, _i64, _i, _i, _i, _i, _d, _u64,
      _u64, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _sz, _p)
+_sig("gc_softmax_xent_workspace", _sz, _i, _i, _i, _i, _i, _i, _i, _i)
+_sig("gc_softmax_xent", _i, _p, _i64, _i, _p, _i64, _i, _p, _i, _i, _i, _i, _i, _p, _p, _p, _p, _i64, _p,
+     _i64, _p, _sz, _p)
 
 
 class GCError(RuntimeError):
@@ -382,6 +385,45 @@ def gc_layer_norm_backward(dy, h, mean, rstd, gamma, N: int, n_c: int, dh=None, 
     return {"dx": dx, "dresidual": dresidual, "G": G}
 
 
+# ---------------------------------------------------------------- softmax cross entropy
+def gc_softmax_xent(X, W, y, N: int, n_c: int, loss=True, row_loss=True, lse=True, dX=True, G=True,
+                    ws: Workspace | None = None):
+    """Softmax cross entropy of the rows X W^T (X N n_c x C, W V x C, float32 or bfloat16 each) at the
+    labels y (int64 or int32; negative: none), with its gradient, neither logits nor probabilities
+    kept.  Returns dict with loss (1 float64, the mean over all points), row_loss, lse (float32), dX
+    (X's type) and G (N x V C float32: per chunk the gradient of W, un-normalised); booleans ask for
+    an output, tensors are written into (G may be a column slice of a larger matrix)."""
+    xt, wt = _elt(X, "X"), _elt(W, "W")
+    T, C = X.shape
+    V = W.shape[0]
+    if T != N * n_c:
+        raise ValueError("X must have N * n_c rows")
+    if y.dtype is not torch.int64 and y.dtype is not torch.int32:
+        raise TypeError("y must be int64 or int32")
+    dev = X.device
+
+    def out(t, shape, dtype):
+        if isinstance(t, torch.Tensor):
+            return t
+        return torch.empty(shape, dtype=dtype, device=dev) if t else None
+    loss, row_loss = out(loss, (1,), torch.float64), out(row_loss, (T,), torch.float32)
+    lse = out(lse, (T,), torch.float32)
+    dX, G = out(dX, X.shape, X.dtype), out(G, (N, V * C), torch.float32)
+    xp, ldx = _rows(X, X.dtype, "X", X.shape)
+    wp_, ldw = _rows(W, W.dtype, "W", (V, C))
+    dp, lddx = _rows(dX, X.dtype, "dX", X.shape)
+    gp, ldg = _rows(G, torch.float32, "G", (N, V * C))
+    e = W.element_size()
+    w_16 = int(wp_ % 16 == 0 and (ldw * e % 16 == 0 or V == 1))
+    ws, (wp, wn) = _ws(ws, _bytes("gc_softmax_xent_workspace", N, n_c, C, V, xt, wt, w_16,
+                                 (dX is not None) + 2 * (G is not None)), dev)
+    _check(lib.gc_softmax_xent(
+        xp, ldx, xt, wp_, ldw, wt, _dev(y, y.dtype, "y", (T,)), int(y.dtype is torch.int64), N, n_c, C, V,
+        _dev(loss, torch.float64, "loss"), _dev(row_loss, torch.float32, "row_loss", (T,)),
+        _dev(lse, torch.float32, "lse", (T,)), dp, lddx, gp, ldg, wp, wn, _stream()))
+    return {"loss": loss, "row_loss": row_loss, "lse": lse, "dX": dX, "G": G}
+
+
 # ---------------------------------------------------------------- Algorithm 1
 def gc_coeff_workspace(N, m, delta, ell, npat):
     return lib.gc_coeff_workspace(N, m, delta, ell, npat)
@@ -584,6 +626,7 @@ def gc_set_wait_limit(cycles: int) -> None:
 GC_STALL_CHUNK_GRADS = 1
 GC_STALL_COMBINE = 2
 GC_STALL_BATCHED = 4
+GC_STALL_XENT = 16
 
 
 def gc_inject_stall(kernels: int) -> None:

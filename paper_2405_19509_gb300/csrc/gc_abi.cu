@@ -114,7 +114,7 @@ int gc_version(void) { return 200; }
 uint64_t gc_kernel_launches(void) { return g_launches.load(); }
 
 int gc_inject_stall(int kernels) {
-  if (kernels & ~(GC_STALL_CHUNK_GRADS | GC_STALL_COMBINE | GC_STALL_BATCHED))
+  if (kernels & ~(GC_STALL_CHUNK_GRADS | GC_STALL_COMBINE | GC_STALL_BATCHED | GC_STALL_XENT))
     return fail(GC_ERR_ARG, "kernels=0x%x has unknown bits", kernels);
   g_stall.store(kernels);
   return GC_OK;
@@ -203,10 +203,11 @@ int gc_status(void* ws, void* stream) {
   GC_CUDA(cudaMemset(ws, 0, sizeof(h)));
   if (h.status & ST_TIMEOUT)
     return fail(GC_ERR_TIMEOUT, "a bounded device wait expired (status 0x%x)", h.status);
-  if (h.status & (ST_BAD_PSI | ST_SINGULAR | ST_BAD_ORDER)) {
-    return fail(GC_ERR_DATA, "device reported:%s%s%s", (h.status & ST_BAD_PSI) ? " psi outside [0, delta];" : "",
+  if (h.status & (ST_BAD_PSI | ST_SINGULAR | ST_BAD_ORDER | ST_BAD_LABEL)) {
+    return fail(GC_ERR_DATA, "device reported:%s%s%s%s", (h.status & ST_BAD_PSI) ? " psi outside [0, delta];" : "",
                 (h.status & ST_SINGULAR) ? " rank-deficient least-squares system;" : "",
-                (h.status & ST_BAD_ORDER) ? " invalid order entry or too many copies of a chunk;" : "");
+                (h.status & ST_BAD_ORDER) ? " invalid order entry or too many copies of a chunk;" : "",
+                (h.status & ST_BAD_LABEL) ? " a label past the vocabulary;" : "");
   }
   return GC_OK;
 }
@@ -367,6 +368,54 @@ int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t 
   const NormGradIO io{dy, h, dh, mean, rstd, gamma, dx, dresidual, G, lddy, ldh, lddh, lddx, lddr, ldg};
   return launch_norm_grad(io, dtype, N, n_c, cols, DropArgs{p, seed, offset, row0}, c,
                           as_stream(stream));
+}
+
+// ---------------------------------------------------------------- softmax cross entropy
+static int check_xent(const XentShape& s) {
+  if (s.x_dtype != GC_F32 && s.x_dtype != GC_BF16) return fail(GC_ERR_ARG, "x_dtype=%d", s.x_dtype);
+  if (s.w_dtype != GC_F32 && s.w_dtype != GC_BF16) return fail(GC_ERR_ARG, "w_dtype=%d", s.w_dtype);
+  if (s.N < 1 || s.n_c < 1 || s.C < 1 || s.V < 1) return fail(GC_ERR_SHAPE, "N, n_c, C, V must be >= 1");
+  if ((long long)s.N * s.n_c > (1LL << 31) - 1) return fail(GC_ERR_UNSUPPORTED, "N*n_c too large");
+  if (s.C > (1 << 20)) return fail(GC_ERR_UNSUPPORTED, "C=%d exceeds %d", s.C, 1 << 20);
+  if (s.V > (1 << 28)) return fail(GC_ERR_UNSUPPORTED, "V=%d exceeds %d", s.V, 1 << 28);
+  // tiles of 256 x 256 are counted in 32 bits
+  const long long mt = ((long long)s.N * s.n_c + 255) / 256, nt = (s.V + 255) / 256, ct = (s.C + 255) / 256;
+  if (mt * nt > (1 << 30) || mt * ct > (1 << 29) || (long long)s.N * nt > (1 << 30) ||
+      (long long)s.N * nt * ct > (1 << 29))
+    return fail(GC_ERR_UNSUPPORTED, "too many tiles: N*n_c=%lld, V=%d, C=%d", (long long)s.N * s.n_c, s.V, s.C);
+  return GC_OK;
+}
+
+size_t gc_softmax_xent_workspace(int N, int n_c, int C, int V, int x_dtype, int w_dtype, int w_16, int want) {
+  const XentShape s{N, n_c, C, V, x_dtype, w_dtype, w_16, want};
+  return check_xent(s) ? 0 : xent_ws_bytes(s);
+}
+
+int gc_softmax_xent(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ldw, int w_dtype,
+                    const void* y, int y64, int N, int n_c, int C, int V, double* loss, float* row_loss,
+                    float* lse, void* dX, int64_t lddx, float* G, int64_t ldg, void* ws, size_t ws_bytes,
+                    void* stream) {
+  NvtxRange nvtx_("gc_softmax_xent");
+  XentShape s{N, n_c, C, V, x_dtype, w_dtype, 0, (dX ? XENT_DX : 0) | (G ? XENT_G : 0)};
+  int rc = check_xent(s);
+  if (rc) return rc;
+  if (!loss && !row_loss && !lse && !s.want) return fail(GC_ERR_ARG, "no output: all of them are NULL");
+  const int64_t T = (int64_t)N * n_c;
+  const int xe = x_dtype == GC_BF16 ? 2 : 4, we = w_dtype == GC_BF16 ? 2 : 4;
+  if ((rc = check_rows("X", X, ldx, T, C, xe, true)) || (rc = check_rows("W", W, ldw, V, C, we, true)) ||
+      (rc = check_rows("y", y, 1, T, 1, y64 ? 8 : 4, true)) ||
+      (rc = check_rows("dX", dX, lddx, T, C, xe, false)) ||
+      (rc = check_rows("G", G, ldg, N, (int64_t)V * C, 4, false)))
+    return rc;
+  // one row needs no stride, but the layout rules below read it
+  if (V == 1) ldw = (C + 7) / 8 * 8;
+  if (T == 1) ldx = lddx = (C + 7) / 8 * 8;
+  if (N == 1) ldg = ((int64_t)V * C + 3) / 4 * 4;
+  s.w_16 = reinterpret_cast<uintptr_t>(W) % 16 == 0 && ldw * we % 16 == 0;
+  if ((rc = check_ws(ws, ws_bytes, xent_ws_bytes(s)))) return rc;
+  Carve c(ws);
+  const XentIO io{X, W, y, y64, loss, row_loss, lse, dX, G, ldx, ldw, lddx, ldg};
+  return launch_xent(s, io, c, status_of(ws), as_stream(stream));
 }
 
 // ---------------------------------------------------------------- Algorithm 1

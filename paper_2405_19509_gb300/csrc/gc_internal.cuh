@@ -17,6 +17,7 @@ enum : uint32_t {
   ST_SINGULAR = 2u,    // a least-squares system was numerically rank deficient
   ST_TIMEOUT = 4u,     // a bounded mbarrier wait expired
   ST_BAD_ORDER = 8u,   // order entry outside [-1, N) or a chunk with > GC_MAX_REPL copies
+  ST_BAD_LABEL = 16u,  // a label past the vocabulary
 };
 constexpr size_t kHeaderBytes = 256;
 
@@ -186,6 +187,25 @@ struct NormGradIO {
 size_t norm_grad_ws_bytes(int N, int n_c, int cols);
 int launch_norm_grad(const NormGradIO& io, int dtype, int N, int n_c, int cols, const DropArgs& d,
                      Carve& ws, cudaStream_t s);
+
+// ---- softmax cross entropy over a vocabulary (k_xent.cu) -------------------
+enum { XENT_DX = 1, XENT_G = 2 };
+struct XentShape {
+  int N, n_c, C, V, x_dtype, w_dtype;
+  int w_16;  // rows of W on 16-byte boundaries
+  int want;  // XENT_DX | XENT_G
+};
+struct XentIO {
+  const void *X, *W, *y;
+  int y64;
+  double* loss;
+  float *row_loss, *lse;
+  void* dX;
+  float* G;
+  int64_t ldx, ldw, lddx, ldg;
+};
+size_t xent_ws_bytes(const XentShape& s);
+int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* status, cudaStream_t st);
 
 // ---- batched decode in residual form (k_decode_resid.cu) -----------------
 // Per pattern the ordered list of decode blocks that differ from I_ell (chunk

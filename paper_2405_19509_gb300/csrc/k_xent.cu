@@ -1,0 +1,731 @@
+// Softmax cross entropy over a large vocabulary, in pieces of it, with its gradient per chunk:
+//   z = X W^T,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_{t, y_t}
+//   P = exp(z - lse) - onehot(y)  (rows without a label: 0),  dX = P W,  G_i = P_i^T X_i
+// for T = N n_c rows of C values and V rows of W.  Neither z nor P exists as a whole:
+//   k_xent<STAT>   z tile by tile in tensor memory; per row and 128 columns the largest and the sum of
+//                  the exponentials about it go to scratch; k_xent_lse joins them
+//   k_xent<PROB>   z again for one piece of the vocabulary, written as P's bf16 parts
+//   k_xent<GRAD>   dX += P W and G_i = P_i^T X_i of that piece, in one launch
+//
+// Bound: the tensor pipe.  Per row, column and value of C: one product for lse, one for P, one for
+// dX, and two for G, whose 32-bit result wants P to 2^-17, as bf16 hi + lo; dX is stored in bf16, so
+// its operands enter in bf16 (2^-9 each, as its own rounding).  fp32 X and W enter as hi + lo too
+// (X_hi W_hi + X_hi W_lo + X_lo W_hi; the dropped term is 2^-18).  All sums are fp32 in tensor memory.
+// z is not kept: T V values of it are gigabytes, while a piece of P is kPieceElems values.
+//
+// One persistent kernel shape: a pair of CTAs (cta_group::2) per 256 x 256 tile, each CTA loading
+// 128 rows of A and of B for a 64-wide K block (warp 0, TMA), the leader's warp 1 issuing the MMAs,
+// eight warps per CTA draining one of two accumulators while the other is filled.  Operands that
+// lie with K outermost (W in dX, P and X in G) are read MN-major: boxes of 64 columns x 64 K rows.
+// Rows past a chunk's end, columns past V and past C are zero-filled by TMA.  A row without a label
+// enters X's copy as zeros, whatever it holds.  Every wait is bounded (GC_ERR_TIMEOUT).
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+
+#include "rowwise.cuh"
+#include "tc_pair.cuh"
+
+namespace gc {
+namespace {
+
+using namespace tcp;
+
+constexpr int TILE = 256, HALF = 128, BK = 64;
+constexpr int OP_BYTES = HALF * BK * 2;  // a CTA's 128 x 64 share of an operand tile
+constexpr int kMaxStages = 6;
+constexpr int kRing = kMaxStages * 2 * OP_BYTES;  // 192 KB
+constexpr int kEpi = 8;
+constexpr int kThreadsX = 64 + 32 * kEpi;
+constexpr size_t kSmemX = kRing + 1024 + 256;
+constexpr long long kSpinX = 1LL << 32;
+constexpr long long kPieceElems = 1LL << 26;  // of P: 256 MB as two bf16 parts
+constexpr float kLog2e = 1.4426950408889634f;
+
+enum { STAT = 0, PROB = 1, GRAD = 2 };
+
+struct XentParams {
+  long long T;
+  int C, V, N, n_c;
+  int nx, nw;          // bf16 parts of X and of W
+  int v0, w;           // PROB, GRAD: the piece is columns [v0, v0 + w)
+  int np, np_dx;       // parts of P: kept, and that enter dX
+  int mt, nt, group;   // tiles of T and of the columns; row tiles that share a sweep of the columns
+  int pairs;
+  // GRAD: dX tiles, round robin; then G's, `extra` each for the pairs past the first `r`, which
+  // have one dX tile less, and the rest round robin
+  int ndx, ct, vt, ndw, r, extra;
+  int stage_ops, stages;
+  int first_piece, last_piece;
+  const int* lab;      // T labels, -1: none
+  const float* lse;
+  float* target;       // STAT: z at the label
+  float2* part;        // STAT: [T][2 nt]
+  __nv_bfloat16* P;    // [np][T][Pp]
+  int Pp;
+  float* acc;          // fp32 dX of the pieces so far
+  long long ld_acc;
+  void* dX;
+  long long ld_dx;
+  int dx_bf16;
+  float* G;
+  long long ldg;
+  long long spin_limit;
+  int stall;
+  uint32_t* status;
+};
+
+struct TileAt {
+  int kind;            // 0: z, 1: dX, 2: G
+  int m0, n0, chunk;
+  int nkb, na, nb;
+};
+
+template <int MODE>
+__device__ __forceinline__ int tiles_of(const XentParams& p, int pair) {
+  if (MODE != GRAD) return (int)(((long long)p.mt * p.nt - pair + p.pairs - 1) / p.pairs);
+  const int nb = p.pairs - p.r;
+  const int ndx = (p.ndx - pair + p.pairs - 1) / p.pairs;
+  const int rest = p.ndw - p.extra * nb;
+  return ndx + (pair >= p.r ? p.extra : 0) + (rest - pair + p.pairs - 1) / p.pairs;
+}
+
+// The k-th tile of a pair.
+template <int MODE>
+__device__ __forceinline__ TileAt tile_at(const XentParams& p, int pair, int k) {
+  TileAt t;
+  if (MODE != GRAD) {
+    const int i = pair + k * p.pairs;
+    const int per = p.group * p.nt, g = i / per, rem = i - g * per;
+    const int gm = min(p.group, p.mt - g * p.group);
+    const int n = rem / gm;
+    t.kind = 0;
+    t.m0 = (g * p.group + rem - n * gm) * TILE;
+    t.n0 = n * TILE;
+    t.chunk = 0;
+    t.nkb = (p.C + BK - 1) / BK;
+    t.na = p.nx;
+    t.nb = p.nw;
+    return t;
+  }
+  const int ndx = (p.ndx - pair + p.pairs - 1) / p.pairs;
+  if (k < ndx) {
+    const int i = pair + k * p.pairs;
+    t.kind = 1;
+    t.m0 = i / p.ct * TILE;
+    t.n0 = i % p.ct * TILE;
+    t.chunk = 0;
+    t.nkb = (p.w + BK - 1) / BK;
+    t.na = p.np_dx;
+    t.nb = p.np_dx == 1 ? 1 : p.nw;
+    return t;
+  }
+  k -= ndx;
+  const int nb = p.pairs - p.r, mine = pair >= p.r ? p.extra : 0;
+  const int i = k < mine ? k * nb + pair - p.r : p.extra * nb + (k - mine) * p.pairs + pair;
+  const int per = p.vt * p.ct, c = i / per, rem = i - c * per;
+  t.kind = 2;
+  t.chunk = c;
+  t.m0 = rem / p.ct * TILE;
+  t.n0 = rem % p.ct * TILE;
+  t.nkb = (p.n_c + BK - 1) / BK;
+  t.na = p.np;
+  t.nb = p.nx;
+  return t;
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// 32 consecutive fp32 values of a row of an output; n: how many of them exist.
+template <typename T>
+__device__ __forceinline__ void store_row(T* dst, const float (&v)[32], int n, bool vec) {
+  if (n >= 32 && vec) {
+    if (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 32; j += 4)
+        *reinterpret_cast<float4*>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; j += 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const __nv_bfloat162 t = __floats2bfloat162_rn(v[j + 2 * e], v[j + 2 * e + 1]);
+          w[e] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+        *reinterpret_cast<uint4*>(dst + j) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (j < n) dst[j] = rowwise::from_f<T>(v[j]);
+}
+
+template <int MODE>
+__device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, uint32_t taddr, long long row_in,
+                                         int half) {
+  if (MODE == STAT) {
+    const bool rv = row_in < p.T;
+    const int lab = rv ? __ldg(p.lab + row_in) : -1;
+    float m = -INFINITY, s = 0.f;
+    for (int c = 0; c < HALF / 32; ++c) {
+      float v[32];
+      __syncwarp();
+      tmem_ld32(taddr + (uint32_t)(c * 32), v);
+      const int col = t.n0 + half * HALF + c * 32;
+      const int n = p.V - col;
+      if (n < 32) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j >= n) v[j] = -INFINITY;
+      }
+      if (lab >= col && lab < col + 32) {
+        float z = 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j == lab - col) z = v[j];
+        p.target[row_in] = z;
+      }
+      float top = m;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) top = fmaxf(top, v[j]);
+      const float ref = top == -INFINITY ? 0.f : top * kLog2e;
+      s *= ex2(fmaf(m, kLog2e, -ref));
+#pragma unroll
+      for (int j = 0; j < 32; ++j) s += ex2(fmaf(v[j], kLog2e, -ref));
+      m = top;
+    }
+    if (rv) p.part[row_in * 2 * p.nt + t.n0 / HALF + half] = make_float2(m, s);
+  } else if (MODE == PROB) {
+    const bool rv = row_in < p.T;
+    const int lab = rv ? __ldg(p.lab + row_in) : -1;
+    const float l2 = rv ? __ldg(p.lse + row_in) * kLog2e : 0.f;
+    __nv_bfloat16* out = p.P + (size_t)(rv ? row_in : 0) * p.Pp + t.n0 + half * HALF;
+    const size_t plane = (size_t)p.T * p.Pp;
+    for (int c = 0; c < HALF / 32; ++c) {
+      float v[32];
+      __syncwarp();
+      tmem_ld32(taddr + (uint32_t)(c * 32), v);
+      const int at = lab - (p.v0 + t.n0 + half * HALF + c * 32);  // the label's place here
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = lab >= 0 ? ex2(fmaf(v[j], kLog2e, -l2)) : 0.f;
+      if (at >= 0 && at < 32) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j == at) v[j] -= 1.f;
+      }
+      if (rv) {
+        store_row(out + c * 32, v, 32, true);
+        if (p.np == 2) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+          store_row(out + plane + c * 32, v, 32, true);
+        }
+      }
+    }
+  } else if (t.kind == 1) {
+    const bool rv = row_in < p.T;
+    for (int c = 0; c < HALF / 32; ++c) {
+      float v[32];
+      __syncwarp();
+      tmem_ld32(taddr + (uint32_t)(c * 32), v);
+      const int col = t.n0 + half * HALF + c * 32, n = p.C - col;
+      if (!rv || n <= 0) continue;
+      float* a = p.acc + row_in * p.ld_acc + col;
+      if (!p.first_piece) {
+        const bool vec = p.ld_acc % 4 == 0 && reinterpret_cast<uintptr_t>(p.acc) % 16 == 0;
+        if (vec && n >= 32) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) {
+            const float4 q = *reinterpret_cast<const float4*>(a + j);
+            v[j] += q.x;
+            v[j + 1] += q.y;
+            v[j + 2] += q.z;
+            v[j + 3] += q.w;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (j < n) v[j] += a[j];
+        }
+      }
+      if (p.last_piece && p.dx_bf16) {
+        __nv_bfloat16* o = (__nv_bfloat16*)p.dX + row_in * p.ld_dx + col;
+        store_row(o, v, n, p.ld_dx % 8 == 0 && reinterpret_cast<uintptr_t>(p.dX) % 16 == 0);
+      } else {
+        store_row(a, v, n, p.ld_acc % 4 == 0 && reinterpret_cast<uintptr_t>(p.acc) % 16 == 0);
+      }
+    }
+  } else {
+    const int lv = (int)row_in;  // row of the piece
+    const bool rv = lv < p.w;
+    float* g = p.G + t.chunk * p.ldg + (long long)(p.v0 + (rv ? lv : 0)) * p.C;
+    const bool vec = p.C % 4 == 0 && p.ldg % 4 == 0 && reinterpret_cast<uintptr_t>(p.G) % 16 == 0;
+    for (int c = 0; c < HALF / 32; ++c) {
+      float v[32];
+      __syncwarp();
+      tmem_ld32(taddr + (uint32_t)(c * 32), v);
+      const int col = t.n0 + half * HALF + c * 32, n = p.C - col;
+      if (rv && n > 0) store_row(g + col, v, n, vec);
+    }
+  }
+}
+
+// Tensor maps: mA, mB of the first product (z: X and W rows; GRAD: P rows and W columns for dX), mP4
+// and mX4 (GRAD: P and X of a chunk, columns x points).
+template <int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsX, 1)
+    k_xent(const __grid_constant__ CUtensorMap mA, const __grid_constant__ CUtensorMap mB,
+           const __grid_constant__ CUtensorMap mP4, const __grid_constant__ CUtensorMap mX4, XentParams p) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kRing);  // the leader's: both CTAs' loads landed
+  uint64_t* empty = full + kMaxStages;                         // each CTA's: the MMAs on the stage are done
+  uint64_t* tfull = empty + kMaxStages;                        // [2] each CTA's: accumulator filled
+  uint64_t* tempty = tfull + 2;                                // [2] the leader's: drained by both CTAs
+  uint64_t* done = tempty + 2;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cta_rank(), pair = blockIdx.x >> 1;
+  const int S = p.stages, stage_bytes = p.stage_ops * OP_BYTES;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(&tfull[a], 1);
+      mbar_init(&tempty[a], 2 * kEpi);
+    }
+    mbar_init(done, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(tmem_holder, 512);
+  fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  fence_after();
+  const uint32_t tmem_base = *tmem_holder;
+  const int ntiles = tiles_of<MODE>(p, pair);
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = !p.stall;
+      for (int k = 0; k < ntiles && ok; ++k) {
+        const TileAt t = tile_at<MODE>(p, pair, k);
+        const int ma = t.m0 + rank * HALF, nb = t.n0 + rank * HALF;
+        const uint32_t bytes = (uint32_t)(t.na + t.nb) * OP_BYTES;
+        for (int kb = 0; kb < t.nkb; ++kb, ++it) {
+          const int s = it % S;
+          if (!mbar_wait(&empty[s], ((it / S) & 1) ^ 1, abort_flag, p.status, p.spin_limit)) {
+            ok = false;
+            break;
+          }
+          if (rank == 0) mbar_expect_tx(&full[s], 2 * bytes);
+          const uint32_t bar = at_leader(&full[s]);
+          uint8_t* st = smem + (size_t)s * stage_bytes;
+          if (t.kind < 2) {
+            for (int i = 0; i < t.na; ++i, st += OP_BYTES) load_3d(st, &mA, kb * BK, ma, i, bar);
+            for (int i = 0; i < t.nb; ++i, st += OP_BYTES) {
+              if (t.kind == 0) {
+                load_3d(st, &mB, kb * BK, p.v0 + nb, i, bar);
+              } else {
+                load_3d(st, &mB, nb, p.v0 + kb * BK, i, bar);
+                load_3d(st + OP_BYTES / 2, &mB, nb + 64, p.v0 + kb * BK, i, bar);
+              }
+            }
+          } else {
+            for (int i = 0; i < t.na; ++i, st += OP_BYTES) {
+              load_4d(st, &mP4, ma, kb * BK, t.chunk, i, bar);
+              load_4d(st + OP_BYTES / 2, &mP4, ma + 64, kb * BK, t.chunk, i, bar);
+            }
+            for (int i = 0; i < t.nb; ++i, st += OP_BYTES) {
+              load_4d(st, &mX4, nb, kb * BK, t.chunk, i, bar);
+              load_4d(st + OP_BYTES / 2, &mX4, nb + 64, kb * BK, t.chunk, i, bar);
+            }
+          }
+        }
+      }
+      // drain: a stage whose MMAs are done has landed in both CTAs.  After an abort nothing arrives any
+      // more; the copies in flight land within the one limit.
+      for (uint32_t k = it > (uint32_t)S ? it - S : 0; k < it; ++k) {
+        volatile int no_abort = 0;
+        if (!mbar_wait(&empty[k % S], (k / S) & 1, &no_abort, p.status, 1LL << 28)) break;
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (int k = 0; k < ntiles && ok; ++k) {
+        const TileAt t = tile_at<MODE>(p, pair, k);
+        const int ab = k & 1;
+        if (!mbar_wait(&tempty[ab], ((k >> 1) & 1) ^ 1, abort_flag, p.status, p.spin_limit)) break;
+        fence_after();
+        const uint32_t d = tmem_base + (uint32_t)(ab * TILE);
+        const bool a_mn = t.kind == 2, b_mn = t.kind >= 1;
+        const uint32_t idesc = idesc_256(a_mn, b_mn);
+        const uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;
+        const uint32_t a_lbo = a_mn ? OP_BYTES / 2 : 16, b_lbo = b_mn ? OP_BYTES / 2 : 16;
+        for (int kb = 0; kb < t.nkb; ++kb, ++it) {
+          const int s = it % S;
+          if (!mbar_wait(&full[s], (it / S) & 1, abort_flag, p.status, p.spin_limit)) {
+            ok = false;
+            break;
+          }
+          fence_after();
+          const uint32_t a0 = smem_u32(smem + (size_t)s * stage_bytes), b0 = a0 + t.na * OP_BYTES;
+          for (int i = 0; i < t.na; ++i)
+            for (int j = 0; j < t.nb && i + j < 2; ++j) {
+#pragma unroll
+              for (int ks = 0; ks < BK / 16; ++ks)
+                mma(d, sdesc(a0 + i * OP_BYTES + ks * a_step, a_lbo, 1024),
+                    sdesc(b0 + j * OP_BYTES + ks * b_step, b_lbo, 1024), idesc,
+                    (kb > 0 || i + j + ks > 0) ? 1u : 0u);
+            }
+          commit_both(&empty[s]);
+        }
+        if (!ok) break;
+        commit_both(&tfull[ab]);
+      }
+      commit_own(done);
+      volatile int no_abort = 0;
+      mbar_wait(done, 0, &no_abort, p.status, 1LL << 28);
+    }
+  } else {
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    for (int k = 0; k < ntiles; ++k) {
+      const TileAt t = tile_at<MODE>(p, pair, k);
+      const int ab = k & 1;
+      const bool ready = mbar_wait(&tfull[ab], (k >> 1) & 1, abort_flag, p.status, p.spin_limit);
+      if (!__all_sync(0xffffffffu, ready)) break;
+      fence_after();
+      epilogue<MODE>(p, t, tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ab * TILE + half * HALF),
+                     (long long)t.m0 + rank * HALF + quarter * 32 + lane, half);
+      fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_remote(at_leader(&tempty[ab]));
+    }
+  }
+  fence_before();
+  __syncthreads();
+  // neither CTA leaves, or gives its tensor memory back, while the other may still reach it
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 1) {
+    fence_after();
+    tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// bf16 parts [parts][rows][Cp] of a matrix: hi = bf16(x), lo = bf16(x - hi), zero from C to Cp.  With
+// labels: lab = the label as an int, or -1 where there is none, whose row enters as zeros.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256)
+    k_xent_parts(const T* __restrict__ x, long long ld, long long rows, int C, int Cp, int parts,
+                 const void* __restrict__ y, int y64, int V, int* __restrict__ lab,
+                 __nv_bfloat16* __restrict__ out, uint32_t* status) {
+  using namespace rowwise;
+  const int lane = threadIdx.x & 31;
+  const int nseg = (Cp + kSeg - 1) / kSeg;
+  const long long step = (long long)gridDim.x * 8;
+  for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < rows * nseg; w += step) {
+    const long long row = w / nseg;
+    const int col0 = (int)(w - row * nseg) * kSeg;
+    bool live = true;
+    if (y) {
+      const long long l = y64 ? reinterpret_cast<const long long*>(y)[row] : reinterpret_cast<const int*>(y)[row];
+      live = l >= 0 && l < V;
+      if (col0 == 0 && lane == 0) {
+        lab[row] = live ? (int)l : -1;
+        if (l >= V) atomicOr(status, ST_BAD_LABEL);
+      }
+    }
+    float v[8];
+    if (live) {
+      load_seg<VEC>(x + row * ld, col0, lane, C, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    }
+    for (int q = 0; q < parts; ++q) {
+      store_seg<VEC>(out + ((size_t)q * rows + row) * Cp, col0, lane, Cp, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+    }
+  }
+}
+
+// lse and loss of a row from its partial sums: a warp a row.
+__global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ part, int n, long long T,
+                                                  const int* __restrict__ lab, const float* __restrict__ target,
+                                                  float* __restrict__ lse, float* __restrict__ lse_out,
+                                                  float* __restrict__ row_loss) {
+  const int lane = threadIdx.x & 31;
+  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= T) return;
+  const float2* p = part + row * n;
+  float m = -INFINITY, s = 0.f;
+  for (int k = lane; k < n; k += 32) {
+    const float2 q = __ldg(p + k);
+    const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
+    s = s * ex2((m - ref) * kLog2e) + q.y * ex2((q.x - ref) * kLog2e);
+    m = top;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
+    const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+    s = s * ex2((m - ref) * kLog2e) + s2 * ex2((m2 - ref) * kLog2e);
+    m = top;
+  }
+  if (lane == 0) {
+    const float l = m + logf(s);
+    if (lse) lse[row] = l;
+    if (lse_out) lse_out[row] = l;
+    if (row_loss) row_loss[row] = lab[row] >= 0 ? l - target[row] : 0.f;
+  }
+}
+
+// (1/T) sum of the rows' losses, in a fixed order.
+__global__ void __launch_bounds__(1024) k_xent_loss(const float* __restrict__ row_loss, long long T,
+                                                    double* __restrict__ loss) {
+  __shared__ double acc[32];
+  double s = 0.0;
+  for (long long i = threadIdx.x; i < T; i += 1024) s += (double)row_loss[i];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((threadIdx.x & 31) == 0) acc[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+    for (int w = 0; w < 32; ++w) s += acc[w];
+    *loss = s / (double)T;
+  }
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn_x() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) ==
+            cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+    return PFN_cuTensorMapEncodeTiled_v12000(nullptr);
+  }();
+  return fn;
+}
+
+// bf16 map of `rank` dimensions, innermost first; ld[i]: elements between neighbours of dimension
+// i + 1.  Box 64 x box_rows x 1 ..., 128-byte swizzle.
+int map_nd(CUtensorMap* map, const void* base, int rank, const long long* dims, const long long* ld,
+           int box_rows) {
+  auto fn = encode_fn_x();
+  if (!fn) return fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
+  cuuint64_t d[4], st[3];
+  cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  for (int i = 0; i < rank; ++i) d[i] = (cuuint64_t)dims[i];
+  for (int i = 0; i + 1 < rank; ++i) st[i] = (cuuint64_t)ld[i] * 2;
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st,
+                        box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? GC_OK : fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
+template <int MODE>
+int launch_mode(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d,
+                const XentParams& p, cudaStream_t s) {
+  static SmemOptIn allow;
+  const cudaError_t e = allow(k_xent<MODE>, kSmemX);
+  if (e != cudaSuccess) return cuda_check(e, "cudaFuncSetAttribute(k_xent)");
+  k_xent<MODE><<<(unsigned)(2 * p.pairs), kThreadsX, kSmemX, s>>>(a, b, c, d, p);
+  count_launches(1);
+  return cuda_check(cudaGetLastError(), "k_xent");
+}
+
+template <typename T>
+int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts, const void* y, int y64, int V,
+             int* lab, __nv_bfloat16* out, uint32_t* status, cudaStream_t s) {
+  const long long warps = rows * ((Cp + rowwise::kSeg - 1) / rowwise::kSeg);
+  const unsigned grid = (unsigned)std::min<long long>((warps + 7) / 8, 8LL * device_sm_count());
+  if (C % 8 == 0 && rowwise::rows_16(x, ld, sizeof(T)))
+    k_xent_parts<T, true><<<grid, 256, 0, s>>>((const T*)x, ld, rows, C, Cp, parts, y, y64, V, lab, out, status);
+  else
+    k_xent_parts<T, false><<<grid, 256, 0, s>>>((const T*)x, ld, rows, C, Cp, parts, y, y64, V, lab, out, status);
+  count_launches(1);
+  return cuda_check(cudaGetLastError(), "k_xent_parts");
+}
+
+int tiles(long long n) { return (int)((n + TILE - 1) / TILE); }
+
+// Columns of a piece: as many as kPieceElems of P allow, the pieces of one width.
+int piece_cols(long long T, int V) {
+  const long long most = std::max<long long>(TILE, kPieceElems / T / TILE * TILE);
+  const int pieces = (int)((V + most - 1) / most);
+  return tiles((V + pieces - 1) / pieces) * TILE;
+}
+
+struct XentScratch {
+  int Cp, nx, nw, piece, np;
+  bool w_in_place;
+  __nv_bfloat16 *X, *W, *P;
+  int* lab;
+  float *lse, *target, *row_loss, *acc;
+  float2* part;
+};
+
+XentScratch carve_xent(Carve& c, const XentShape& s) {
+  XentScratch w{};
+  const long long T = (long long)s.N * s.n_c;
+  w.Cp = (s.C + 7) / 8 * 8;
+  w.nx = s.x_dtype == GC_BF16 ? 1 : 2;
+  w.nw = s.w_dtype == GC_BF16 ? 1 : 2;
+  w.w_in_place = s.w_dtype == GC_BF16 && s.w_16;
+  w.X = c.take<__nv_bfloat16>((size_t)w.nx * T * w.Cp);
+  w.W = w.w_in_place ? nullptr : c.take<__nv_bfloat16>((size_t)w.nw * s.V * w.Cp);
+  w.lab = c.take<int>((size_t)T);
+  w.lse = c.take<float>((size_t)T);
+  w.target = c.take<float>((size_t)T);
+  w.row_loss = c.take<float>((size_t)T);
+  w.part = c.take<float2>((size_t)T * 2 * tiles(s.V));
+  if (s.want & (XENT_DX | XENT_G)) {
+    w.piece = piece_cols(T, s.V);
+    w.np = (s.want & XENT_G) || s.x_dtype == GC_F32 ? 2 : 1;
+    w.P = c.take<__nv_bfloat16>((size_t)w.np * T * w.piece);
+    // bf16 dX: the pieces' sum in fp32 (an fp32 dX holds it itself)
+    if ((s.want & XENT_DX) && s.x_dtype == GC_BF16 && w.piece < s.V)
+      w.acc = c.take<float>((size_t)T * ((s.C + 3) / 4 * 4));
+  }
+  return w;
+}
+
+}  // namespace
+
+size_t xent_ws_bytes(const XentShape& s) {
+  Carve c(nullptr);
+  carve_xent(c, s);
+  return c.bytes();
+}
+
+int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* status, cudaStream_t st) {
+  const XentScratch w = carve_xent(ws, s);
+  const long long T = (long long)s.N * s.n_c;
+  const bool xb = s.x_dtype == GC_BF16, wb = s.w_dtype == GC_BF16;
+  int rc = xb ? parts_of<__nv_bfloat16>(io.X, io.ldx, T, s.C, w.Cp, 1, io.y, io.y64, s.V, w.lab, w.X, status, st)
+              : parts_of<float>(io.X, io.ldx, T, s.C, w.Cp, 2, io.y, io.y64, s.V, w.lab, w.X, status, st);
+  if (rc) return rc;
+  if (!w.w_in_place) {
+    rc = wb ? parts_of<__nv_bfloat16>(io.W, io.ldw, s.V, s.C, w.Cp, 1, nullptr, 0, 0, nullptr, w.W, status, st)
+            : parts_of<float>(io.W, io.ldw, s.V, s.C, w.Cp, 2, nullptr, 0, 0, nullptr, w.W, status, st);
+    if (rc) return rc;
+  }
+  const void* W = w.w_in_place ? io.W : w.W;
+  const long long ldw = w.w_in_place ? io.ldw : w.Cp;
+  const long long Cin = w.w_in_place ? s.C : w.Cp;
+
+  XentParams p{};
+  p.T = T;
+  p.C = s.C;
+  p.V = s.V;
+  p.N = s.N;
+  p.n_c = s.n_c;
+  p.nx = w.nx;
+  p.nw = w.nw;
+  p.mt = tiles(T);
+  p.nt = tiles(s.V);
+  p.group = std::min(p.mt, 16);
+  const int pairs = device_sm_count() / 2;
+  p.pairs = (int)std::min<long long>(pairs, (long long)p.mt * p.nt);
+  p.stage_ops = w.nx + w.nw;
+  p.stages = kRing / (p.stage_ops * OP_BYTES);
+  p.lab = w.lab;
+  p.lse = w.lse;
+  p.target = w.target;
+  p.part = w.part;
+  p.spin_limit = wait_limit(kSpinX);
+  p.stall = take_stall(GC_STALL_XENT) ? 1 : 0;
+  p.status = status;
+
+  // z: rows of X and of W, K innermost
+  CUtensorMap mX, mW, mP, mWt, mP4, mX4;
+  {
+    const long long dx[3] = {w.Cp, T, w.nx}, lx[2] = {w.Cp, T * w.Cp};
+    const long long dw[3] = {Cin, s.V, w.nw}, lw[2] = {ldw, (long long)s.V * ldw};
+    if ((rc = map_nd(&mX, w.X, 3, dx, lx, HALF)) || (rc = map_nd(&mW, W, 3, dw, lw, HALF)) ||
+        (rc = map_nd(&mWt, W, 3, dw, lw, BK)))
+      return rc;
+    const long long d4[4] = {w.Cp, s.n_c, s.N, w.nx};
+    const long long l4[3] = {w.Cp, (long long)s.n_c * w.Cp, T * w.Cp};
+    if ((rc = map_nd(&mX4, w.X, 4, d4, l4, BK))) return rc;
+  }
+  if ((rc = launch_mode<STAT>(mX, mW, mX, mX, p, st))) return rc;
+  float* row_loss = io.row_loss ? io.row_loss : io.loss ? w.row_loss : nullptr;
+  k_xent_lse<<<(unsigned)((T + 7) / 8), 256, 0, st>>>(w.part, 2 * p.nt, T, w.lab, w.target, w.lse, io.lse,
+                                                      row_loss);
+  count_launches(1);
+  if ((rc = cuda_check(cudaGetLastError(), "k_xent_lse"))) return rc;
+  if (io.loss) {
+    k_xent_loss<<<1, 1024, 0, st>>>(row_loss, T, io.loss);
+    count_launches(1);
+    if ((rc = cuda_check(cudaGetLastError(), "k_xent_loss"))) return rc;
+  }
+  if (!(s.want & (XENT_DX | XENT_G))) return GC_OK;
+
+  p.P = w.P;
+  p.Pp = w.piece;
+  p.np = w.np;
+  p.np_dx = xb ? 1 : 2;
+  p.dx_bf16 = xb;
+  p.dX = io.dX;
+  p.ld_dx = io.lddx;
+  p.acc = xb ? w.acc : (float*)io.dX;
+  p.ld_acc = xb ? (s.C + 3) / 4 * 4 : io.lddx;
+  p.G = io.G;
+  p.ldg = io.ldg;
+  p.stall = 0;
+  for (int v0 = 0; v0 < s.V; v0 += w.piece) {
+    p.v0 = v0;
+    p.w = std::min(w.piece, s.V - v0);
+    p.first_piece = v0 == 0;
+    p.last_piece = v0 + w.piece >= s.V;
+    p.nt = tiles(p.w);
+    p.pairs = (int)std::min<long long>(pairs, (long long)p.mt * p.nt);
+    p.stage_ops = w.nx + w.nw;
+    p.stages = kRing / (p.stage_ops * OP_BYTES);
+    if ((rc = launch_mode<PROB>(mX, mW, mX, mX, p, st))) return rc;
+    const long long dp[3] = {p.w, T, w.np}, lp[2] = {w.piece, T * w.piece};
+    const long long d4[4] = {p.w, s.n_c, s.N, w.np};
+    const long long l4[3] = {w.piece, (long long)s.n_c * w.piece, T * w.piece};
+    if ((rc = map_nd(&mP, w.P, 3, dp, lp, HALF)) || (rc = map_nd(&mP4, w.P, 4, d4, l4, BK))) return rc;
+    p.ct = tiles(s.C);
+    p.vt = tiles(p.w);
+    p.ndx = s.want & XENT_DX ? p.mt * p.ct : 0;
+    p.ndw = s.want & XENT_G ? s.N * p.vt * p.ct : 0;
+    p.pairs = (int)std::min<long long>(pairs, (long long)p.ndx + p.ndw);
+    // the pairs with one dX tile less take that much more of G
+    p.r = p.ndx % p.pairs;
+    const int dx_prod = p.np_dx == 1 ? 1 : 1 + w.nw;
+    const double cost_dx = (double)((p.w + BK - 1) / BK) * dx_prod;
+    const double cost_dw = (double)((s.n_c + BK - 1) / BK) * (1 + w.nx);
+    p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_dw + 0.5), p.ndw / (p.pairs - p.r));
+    p.stage_ops = std::max(p.ndx ? p.np_dx + (p.np_dx == 1 ? 1 : w.nw) : 0, p.ndw ? w.np + w.nx : 0);
+    p.stages = kRing / (p.stage_ops * OP_BYTES);
+    if ((rc = launch_mode<GRAD>(mP, mWt, mP4, mX4, p, st))) return rc;
+  }
+  return GC_OK;
+}
+
+}  // namespace gc
