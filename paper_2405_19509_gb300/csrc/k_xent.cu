@@ -17,8 +17,8 @@
 // 128 rows of A and of B for a 64-wide K block (warp 0, TMA), the leader's warp 1 issuing the MMAs,
 // eight warps per CTA draining one of two accumulators while the other is filled.  Operands that
 // lie with K outermost (W in dX, P and X in G) are read MN-major: boxes of 64 columns x 64 K rows.
-// Rows past a chunk's end, columns past V and past C are zero-filled by TMA.  A row without a label
-// enters X's copy as zeros, whatever it holds.  Every wait is bounded (GC_ERR_TIMEOUT).
+// Rows past a chunk's end, columns past V and past C are zero-filled by TMA.  Every wait is bounded
+// (GC_ERR_TIMEOUT).
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -57,7 +57,7 @@ struct XentParams {
   int ndx, ct, vt, ndw, r, extra;
   int stage_ops, stages;
   int first_piece, last_piece;
-  const int* lab;      // T labels, -1: none
+  const int* lab;      // T labels, negative: none
   const float* lse;
   float* target;       // STAT: z at the label
   float2* part;        // STAT: [T][2 nt]
@@ -430,40 +430,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsX, 1)
   }
 }
 
-// bf16 parts [parts][rows][Cp] of a matrix: hi = bf16(x), lo = bf16(x - hi), zero from C to Cp.  With
-// labels: lab = the label as an int, or -1 where there is none, whose row enters as zeros.
+// bf16 parts [parts][rows][Cp] of a matrix: hi = bf16(x), lo = bf16(x - hi), zero from C to Cp.  A block
+// a row at a time.  With labels: lab = the label as an int, kNone where there is none.  The products
+// that follow multiply such a row by zeros, so what is not finite in it enters as zero (kNoneBad).
+constexpr int kNone = -1, kNoneBad = -2;
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256)
     k_xent_parts(const T* __restrict__ x, long long ld, long long rows, int C, int Cp, int parts,
                  const void* __restrict__ y, int y64, int V, int* __restrict__ lab,
                  __nv_bfloat16* __restrict__ out, uint32_t* status) {
   using namespace rowwise;
-  const int lane = threadIdx.x & 31;
-  const int nseg = (Cp + kSeg - 1) / kSeg;
-  const long long step = (long long)gridDim.x * 8;
-  for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < rows * nseg; w += step) {
-    const long long row = w / nseg;
-    const int col0 = (int)(w - row * nseg) * kSeg;
-    bool live = true;
-    if (y) {
-      const long long l = y64 ? reinterpret_cast<const long long*>(y)[row] : reinterpret_cast<const int*>(y)[row];
-      live = l >= 0 && l < V;
-      if (col0 == 0 && lane == 0) {
-        lab[row] = live ? (int)l : -1;
-        if (l >= V) atomicOr(status, ST_BAD_LABEL);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+    long long l = 0;
+    if (y) l = y64 ? reinterpret_cast<const long long*>(y)[row] : reinterpret_cast<const int*>(y)[row];
+    const bool live = !y || (l >= 0 && l < V);
+    int bad = 0;
+    for (int col0 = warp * kSeg; col0 < Cp; col0 += 8 * kSeg) {
+      float v[8];
+      load_seg<VEC>(x + row * ld, col0, lane, C, v);
+      if (!live) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (!isfinite(v[j])) {
+            v[j] = 0.f;
+            bad = 1;
+          }
+      }
+      for (int q = 0; q < parts; ++q) {
+        store_seg<VEC>(out + ((size_t)q * rows + row) * Cp, col0, lane, Cp, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
       }
     }
-    float v[8];
-    if (live) {
-      load_seg<VEC>(x + row * ld, col0, lane, C, v);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    }
-    for (int q = 0; q < parts; ++q) {
-      store_seg<VEC>(out + ((size_t)q * rows + row) * Cp, col0, lane, Cp, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+    if (y) {
+      if (!live) bad = __syncthreads_or(bad);
+      if (threadIdx.x == 0) {
+        lab[row] = live ? (int)l : bad ? kNoneBad : kNone;
+        if (l >= V) atomicOr(status, ST_BAD_LABEL);
+      }
     }
   }
 }
@@ -492,7 +497,7 @@ __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ par
     m = top;
   }
   if (lane == 0) {
-    const float l = m + logf(s);
+    const float l = lab[row] == kNoneBad ? NAN : m + logf(s);
     if (lse) lse[row] = l;
     if (lse_out) lse_out[row] = l;
     if (row_loss) row_loss[row] = lab[row] >= 0 ? l - target[row] : 0.f;
@@ -559,8 +564,7 @@ int launch_mode(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c
 template <typename T>
 int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts, const void* y, int y64, int V,
              int* lab, __nv_bfloat16* out, uint32_t* status, cudaStream_t s) {
-  const long long warps = rows * ((Cp + rowwise::kSeg - 1) / rowwise::kSeg);
-  const unsigned grid = (unsigned)std::min<long long>((warps + 7) / 8, 8LL * device_sm_count());
+  const unsigned grid = (unsigned)std::min<long long>(rows, 8LL * device_sm_count());
   if (C % 8 == 0 && rowwise::rows_16(x, ld, sizeof(T)))
     k_xent_parts<T, true><<<grid, 256, 0, s>>>((const T*)x, ld, rows, C, Cp, parts, y, y64, V, lab, out, status);
   else
