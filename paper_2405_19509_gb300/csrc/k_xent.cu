@@ -13,9 +13,15 @@
 // (X_hi W_hi + X_hi W_lo + X_lo W_hi; the dropped term is 2^-18).  All sums are fp32 in tensor memory.
 // z is not kept: T V values of it are gigabytes, while a piece of P is kPieceElems values.
 //
-// One persistent kernel shape: a pair of CTAs (cta_group::2) per 256 x 256 tile, each CTA loading
+// One persistent kernel shape: a pair of CTAs (cta_group::2) per 256 x 256 tile, each CTA holding
 // 128 rows of A and of B for a 64-wide K block (warp 0, TMA), the leader's warp 1 issuing the MMAs,
-// eight warps per CTA draining one of two accumulators while the other is filled.  Operands that
+// eight warps per CTA draining one of two accumulators while the other is filled.  Clusters of four hold
+// two pairs on neighbouring column tiles, and each loads half of A's rows for both (multicast): a
+// quarter less from L2, on 144 SMs instead of 152.  MMAs and copies are issued by an elected lane of a
+// warp that stays together: from a branch on the lane a 64-wide K block took 900 clocks to issue where
+// its MMAs take 512 (8,192 rows, C = 2048, V = 65536, losses alone: 1646 -> 1215 us, 1810 TFLOP/s, 93%
+// of the rate of the library's bf16 product; two pairs to a cluster 1218, and 6887 -> 6684 us with the
+// gradient, which runs at the power limit).  Operands that
 // lie with K outermost (W in dX, P and X in G) are read MN-major: boxes of 64 columns x 64 K rows.
 // Rows past a chunk's end, columns past V and past C are zero-filled by TMA.  Every wait is bounded
 // (GC_ERR_TIMEOUT).
@@ -51,8 +57,8 @@ struct XentParams {
   int v0, w;           // PROB, GRAD: the piece is columns [v0, v0 + w)
   int np, np_dx;       // parts of P: kept, and that enter dX
   int mt, nt, group;   // tiles of T and of the columns; row tiles that share a sweep of the columns
-  int pairs;
-  // GRAD: dX tiles, round robin; then G's, `extra` each for the pairs past the first `r`, which
+  int units;           // clusters; a cluster's tile is 256 x 128 times its CTAs
+  // GRAD: dX tiles, round robin; then G's, `extra` each for the units past the first `r`, which
   // have one dX tile less, and the rest round robin
   int ndx, ct, vt, ndw, r, extra;
   int stage_ops, stages;
@@ -60,7 +66,8 @@ struct XentParams {
   const int* lab;      // T labels, negative: none
   const float* lse;
   float* target;       // STAT: z at the label
-  float2* part;        // STAT: [T][2 nt]
+  float2* part;        // STAT: [T][slots], 128 columns a slot
+  int slots;
   __nv_bfloat16* P;    // [np][T][Pp]
   int Pp;
   float* acc;          // fp32 dX of the pieces so far
@@ -82,38 +89,38 @@ struct TileAt {
 };
 
 template <int MODE>
-__device__ __forceinline__ int tiles_of(const XentParams& p, int pair) {
-  if (MODE != GRAD) return (int)(((long long)p.mt * p.nt - pair + p.pairs - 1) / p.pairs);
-  const int nb = p.pairs - p.r;
-  const int ndx = (p.ndx - pair + p.pairs - 1) / p.pairs;
+__device__ __forceinline__ int tiles_of(const XentParams& p, int unit) {
+  if (MODE != GRAD) return (int)(((long long)p.mt * p.nt - unit + p.units - 1) / p.units);
+  const int nb = p.units - p.r;
+  const int ndx = (p.ndx - unit + p.units - 1) / p.units;
   const int rest = p.ndw - p.extra * nb;
-  return ndx + (pair >= p.r ? p.extra : 0) + (rest - pair + p.pairs - 1) / p.pairs;
+  return ndx + (unit >= p.r ? p.extra : 0) + (rest - unit + p.units - 1) / p.units;
 }
 
-// The k-th tile of a pair.
-template <int MODE>
-__device__ __forceinline__ TileAt tile_at(const XentParams& p, int pair, int k) {
+// The k-th tile of a unit; WIDE columns.
+template <int MODE, int WIDE>
+__device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) {
   TileAt t;
   if (MODE != GRAD) {
-    const int i = pair + k * p.pairs;
+    const int i = unit + k * p.units;
     const int per = p.group * p.nt, g = i / per, rem = i - g * per;
     const int gm = min(p.group, p.mt - g * p.group);
     const int n = rem / gm;
     t.kind = 0;
     t.m0 = (g * p.group + rem - n * gm) * TILE;
-    t.n0 = n * TILE;
+    t.n0 = n * WIDE;
     t.chunk = 0;
     t.nkb = (p.C + BK - 1) / BK;
     t.na = p.nx;
     t.nb = p.nw;
     return t;
   }
-  const int ndx = (p.ndx - pair + p.pairs - 1) / p.pairs;
+  const int ndx = (p.ndx - unit + p.units - 1) / p.units;
   if (k < ndx) {
-    const int i = pair + k * p.pairs;
+    const int i = unit + k * p.units;
     t.kind = 1;
     t.m0 = i / p.ct * TILE;
-    t.n0 = i % p.ct * TILE;
+    t.n0 = i % p.ct * WIDE;
     t.chunk = 0;
     t.nkb = (p.w + BK - 1) / BK;
     t.na = p.np_dx;
@@ -121,13 +128,13 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int pair, int k) 
     return t;
   }
   k -= ndx;
-  const int nb = p.pairs - p.r, mine = pair >= p.r ? p.extra : 0;
-  const int i = k < mine ? k * nb + pair - p.r : p.extra * nb + (k - mine) * p.pairs + pair;
+  const int nb = p.units - p.r, mine = unit >= p.r ? p.extra : 0;
+  const int i = k < mine ? k * nb + unit - p.r : p.extra * nb + (k - mine) * p.units + unit;
   const int per = p.vt * p.ct, c = i / per, rem = i - c * per;
   t.kind = 2;
   t.chunk = c;
   t.m0 = rem / p.ct * TILE;
-  t.n0 = rem % p.ct * TILE;
+  t.n0 = rem % p.ct * WIDE;
   t.nkb = (p.n_c + BK - 1) / BK;
   t.na = p.np;
   t.nb = p.nx;
@@ -201,12 +208,12 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
       for (int j = 0; j < 32; ++j) s += ex2(fmaf(v[j], kLog2e, -ref));
       m = top;
     }
-    if (rv) p.part[row_in * 2 * p.nt + t.n0 / HALF + half] = make_float2(m, s);
+    if (rv && t.n0 < p.V) p.part[row_in * p.slots + t.n0 / HALF + half] = make_float2(m, s);
   } else if (MODE == PROB) {
-    const bool rv = row_in < p.T;
+    const bool rv = row_in < p.T && t.n0 < p.w;
     const int lab = rv ? __ldg(p.lab + row_in) : -1;
     const float l2 = rv ? __ldg(p.lse + row_in) * kLog2e : 0.f;
-    __nv_bfloat16* out = p.P + (size_t)(rv ? row_in : 0) * p.Pp + t.n0 + half * HALF;
+    __nv_bfloat16* out = p.P + (rv ? (size_t)row_in * p.Pp + t.n0 + half * HALF : 0);
     const size_t plane = (size_t)p.T * p.Pp;
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
@@ -279,15 +286,15 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
 
 // Tensor maps: mA, mB of the first product (z: X and W rows; GRAD: P rows and W columns for dX), mP4
 // and mX4 (GRAD: P and X of a chunk, columns x points).
-template <int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsX, 1)
+template <int MODE, int CL>
+__global__ void __launch_bounds__(kThreadsX, 1)
     k_xent(const __grid_constant__ CUtensorMap mA, const __grid_constant__ CUtensorMap mB,
            const __grid_constant__ CUtensorMap mP4, const __grid_constant__ CUtensorMap mX4, XentParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kRing);  // the leader's: both CTAs' loads landed
-  uint64_t* empty = full + kMaxStages;                         // each CTA's: the MMAs on the stage are done
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kRing);  // a leader's: its pair's loads landed
+  uint64_t* empty = full + kMaxStages;                         // each CTA's: every pair's MMAs on the stage are done
   uint64_t* tfull = empty + kMaxStages;                        // [2] each CTA's: accumulator filled
   uint64_t* tempty = tfull + 2;                                // [2] the leader's: drained by both CTAs
   uint64_t* done = tempty + 2;
@@ -295,12 +302,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsX, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = (int)cta_rank(), pair = blockIdx.x >> 1;
+  constexpr int PAIRS = CL / 2, WIDE = PAIRS * TILE;
+  const int unit = blockIdx.x / CL;
+  const int rank = (int)cta_rank(), q = rank >> 1, half_m = rank & 1;  // the pair in the cluster, the half of its rows
   const int S = p.stages, stage_bytes = p.stage_ops * OP_BYTES;
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 1);
+      mbar_init(&empty[s], PAIRS);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(&tfull[a], 1);
@@ -317,111 +326,141 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreadsX, 1)
   cluster_wait();
   fence_after();
   const uint32_t tmem_base = *tmem_holder;
-  const int ntiles = tiles_of<MODE>(p, pair);
+  const int ntiles = tiles_of<MODE>(p, unit);
 
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = !p.stall;
-      for (int k = 0; k < ntiles && ok; ++k) {
-        const TileAt t = tile_at<MODE>(p, pair, k);
-        const int ma = t.m0 + rank * HALF, nb = t.n0 + rank * HALF;
-        const uint32_t bytes = (uint32_t)(t.na + t.nb) * OP_BYTES;
-        for (int kb = 0; kb < t.nkb; ++kb, ++it) {
-          const int s = it % S;
-          if (!mbar_wait(&empty[s], ((it / S) & 1) ^ 1, abort_flag, p.status, p.spin_limit)) {
-            ok = false;
-            break;
-          }
-          if (rank == 0) mbar_expect_tx(&full[s], 2 * bytes);
-          const uint32_t bar = at_leader(&full[s]);
+    const bool one = elect_one();
+    const uint16_t to = (uint16_t)(0x5 << half_m);  // the CTAs that hold the same rows of A
+    uint32_t it = 0, ph = 0;
+    int s = 0;
+    bool ok = !p.stall;
+    for (int k = 0; k < ntiles && ok; ++k) {
+      const TileAt t = tile_at<MODE, WIDE>(p, unit, k);
+      const int ma = t.m0 + half_m * HALF, nb = t.n0 + q * TILE + half_m * HALF;
+      const uint32_t bytes = (uint32_t)(t.na + t.nb) * OP_BYTES;
+      for (int kb = 0; kb < t.nkb; ++kb, ++it) {
+        if (!mbar_wait(&empty[s], ph ^ 1, abort_flag, p.status, p.spin_limit)) ok = false;
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          break;
+        }
+        if (one) {
+          if (half_m == 0) mbar_expect_tx(&full[s], 2 * bytes);
+          const uint32_t bar = at_rank(&full[s], q * 2);
           uint8_t* st = smem + (size_t)s * stage_bytes;
-          if (t.kind < 2) {
-            for (int i = 0; i < t.na; ++i, st += OP_BYTES) load_3d(st, &mA, kb * BK, ma, i, bar);
-            for (int i = 0; i < t.nb; ++i, st += OP_BYTES) {
-              if (t.kind == 0) {
-                load_3d(st, &mB, kb * BK, p.v0 + nb, i, bar);
-              } else {
-                load_3d(st, &mB, nb, p.v0 + kb * BK, i, bar);
-                load_3d(st + OP_BYTES / 2, &mB, nb + 64, p.v0 + kb * BK, i, bar);
-              }
-            }
-          } else {
-            for (int i = 0; i < t.na; ++i, st += OP_BYTES) {
+          for (int i = 0; i < t.na; ++i, st += OP_BYTES) {
+            uint8_t* dst = st + q * (OP_BYTES / 2);
+            if (t.kind < 2) {
+              if (CL == 2)
+                load_3d(st, &mA, kb * BK, ma, i, bar);
+              else
+                load_3d_to(dst, &mA, kb * BK, ma + q * 64, i, bar, to);
+            } else if (CL == 2) {
               load_4d(st, &mP4, ma, kb * BK, t.chunk, i, bar);
               load_4d(st + OP_BYTES / 2, &mP4, ma + 64, kb * BK, t.chunk, i, bar);
+            } else {
+              load_4d_to(dst, &mP4, ma + q * 64, kb * BK, t.chunk, i, bar, to);
             }
-            for (int i = 0; i < t.nb; ++i, st += OP_BYTES) {
+          }
+          for (int i = 0; i < t.nb; ++i, st += OP_BYTES) {
+            if (t.kind == 0) {
+              load_3d(st, &mB, kb * BK, p.v0 + nb, i, bar);
+            } else if (t.kind == 1) {
+              load_3d(st, &mB, nb, p.v0 + kb * BK, i, bar);
+              load_3d(st + OP_BYTES / 2, &mB, nb + 64, p.v0 + kb * BK, i, bar);
+            } else {
               load_4d(st, &mX4, nb, kb * BK, t.chunk, i, bar);
               load_4d(st + OP_BYTES / 2, &mX4, nb + 64, kb * BK, t.chunk, i, bar);
             }
           }
         }
-      }
-      // drain: a stage whose MMAs are done has landed in both CTAs.  After an abort nothing arrives any
-      // more; the copies in flight land within the one limit.
-      for (uint32_t k = it > (uint32_t)S ? it - S : 0; k < it; ++k) {
-        volatile int no_abort = 0;
-        if (!mbar_wait(&empty[k % S], (k / S) & 1, &no_abort, p.status, 1LL << 28)) break;
+        __syncwarp();
+        if (++s == S) {
+          s = 0;
+          ph ^= 1;
+        }
       }
     }
+    // drain: a stage whose MMAs are done has landed everywhere.  After an abort nothing arrives any
+    // more; the copies in flight land within the one limit.
+    for (uint32_t k = it > (uint32_t)S ? it - S : 0; k < it; ++k) {
+      volatile int no_abort = 0;
+      const bool in = mbar_wait(&empty[k % S], (k / S) & 1, &no_abort, p.status, 1LL << 28);
+      if (!__all_sync(0xffffffffu, in)) break;
+    }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
-      uint32_t it = 0;
+    if (half_m == 0) {
+      const bool one = elect_one();
+      const uint16_t all = (uint16_t)((1 << CL) - 1), pair = (uint16_t)(3 << (2 * q));
+      uint32_t ph = 0;
+      int s = 0;
       bool ok = true;
       for (int k = 0; k < ntiles && ok; ++k) {
-        const TileAt t = tile_at<MODE>(p, pair, k);
+        const TileAt t = tile_at<MODE, WIDE>(p, unit, k);
         const int ab = k & 1;
-        if (!mbar_wait(&tempty[ab], ((k >> 1) & 1) ^ 1, abort_flag, p.status, p.spin_limit)) break;
+        ok = mbar_wait(&tempty[ab], ((k >> 1) & 1) ^ 1, abort_flag, p.status, p.spin_limit);
+        if (!__all_sync(0xffffffffu, ok)) break;
         fence_after();
         const uint32_t d = tmem_base + (uint32_t)(ab * TILE);
         const bool a_mn = t.kind == 2, b_mn = t.kind >= 1;
         const uint32_t idesc = idesc_256(a_mn, b_mn);
-        const uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;
-        const uint32_t a_lbo = a_mn ? OP_BYTES / 2 : 16, b_lbo = b_mn ? OP_BYTES / 2 : 16;
-        for (int kb = 0; kb < t.nkb; ++kb, ++it) {
-          const int s = it % S;
-          if (!mbar_wait(&full[s], (it / S) & 1, abort_flag, p.status, p.spin_limit)) {
+        const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
+        const uint64_t da0 = sdesc(smem_u32(smem), a_mn ? OP_BYTES / 2 : 16, 1024);
+        const uint64_t db0 = sdesc(smem_u32(smem) + t.na * OP_BYTES, b_mn ? OP_BYTES / 2 : 16, 1024);
+        for (int kb = 0; kb < t.nkb; ++kb) {
+          ok = mbar_wait(&full[s], ph, abort_flag, p.status, p.spin_limit);
+          if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
             break;
           }
-          fence_after();
-          const uint32_t a0 = smem_u32(smem + (size_t)s * stage_bytes), b0 = a0 + t.na * OP_BYTES;
-          for (int i = 0; i < t.na; ++i)
-            for (int j = 0; j < t.nb && i + j < 2; ++j) {
+          if (one) {
+            // the descriptors of the stage: only the address, in 16-byte units, differs
+            const uint64_t at = (uint64_t)((uint32_t)s * (uint32_t)stage_bytes >> 4);
+            uint64_t da = da0 + at;
+            for (int i = 0; i < t.na; ++i, da += OP_BYTES >> 4) {
+              uint64_t db = db0 + at;
+              for (int j = 0; j < t.nb && i + j < 2; ++j, db += OP_BYTES >> 4) {
 #pragma unroll
-              for (int ks = 0; ks < BK / 16; ++ks)
-                mma(d, sdesc(a0 + i * OP_BYTES + ks * a_step, a_lbo, 1024),
-                    sdesc(b0 + j * OP_BYTES + ks * b_step, b_lbo, 1024), idesc,
-                    (kb > 0 || i + j + ks > 0) ? 1u : 0u);
+                for (int ks = 0; ks < BK / 16; ++ks)
+                  mma(d, da + (uint64_t)(ks * a_step), db + (uint64_t)(ks * b_step), idesc,
+                      (kb > 0 || i + j + ks > 0) ? 1u : 0u);
+              }
             }
-          commit_both(&empty[s]);
+            commit_to(&empty[s], all);
+            if (kb == t.nkb - 1) commit_to(&tfull[ab], pair);
+          }
+          __syncwarp();
+          if (++s == S) {
+            s = 0;
+            ph ^= 1;
+          }
         }
-        if (!ok) break;
-        commit_both(&tfull[ab]);
       }
-      commit_own(done);
+      if (one) commit_own(done);
+      __syncwarp();
       volatile int no_abort = 0;
       mbar_wait(done, 0, &no_abort, p.status, 1LL << 28);
+      __syncwarp();
     }
   } else {
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     for (int k = 0; k < ntiles; ++k) {
-      const TileAt t = tile_at<MODE>(p, pair, k);
+      TileAt t = tile_at<MODE, WIDE>(p, unit, k);
+      t.n0 += q * TILE;
       const int ab = k & 1;
       const bool ready = mbar_wait(&tfull[ab], (k >> 1) & 1, abort_flag, p.status, p.spin_limit);
       if (!__all_sync(0xffffffffu, ready)) break;
       fence_after();
       epilogue<MODE>(p, t, tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ab * TILE + half * HALF),
-                     (long long)t.m0 + rank * HALF + quarter * 32 + lane, half);
+                     (long long)t.m0 + half_m * HALF + quarter * 32 + lane, half);
       fence_before();
       __syncwarp();
-      if (lane == 0) arrive_remote(at_leader(&tempty[ab]));
+      if (lane == 0) arrive_remote(at_rank(&tempty[ab], q * 2));
     }
   }
   fence_before();
   __syncthreads();
-  // neither CTA leaves, or gives its tensor memory back, while the other may still reach it
+  // no CTA leaves, or gives its tensor memory back, while another may still reach it
   cluster_arrive();
   cluster_wait();
   if (warp == 1) {
@@ -550,15 +589,51 @@ int map_nd(CUtensorMap* map, const void* base, int rank, const long long* dims, 
   return r == CUDA_SUCCESS ? GC_OK : fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
-template <int MODE>
+// Clusters of CL CTAs that the current device holds at once.
+template <int MODE, int CL>
+int resident(int* units) {
+  static std::atomic<int> cache[64];
+  int dev = 0, n = 0;
+  GC_CUDA(cudaGetDevice(&dev));
+  if (dev >= 0 && dev < 64) n = cache[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    static SmemOptIn allow;
+    GC_CUDA(allow(k_xent<MODE, CL>, kSmemX));
+    cudaLaunchAttribute at[1];
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(CL);
+    cfg.blockDim = dim3(kThreadsX);
+    cfg.dynamicSmemBytes = kSmemX;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CL;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    GC_CUDA(cudaOccupancyMaxActiveClusters(&n, k_xent<MODE, CL>, &cfg));
+    if (n < 1) return fail(GC_ERR_CUDA, "no cluster of %d CTAs fits the device", CL);
+    if (dev >= 0 && dev < 64) cache[dev].store(n, std::memory_order_relaxed);
+  }
+  *units = n;
+  return GC_OK;
+}
+
+template <int MODE, int CL>
 int launch_mode(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d,
                 const XentParams& p, cudaStream_t s) {
-  static SmemOptIn allow;
-  const cudaError_t e = allow(k_xent<MODE>, kSmemX);
-  if (e != cudaSuccess) return cuda_check(e, "cudaFuncSetAttribute(k_xent)");
-  k_xent<MODE><<<(unsigned)(2 * p.pairs), kThreadsX, kSmemX, s>>>(a, b, c, d, p);
+  cudaLaunchAttribute at[1];
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(CL * p.units));
+  cfg.blockDim = dim3(kThreadsX);
+  cfg.dynamicSmemBytes = kSmemX;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = CL;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_xent<MODE, CL>, a, b, c, d, p);
   count_launches(1);
-  return cuda_check(cudaGetLastError(), "k_xent");
+  return cuda_check(e, "k_xent");
 }
 
 template <typename T>
@@ -573,7 +648,7 @@ int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts
   return cuda_check(cudaGetLastError(), "k_xent_parts");
 }
 
-int tiles(long long n) { return (int)((n + TILE - 1) / TILE); }
+int tiles(long long n, int wide = TILE) { return (int)((n + wide - 1) / wide); }
 
 // Columns of a piece: as many as kPieceElems of P allow, the pieces of one width.
 int piece_cols(long long T, int V) {
@@ -616,6 +691,48 @@ XentScratch carve_xent(Carve& c, const XentShape& s) {
   return w;
 }
 
+// Two pairs to a cluster where there are columns and tiles for them (two a cluster at least), and rows
+// enough for the sharing of A's to count: of one row tile A is little, and reading B takes every SM
+// (one row, C = 2048, V = 65536: 98 us in pairs, 136 in clusters of two; 2,048 rows, C = 1024, V = 32000:
+// 121 and 116).
+bool two_pairs(long long row_tiles, int cols) {
+  return row_tiles >= 4 && cols > TILE && row_tiles * tiles(cols, 2 * TILE) >= 2 * (device_sm_count() / 4);
+}
+
+template <int MODE, int CL>
+int run_z(XentParams p, const CUtensorMap& mX, const CUtensorMap& mW, cudaStream_t st) {
+  int n = 0;
+  const int rc = resident<MODE, CL>(&n);
+  if (rc) return rc;
+  p.nt = tiles(MODE == STAT ? p.V : p.w, CL / 2 * TILE);
+  p.units = (int)std::min<long long>(n, (long long)p.mt * p.nt);
+  p.stage_ops = p.nx + p.nw;
+  p.stages = kRing / (p.stage_ops * OP_BYTES);
+  return launch_mode<MODE, CL>(mX, mW, mX, mX, p, st);
+}
+
+template <int CL>
+int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& mWt, const CUtensorMap& mP4,
+             const CUtensorMap& mX4, cudaStream_t st) {
+  int n = 0;
+  const int rc = resident<GRAD, CL>(&n);
+  if (rc) return rc;
+  p.ct = tiles(p.C, CL / 2 * TILE);
+  p.vt = tiles(p.w);
+  p.ndx = want & XENT_DX ? p.mt * p.ct : 0;
+  p.ndw = want & XENT_G ? p.N * p.vt * p.ct : 0;
+  p.units = (int)std::min<long long>(n, (long long)p.ndx + p.ndw);
+  // the units with one dX tile less take that much more of G
+  p.r = p.ndx % p.units;
+  const int dx_a = p.np_dx, dx_b = p.np_dx == 1 ? 1 : p.nw, dx_prod = p.np_dx == 1 ? 1 : 1 + p.nw;
+  const double cost_dx = (double)((p.w + BK - 1) / BK) * dx_prod;
+  const double cost_dw = (double)((p.n_c + BK - 1) / BK) * (1 + p.nx);
+  p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_dw + 0.5), p.ndw / (p.units - p.r));
+  p.stage_ops = std::max(p.ndx ? dx_a + dx_b : 0, p.ndw ? p.np + p.nx : 0);
+  p.stages = kRing / (p.stage_ops * OP_BYTES);
+  return launch_mode<GRAD, CL>(mP, mWt, mP4, mX4, p, st);
+}
+
 }  // namespace
 
 size_t xent_ws_bytes(const XentShape& s) {
@@ -649,12 +766,8 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.nx = w.nx;
   p.nw = w.nw;
   p.mt = tiles(T);
-  p.nt = tiles(s.V);
   p.group = std::min(p.mt, 16);
-  const int pairs = device_sm_count() / 2;
-  p.pairs = (int)std::min<long long>(pairs, (long long)p.mt * p.nt);
-  p.stage_ops = w.nx + w.nw;
-  p.stages = kRing / (p.stage_ops * OP_BYTES);
+  p.slots = 2 * tiles(s.V);
   p.lab = w.lab;
   p.lse = w.lse;
   p.target = w.target;
@@ -664,20 +777,21 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.status = status;
 
   // z: rows of X and of W, K innermost
-  CUtensorMap mX, mW, mP, mWt, mP4, mX4;
+  CUtensorMap mX, mX2, mW, mP, mWt, mP4, mX4;  // mX2: boxes of half the rows, for two pairs
   {
     const long long dx[3] = {w.Cp, T, w.nx}, lx[2] = {w.Cp, T * w.Cp};
     const long long dw[3] = {Cin, s.V, w.nw}, lw[2] = {ldw, (long long)s.V * ldw};
-    if ((rc = map_nd(&mX, w.X, 3, dx, lx, HALF)) || (rc = map_nd(&mW, W, 3, dw, lw, HALF)) ||
+    if ((rc = map_nd(&mX, w.X, 3, dx, lx, HALF)) || (rc = map_nd(&mX2, w.X, 3, dx, lx, HALF / 2)) || (rc = map_nd(&mW, W, 3, dw, lw, HALF)) ||
         (rc = map_nd(&mWt, W, 3, dw, lw, BK)))
       return rc;
     const long long d4[4] = {w.Cp, s.n_c, s.N, w.nx};
     const long long l4[3] = {w.Cp, (long long)s.n_c * w.Cp, T * w.Cp};
     if ((rc = map_nd(&mX4, w.X, 4, d4, l4, BK))) return rc;
   }
-  if ((rc = launch_mode<STAT>(mX, mW, mX, mX, p, st))) return rc;
+  rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, st) : run_z<STAT, 2>(p, mX, mW, st);
+  if (rc) return rc;
   float* row_loss = io.row_loss ? io.row_loss : io.loss ? w.row_loss : nullptr;
-  k_xent_lse<<<(unsigned)((T + 7) / 8), 256, 0, st>>>(w.part, 2 * p.nt, T, w.lab, w.target, w.lse, io.lse,
+  k_xent_lse<<<(unsigned)((T + 7) / 8), 256, 0, st>>>(w.part, p.slots, T, w.lab, w.target, w.lse, io.lse,
                                                       row_loss);
   count_launches(1);
   if ((rc = cuda_check(cudaGetLastError(), "k_xent_lse"))) return rc;
@@ -705,29 +819,16 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     p.w = std::min(w.piece, s.V - v0);
     p.first_piece = v0 == 0;
     p.last_piece = v0 + w.piece >= s.V;
-    p.nt = tiles(p.w);
-    p.pairs = (int)std::min<long long>(pairs, (long long)p.mt * p.nt);
-    p.stage_ops = w.nx + w.nw;
-    p.stages = kRing / (p.stage_ops * OP_BYTES);
-    if ((rc = launch_mode<PROB>(mX, mW, mX, mX, p, st))) return rc;
+    rc = two_pairs(p.mt, p.w) ? run_z<PROB, 4>(p, mX2, mW, st) : run_z<PROB, 2>(p, mX, mW, st);
+    if (rc) return rc;
+    const bool two = two_pairs((s.want & XENT_DX ? p.mt : 0) + (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0), s.C);
     const long long dp[3] = {p.w, T, w.np}, lp[2] = {w.piece, T * w.piece};
     const long long d4[4] = {p.w, s.n_c, s.N, w.np};
     const long long l4[3] = {w.piece, (long long)s.n_c * w.piece, T * w.piece};
-    if ((rc = map_nd(&mP, w.P, 3, dp, lp, HALF)) || (rc = map_nd(&mP4, w.P, 4, d4, l4, BK))) return rc;
-    p.ct = tiles(s.C);
-    p.vt = tiles(p.w);
-    p.ndx = s.want & XENT_DX ? p.mt * p.ct : 0;
-    p.ndw = s.want & XENT_G ? s.N * p.vt * p.ct : 0;
-    p.pairs = (int)std::min<long long>(pairs, (long long)p.ndx + p.ndw);
-    // the pairs with one dX tile less take that much more of G
-    p.r = p.ndx % p.pairs;
-    const int dx_prod = p.np_dx == 1 ? 1 : 1 + w.nw;
-    const double cost_dx = (double)((p.w + BK - 1) / BK) * dx_prod;
-    const double cost_dw = (double)((s.n_c + BK - 1) / BK) * (1 + w.nx);
-    p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_dw + 0.5), p.ndw / (p.pairs - p.r));
-    p.stage_ops = std::max(p.ndx ? p.np_dx + (p.np_dx == 1 ? 1 : w.nw) : 0, p.ndw ? w.np + w.nx : 0);
-    p.stages = kRing / (p.stage_ops * OP_BYTES);
-    if ((rc = launch_mode<GRAD>(mP, mWt, mP4, mX4, p, st))) return rc;
+    if ((rc = map_nd(&mP, w.P, 3, dp, lp, two ? HALF / 2 : HALF)) || (rc = map_nd(&mP4, w.P, 4, d4, l4, BK)))
+      return rc;
+    rc = two ? run_grad<4>(p, s.want, mP, mWt, mP4, mX4, st) : run_grad<2>(p, s.want, mP, mWt, mP4, mX4, st);
+    if (rc) return rc;
   }
   return GC_OK;
 }

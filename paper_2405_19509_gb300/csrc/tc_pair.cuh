@@ -1,7 +1,8 @@
 // Inline-PTX wrappers for tcgen05 on a pair of CTAs (cta_group::2): a cluster of two whose SMs work on
 // one 256-row tile, each holding half of A's and half of B's rows in its own shared memory and half of
-// the accumulator's rows in its tensor memory.  The CTA of rank 0 leads: it issues the MMAs, and
-// the barriers that its MMA thread waits on live in its shared memory.
+// the accumulator's rows in its tensor memory.  The CTA of even rank leads: it issues the MMAs, and
+// the barriers that its MMA thread waits on live in its shared memory.  A cluster is one pair, or two
+// that share A's rows.
 #pragma once
 
 #include "tc_ptx.cuh"
@@ -11,15 +12,22 @@ namespace tcp {
 
 using namespace tcw;
 
+// One lane of a whole warp.  MMAs and TMA copies take uniform registers: issued by an elected lane of a
+// warp that stays together they are four times as fast to issue as from a branch on the lane.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
 __device__ __forceinline__ uint32_t cta_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-// The leader's copy of a barrier, as a shared::cluster address.
-__device__ __forceinline__ uint32_t at_leader(const void* p) {
+// A barrier of the cluster's CTA `rank`, as a shared::cluster address.
+__device__ __forceinline__ uint32_t at_rank(const void* p, int rank) {
   uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
   return r;
 }
 __device__ __forceinline__ void cluster_arrive() {
@@ -47,6 +55,24 @@ __device__ __forceinline__ void load_4d(void* dst, const CUtensorMap* map, int x
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
       : "memory");
 }
+// The same into every CTA of `mask`, at this offset, completing on the barriers at bar's offset in
+// the CTAs of bar's parity of their pairs.
+__device__ __forceinline__ void load_3d_to(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar,
+                                           uint16_t mask) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster"
+      ".cta_group::2 [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "h"(mask)
+      : "memory");
+}
+__device__ __forceinline__ void load_4d_to(void* dst, const CUtensorMap* map, int x, int y, int z, int w,
+                                           uint32_t bar, uint16_t mask) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster"
+      ".cta_group::2 [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "h"(mask)
+      : "memory");
+}
 // Instruction descriptor, kind::f16: D fp32, A and B bf16, M = 256 and N = 256 over the pair; operands
 // K-major or MN-major.
 __device__ __forceinline__ uint32_t idesc_256(bool a_mn, bool b_mn) {
@@ -61,12 +87,12 @@ __device__ __forceinline__ void mma(uint32_t d_tmem, uint64_t a, uint64_t b, uin
       "l"(a), "l"(b), "r"(idesc), "r"(accum)
       : "memory");
 }
-// Arrives on the barrier at this offset in both CTAs when the MMAs issued so far are done.
-__device__ __forceinline__ void commit_both(uint64_t* bar) {
+// Arrives on the barrier at this offset in every CTA of `mask` when the MMAs issued so far are done.
+__device__ __forceinline__ void commit_to(uint64_t* bar, uint16_t mask) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
           smem_u32(bar)),
-      "h"((uint16_t)3)
+      "h"(mask)
       : "memory");
 }
 // ... on the barrier of this CTA alone.

@@ -109,6 +109,21 @@ def test_matches_reference(gc, N, n_c, C, V, x, w, layout):
         assert (dbuf[:, :first] == -77).all() and (dbuf[:, first + C:] == -77).all()
 
 
+@pytest.mark.parametrize("x,w", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("N,n_c,C,V", [(20, 20, 520, 3000), (3, 700, 600, 9001), (2, 1100, 770, 5000)])
+def test_two_pairs_to_a_cluster(gc, N, n_c, C, V, x, w):
+    """Enough tiles for clusters of two pairs; the last column tile is half or wholly past the columns."""
+    X, W, y = _data(N, n_c, C, V, x, w, N + n_c + C + V)
+    ref = _reference(X, W, y, N)
+    ws = gc.Workspace()
+    got = gc.gc_softmax_xent(X, W, y, N, n_c, ws=ws)
+    gc.gc_status(ws)
+    for k in ref:
+        _close(got[k], ref[k], k)
+    again = gc.gc_softmax_xent(X, W, y, N, n_c, ws=ws)
+    assert all(torch.equal(got[k], again[k]) for k in got)
+
+
 def test_reference_is_the_oracle(gc):
     X, W, y = _data(3, 6, 10, 40, "f32", "f32", 1)
     ref = _reference(X, W, y, 3)
