@@ -40,15 +40,19 @@ using namespace tcp;
 constexpr int TILE = 256, HALF = 128, BK = 64;
 constexpr int OP_BYTES = HALF * BK * 2;  // a CTA's 128 x 64 share of an operand tile
 constexpr int kMaxStages = 6;
-constexpr int kRing = kMaxStages * 2 * OP_BYTES;  // 192 KB
 constexpr int kEpi = 8;
 constexpr int kThreadsX = 64 + 32 * kEpi;
-constexpr size_t kSmemX = kRing + 1024 + 256;
+constexpr int BOX = 32 * 128;  // a store box: 32 rows of 128 bytes, 128-byte swizzle
 constexpr long long kSpinX = 1LL << 32;
 constexpr long long kPieceElems = 1LL << 26;  // of P: 256 MB as two bf16 parts
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum { STAT = 0, PROB = 1, GRAD = 2 };
+// The ring of operand stages and the store boxes of each epilogue warp.
+constexpr int ring_bytes(int mode) { return (mode == PROB ? 10 : 12) * OP_BYTES; }
+constexpr int boxes(int mode) { return mode == PROB ? 2 : mode == GRAD ? 1 : 0; }
+constexpr size_t smem_bytes(int mode) { return ring_bytes(mode) + kEpi * boxes(mode) * BOX + 1024 + 256; }
+static_assert(smem_bytes(PROB) <= kSmemMax && smem_bytes(GRAD) <= kSmemMax, "shared memory");
 
 struct XentParams {
   long long T;
@@ -77,6 +81,7 @@ struct XentParams {
   int dx_bf16;
   float* G;
   long long ldg;
+  int g_box, acc_box;  // G and the fp32 dX in whole boxes: rows on 16-byte boundaries
   long long spin_limit;
   int stall;
   uint32_t* status;
@@ -174,9 +179,42 @@ __device__ __forceinline__ void store_row(T* dst, const float (&v)[32], int n, b
     if (j < n) dst[j] = rowwise::from_f<T>(v[j]);
 }
 
+// Row `lane` of a box: 16-byte piece j lies at j ^ (row mod 8), which makes both the rows' and the
+// columns' accesses free of bank conflicts.
+__device__ __forceinline__ void box_row(uint8_t* box, int lane, const float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    *reinterpret_cast<float4*>(box + lane * 128 + ((j ^ (lane & 7)) * 16)) =
+        make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+}
+__device__ __forceinline__ void box_row_half(uint8_t* box, int lane, int first, const float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __nv_bfloat162 t = __floats2bfloat162_rn(v[8 * j + 2 * e], v[8 * j + 2 * e + 1]);
+      w[e] = *reinterpret_cast<const uint32_t*>(&t);
+    }
+    *reinterpret_cast<uint4*>(box + lane * 128 + (((first + j) ^ (lane & 7)) * 16)) =
+        make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+// The box may be written again: its last store has read it.
+__device__ __forceinline__ void box_free(int lane) {
+  if (lane == 0) bulk_wait_read<0>();
+  __syncwarp();
+}
+// What the warp wrote to its box is there for a store, which lane 0 issues.
+__device__ __forceinline__ void box_ready() {
+  fence_async_smem();
+  __syncwarp();
+}
+
 template <int MODE>
 __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, uint32_t taddr, long long row_in,
-                                         int half) {
+                                         int half, uint8_t* box, const CUtensorMap* mOut, const CUtensorMap* mAcc) {
+  const int lane = threadIdx.x & 31;
   if (MODE == STAT) {
     const bool rv = row_in < p.T;
     const int lab = rv ? __ldg(p.lab + row_in) : -1;
@@ -213,12 +251,11 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
     const bool rv = row_in < p.T && t.n0 < p.w;
     const int lab = rv ? __ldg(p.lab + row_in) : -1;
     const float l2 = rv ? __ldg(p.lse + row_in) * kLog2e : 0.f;
-    __nv_bfloat16* out = p.P + (rv ? (size_t)row_in * p.Pp + t.n0 + half * HALF : 0);
-    const size_t plane = (size_t)p.T * p.Pp;
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
       __syncwarp();
       tmem_ld32(taddr + (uint32_t)(c * 32), v);
+      if (t.n0 >= p.w || row_in - lane >= p.T) continue;  // nothing of the warp's rows or columns exists
       const int at = lab - (p.v0 + t.n0 + half * HALF + c * 32);  // the label's place here
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] = lab >= 0 ? ex2(fmaf(v[j], kLog2e, -l2)) : 0.f;
@@ -227,26 +264,47 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
         for (int j = 0; j < 32; ++j)
           if (j == at) v[j] -= 1.f;
       }
-      if (rv) {
-        store_row(out + c * 32, v, 32, true);
-        if (p.np == 2) {
+      if (c % 2 == 0) box_free(lane);
+      box_row_half(box, lane, c % 2 * 4, v);
+      if (p.np == 2) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
-          store_row(out + plane + c * 32, v, 32, true);
+        for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+        box_row_half(box + BOX, lane, c % 2 * 4, v);
+      }
+      if (c % 2) {  // 64 columns, all parts in one store
+        box_ready();
+        if (lane == 0) {
+          store_3d(mOut, box, t.n0 + half * HALF + (c - 1) * 32, (int)row_in, 0);
+          bulk_commit();
         }
       }
     }
   } else if (t.kind == 1) {
     const bool rv = row_in < p.T;
+    const bool out = p.last_piece && p.dx_bf16;  // the sum is complete and leaves in bf16
+    const bool vec = p.ld_acc % 4 == 0 && reinterpret_cast<uintptr_t>(p.acc) % 16 == 0;
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
       __syncwarp();
       tmem_ld32(taddr + (uint32_t)(c * 32), v);
       const int col = t.n0 + half * HALF + c * 32, n = p.C - col;
-      if (!rv || n <= 0) continue;
+      if (n <= 0 || row_in - lane >= p.T) continue;
+      if (!out && p.acc_box) {
+        box_free(lane);
+        box_row(box, lane, v);
+        box_ready();
+        if (lane == 0) {
+          if (p.first_piece)
+            store_3d(mAcc, box, col, (int)row_in, 0);
+          else
+            add_3d(mAcc, box, col, (int)row_in, 0);  // one addition an element and piece, in the pieces' order
+          bulk_commit();
+        }
+        continue;
+      }
+      if (!rv) continue;
       float* a = p.acc + row_in * p.ld_acc + col;
       if (!p.first_piece) {
-        const bool vec = p.ld_acc % 4 == 0 && reinterpret_cast<uintptr_t>(p.acc) % 16 == 0;
         if (vec && n >= 32) {
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
@@ -262,38 +320,56 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
             if (j < n) v[j] += a[j];
         }
       }
-      if (p.last_piece && p.dx_bf16) {
+      if (out) {
         __nv_bfloat16* o = (__nv_bfloat16*)p.dX + row_in * p.ld_dx + col;
         store_row(o, v, n, p.ld_dx % 8 == 0 && reinterpret_cast<uintptr_t>(p.dX) % 16 == 0);
       } else {
-        store_row(a, v, n, p.ld_acc % 4 == 0 && reinterpret_cast<uintptr_t>(p.acc) % 16 == 0);
+        store_row(a, v, n, vec);
       }
     }
   } else {
     const int lv = (int)row_in;  // row of the piece
-    const bool rv = lv < p.w;
-    float* g = p.G + t.chunk * p.ldg + (long long)(p.v0 + (rv ? lv : 0)) * p.C;
-    const bool vec = p.C % 4 == 0 && p.ldg % 4 == 0 && reinterpret_cast<uintptr_t>(p.G) % 16 == 0;
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
       __syncwarp();
       tmem_ld32(taddr + (uint32_t)(c * 32), v);
       const int col = t.n0 + half * HALF + c * 32, n = p.C - col;
-      if (rv && n > 0) store_row(g + col, v, n, vec);
+      if (n <= 0 || lv - lane >= p.w) continue;
+      box_free(lane);
+      box_row(box, lane, v);
+      if (p.g_box) {
+        box_ready();
+        if (lane == 0) {
+          store_3d(mOut, box, col, p.v0 + lv, t.chunk);
+          bulk_commit();
+        }
+      } else {  // row by row, 32 neighbouring values a store
+        __syncwarp();
+        float* g = p.G + t.chunk * p.ldg + (long long)(p.v0 + lv - lane) * p.C + col + lane;
+        const int rows = p.w - (lv - lane);
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r) {
+          const float x = *reinterpret_cast<const float*>(box + r * 128 + (((lane / 4) ^ (r & 7)) * 16) + lane % 4 * 4);
+          if (r < rows && lane < n) g[(long long)r * p.C] = x;
+        }
+      }
     }
   }
 }
 
 // Tensor maps: mA, mB of the first product (z: X and W rows; GRAD: P rows and W columns for dX), mP4
-// and mX4 (GRAD: P and X of a chunk, columns x points).
+// and mX4 (GRAD: P and X of a chunk, columns x points); of the stores, mOut (PROB: P; GRAD: G) and
+// mAcc (GRAD: the fp32 dX).
 template <int MODE, int CL>
 __global__ void __launch_bounds__(kThreadsX, 1)
     k_xent(const __grid_constant__ CUtensorMap mA, const __grid_constant__ CUtensorMap mB,
-           const __grid_constant__ CUtensorMap mP4, const __grid_constant__ CUtensorMap mX4, XentParams p) {
+           const __grid_constant__ CUtensorMap mP4, const __grid_constant__ CUtensorMap mX4,
+           const __grid_constant__ CUtensorMap mOut, const __grid_constant__ CUtensorMap mAcc, XentParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kRing);  // a leader's: its pair's loads landed
+  uint8_t* store_box = smem + ring_bytes(MODE);  // boxes(MODE) an epilogue warp
+  uint64_t* full = reinterpret_cast<uint64_t*>(store_box + kEpi * boxes(MODE) * BOX);  // a leader's: its pair's loads landed
   uint64_t* empty = full + kMaxStages;                         // each CTA's: every pair's MMAs on the stage are done
   uint64_t* tfull = empty + kMaxStages;                        // [2] each CTA's: accumulator filled
   uint64_t* tempty = tfull + 2;                                // [2] the leader's: drained by both CTAs
@@ -452,11 +528,13 @@ __global__ void __launch_bounds__(kThreadsX, 1)
       if (!__all_sync(0xffffffffu, ready)) break;
       fence_after();
       epilogue<MODE>(p, t, tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ab * TILE + half * HALF),
-                     (long long)t.m0 + half_m * HALF + quarter * 32 + lane, half);
+                     (long long)t.m0 + half_m * HALF + quarter * 32 + lane, half,
+                     store_box + (warp - 2) * boxes(MODE) * BOX, &mOut, &mAcc);
       fence_before();
       __syncwarp();
       if (lane == 0) arrive_remote(at_rank(&tempty[ab], q * 2));
     }
+    if (boxes(MODE) && lane == 0) bulk_wait_all();
   }
   fence_before();
   __syncthreads();
@@ -573,17 +651,17 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn_x() {
   return fn;
 }
 
-// bf16 map of `rank` dimensions, innermost first; ld[i]: elements between neighbours of dimension
-// i + 1.  Box 64 x box_rows x 1 ..., 128-byte swizzle.
+// Map of `rank` dimensions, bf16 or fp32, innermost first; ld[i]: elements between neighbours of
+// dimension i + 1.  Box 128 bytes x box_rows x box_planes, 128-byte swizzle.
 int map_nd(CUtensorMap* map, const void* base, int rank, const long long* dims, const long long* ld,
-           int box_rows) {
+           int box_rows, int box_planes = 1, bool f32 = false) {
   auto fn = encode_fn_x();
   if (!fn) return fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
   cuuint64_t d[4], st[3];
-  cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  cuuint32_t box[4] = {f32 ? 32u : 64u, (cuuint32_t)box_rows, (cuuint32_t)box_planes, 1}, one[4] = {1, 1, 1, 1};
   for (int i = 0; i < rank; ++i) d[i] = (cuuint64_t)dims[i];
-  for (int i = 0; i + 1 < rank; ++i) st[i] = (cuuint64_t)ld[i] * 2;
-  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st,
+  for (int i = 0; i + 1 < rank; ++i) st[i] = (cuuint64_t)ld[i] * (f32 ? 4 : 2);
+  const CUresult r = fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st,
                         box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? GC_OK : fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
@@ -598,12 +676,12 @@ int resident(int* units) {
   if (dev >= 0 && dev < 64) n = cache[dev].load(std::memory_order_relaxed);
   if (n == 0) {
     static SmemOptIn allow;
-    GC_CUDA(allow(k_xent<MODE, CL>, kSmemX));
+    GC_CUDA(allow(k_xent<MODE, CL>, smem_bytes(MODE)));
     cudaLaunchAttribute at[1];
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(CL);
     cfg.blockDim = dim3(kThreadsX);
-    cfg.dynamicSmemBytes = kSmemX;
+    cfg.dynamicSmemBytes = smem_bytes(MODE);
     cfg.attrs = at;
     cfg.numAttrs = 1;
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -619,19 +697,19 @@ int resident(int* units) {
 
 template <int MODE, int CL>
 int launch_mode(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d,
-                const XentParams& p, cudaStream_t s) {
+                const CUtensorMap& out, const CUtensorMap& acc, const XentParams& p, cudaStream_t s) {
   cudaLaunchAttribute at[1];
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(CL * p.units));
   cfg.blockDim = dim3(kThreadsX);
-  cfg.dynamicSmemBytes = kSmemX;
+  cfg.dynamicSmemBytes = smem_bytes(MODE);
   cfg.stream = s;
   cfg.attrs = at;
   cfg.numAttrs = 1;
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = CL;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_xent<MODE, CL>, a, b, c, d, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_xent<MODE, CL>, a, b, c, d, out, acc, p);
   count_launches(1);
   return cuda_check(e, "k_xent");
 }
@@ -700,20 +778,20 @@ bool two_pairs(long long row_tiles, int cols) {
 }
 
 template <int MODE, int CL>
-int run_z(XentParams p, const CUtensorMap& mX, const CUtensorMap& mW, cudaStream_t st) {
+int run_z(XentParams p, const CUtensorMap& mX, const CUtensorMap& mW, const CUtensorMap& mOut, cudaStream_t st) {
   int n = 0;
   const int rc = resident<MODE, CL>(&n);
   if (rc) return rc;
   p.nt = tiles(MODE == STAT ? p.V : p.w, CL / 2 * TILE);
   p.units = (int)std::min<long long>(n, (long long)p.mt * p.nt);
   p.stage_ops = p.nx + p.nw;
-  p.stages = kRing / (p.stage_ops * OP_BYTES);
-  return launch_mode<MODE, CL>(mX, mW, mX, mX, p, st);
+  p.stages = ring_bytes(MODE) / (p.stage_ops * OP_BYTES);
+  return launch_mode<MODE, CL>(mX, mW, mX, mX, mOut, mX, p, st);
 }
 
 template <int CL>
 int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& mWt, const CUtensorMap& mP4,
-             const CUtensorMap& mX4, cudaStream_t st) {
+             const CUtensorMap& mX4, const CUtensorMap& mG, const CUtensorMap& mAcc, cudaStream_t st) {
   int n = 0;
   const int rc = resident<GRAD, CL>(&n);
   if (rc) return rc;
@@ -729,8 +807,8 @@ int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& m
   const double cost_dw = (double)((p.n_c + BK - 1) / BK) * (1 + p.nx);
   p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_dw + 0.5), p.ndw / (p.units - p.r));
   p.stage_ops = std::max(p.ndx ? dx_a + dx_b : 0, p.ndw ? p.np + p.nx : 0);
-  p.stages = kRing / (p.stage_ops * OP_BYTES);
-  return launch_mode<GRAD, CL>(mP, mWt, mP4, mX4, p, st);
+  p.stages = ring_bytes(GRAD) / (p.stage_ops * OP_BYTES);
+  return launch_mode<GRAD, CL>(mP, mWt, mP4, mX4, mG, mAcc, p, st);
 }
 
 }  // namespace
@@ -788,7 +866,7 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     const long long l4[3] = {w.Cp, (long long)s.n_c * w.Cp, T * w.Cp};
     if ((rc = map_nd(&mX4, w.X, 4, d4, l4, BK))) return rc;
   }
-  rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, st) : run_z<STAT, 2>(p, mX, mW, st);
+  rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, mX, st) : run_z<STAT, 2>(p, mX, mW, mX, st);
   if (rc) return rc;
   float* row_loss = io.row_loss ? io.row_loss : io.loss ? w.row_loss : nullptr;
   k_xent_lse<<<(unsigned)((T + 7) / 8), 256, 0, st>>>(w.part, p.slots, T, w.lab, w.target, w.lse, io.lse,
@@ -814,20 +892,34 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.G = io.G;
   p.ldg = io.ldg;
   p.stall = 0;
+  CUtensorMap mPs, mG = mX, mAcc = mX;
+  p.g_box = io.G && s.C % 4 == 0 && rowwise::rows_16(io.G, io.ldg, 4);
+  if (p.g_box) {
+    const long long dg[3] = {s.C, s.V, s.N}, lg[2] = {s.C, io.ldg};
+    if ((rc = map_nd(&mG, io.G, 3, dg, lg, 32, 1, true))) return rc;
+  }
+  p.acc_box = p.acc && (s.want & XENT_DX) && rowwise::rows_16(p.acc, p.ld_acc, 4);
+  if (p.acc_box) {
+    const long long da[3] = {s.C, T, 1}, la[2] = {p.ld_acc, T * p.ld_acc};
+    if ((rc = map_nd(&mAcc, p.acc, 3, da, la, 32, 1, true))) return rc;
+  }
   for (int v0 = 0; v0 < s.V; v0 += w.piece) {
     p.v0 = v0;
     p.w = std::min(w.piece, s.V - v0);
     p.first_piece = v0 == 0;
     p.last_piece = v0 + w.piece >= s.V;
-    rc = two_pairs(p.mt, p.w) ? run_z<PROB, 4>(p, mX2, mW, st) : run_z<PROB, 2>(p, mX, mW, st);
+    const long long lp[2] = {w.piece, T * w.piece}, dps[3] = {w.piece, T, w.np};
+    if ((rc = map_nd(&mPs, w.P, 3, dps, lp, 32, w.np))) return rc;
+    rc = two_pairs(p.mt, p.w) ? run_z<PROB, 4>(p, mX2, mW, mPs, st) : run_z<PROB, 2>(p, mX, mW, mPs, st);
     if (rc) return rc;
     const bool two = two_pairs((s.want & XENT_DX ? p.mt : 0) + (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0), s.C);
-    const long long dp[3] = {p.w, T, w.np}, lp[2] = {w.piece, T * w.piece};
+    const long long dp[3] = {p.w, T, w.np};
     const long long d4[4] = {p.w, s.n_c, s.N, w.np};
     const long long l4[3] = {w.piece, (long long)s.n_c * w.piece, T * w.piece};
     if ((rc = map_nd(&mP, w.P, 3, dp, lp, two ? HALF / 2 : HALF)) || (rc = map_nd(&mP4, w.P, 4, d4, l4, BK)))
       return rc;
-    rc = two ? run_grad<4>(p, s.want, mP, mWt, mP4, mX4, st) : run_grad<2>(p, s.want, mP, mWt, mP4, mX4, st);
+    rc = two ? run_grad<4>(p, s.want, mP, mWt, mP4, mX4, mG, mAcc, st)
+             : run_grad<2>(p, s.want, mP, mWt, mP4, mX4, mG, mAcc, st);
     if (rc) return rc;
   }
   return GC_OK;
