@@ -321,7 +321,7 @@ int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t 
  *   dX[t]       = sum_v P[t][v] W[v]
  *   G[i][v]     = sum_{t in chunk i} P[t][v] X[t]        (chunk i: points [i n_c, (i + 1) n_c)).
  * A point whose label is negative (padding) has row_loss 0 and enters no gradient, whatever its row
- * of X holds; its lse is formed all the same, NaN where the row holds a NaN or an infinity.  A label
+ * of X holds; its lse is formed all the same (not finite where the row is not).  A label
  * >= V is treated so too, and raises GC_ERR_DATA in the status header.  Neither z nor P is kept: both are formed for a piece of the vocabulary at a
  * time (a piece of P is at most about 2^26 values), the products on the tensor cores with fp32 sums.
  * bf16 operands are used as they are, fp32 ones as bf16 hi + lo (2^-17); P enters G as hi + lo, and

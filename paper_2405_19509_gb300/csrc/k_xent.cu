@@ -47,6 +47,7 @@ constexpr long long kSpinX = 1LL << 32;
 constexpr long long kPieceElems = 1LL << 26;  // of P: 256 MB as two bf16 parts
 constexpr float kLog2e = 1.4426950408889634f;
 
+constexpr int kNone = -1, kNoneBad = -2;  // labels that are none, the latter of a row that is not finite
 enum { STAT = 0, PROB = 1, GRAD = 2 };
 // The ring of operand stages and the store boxes of each epilogue warp.
 constexpr int ring_bytes(int mode) { return (mode == PROB ? 10 : 12) * OP_BYTES; }
@@ -62,6 +63,9 @@ struct XentParams {
   int np, np_dx;       // parts of P: kept, and that enter dX
   int mt, nt, group;   // tiles of T and of the columns; row tiles that share a sweep of the columns
   int units;           // clusters; a cluster's tile is 256 x 128 times its CTAs
+  // rows of A that a CTA loads of X's and P's rows, and whether the second half of a tile has any: of a few
+  // points no more than there are (the rows of the accumulator past them hold anything, and are not read)
+  int a_rows, a_both;
   // GRAD: dX tiles, round robin; then G's, `extra` each for the units past the first `r`, which
   // have one dX tile less, and the rest round robin
   int ndx, ct, vt, ndw, r, extra;
@@ -413,7 +417,9 @@ __global__ void __launch_bounds__(kThreadsX, 1)
     for (int k = 0; k < ntiles && ok; ++k) {
       const TileAt t = tile_at<MODE, WIDE>(p, unit, k);
       const int ma = t.m0 + half_m * HALF, nb = t.n0 + q * TILE + half_m * HALF;
-      const uint32_t bytes = (uint32_t)(t.na + t.nb) * OP_BYTES;
+      const bool rows_a = t.kind < 2, skip_a = rows_a && half_m == 1 && !p.a_both;
+      const uint32_t bytes = 2 * t.nb * OP_BYTES + (rows_a ? t.na * p.a_rows * BK * 2 * (p.a_both ? 2 : 1)
+                                                           : 2 * t.na * OP_BYTES);
       for (int kb = 0; kb < t.nkb; ++kb, ++it) {
         if (!mbar_wait(&empty[s], ph ^ 1, abort_flag, p.status, p.spin_limit)) ok = false;
         if (!__all_sync(0xffffffffu, ok)) {
@@ -421,12 +427,13 @@ __global__ void __launch_bounds__(kThreadsX, 1)
           break;
         }
         if (one) {
-          if (half_m == 0) mbar_expect_tx(&full[s], 2 * bytes);
+          if (half_m == 0) mbar_expect_tx(&full[s], bytes);
           const uint32_t bar = at_rank(&full[s], q * 2);
           uint8_t* st = smem + (size_t)s * stage_bytes;
           for (int i = 0; i < t.na; ++i, st += OP_BYTES) {
             uint8_t* dst = st + q * (OP_BYTES / 2);
-            if (t.kind < 2) {
+            if (rows_a) {
+              if (skip_a) continue;
               if (CL == 2)
                 load_3d(st, &mA, kb * BK, ma, i, bar);
               else
@@ -550,7 +557,6 @@ __global__ void __launch_bounds__(kThreadsX, 1)
 // bf16 parts [parts][rows][Cp] of a matrix: hi = bf16(x), lo = bf16(x - hi), zero from C to Cp.  A block
 // a row at a time.  With labels: lab = the label as an int, kNone where there is none.  The products
 // that follow multiply such a row by zeros, so what is not finite in it enters as zero (kNoneBad).
-constexpr int kNone = -1, kNoneBad = -2;
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256)
     k_xent_parts(const T* __restrict__ x, long long ld, long long rows, int C, int Cp, int parts,
@@ -590,6 +596,116 @@ __global__ void __launch_bounds__(256)
   }
 }
 
+// Losses of NT points: the W rows stream once through registers, and a tile of the tensor cores
+// would be nearly empty.  Bound: HBM.  A warp takes four neighbouring rows of W at a time (2 to 16 KB in
+// flight), x lies in shared memory as fp32 in the order in which lanes read it, and the largest value
+// and the sum of exponentials of a warp's rows stay in registers.  One slot of `part` a block.
+// (One point, C = 2048, V = 65536 bf16, 268 MB: 46 us, 5.8 TB/s; the tile kernel 59.)
+constexpr int kFewRows = 4;
+template <typename TX, typename TW, bool VEC, int NT>
+__global__ void __launch_bounds__(256)
+    k_xent_few(const TX* __restrict__ X, long long ldx, const TW* __restrict__ W, long long ldw, int T, int C, int V,
+               const void* __restrict__ y, int y64, int* __restrict__ lab, float* __restrict__ target,
+               float2* __restrict__ part, uint32_t* status) {
+  using namespace rowwise;
+  extern __shared__ __align__(16) float xs[];  // [NT][segments][2][32][4]
+  __shared__ float2 red[8][NT];
+  __shared__ int label[NT];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int nseg = (C + kSeg - 1) / kSeg;
+  for (int i = warp; i < NT * nseg; i += 8) {
+    const int t = i / nseg, seg = i - t * nseg;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    if (t < T) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int c = seg_col<VEC>(seg * kSeg, lane, j);
+        if (c < C) v[j] = to_f(X[t * ldx + c]);
+      }
+    }
+    float4* d = reinterpret_cast<float4*>(xs + (size_t)i * kSeg);
+    d[lane] = make_float4(v[0], v[1], v[2], v[3]);
+    d[32 + lane] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  if (threadIdx.x < NT) {
+    long long l = -1;
+    if ((int)threadIdx.x < T)
+      l = y64 ? reinterpret_cast<const long long*>(y)[threadIdx.x] : reinterpret_cast<const int*>(y)[threadIdx.x];
+    const int at = l >= 0 && l < V ? (int)l : kNone;
+    label[threadIdx.x] = at;
+    if (blockIdx.x == 0 && (int)threadIdx.x < T) {
+      lab[threadIdx.x] = at;
+      if (l >= V) atomicOr(status, ST_BAD_LABEL);
+    }
+  }
+  __syncthreads();
+  float m[NT], s[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    m[t] = -INFINITY;
+    s[t] = 0.f;
+  }
+  const long long step = (long long)gridDim.x * 8 * kFewRows;
+  for (long long v0 = ((long long)blockIdx.x * 8 + warp) * kFewRows; v0 < V; v0 += step) {
+    float z[kFewRows][NT];
+#pragma unroll
+    for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) z[r][t] = 0.f;
+#pragma unroll 2
+    for (int seg = 0; seg < nseg; ++seg) {
+      float w[kFewRows][8];
+#pragma unroll
+      for (int r = 0; r < kFewRows; ++r)
+        load_seg<VEC>(W + min(v0 + r, (long long)V - 1) * ldw, seg * kSeg, lane, C, w[r]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float4* d = reinterpret_cast<const float4*>(xs + (size_t)(t * nseg + seg) * kSeg);
+        const float4 a = d[lane], b = d[32 + lane];
+        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) z[r][t] = fmaf(w[r][j], x[j], z[r][t]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float top = m[t];
+#pragma unroll
+      for (int r = 0; r < kFewRows; ++r) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) z[r][t] += __shfl_xor_sync(0xffffffffu, z[r][t], o);
+        if (v0 + r >= V) z[r][t] = -INFINITY;
+        if (v0 + r == label[t] && lane == 0) target[t] = z[r][t];
+        top = fmaxf(top, z[r][t]);
+      }
+      const float ref = top == -INFINITY ? 0.f : top * kLog2e;
+      s[t] *= ex2(fmaf(m[t], kLog2e, -ref));
+#pragma unroll
+      for (int r = 0; r < kFewRows; ++r) s[t] += ex2(fmaf(z[r][t], kLog2e, -ref));
+      m[t] = top;
+    }
+  }
+  if (lane == 0) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) red[warp][t] = make_float2(m[t], s[t]);
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < T && threadIdx.x < NT) {
+    float M = -INFINITY, S = 0.f;
+    for (int w = 0; w < 8; ++w) {
+      const float2 q = red[w][threadIdx.x];
+      const float top = fmaxf(M, q.x), ref = top == -INFINITY ? 0.f : top;
+      S = S * ex2((M - ref) * kLog2e) + q.y * ex2((q.x - ref) * kLog2e);
+      M = top;
+    }
+    part[(long long)threadIdx.x * gridDim.x + blockIdx.x] = make_float2(M, S);
+  }
+}
+
 // lse and loss of a row from its partial sums: a warp a row.
 __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ part, int n, long long T,
                                                   const int* __restrict__ lab, const float* __restrict__ target,
@@ -600,6 +716,7 @@ __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ par
   if (row >= T) return;
   const float2* p = part + row * n;
   float m = -INFINITY, s = 0.f;
+#pragma unroll 8
   for (int k = lane; k < n; k += 32) {
     const float2 q = __ldg(p + k);
     const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
@@ -728,6 +845,37 @@ int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts
 
 int tiles(long long n, int wide = TILE) { return (int)((n + wide - 1) / wide); }
 
+// The form for few points, and its blocks (all resident: three an SM; each slot of `part` a block).
+// (C = 2048, V = 65536: 54 us for one point, 56 for two; 81 for four, where the tile kernel takes 69.)
+constexpr int kFewPoints = 2;
+constexpr size_t kFewSmem = 64 * 1024;
+bool few_points(long long T, int C) {
+  return T <= kFewPoints && (size_t)T * ((C + rowwise::kSeg - 1) / rowwise::kSeg * rowwise::kSeg) * 4 <= kFewSmem;
+}
+int few_blocks(int V) { return std::min((V + 8 * kFewRows - 1) / (8 * kFewRows), 3 * device_sm_count()); }
+
+template <typename TX, typename TW, bool VEC, int NT>
+int few_go(const XentShape& s, const XentIO& io, int* lab, float* target, float2* part, uint32_t* status,
+           cudaStream_t st) {
+  const size_t smem = (size_t)NT * ((s.C + rowwise::kSeg - 1) / rowwise::kSeg * rowwise::kSeg) * 4;
+  static SmemOptIn allow;
+  GC_CUDA(allow(k_xent_few<TX, TW, VEC, NT>, kFewSmem));
+  k_xent_few<TX, TW, VEC, NT><<<(unsigned)few_blocks(s.V), 256, smem, st>>>(
+      (const TX*)io.X, io.ldx, (const TW*)io.W, io.ldw, s.N * s.n_c, s.C, s.V, io.y, io.y64, lab, target, part, status);
+  count_launches(1);
+  return cuda_check(cudaGetLastError(), "k_xent_few");
+}
+template <typename TX, typename TW>
+int few_by_size(const XentShape& s, const XentIO& io, int* lab, float* target, float2* part, uint32_t* status,
+                cudaStream_t st) {
+  const bool vec = s.C % 8 == 0 && rowwise::rows_16(io.W, io.ldw, sizeof(TW));
+  if (s.N * s.n_c == 1)
+    return vec ? few_go<TX, TW, true, 1>(s, io, lab, target, part, status, st)
+               : few_go<TX, TW, false, 1>(s, io, lab, target, part, status, st);
+  return vec ? few_go<TX, TW, true, 2>(s, io, lab, target, part, status, st)
+             : few_go<TX, TW, false, 2>(s, io, lab, target, part, status, st);
+}
+
 // Columns of a piece: as many as kPieceElems of P allow, the pieces of one width.
 int piece_cols(long long T, int V) {
   const long long most = std::max<long long>(TILE, kPieceElems / T / TILE * TILE);
@@ -737,7 +885,7 @@ int piece_cols(long long T, int V) {
 
 struct XentScratch {
   int Cp, nx, nw, piece, np;
-  bool w_in_place;
+  bool w_in_place, few;
   __nv_bfloat16 *X, *W, *P;
   int* lab;
   float *lse, *target, *row_loss, *acc;
@@ -751,13 +899,16 @@ XentScratch carve_xent(Carve& c, const XentShape& s) {
   w.nx = s.x_dtype == GC_BF16 ? 1 : 2;
   w.nw = s.w_dtype == GC_BF16 ? 1 : 2;
   w.w_in_place = s.w_dtype == GC_BF16 && s.w_16;
-  w.X = c.take<__nv_bfloat16>((size_t)w.nx * T * w.Cp);
-  w.W = w.w_in_place ? nullptr : c.take<__nv_bfloat16>((size_t)w.nw * s.V * w.Cp);
+  w.few = few_points(T, s.C);
+  if (!w.few || s.want) {  // few points' losses take X and W as they are
+    w.X = c.take<__nv_bfloat16>((size_t)w.nx * T * w.Cp);
+    w.W = w.w_in_place ? nullptr : c.take<__nv_bfloat16>((size_t)w.nw * s.V * w.Cp);
+  }
   w.lab = c.take<int>((size_t)T);
   w.lse = c.take<float>((size_t)T);
   w.target = c.take<float>((size_t)T);
   w.row_loss = c.take<float>((size_t)T);
-  w.part = c.take<float2>((size_t)T * 2 * tiles(s.V));
+  w.part = c.take<float2>((size_t)T * (w.few ? few_blocks(s.V) : 2 * tiles(s.V)));
   if (s.want & (XENT_DX | XENT_G)) {
     w.piece = piece_cols(T, s.V);
     w.np = (s.want & XENT_G) || s.x_dtype == GC_F32 ? 2 : 1;
@@ -811,6 +962,18 @@ int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& m
   return launch_mode<GRAD, CL>(mP, mWt, mP4, mX4, mG, mAcc, p, st);
 }
 
+// Rows' log-sum-exp and losses from their partial sums, and the mean.
+int join_rows(const XentScratch& w, int slots, long long T, const XentIO& io, cudaStream_t st) {
+  float* row_loss = io.row_loss ? io.row_loss : io.loss ? w.row_loss : nullptr;
+  k_xent_lse<<<(unsigned)((T + 7) / 8), 256, 0, st>>>(w.part, slots, T, w.lab, w.target, w.lse, io.lse, row_loss);
+  count_launches(1);
+  int rc = cuda_check(cudaGetLastError(), "k_xent_lse");
+  if (rc || !io.loss) return rc;
+  k_xent_loss<<<1, 1024, 0, st>>>(row_loss, T, io.loss);
+  count_launches(1);
+  return cuda_check(cudaGetLastError(), "k_xent_loss");
+}
+
 }  // namespace
 
 size_t xent_ws_bytes(const XentShape& s) {
@@ -823,8 +986,17 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   const XentScratch w = carve_xent(ws, s);
   const long long T = (long long)s.N * s.n_c;
   const bool xb = s.x_dtype == GC_BF16, wb = s.w_dtype == GC_BF16;
-  int rc = xb ? parts_of<__nv_bfloat16>(io.X, io.ldx, T, s.C, w.Cp, 1, io.y, io.y64, s.V, w.lab, w.X, status, st)
-              : parts_of<float>(io.X, io.ldx, T, s.C, w.Cp, 2, io.y, io.y64, s.V, w.lab, w.X, status, st);
+  int rc = GC_OK;
+  if (w.few) {
+    rc = xb ? wb ? few_by_size<__nv_bfloat16, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
+                 : few_by_size<__nv_bfloat16, float>(s, io, w.lab, w.target, w.part, status, st)
+            : wb ? few_by_size<float, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
+                 : few_by_size<float, float>(s, io, w.lab, w.target, w.part, status, st);
+    if (rc) return rc;
+    if (!s.want) return join_rows(w, few_blocks(s.V), T, io, st);
+  }
+  rc = xb ? parts_of<__nv_bfloat16>(io.X, io.ldx, T, s.C, w.Cp, 1, io.y, io.y64, s.V, w.lab, w.X, status, st)
+          : parts_of<float>(io.X, io.ldx, T, s.C, w.Cp, 2, io.y, io.y64, s.V, w.lab, w.X, status, st);
   if (rc) return rc;
   if (!w.w_in_place) {
     rc = wb ? parts_of<__nv_bfloat16>(io.W, io.ldw, s.V, s.C, w.Cp, 1, nullptr, 0, 0, nullptr, w.W, status, st)
@@ -845,6 +1017,8 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.nw = w.nw;
   p.mt = tiles(T);
   p.group = std::min(p.mt, 16);
+  p.a_both = T > HALF;
+  p.a_rows = T > HALF ? HALF : (int)(T + 7) / 8 * 8;
   p.slots = 2 * tiles(s.V);
   p.lab = w.lab;
   p.lse = w.lse;
@@ -859,25 +1033,18 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   {
     const long long dx[3] = {w.Cp, T, w.nx}, lx[2] = {w.Cp, T * w.Cp};
     const long long dw[3] = {Cin, s.V, w.nw}, lw[2] = {ldw, (long long)s.V * ldw};
-    if ((rc = map_nd(&mX, w.X, 3, dx, lx, HALF)) || (rc = map_nd(&mX2, w.X, 3, dx, lx, HALF / 2)) || (rc = map_nd(&mW, W, 3, dw, lw, HALF)) ||
+    if ((rc = map_nd(&mX, w.X, 3, dx, lx, p.a_rows)) || (rc = map_nd(&mX2, w.X, 3, dx, lx, HALF / 2)) || (rc = map_nd(&mW, W, 3, dw, lw, HALF)) ||
         (rc = map_nd(&mWt, W, 3, dw, lw, BK)))
       return rc;
     const long long d4[4] = {w.Cp, s.n_c, s.N, w.nx};
     const long long l4[3] = {w.Cp, (long long)s.n_c * w.Cp, T * w.Cp};
     if ((rc = map_nd(&mX4, w.X, 4, d4, l4, BK))) return rc;
   }
-  rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, mX, st) : run_z<STAT, 2>(p, mX, mW, mX, st);
-  if (rc) return rc;
-  float* row_loss = io.row_loss ? io.row_loss : io.loss ? w.row_loss : nullptr;
-  k_xent_lse<<<(unsigned)((T + 7) / 8), 256, 0, st>>>(w.part, p.slots, T, w.lab, w.target, w.lse, io.lse,
-                                                      row_loss);
-  count_launches(1);
-  if ((rc = cuda_check(cudaGetLastError(), "k_xent_lse"))) return rc;
-  if (io.loss) {
-    k_xent_loss<<<1, 1024, 0, st>>>(row_loss, T, io.loss);
-    count_launches(1);
-    if ((rc = cuda_check(cudaGetLastError(), "k_xent_loss"))) return rc;
+  if (!w.few) {
+    rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, mX, st) : run_z<STAT, 2>(p, mX, mW, mX, st);
+    if (rc) return rc;
   }
+  if ((rc = join_rows(w, w.few ? few_blocks(s.V) : p.slots, T, io, st))) return rc;
   if (!(s.want & (XENT_DX | XENT_G))) return GC_OK;
 
   p.P = w.P;
@@ -912,11 +1079,11 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     if ((rc = map_nd(&mPs, w.P, 3, dps, lp, 32, w.np))) return rc;
     rc = two_pairs(p.mt, p.w) ? run_z<PROB, 4>(p, mX2, mW, mPs, st) : run_z<PROB, 2>(p, mX, mW, mPs, st);
     if (rc) return rc;
-    const bool two = two_pairs((s.want & XENT_DX ? p.mt : 0) + (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0), s.C);
+    const bool two = T > HALF && two_pairs((s.want & XENT_DX ? p.mt : 0) + (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0), s.C);
     const long long dp[3] = {p.w, T, w.np};
     const long long d4[4] = {p.w, s.n_c, s.N, w.np};
     const long long l4[3] = {w.piece, (long long)s.n_c * w.piece, T * w.piece};
-    if ((rc = map_nd(&mP, w.P, 3, dp, lp, two ? HALF / 2 : HALF)) || (rc = map_nd(&mP4, w.P, 4, d4, l4, BK)))
+    if ((rc = map_nd(&mP, w.P, 3, dp, lp, two ? HALF / 2 : p.a_rows)) || (rc = map_nd(&mP4, w.P, 4, d4, l4, BK)))
       return rc;
     rc = two ? run_grad<4>(p, s.want, mP, mWt, mP4, mX4, mG, mAcc, st)
              : run_grad<2>(p, s.want, mP, mWt, mP4, mX4, mG, mAcc, st);

@@ -36,7 +36,7 @@ def test_workspace_keeps_no_logits():
     assert 0 < score < full < 1 << 30
     assert L.gc_softmax_xent_workspace(0, 1, 1, 1, 1, 1, 1, 0) == 0
     # rows off the 16-byte boundaries are copied
-    assert L.gc_softmax_xent_workspace(1, 1, 512, 65536, 1, 1, 0, 0) >= 65536 * 1024
+    assert L.gc_softmax_xent_workspace(1, 9, 512, 65536, 1, 1, 0, 0) >= 65536 * 1024
 
 
 def test_binding_checks():

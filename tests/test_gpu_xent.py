@@ -124,6 +124,41 @@ def test_two_pairs_to_a_cluster(gc, N, n_c, C, V, x, w):
     assert all(torch.equal(got[k], again[k]) for k in got)
 
 
+@pytest.mark.parametrize("x,w", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("layout", ["dense", "ragged"])
+@pytest.mark.parametrize("T,C,V", [(1, 1, 1), (1, 2048, 5000), (2, 300, 33), (3, 1000, 20001), (4, 64, 12000),
+                                   (5, 257, 1000), (8, 520, 4096), (8, 4096, 300), (9, 128, 1000), (1, 16384, 40)])
+def test_few_points(gc, T, C, V, x, w, layout):
+    """One or two points take W as it lies; a few more do not; the same with the gradient asked for."""
+    X, W, y = _data(1, T, C, V, x, w, T + C + V, layout=layout)
+    ref = _reference(X, W, y, 1)
+    ws = gc.Workspace()
+    got = gc.gc_softmax_xent(X, W, y, 1, T, dX=False, G=False, ws=ws)
+    full = gc.gc_softmax_xent(X, W, y.int(), 1, T, ws=ws)
+    gc.gc_status(ws)
+    for k in ("loss", "row_loss", "lse"):
+        _close(got[k], ref[k], k)
+        assert torch.equal(got[k], full[k])
+    for k in ("dX", "G"):
+        _close(full[k], ref[k], k)
+
+
+def test_few_points_labels(gc):
+    X, W, y = _data(1, 4, 96, 700, "bf16", "bf16", 3, ignore=0)
+    want = gc.gc_softmax_xent(X, W, y, 1, 4)
+    y2, X2 = y.clone(), X.clone()
+    y2[1], y2[3] = -7, 700
+    X2[1, 5] = float("nan")
+    ws = gc.Workspace()
+    got = gc.gc_softmax_xent(X2, W, y2, 1, 4, ws=ws)
+    with pytest.raises(gc.GCError) as e:
+        gc.gc_status(ws)
+    assert e.value.code == -7
+    assert torch.equal(got["row_loss"][[0, 2]], want["row_loss"][[0, 2]]) and not got["row_loss"][[1, 3]].any()
+    assert torch.equal(got["dX"][[0, 2]], want["dX"][[0, 2]]) and not got["dX"][[1, 3]].any()
+    assert torch.isfinite(got["G"]).all() and torch.equal(got["lse"][[0, 2, 3]], want["lse"][[0, 2, 3]])
+
+
 def test_reference_is_the_oracle(gc):
     X, W, y = _data(3, 6, 10, 40, "f32", "f32", 1)
     ref = _reference(X, W, y, 3)
