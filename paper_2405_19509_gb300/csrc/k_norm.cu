@@ -32,6 +32,13 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
+// s / n with the quotient of a division where 1 / n is at hand: one correction of s * (1 / n).
+__device__ __forceinline__ float div_by(float s, float n, float inv) {
+  const float q = s * inv;
+  const float r = fmaf(-q, n, s);
+  return isfinite(r) ? fmaf(r, inv, q) : q;
+}
+
 // The eight values at the segment's columns of a per-column vector, `dflt` where there is none.
 template <bool VEC>
 __device__ __forceinline__ void load_cols(const float* p, float dflt, bool vec, int col0, int lane,
@@ -58,37 +65,56 @@ struct NormArgs {
   Mask m;
 };
 
-// TPR threads a row, VPT segments a warp of them.  A warp a row: four rows a block, no barrier.
+// TPR threads a row, VPT segments a warp of them.  A warp a row: four rows a block, no barrier.  With one
+// segment a warp the next row is on its way while this one is worked on, and gamma and beta stay in
+// registers: otherwise every row waits for memory (16,384 rows of 4096 bf16 with dropout and residual,
+// 537 MB: 155 us by four segments a warp and no row ahead).
 template <typename T, bool VEC, int TPR, int VPT>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR)
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / TPR)
     k_norm(NormArgs a) {
   constexpr int WPR = TPR / 32;                       // warps a row
   constexpr int RPB = TPR == 32 ? 4 : 1;              // rows a block
+  constexpr bool AHEAD = VPT == 1;
   __shared__ float2 part[2][WPR];
   const int lane = threadIdx.x & 31;
   const int warp = TPR == 32 ? 0 : threadIdx.x >> 5;
-  int flip = 0;
-  for (long long row = (long long)blockIdx.x * RPB + (TPR == 32 ? threadIdx.x >> 5 : 0); row < a.rows;
-       row += (long long)gridDim.x * RPB, flip ^= 1) {
-    float v[VPT][8];
-    const T* xr = (const T*)a.x + row * a.ldx;
+  const long long step = (long long)gridDim.x * RPB;
+  long long row = (long long)blockIdx.x * RPB + (TPR == 32 ? threadIdx.x >> 5 : 0);
+  float g[8], b[8];
+  RawSeg<VEC, T> x[VPT], r[VPT];
+  int n_w = 0;  // columns of this warp
 #pragma unroll
-    for (int q = 0; q < VPT; ++q) load_seg<VEC>(xr, (q * WPR + warp) * kSeg, lane, a.cols, v[q]);
+  for (int q = 0; q < VPT; ++q) n_w += max(0, min(kSeg, a.cols - (q * WPR + warp) * kSeg));
+  const float inv_w = 1.f / (float)max(n_w, 1), inv = 1.f / (float)a.cols;
+  auto fetch = [&](long long at) {
+#pragma unroll
+    for (int q = 0; q < VPT; ++q) x[q].load((const T*)a.x + at * a.ldx, (q * WPR + warp) * kSeg, lane, a.cols);
     if (a.res) {
-      const T* rr = (const T*)a.res + row * a.ldr;
 #pragma unroll
-      for (int q = 0; q < VPT; ++q) {
-        float r[8];
-        const int col0 = (q * WPR + warp) * kSeg;
-        load_seg<VEC>(rr, col0, lane, a.cols, r);
-        if (a.m.t) drop_seg<VEC>(a.m, row, col0, lane, v[q]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[q][j] += r[j];
-      }
-    } else if (a.m.t) {
-#pragma unroll
-      for (int q = 0; q < VPT; ++q) drop_seg<VEC>(a.m, row, (q * WPR + warp) * kSeg, lane, v[q]);
+      for (int q = 0; q < VPT; ++q) r[q].load((const T*)a.res + at * a.ldr, (q * WPR + warp) * kSeg, lane, a.cols);
     }
+  };
+  if (AHEAD) {
+    load_cols<VEC>(a.gamma, 1.f, a.vec_cols, warp * kSeg, lane, a.cols, g);
+    load_cols<VEC>(a.beta, 0.f, a.vec_cols, warp * kSeg, lane, a.cols, b);
+    if (row < a.rows) fetch(row);
+  }
+  int flip = 0;
+  for (; row < a.rows; row += step, flip ^= 1) {
+    float v[VPT][8];
+    if (!AHEAD) fetch(row);
+#pragma unroll
+    for (int q = 0; q < VPT; ++q) {
+      x[q].values(v[q]);
+      if (a.m.t) drop_seg<VEC>(a.m, row, (q * WPR + warp) * kSeg, lane, v[q]);
+      if (a.res) {
+        float t[8];
+        r[q].values(t);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[q][j] += t[j];
+      }
+    }
+    if (AHEAD && row + step < a.rows) fetch(row + step);
     if (a.h) {
 #pragma unroll
       for (int q = 0; q < VPT; ++q)
@@ -96,23 +122,19 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR)
     }
     // the warp's sum, and its squares about its own mean
     float s = 0.f;
-    int n_w = 0;  // columns of this warp
 #pragma unroll
-    for (int q = 0; q < VPT; ++q) {
-      n_w += max(0, min(kSeg, a.cols - (q * WPR + warp) * kSeg));
+    for (int q = 0; q < VPT; ++q)
 #pragma unroll
       for (int j = 0; j < 8; ++j) s += v[q][j];
-    }
     s = warp_sum(s);
-    const float mu_w = s / (float)max(n_w, 1);
+    const float mu_w = n_w == 0 ? 0.f : div_by(s, (float)n_w, inv_w);
     float m2 = 0.f;
 #pragma unroll
     for (int q = 0; q < VPT; ++q)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int c = seg_col<VEC>((q * WPR + warp) * kSeg, lane, j);
         const float d = v[q][j] - mu_w;
-        if (c < a.cols) m2 = fmaf(d, d, m2);
+        if (in_row<VEC>((q * WPR + warp) * kSeg, lane, j, a.cols)) m2 = fmaf(d, d, m2);
       }
     m2 = warp_sum(m2);
     float mu = mu_w, M2 = m2;
@@ -126,11 +148,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR)
 #pragma unroll
         for (int q = 0; q < VPT; ++q) n_l += max(0, min(kSeg, a.cols - (q * WPR + lane) * kSeg));
       }
-      mu = warp_sum(p.x) / (float)a.cols;
+      mu = div_by(warp_sum(p.x), (float)a.cols, inv);
       const float d = n_l > 0 ? p.x / (float)n_l - mu : 0.f;
       M2 = warp_sum(fmaf((float)n_l * d, d, p.y));
     }
-    const float rstd = rsqrtf(M2 / (float)a.cols + a.eps);
+    const float rstd = rsqrtf(M2 * inv + a.eps);
     if (warp == 0 && lane == 0) {
       if (a.mean) a.mean[row] = mu;
       if (a.rstd) a.rstd[row] = rstd;
@@ -138,9 +160,10 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR)
 #pragma unroll
     for (int q = 0; q < VPT; ++q) {
       const int col0 = (q * WPR + warp) * kSeg;
-      float g[8], b[8];
-      load_cols<VEC>(a.gamma, 1.f, a.vec_cols, col0, lane, a.cols, g);
-      load_cols<VEC>(a.beta, 0.f, a.vec_cols, col0, lane, a.cols, b);
+      if (!AHEAD) {
+        load_cols<VEC>(a.gamma, 1.f, a.vec_cols, col0, lane, a.cols, g);
+        load_cols<VEC>(a.beta, 0.f, a.vec_cols, col0, lane, a.cols, b);
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[q][j] = fmaf((v[q][j] - mu) * rstd, g[j], b[j]);
       store_seg<VEC>((T*)a.y + row * a.ldy, col0, lane, a.cols, v[q]);
@@ -153,27 +176,22 @@ int go_norm(const NormArgs& a, cudaStream_t s) {
   constexpr int RPB = TPR == 32 ? 4 : 1;
   constexpr int threads = TPR == 32 ? 128 : TPR;
   const long long blocks = (a.rows + RPB - 1) / RPB;
-  const long long grid = std::min<long long>(blocks, (long long)device_sm_count() * (2048 / threads));
+  const long long grid = std::min<long long>(blocks, (long long)device_sm_count() * (1024 / threads));
   k_norm<T, VEC, TPR, VPT><<<(unsigned)grid, threads, 0, s>>>(a);
   count_launches(1);
   return cuda_check(cudaGetLastError(), "k_norm");
 }
 
-// Up to 1024 columns a warp a row; wider ones a block, with up to four segments a warp.  Where rows
-// are fewer than SMs (single tokens) a warp takes one segment: latency counts, not registers.
+// One segment a warp up to 8192 columns, 1024 threads an SM; wider rows by four.
 template <typename T, bool VEC>
 int norm_by_width(const NormArgs& a, cudaStream_t s) {
   const int c = a.cols;
   if (c <= 256) return go_norm<T, VEC, 32, 1>(a, s);
-  if (a.rows < device_sm_count() && c <= 8192) {
-    if (c <= 1024) return go_norm<T, VEC, 128, 1>(a, s);
-    return go_norm<T, VEC, 1024, 1>(a, s);
-  }
-  if (c <= 512) return go_norm<T, VEC, 32, 2>(a, s);
-  if (c <= 1024) return go_norm<T, VEC, 32, 4>(a, s);
-  if (c <= 2048) return go_norm<T, VEC, 128, 2>(a, s);
-  if (c <= 4096) return go_norm<T, VEC, 128, 4>(a, s);
-  if (c <= 8192) return go_norm<T, VEC, 256, 4>(a, s);
+  if (c <= 512) return go_norm<T, VEC, 64, 1>(a, s);
+  if (c <= 1024) return go_norm<T, VEC, 128, 1>(a, s);
+  if (c <= 2048) return go_norm<T, VEC, 256, 1>(a, s);
+  if (c <= 4096) return go_norm<T, VEC, 512, 1>(a, s);
+  if (c <= 8192) return go_norm<T, VEC, 1024, 1>(a, s);
   return go_norm<T, VEC, 1024, 4>(a, s);
 }
 
@@ -190,56 +208,60 @@ struct NormGradArgs {
   Mask m;
 };
 
-// TPR threads a row, VPT segments a warp of them; a block takes a slice of a chunk's rows.  SUMS: the
-// column sums for G as well.
-template <typename T, bool VEC, int TPR, int VPT, bool SUMS>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR)
+// TPR threads a row, one segment a warp; a block takes a slice of a chunk's rows, the next one on its way
+// while one is worked on.  SUMS: the column sums for G as well.  (16,384 rows of 4096 bf16 with dropout
+// and residual, 671 MB: 168 us with no row ahead.)
+template <typename T, bool VEC, int TPR, bool SUMS>
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / TPR)
     k_norm_grad(NormGradArgs a) {
   constexpr int WPR = TPR / 32;
   constexpr int RPB = TPR == 32 ? 4 : 1;
   __shared__ float2 part[2][WPR];
   const int lane = threadIdx.x & 31;
   const int warp = TPR == 32 ? 0 : threadIdx.x >> 5;
+  const int col0 = warp * kSeg;
   const int chunk = blockIdx.x / a.slices, slice = blockIdx.x - chunk * a.slices;
   const int r_end = min(a.n_c, (slice + 1) * a.rows_per_slice);
-  float sg[SUMS ? VPT : 1][8], sb[SUMS ? VPT : 1][8];
+  int r = slice * a.rows_per_slice + (TPR == 32 ? threadIdx.x >> 5 : 0);
+  const long long first = (long long)chunk * a.n_c;
+  float sg[8], sb[8], g[8];
 #pragma unroll
-  for (int q = 0; q < (SUMS ? VPT : 1); ++q)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sg[q][j] = sb[q][j] = 0.f;
+  for (int j = 0; j < 8; ++j) sg[j] = sb[j] = 0.f;
+  load_cols<VEC>(a.gamma, 1.f, a.vec_cols, col0, lane, a.cols, g);
   const float inv = 1.f / (float)a.cols;
+  RawSeg<VEC, T> xd, xh, xa;
+  float mu, rstd;
+  auto fetch = [&](long long row) {
+    mu = __ldg(a.mean + row);
+    rstd = __ldg(a.rstd + row);
+    xd.load((const T*)a.dy + row * a.lddy, col0, lane, a.cols);
+    xh.load((const T*)a.h + row * a.ldh, col0, lane, a.cols);
+    if (a.dh) xa.load((const T*)a.dh + row * a.lddh, col0, lane, a.cols);
+  };
+  if (r < r_end) fetch(first + r);
   int flip = 0;
-  for (int r = slice * a.rows_per_slice + (TPR == 32 ? threadIdx.x >> 5 : 0); r < r_end; r += RPB, flip ^= 1) {
-    const long long row = (long long)chunk * a.n_c + r;
-    const float mu = __ldg(a.mean + row), rstd = __ldg(a.rstd + row);
-    float d[VPT][8], n[VPT][8];
+  for (; r < r_end; r += RPB, flip ^= 1) {
+    const long long row = first + r;
+    float d[8], n[8];
     float c1 = 0.f, c2 = 0.f;
+    xd.values(d);
+    xh.values(n);
+    const RawSeg<VEC, T> ya = xa;
+    const float scale = rstd;
 #pragma unroll
-    for (int q = 0; q < VPT; ++q) {
-      const int col0 = (q * WPR + warp) * kSeg;
-      load_seg<VEC>((const T*)a.dy + row * a.lddy, col0, lane, a.cols, d[q]);
-      load_seg<VEC>((const T*)a.h + row * a.ldh, col0, lane, a.cols, n[q]);
-    }
-#pragma unroll
-    for (int q = 0; q < VPT; ++q) {
-      const int col0 = (q * WPR + warp) * kSeg;
-      float g[8];
-      load_cols<VEC>(a.gamma, 1.f, a.vec_cols, col0, lane, a.cols, g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        n[q][j] = (n[q][j] - mu) * rstd;
-        if (SUMS) {
-          sg[q][j] = fmaf(d[q][j], n[q][j], sg[q][j]);
-          sb[q][j] += d[q][j];
-        }
-        const int c = seg_col<VEC>(col0, lane, j);
-        d[q][j] *= g[j];
-        if (c < a.cols) {  // past the row's end n is not zero
-          c1 += d[q][j];
-          c2 = fmaf(d[q][j], n[q][j], c2);
-        }
+    for (int j = 0; j < 8; ++j) {
+      n[j] = (n[j] - mu) * scale;
+      if (SUMS) {
+        sg[j] = fmaf(d[j], n[j], sg[j]);
+        sb[j] += d[j];
+      }
+      d[j] *= g[j];
+      if (in_row<VEC>(col0, lane, j, a.cols)) {  // past the row's end n is not zero
+        c1 += d[j];
+        c2 = fmaf(d[j], n[j], c2);
       }
     }
+    if (r + RPB < r_end) fetch(row + RPB);
     c1 = warp_sum(c1);
     c2 = warp_sum(c2);
     if (WPR > 1) {
@@ -251,52 +273,42 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR)
     }
     c1 *= inv;
     c2 *= inv;
+    float t[8];
+    if (a.dh) ya.values(t);
 #pragma unroll
-    for (int q = 0; q < VPT; ++q) {
-      const int col0 = (q * WPR + warp) * kSeg;
-      float t[8];
-      if (a.dh) load_seg<VEC>((const T*)a.dh + row * a.lddh, col0, lane, a.cols, t);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float g = rstd * (d[q][j] - c1 - n[q][j] * c2);
-        d[q][j] = a.dh ? g + t[j] : g;
-      }
-      if (a.dres) store_seg<VEC>((T*)a.dres + row * a.lddr, col0, lane, a.cols, d[q]);
-      if (a.dx) {
-        if (a.m.t) drop_seg<VEC>(a.m, row, col0, lane, d[q]);
-        store_seg<VEC>((T*)a.dx + row * a.lddx, col0, lane, a.cols, d[q]);
-      }
+    for (int j = 0; j < 8; ++j) {
+      const float v = scale * (d[j] - c1 - n[j] * c2);
+      d[j] = a.dh ? v + t[j] : v;
+    }
+    if (a.dres) store_seg<VEC>((T*)a.dres + row * a.lddr, col0, lane, a.cols, d);
+    if (a.dx) {
+      if (a.m.t) drop_seg<VEC>(a.m, row, col0, lane, d);
+      store_seg<VEC>((T*)a.dx + row * a.lddx, col0, lane, a.cols, d);
     }
   }
   if (!SUMS) return;
   // the block's column sums; where a warp takes a row, the four warps' in order
   float* out = a.sums + (size_t)blockIdx.x * a.sums_ld;
   if constexpr (TPR == 32) {
-    __shared__ float acc[4][VPT * kSeg];
+    __shared__ float acc[4][kSeg];
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-      const int w = threadIdx.x >> 5;
       __syncthreads();
 #pragma unroll
-      for (int q = 0; q < (SUMS ? VPT : 1); ++q)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          acc[w][seg_col<VEC>(q * kSeg, lane, j)] = which ? sb[q][j] : sg[q][j];
+      for (int j = 0; j < 8; ++j) acc[threadIdx.x >> 5][seg_col<VEC>(0, lane, j)] = which ? sb[j] : sg[j];
       __syncthreads();
       for (int c = threadIdx.x; c < a.cols; c += 128)
         out[(size_t)which * a.cols + c] = acc[0][c] + acc[1][c] + acc[2][c] + acc[3][c];
     }
   } else {
 #pragma unroll
-    for (int q = 0; q < (SUMS ? VPT : 1); ++q)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = seg_col<VEC>((q * WPR + warp) * kSeg, lane, j);
-        if (c < a.cols) {
-          out[c] = sg[q][j];
-          out[(size_t)a.cols + c] = sb[q][j];
-        }
+    for (int j = 0; j < 8; ++j) {
+      const int c = seg_col<VEC>(col0, lane, j);
+      if (c < a.cols) {
+        out[c] = sg[j];
+        out[(size_t)a.cols + c] = sb[j];
       }
+    }
   }
 }
 
@@ -394,8 +406,12 @@ __global__ void __launch_bounds__(256) k_norm_grad_reduce(const float* __restric
   }
 }
 
-// Threads a row of the fused form (one segment a warp, two for a warp a row).
-int grad_tpr(int cols) { return cols <= 512 ? 32 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024; }
+// Threads a row of the fused form: one segment a warp.
+int grad_tpr(int cols) {
+  int t = 32;
+  while (t * 8 < cols) t *= 2;
+  return t;
+}
 
 struct Slices {
   int count, rows;
@@ -415,22 +431,23 @@ Slices grad_slices(int N, int n_c, int cols) {
   return slices_of(N, n_c, tpr == 32 ? 128 : tpr, tpr == 32 ? 16 : 4);
 }
 
-template <typename T, bool VEC, int TPR, int VPT, bool SUMS>
+template <typename T, bool VEC, int TPR, bool SUMS>
 int go_grad(const NormGradArgs& a, int N, cudaStream_t s) {
-  k_norm_grad<T, VEC, TPR, VPT, SUMS><<<(unsigned)(N * a.slices), TPR == 32 ? 128 : TPR, 0, s>>>(a);
+  k_norm_grad<T, VEC, TPR, SUMS><<<(unsigned)(N * a.slices), TPR == 32 ? 128 : TPR, 0, s>>>(a);
   count_launches(1);
   return cuda_check(cudaGetLastError(), "k_norm_grad");
 }
 
 template <typename T, bool VEC, bool SUMS>
 int grad_by_width(const NormGradArgs& a, int N, cudaStream_t s) {
-  const int c = a.cols;
-  if (c <= 256) return go_grad<T, VEC, 32, 1, SUMS>(a, N, s);
-  if (c <= 512) return go_grad<T, VEC, 32, 2, SUMS>(a, N, s);
-  if (c <= 1024) return go_grad<T, VEC, 128, 1, SUMS>(a, N, s);
-  if (c <= 2048) return go_grad<T, VEC, 256, 1, SUMS>(a, N, s);
-  if (c <= 4096) return go_grad<T, VEC, 512, 1, SUMS>(a, N, s);
-  return go_grad<T, VEC, 1024, 1, SUMS>(a, N, s);
+  switch (grad_tpr(a.cols)) {
+    case 32: return go_grad<T, VEC, 32, SUMS>(a, N, s);
+    case 64: return go_grad<T, VEC, 64, SUMS>(a, N, s);
+    case 128: return go_grad<T, VEC, 128, SUMS>(a, N, s);
+    case 256: return go_grad<T, VEC, 256, SUMS>(a, N, s);
+    case 512: return go_grad<T, VEC, 512, SUMS>(a, N, s);
+    default: return go_grad<T, VEC, 1024, SUMS>(a, N, s);
+  }
 }
 
 template <typename T>

@@ -27,35 +27,67 @@ __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// The segment at col0 of a row; zeros past its end.
+// The segment at col0 of a row as it lies in memory, and its values (zeros past the row's end): a load
+// may be issued long before its values are wanted.
 template <bool VEC, typename T>
-__device__ __forceinline__ void load_seg(const T* row, int col0, int lane, int cols, float (&v)[8]) {
-  if (VEC) {
+struct RawSeg;
+template <>
+struct RawSeg<true, __nv_bfloat16> {
+  uint4 q;
+  __device__ __forceinline__ void load(const __nv_bfloat16* row, int col0, int lane, int cols) {
     const int c = col0 + lane * 8;
-    if (c >= cols) {
+    q = c < cols ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    } else if (sizeof(T) == 2) {
-      const uint4 q = *reinterpret_cast<const uint4*>(row + c);
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[2 * j] = __uint_as_float(w[j] << 16);
-        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-      }
-    } else {
-      const float4 a = *reinterpret_cast<const float4*>(row + c);
-      const float4 b = *reinterpret_cast<const float4*>(row + c + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = __uint_as_float(w[j] << 16);
+      v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
     }
-  } else {
+  }
+};
+template <>
+struct RawSeg<true, float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* row, int col0, int lane, int cols) {
+    const int c = col0 + lane * 8;
+    a = b = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < cols) {
+      a = *reinterpret_cast<const float4*>(row + c);
+      b = *reinterpret_cast<const float4*>(row + c + 4);
+    }
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+};
+template <typename T>
+struct RawSeg<false, T> {
+  T x[8];
+  __device__ __forceinline__ void load(const T* row, int col0, int lane, int cols) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int c = col0 + j * 32 + lane;
-      v[j] = c < cols ? to_f(row[c]) : 0.f;
+      x[j] = c < cols ? row[c] : from_f<T>(0.f);
     }
   }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = to_f(x[j]);
+  }
+};
+template <bool VEC, typename T>
+__device__ __forceinline__ void load_seg(const T* row, int col0, int lane, int cols, float (&v)[8]) {
+  RawSeg<VEC, T> r;
+  r.load(row, col0, lane, cols);
+  r.values(v);
+}
+// Whether value j of the segment is a column of the row: all of a lane's eight are, or none, when VEC.
+template <bool VEC>
+__device__ __forceinline__ bool in_row(int col0, int lane, int j, int cols) {
+  return VEC ? col0 + lane * 8 < cols : col0 + j * 32 + lane < cols;
 }
 
 template <bool VEC, typename T>
@@ -90,7 +122,8 @@ __device__ __forceinline__ void store_seg(T* row, int col0, int lane, int cols, 
 // offset) under the key `seed`: a function of the point and the column alone, so that every worker
 // that holds a point draws the same mask, whatever rows it works on.
 struct Mask {
-  uint32_t k0, k1, c2, c3;
+  uint32_t k[20];   // the rounds' keys
+  uint32_t c2, c3;
   uint32_t t;       // drop below, of 2^16; 0: nothing is dropped
   float scale;      // 2^16 / (2^16 - t)
   long long row0;   // point of the first row
@@ -102,17 +135,14 @@ __device__ __forceinline__ void philox(const Mask& m, unsigned long long e, uint
   x[1] = (uint32_t)(e >> 32);
   x[2] = m.c2;
   x[3] = m.c3;
-  uint32_t k0 = m.k0, k1 = m.k1;
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const unsigned long long a = (unsigned long long)x[0] * 0xD2511F53u;
     const unsigned long long b = (unsigned long long)x[2] * 0xCD9E8D57u;
-    x[0] = (uint32_t)(b >> 32) ^ x[1] ^ k0;
+    x[0] = (uint32_t)(b >> 32) ^ x[1] ^ m.k[2 * r];
     x[1] = (uint32_t)b;
-    x[2] = (uint32_t)(a >> 32) ^ x[3] ^ k1;
+    x[2] = (uint32_t)(a >> 32) ^ x[3] ^ m.k[2 * r + 1];
     x[3] = (uint32_t)a;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
   }
 }
 
@@ -152,8 +182,10 @@ inline Mask make_mask(double p, uint64_t seed, uint64_t offset, int64_t row0, in
   if (t > 65535) t = 65535;
   m.t = (uint32_t)t;
   m.scale = 65536.f / (float)(65536 - t);
-  m.k0 = (uint32_t)seed;
-  m.k1 = (uint32_t)(seed >> 32);
+  for (int r = 0; r < 10; ++r) {
+    m.k[2 * r] = (uint32_t)seed + (uint32_t)r * 0x9E3779B9u;
+    m.k[2 * r + 1] = (uint32_t)(seed >> 32) + (uint32_t)r * 0xBB67AE85u;
+  }
   m.c2 = (uint32_t)offset;
   m.c3 = (uint32_t)(offset >> 32);
   m.row0 = row0;
