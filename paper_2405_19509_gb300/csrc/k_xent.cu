@@ -156,6 +156,19 @@ __device__ __forceinline__ float ex2(float x) {
   return r;
 }
 
+// v[at] for an index that is not known beforehand: a tree of selections (an indexed array of registers
+// would go through local memory with all its values).
+__device__ __forceinline__ float pick(const float (&v)[64], int at) {
+  float w[32];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) w[j] = at & 32 ? v[j + 32] : v[j];
+#pragma unroll
+  for (int h = 16; h; h >>= 1)
+#pragma unroll
+    for (int j = 0; j < h; ++j) w[j] = at & h ? w[j + h] : w[j];
+  return w[0];
+}
+
 // 32 consecutive fp32 values of a row of an output; n: how many of them exist.
 template <typename T>
 __device__ __forceinline__ void store_row(T* dst, const float (&v)[32], int n, bool vec) {
@@ -223,32 +236,29 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
     const bool rv = row_in < p.T;
     const int lab = rv ? __ldg(p.lab + row_in) : -1;
     float m = -INFINITY, s = 0.f;
-    for (int c = 0; c < HALF / 32; ++c) {
-      float v[32];
+#pragma unroll 1
+    for (int c = 0; c < HALF / 64; ++c) {
+      float v[64];
       __syncwarp();
-      tmem_ld32(taddr + (uint32_t)(c * 32), v);
-      const int col = t.n0 + half * HALF + c * 32;
+      tmem_ld64(taddr + (uint32_t)(c * 64), v);
+      const int col = t.n0 + half * HALF + c * 64;
       const int n = p.V - col;
-      if (n < 32) {
+      if (n < 64) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
+        for (int j = 0; j < 64; ++j)
           if (j >= n) v[j] = -INFINITY;
       }
-      if (lab >= col && lab < col + 32) {
-        float z = 0.f;
+      if (lab >= col && lab < col + 64) p.target[row_in] = pick(v, lab - col);
+      float top[4] = {m, v[0], v[1], v[2]};
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (j == lab - col) z = v[j];
-        p.target[row_in] = z;
-      }
-      float top = m;
+      for (int j = 3; j < 64; ++j) top[j % 4] = fmaxf(top[j % 4], v[j]);
+      const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      const float ref = most == -INFINITY ? 0.f : most * kLog2e;
+      float e[4] = {s * ex2(fmaf(m, kLog2e, -ref)), 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < 32; ++j) top = fmaxf(top, v[j]);
-      const float ref = top == -INFINITY ? 0.f : top * kLog2e;
-      s *= ex2(fmaf(m, kLog2e, -ref));
-#pragma unroll
-      for (int j = 0; j < 32; ++j) s += ex2(fmaf(v[j], kLog2e, -ref));
-      m = top;
+      for (int j = 0; j < 64; ++j) e[j % 4] += ex2(fmaf(v[j], kLog2e, -ref));
+      s = (e[0] + e[1]) + (e[2] + e[3]);
+      m = most;
     }
     if (rv && t.n0 < p.V) p.part[row_in * p.slots + t.n0 / HALF + half] = make_float2(m, s);
   } else if (MODE == PROB) {
