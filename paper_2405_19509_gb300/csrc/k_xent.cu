@@ -150,6 +150,11 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
   return t;
 }
 
+// The kernels of a call are a chain, each launched while the one before it runs (programmatic dependent
+// launches): a kernel lets the next one start, and touches nothing that another wrote before wait_prior().
+__device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_prior() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ float ex2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -416,6 +421,8 @@ __global__ void __launch_bounds__(kThreadsX, 1)
   cluster_wait();
   fence_after();
   const uint32_t tmem_base = *tmem_holder;
+  start_next();
+  wait_prior();
   const int ntiles = tiles_of<MODE>(p, unit);
 
   if (warp == 0) {
@@ -574,6 +581,8 @@ __global__ void __launch_bounds__(256)
                  __nv_bfloat16* __restrict__ out, uint32_t* status) {
   using namespace rowwise;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  start_next();
+  wait_prior();
   for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
     long long l = 0;
     if (y) l = y64 ? reinterpret_cast<const long long*>(y)[row] : reinterpret_cast<const int*>(y)[row];
@@ -623,6 +632,8 @@ __global__ void __launch_bounds__(256)
   __shared__ int label[NT];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int nseg = (C + kSeg - 1) / kSeg;
+  start_next();
+  wait_prior();
   for (int i = warp; i < NT * nseg; i += 8) {
     const int t = i / nseg, seg = i - t * nseg;
     float v[8];
@@ -723,6 +734,8 @@ __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ par
                                                   float* __restrict__ row_loss) {
   const int lane = threadIdx.x & 31;
   const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  start_next();
+  wait_prior();
   if (row >= T) return;
   const float2* p = part + row * n;
   float m = -INFINITY, s = 0.f;
@@ -752,6 +765,8 @@ __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ par
 __global__ void __launch_bounds__(1024) k_xent_loss(const float* __restrict__ row_loss, long long T,
                                                     double* __restrict__ loss) {
   __shared__ double acc[32];
+  start_next();
+  wait_prior();
   double s = 0.0;
   for (long long i = threadIdx.x; i < T; i += 1024) s += (double)row_loss[i];
 #pragma unroll
@@ -794,6 +809,33 @@ int map_nd(CUtensorMap* map, const void* base, int rank, const long long* dims, 
   return r == CUDA_SUCCESS ? GC_OK : fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
+// A launch with clusters of `cl` CTAs (1: none); `chained`: as a dependent of the call's kernel before it.
+template <typename... P, typename... A>
+int launch_chain(void (*kern)(P...), const char* name, unsigned grid, int block, size_t smem, int cl, bool chained,
+                 cudaStream_t s, A... args) {
+  cudaLaunchAttribute at[2];
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3((unsigned)block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = at;
+  if (cl > 1) {
+    at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    at[cfg.numAttrs].val.clusterDim.x = (unsigned)cl;
+    at[cfg.numAttrs].val.clusterDim.y = at[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  if (chained) {
+    at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+    ++cfg.numAttrs;
+  }
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+  count_launches(1);
+  return cuda_check(e, name);
+}
+
 // Clusters of CL CTAs that the current device holds at once.
 template <int MODE, int CL>
 int resident(int* units) {
@@ -825,32 +867,17 @@ int resident(int* units) {
 template <int MODE, int CL>
 int launch_mode(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d,
                 const CUtensorMap& out, const CUtensorMap& acc, const XentParams& p, cudaStream_t s) {
-  cudaLaunchAttribute at[1];
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(CL * p.units));
-  cfg.blockDim = dim3(kThreadsX);
-  cfg.dynamicSmemBytes = smem_bytes(MODE);
-  cfg.stream = s;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = CL;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_xent<MODE, CL>, a, b, c, d, out, acc, p);
-  count_launches(1);
-  return cuda_check(e, "k_xent");
+  return launch_chain(k_xent<MODE, CL>, "k_xent", (unsigned)(CL * p.units), kThreadsX, smem_bytes(MODE), CL, true, s,
+                      a, b, c, d, out, acc, p);
 }
 
 template <typename T>
 int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts, const void* y, int y64, int V,
-             int* lab, __nv_bfloat16* out, uint32_t* status, cudaStream_t s) {
+             int* lab, __nv_bfloat16* out, uint32_t* status, bool chained, cudaStream_t s) {
   const unsigned grid = (unsigned)std::min<long long>(rows, 8LL * device_sm_count());
-  if (C % 8 == 0 && rowwise::rows_16(x, ld, sizeof(T)))
-    k_xent_parts<T, true><<<grid, 256, 0, s>>>((const T*)x, ld, rows, C, Cp, parts, y, y64, V, lab, out, status);
-  else
-    k_xent_parts<T, false><<<grid, 256, 0, s>>>((const T*)x, ld, rows, C, Cp, parts, y, y64, V, lab, out, status);
-  count_launches(1);
-  return cuda_check(cudaGetLastError(), "k_xent_parts");
+  auto* kern = C % 8 == 0 && rowwise::rows_16(x, ld, sizeof(T)) ? k_xent_parts<T, true> : k_xent_parts<T, false>;
+  return launch_chain(kern, "k_xent_parts", grid, 256, 0, 1, chained, s, (const T*)x, (long long)ld, rows, C, Cp, parts,
+                      y, y64, V, lab, out, status);
 }
 
 int tiles(long long n, int wide = TILE) { return (int)((n + wide - 1) / wide); }
@@ -870,10 +897,9 @@ int few_go(const XentShape& s, const XentIO& io, int* lab, float* target, float2
   const size_t smem = (size_t)NT * ((s.C + rowwise::kSeg - 1) / rowwise::kSeg * rowwise::kSeg) * 4;
   static SmemOptIn allow;
   GC_CUDA(allow(k_xent_few<TX, TW, VEC, NT>, kFewSmem));
-  k_xent_few<TX, TW, VEC, NT><<<(unsigned)few_blocks(s.V), 256, smem, st>>>(
-      (const TX*)io.X, io.ldx, (const TW*)io.W, io.ldw, s.N * s.n_c, s.C, s.V, io.y, io.y64, lab, target, part, status);
-  count_launches(1);
-  return cuda_check(cudaGetLastError(), "k_xent_few");
+  return launch_chain(k_xent_few<TX, TW, VEC, NT>, "k_xent_few", (unsigned)few_blocks(s.V), 256, smem, 1, false, st,
+                      (const TX*)io.X, (long long)io.ldx, (const TW*)io.W, (long long)io.ldw, s.N * s.n_c, s.C, s.V,
+                      io.y, io.y64, lab, target, part, status);
 }
 template <typename TX, typename TW>
 int few_by_size(const XentShape& s, const XentIO& io, int* lab, float* target, float2* part, uint32_t* status,
@@ -975,13 +1001,10 @@ int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& m
 // Rows' log-sum-exp and losses from their partial sums, and the mean.
 int join_rows(const XentScratch& w, int slots, long long T, const XentIO& io, cudaStream_t st) {
   float* row_loss = io.row_loss ? io.row_loss : io.loss ? w.row_loss : nullptr;
-  k_xent_lse<<<(unsigned)((T + 7) / 8), 256, 0, st>>>(w.part, slots, T, w.lab, w.target, w.lse, io.lse, row_loss);
-  count_launches(1);
-  int rc = cuda_check(cudaGetLastError(), "k_xent_lse");
+  const int rc = launch_chain(k_xent_lse, "k_xent_lse", (unsigned)((T + 7) / 8), 256, 0, 1, true, st, w.part, slots, T,
+                              w.lab, w.target, w.lse, io.lse, row_loss);
   if (rc || !io.loss) return rc;
-  k_xent_loss<<<1, 1024, 0, st>>>(row_loss, T, io.loss);
-  count_launches(1);
-  return cuda_check(cudaGetLastError(), "k_xent_loss");
+  return launch_chain(k_xent_loss, "k_xent_loss", 1, 1024, 0, 1, true, st, row_loss, T, io.loss);
 }
 
 }  // namespace
@@ -1005,12 +1028,12 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     if (rc) return rc;
     if (!s.want) return join_rows(w, few_blocks(s.V), T, io, st);
   }
-  rc = xb ? parts_of<__nv_bfloat16>(io.X, io.ldx, T, s.C, w.Cp, 1, io.y, io.y64, s.V, w.lab, w.X, status, st)
-          : parts_of<float>(io.X, io.ldx, T, s.C, w.Cp, 2, io.y, io.y64, s.V, w.lab, w.X, status, st);
+  rc = xb ? parts_of<__nv_bfloat16>(io.X, io.ldx, T, s.C, w.Cp, 1, io.y, io.y64, s.V, w.lab, w.X, status, w.few, st)
+          : parts_of<float>(io.X, io.ldx, T, s.C, w.Cp, 2, io.y, io.y64, s.V, w.lab, w.X, status, w.few, st);
   if (rc) return rc;
   if (!w.w_in_place) {
-    rc = wb ? parts_of<__nv_bfloat16>(io.W, io.ldw, s.V, s.C, w.Cp, 1, nullptr, 0, 0, nullptr, w.W, status, st)
-            : parts_of<float>(io.W, io.ldw, s.V, s.C, w.Cp, 2, nullptr, 0, 0, nullptr, w.W, status, st);
+    rc = wb ? parts_of<__nv_bfloat16>(io.W, io.ldw, s.V, s.C, w.Cp, 1, nullptr, 0, 0, nullptr, w.W, status, true, st)
+            : parts_of<float>(io.W, io.ldw, s.V, s.C, w.Cp, 2, nullptr, 0, 0, nullptr, w.W, status, true, st);
     if (rc) return rc;
   }
   const void* W = w.w_in_place ? io.W : w.W;
