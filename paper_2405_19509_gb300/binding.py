@@ -154,18 +154,17 @@ def _rows(t, dtype, name, shape):
     """(device pointer, row stride) of a CUDA matrix whose rows may lie apart (None -> NULL, 0)."""
     if t is None:
         return None, 0
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == shape:
+        ld, one = t.stride()
+        if (one == 1 or shape[1] <= 1) and (ld >= shape[1] or shape[0] <= 1):
+            return t.data_ptr(), ld
+        raise ValueError(f"the rows of {name} overlap" if one == 1 or shape[1] <= 1 else
+                         f"the elements of a row of {name} must lie next to each other")
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    ld, one = t.stride()
-    if one != 1 and shape[1] > 1:
-        raise ValueError(f"the elements of a row of {name} must lie next to each other")
-    if ld < shape[1] and shape[0] > 1:
-        raise ValueError(f"the rows of {name} overlap")
-    return t.data_ptr(), ld
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
 def _elt(t, name):
@@ -339,7 +338,10 @@ def gc_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, p:
         mean = torch.empty(rows, dtype=torch.float32, device=dev)
     if rstd is True:
         rstd = torch.empty(rows, dtype=torch.float32, device=dev)
-    mean, rstd = (t if isinstance(t, torch.Tensor) else None for t in (mean, rstd))
+    if not isinstance(mean, torch.Tensor):
+        mean = None
+    if not isinstance(rstd, torch.Tensor):
+        rstd = None
     xp, ldx = _rows(x, x.dtype, "x", x.shape)
     rp, ldr = _rows(residual, x.dtype, "residual", x.shape)
     yp, ldy = _rows(y, x.dtype, "y", x.shape)

@@ -615,115 +615,105 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// Losses of NT points: the W rows stream once through registers, and a tile of the tensor cores
-// would be nearly empty.  Bound: HBM.  A warp takes four neighbouring rows of W at a time (2 to 16 KB in
-// flight), x lies in shared memory as fp32 in the order in which lanes read it, and the largest value
-// and the sum of exponentials of a warp's rows stay in registers.  One slot of `part` a block.
-// (One point, C = 2048, V = 65536 bf16, 268 MB: 46 us, 5.8 TB/s; the tile kernel 59.)
+// The loss of one point: the W rows stream once through registers, where a tile of the tensor cores
+// would be nearly empty.  Bound: HBM.  A warp takes four neighbouring rows of W at a time, with the next two
+// segments of them on their way; x lies in shared memory as fp32 in the order in which lanes read it,
+// and the largest value and the sum of exponentials of a warp's rows stay in registers.  One slot of
+// `part` a block.  (C = 2048, V = 65536 bf16, 268 MB: 46 us, 5.8 TB/s; 58 with the loads of a segment
+// issued when it is wanted; the tile kernel 54 for any number of points up to 256, and two points here 65.)
 constexpr int kFewRows = 4;
-template <typename TX, typename TW, bool VEC, int NT>
+template <typename TX, typename TW, bool VEC>
 __global__ void __launch_bounds__(256)
-    k_xent_few(const TX* __restrict__ X, long long ldx, const TW* __restrict__ W, long long ldw, int T, int C, int V,
+    k_xent_one(const TX* __restrict__ X, const TW* __restrict__ W, long long ldw, int C, int V,
                const void* __restrict__ y, int y64, int* __restrict__ lab, float* __restrict__ target,
                float2* __restrict__ part, uint32_t* status) {
   using namespace rowwise;
-  extern __shared__ __align__(16) float xs[];  // [NT][segments][2][32][4]
-  __shared__ float2 red[8][NT];
-  __shared__ int label[NT];
+  extern __shared__ __align__(16) float xs[];  // [segments][2][32][4]
+  __shared__ float2 red[8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int nseg = (C + kSeg - 1) / kSeg;
   start_next();
   wait_prior();
-  for (int i = warp; i < NT * nseg; i += 8) {
-    const int t = i / nseg, seg = i - t * nseg;
+  for (int seg = warp; seg < nseg; seg += 8) {
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    if (t < T) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = seg_col<VEC>(seg * kSeg, lane, j);
-        if (c < C) v[j] = to_f(X[t * ldx + c]);
-      }
+    for (int j = 0; j < 8; ++j) {
+      const int c = seg_col<VEC>(seg * kSeg, lane, j);
+      v[j] = c < C ? to_f(X[c]) : 0.f;
     }
-    float4* d = reinterpret_cast<float4*>(xs + (size_t)i * kSeg);
+    float4* d = reinterpret_cast<float4*>(xs + (size_t)seg * kSeg);
     d[lane] = make_float4(v[0], v[1], v[2], v[3]);
     d[32 + lane] = make_float4(v[4], v[5], v[6], v[7]);
   }
-  if (threadIdx.x < NT) {
-    long long l = -1;
-    if ((int)threadIdx.x < T)
-      l = y64 ? reinterpret_cast<const long long*>(y)[threadIdx.x] : reinterpret_cast<const int*>(y)[threadIdx.x];
-    const int at = l >= 0 && l < V ? (int)l : kNone;
-    label[threadIdx.x] = at;
-    if (blockIdx.x == 0 && (int)threadIdx.x < T) {
-      lab[threadIdx.x] = at;
-      if (l >= V) atomicOr(status, ST_BAD_LABEL);
-    }
+  const long long l = y64 ? *reinterpret_cast<const long long*>(y) : *reinterpret_cast<const int*>(y);
+  const int label = l >= 0 && l < V ? (int)l : kNone;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *lab = label;
+    if (l >= V) atomicOr(status, ST_BAD_LABEL);
   }
   __syncthreads();
-  float m[NT], s[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    m[t] = -INFINITY;
-    s[t] = 0.f;
-  }
+  float m = -INFINITY, s = 0.f;
   const long long step = (long long)gridDim.x * 8 * kFewRows;
-  for (long long v0 = ((long long)blockIdx.x * 8 + warp) * kFewRows; v0 < V; v0 += step) {
-    float z[kFewRows][NT];
+  long long v0 = ((long long)blockIdx.x * 8 + warp) * kFewRows;
+  // the next two segments of the rows, over the end of a row to the warp's next ones
+  RawSeg<VEC, TW> ahead[2][kFewRows];
+  long long fv = v0;
+  int fs = 0;
+  auto fetch = [&](RawSeg<VEC, TW>(&to)[kFewRows]) {
+    if (fv >= V) return;
 #pragma unroll
-    for (int r = 0; r < kFewRows; ++r)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) z[r][t] = 0.f;
-#pragma unroll 2
+    for (int r = 0; r < kFewRows; ++r) to[r].load(W + min(fv + r, (long long)V - 1) * ldw, fs * kSeg, lane, C);
+    if (++fs == nseg) {
+      fs = 0;
+      fv += step;
+    }
+  };
+  fetch(ahead[0]);
+  fetch(ahead[1]);
+  for (; v0 < V; v0 += step) {
+    float z[kFewRows] = {0.f, 0.f, 0.f, 0.f};
     for (int seg = 0; seg < nseg; ++seg) {
       float w[kFewRows][8];
 #pragma unroll
-      for (int r = 0; r < kFewRows; ++r)
-        load_seg<VEC>(W + min(v0 + r, (long long)V - 1) * ldw, seg * kSeg, lane, C, w[r]);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const float4* d = reinterpret_cast<const float4*>(xs + (size_t)(t * nseg + seg) * kSeg);
-        const float4 a = d[lane], b = d[32 + lane];
-        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int r = 0; r < kFewRows; ++r)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) z[r][t] = fmaf(w[r][j], x[j], z[r][t]);
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float top = m[t];
-#pragma unroll
       for (int r = 0; r < kFewRows; ++r) {
-#pragma unroll
-        for (int o = 16; o; o >>= 1) z[r][t] += __shfl_xor_sync(0xffffffffu, z[r][t], o);
-        if (v0 + r >= V) z[r][t] = -INFINITY;
-        if (v0 + r == label[t] && lane == 0) target[t] = z[r][t];
-        top = fmaxf(top, z[r][t]);
+        ahead[0][r].values(w[r]);
+        ahead[0][r] = ahead[1][r];
       }
-      const float ref = top == -INFINITY ? 0.f : top * kLog2e;
-      s[t] *= ex2(fmaf(m[t], kLog2e, -ref));
+      fetch(ahead[1]);
+      const float4* d = reinterpret_cast<const float4*>(xs + (size_t)seg * kSeg);
+      const float4 a = d[lane], b = d[32 + lane];
+      const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-      for (int r = 0; r < kFewRows; ++r) s[t] += ex2(fmaf(z[r][t], kLog2e, -ref));
-      m[t] = top;
+      for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[r] = fmaf(w[r][j], x[j], z[r]);
     }
-  }
-  if (lane == 0) {
+    float top = m;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) red[warp][t] = make_float2(m[t], s[t]);
+    for (int r = 0; r < kFewRows; ++r) {
+#pragma unroll
+      for (int o = 16; o; o >>= 1) z[r] += __shfl_xor_sync(0xffffffffu, z[r], o);
+      if (v0 + r >= V) z[r] = -INFINITY;
+      if (v0 + r == label && lane == 0) *target = z[r];
+      top = fmaxf(top, z[r]);
+    }
+    const float ref = top == -INFINITY ? 0.f : top * kLog2e;
+    s *= ex2(fmaf(m, kLog2e, -ref));
+#pragma unroll
+    for (int r = 0; r < kFewRows; ++r) s += ex2(fmaf(z[r], kLog2e, -ref));
+    m = top;
   }
+  if (lane == 0) red[warp] = make_float2(m, s);
   __syncthreads();
-  if ((int)threadIdx.x < T && threadIdx.x < NT) {
+  if (threadIdx.x == 0) {
     float M = -INFINITY, S = 0.f;
     for (int w = 0; w < 8; ++w) {
-      const float2 q = red[w][threadIdx.x];
+      const float2 q = red[w];
       const float top = fmaxf(M, q.x), ref = top == -INFINITY ? 0.f : top;
       S = S * ex2((M - ref) * kLog2e) + q.y * ex2((q.x - ref) * kLog2e);
       M = top;
     }
-    part[(long long)threadIdx.x * gridDim.x + blockIdx.x] = make_float2(M, S);
+    part[blockIdx.x] = make_float2(M, S);
   }
 }
 
@@ -882,34 +872,22 @@ int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts
 
 int tiles(long long n, int wide = TILE) { return (int)((n + wide - 1) / wide); }
 
-// The form for few points, and its blocks (all resident: three an SM; each slot of `part` a block).
-// (C = 2048, V = 65536: 54 us for one point, 56 for two; 81 for four, where the tile kernel takes 69.)
-constexpr int kFewPoints = 2;
-constexpr size_t kFewSmem = 64 * 1024;
-bool few_points(long long T, int C) {
-  return T <= kFewPoints && (size_t)T * ((C + rowwise::kSeg - 1) / rowwise::kSeg * rowwise::kSeg) * 4 <= kFewSmem;
-}
-int few_blocks(int V) { return std::min((V + 8 * kFewRows - 1) / (8 * kFewRows), 3 * device_sm_count()); }
+// The form for one point, and its blocks (two an SM; each a slot of `part`).
+constexpr size_t kOneSmem = 64 * 1024;
+size_t one_smem(int C) { return (size_t)(C + rowwise::kSeg - 1) / rowwise::kSeg * rowwise::kSeg * sizeof(float); }
+bool one_point(long long T, int C) { return T == 1 && one_smem(C) <= kOneSmem; }
+int one_blocks(int V) { return std::min((V + 8 * kFewRows - 1) / (8 * kFewRows), 2 * device_sm_count()); }
 
-template <typename TX, typename TW, bool VEC, int NT>
-int few_go(const XentShape& s, const XentIO& io, int* lab, float* target, float2* part, uint32_t* status,
-           cudaStream_t st) {
-  const size_t smem = (size_t)NT * ((s.C + rowwise::kSeg - 1) / rowwise::kSeg * rowwise::kSeg) * 4;
-  static SmemOptIn allow;
-  GC_CUDA(allow(k_xent_few<TX, TW, VEC, NT>, kFewSmem));
-  return launch_chain(k_xent_few<TX, TW, VEC, NT>, "k_xent_few", (unsigned)few_blocks(s.V), 256, smem, 1, false, st,
-                      (const TX*)io.X, (long long)io.ldx, (const TW*)io.W, (long long)io.ldw, s.N * s.n_c, s.C, s.V,
-                      io.y, io.y64, lab, target, part, status);
-}
 template <typename TX, typename TW>
-int few_by_size(const XentShape& s, const XentIO& io, int* lab, float* target, float2* part, uint32_t* status,
-                cudaStream_t st) {
+int launch_one(const XentShape& s, const XentIO& io, int* lab, float* target, float2* part, uint32_t* status,
+               cudaStream_t st) {
   const bool vec = s.C % 8 == 0 && rowwise::rows_16(io.W, io.ldw, sizeof(TW));
-  if (s.N * s.n_c == 1)
-    return vec ? few_go<TX, TW, true, 1>(s, io, lab, target, part, status, st)
-               : few_go<TX, TW, false, 1>(s, io, lab, target, part, status, st);
-  return vec ? few_go<TX, TW, true, 2>(s, io, lab, target, part, status, st)
-             : few_go<TX, TW, false, 2>(s, io, lab, target, part, status, st);
+  auto* kern = vec ? k_xent_one<TX, TW, true> : k_xent_one<TX, TW, false>;
+  static SmemOptIn allow[2];
+  GC_CUDA(allow[vec](kern, kOneSmem));
+  return launch_chain(kern, "k_xent_one", (unsigned)one_blocks(s.V), 256, one_smem(s.C), 1, false, st,
+                      (const TX*)io.X, (const TW*)io.W, (long long)io.ldw, s.C, s.V, io.y, io.y64, lab, target, part,
+                      status);
 }
 
 // Columns of a piece: as many as kPieceElems of P allow, the pieces of one width.
@@ -921,7 +899,7 @@ int piece_cols(long long T, int V) {
 
 struct XentScratch {
   int Cp, nx, nw, piece, np;
-  bool w_in_place, few;
+  bool w_in_place, one;
   __nv_bfloat16 *X, *W, *P;
   int* lab;
   float *lse, *target, *row_loss, *acc;
@@ -935,8 +913,8 @@ XentScratch carve_xent(Carve& c, const XentShape& s) {
   w.nx = s.x_dtype == GC_BF16 ? 1 : 2;
   w.nw = s.w_dtype == GC_BF16 ? 1 : 2;
   w.w_in_place = s.w_dtype == GC_BF16 && s.w_16;
-  w.few = few_points(T, s.C);
-  if (!w.few || s.want) {  // few points' losses take X and W as they are
+  w.one = one_point(T, s.C);
+  if (!w.one || s.want) {  // one point's loss takes X and W as they are
     w.X = c.take<__nv_bfloat16>((size_t)w.nx * T * w.Cp);
     w.W = w.w_in_place ? nullptr : c.take<__nv_bfloat16>((size_t)w.nw * s.V * w.Cp);
   }
@@ -944,7 +922,7 @@ XentScratch carve_xent(Carve& c, const XentShape& s) {
   w.lse = c.take<float>((size_t)T);
   w.target = c.take<float>((size_t)T);
   w.row_loss = c.take<float>((size_t)T);
-  w.part = c.take<float2>((size_t)T * (w.few ? few_blocks(s.V) : 2 * tiles(s.V)));
+  w.part = c.take<float2>((size_t)T * (w.one ? one_blocks(s.V) : 2 * tiles(s.V)));
   if (s.want & (XENT_DX | XENT_G)) {
     w.piece = piece_cols(T, s.V);
     w.np = (s.want & XENT_G) || s.x_dtype == GC_F32 ? 2 : 1;
@@ -1020,16 +998,16 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   const long long T = (long long)s.N * s.n_c;
   const bool xb = s.x_dtype == GC_BF16, wb = s.w_dtype == GC_BF16;
   int rc = GC_OK;
-  if (w.few) {
-    rc = xb ? wb ? few_by_size<__nv_bfloat16, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
-                 : few_by_size<__nv_bfloat16, float>(s, io, w.lab, w.target, w.part, status, st)
-            : wb ? few_by_size<float, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
-                 : few_by_size<float, float>(s, io, w.lab, w.target, w.part, status, st);
+  if (w.one) {
+    rc = xb ? wb ? launch_one<__nv_bfloat16, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
+                 : launch_one<__nv_bfloat16, float>(s, io, w.lab, w.target, w.part, status, st)
+            : wb ? launch_one<float, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
+                 : launch_one<float, float>(s, io, w.lab, w.target, w.part, status, st);
     if (rc) return rc;
-    if (!s.want) return join_rows(w, few_blocks(s.V), T, io, st);
+    if (!s.want) return join_rows(w, one_blocks(s.V), T, io, st);
   }
-  rc = xb ? parts_of<__nv_bfloat16>(io.X, io.ldx, T, s.C, w.Cp, 1, io.y, io.y64, s.V, w.lab, w.X, status, w.few, st)
-          : parts_of<float>(io.X, io.ldx, T, s.C, w.Cp, 2, io.y, io.y64, s.V, w.lab, w.X, status, w.few, st);
+  rc = xb ? parts_of<__nv_bfloat16>(io.X, io.ldx, T, s.C, w.Cp, 1, io.y, io.y64, s.V, w.lab, w.X, status, w.one, st)
+          : parts_of<float>(io.X, io.ldx, T, s.C, w.Cp, 2, io.y, io.y64, s.V, w.lab, w.X, status, w.one, st);
   if (rc) return rc;
   if (!w.w_in_place) {
     rc = wb ? parts_of<__nv_bfloat16>(io.W, io.ldw, s.V, s.C, w.Cp, 1, nullptr, 0, 0, nullptr, w.W, status, true, st)
@@ -1073,11 +1051,11 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     const long long l4[3] = {w.Cp, (long long)s.n_c * w.Cp, T * w.Cp};
     if ((rc = map_nd(&mX4, w.X, 4, d4, l4, BK))) return rc;
   }
-  if (!w.few) {
+  if (!w.one) {
     rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, mX, st) : run_z<STAT, 2>(p, mX, mW, mX, st);
     if (rc) return rc;
   }
-  if ((rc = join_rows(w, w.few ? few_blocks(s.V) : p.slots, T, io, st))) return rc;
+  if ((rc = join_rows(w, w.one ? one_blocks(s.V) : p.slots, T, io, st))) return rc;
   if (!(s.want & (XENT_DX | XENT_G))) return GC_OK;
 
   p.P = w.P;

@@ -129,7 +129,7 @@ def test_two_pairs_to_a_cluster(gc, N, n_c, C, V, x, w):
 @pytest.mark.parametrize("T,C,V", [(1, 1, 1), (1, 2048, 5000), (2, 300, 33), (3, 1000, 20001), (4, 64, 12000),
                                    (5, 257, 1000), (8, 520, 4096), (8, 4096, 300), (9, 128, 1000), (1, 16384, 40)])
 def test_few_points(gc, T, C, V, x, w, layout):
-    """One or two points take W as it lies; a few more do not; the same with the gradient asked for."""
+    """One point takes W as it lies; a few more do not; the same with the gradient asked for."""
     X, W, y = _data(1, T, C, V, x, w, T + C + V, layout=layout)
     ref = _reference(X, W, y, 1)
     ws = gc.Workspace()
