@@ -9,7 +9,8 @@ vocabulary.  An iteration does what the workers and the parameter server would:
   code      coefficients for the chunks that were finished (Algorithm 1), encode, decode and update
 
 The dropout mask is a function of (seed, iteration, point, column), so the workers that hold a chunk
-agree on its gradient to the bit: worker_gradient() is what one of them computes from its own rows.
+agree on its gradient, up to the order of sums: worker_gradient() is what one of them computes from its
+own rows.
 
     python examples/lm_head_step.py [iterations]
 """
@@ -100,7 +101,8 @@ def train(pb: Problem, iterations: int, lr: float = 2.0):
 if __name__ == "__main__":
     n = int(sys.argv[1]) if len(sys.argv) > 1 else 40
     pb = Problem()
-    same = torch.equal(worker_gradient(pb, 0, 2), gradients(pb, 0)[1][2])
+    whole = gradients(pb, 0)[1][2]
+    off = (worker_gradient(pb, 0, 2) - whole).abs().max() / whole.abs().max()
     losses = train(pb, n)
-    print(f"a worker's gradient of its chunk is the server's to the bit: {same}")
+    print(f"a worker's gradient of its chunk against that of all chunks together: {off.item():.1e} of the largest")
     print("loss " + " ".join(f"{v:.3f}" for v in losses[:: max(1, n // 10)]) + f" -> {losses[-1]:.3f}")

@@ -69,6 +69,8 @@ struct XentParams {
   // GRAD: dX tiles, round robin; then G's, `extra` each for the units past the first `r`, which
   // have one dX tile less, and the rest round robin
   int ndx, ct, vt, ndw, r, extra;
+  int ks, split;       // K ranges of a dX tile (ndx counts each); split: they leave their sums in `acc` as
+                       // [ks][T][ld_acc], for k_xent_dx to add
   int stage_ops, stages;
   int first_piece, last_piece;
   const int* lab;      // T labels, negative: none
@@ -95,6 +97,7 @@ struct TileAt {
   int kind;            // 0: z, 1: dX, 2: G
   int m0, n0, chunk;
   int nkb, na, nb;
+  int kb0, range;      // dX: the first K block, the K range
 };
 
 template <int MODE>
@@ -118,7 +121,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
     t.kind = 0;
     t.m0 = (g * p.group + rem - n * gm) * TILE;
     t.n0 = n * WIDE;
-    t.chunk = 0;
+    t.chunk = t.kb0 = t.range = 0;
     t.nkb = (p.C + BK - 1) / BK;
     t.na = p.nx;
     t.nb = p.nw;
@@ -126,12 +129,14 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
   }
   const int ndx = (p.ndx - unit + p.units - 1) / p.units;
   if (k < ndx) {
-    const int i = unit + k * p.units;
+    const int i = unit + k * p.units, at = i / p.ks, nkb = (p.w + BK - 1) / BK;
     t.kind = 1;
-    t.m0 = i / p.ct * TILE;
-    t.n0 = i % p.ct * WIDE;
+    t.range = i - at * p.ks;
+    t.m0 = at / p.ct * TILE;
+    t.n0 = at % p.ct * WIDE;
     t.chunk = 0;
-    t.nkb = (p.w + BK - 1) / BK;
+    t.kb0 = (int)((long long)t.range * nkb / p.ks);
+    t.nkb = (int)((long long)(t.range + 1) * nkb / p.ks) - t.kb0;
     t.na = p.np_dx;
     t.nb = p.np_dx == 1 ? 1 : p.nw;
     return t;
@@ -141,6 +146,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
   const int i = k < mine ? k * nb + unit - p.r : p.extra * nb + (k - mine) * p.units + unit;
   const int per = p.vt * p.ct, c = i / per, rem = i - c * per;
   t.kind = 2;
+  t.kb0 = t.range = 0;
   t.chunk = c;
   t.m0 = rem / p.ct * TILE;
   t.n0 = rem % p.ct * WIDE;
@@ -300,7 +306,9 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
     }
   } else if (t.kind == 1) {
     const bool rv = row_in < p.T;
-    const bool out = p.last_piece && p.dx_bf16;  // the sum is complete and leaves in bf16
+    const bool out = p.last_piece && p.dx_bf16 && !p.split;  // the sum is complete and leaves in bf16
+    const bool first = p.first_piece || p.split;
+    float* acc = p.acc + (p.split ? (size_t)t.range * p.T * p.ld_acc : 0);
     const bool vec = p.ld_acc % 4 == 0 && reinterpret_cast<uintptr_t>(p.acc) % 16 == 0;
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
@@ -313,8 +321,8 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
         box_row(box, lane, v);
         box_ready();
         if (lane == 0) {
-          if (p.first_piece)
-            store_3d(mAcc, box, col, (int)row_in, 0);
+          if (first)
+            store_3d(mAcc, box, col, (int)row_in, t.range);
           else
             add_3d(mAcc, box, col, (int)row_in, 0);  // one addition an element and piece, in the pieces' order
           bulk_commit();
@@ -322,8 +330,8 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
         continue;
       }
       if (!rv) continue;
-      float* a = p.acc + row_in * p.ld_acc + col;
-      if (!p.first_piece) {
+      float* a = acc + row_in * p.ld_acc + col;
+      if (!first) {
         if (vec && n >= 32) {
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
@@ -437,7 +445,7 @@ __global__ void __launch_bounds__(kThreadsX, 1)
       const bool rows_a = t.kind < 2, skip_a = rows_a && half_m == 1 && !p.a_both;
       const uint32_t bytes = 2 * t.nb * OP_BYTES + (rows_a ? t.na * p.a_rows * BK * 2 * (p.a_both ? 2 : 1)
                                                            : 2 * t.na * OP_BYTES);
-      for (int kb = 0; kb < t.nkb; ++kb, ++it) {
+      for (int kb = t.kb0; kb < t.kb0 + t.nkb; ++kb, ++it) {
         if (!mbar_wait(&empty[s], ph ^ 1, abort_flag, p.status, p.spin_limit)) ok = false;
         if (!__all_sync(0xffffffffu, ok)) {
           ok = false;
@@ -717,6 +725,39 @@ __global__ void __launch_bounds__(256)
   }
 }
 
+// dX from the sums of its K ranges, in their order after that of the pieces before; `sum` (fp32) holds it
+// until the last piece, whose sum leaves as T.
+template <typename T>
+__global__ void __launch_bounds__(256) k_xent_dx(const float* __restrict__ part, int ks, long long rows, int C,
+                                                 int ld, float* __restrict__ sum, int first, T* __restrict__ dX,
+                                                 long long ld_dx) {
+  start_next();
+  wait_prior();
+  const int per = (C + 3) / 4;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / per;
+  if (row >= rows) return;
+  const int c = (int)(i - row * per) * 4;
+  const size_t at = (size_t)row * ld + c;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (!first) s = *reinterpret_cast<const float4*>(sum + at);
+#pragma unroll 8
+  for (int k = 0; k < ks; ++k) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(part + (size_t)k * rows * ld + at));
+    s.x += v.x;
+    s.y += v.y;
+    s.z += v.z;
+    s.w += v.w;
+  }
+  if (!dX) {
+    *reinterpret_cast<float4*>(sum + at) = s;
+    return;
+  }
+  const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (c + e < C) dX[row * ld_dx + c + e] = rowwise::from_f<T>(v[e]);
+}
+
 // lse and loss of a row from its partial sums: a warp a row.
 __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ part, int n, long long T,
                                                   const int* __restrict__ lab, const float* __restrict__ target,
@@ -897,12 +938,20 @@ int piece_cols(long long T, int V) {
   return tiles((V + pieces - 1) / pieces) * TILE;
 }
 
+// K ranges of a dX tile: with few tiles (few points, or few columns) the sum over a piece of the
+// vocabulary, one 64-wide block after the other, would outlast all else (1,024 points, C = 256, V = 65536:
+// four tiles of 1,024 blocks, 276 us at the full rate).  128 tiles in all, sixteen blocks each at least.
+int dx_ranges(long long T, int C, int piece) {
+  const long long n = (long long)tiles(T) * tiles(C);
+  return (int)std::max<long long>(1, std::min<long long>({(128 + n - 1) / n, piece / (16 * BK), 32}));
+}
+
 struct XentScratch {
-  int Cp, nx, nw, piece, np;
+  int Cp, nx, nw, piece, np, ks, ld_acc;
   bool w_in_place, one;
   __nv_bfloat16 *X, *W, *P;
   int* lab;
-  float *lse, *target, *row_loss, *acc;
+  float *lse, *target, *row_loss, *acc, *ranges;
   float2* part;
 };
 
@@ -927,9 +976,13 @@ XentScratch carve_xent(Carve& c, const XentShape& s) {
     w.piece = piece_cols(T, s.V);
     w.np = (s.want & XENT_G) || s.x_dtype == GC_F32 ? 2 : 1;
     w.P = c.take<__nv_bfloat16>((size_t)w.np * T * w.piece);
-    // bf16 dX: the pieces' sum in fp32 (an fp32 dX holds it itself)
-    if ((s.want & XENT_DX) && s.x_dtype == GC_BF16 && w.piece < s.V)
-      w.acc = c.take<float>((size_t)T * ((s.C + 3) / 4 * 4));
+    if (s.want & XENT_DX) {
+      w.ks = dx_ranges(T, s.C, std::min(w.piece, s.V));
+      w.ld_acc = (s.C + 3) / 4 * 4;
+      if (w.ks > 1) w.ranges = c.take<float>((size_t)w.ks * T * w.ld_acc);
+      // the pieces' sum in fp32 (with one range to a tile an fp32 dX holds it itself)
+      if (w.piece < s.V && (w.ks > 1 || s.x_dtype == GC_BF16)) w.acc = c.take<float>((size_t)T * w.ld_acc);
+    }
   }
   return w;
 }
@@ -962,13 +1015,13 @@ int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& m
   if (rc) return rc;
   p.ct = tiles(p.C, CL / 2 * TILE);
   p.vt = tiles(p.w);
-  p.ndx = want & XENT_DX ? p.mt * p.ct : 0;
+  p.ndx = want & XENT_DX ? p.mt * p.ct * p.ks : 0;
   p.ndw = want & XENT_G ? p.N * p.vt * p.ct : 0;
   p.units = (int)std::min<long long>(n, (long long)p.ndx + p.ndw);
   // the units with one dX tile less take that much more of G
   p.r = p.ndx % p.units;
   const int dx_a = p.np_dx, dx_b = p.np_dx == 1 ? 1 : p.nw, dx_prod = p.np_dx == 1 ? 1 : 1 + p.nw;
-  const double cost_dx = (double)((p.w + BK - 1) / BK) * dx_prod;
+  const double cost_dx = (double)((p.w + BK - 1) / BK) / p.ks * dx_prod;
   const double cost_dw = (double)((p.n_c + BK - 1) / BK) * (1 + p.nx);
   p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_dw + 0.5), p.ndw / (p.units - p.r));
   p.stage_ops = std::max(p.ndx ? dx_a + dx_b : 0, p.ndw ? p.np + p.nx : 0);
@@ -1065,8 +1118,9 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.dx_bf16 = xb;
   p.dX = io.dX;
   p.ld_dx = io.lddx;
-  p.acc = xb ? w.acc : (float*)io.dX;
-  p.ld_acc = xb ? (s.C + 3) / 4 * 4 : io.lddx;
+  p.split = w.ks > 1;
+  p.acc = p.split ? w.ranges : xb ? w.acc : (float*)io.dX;
+  p.ld_acc = p.split || xb ? w.ld_acc : io.lddx;
   p.G = io.G;
   p.ldg = io.ldg;
   p.stall = 0;
@@ -1078,19 +1132,20 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   }
   p.acc_box = p.acc && (s.want & XENT_DX) && rowwise::rows_16(p.acc, p.ld_acc, 4);
   if (p.acc_box) {
-    const long long da[3] = {s.C, T, 1}, la[2] = {p.ld_acc, T * p.ld_acc};
+    const long long da[3] = {s.C, T, std::max(1, w.ks)}, la[2] = {p.ld_acc, T * p.ld_acc};
     if ((rc = map_nd(&mAcc, p.acc, 3, da, la, 32, 1, true))) return rc;
   }
   for (int v0 = 0; v0 < s.V; v0 += w.piece) {
     p.v0 = v0;
     p.w = std::min(w.piece, s.V - v0);
+    p.ks = std::max(1, std::min(w.ks, (p.w + BK - 1) / BK));  // a short last piece has no empty range
     p.first_piece = v0 == 0;
     p.last_piece = v0 + w.piece >= s.V;
     const long long lp[2] = {w.piece, T * w.piece}, dps[3] = {w.piece, T, w.np};
     if ((rc = map_nd(&mPs, w.P, 3, dps, lp, 32, w.np))) return rc;
     rc = two_pairs(p.mt, p.w) ? run_z<PROB, 4>(p, mX2, mW, mPs, st) : run_z<PROB, 2>(p, mX, mW, mPs, st);
     if (rc) return rc;
-    const bool two = T > HALF && two_pairs((s.want & XENT_DX ? p.mt : 0) + (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0), s.C);
+    const bool two = T > HALF && two_pairs((s.want & XENT_DX ? (long long)p.mt * p.ks : 0) + (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0), s.C);
     const long long dp[3] = {p.w, T, w.np};
     const long long d4[4] = {p.w, s.n_c, s.N, w.np};
     const long long l4[3] = {w.piece, (long long)s.n_c * w.piece, T * w.piece};
@@ -1099,6 +1154,15 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     rc = two ? run_grad<4>(p, s.want, mP, mWt, mP4, mX4, mG, mAcc, st)
              : run_grad<2>(p, s.want, mP, mWt, mP4, mX4, mG, mAcc, st);
     if (rc) return rc;
+    if (p.split && (s.want & XENT_DX)) {
+      const unsigned grid = (unsigned)((T * ((s.C + 3) / 4) + 255) / 256);
+      void* out = p.last_piece ? io.dX : nullptr;
+      rc = xb ? launch_chain(k_xent_dx<__nv_bfloat16>, "k_xent_dx", grid, 256, 0, 1, true, st, w.ranges, p.ks, T, s.C,
+                             w.ld_acc, w.acc, p.first_piece, (__nv_bfloat16*)out, (long long)io.lddx)
+              : launch_chain(k_xent_dx<float>, "k_xent_dx", grid, 256, 0, 1, true, st, w.ranges, p.ks, T, s.C,
+                             w.ld_acc, w.acc, p.first_piece, (float*)out, (long long)io.lddx);
+      if (rc) return rc;
+    }
   }
   return GC_OK;
 }

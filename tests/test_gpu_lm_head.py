@@ -25,6 +25,7 @@ def ex():
 
 
 def test_a_worker_alone_computes_the_same_bits(ex):
+    """The mask is that of the points, and at these sizes the sums run in one order."""
     pb = ex.Problem(N=6, n_c=40, C=136, V=300)
     G = ex.gradients(pb, 3)[1]
     for chunk in (0, 2, 5):

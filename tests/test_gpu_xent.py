@@ -179,6 +179,33 @@ def test_several_pieces_of_the_vocabulary(gc, x, w):
         _close(got[k], ref[k], k)
 
 
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("N,n_c,C,V", [(2, 20, 100, 6000), (1, 300, 136, 20011), (3, 500, 24, 50000), (1, 1, 64, 9000)])
+def test_few_tiles_of_the_row_gradient(gc, N, n_c, C, V, x):
+    """Few rows and columns against a long vocabulary: the sum over it runs in ranges, added in order."""
+    X, W, y = _data(N, n_c, C, V, x, "bf16", N + n_c + C + V, layout="ragged")
+    ref = _reference(X, W, y, N)
+    ws = gc.Workspace()
+    got = gc.gc_softmax_xent(X, W, y, N, n_c, ws=ws)
+    gc.gc_status(ws)
+    for k in ref:
+        _close(got[k], ref[k], k)
+    again = gc.gc_softmax_xent(X, W, y, N, n_c, G=False, ws=ws)
+    assert torch.equal(again["dX"], got["dX"])
+
+
+def test_ranges_and_pieces_together(gc):
+    """32,000 points and 24 columns: nine pieces of 2,048 columns in two ranges each, the last piece of one
+    column in one."""
+    X, W, y = _data(2, 16000, 24, 8 * 2048 + 1, "bf16", "bf16", 21)
+    ref = _reference(X, W, y, 2)
+    ws = gc.Workspace()
+    got = gc.gc_softmax_xent(X, W, y, 2, 16000, ws=ws)
+    gc.gc_status(ws)
+    for k in ref:
+        _close(got[k], ref[k], k)
+
+
 def test_outputs_alone_and_repeated(gc):
     X, W, y = _data(3, 200, 136, 900, "bf16", "bf16", 3)
     ws = gc.Workspace()
