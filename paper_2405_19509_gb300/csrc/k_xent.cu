@@ -76,8 +76,7 @@ struct XentParams {
   const int* lab;      // T labels, negative: none
   const float* lse;
   float* target;       // STAT: z at the label
-  float2* part;        // STAT: [T][slots], 128 columns a slot
-  int slots;
+  float2* part;        // STAT: [slots][T], 128 columns a slot
   __nv_bfloat16* P;    // [np][T][Pp]
   int Pp;
   float* acc;          // fp32 dX of the pieces so far
@@ -239,19 +238,20 @@ __device__ __forceinline__ void box_ready() {
   __syncwarp();
 }
 
-template <int MODE>
+// `release` hands the accumulator back: called once, when the last of it is in registers.
+template <int MODE, typename Release>
 __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, uint32_t taddr, long long row_in,
-                                         int half, uint8_t* box, const CUtensorMap* mOut, const CUtensorMap* mAcc) {
+                                         int half, int lab, float l2, uint8_t* box, const CUtensorMap* mOut,
+                                         const CUtensorMap* mAcc, Release release) {
   const int lane = threadIdx.x & 31;
   if (MODE == STAT) {
-    const bool rv = row_in < p.T;
-    const int lab = rv ? __ldg(p.lab + row_in) : -1;
     float m = -INFINITY, s = 0.f;
 #pragma unroll 1
     for (int c = 0; c < HALF / 64; ++c) {
       float v[64];
       __syncwarp();
       tmem_ld64(taddr + (uint32_t)(c * 64), v);
+      if (c == HALF / 64 - 1) release();
       const int col = t.n0 + half * HALF + c * 64;
       const int n = p.V - col;
       if (n < 64) {
@@ -265,25 +265,30 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
       for (int j = 3; j < 64; ++j) top[j % 4] = fmaxf(top[j % 4], v[j]);
       const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
       const float ref = most == -INFINITY ? 0.f : most * kLog2e;
-      float e[4] = {s * ex2(fmaf(m, kLog2e, -ref)), 0.f, 0.f, 0.f};
+      float2 e[2] = {make_float2(s * ex2(fmaf(m, kLog2e, -ref)), 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-      for (int j = 0; j < 64; ++j) e[j % 4] += ex2(fmaf(v[j], kLog2e, -ref));
-      s = (e[0] + e[1]) + (e[2] + e[3]);
+      for (int j = 0; j < 64; j += 2) {
+        const float2 a = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(kLog2e, kLog2e), make_float2(-ref, -ref));
+        e[j / 2 % 2] = __fadd2_rn(e[j / 2 % 2], make_float2(ex2(a.x), ex2(a.y)));
+      }
+      s = (e[0].x + e[0].y) + (e[1].x + e[1].y);
       m = most;
     }
-    if (rv && t.n0 < p.V) p.part[row_in * p.slots + t.n0 / HALF + half] = make_float2(m, s);
+    if (row_in < p.T && t.n0 < p.V) p.part[(long long)(t.n0 / HALF + half) * p.T + row_in] = make_float2(m, s);
   } else if (MODE == PROB) {
-    const bool rv = row_in < p.T && t.n0 < p.w;
-    const int lab = rv ? __ldg(p.lab + row_in) : -1;
-    const float l2 = rv ? __ldg(p.lse + row_in) * kLog2e : 0.f;
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
       __syncwarp();
       tmem_ld32(taddr + (uint32_t)(c * 32), v);
+      if (c == HALF / 32 - 1) release();
       if (t.n0 >= p.w || row_in - lane >= p.T) continue;  // nothing of the warp's rows or columns exists
       const int at = lab - (p.v0 + t.n0 + half * HALF + c * 32);  // the label's place here
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = lab >= 0 ? ex2(fmaf(v[j], kLog2e, -l2)) : 0.f;
+      for (int j = 0; j < 32; j += 2) {
+        const float2 a = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(kLog2e, kLog2e), make_float2(-l2, -l2));
+        v[j] = lab >= 0 ? ex2(a.x) : 0.f;
+        v[j + 1] = lab >= 0 ? ex2(a.y) : 0.f;
+      }
       if (at >= 0 && at < 32) {
 #pragma unroll
         for (int j = 0; j < 32; ++j)
@@ -314,6 +319,7 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
       float v[32];
       __syncwarp();
       tmem_ld32(taddr + (uint32_t)(c * 32), v);
+      if (c == HALF / 32 - 1) release();
       const int col = t.n0 + half * HALF + c * 32, n = p.C - col;
       if (n <= 0 || row_in - lane >= p.T) continue;
       if (!out && p.acc_box) {
@@ -360,6 +366,7 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
       float v[32];
       __syncwarp();
       tmem_ld32(taddr + (uint32_t)(c * 32), v);
+      if (c == HALF / 32 - 1) release();
       const int col = t.n0 + half * HALF + c * 32, n = p.C - col;
       if (n <= 0 || lv - lane >= p.w) continue;
       box_free(lane);
@@ -556,15 +563,22 @@ __global__ void __launch_bounds__(kThreadsX, 1)
       TileAt t = tile_at<MODE, WIDE>(p, unit, k);
       t.n0 += q * TILE;
       const int ab = k & 1;
+      const long long row = (long long)t.m0 + half_m * HALF + quarter * 32 + lane;
+      int lab = kNone;
+      float l2 = 0.f;  // the row's lse, in powers of two
+      if (MODE != GRAD && row < p.T) {  // on their way while the accumulator fills
+        lab = __ldg(p.lab + row);
+        if (MODE == PROB) l2 = __ldg(p.lse + row) * kLog2e;
+      }
       const bool ready = mbar_wait(&tfull[ab], (k >> 1) & 1, abort_flag, p.status, p.spin_limit);
       if (!__all_sync(0xffffffffu, ready)) break;
       fence_after();
-      epilogue<MODE>(p, t, tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ab * TILE + half * HALF),
-                     (long long)t.m0 + half_m * HALF + quarter * 32 + lane, half,
-                     store_box + (warp - 2) * boxes(MODE) * BOX, &mOut, &mAcc);
-      fence_before();
-      __syncwarp();
-      if (lane == 0) arrive_remote(at_rank(&tempty[ab], q * 2));
+      epilogue<MODE>(p, t, tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ab * TILE + half * HALF), row,
+                     half, lab, l2, store_box + (warp - 2) * boxes(MODE) * BOX, &mOut, &mAcc, [&] {
+                       fence_before();
+                       __syncwarp();
+                       if (lane == 0) arrive_remote(at_rank(&tempty[ab], q * 2));
+                     });
     }
     if (boxes(MODE) && lane == 0) bulk_wait_all();
   }
@@ -580,23 +594,25 @@ __global__ void __launch_bounds__(kThreadsX, 1)
 }
 
 // bf16 parts [parts][rows][Cp] of a matrix: hi = bf16(x), lo = bf16(x - hi), zero from C to Cp.  A block
-// a row at a time.  With labels: lab = the label as an int, kNone where there is none.  The products
+// a row at a time, or a warp (WPR = 1: short rows).  With labels: lab = the label as an int, kNone where there is none.  The products
 // that follow multiply such a row by zeros, so what is not finite in it enters as zero (kNoneBad).
-template <typename T, bool VEC>
+template <typename T, bool VEC, int WPR>
 __global__ void __launch_bounds__(256)
     k_xent_parts(const T* __restrict__ x, long long ld, long long rows, int C, int Cp, int parts,
                  const void* __restrict__ y, int y64, int V, int* __restrict__ lab,
                  __nv_bfloat16* __restrict__ out, uint32_t* status) {
   using namespace rowwise;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = WPR == 1 ? 0 : threadIdx.x >> 5;
   start_next();
   wait_prior();
-  for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+  constexpr int RPB = 8 / WPR;
+  for (long long row = (long long)blockIdx.x * RPB + (WPR == 1 ? threadIdx.x >> 5 : 0); row < rows;
+       row += (long long)gridDim.x * RPB) {
     long long l = 0;
     if (y) l = y64 ? reinterpret_cast<const long long*>(y)[row] : reinterpret_cast<const int*>(y)[row];
     const bool live = !y || (l >= 0 && l < V);
     int bad = 0;
-    for (int col0 = warp * kSeg; col0 < Cp; col0 += 8 * kSeg) {
+    for (int col0 = warp * kSeg; col0 < Cp; col0 += WPR * kSeg) {
       float v[8];
       load_seg<VEC>(x + row * ld, col0, lane, C, v);
       if (!live) {
@@ -614,8 +630,8 @@ __global__ void __launch_bounds__(256)
       }
     }
     if (y) {
-      if (!live) bad = __syncthreads_or(bad);
-      if (threadIdx.x == 0) {
+      if (!live) bad = WPR == 1 ? __any_sync(0xffffffffu, bad) : __syncthreads_or(bad);
+      if (lane == 0 && warp == 0) {
         lab[row] = live ? (int)l : bad ? kNoneBad : kNone;
         if (l >= V) atomicOr(status, ST_BAD_LABEL);
       }
@@ -758,37 +774,48 @@ __global__ void __launch_bounds__(256) k_xent_dx(const float* __restrict__ part,
     if (c + e < C) dX[row * ld_dx + c + e] = rowwise::from_f<T>(v[e]);
 }
 
-// lse and loss of a row from its partial sums: a warp a row.
+// (m, s) += (m2, s2), the largest value and the sum of exponentials about it.
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
+  const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+  s = s * ex2((m - ref) * kLog2e) + s2 * ex2((m2 - ref) * kLog2e);
+  m = top;
+}
+
+// lse and loss of the rows from their n partial sums [n][T].  A block takes R rows: a warp's lanes are R
+// rows by 32 / R slots, its eight warps take the slots in turn (R = 32: whole 256-byte reads; 4: whole sectors, for few rows).
+template <int R>
 __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ part, int n, long long T,
                                                   const int* __restrict__ lab, const float* __restrict__ target,
                                                   float* __restrict__ lse, float* __restrict__ lse_out,
                                                   float* __restrict__ row_loss) {
-  const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  __shared__ float2 sums[8][R];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane % R;
+  const long long row = (long long)blockIdx.x * R + r;
   start_next();
   wait_prior();
-  if (row >= T) return;
-  const float2* p = part + row * n;
   float m = -INFINITY, s = 0.f;
+  if (row < T) {
 #pragma unroll 8
-  for (int k = lane; k < n; k += 32) {
-    const float2 q = __ldg(p + k);
-    const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
-    s = s * ex2((m - ref) * kLog2e) + q.y * ex2((q.x - ref) * kLog2e);
-    m = top;
+    for (int k = warp * (32 / R) + lane / R; k < n; k += 8 * (32 / R)) {
+      const float2 q = __ldcg(part + k * T + row);
+      join(m, s, q.x, q.y);
+    }
   }
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
+  for (int o = 16; o >= R; o >>= 1) {
     const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
-    const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-    s = s * ex2((m - ref) * kLog2e) + s2 * ex2((m2 - ref) * kLog2e);
-    m = top;
+    join(m, s, m2, s2);
   }
-  if (lane == 0) {
-    const float l = lab[row] == kNoneBad ? NAN : m + logf(s);
+  if (lane < R) sums[warp][r] = make_float2(m, s);
+  __syncthreads();
+  if (warp == 0 && lane < R && row < T) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) join(m, s, sums[w][r].x, sums[w][r].y);
+    const int at = lab[row];
+    const float l = at == kNoneBad ? NAN : m + logf(s);
     if (lse) lse[row] = l;
     if (lse_out) lse_out[row] = l;
-    if (row_loss) row_loss[row] = lab[row] >= 0 ? l - target[row] : 0.f;
+    if (row_loss) row_loss[row] = at >= 0 ? l - target[row] : 0.f;
   }
 }
 
@@ -905,8 +932,11 @@ int launch_mode(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c
 template <typename T>
 int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts, const void* y, int y64, int V,
              int* lab, __nv_bfloat16* out, uint32_t* status, bool chained, cudaStream_t s) {
-  const unsigned grid = (unsigned)std::min<long long>(rows, 8LL * device_sm_count());
-  auto* kern = C % 8 == 0 && rowwise::rows_16(x, ld, sizeof(T)) ? k_xent_parts<T, true> : k_xent_parts<T, false>;
+  const bool vec = C % 8 == 0 && rowwise::rows_16(x, ld, sizeof(T)), shorter = Cp <= 4 * rowwise::kSeg;
+  const long long blocks = shorter ? (rows + 7) / 8 : rows;
+  const unsigned grid = (unsigned)std::min<long long>(blocks, 8LL * device_sm_count());
+  auto* kern = shorter ? vec ? k_xent_parts<T, true, 1> : k_xent_parts<T, false, 1>
+                       : vec ? k_xent_parts<T, true, 8> : k_xent_parts<T, false, 8>;
   return launch_chain(kern, "k_xent_parts", grid, 256, 0, 1, chained, s, (const T*)x, (long long)ld, rows, C, Cp, parts,
                       y, y64, V, lab, out, status);
 }
@@ -1032,8 +1062,11 @@ int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& m
 // Rows' log-sum-exp and losses from their partial sums, and the mean.
 int join_rows(const XentScratch& w, int slots, long long T, const XentIO& io, cudaStream_t st) {
   float* row_loss = io.row_loss ? io.row_loss : io.loss ? w.row_loss : nullptr;
-  const int rc = launch_chain(k_xent_lse, "k_xent_lse", (unsigned)((T + 7) / 8), 256, 0, 1, true, st, w.part, slots, T,
-                              w.lab, w.target, w.lse, io.lse, row_loss);
+  // rows enough for a block an SM: 32 each
+  const bool wide = T >= 32LL * device_sm_count();
+  const int rc = launch_chain(wide ? k_xent_lse<32> : k_xent_lse<4>, "k_xent_lse",
+                              (unsigned)((T + (wide ? 31 : 3)) / (wide ? 32 : 4)), 256, 0, 1, true, st, w.part, slots,
+                              T, w.lab, w.target, w.lse, io.lse, row_loss);
   if (rc || !io.loss) return rc;
   return launch_chain(k_xent_loss, "k_xent_loss", 1, 1024, 0, 1, true, st, row_loss, T, io.loss);
 }
@@ -1083,7 +1116,6 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.group = std::min(p.mt, 16);
   p.a_both = T > HALF;
   p.a_rows = T > HALF ? HALF : (int)(T + 7) / 8 * 8;
-  p.slots = 2 * tiles(s.V);
   p.lab = w.lab;
   p.lse = w.lse;
   p.target = w.target;
@@ -1108,7 +1140,7 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, mX, st) : run_z<STAT, 2>(p, mX, mW, mX, st);
     if (rc) return rc;
   }
-  if ((rc = join_rows(w, w.one ? one_blocks(s.V) : p.slots, T, io, st))) return rc;
+  if ((rc = join_rows(w, w.one ? one_blocks(s.V) : 2 * tiles(s.V), T, io, st))) return rc;
   if (!(s.want & (XENT_DX | XENT_G))) return GC_OK;
 
   p.P = w.P;
