@@ -416,8 +416,8 @@ int grad_tpr(int cols) {
 struct Slices {
   int count, rows;
 };
-// Row ranges of a chunk: enough blocks of `threads` for every SM to hold 1024 threads, at least four
-// rows a warp (the sums of a range are written and read once more).
+// Row ranges of a chunk: enough blocks of `threads` for every SM to hold 1024 threads, at least four or
+// eight rows a warp (the sums of a range are written and read once more).
 Slices slices_of(int N, int n_c, int threads, int min_rows) {
   const long long blocks = (long long)device_sm_count() * std::max(1, 1024 / threads);
   long long want = std::max<long long>(1, blocks / N);
@@ -428,7 +428,7 @@ Slices slices_of(int N, int n_c, int threads, int min_rows) {
 Slices grad_slices(int N, int n_c, int cols) {
   if (cols > kFusedCols) return slices_of(N, n_c, 256, 32);
   const int tpr = grad_tpr(cols);
-  return slices_of(N, n_c, tpr == 32 ? 128 : tpr, tpr == 32 ? 16 : 4);
+  return slices_of(N, n_c, tpr == 32 ? 128 : tpr, tpr == 32 ? 32 : 4);
 }
 
 template <typename T, bool VEC, int TPR, bool SUMS>
