@@ -41,14 +41,18 @@ constexpr int TILE = 256, HALF = 128, BK = 64;
 constexpr int OP_BYTES = HALF * BK * 2;  // a CTA's 128 x 64 share of an operand tile
 constexpr int kMaxStages = 6;
 constexpr int kEpi = 8;
-constexpr int kThreadsX = 64 + 32 * kEpi;
 constexpr int BOX = 32 * 128;  // a store box: 32 rows of 128 bytes, 128-byte swizzle
 constexpr long long kSpinX = 1LL << 32;
 constexpr long long kPieceElems = 1LL << 26;  // of P: 256 MB as two bf16 parts
 constexpr float kLog2e = 1.4426950408889634f;
 
 constexpr int kNone = -1, kNoneBad = -2;  // labels that are none, the latter of a row that is not finite
+// K blocks of a product for a 32-bit result that are summed in tensor memory before the sum goes to
+// registers: an addition there is cut off, not rounded, and all errors have one sign (5,569 points, C = 384,
+// fp32: G was 1.9e-5 off in one sum, 2e-8 a step).  bf16 results and z, a few hundred steps long, do without.
+constexpr int kSegment = 8;
 enum { STAT = 0, PROB = 1, GRAD = 2 };
+constexpr int kThreadsX = 64 + 32 * kEpi;
 // The ring of operand stages and the store boxes of each epilogue warp.
 constexpr int ring_bytes(int mode) { return (mode == PROB ? 10 : 12) * OP_BYTES; }
 constexpr int boxes(int mode) { return mode == PROB ? 2 : mode == GRAD ? 1 : 0; }
@@ -97,6 +101,7 @@ struct TileAt {
   int m0, n0, chunk;
   int nkb, na, nb;
   int kb0, range;      // dX: the first K block, the K range
+  int seg;             // K blocks that are summed in tensor memory at a time
 };
 
 template <int MODE>
@@ -124,6 +129,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
     t.nkb = (p.C + BK - 1) / BK;
     t.na = p.nx;
     t.nb = p.nw;
+    t.seg = t.nkb;
     return t;
   }
   const int ndx = (p.ndx - unit + p.units - 1) / p.units;
@@ -138,6 +144,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
     t.nkb = (int)((long long)(t.range + 1) * nkb / p.ks) - t.kb0;
     t.na = p.np_dx;
     t.nb = p.np_dx == 1 ? 1 : p.nw;
+    t.seg = p.dx_bf16 ? t.nkb : kSegment;
     return t;
   }
   k -= ndx;
@@ -152,6 +159,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
   t.nkb = (p.n_c + BK - 1) / BK;
   t.na = p.np;
   t.nb = p.nx;
+  t.seg = kSegment;
   return t;
 }
 
@@ -238,11 +246,12 @@ __device__ __forceinline__ void box_ready() {
   __syncwarp();
 }
 
-// `release` hands the accumulator back: called once, when the last of it is in registers.
+// The epilogue of STAT and PROB.  `release` hands the accumulator back: called once, when the last of it is
+// in registers.
 template <int MODE, typename Release>
 __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, uint32_t taddr, long long row_in,
                                          int half, int lab, float l2, uint8_t* box, const CUtensorMap* mOut,
-                                         const CUtensorMap* mAcc, Release release) {
+                                         Release release) {
   const int lane = threadIdx.x & 31;
   if (MODE == STAT) {
     float m = -INFINITY, s = 0.f;
@@ -275,7 +284,7 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
       m = most;
     }
     if (row_in < p.T && t.n0 < p.V) p.part[(long long)(t.n0 / HALF + half) * p.T + row_in] = make_float2(m, s);
-  } else if (MODE == PROB) {
+  } else {
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
       __syncwarp();
@@ -309,17 +318,25 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
         }
       }
     }
-  } else if (t.kind == 1) {
+  }
+}
+
+// The epilogue of GRAD: `get` gives 32 columns of a lane's row, in turn.
+template <typename Get>
+__device__ __forceinline__ void store_grad(const XentParams& p, const TileAt& t, long long row_in, int half, uint8_t* box,
+                                           const CUtensorMap* mOut, const CUtensorMap* mAcc, Get get) {
+  const int lane = threadIdx.x & 31;
+  if (t.kind == 1) {
     const bool rv = row_in < p.T;
     const bool out = p.last_piece && p.dx_bf16 && !p.split;  // the sum is complete and leaves in bf16
     const bool first = p.first_piece || p.split;
     float* acc = p.acc + (p.split ? (size_t)t.range * p.T * p.ld_acc : 0);
     const bool vec = p.ld_acc % 4 == 0 && reinterpret_cast<uintptr_t>(p.acc) % 16 == 0;
+#pragma unroll
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
       __syncwarp();
-      tmem_ld32(taddr + (uint32_t)(c * 32), v);
-      if (c == HALF / 32 - 1) release();
+      get(c, v);
       const int col = t.n0 + half * HALF + c * 32, n = p.C - col;
       if (n <= 0 || row_in - lane >= p.T) continue;
       if (!out && p.acc_box) {
@@ -362,11 +379,11 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
     }
   } else {
     const int lv = (int)row_in;  // row of the piece
+#pragma unroll
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
       __syncwarp();
-      tmem_ld32(taddr + (uint32_t)(c * 32), v);
-      if (c == HALF / 32 - 1) release();
+      get(c, v);
       const int col = t.n0 + half * HALF + c * 32, n = p.C - col;
       if (n <= 0 || lv - lane >= p.w) continue;
       box_free(lane);
@@ -439,7 +456,6 @@ __global__ void __launch_bounds__(kThreadsX, 1)
   start_next();
   wait_prior();
   const int ntiles = tiles_of<MODE>(p, unit);
-
   if (warp == 0) {
     const bool one = elect_one();
     const uint16_t to = (uint16_t)(0x5 << half_m);  // the CTAs that hold the same rows of A
@@ -507,28 +523,31 @@ __global__ void __launch_bounds__(kThreadsX, 1)
     if (half_m == 0) {
       const bool one = elect_one();
       const uint16_t all = (uint16_t)((1 << CL) - 1), pair = (uint16_t)(3 << (2 * q));
-      uint32_t ph = 0;
+      uint32_t ph = 0, use = 0;  // use: accumulators filled so far, in turn the one and the other
       int s = 0;
       bool ok = true;
       for (int k = 0; k < ntiles && ok; ++k) {
         const TileAt t = tile_at<MODE, WIDE>(p, unit, k);
-        const int ab = k & 1;
-        ok = mbar_wait(&tempty[ab], ((k >> 1) & 1) ^ 1, abort_flag, p.status, p.spin_limit);
-        if (!__all_sync(0xffffffffu, ok)) break;
-        fence_after();
-        const uint32_t d = tmem_base + (uint32_t)(ab * TILE);
         const bool a_mn = t.kind == 2, b_mn = t.kind >= 1;
         const uint32_t idesc = idesc_256(a_mn, b_mn);
         const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
         const uint64_t da0 = sdesc(smem_u32(smem), a_mn ? OP_BYTES / 2 : 16, 1024);
         const uint64_t db0 = sdesc(smem_u32(smem) + t.na * OP_BYTES, b_mn ? OP_BYTES / 2 : 16, 1024);
-        for (int kb = 0; kb < t.nkb; ++kb) {
-          ok = mbar_wait(&full[s], ph, abort_flag, p.status, p.spin_limit);
+        for (int kb = 0, left = 0; kb < t.nkb; ++kb) {
+          const int ab = use & 1;
+          if (left == 0) {
+            left = t.seg;
+            ok = mbar_wait(&tempty[ab], ((use >> 1) & 1) ^ 1, abort_flag, p.status, p.spin_limit);
+          }
+          ok = ok && mbar_wait(&full[s], ph, abort_flag, p.status, p.spin_limit);
           if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
             break;
           }
+          const bool opens = left == t.seg, closes = --left == 0 || kb == t.nkb - 1;
+          if (opens) fence_after();
           if (one) {
+            const uint32_t d = tmem_base + (uint32_t)(ab * TILE);
             // the descriptors of the stage: only the address, in 16-byte units, differs
             const uint64_t at = (uint64_t)((uint32_t)s * (uint32_t)stage_bytes >> 4);
             uint64_t da = da0 + at;
@@ -538,13 +557,17 @@ __global__ void __launch_bounds__(kThreadsX, 1)
 #pragma unroll
                 for (int ks = 0; ks < BK / 16; ++ks)
                   mma(d, da + (uint64_t)(ks * a_step), db + (uint64_t)(ks * b_step), idesc,
-                      (kb > 0 || i + j + ks > 0) ? 1u : 0u);
+                      (!opens || i + j + ks > 0) ? 1u : 0u);
               }
             }
             commit_to(&empty[s], all);
-            if (kb == t.nkb - 1) commit_to(&tfull[ab], pair);
+            if (closes) commit_to(&tfull[ab], pair);
           }
           __syncwarp();
+          if (closes) {
+            left = 0;
+            ++use;
+          }
           if (++s == S) {
             s = 0;
             ph ^= 1;
@@ -559,10 +582,25 @@ __global__ void __launch_bounds__(kThreadsX, 1)
     }
   } else {
     const int quarter = warp & 3, half = (warp - 2) >> 2;
-    for (int k = 0; k < ntiles; ++k) {
+    uint32_t use = 0;
+    bool ok = true;
+    auto filled = [&] {
+      ok = mbar_wait(&tfull[use & 1], (use >> 1) & 1, abort_flag, p.status, p.spin_limit);
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok) fence_after();
+      return ok;
+    };
+    auto release = [&] {
+      fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_remote(at_rank(&tempty[use & 1], q * 2));
+    };
+    auto at = [&] {
+      return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((use & 1) * TILE + half * HALF);
+    };
+    for (int k = 0; k < ntiles && ok; ++k) {
       TileAt t = tile_at<MODE, WIDE>(p, unit, k);
       t.n0 += q * TILE;
-      const int ab = k & 1;
       const long long row = (long long)t.m0 + half_m * HALF + quarter * 32 + lane;
       int lab = kNone;
       float l2 = 0.f;  // the row's lse, in powers of two
@@ -570,15 +608,32 @@ __global__ void __launch_bounds__(kThreadsX, 1)
         lab = __ldg(p.lab + row);
         if (MODE == PROB) l2 = __ldg(p.lse + row) * kLog2e;
       }
-      const bool ready = mbar_wait(&tfull[ab], (k >> 1) & 1, abort_flag, p.status, p.spin_limit);
-      if (!__all_sync(0xffffffffu, ready)) break;
-      fence_after();
-      epilogue<MODE>(p, t, tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(ab * TILE + half * HALF), row,
-                     half, lab, l2, store_box + (warp - 2) * boxes(MODE) * BOX, &mOut, &mAcc, [&] {
-                       fence_before();
-                       __syncwarp();
-                       if (lane == 0) arrive_remote(at_rank(&tempty[ab], q * 2));
-                     });
+      uint8_t* box = store_box + (warp - 2) * boxes(MODE) * BOX;
+      if (MODE == GRAD && t.nkb > t.seg) {
+        float sum[HALF];
+#pragma unroll
+        for (int j = 0; j < HALF; ++j) sum[j] = 0.f;
+        for (int left = t.nkb; left > 0 && filled(); left -= t.seg, ++use) {
+#pragma unroll
+          for (int j = 0; j < HALF; j += 16) tmem_add16(at() + (uint32_t)j, sum + j);
+          release();
+        }
+        if (!ok) break;
+        store_grad(p, t, row, half, box, &mOut, &mAcc, [&](int c, float(&v)[32]) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = sum[c * 32 + j];
+        });
+        continue;
+      }
+      if (!filled()) break;
+      if (MODE == GRAD)
+        store_grad(p, t, row, half, box, &mOut, &mAcc, [&](int c, float(&v)[32]) {
+          tmem_ld32(at() + (uint32_t)(c * 32), v);
+          if (c == HALF / 32 - 1) release();
+        });
+      else
+        epilogue<MODE>(p, t, at(), row, half, lab, l2, box, &mOut, release);
+      ++use;
     }
     if (boxes(MODE) && lane == 0) bulk_wait_all();
   }

@@ -206,6 +206,21 @@ def test_ranges_and_pieces_together(gc):
         _close(got[k], ref[k], k)
 
 
+@pytest.mark.parametrize("x,N,n_c,C,V", [("f32", 1, 5569, 384, 4112), ("bf16", 1, 8000, 200, 3000), ("bf16", 2, 1024, 512, 2000),
+                                         ("f32", 1, 2000, 64, 30000)])
+def test_long_sums_keep_their_digits(gc, x, N, n_c, C, V):
+    """32-bit results of sums over thousands of points or columns, in the 2-norm.  Tensor memory is
+    added to at most 96 times in a row, each addition cut off by 2^-24 on average, of a running sum
+    two thirds of the last: 3.8e-6; the operands' parts are off by 2^-17 at most, 2e-6 on average; z is
+    off as the sums are, which moves the probabilities, a smaller part of the results: 8e-6 together."""
+    X, W, y = _data(N, n_c, C, V, x, x, n_c + V)
+    ref = _reference(X, W, y, N)
+    got = gc.gc_softmax_xent(X, W, y, N, n_c)
+    for k in ("G", "dX") if x == "f32" else ("G",):
+        value = ref[k][0]
+        assert ((got[k].double() - value).norm() / value.norm()).item() <= 8e-6, k
+
+
 def test_outputs_alone_and_repeated(gc):
     X, W, y = _data(3, 200, 136, 900, "bf16", "bf16", 3)
     ws = gc.Workspace()
