@@ -323,7 +323,7 @@ int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t 
  * A point whose label is negative (padding) has row_loss 0 and enters no gradient, whatever its row
  * of X holds; its lse is formed all the same (not finite where the row is not).  A label
  * >= V is treated so too, and raises GC_ERR_DATA in the status header.  Neither z nor P is kept: both are formed for a piece of the vocabulary at a
- * time (a piece of P is at most about 2^26 values), the products on the tensor cores with fp32 sums.
+ * time (a piece of P is at most about 2^27 values), the products on the tensor cores with fp32 sums.
  * bf16 operands are used as they are, fp32 ones as bf16 hi + lo (2^-17); P enters G as hi + lo, and
  * a bf16 dX in bf16.
  *   X    N n_c rows of C values of x_dtype, ldx elements apart.    W   V rows, ldw apart, w_dtype.

@@ -43,7 +43,10 @@ constexpr int kMaxStages = 6;
 constexpr int kEpi = 8;
 constexpr int BOX = 32 * 128;  // a store box: 32 rows of 128 bytes, 128-byte swizzle
 constexpr long long kSpinX = 1LL << 32;
-constexpr long long kPieceElems = 1LL << 26;  // of P: 256 MB as two bf16 parts
+// Values of a piece of P: 512 MB as two bf16 parts.  Larger pieces mean fewer waves that are not full and fewer
+// sums of dX to add to (8,192 points, V = 65536, C = 2048, 2^24 to 2^27: 7.1, 6.6, 6.5, 6.3 ms; 4,096 points,
+// V = 32768, C = 256: 514, 483, 445, 400 us), though from 2^25 on they leave L2.
+constexpr long long kPieceElems = 1LL << 27;
 constexpr float kLog2e = 1.4426950408889634f;
 
 constexpr int kNone = -1, kNoneBad = -2;  // labels that are none, the latter of a row that is not finite
