@@ -32,11 +32,17 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// s / n with the quotient of a division where 1 / n is at hand: one correction of s * (1 / n).
+// s / n to the last digit or so where 1 / n is at hand: s * (1 / n) and one correction.
 __device__ __forceinline__ float div_by(float s, float n, float inv) {
   const float q = s * inv;
-  const float r = fmaf(-q, n, s);
-  return isfinite(r) ? fmaf(r, inv, q) : q;
+  return fmaf(fmaf(-q, n, s), inv, q);
+}
+// The sum over the first W lanes (a power of two; the others hold zeros), in every lane of them.
+template <int W>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = W / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return W < 32 ? __shfl_sync(0xffffffffu, v, 0) : v;
 }
 
 // The eight values at the segment's columns of a per-column vector, `dflt` where there is none.
@@ -65,27 +71,31 @@ struct NormArgs {
   Mask m;
 };
 
-// TPR threads a row, VPT segments a warp of them.  A warp a row: four rows a block, no barrier.  With one
-// segment a warp the next row is on its way while this one is worked on, and gamma and beta stay in
-// registers: otherwise every row waits for memory (16,384 rows of 4096 bf16 with dropout and residual,
-// 537 MB: 155 us by four segments a warp and no row ahead).
+// TPR threads a row, VPT segments a warp of them.  A warp a row: four rows a block, no barrier.  Up to two
+// segments a warp the next row is on its way while this one is worked on.  What bounds it then is the
+// instructions: a row's exchange is the same hundred a lane for one segment or for two.  (16,384 rows of
+// 4096 bf16 with dropout and residual, 537 MB: four segments and no row ahead 155 us, one and a row ahead 105, two 102;
+// 65,536 rows of 1024: one 110, two 100.)
 template <typename T, bool VEC, int TPR, int VPT>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / TPR)
     k_norm(NormArgs a) {
   constexpr int WPR = TPR / 32;                       // warps a row
   constexpr int RPB = TPR == 32 ? 4 : 1;              // rows a block
-  constexpr bool AHEAD = VPT == 1;
+  constexpr bool AHEAD = VPT <= 2;
   __shared__ float2 part[2][WPR];
   const int lane = threadIdx.x & 31;
   const int warp = TPR == 32 ? 0 : threadIdx.x >> 5;
   const long long step = (long long)gridDim.x * RPB;
   long long row = (long long)blockIdx.x * RPB + (TPR == 32 ? threadIdx.x >> 5 : 0);
-  float g[8], b[8];
   RawSeg<VEC, T> x[VPT], r[VPT];
-  int n_w = 0;  // columns of this warp
+  int n_w = 0, n_l = 0;  // columns of this warp, and of warp `lane`
 #pragma unroll
-  for (int q = 0; q < VPT; ++q) n_w += max(0, min(kSeg, a.cols - (q * WPR + warp) * kSeg));
-  const float inv_w = 1.f / (float)max(n_w, 1), inv = 1.f / (float)a.cols;
+  for (int q = 0; q < VPT; ++q) {
+    n_w += max(0, min(kSeg, a.cols - (q * WPR + warp) * kSeg));
+    if (lane < WPR) n_l += max(0, min(kSeg, a.cols - (q * WPR + lane) * kSeg));
+  }
+  const float fn_w = (float)n_w, fn_l = (float)n_l, fn = (float)a.cols;
+  const float inv_w = n_w ? 1.f / fn_w : 0.f, inv_l = n_l ? 1.f / fn_l : 0.f, inv = 1.f / fn;
   auto fetch = [&](long long at) {
 #pragma unroll
     for (int q = 0; q < VPT; ++q) x[q].load((const T*)a.x + at * a.ldx, (q * WPR + warp) * kSeg, lane, a.cols);
@@ -94,11 +104,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / 
       for (int q = 0; q < VPT; ++q) r[q].load((const T*)a.res + at * a.ldr, (q * WPR + warp) * kSeg, lane, a.cols);
     }
   };
-  if (AHEAD) {
-    load_cols<VEC>(a.gamma, 1.f, a.vec_cols, warp * kSeg, lane, a.cols, g);
-    load_cols<VEC>(a.beta, 0.f, a.vec_cols, warp * kSeg, lane, a.cols, b);
-    if (row < a.rows) fetch(row);
-  }
+  if (AHEAD && row < a.rows) fetch(row);
   int flip = 0;
   for (; row < a.rows; row += step, flip ^= 1) {
     float v[VPT][8];
@@ -127,7 +133,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / 
 #pragma unroll
       for (int j = 0; j < 8; ++j) s += v[q][j];
     s = warp_sum(s);
-    const float mu_w = n_w == 0 ? 0.f : div_by(s, (float)n_w, inv_w);
+    const float mu_w = div_by(s, fn_w, inv_w);
     float m2 = 0.f;
 #pragma unroll
     for (int q = 0; q < VPT; ++q)
@@ -143,14 +149,9 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / 
       __syncthreads();  // the two buffers alternate: one barrier a row
       // lane w merges warp w's part
       const float2 p = lane < WPR ? part[flip][lane] : make_float2(0.f, 0.f);
-      int n_l = 0;
-      if (lane < WPR) {
-#pragma unroll
-        for (int q = 0; q < VPT; ++q) n_l += max(0, min(kSeg, a.cols - (q * WPR + lane) * kSeg));
-      }
-      mu = div_by(warp_sum(p.x), (float)a.cols, inv);
-      const float d = n_l > 0 ? p.x / (float)n_l - mu : 0.f;
-      M2 = warp_sum(fmaf((float)n_l * d, d, p.y));
+      mu = div_by(lanes_sum<WPR>(p.x), fn, inv);
+      const float d = div_by(p.x, fn_l, inv_l) - mu;
+      M2 = lanes_sum<WPR>(fmaf(fn_l * d, d, p.y));
     }
     const float rstd = rsqrtf(M2 * inv + a.eps);
     if (warp == 0 && lane == 0) {
@@ -160,10 +161,9 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / 
 #pragma unroll
     for (int q = 0; q < VPT; ++q) {
       const int col0 = (q * WPR + warp) * kSeg;
-      if (!AHEAD) {
-        load_cols<VEC>(a.gamma, 1.f, a.vec_cols, col0, lane, a.cols, g);
-        load_cols<VEC>(a.beta, 0.f, a.vec_cols, col0, lane, a.cols, b);
-      }
+      float g[8], b[8];
+      load_cols<VEC>(a.gamma, 1.f, a.vec_cols, col0, lane, a.cols, g);
+      load_cols<VEC>(a.beta, 0.f, a.vec_cols, col0, lane, a.cols, b);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[q][j] = fmaf((v[q][j] - mu) * rstd, g[j], b[j]);
       store_seg<VEC>((T*)a.y + row * a.ldy, col0, lane, a.cols, v[q]);
@@ -182,16 +182,18 @@ int go_norm(const NormArgs& a, cudaStream_t s) {
   return cuda_check(cudaGetLastError(), "k_norm");
 }
 
-// One segment a warp up to 8192 columns, 1024 threads an SM; wider rows by four.
+// Two segments a warp up to 16384 columns (but for one that fills a block), 1024 threads an SM; wider rows
+// by four.
 template <typename T, bool VEC>
 int norm_by_width(const NormArgs& a, cudaStream_t s) {
   const int c = a.cols;
   if (c <= 256) return go_norm<T, VEC, 32, 1>(a, s);
-  if (c <= 512) return go_norm<T, VEC, 64, 1>(a, s);
-  if (c <= 1024) return go_norm<T, VEC, 128, 1>(a, s);
-  if (c <= 2048) return go_norm<T, VEC, 256, 1>(a, s);
-  if (c <= 4096) return go_norm<T, VEC, 512, 1>(a, s);
-  if (c <= 8192) return go_norm<T, VEC, 1024, 1>(a, s);
+  if (c <= 512) return go_norm<T, VEC, 32, 2>(a, s);
+  if (c <= 1024) return go_norm<T, VEC, 64, 2>(a, s);
+  if (c <= 2048) return go_norm<T, VEC, 128, 2>(a, s);
+  if (c <= 4096) return go_norm<T, VEC, 256, 2>(a, s);
+  if (c <= 8192) return go_norm<T, VEC, 1024, 1>(a, s);  // 210 us for 16,384 rows of 8192, 225 by two segments
+  if (c <= 16384) return go_norm<T, VEC, 1024, 2>(a, s);
   return go_norm<T, VEC, 1024, 4>(a, s);
 }
 
@@ -208,57 +210,70 @@ struct NormGradArgs {
   Mask m;
 };
 
-// TPR threads a row, one segment a warp; a block takes a slice of a chunk's rows, the next one on its way
-// while one is worked on.  SUMS: the column sums for G as well.  (16,384 rows of 4096 bf16 with dropout
-// and residual, 671 MB: 168 us with no row ahead.)
+// TPR threads a row, two segments a warp; a block takes a slice of a chunk's rows, the next one on its way
+// while one is worked on.  SUMS: the column sums for G as well.  512 threads an SM have registers for
+// all that.  (16,384 rows of 4096 bf16 with residual, 671 MB, with dropout and without it: no row ahead 168 us;
+// one segment a warp, 1024 threads 144 and 123; two 133 and 125; two, 768 threads, which spill, 179 and 165.)
+constexpr int kGradSegs = 2;
+constexpr int kGradThreads = 512;  // an SM
 template <typename T, bool VEC, int TPR, bool SUMS>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / TPR)
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? kGradThreads / 128 : kGradThreads / TPR)
     k_norm_grad(NormGradArgs a) {
-  constexpr int WPR = TPR / 32;
-  constexpr int RPB = TPR == 32 ? 4 : 1;
+  constexpr int WPR = TPR / 32, RPB = TPR == 32 ? 4 : 1, Q = kGradSegs;
   __shared__ float2 part[2][WPR];
   const int lane = threadIdx.x & 31;
   const int warp = TPR == 32 ? 0 : threadIdx.x >> 5;
-  const int col0 = warp * kSeg;
   const int chunk = blockIdx.x / a.slices, slice = blockIdx.x - chunk * a.slices;
   const int r_end = min(a.n_c, (slice + 1) * a.rows_per_slice);
   int r = slice * a.rows_per_slice + (TPR == 32 ? threadIdx.x >> 5 : 0);
   const long long first = (long long)chunk * a.n_c;
-  float sg[8], sb[8], g[8];
+  float sg[Q][8], sb[Q][8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) sg[j] = sb[j] = 0.f;
-  load_cols<VEC>(a.gamma, 1.f, a.vec_cols, col0, lane, a.cols, g);
+  for (int q = 0; q < Q; ++q)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sg[q][j] = sb[q][j] = 0.f;
   const float inv = 1.f / (float)a.cols;
-  RawSeg<VEC, T> xd, xh, xa;
+  RawSeg<VEC, T> xd[Q], xh[Q], xa[Q];
   float mu, rstd;
   auto fetch = [&](long long row) {
     mu = __ldg(a.mean + row);
     rstd = __ldg(a.rstd + row);
-    xd.load((const T*)a.dy + row * a.lddy, col0, lane, a.cols);
-    xh.load((const T*)a.h + row * a.ldh, col0, lane, a.cols);
-    if (a.dh) xa.load((const T*)a.dh + row * a.lddh, col0, lane, a.cols);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int col0 = (q * WPR + warp) * kSeg;
+      xd[q].load((const T*)a.dy + row * a.lddy, col0, lane, a.cols);
+      xh[q].load((const T*)a.h + row * a.ldh, col0, lane, a.cols);
+      if (a.dh) xa[q].load((const T*)a.dh + row * a.lddh, col0, lane, a.cols);
+    }
   };
   if (r < r_end) fetch(first + r);
   int flip = 0;
   for (; r < r_end; r += RPB, flip ^= 1) {
     const long long row = first + r;
-    float d[8], n[8];
+    float d[Q][8], n[Q][8];
     float c1 = 0.f, c2 = 0.f;
-    xd.values(d);
-    xh.values(n);
-    const RawSeg<VEC, T> ya = xa;
+    RawSeg<VEC, T> ya[Q];
     const float scale = rstd;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      n[j] = (n[j] - mu) * scale;
-      if (SUMS) {
-        sg[j] = fmaf(d[j], n[j], sg[j]);
-        sb[j] += d[j];
-      }
-      d[j] *= g[j];
-      if (in_row<VEC>(col0, lane, j, a.cols)) {  // past the row's end n is not zero
-        c1 += d[j];
-        c2 = fmaf(d[j], n[j], c2);
+    for (int q = 0; q < Q; ++q) {
+      const int col0 = (q * WPR + warp) * kSeg;
+      float g[8];
+      load_cols<VEC>(a.gamma, 1.f, a.vec_cols, col0, lane, a.cols, g);
+      xd[q].values(d[q]);
+      xh[q].values(n[q]);
+      ya[q] = xa[q];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        n[q][j] = (n[q][j] - mu) * scale;
+        if (SUMS) {
+          sg[q][j] = fmaf(d[q][j], n[q][j], sg[q][j]);
+          sb[q][j] += d[q][j];
+        }
+        d[q][j] *= g[j];
+        if (in_row<VEC>(col0, lane, j, a.cols)) {  // past the row's end n is not zero
+          c1 += d[q][j];
+          c2 = fmaf(d[q][j], n[q][j], c2);
+        }
       }
     }
     if (r + RPB < r_end) fetch(row + RPB);
@@ -268,47 +283,56 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / 
       if (lane == 0) part[flip][warp] = make_float2(c1, c2);
       __syncthreads();
       const float2 p = lane < WPR ? part[flip][lane] : make_float2(0.f, 0.f);
-      c1 = warp_sum(p.x);
-      c2 = warp_sum(p.y);
+      c1 = lanes_sum<WPR>(p.x);
+      c2 = lanes_sum<WPR>(p.y);
     }
     c1 *= inv;
     c2 *= inv;
-    float t[8];
-    if (a.dh) ya.values(t);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float v = scale * (d[j] - c1 - n[j] * c2);
-      d[j] = a.dh ? v + t[j] : v;
-    }
-    if (a.dres) store_seg<VEC>((T*)a.dres + row * a.lddr, col0, lane, a.cols, d);
-    if (a.dx) {
-      if (a.m.t) drop_seg<VEC>(a.m, row, col0, lane, d);
-      store_seg<VEC>((T*)a.dx + row * a.lddx, col0, lane, a.cols, d);
+    for (int q = 0; q < Q; ++q) {
+      const int col0 = (q * WPR + warp) * kSeg;
+      float t[8];
+      if (a.dh) ya[q].values(t);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float v = scale * (d[q][j] - c1 - n[q][j] * c2);
+        d[q][j] = a.dh ? v + t[j] : v;
+      }
+      if (a.dres) store_seg<VEC>((T*)a.dres + row * a.lddr, col0, lane, a.cols, d[q]);
+      if (a.dx) {
+        if (a.m.t) drop_seg<VEC>(a.m, row, col0, lane, d[q]);
+        store_seg<VEC>((T*)a.dx + row * a.lddx, col0, lane, a.cols, d[q]);
+      }
     }
   }
   if (!SUMS) return;
   // the block's column sums; where a warp takes a row, the four warps' in order
   float* out = a.sums + (size_t)blockIdx.x * a.sums_ld;
   if constexpr (TPR == 32) {
-    __shared__ float acc[4][kSeg];
+    __shared__ float acc[4][Q * kSeg];
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[threadIdx.x >> 5][seg_col<VEC>(0, lane, j)] = which ? sb[j] : sg[j];
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          acc[threadIdx.x >> 5][seg_col<VEC>(q * kSeg, lane, j)] = which ? sb[q][j] : sg[q][j];
       __syncthreads();
       for (int c = threadIdx.x; c < a.cols; c += 128)
         out[(size_t)which * a.cols + c] = acc[0][c] + acc[1][c] + acc[2][c] + acc[3][c];
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int c = seg_col<VEC>(col0, lane, j);
-      if (c < a.cols) {
-        out[c] = sg[j];
-        out[(size_t)a.cols + c] = sb[j];
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int c = seg_col<VEC>((q * WPR + warp) * kSeg, lane, j);
+        if (c < a.cols) {
+          out[c] = sg[q][j];
+          out[(size_t)a.cols + c] = sb[q][j];
+        }
       }
-    }
   }
 }
 
@@ -406,20 +430,20 @@ __global__ void __launch_bounds__(256) k_norm_grad_reduce(const float* __restric
   }
 }
 
-// Threads a row of the fused form: one segment a warp.
+// Threads a row of the fused form.
 int grad_tpr(int cols) {
   int t = 32;
-  while (t * 8 < cols) t *= 2;
+  while (t * 8 * kGradSegs < cols) t *= 2;
   return t;
 }
 
 struct Slices {
   int count, rows;
 };
-// Row ranges of a chunk: enough blocks of `threads` for every SM to hold 1024 threads, at least four or
+// Row ranges of a chunk: enough blocks of `threads` for every SM to hold kGradThreads, at least four or
 // eight rows a warp (the sums of a range are written and read once more).
 Slices slices_of(int N, int n_c, int threads, int min_rows) {
-  const long long blocks = (long long)device_sm_count() * std::max(1, 1024 / threads);
+  const long long blocks = (long long)device_sm_count() * std::max(1, kGradThreads / threads);
   long long want = std::max<long long>(1, blocks / N);
   want = std::min<long long>(want, (n_c + min_rows - 1) / min_rows);
   const int rows = (int)((n_c + want - 1) / want);
@@ -445,8 +469,7 @@ int grad_by_width(const NormGradArgs& a, int N, cudaStream_t s) {
     case 64: return go_grad<T, VEC, 64, SUMS>(a, N, s);
     case 128: return go_grad<T, VEC, 128, SUMS>(a, N, s);
     case 256: return go_grad<T, VEC, 256, SUMS>(a, N, s);
-    case 512: return go_grad<T, VEC, 512, SUMS>(a, N, s);
-    default: return go_grad<T, VEC, 1024, SUMS>(a, N, s);
+    default: return go_grad<T, VEC, 512, SUMS>(a, N, s);
   }
 }
 
