@@ -17,6 +17,8 @@ Pin status (what fixes each function other than itself; tests/test_oracle_pins.p
   coefficient_error / error_estimate         -- per-pattern rank identity vs eq. (7)
   gradient_mse                               -- l = 1 closed form, exact patterns
   sgd_step / full_loss                       -- finite differences of L = (1/N~) sum l
+  lm_oracle (dropout, layer norm, softmax    -- published vectors of the generator, central differences
+    cross entropy; tests/test_lm_oracle_pins.py)  of every gradient
 """
 from .gc_oracle import *  # noqa: F401,F403
 from . import gc_oracle  # noqa: F401
