@@ -333,7 +333,8 @@ int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t 
  *        not all of them.  dX must not overlap X.  Any alignment; the sums have a fixed order.
  *   Limits: C <= 2^20, V <= 2^28, N n_c < 2^31, and at most 2^29 tiles of 256 x 256.
  * Workspace: gc_softmax_xent_workspace bytes.  w_16: whether W and its rows lie on 16-byte boundaries
- * (bf16 rows that do are read in place; others are copied); want: 1 with dX, 2 with G, added up.
+ * (bf16 rows that do are read in place; others are copied); want: 1 with dX, 2 with G, added up.  The size
+ * depends on the current device's number of SMs.
  */
 size_t gc_softmax_xent_workspace(int N, int n_c, int C, int V, int x_dtype, int w_dtype, int w_16, int want);
 int gc_softmax_xent(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ldw, int w_dtype,

@@ -417,8 +417,8 @@ def gc_softmax_xent(X, W, y, N: int, n_c: int, loss=True, row_loss=True, lse=Tru
     gp, ldg = _rows(G, torch.float32, "G", (N, V * C))
     e = W.element_size()
     w_16 = int(wp_ % 16 == 0 and (ldw * e % 16 == 0 or V == 1))
-    ws, (wp, wn) = _ws(ws, _bytes("gc_softmax_xent_workspace", N, n_c, C, V, xt, wt, w_16,
-                                 (dX is not None) + 2 * (G is not None)), dev)
+    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_softmax_xent_workspace", N, n_c, C,
+                                        V, xt, wt, w_16, (dX is not None) + 2 * (G is not None)), dev)
     _check(lib.gc_softmax_xent(
         xp, ldx, xt, wp_, ldw, wt, _dev(y, y.dtype, "y", (T,)), int(y.dtype is torch.int64), N, n_c, C, V,
         _dev(loss, torch.float64, "loss"), _dev(row_loss, torch.float32, "row_loss", (T,)),

@@ -109,7 +109,7 @@ extern "C" {
 
 const char* gc_last_error(void) { return g_err; }
 
-int gc_version(void) { return 200; }
+int gc_version(void) { return 300; }
 
 uint64_t gc_kernel_launches(void) { return g_launches.load(); }
 
