@@ -2,7 +2,8 @@
 //   z = X W^T,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_{t, y_t}
 //   P = exp(z - lse) - onehot(y)  (rows without a label: 0),  dX = P W,  G_i = P_i^T X_i
 // for T = N n_c rows of C values and V rows of W.  Neither z nor P exists as a whole:
-//   k_xent_parts   X (and W where it is fp32, or does not lie on 16-byte boundaries) as bf16 parts
+//   k_xent_parts   X (and W where it is fp32, or does not lie on 16-byte boundaries) as bf16 parts; losses
+//                  alone read bf16 rows where they lie
 //   k_xent<STAT>   z tile by tile in tensor memory; per row and 128 columns the largest and the sum of
 //                  the exponentials about it go to scratch; k_xent_lse joins them
 //   k_xent<PROB>   z again for one piece of the vocabulary, written as P's bf16 parts
@@ -70,6 +71,21 @@ constexpr int boxes(int mode) { return mode == PROB ? 2 : mode == GRAD ? 1 : 0; 
 constexpr size_t smem_bytes(int mode) { return ring_bytes(mode) + kEpi * boxes(mode) * BOX + 1024 + 256; }
 static_assert(smem_bytes(PROB) <= kSmemMax && smem_bytes(GRAD) <= kSmemMax, "shared memory");
 
+// A point's label: from the array that k_xent_parts leaves, or where X needs no copy as the caller gave it.
+struct Labels {
+  const int* lab;  // negative: none
+  const void* y;   // used where lab is NULL
+  int y64, V;
+  __device__ __forceinline__ long long given(long long row) const {
+    return y64 ? __ldg(reinterpret_cast<const long long*>(y) + row) : __ldg(reinterpret_cast<const int*>(y) + row);
+  }
+  __device__ __forceinline__ int at(long long row) const {
+    if (lab) return __ldg(lab + row);
+    const long long l = given(row);
+    return l >= 0 && l < V ? (int)l : kNone;
+  }
+};
+
 struct XentParams {
   long long T;
   int C, V, N, n_c;
@@ -88,7 +104,7 @@ struct XentParams {
                        // [ks][T][ld_acc], for k_xent_dx to add
   int stage_ops, stages;
   int first_piece, last_piece;
-  const int* lab;      // T labels, negative: none
+  Labels lab;
   const float* lse;
   float* target;       // STAT: z at the label
   float2* part;        // STAT: [slots][T], 128 columns a slot
@@ -616,7 +632,7 @@ __global__ void __launch_bounds__(kThreadsX, 1)
       int lab = kNone;
       float l2 = 0.f;  // the row's lse, in powers of two
       if (MODE != GRAD && row < p.T) {  // on their way while the accumulator fills
-        lab = __ldg(p.lab + row);
+        lab = p.lab.at(row);
         if (MODE == PROB) l2 = __ldg(p.lse + row) * kLog2e;
       }
       uint8_t* box = store_box + (warp - 2) * boxes(MODE) * BOX;
@@ -851,7 +867,7 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
 // rows by 32 / R slots, its eight warps take the slots in turn (R = 32: whole 256-byte reads; 4: whole sectors, for few rows).
 template <int R>
 __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ part, int n, long long T,
-                                                  const int* __restrict__ lab, const float* __restrict__ target,
+                                                  Labels lab, const float* __restrict__ target, uint32_t* status,
                                                   float* __restrict__ lse, float* __restrict__ lse_out,
                                                   float* __restrict__ row_loss) {
   __shared__ float2 sums[8][R];
@@ -877,7 +893,8 @@ __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ par
   if (warp == 0 && lane < R && row < T) {
 #pragma unroll
     for (int w = 1; w < 8; ++w) join(m, s, sums[w][r].x, sums[w][r].y);
-    const int at = lab[row];
+    const int at = lab.at(row);
+    if (!lab.lab && lab.given(row) >= lab.V) atomicOr(status, ST_BAD_LABEL);
     const float l = at == kNoneBad ? NAN : m + logf(s);
     if (lse) lse[row] = l;
     if (lse_out) lse_out[row] = l;
@@ -990,8 +1007,8 @@ int resident(int* units) {
 
 template <int MODE, int CL>
 int launch_mode(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d,
-                const CUtensorMap& out, const CUtensorMap& acc, const XentParams& p, cudaStream_t s) {
-  return launch_chain(k_xent<MODE, CL>, "k_xent", (unsigned)(CL * p.units), kThreadsX, smem_bytes(MODE), CL, true, s,
+                const CUtensorMap& out, const CUtensorMap& acc, const XentParams& p, bool chained, cudaStream_t s) {
+  return launch_chain(k_xent<MODE, CL>, "k_xent", (unsigned)(CL * p.units), kThreadsX, smem_bytes(MODE), CL, chained, s,
                       a, b, c, d, out, acc, p);
 }
 
@@ -1092,7 +1109,8 @@ bool two_pairs(long long row_tiles, int cols) {
 }
 
 template <int MODE, int CL>
-int run_z(XentParams p, const CUtensorMap& mX, const CUtensorMap& mW, const CUtensorMap& mOut, cudaStream_t st) {
+int run_z(XentParams p, const CUtensorMap& mX, const CUtensorMap& mW, const CUtensorMap& mOut, bool chained,
+          cudaStream_t st) {
   int n = 0;
   const int rc = resident<MODE, CL>(&n);
   if (rc) return rc;
@@ -1100,7 +1118,7 @@ int run_z(XentParams p, const CUtensorMap& mX, const CUtensorMap& mW, const CUte
   p.units = (int)std::min<long long>(n, (long long)p.mt * p.nt);
   p.stage_ops = p.nx + p.nw;
   p.stages = ring_bytes(MODE) / (p.stage_ops * OP_BYTES);
-  return launch_mode<MODE, CL>(mX, mW, mX, mX, mOut, mX, p, st);
+  return launch_mode<MODE, CL>(mX, mW, mX, mX, mOut, mX, p, chained, st);
 }
 
 template <int CL>
@@ -1122,17 +1140,18 @@ int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& m
   p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_dw + 0.5), p.ndw / (p.units - p.r));
   p.stage_ops = std::max(p.ndx ? dx_a + dx_b : 0, p.ndw ? p.np + p.nx : 0);
   p.stages = ring_bytes(GRAD) / (p.stage_ops * OP_BYTES);
-  return launch_mode<GRAD, CL>(mP, mWt, mP4, mX4, mG, mAcc, p, st);
+  return launch_mode<GRAD, CL>(mP, mWt, mP4, mX4, mG, mAcc, p, true, st);
 }
 
 // Rows' log-sum-exp and losses from their partial sums, and the mean.
-int join_rows(const XentScratch& w, int slots, long long T, const XentIO& io, cudaStream_t st) {
+int join_rows(const XentScratch& w, int slots, long long T, const Labels& lab, const XentIO& io, uint32_t* status,
+              cudaStream_t st) {
   float* row_loss = io.row_loss ? io.row_loss : io.loss ? w.row_loss : nullptr;
   // rows enough for a block an SM: 32 each
   const bool wide = T >= 32LL * device_sm_count();
   const int rc = launch_chain(wide ? k_xent_lse<32> : k_xent_lse<4>, "k_xent_lse",
                               (unsigned)((T + (wide ? 31 : 3)) / (wide ? 32 : 4)), 256, 0, 1, true, st, w.part, slots,
-                              T, w.lab, w.target, w.lse, io.lse, row_loss);
+                              T, lab, w.target, status, w.lse, io.lse, row_loss);
   if (rc || !io.loss) return rc;
   return launch_chain(k_xent_loss, "k_xent_loss", 1, 1024, 0, 1, true, st, row_loss, T, io.loss);
 }
@@ -1150,25 +1169,35 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   const long long T = (long long)s.N * s.n_c;
   const bool xb = s.x_dtype == GC_BF16, wb = s.w_dtype == GC_BF16;
   int rc = GC_OK;
+  Labels lab{w.lab, nullptr, 0, s.V};
   if (w.one) {
     rc = xb ? wb ? launch_one<__nv_bfloat16, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
                  : launch_one<__nv_bfloat16, float>(s, io, w.lab, w.target, w.part, status, st)
             : wb ? launch_one<float, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
                  : launch_one<float, float>(s, io, w.lab, w.target, w.part, status, st);
     if (rc) return rc;
-    if (!s.want) return join_rows(w, one_blocks(s.V), T, io, st);
+    if (!s.want) return join_rows(w, one_blocks(s.V), T, lab, io, status, st);
   }
-  rc = xb ? parts_of<__nv_bfloat16>(io.X, io.ldx, T, s.C, w.Cp, 1, io.y, io.y64, s.V, w.lab, w.X, status, w.one, st)
-          : parts_of<float>(io.X, io.ldx, T, s.C, w.Cp, 2, io.y, io.y64, s.V, w.lab, w.X, status, w.one, st);
-  if (rc) return rc;
-  if (!w.w_in_place) {
-    rc = wb ? parts_of<__nv_bfloat16>(io.W, io.ldw, s.V, s.C, w.Cp, 1, nullptr, 0, 0, nullptr, w.W, status, true, st)
-            : parts_of<float>(io.W, io.ldw, s.V, s.C, w.Cp, 2, nullptr, 0, 0, nullptr, w.W, status, true, st);
+  // losses alone read bf16 rows where they lie; the products of the gradient want a copy that is finite
+  const bool x_in_place = !s.want && xb && rowwise::rows_16(io.X, io.ldx, 2);
+  bool chained = w.one;  // whether the call has launched a kernel before
+  if (x_in_place) {
+    lab = Labels{nullptr, io.y, io.y64, s.V};
+  } else {
+    rc = xb ? parts_of<__nv_bfloat16>(io.X, io.ldx, T, s.C, w.Cp, 1, io.y, io.y64, s.V, w.lab, w.X, status, chained, st)
+            : parts_of<float>(io.X, io.ldx, T, s.C, w.Cp, 2, io.y, io.y64, s.V, w.lab, w.X, status, chained, st);
     if (rc) return rc;
+    chained = true;
   }
-  const void* W = w.w_in_place ? io.W : w.W;
-  const long long ldw = w.w_in_place ? io.ldw : w.Cp;
-  const long long Cin = w.w_in_place ? s.C : w.Cp;
+  if (!w.w_in_place) {
+    rc = wb ? parts_of<__nv_bfloat16>(io.W, io.ldw, s.V, s.C, w.Cp, 1, nullptr, 0, 0, nullptr, w.W, status, chained, st)
+            : parts_of<float>(io.W, io.ldw, s.V, s.C, w.Cp, 2, nullptr, 0, 0, nullptr, w.W, status, chained, st);
+    if (rc) return rc;
+    chained = true;
+  }
+  const void *X = x_in_place ? io.X : w.X, *W = w.w_in_place ? io.W : w.W;
+  const long long ldx = x_in_place ? io.ldx : w.Cp, ldw = w.w_in_place ? io.ldw : w.Cp;
+  const long long xc = x_in_place ? s.C : w.Cp, wc = w.w_in_place ? s.C : w.Cp;
 
   XentParams p{};
   p.T = T;
@@ -1182,7 +1211,7 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.group = std::min(p.mt, 16);
   p.a_both = T > HALF;
   p.a_rows = T > HALF ? HALF : (int)(T + 7) / 8 * 8;
-  p.lab = w.lab;
+  p.lab = lab;
   p.lse = w.lse;
   p.target = w.target;
   p.part = w.part;
@@ -1190,25 +1219,23 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.stall = take_stall(GC_STALL_XENT) ? 1 : 0;
   p.status = status;
 
-  // z: rows of X and of W, K innermost
-  CUtensorMap mX, mX2, mW, mP, mWt, mP4, mX4;  // mX2: boxes of half the rows, for two pairs
-  {
-    const long long dx[3] = {w.Cp, T, w.nx}, lx[2] = {w.Cp, T * w.Cp};
-    const long long dw[3] = {Cin, s.V, w.nw}, lw[2] = {ldw, (long long)s.V * ldw};
-    if ((rc = map_nd(&mX, w.X, 3, dx, lx, p.a_rows)) || (rc = map_nd(&mX2, w.X, 3, dx, lx, HALF / 2)) || (rc = map_nd(&mW, W, 3, dw, lw, HALF)) ||
-        (rc = map_nd(&mWt, W, 3, dw, lw, BK)))
-      return rc;
-    const long long d4[4] = {w.Cp, s.n_c, s.N, w.nx};
-    const long long l4[3] = {w.Cp, (long long)s.n_c * w.Cp, T * w.Cp};
-    if ((rc = map_nd(&mX4, w.X, 4, d4, l4, BK))) return rc;
-  }
+  // z: rows of X (boxes of half of them for two pairs) and of W, K innermost
+  CUtensorMap mX, mX2, mW, mP, mWt, mP4, mX4;
+  const long long dx[3] = {xc, T, w.nx}, lx[2] = {ldx, T * ldx};
+  const long long dw[3] = {wc, s.V, w.nw}, lw[2] = {ldw, (long long)s.V * ldw};
+  if ((rc = map_nd(&mX, X, 3, dx, lx, p.a_rows)) || (rc = map_nd(&mX2, X, 3, dx, lx, HALF / 2)) ||
+      (rc = map_nd(&mW, W, 3, dw, lw, HALF)))
+    return rc;
   if (!w.one) {
-    rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, mX, st) : run_z<STAT, 2>(p, mX, mW, mX, st);
+    rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, mX, chained, st) : run_z<STAT, 2>(p, mX, mW, mX, chained, st);
     if (rc) return rc;
   }
-  if ((rc = join_rows(w, w.one ? one_blocks(s.V) : 2 * tiles(s.V), T, io, st))) return rc;
+  if ((rc = join_rows(w, w.one ? one_blocks(s.V) : 2 * tiles(s.V), T, lab, io, status, st))) return rc;
   if (!(s.want & (XENT_DX | XENT_G))) return GC_OK;
 
+  const long long d4x[4] = {w.Cp, s.n_c, s.N, w.nx};
+  const long long l4x[3] = {w.Cp, (long long)s.n_c * w.Cp, T * w.Cp};
+  if ((rc = map_nd(&mWt, W, 3, dw, lw, BK)) || (rc = map_nd(&mX4, w.X, 4, d4x, l4x, BK))) return rc;
   p.P = w.P;
   p.Pp = w.piece;
   p.np = w.np;
@@ -1241,7 +1268,8 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     p.last_piece = v0 + w.piece >= s.V;
     const long long lp[2] = {w.piece, T * w.piece}, dps[3] = {w.piece, T, w.np};
     if ((rc = map_nd(&mPs, w.P, 3, dps, lp, 32, w.np))) return rc;
-    rc = two_pairs(p.mt, p.w) ? run_z<PROB, 4>(p, mX2, mW, mPs, st) : run_z<PROB, 2>(p, mX, mW, mPs, st);
+    rc = two_pairs(p.mt, p.w) ? run_z<PROB, 4>(p, mX2, mW, mPs, true, st)
+                              : run_z<PROB, 2>(p, mX, mW, mPs, true, st);
     if (rc) return rc;
     const bool two = T > HALF && two_pairs((s.want & XENT_DX ? (long long)p.mt * p.ks : 0) + (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0), s.C);
     const long long dp[3] = {p.w, T, w.np};

@@ -280,6 +280,28 @@ def test_label_past_the_vocabulary_is_reported(gc):
     assert all(torch.equal(got[k], want[k]) for k in want)
 
 
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_losses_alone_of_labels_that_are_none(gc, x):
+    """Losses alone take the labels and bf16 rows as they lie: negative labels, labels past the vocabulary
+    and rows without a label that are not finite give what they give with the gradient."""
+    X, W, y = _data(1, 300, 96, 700, x, "bf16", 31, ignore=0.2)
+    y[5], y[6], y[7] = 700, -1, -(1 << 40)
+    X[6, 3], X[7, 1] = float("nan"), float("-inf")
+    ws = gc.Workspace()
+    for labels in (y, y.clamp_min(-(1 << 30)).int()):
+        full = gc.gc_softmax_xent(X, W, labels, 1, 300, ws=ws)
+        with pytest.raises(gc.GCError) as e:
+            gc.gc_status(ws)
+        assert e.value.code == -7
+        only = gc.gc_softmax_xent(X, W, labels, 1, 300, dX=False, G=False, ws=ws)
+        with pytest.raises(gc.GCError):
+            gc.gc_status(ws)
+        assert torch.equal(only["row_loss"], full["row_loss"]) and torch.equal(only["loss"], full["loss"])
+        finite = torch.isfinite(full["lse"])
+        assert finite.sum().item() == 298 and torch.equal(only["lse"][finite], full["lse"][finite])
+        assert not torch.isfinite(only["lse"][~finite]).any()
+
+
 def test_nonfinite_rows_stay_in_their_chunk(gc):
     X, W, y = _data(3, 40, 64, 500, "bf16", "bf16", 8, ignore=0)
     want = gc.gc_softmax_xent(X, W, y, 3, 40)
