@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / 
         float t[8];
         r[q].values(t);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[q][j] += t[j];
+        for (int j = 0; j < 4; ++j) put(v[q], j, __fadd2_rn(two(v[q], j), two(t, j)));
       }
     }
     if (AHEAD && row + step < a.rows) fetch(row + step);
@@ -127,22 +127,25 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / 
         store_seg<VEC>((T*)a.h + row * a.ldh, (q * WPR + warp) * kSeg, lane, a.cols, v[q]);
     }
     // the warp's sum, and its squares about its own mean
-    float s = 0.f;
+    float2 pair = both(0.f);
 #pragma unroll
     for (int q = 0; q < VPT; ++q)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s += v[q][j];
-    s = warp_sum(s);
+      for (int j = 0; j < 4; ++j) pair = __fadd2_rn(pair, two(v[q], j));
+    const float s = warp_sum(pair.x + pair.y);
     const float mu_w = div_by(s, fn_w, inv_w);
-    float m2 = 0.f;
+    pair = both(0.f);
 #pragma unroll
     for (int q = 0; q < VPT; ++q)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float d = v[q][j] - mu_w;
-        if (in_row<VEC>((q * WPR + warp) * kSeg, lane, j, a.cols)) m2 = fmaf(d, d, m2);
+      for (int j = 0; j < 4; ++j) {
+        float2 d = __fadd2_rn(two(v[q], j), both(-mu_w));
+        const int col0 = (q * WPR + warp) * kSeg;
+        if (!in_row<VEC>(col0, lane, 2 * j, a.cols)) d.x = 0.f;
+        if (!in_row<VEC>(col0, lane, 2 * j + 1, a.cols)) d.y = 0.f;
+        pair = __ffma2_rn(d, d, pair);
       }
-    m2 = warp_sum(m2);
+    const float m2 = warp_sum(pair.x + pair.y);
     float mu = mu_w, M2 = m2;
     if (WPR > 1) {
       if (lane == 0) part[flip][warp] = make_float2(s, m2);
@@ -165,7 +168,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / 
       load_cols<VEC>(a.gamma, 1.f, a.vec_cols, col0, lane, a.cols, g);
       load_cols<VEC>(a.beta, 0.f, a.vec_cols, col0, lane, a.cols, b);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[q][j] = fmaf((v[q][j] - mu) * rstd, g[j], b[j]);
+      for (int j = 0; j < 4; ++j)
+        put(v[q], j, __ffma2_rn(__fmul2_rn(__fadd2_rn(two(v[q], j), both(-mu)), both(rstd)), two(g, j), two(b, j)));
       store_seg<VEC>((T*)a.y + row * a.ldy, col0, lane, a.cols, v[q]);
     }
   }
@@ -251,7 +255,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? kGradThread
   for (; r < r_end; r += RPB, flip ^= 1) {
     const long long row = first + r;
     float d[Q][8], n[Q][8];
-    float c1 = 0.f, c2 = 0.f;
+    float2 p1 = both(0.f), p2 = both(0.f);
     RawSeg<VEC, T> ya[Q];
     const float scale = rstd;
 #pragma unroll
@@ -263,22 +267,22 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? kGradThread
       xh[q].values(n[q]);
       ya[q] = xa[q];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        n[q][j] = (n[q][j] - mu) * scale;
+      for (int j = 0; j < 4; ++j) {
+        // past the row's end h is not the mean, but dy is zero, and gamma finite
+        const float2 y = two(d[q], j), x = __fmul2_rn(__fadd2_rn(two(n[q], j), both(-mu)), both(scale));
         if (SUMS) {
-          sg[q][j] = fmaf(d[q][j], n[q][j], sg[q][j]);
-          sb[q][j] += d[q][j];
+          put(sg[q], j, __ffma2_rn(y, x, two(sg[q], j)));
+          put(sb[q], j, __fadd2_rn(y, two(sb[q], j)));
         }
-        d[q][j] *= g[j];
-        if (in_row<VEC>(col0, lane, j, a.cols)) {  // past the row's end n is not zero
-          c1 += d[q][j];
-          c2 = fmaf(d[q][j], n[q][j], c2);
-        }
+        const float2 e = __fmul2_rn(y, two(g, j));
+        p1 = __fadd2_rn(p1, e);
+        p2 = __ffma2_rn(e, x, p2);
+        put(n[q], j, x);
+        put(d[q], j, e);
       }
     }
     if (r + RPB < r_end) fetch(row + RPB);
-    c1 = warp_sum(c1);
-    c2 = warp_sum(c2);
+    float c1 = warp_sum(p1.x + p1.y), c2 = warp_sum(p2.x + p2.y);
     if (WPR > 1) {
       if (lane == 0) part[flip][warp] = make_float2(c1, c2);
       __syncthreads();
@@ -291,12 +295,12 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? kGradThread
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       const int col0 = (q * WPR + warp) * kSeg;
-      float t[8];
+      float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (a.dh) ya[q].values(t);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float v = scale * (d[q][j] - c1 - n[q][j] * c2);
-        d[q][j] = a.dh ? v + t[j] : v;
+      for (int j = 0; j < 4; ++j) {
+        const float2 e = __ffma2_rn(two(n[q], j), both(-c2), __fadd2_rn(two(d[q], j), both(-c1)));
+        put(d[q], j, __ffma2_rn(e, both(scale), two(t, j)));
       }
       if (a.dres) store_seg<VEC>((T*)a.dres + row * a.lddr, col0, lane, a.cols, d[q]);
       if (a.dx) {

@@ -84,6 +84,14 @@ __device__ __forceinline__ void load_seg(const T* row, int col0, int lane, int c
   r.load(row, col0, lane, cols);
   r.values(v);
 }
+// Values 2j, 2j + 1 of a segment for the two-wide instructions.
+__device__ __forceinline__ float2 two(const float (&v)[8], int j) { return make_float2(v[2 * j], v[2 * j + 1]); }
+__device__ __forceinline__ void put(float (&v)[8], int j, float2 x) {
+  v[2 * j] = x.x;
+  v[2 * j + 1] = x.y;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 // Whether value j of the segment is a column of the row: all of a lane's eight are, or none, when VEC.
 template <bool VEC>
 __device__ __forceinline__ bool in_row(int col0, int lane, int j, int cols) {
@@ -157,9 +165,10 @@ __device__ __forceinline__ void drop_seg(const Mask& m, long long row, int col0,
   const uint32_t th = m.t << 16;
   if (VEC) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t u = j % 2 ? x[j / 2] : x[j / 2] << 16;  // th's low half is zero
-      v[j] = u >= th ? v[j] * m.scale : 0.f;
+    for (int j = 0; j < 4; ++j) {
+      const float2 y = __fmul2_rn(two(v, j), both(m.scale));
+      v[2 * j] = x[j] << 16 >= th ? y.x : 0.f;  // th's low half is zero
+      v[2 * j + 1] = x[j] >= th ? y.y : 0.f;
     }
   } else {
     uint32_t bits = 0;
