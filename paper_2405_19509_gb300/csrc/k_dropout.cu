@@ -7,7 +7,8 @@
 // instructions an element against four to six bytes of it.  A 32-bit number an element would double
 // that; 2^-16 is the resolution of p instead, and the scale is that of the p that is drawn, so that
 // the expectation of D(x) is x.  A warp takes 256 columns of a row at a time.  32,768 rows of 4096 bf16
-// with residual, 805 MB: 128 to 130 us, 6.2 to 6.3 TB/s (136 with the rounds' keys formed in the kernel).
+// with residual, 805 MB: 126 us, 6.4 TB/s (136 with the rounds' keys formed in the kernel and eight blocks an
+// SM).
 #include <algorithm>
 
 #include "rowwise.cuh"
@@ -52,9 +53,10 @@ int go(const void* x, int64_t ldx, const void* res, int64_t ldr, void* out, int6
        int cols, const Mask& m, cudaStream_t s) {
   const int nseg = (cols + kSeg - 1) / kSeg;
   const long long warps = rows * nseg;
-  // as many blocks as are resident at once, each warp with several segments to follow
+  // blocks an SM, each warp with several segments to follow: bf16 with residual (805 MB) 139, 130, 126, 132 us by
+  // 4, 5, 6, 8, fp32 (773 MB) 121, 126, 129, 136
   const long long grid = std::min<long long>((warps * 32 + kThreadsD - 1) / kThreadsD,
-                                             (long long)device_sm_count() * 8);
+                                             (long long)device_sm_count() * (sizeof(T) == 2 ? 6 : 4));
   const long long W = grid * (kThreadsD / 32);
   k_dropout<T, VEC, RES><<<(unsigned)grid, kThreadsD, 0, s>>>(
       (const T*)x, ldx, (const T*)res, ldr, (T*)out, ldo, rows, cols, nseg, W / nseg, (int)(W % nseg), m);
