@@ -74,8 +74,8 @@ struct NormArgs {
 // TPR threads a row, VPT segments a warp of them.  A warp a row: four rows a block, no barrier.  Up to two
 // segments a warp the next row is on its way while this one is worked on.  What bounds it then is the
 // instructions: a row's exchange is the same hundred a lane for one segment or for two.  (16,384 rows of
-// 4096 bf16 with dropout and residual, 537 MB: four segments and no row ahead 155 us, one and a row ahead 105, two 102;
-// 65,536 rows of 1024: one 110, two 100.)
+// 4096 bf16 with dropout and residual, 537 MB: four segments and no row ahead 155 us, one and a row ahead 105, two 102,
+// and 92 with two-wide arithmetic; 65,536 rows of 1024: one 110, two 100, two-wide 91.)
 template <typename T, bool VEC, int TPR, int VPT>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? 8 : 1024 / TPR)
     k_norm(NormArgs a) {
@@ -180,7 +180,11 @@ int go_norm(const NormArgs& a, cudaStream_t s) {
   constexpr int RPB = TPR == 32 ? 4 : 1;
   constexpr int threads = TPR == 32 ? 128 : TPR;
   const long long blocks = (a.rows + RPB - 1) / RPB;
-  const long long grid = std::min<long long>(blocks, (long long)device_sm_count() * (1024 / threads));
+  // bf16 rows without dropout leave the SMs idle half the time, and fewer rows at once suit the memory better:
+  // 16,384 rows of 4096 with residual 85 us by 768 threads an SM, 96 by 1024 (with dropout 96 and 92; fp32 113
+  // and 103).
+  const int per_sm = sizeof(T) == 2 && !a.m.t && threads <= 256 ? 768 : 1024;
+  const long long grid = std::min<long long>(blocks, (long long)device_sm_count() * (per_sm / threads));
   k_norm<T, VEC, TPR, VPT><<<(unsigned)grid, threads, 0, s>>>(a);
   count_launches(1);
   return cuda_check(cudaGetLastError(), "k_norm");
@@ -217,7 +221,8 @@ struct NormGradArgs {
 // TPR threads a row, two segments a warp; a block takes a slice of a chunk's rows, the next one on its way
 // while one is worked on.  SUMS: the column sums for G as well.  512 threads an SM have registers for
 // all that.  (16,384 rows of 4096 bf16 with residual, 671 MB, with dropout and without it: no row ahead 168 us;
-// one segment a warp, 1024 threads 144 and 123; two 133 and 125; two, 768 threads, which spill, 179 and 165.)
+// one segment a warp, 1024 threads 144 and 123; two 133 and 125; two, 768 threads, which spill, 179 and 165;
+// two with two-wide arithmetic 129 and 123.)
 constexpr int kGradSegs = 2;
 constexpr int kGradThreads = 512;  // an SM
 template <typename T, bool VEC, int TPR, bool SUMS>
