@@ -447,10 +447,11 @@ __global__ void __launch_bounds__(kThreadsX, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   uint8_t* store_box = smem + ring_bytes(MODE);  // boxes(MODE) an epilogue warp
-  uint64_t* full = reinterpret_cast<uint64_t*>(store_box + kEpi * boxes(MODE) * BOX);  // a leader's: its pair's loads landed
-  uint64_t* empty = full + kMaxStages;                         // each CTA's: every pair's MMAs on the stage are done
-  uint64_t* tfull = empty + kMaxStages;                        // [2] each CTA's: accumulator filled
-  uint64_t* tempty = tfull + 2;                                // [2] the leader's: drained by both CTAs
+  // a leader's: its pair's loads landed; each CTA's: every pair's MMAs on the stage are done
+  uint64_t* full = reinterpret_cast<uint64_t*>(store_box + kEpi * boxes(MODE) * BOX);
+  uint64_t* empty = full + kMaxStages;
+  uint64_t* tfull = empty + kMaxStages;  // [2] each CTA's: accumulator filled
+  uint64_t* tempty = tfull + 2;          // [2] the leader's: drained by both CTAs
   uint64_t* done = tempty + 2;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
@@ -676,8 +677,9 @@ __global__ void __launch_bounds__(kThreadsX, 1)
 }
 
 // bf16 parts [parts][rows][Cp] of a matrix: hi = bf16(x), lo = bf16(x - hi), zero from C to Cp.  A block
-// a row at a time, or a warp (WPR = 1: short rows).  With labels: lab = the label as an int, kNone where there is none.  The products
-// that follow multiply such a row by zeros, so what is not finite in it enters as zero (kNoneBad).
+// a row at a time, or a warp (WPR = 1: short rows).  With labels: lab = the label as an int, kNone where
+// there is none.  The products that follow multiply such a row by zeros, so what is not finite in it, or
+// would not be in bf16, enters as zero (kNoneBad).
 template <typename T, bool VEC, int WPR>
 __global__ void __launch_bounds__(256)
     k_xent_parts(const T* __restrict__ x, long long ld, long long rows, int C, int Cp, int parts,
@@ -700,7 +702,7 @@ __global__ void __launch_bounds__(256)
       if (!live) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (!isfinite(v[j])) {
+          if (!(fabsf(v[j]) < 3.38e38f)) {
             v[j] = 0.f;
             bad = 1;
           }

@@ -281,6 +281,19 @@ def test_label_past_the_vocabulary_is_reported(gc):
 
 
 @pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_rows_without_a_label_at_the_end_of_the_range(gc, x):
+    """The largest fp32 values round to infinity in bf16: in a row without a label they leave no trace."""
+    X, W, y = _data(2, 20, 64, 200, x, "bf16", 33, ignore=0)
+    y[3] = -1
+    want = gc.gc_softmax_xent(X, W, y, 2, 20)
+    X[3] = 3.4e38 if x == "f32" else float("inf")
+    got = gc.gc_softmax_xent(X, W, y, 2, 20)
+    live = y >= 0
+    assert torch.equal(got["G"], want["G"]) and torch.equal(got["dX"], want["dX"])
+    assert torch.equal(got["lse"][live], want["lse"][live])
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
 def test_losses_alone_of_labels_that_are_none(gc, x):
     """Losses alone take the labels and bf16 rows as they lie: negative labels, labels past the vocabulary
     and rows without a label that are not finite give what they give with the gradient."""
