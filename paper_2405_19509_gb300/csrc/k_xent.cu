@@ -723,21 +723,30 @@ __global__ void __launch_bounds__(256)
   }
 }
 
+// (m, s) += (m2, s2), the largest value and the sum of exponentials about it.
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
+  const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+  s = s * ex2((m - ref) * kLog2e) + s2 * ex2((m2 - ref) * kLog2e);
+  m = top;
+}
+
 // The loss of one point: the W rows stream once through registers, where a tile of the tensor cores
 // would be nearly empty.  Bound: HBM.  A warp takes four neighbouring rows of W at a time, with the next two
 // segments of them on their way; x lies in shared memory as fp32 in the order in which lanes read it,
-// and the largest value and the sum of exponentials of a warp's rows stay in registers.  One slot of
-// `part` a block.  (C = 2048, V = 65536 bf16, 268 MB: 46 us, 5.8 TB/s; 58 with the loads of a segment
-// issued when it is wanted; the tile kernel 54 for any number of points up to 256, and two points here 65.)
+// and the largest value and the sum of exponentials of a warp's rows stay in registers.  The last block
+// to finish joins the blocks' sums, in their order.  (C = 2048, V = 65536 bf16, 268 MB: 46 us, 5.8 TB/s; 58
+// with the loads of a segment issued when it is wanted; the tile kernel 54 for any number of points up to
+// 256, and two points here 65.)
 constexpr int kFewRows = 4;
 template <typename TX, typename TW, bool VEC>
 __global__ void __launch_bounds__(256)
     k_xent_one(const TX* __restrict__ X, const TW* __restrict__ W, long long ldw, int C, int V,
-               const void* __restrict__ y, int y64, int* __restrict__ lab, float* __restrict__ target,
-               float2* __restrict__ part, uint32_t* status) {
+               const void* __restrict__ y, int y64, float* target, float2* part, float* lse, float* lse_out,
+               float* row_loss, double* loss, unsigned int* counter, uint32_t* status) {
   using namespace rowwise;
   extern __shared__ __align__(16) float xs[];  // [segments][2][32][4]
   __shared__ float2 red[8];
+  __shared__ int last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int nseg = (C + kSeg - 1) / kSeg;
   start_next();
@@ -755,10 +764,7 @@ __global__ void __launch_bounds__(256)
   }
   const long long l = y64 ? *reinterpret_cast<const long long*>(y) : *reinterpret_cast<const int*>(y);
   const int label = l >= 0 && l < V ? (int)l : kNone;
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    *lab = label;
-    if (l >= V) atomicOr(status, ST_BAD_LABEL);
-  }
+  if (blockIdx.x == 0 && threadIdx.x == 0 && l >= V) atomicOr(status, ST_BAD_LABEL);
   __syncthreads();
   float m = -INFINITY, s = 0.f;
   const long long step = (long long)gridDim.x * 8 * kFewRows;
@@ -814,14 +820,37 @@ __global__ void __launch_bounds__(256)
   if (lane == 0) red[warp] = make_float2(m, s);
   __syncthreads();
   if (threadIdx.x == 0) {
-    float M = -INFINITY, S = 0.f;
-    for (int w = 0; w < 8; ++w) {
-      const float2 q = red[w];
-      const float top = fmaxf(M, q.x), ref = top == -INFINITY ? 0.f : top;
-      S = S * ex2((M - ref) * kLog2e) + q.y * ex2((q.x - ref) * kLog2e);
-      M = top;
-    }
-    part[blockIdx.x] = make_float2(M, S);
+#pragma unroll
+    for (int w = 1; w < 8; ++w) join(m, s, red[w].x, red[w].y);
+    part[blockIdx.x] = make_float2(m, s);
+    __threadfence();
+    // the counter is back at zero for the next call
+    last = atomicInc(counter, gridDim.x - 1) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  m = -INFINITY;
+  s = 0.f;
+  for (int k = threadIdx.x; k < (int)gridDim.x; k += 256) {
+    const float2 q = __ldcg(part + k);
+    join(m, s, q.x, q.y);
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
+    join(m, s, m2, s2);
+  }
+  if (lane == 0) red[warp] = make_float2(m, s);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) join(m, s, red[w].x, red[w].y);
+    const float v = m + logf(s), r = label >= 0 ? v - __ldcg(target) : 0.f;
+    *lse = v;
+    if (lse_out) *lse_out = v;
+    if (row_loss) *row_loss = r;
+    if (loss) *loss = (double)r;
   }
 }
 
@@ -856,13 +885,6 @@ __global__ void __launch_bounds__(256) k_xent_dx(const float* __restrict__ part,
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (c + e < C) dX[row * ld_dx + c + e] = rowwise::from_f<T>(v[e]);
-}
-
-// (m, s) += (m2, s2), the largest value and the sum of exponentials about it.
-__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
-  const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-  s = s * ex2((m - ref) * kLog2e) + s2 * ex2((m2 - ref) * kLog2e);
-  m = top;
 }
 
 // lse and loss of the rows from their n partial sums [n][T].  A block takes R rows: a warp's lanes are R
@@ -1028,22 +1050,24 @@ int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts
 
 int tiles(long long n, int wide = TILE) { return (int)((n + wide - 1) / wide); }
 
-// The form for one point, and its blocks (two an SM; each a slot of `part`).
+// The form for one point, and its blocks (two an SM; each a slot of `part`).  It counts finished blocks in a
+// word of the workspace header, zero between calls.
+constexpr int kOneCounter = 7;
 constexpr size_t kOneSmem = 64 * 1024;
 size_t one_smem(int C) { return (size_t)(C + rowwise::kSeg - 1) / rowwise::kSeg * rowwise::kSeg * sizeof(float); }
 bool one_point(long long T, int C) { return T == 1 && one_smem(C) <= kOneSmem; }
 int one_blocks(int V) { return std::min((V + 8 * kFewRows - 1) / (8 * kFewRows), 2 * device_sm_count()); }
 
 template <typename TX, typename TW>
-int launch_one(const XentShape& s, const XentIO& io, int* lab, float* target, float2* part, uint32_t* status,
+int launch_one(const XentShape& s, const XentIO& io, float* target, float2* part, float* lse, uint32_t* status,
                cudaStream_t st) {
   const bool vec = s.C % 8 == 0 && rowwise::rows_16(io.W, io.ldw, sizeof(TW));
   auto* kern = vec ? k_xent_one<TX, TW, true> : k_xent_one<TX, TW, false>;
   static SmemOptIn allow[2];
   GC_CUDA(allow[vec](kern, kOneSmem));
   return launch_chain(kern, "k_xent_one", (unsigned)one_blocks(s.V), 256, one_smem(s.C), 1, false, st,
-                      (const TX*)io.X, (const TW*)io.W, (long long)io.ldw, s.C, s.V, io.y, io.y64, lab, target, part,
-                      status);
+                      (const TX*)io.X, (const TW*)io.W, (long long)io.ldw, s.C, s.V, io.y, io.y64, target, part, lse,
+                      io.lse, io.row_loss, io.loss, status + kOneCounter, status);
 }
 
 // Columns of a piece: as many as kPieceElems of P allow, the pieces of one width.
@@ -1173,12 +1197,11 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   int rc = GC_OK;
   Labels lab{w.lab, nullptr, 0, s.V};
   if (w.one) {
-    rc = xb ? wb ? launch_one<__nv_bfloat16, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
-                 : launch_one<__nv_bfloat16, float>(s, io, w.lab, w.target, w.part, status, st)
-            : wb ? launch_one<float, __nv_bfloat16>(s, io, w.lab, w.target, w.part, status, st)
-                 : launch_one<float, float>(s, io, w.lab, w.target, w.part, status, st);
-    if (rc) return rc;
-    if (!s.want) return join_rows(w, one_blocks(s.V), T, lab, io, status, st);
+    rc = xb ? wb ? launch_one<__nv_bfloat16, __nv_bfloat16>(s, io, w.target, w.part, w.lse, status, st)
+                 : launch_one<__nv_bfloat16, float>(s, io, w.target, w.part, w.lse, status, st)
+            : wb ? launch_one<float, __nv_bfloat16>(s, io, w.target, w.part, w.lse, status, st)
+                 : launch_one<float, float>(s, io, w.target, w.part, w.lse, status, st);
+    if (rc || !s.want) return rc;
   }
   // losses alone read bf16 rows where they lie; the products of the gradient want a copy that is finite
   const bool x_in_place = !s.want && xb && rowwise::rows_16(io.X, io.ldx, 2);
@@ -1231,8 +1254,8 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   if (!w.one) {
     rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, mX, chained, st) : run_z<STAT, 2>(p, mX, mW, mX, chained, st);
     if (rc) return rc;
+    if ((rc = join_rows(w, 2 * tiles(s.V), T, lab, io, status, st))) return rc;
   }
-  if ((rc = join_rows(w, w.one ? one_blocks(s.V) : 2 * tiles(s.V), T, lab, io, status, st))) return rc;
   if (!(s.want & (XENT_DX | XENT_G))) return GC_OK;
 
   const long long d4x[4] = {w.Cp, s.n_c, s.N, w.nx};
