@@ -734,9 +734,9 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
 // would be nearly empty.  Bound: HBM.  A warp takes four neighbouring rows of W at a time, with the next two
 // segments of them on their way; x lies in shared memory as fp32 in the order in which lanes read it,
 // and the largest value and the sum of exponentials of a warp's rows stay in registers.  The last block
-// to finish joins the blocks' sums, in their order.  (C = 2048, V = 65536 bf16, 268 MB: 46 us, 5.8 TB/s; 58
-// with the loads of a segment issued when it is wanted; the tile kernel 54 for any number of points up to
-// 256, and two points here 65.)
+// to finish joins the blocks' sums, in their order.  (C = 2048, V = 65536 bf16, 268 MB: 51 us a call, 5.3
+// TB/s; 64 with the loads of a segment issued when it is wanted; the tile kernel takes 59 for any number of
+// points up to 256, and two points here 71.)
 constexpr int kFewRows = 4;
 template <typename TX, typename TW, bool VEC>
 __global__ void __launch_bounds__(256)
@@ -1050,13 +1050,16 @@ int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts
 
 int tiles(long long n, int wide = TILE) { return (int)((n + wide - 1) / wide); }
 
-// The form for one point, and its blocks (two an SM; each a slot of `part`).  It counts finished blocks in a
-// word of the workspace header, zero between calls.
+// The form for one point, and its blocks (each a slot of `part`): three an SM for bf16 rows (the registers' limit;
+// 268 MB: 56, 51, 57 us by 2, 3, 4), two for fp32 ones (131 MB: 28, 30, 30).  It counts finished blocks in a word
+// of the workspace header, zero between calls.
 constexpr int kOneCounter = 7;
 constexpr size_t kOneSmem = 64 * 1024;
 size_t one_smem(int C) { return (size_t)(C + rowwise::kSeg - 1) / rowwise::kSeg * rowwise::kSeg * sizeof(float); }
 bool one_point(long long T, int C) { return T == 1 && one_smem(C) <= kOneSmem; }
-int one_blocks(int V) { return std::min((V + 8 * kFewRows - 1) / (8 * kFewRows), 2 * device_sm_count()); }
+int one_blocks(const XentShape& s) {
+  return std::min((s.V + 8 * kFewRows - 1) / (8 * kFewRows), (s.w_dtype == GC_BF16 ? 3 : 2) * device_sm_count());
+}
 
 template <typename TX, typename TW>
 int launch_one(const XentShape& s, const XentIO& io, float* target, float2* part, float* lse, uint32_t* status,
@@ -1065,7 +1068,7 @@ int launch_one(const XentShape& s, const XentIO& io, float* target, float2* part
   auto* kern = vec ? k_xent_one<TX, TW, true> : k_xent_one<TX, TW, false>;
   static SmemOptIn allow[2];
   GC_CUDA(allow[vec](kern, kOneSmem));
-  return launch_chain(kern, "k_xent_one", (unsigned)one_blocks(s.V), 256, one_smem(s.C), 1, false, st,
+  return launch_chain(kern, "k_xent_one", (unsigned)one_blocks(s), 256, one_smem(s.C), 1, false, st,
                       (const TX*)io.X, (const TW*)io.W, (long long)io.ldw, s.C, s.V, io.y, io.y64, target, part, lse,
                       io.lse, io.row_loss, io.loss, status + kOneCounter, status);
 }
@@ -1110,7 +1113,7 @@ XentScratch carve_xent(Carve& c, const XentShape& s) {
   w.lse = c.take<float>((size_t)T);
   w.target = c.take<float>((size_t)T);
   w.row_loss = c.take<float>((size_t)T);
-  w.part = c.take<float2>((size_t)T * (w.one ? one_blocks(s.V) : 2 * tiles(s.V)));
+  w.part = c.take<float2>((size_t)T * (w.one ? one_blocks(s) : 2 * tiles(s.V)));
   if (s.want & (XENT_DX | XENT_G)) {
     w.piece = piece_cols(T, s.V);
     w.np = (s.want & XENT_G) || s.x_dtype == GC_F32 ? 2 : 1;
