@@ -214,31 +214,25 @@ __device__ __forceinline__ float pick(const float (&v)[64], int at) {
   return w[0];
 }
 
-// 32 consecutive fp32 values of a row of an output; n: how many of them exist.
+// 32 consecutive values of a row of an output on a 16-byte boundary.
 template <typename T>
-__device__ __forceinline__ void store_row(T* dst, const float (&v)[32], int n, bool vec) {
-  if (n >= 32 && vec) {
-    if (sizeof(T) == 4) {
+__device__ __forceinline__ void store_row(T* dst, const float (&v)[32]) {
+  if (sizeof(T) == 4) {
 #pragma unroll
-      for (int j = 0; j < 32; j += 4)
-        *reinterpret_cast<float4*>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-    } else {
+    for (int j = 0; j < 32; j += 4)
+      *reinterpret_cast<float4*>(dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+  } else {
 #pragma unroll
-      for (int j = 0; j < 32; j += 8) {
-        uint32_t w[4];
+    for (int j = 0; j < 32; j += 8) {
+      uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const __nv_bfloat162 t = __floats2bfloat162_rn(v[j + 2 * e], v[j + 2 * e + 1]);
-          w[e] = *reinterpret_cast<const uint32_t*>(&t);
-        }
-        *reinterpret_cast<uint4*>(dst + j) = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int e = 0; e < 4; ++e) {
+        const __nv_bfloat162 t = __floats2bfloat162_rn(v[j + 2 * e], v[j + 2 * e + 1]);
+        w[e] = *reinterpret_cast<const uint32_t*>(&t);
       }
+      *reinterpret_cast<uint4*>(dst + j) = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    return;
   }
-#pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (j < n) dst[j] = rowwise::from_f<T>(v[j]);
 }
 
 // Row `lane` of a box: 16-byte piece j lies at j ^ (row mod 8), which makes both the rows' and the
@@ -266,6 +260,16 @@ __device__ __forceinline__ void box_row_half(uint8_t* box, int lane, int first, 
 __device__ __forceinline__ void box_free(int lane) {
   if (lane == 0) bulk_wait_read<0>();
   __syncwarp();
+}
+// The box's rows in turn, a lane a column, U at a time: f(row, value) for outputs whose rows lie on no 16-byte
+// boundary.
+template <int U, typename F>
+__device__ __forceinline__ void by_rows(const uint8_t* box, int lane, int rows, F f) {
+#pragma unroll U
+  for (int r = 0; r < 32; ++r) {
+    const float x = *reinterpret_cast<const float*>(box + r * 128 + (((lane / 4) ^ (r & 7)) * 16) + lane % 4 * 4);
+    if (r < rows) f(r, x);
+  }
 }
 // What the warp wrote to its box is there for a store, which lane 0 issues.
 __device__ __forceinline__ void box_ready() {
@@ -354,11 +358,11 @@ __device__ __forceinline__ void store_grad(const XentParams& p, const TileAt& t,
                                            const CUtensorMap* mOut, const CUtensorMap* mAcc, Get get) {
   const int lane = threadIdx.x & 31;
   if (t.kind == 1) {
-    const bool rv = row_in < p.T;
     const bool out = p.last_piece && p.dx_bf16 && !p.split;  // the sum is complete and leaves in bf16
     const bool first = p.first_piece || p.split;
     float* acc = p.acc + (p.split ? (size_t)t.range * p.T * p.ld_acc : 0);
-    const bool vec = p.ld_acc % 4 == 0 && reinterpret_cast<uintptr_t>(p.acc) % 16 == 0;
+    const bool vec = p.ld_acc % 4 == 0 && reinterpret_cast<uintptr_t>(p.acc) % 16 == 0 &&
+                     (!out || (p.ld_dx % 8 == 0 && reinterpret_cast<uintptr_t>(p.dX) % 16 == 0));
 #pragma unroll
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
@@ -379,30 +383,38 @@ __device__ __forceinline__ void store_grad(const XentParams& p, const TileAt& t,
         }
         continue;
       }
-      if (!rv) continue;
+      if (!vec || n < 32) {
+        box_free(lane);
+        box_row(box, lane, v);
+        __syncwarp();
+        float* a = acc + (row_in - lane) * p.ld_acc + col + lane;
+        __nv_bfloat16* o = (__nv_bfloat16*)p.dX + (row_in - lane) * p.ld_dx + col + lane;
+        const long long rows = p.T - (row_in - lane);
+        by_rows<2>(box, lane, lane < n ? (int)min(rows, 32LL) : 0, [&](int r, float x) {
+          if (!first) x += a[r * p.ld_acc];
+          if (out)
+            o[r * p.ld_dx] = __float2bfloat16_rn(x);
+          else
+            a[r * p.ld_acc] = x;
+        });
+        continue;
+      }
+      if (row_in >= p.T) continue;
       float* a = acc + row_in * p.ld_acc + col;
       if (!first) {
-        if (vec && n >= 32) {
 #pragma unroll
-          for (int j = 0; j < 32; j += 4) {
-            const float4 q = *reinterpret_cast<const float4*>(a + j);
-            v[j] += q.x;
-            v[j + 1] += q.y;
-            v[j + 2] += q.z;
-            v[j + 3] += q.w;
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (j < n) v[j] += a[j];
+        for (int j = 0; j < 32; j += 4) {
+          const float4 q = *reinterpret_cast<const float4*>(a + j);
+          v[j] += q.x;
+          v[j + 1] += q.y;
+          v[j + 2] += q.z;
+          v[j + 3] += q.w;
         }
       }
-      if (out) {
-        __nv_bfloat16* o = (__nv_bfloat16*)p.dX + row_in * p.ld_dx + col;
-        store_row(o, v, n, p.ld_dx % 8 == 0 && reinterpret_cast<uintptr_t>(p.dX) % 16 == 0);
-      } else {
-        store_row(a, v, n, vec);
-      }
+      if (out)
+        store_row((__nv_bfloat16*)p.dX + row_in * p.ld_dx + col, v);
+      else
+        store_row(a, v);
     }
   } else {
     const int lv = (int)row_in;  // row of the piece
@@ -421,15 +433,11 @@ __device__ __forceinline__ void store_grad(const XentParams& p, const TileAt& t,
           store_3d(mOut, box, col, p.v0 + lv, t.chunk);
           bulk_commit();
         }
-      } else {  // row by row, 32 neighbouring values a store
+      } else {
         __syncwarp();
         float* g = p.G + t.chunk * p.ldg + (long long)(p.v0 + lv - lane) * p.C + col + lane;
-        const int rows = p.w - (lv - lane);
-#pragma unroll 8
-        for (int r = 0; r < 32; ++r) {
-          const float x = *reinterpret_cast<const float*>(box + r * 128 + (((lane / 4) ^ (r & 7)) * 16) + lane % 4 * 4);
-          if (r < rows && lane < n) g[(long long)r * p.C] = x;
-        }
+        by_rows<8>(box, lane, lane < n ? min(p.w - (lv - lane), 32) : 0,
+                   [&](int r, float x) { g[(long long)r * p.C] = x; });
       }
     }
   }
@@ -888,7 +896,8 @@ __global__ void __launch_bounds__(256) k_xent_dx(const float* __restrict__ part,
 }
 
 // lse and loss of the rows from their n partial sums [n][T].  A block takes R rows: a warp's lanes are R
-// rows by 32 / R slots, its eight warps take the slots in turn (R = 32: whole 256-byte reads; 4: whole sectors, for few rows).
+// rows by 32 / R slots, its eight warps take the slots in turn (R = 32: whole 256-byte reads; 4: whole
+// sectors, for few rows).
 template <int R>
 __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ part, int n, long long T,
                                                   Labels lab, const float* __restrict__ target, uint32_t* status,
@@ -1299,7 +1308,9 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     rc = two_pairs(p.mt, p.w) ? run_z<PROB, 4>(p, mX2, mW, mPs, true, st)
                               : run_z<PROB, 2>(p, mX, mW, mPs, true, st);
     if (rc) return rc;
-    const bool two = T > HALF && two_pairs((s.want & XENT_DX ? (long long)p.mt * p.ks : 0) + (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0), s.C);
+    const long long row_tiles = (s.want & XENT_DX ? (long long)p.mt * p.ks : 0) +
+                                (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0);
+    const bool two = T > HALF && two_pairs(row_tiles, s.C);
     const long long dp[3] = {p.w, T, w.np};
     const long long d4[4] = {p.w, s.n_c, s.N, w.np};
     const long long l4[3] = {w.piece, (long long)s.n_c * w.piece, T * w.piece};
