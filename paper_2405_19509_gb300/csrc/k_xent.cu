@@ -13,8 +13,8 @@
 //
 // Bound: the tensor pipe.  Per row, column and value of C: one product for lse, one for P, one for
 // dX, and two for G, whose 32-bit result wants P to 2^-17, as bf16 hi + lo; a bf16 dX is rounded to 2^-8,
-// and so are the operands that make it.  fp32 X and W enter as hi + lo too (X_hi W_hi + X_hi W_lo + X_lo W_hi;
-// the dropped term is 2^-16 at most).  All sums are fp32.  z is not kept: T V values of it are gigabytes,
+// and takes P so too, the hi alone.  fp32 X and W enter as hi + lo too, W in a bf16 dX as well (X_hi W_hi +
+// X_hi W_lo + X_lo W_hi; the dropped term is 2^-16 at most).  All sums are fp32.  z is not kept: T V values of it are gigabytes,
 // while a piece of P is kPieceElems values.
 //
 // One persistent kernel shape: a pair of CTAs (cta_group::2) per 256 x 256 tile, each CTA holding
@@ -170,7 +170,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
     t.kb0 = (int)((long long)t.range * nkb / p.ks);
     t.nkb = (int)((long long)(t.range + 1) * nkb / p.ks) - t.kb0;
     t.na = p.np_dx;
-    t.nb = p.np_dx == 1 ? 1 : p.nw;
+    t.nb = p.nw;
     t.seg = p.dx_bf16 ? t.nkb : kSegment;
     return t;
   }
@@ -1172,11 +1172,11 @@ int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& m
   p.units = (int)std::min<long long>(n, (long long)p.ndx + p.ndw);
   // the units with one dX tile less take that much more of G
   p.r = p.ndx % p.units;
-  const int dx_a = p.np_dx, dx_b = p.np_dx == 1 ? 1 : p.nw, dx_prod = p.np_dx == 1 ? 1 : 1 + p.nw;
+  const int dx_prod = p.np_dx == 1 ? p.nw : 1 + p.nw;
   const double cost_dx = (double)((p.w + BK - 1) / BK) / p.ks * dx_prod;
   const double cost_dw = (double)((p.n_c + BK - 1) / BK) * (1 + p.nx);
   p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_dw + 0.5), p.ndw / (p.units - p.r));
-  p.stage_ops = std::max(p.ndx ? dx_a + dx_b : 0, p.ndw ? p.np + p.nx : 0);
+  p.stage_ops = std::max(p.ndx ? p.np_dx + p.nw : 0, p.ndw ? p.np + p.nx : 0);
   p.stages = ring_bytes(GRAD) / (p.stage_ops * OP_BYTES);
   return launch_mode<GRAD, CL>(mP, mWt, mP4, mX4, mG, mAcc, p, true, st);
 }

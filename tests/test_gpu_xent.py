@@ -395,3 +395,19 @@ def test_stall_times_out_then_recovers(gc):
     got = gc.gc_softmax_xent(X, W, y, 2, 300, ws=ws)
     gc.gc_status(ws)
     assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+@pytest.mark.parametrize("T,C", [(1, 40), (40, 96), (300, 257)])
+def test_row_gradient_keeps_the_digits_of_fp32_weights(gc, T, C):
+    """Two classes of equal logits: P is 1/2 and -1/2 and dX half the difference of W's rows, 1 + at most
+    2^-7 each, which W's first bf16 part alone does not hold.  Both parts are off by 2^-17 a row, P is off by
+    2^-20, two additions in tensor memory by 2^-23: 2^-15 together, beside dX's own rounding."""
+    g = torch.Generator(device="cuda").manual_seed(T + C)
+    W = 1 + (torch.rand(2, C, generator=g, device="cuda") - 0.5) * 2.0 ** -6
+    W[:, 0] = 0
+    X = torch.zeros(T, C, dtype=torch.bfloat16, device="cuda")
+    X[:, 0] = torch.randn(T, generator=g, device="cuda").bfloat16()
+    y = torch.randint(0, 2, (T,), generator=g, device="cuda")
+    want = 0.5 * (W[1 - y].double() - W[y].double())
+    got = gc.gc_softmax_xent(X, W, y, 1, T)["dX"].double()
+    assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -15).all()
