@@ -19,9 +19,8 @@
 //
 // One persistent kernel shape: a pair of CTAs (cta_group::2) per 256 x 256 tile, each CTA holding
 // 128 rows of A and of B for a 64-wide K block (warp 0, TMA), the leader's warp 1 issuing the MMAs,
-// eight warps per CTA draining one of two accumulators while the other is filled.  Clusters of four hold
-// two pairs on neighbouring column tiles, and each loads half of A's rows for both (multicast): a
-// quarter less from L2, on 144 SMs instead of 152.  MMAs and copies are issued by an elected lane of a
+// eight warps per CTA draining one of two accumulators while the other is filled.  Each CTA loads its own
+// rows: no copy goes to another SM.  MMAs and copies are issued by an elected lane of a
 // warp that stays together: from a branch on the lane a 64-wide K block took 900 clocks to issue where
 // its MMAs take 512.  Operands that lie with K outermost (W in dX, P and X in G) are read MN-major: boxes of
 // 64 columns x 64 K rows.  Rows past a chunk's end, columns past V and past C are zero-filled by TMA.  P, G
@@ -30,8 +29,7 @@
 //
 // 8,192 points, C = 2048, V = 65536, bf16: losses alone 1.2 ms, 1810 TFLOP/s, 93% of the rate of the library's
 // bf16 product (the tensor pipe is active 90% of the clocks), 1.65 ms with MMAs issued from a branch; with the
-// gradient in eight chunks 6.6 to 6.9 ms, 11.0 TFLOP issued at 1.6 to 1.67 PFLOP/s, near what the power limit
-// allows (1.7); with G in one sum, 6.4 ms, 6.9 in pairs alone, 8.3 from a branch.
+// gradient in eight chunks 7.0 ms, 11.0 TFLOP issued at 1.57 PFLOP/s, near what the power limit allows (1.7).
 #include <cudaTypedefs.h>
 
 #include <algorithm>
@@ -93,7 +91,7 @@ struct XentParams {
   int v0, w;           // PROB, GRAD: the piece is columns [v0, v0 + w)
   int np, np_dx;       // parts of P: kept, and that enter dX
   int mt, nt, group;   // tiles of T and of the columns; row tiles that share a sweep of the columns
-  int units;           // clusters; a cluster's tile is 256 x 128 times its CTAs
+  int units;           // clusters, one tile each at a time
   // rows of A that a CTA loads of X's and P's rows, and whether the second half of a tile has any: of a few
   // points no more than there are (the rows of the accumulator past them hold anything, and are not read)
   int a_rows, a_both;
@@ -140,8 +138,8 @@ __device__ __forceinline__ int tiles_of(const XentParams& p, int unit) {
   return ndx + (unit >= p.r ? p.extra : 0) + (rest - unit + p.units - 1) / p.units;
 }
 
-// The k-th tile of a unit; WIDE columns.
-template <int MODE, int WIDE>
+// The k-th tile of a unit.
+template <int MODE>
 __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) {
   TileAt t;
   if (MODE != GRAD) {
@@ -151,7 +149,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
     const int n = rem / gm;
     t.kind = 0;
     t.m0 = (g * p.group + rem - n * gm) * TILE;
-    t.n0 = n * WIDE;
+    t.n0 = n * TILE;
     t.chunk = t.kb0 = t.range = 0;
     t.nkb = (p.C + BK - 1) / BK;
     t.na = p.nx;
@@ -165,7 +163,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
     t.kind = 1;
     t.range = i - at * p.ks;
     t.m0 = at / p.ct * TILE;
-    t.n0 = at % p.ct * WIDE;
+    t.n0 = at % p.ct * TILE;
     t.chunk = 0;
     t.kb0 = (int)((long long)t.range * nkb / p.ks);
     t.nkb = (int)((long long)(t.range + 1) * nkb / p.ks) - t.kb0;
@@ -182,7 +180,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
   t.kb0 = t.range = 0;
   t.chunk = c;
   t.m0 = rem / p.ct * TILE;
-  t.n0 = rem % p.ct * WIDE;
+  t.n0 = rem % p.ct * TILE;
   t.nkb = (p.n_c + BK - 1) / BK;
   t.na = p.np;
   t.nb = p.nx;
@@ -446,7 +444,7 @@ __device__ __forceinline__ void store_grad(const XentParams& p, const TileAt& t,
 // Tensor maps: mA, mB of the first product (z: X and W rows; GRAD: P rows and W columns for dX), mP4
 // and mX4 (GRAD: P and X of a chunk, columns x points); of the stores, mOut (PROB: P; GRAD: G) and
 // mAcc (GRAD: the fp32 dX).
-template <int MODE, int CL>
+template <int MODE>
 __global__ void __launch_bounds__(kThreadsX, 1)
     k_xent(const __grid_constant__ CUtensorMap mA, const __grid_constant__ CUtensorMap mB,
            const __grid_constant__ CUtensorMap mP4, const __grid_constant__ CUtensorMap mX4,
@@ -455,7 +453,7 @@ __global__ void __launch_bounds__(kThreadsX, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   uint8_t* store_box = smem + ring_bytes(MODE);  // boxes(MODE) an epilogue warp
-  // a leader's: its pair's loads landed; each CTA's: every pair's MMAs on the stage are done
+  // the leader's: the pair's loads landed; each CTA's: the MMAs on the stage are done
   uint64_t* full = reinterpret_cast<uint64_t*>(store_box + kEpi * boxes(MODE) * BOX);
   uint64_t* empty = full + kMaxStages;
   uint64_t* tfull = empty + kMaxStages;  // [2] each CTA's: accumulator filled
@@ -465,14 +463,13 @@ __global__ void __launch_bounds__(kThreadsX, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int PAIRS = CL / 2, WIDE = PAIRS * TILE;
-  const int unit = blockIdx.x / CL;
-  const int rank = (int)cta_rank(), q = rank >> 1, half_m = rank & 1;  // the pair in the cluster, the half of its rows
+  const int unit = blockIdx.x / 2;
+  const int half_m = (int)cta_rank();  // the half of the pair's rows
   const int S = p.stages, stage_bytes = p.stage_ops * OP_BYTES;
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], PAIRS);
+      mbar_init(&empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(&tfull[a], 1);
@@ -494,13 +491,12 @@ __global__ void __launch_bounds__(kThreadsX, 1)
   const int ntiles = tiles_of<MODE>(p, unit);
   if (warp == 0) {
     const bool one = elect_one();
-    const uint16_t to = (uint16_t)(0x5 << half_m);  // the CTAs that hold the same rows of A
     uint32_t it = 0, ph = 0;
     int s = 0;
     bool ok = !p.stall;
     for (int k = 0; k < ntiles && ok; ++k) {
-      const TileAt t = tile_at<MODE, WIDE>(p, unit, k);
-      const int ma = t.m0 + half_m * HALF, nb = t.n0 + q * TILE + half_m * HALF;
+      const TileAt t = tile_at<MODE>(p, unit, k);
+      const int ma = t.m0 + half_m * HALF, nb = t.n0 + half_m * HALF;
       const bool rows_a = t.kind < 2, skip_a = rows_a && half_m == 1 && !p.a_both;
       const uint32_t bytes = 2 * t.nb * OP_BYTES + (rows_a ? t.na * p.a_rows * BK * 2 * (p.a_both ? 2 : 1)
                                                            : 2 * t.na * OP_BYTES);
@@ -512,21 +508,14 @@ __global__ void __launch_bounds__(kThreadsX, 1)
         }
         if (one) {
           if (half_m == 0) mbar_expect_tx(&full[s], bytes);
-          const uint32_t bar = at_rank(&full[s], q * 2);
+          const uint32_t bar = at_rank(&full[s], 0);
           uint8_t* st = smem + (size_t)s * stage_bytes;
           for (int i = 0; i < t.na; ++i, st += OP_BYTES) {
-            uint8_t* dst = st + q * (OP_BYTES / 2);
-            if (rows_a) {
-              if (skip_a) continue;
-              if (CL == 2)
-                load_3d(st, &mA, kb * BK, ma, i, bar);
-              else
-                load_3d_to(dst, &mA, kb * BK, ma + q * 64, i, bar, to);
-            } else if (CL == 2) {
+            if (!rows_a) {
               load_4d(st, &mP4, ma, kb * BK, t.chunk, i, bar);
               load_4d(st + OP_BYTES / 2, &mP4, ma + 64, kb * BK, t.chunk, i, bar);
-            } else {
-              load_4d_to(dst, &mP4, ma + q * 64, kb * BK, t.chunk, i, bar, to);
+            } else if (!skip_a) {
+              load_3d(st, &mA, kb * BK, ma, i, bar);
             }
           }
           for (int i = 0; i < t.nb; ++i, st += OP_BYTES) {
@@ -558,12 +547,12 @@ __global__ void __launch_bounds__(kThreadsX, 1)
   } else if (warp == 1) {
     if (half_m == 0) {
       const bool one = elect_one();
-      const uint16_t all = (uint16_t)((1 << CL) - 1), pair = (uint16_t)(3 << (2 * q));
+      const uint16_t pair = 3;
       uint32_t ph = 0, use = 0;  // use: accumulators filled so far, in turn the one and the other
       int s = 0;
       bool ok = true;
       for (int k = 0; k < ntiles && ok; ++k) {
-        const TileAt t = tile_at<MODE, WIDE>(p, unit, k);
+        const TileAt t = tile_at<MODE>(p, unit, k);
         const bool a_mn = t.kind == 2, b_mn = t.kind >= 1;
         const uint32_t idesc = idesc_256(a_mn, b_mn);
         const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
@@ -596,7 +585,7 @@ __global__ void __launch_bounds__(kThreadsX, 1)
                       (!opens || i + j + ks > 0) ? 1u : 0u);
               }
             }
-            commit_to(&empty[s], all);
+            commit_to(&empty[s], pair);
             if (closes) commit_to(&tfull[ab], pair);
           }
           __syncwarp();
@@ -629,14 +618,13 @@ __global__ void __launch_bounds__(kThreadsX, 1)
     auto release = [&] {
       fence_before();
       __syncwarp();
-      if (lane == 0) arrive_remote(at_rank(&tempty[use & 1], q * 2));
+      if (lane == 0) arrive_remote(at_rank(&tempty[use & 1], 0));
     };
     auto at = [&] {
       return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((use & 1) * TILE + half * HALF);
     };
     for (int k = 0; k < ntiles && ok; ++k) {
-      TileAt t = tile_at<MODE, WIDE>(p, unit, k);
-      t.n0 += q * TILE;
+      const TileAt t = tile_at<MODE>(p, unit, k);
       const long long row = (long long)t.m0 + half_m * HALF + quarter * 32 + lane;
       int lab = kNone;
       float l2 = 0.f;  // the row's lse, in powers of two
@@ -1010,8 +998,8 @@ int launch_chain(void (*kern)(P...), const char* name, unsigned grid, int block,
   return cuda_check(e, name);
 }
 
-// Clusters of CL CTAs that the current device holds at once.
-template <int MODE, int CL>
+// Pairs that the current device holds at once.
+template <int MODE>
 int resident(int* units) {
   static std::atomic<int> cache[64];
   int dev = 0, n = 0;
@@ -1019,29 +1007,29 @@ int resident(int* units) {
   if (dev >= 0 && dev < 64) n = cache[dev].load(std::memory_order_relaxed);
   if (n == 0) {
     static SmemOptIn allow;
-    GC_CUDA(allow(k_xent<MODE, CL>, smem_bytes(MODE)));
+    GC_CUDA(allow(k_xent<MODE>, smem_bytes(MODE)));
     cudaLaunchAttribute at[1];
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(CL);
+    cfg.gridDim = dim3(2);
     cfg.blockDim = dim3(kThreadsX);
     cfg.dynamicSmemBytes = smem_bytes(MODE);
     cfg.attrs = at;
     cfg.numAttrs = 1;
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CL;
+    at[0].val.clusterDim.x = 2;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    GC_CUDA(cudaOccupancyMaxActiveClusters(&n, k_xent<MODE, CL>, &cfg));
-    if (n < 1) return fail(GC_ERR_CUDA, "no cluster of %d CTAs fits the device", CL);
+    GC_CUDA(cudaOccupancyMaxActiveClusters(&n, k_xent<MODE>, &cfg));
+    if (n < 1) return fail(GC_ERR_CUDA, "no pair of CTAs fits the device");
     if (dev >= 0 && dev < 64) cache[dev].store(n, std::memory_order_relaxed);
   }
   *units = n;
   return GC_OK;
 }
 
-template <int MODE, int CL>
+template <int MODE>
 int launch_mode(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const CUtensorMap& d,
                 const CUtensorMap& out, const CUtensorMap& acc, const XentParams& p, bool chained, cudaStream_t s) {
-  return launch_chain(k_xent<MODE, CL>, "k_xent", (unsigned)(CL * p.units), kThreadsX, smem_bytes(MODE), CL, chained, s,
+  return launch_chain(k_xent<MODE>, "k_xent", (unsigned)(2 * p.units), kThreadsX, smem_bytes(MODE), 2, chained, s,
                       a, b, c, d, out, acc, p);
 }
 
@@ -1057,7 +1045,7 @@ int parts_of(const void* x, int64_t ld, long long rows, int C, int Cp, int parts
                       y, y64, V, lab, out, status);
 }
 
-int tiles(long long n, int wide = TILE) { return (int)((n + wide - 1) / wide); }
+int tiles(long long n) { return (int)((n + TILE - 1) / TILE); }
 
 // The form for one point, and its blocks (each a slot of `part`): three an SM for bf16 rows (the registers' limit;
 // 268 MB: 56, 51, 57 us by 2, 3, 4), two for fp32 ones (131 MB: 28, 30, 30).  It counts finished blocks in a word
@@ -1138,34 +1126,25 @@ XentScratch carve_xent(Carve& c, const XentShape& s) {
   return w;
 }
 
-// Two pairs to a cluster where there are columns and tiles for them (two a cluster at least), and rows
-// enough for the sharing of A's to count: of one row tile A is little, and reading B takes every SM
-// (one row, C = 2048, V = 65536: 98 us in pairs, 136 in clusters of two; 2,048 rows, C = 1024, V = 32000:
-// 121 and 116).
-bool two_pairs(long long row_tiles, int cols) {
-  return row_tiles >= 4 && cols > TILE && row_tiles * tiles(cols, 2 * TILE) >= 2 * (device_sm_count() / 4);
-}
-
-template <int MODE, int CL>
+template <int MODE>
 int run_z(XentParams p, const CUtensorMap& mX, const CUtensorMap& mW, const CUtensorMap& mOut, bool chained,
           cudaStream_t st) {
   int n = 0;
-  const int rc = resident<MODE, CL>(&n);
+  const int rc = resident<MODE>(&n);
   if (rc) return rc;
-  p.nt = tiles(MODE == STAT ? p.V : p.w, CL / 2 * TILE);
+  p.nt = tiles(MODE == STAT ? p.V : p.w);
   p.units = (int)std::min<long long>(n, (long long)p.mt * p.nt);
   p.stage_ops = p.nx + p.nw;
   p.stages = ring_bytes(MODE) / (p.stage_ops * OP_BYTES);
-  return launch_mode<MODE, CL>(mX, mW, mX, mX, mOut, mX, p, chained, st);
+  return launch_mode<MODE>(mX, mW, mX, mX, mOut, mX, p, chained, st);
 }
 
-template <int CL>
 int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& mWt, const CUtensorMap& mP4,
              const CUtensorMap& mX4, const CUtensorMap& mG, const CUtensorMap& mAcc, cudaStream_t st) {
   int n = 0;
-  const int rc = resident<GRAD, CL>(&n);
+  const int rc = resident<GRAD>(&n);
   if (rc) return rc;
-  p.ct = tiles(p.C, CL / 2 * TILE);
+  p.ct = tiles(p.C);
   p.vt = tiles(p.w);
   p.ndx = want & XENT_DX ? p.mt * p.ct * p.ks : 0;
   p.ndw = want & XENT_G ? p.N * p.vt * p.ct : 0;
@@ -1178,7 +1157,7 @@ int run_grad(XentParams p, int want, const CUtensorMap& mP, const CUtensorMap& m
   p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_dw + 0.5), p.ndw / (p.units - p.r));
   p.stage_ops = std::max(p.ndx ? p.np_dx + p.nw : 0, p.ndw ? p.np + p.nx : 0);
   p.stages = ring_bytes(GRAD) / (p.stage_ops * OP_BYTES);
-  return launch_mode<GRAD, CL>(mP, mWt, mP4, mX4, mG, mAcc, p, true, st);
+  return launch_mode<GRAD>(mP, mWt, mP4, mX4, mG, mAcc, p, true, st);
 }
 
 // Rows' log-sum-exp and losses from their partial sums, and the mean.
@@ -1256,16 +1235,13 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.stall = take_stall(GC_STALL_XENT) ? 1 : 0;
   p.status = status;
 
-  // z: rows of X (boxes of half of them for two pairs) and of W, K innermost
-  CUtensorMap mX, mX2, mW, mP, mWt, mP4, mX4;
+  // z: rows of X and of W, K innermost
+  CUtensorMap mX, mW, mP, mWt, mP4, mX4;
   const long long dx[3] = {xc, T, w.nx}, lx[2] = {ldx, T * ldx};
   const long long dw[3] = {wc, s.V, w.nw}, lw[2] = {ldw, (long long)s.V * ldw};
-  if ((rc = map_nd(&mX, X, 3, dx, lx, p.a_rows)) || (rc = map_nd(&mX2, X, 3, dx, lx, HALF / 2)) ||
-      (rc = map_nd(&mW, W, 3, dw, lw, HALF)))
-    return rc;
+  if ((rc = map_nd(&mX, X, 3, dx, lx, p.a_rows)) || (rc = map_nd(&mW, W, 3, dw, lw, HALF))) return rc;
   if (!w.one) {
-    rc = two_pairs(p.mt, s.V) ? run_z<STAT, 4>(p, mX2, mW, mX, chained, st) : run_z<STAT, 2>(p, mX, mW, mX, chained, st);
-    if (rc) return rc;
+    if ((rc = run_z<STAT>(p, mX, mW, mX, chained, st))) return rc;
     if ((rc = join_rows(w, 2 * tiles(s.V), T, lab, io, status, st))) return rc;
   }
   if (!(s.want & (XENT_DX | XENT_G))) return GC_OK;
@@ -1305,20 +1281,13 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
     p.last_piece = v0 + w.piece >= s.V;
     const long long lp[2] = {w.piece, T * w.piece}, dps[3] = {w.piece, T, w.np};
     if ((rc = map_nd(&mPs, w.P, 3, dps, lp, 32, w.np))) return rc;
-    rc = two_pairs(p.mt, p.w) ? run_z<PROB, 4>(p, mX2, mW, mPs, true, st)
-                              : run_z<PROB, 2>(p, mX, mW, mPs, true, st);
-    if (rc) return rc;
-    const long long row_tiles = (s.want & XENT_DX ? (long long)p.mt * p.ks : 0) +
-                                (s.want & XENT_G ? (long long)s.N * tiles(p.w) : 0);
-    const bool two = T > HALF && two_pairs(row_tiles, s.C);
+    if ((rc = run_z<PROB>(p, mX, mW, mPs, true, st))) return rc;
     const long long dp[3] = {p.w, T, w.np};
     const long long d4[4] = {p.w, s.n_c, s.N, w.np};
     const long long l4[3] = {w.piece, (long long)s.n_c * w.piece, T * w.piece};
-    if ((rc = map_nd(&mP, w.P, 3, dp, lp, two ? HALF / 2 : p.a_rows)) || (rc = map_nd(&mP4, w.P, 4, d4, l4, BK)))
+    if ((rc = map_nd(&mP, w.P, 3, dp, lp, p.a_rows)) || (rc = map_nd(&mP4, w.P, 4, d4, l4, BK)))
       return rc;
-    rc = two ? run_grad<4>(p, s.want, mP, mWt, mP4, mX4, mG, mAcc, st)
-             : run_grad<2>(p, s.want, mP, mWt, mP4, mX4, mG, mAcc, st);
-    if (rc) return rc;
+    if ((rc = run_grad(p, s.want, mP, mWt, mP4, mX4, mG, mAcc, st))) return rc;
     if (p.split && (s.want & XENT_DX)) {
       const unsigned grid = (unsigned)((T * ((s.C + 3) / 4) + 255) / 256);
       void* out = p.last_piece ? io.dX : nullptr;

@@ -1,8 +1,7 @@
 // Inline-PTX wrappers for tcgen05 on a pair of CTAs (cta_group::2): a cluster of two whose SMs work on
 // one 256-row tile, each holding half of A's and half of B's rows in its own shared memory and half of
 // the accumulator's rows in its tensor memory.  The CTA of even rank leads: it issues the MMAs, and
-// the barriers that its MMA thread waits on live in its shared memory.  A cluster is one pair, or two
-// that share A's rows.
+// the barriers that its MMA thread waits on live in its shared memory.  A cluster is one pair.
 #pragma once
 
 #include "tc_ptx.cuh"
@@ -54,24 +53,6 @@ __device__ __forceinline__ void load_4d(void* dst, const CUtensorMap* map, int x
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
       "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
-      : "memory");
-}
-// The same into every CTA of `mask`, at this offset, completing on the barriers at bar's offset in
-// the CTAs of bar's parity of their pairs.
-__device__ __forceinline__ void load_3d_to(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar,
-                                           uint16_t mask) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster"
-      ".cta_group::2 [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "h"(mask)
-      : "memory");
-}
-__device__ __forceinline__ void load_4d_to(void* dst, const CUtensorMap* map, int x, int y, int z, int w,
-                                           uint32_t bar, uint16_t mask) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster"
-      ".cta_group::2 [%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "h"(mask)
       : "memory");
 }
 // Stores from this CTA's shared memory (bulk groups), and the same added to what is there.

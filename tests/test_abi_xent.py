@@ -48,3 +48,17 @@ def test_binding_checks():
         gc.gc_softmax_xent(X, W, torch.zeros(6), 2, 3)
     with pytest.raises(TypeError):
         gc.gc_softmax_xent(X, W, torch.zeros(6, dtype=torch.long), 2, 3)   # not on the GPU
+
+
+def test_no_copy_goes_to_another_sm():
+    """The library also runs in programs of several GPUs: no TMA copy in its sources names more than one CTA."""
+    import glob
+    import os
+    import re
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2405_19509_gb300", "csrc")
+    files = sorted(glob.glob(os.path.join(csrc, "*.cu*")))
+    assert files
+    for f in files:
+        with open(f) as h:
+            text = re.sub(r'"\s*"', "", h.read())       # neighbouring string literals are one
+        assert not re.search(r"cp\.async\.bulk[\w.:]*multicast", text), os.path.basename(f)
