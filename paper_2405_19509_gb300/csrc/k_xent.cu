@@ -719,10 +719,11 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// (m, s) += (m2, s2), the largest value and the sum of exponentials about it.
+// (m, s) += (m2, s2), the largest value and the sum of exponentials about it.  The same bits wherever it is
+// inlined: the product and the sum are not left to the compiler to contract.
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
   const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-  s = s * ex2((m - ref) * kLog2e) + s2 * ex2((m2 - ref) * kLog2e);
+  s = __fmaf_rn(s2, ex2((m2 - ref) * kLog2e), __fmul_rn(s, ex2((m - ref) * kLog2e)));
   m = top;
 }
 
@@ -884,8 +885,9 @@ __global__ void __launch_bounds__(256) k_xent_dx(const float* __restrict__ part,
 }
 
 // lse and loss of the rows from their n partial sums [n][T].  A block takes R rows: a warp's lanes are R
-// rows by 32 / R slots, its eight warps take the slots in turn (R = 32: whole 256-byte reads; 4: whole
-// sectors, for few rows).
+// rows by 32 / R slots (R = 32: whole 256-byte reads; 4: whole sectors, for few rows).  Either way slot k adds to
+// sum k mod 64, a warp joins its eight neighbouring sums as a tree and the eight warps' come in turn: a
+// point has the same bits in a call of any number of points.
 template <int R>
 __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ part, int n, long long T,
                                                   Labels lab, const float* __restrict__ target, uint32_t* status,
@@ -896,19 +898,37 @@ __global__ void __launch_bounds__(256) k_xent_lse(const float2* __restrict__ par
   const long long row = (long long)blockIdx.x * R + r;
   start_next();
   wait_prior();
-  float m = -INFINITY, s = 0.f;
+  constexpr int L = 32 / R, A = 8 / L;  // lanes of a row, sums of a lane: number a L + lane / R of the warp's
+  float am[A], as[A];
+#pragma unroll
+  for (int a = 0; a < A; ++a) {
+    am[a] = -INFINITY;
+    as[a] = 0.f;
+  }
   if (row < T) {
-#pragma unroll 8
-    for (int k = warp * (32 / R) + lane / R; k < n; k += 8 * (32 / R)) {
-      const float2 q = __ldcg(part + k * T + row);
-      join(m, s, q.x, q.y);
+#pragma unroll(8 / A)
+    for (int k0 = warp * 8 + lane / R; k0 < n; k0 += 64) {
+#pragma unroll
+      for (int a = 0; a < A; ++a) {
+        if (k0 + a * L < n) {
+          const float2 q = __ldcg(part + (k0 + a * L) * T + row);
+          join(am[a], as[a], q.x, q.y);
+        }
+      }
     }
   }
+  // sums 0 .. 3 += 4 .. 7, 0, 1 += 2, 3, 0 += 1
 #pragma unroll
-  for (int o = 16; o >= R; o >>= 1) {
-    const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
-    join(m, s, m2, s2);
+  for (int h = 4; h; h >>= 1) {
+    if (h >= L) {
+#pragma unroll
+      for (int a = 0; a < h / L; ++a) join(am[a], as[a], am[a + h / L], as[a + h / L]);
+    } else {
+      const float m2 = __shfl_down_sync(0xffffffffu, am[0], h * R), s2 = __shfl_down_sync(0xffffffffu, as[0], h * R);
+      join(am[0], as[0], m2, s2);
+    }
   }
+  float m = am[0], s = as[0];
   if (lane < R) sums[warp][r] = make_float2(m, s);
   __syncthreads();
   if (warp == 0 && lane < R && row < T) {

@@ -411,3 +411,15 @@ def test_row_gradient_keeps_the_digits_of_fp32_weights(gc, T, C):
     want = 0.5 * (W[1 - y].double() - W[y].double())
     got = gc.gc_softmax_xent(X, W, y, 1, T)["dX"].double()
     assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -15).all()
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("N,n_c,C,V", [(8, 1024, 64, 20000), (24, 256, 40, 9000)])
+def test_a_chunk_alone_gives_the_same_bits_beside_many(gc, N, n_c, C, V, x):
+    """The sums of the losses are joined in one order, however many points the call has."""
+    X, W, y = _data(N, n_c, C, V, x, "bf16", N + V)
+    full = gc.gc_softmax_xent(X, W, y, N, n_c)
+    rows = slice(2 * n_c, 3 * n_c)
+    one = gc.gc_softmax_xent(X[rows], W, y[rows], 1, n_c)
+    assert torch.equal(one["lse"], full["lse"][rows]) and torch.equal(one["row_loss"], full["row_loss"][rows])
+    assert torch.equal(one["G"][0], full["G"][2])
