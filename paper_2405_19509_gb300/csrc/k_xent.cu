@@ -9,7 +9,8 @@
 //   k_xent<PROB>   z again for one piece of the vocabulary, written as P's bf16 parts
 //   k_xent<GRAD>   dX += P W and G_i = P_i^T X_i of that piece, in one launch (k_xent_dx where the sum of dX
 //                  runs in ranges)
-// The loss of a single point is a pass over W (k_xent_one).
+// The loss of a single point is a pass over W (k_xent_one); its gradient is formed like those of more points, with
+// the lse of the tiles, so that a chunk of one point has the same G in a call of its own and beside others.
 //
 // Bound: the tensor pipe.  Per row, column and value of C: one product for lse, one for P, one for
 // dX, and two for G, whose 32-bit result wants P to 2^-17, as bf16 hi + lo; a bf16 dX is rounded to 2^-8,
@@ -1130,7 +1131,7 @@ XentScratch carve_xent(Carve& c, const XentShape& s) {
   w.lse = c.take<float>((size_t)T);
   w.target = c.take<float>((size_t)T);
   w.row_loss = c.take<float>((size_t)T);
-  w.part = c.take<float2>((size_t)T * (w.one ? one_blocks(s) : 2 * tiles(s.V)));
+  w.part = c.take<float2>((size_t)T * std::max(w.one ? one_blocks(s) : 0, !w.one || s.want ? 2 * tiles(s.V) : 0));
   if (s.want & (XENT_DX | XENT_G)) {
     w.piece = piece_cols(T, s.V);
     w.np = (s.want & XENT_G) || s.x_dtype == GC_F32 ? 2 : 1;
@@ -1207,7 +1208,8 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   const bool xb = s.x_dtype == GC_BF16, wb = s.w_dtype == GC_BF16;
   int rc = GC_OK;
   Labels lab{w.lab, nullptr, 0, s.V};
-  if (w.one) {
+  const bool one = w.one && (io.loss || io.row_loss || io.lse);
+  if (one) {
     rc = xb ? wb ? launch_one<__nv_bfloat16, __nv_bfloat16>(s, io, w.target, w.part, w.lse, status, st)
                  : launch_one<__nv_bfloat16, float>(s, io, w.target, w.part, w.lse, status, st)
             : wb ? launch_one<float, __nv_bfloat16>(s, io, w.target, w.part, w.lse, status, st)
@@ -1216,7 +1218,7 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   }
   // losses alone read bf16 rows where they lie; the products of the gradient want a copy that is finite
   const bool x_in_place = !s.want && xb && rowwise::rows_16(io.X, io.ldx, 2);
-  bool chained = w.one;  // whether the call has launched a kernel before
+  bool chained = one;  // whether the call has launched a kernel before
   if (x_in_place) {
     lab = Labels{nullptr, io.y, io.y64, s.V};
   } else {
@@ -1260,10 +1262,13 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   const long long dx[3] = {xc, T, w.nx}, lx[2] = {ldx, T * ldx};
   const long long dw[3] = {wc, s.V, w.nw}, lw[2] = {ldw, (long long)s.V * ldw};
   if ((rc = map_nd(&mX, X, 3, dx, lx, p.a_rows)) || (rc = map_nd(&mW, W, 3, dw, lw, HALF))) return rc;
-  if (!w.one) {
-    if ((rc = run_z<STAT>(p, mX, mW, mX, chained, st))) return rc;
-    if ((rc = join_rows(w, 2 * tiles(s.V), T, lab, io, status, st))) return rc;
+  XentIO sums = io;
+  if (w.one) {  // the lse of P alone: the outputs are there
+    sums.loss = nullptr;
+    sums.row_loss = sums.lse = nullptr;
   }
+  if ((rc = run_z<STAT>(p, mX, mW, mX, chained, st))) return rc;
+  if ((rc = join_rows(w, 2 * tiles(s.V), T, lab, sums, status, st))) return rc;
   if (!(s.want & (XENT_DX | XENT_G))) return GC_OK;
 
   const long long d4x[4] = {w.Cp, s.n_c, s.N, w.nx};

@@ -423,3 +423,13 @@ def test_a_chunk_alone_gives_the_same_bits_beside_many(gc, N, n_c, C, V, x):
     one = gc.gc_softmax_xent(X[rows], W, y[rows], 1, n_c)
     assert torch.equal(one["lse"], full["lse"][rows]) and torch.equal(one["row_loss"], full["row_loss"][rows])
     assert torch.equal(one["G"][0], full["G"][2])
+
+
+@pytest.mark.parametrize("x,w", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("layout", ["dense", "ragged"])
+def test_a_chunk_of_one_point_alone_gives_the_same_bits(gc, x, w, layout):
+    X, W, y = _data(5, 1, 200, 3001, x, w, 17, ignore=0, layout=layout)
+    full = gc.gc_softmax_xent(X, W, y, 5, 1)
+    for i in range(5):
+        one = gc.gc_softmax_xent(X[i:i + 1], W, y[i:i + 1], 1, 1)
+        assert torch.equal(one["G"][0], full["G"][i])
