@@ -325,14 +325,16 @@ def gc_dropout(x, p: float, seed: int, offset: int = 0, row0: int = 0, residual=
 def gc_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, p: float = 0.0,
                   seed: int = 0, offset: int = 0, row0: int = 0, y=None, h=None, mean=True, rstd=True):
     """y = layer norm of h = residual + D(x) (gc_dropout's D; h = x without both).  Returns dict with
-    y, h (x itself where there is neither residual nor dropout and no tensor is given for it), and
-    mean, rstd (rows, float32; None where False is passed): what gc_layer_norm_backward takes."""
+    y, h (x itself where there is neither residual nor dropout, no tensor is given for it and y is not
+    written over x), and mean, rstd (rows, float32; None where False is passed): what
+    gc_layer_norm_backward takes."""
     dt = _elt(x, "x")
     rows, cols = x.shape
     dev = x.device
+    over = isinstance(y, torch.Tensor) and y.data_ptr() == x.data_ptr()
     if y is None:
         y = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    if h is None and (residual is not None or p > 0):
+    if h is None and (residual is not None or p > 0 or over):
         h = torch.empty(x.shape, dtype=x.dtype, device=dev)
     if mean is True:
         mean = torch.empty(rows, dtype=torch.float32, device=dev)

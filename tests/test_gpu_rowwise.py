@@ -306,3 +306,19 @@ def test_rowwise_on_another_stream(gc):
         out = gc.gc_dropout(got, 0.0, 1)
     s.synchronize()
     assert torch.equal(got, want) and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [256, 1001, 9000])
+def test_layer_norm_over_its_input_gives_what_the_gradient_takes(gc, dtype, cols):
+    """y written over x, nothing else asked for: h is x as it was."""
+    rng = np.random.default_rng(cols)
+    x = _mat(rng, 12, cols, dtype, "strided")
+    before = x.clone()
+    want = gc.gc_layer_norm(before)
+    f = gc.gc_layer_norm(x, y=x)
+    assert f["y"] is x and torch.equal(x, want["y"]) and torch.equal(f["h"], before)
+    dy = _mat(rng, 12, cols, dtype)
+    a = gc.gc_layer_norm_backward(dy, want["h"], want["mean"], want["rstd"], None, 3, 4)
+    b = gc.gc_layer_norm_backward(dy, f["h"], f["mean"], f["rstd"], None, 3, 4)
+    assert torch.equal(a["dx"], b["dx"]) and torch.equal(a["G"], b["G"])
