@@ -213,7 +213,8 @@ struct NormGradArgs {
   float* sums;         // per (chunk, slice) 2 * cols column sums: G itself or partial ones
   long long sums_ld;   // between slices
   long long lddy, ldh, lddh, lddx, lddr;
-  int n_c, slices, rows_per_slice;
+  int slices;
+  uint32_t n_c, rows_per_slice;  // a slice's end, and the row after a chunk's last, may be past 2^31
   int cols, vec_cols;
   Mask m;
 };
@@ -233,8 +234,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? kGradThread
   const int lane = threadIdx.x & 31;
   const int warp = TPR == 32 ? 0 : threadIdx.x >> 5;
   const int chunk = blockIdx.x / a.slices, slice = blockIdx.x - chunk * a.slices;
-  const int r_end = min(a.n_c, (slice + 1) * a.rows_per_slice);
-  int r = slice * a.rows_per_slice + (TPR == 32 ? threadIdx.x >> 5 : 0);
+  const uint32_t r_end = min(a.n_c, (slice + 1) * a.rows_per_slice);
+  uint32_t r = slice * a.rows_per_slice + (TPR == 32 ? threadIdx.x >> 5 : 0);
   const long long first = (long long)chunk * a.n_c;
   float sg[Q][8], sb[Q][8];
 #pragma unroll
@@ -402,11 +403,11 @@ template <typename T>
 __global__ void __launch_bounds__(256) k_norm_cols(NormGradArgs a) {
   const int c = blockIdx.y * 256 + threadIdx.x;
   const int chunk = blockIdx.x / a.slices, slice = blockIdx.x - chunk * a.slices;
-  const int r_end = min(a.n_c, (slice + 1) * a.rows_per_slice);
+  const uint32_t r_end = min(a.n_c, (slice + 1) * a.rows_per_slice);
   if (c >= a.cols) return;
   float sg = 0.f, sb = 0.f;
 #pragma unroll 4
-  for (int r = slice * a.rows_per_slice; r < r_end; ++r) {
+  for (uint32_t r = slice * a.rows_per_slice; r < r_end; ++r) {
     const long long row = (long long)chunk * a.n_c + r;
     const float d = to_f(((const T*)a.dy)[row * a.lddy + c]);
     const float n = (to_f(((const T*)a.h)[row * a.ldh + c]) - __ldg(a.mean + row)) * __ldg(a.rstd + row);
@@ -454,9 +455,9 @@ struct Slices {
 Slices slices_of(int N, int n_c, int threads, int min_rows) {
   const long long blocks = (long long)device_sm_count() * std::max(1, kGradThreads / threads);
   long long want = std::max<long long>(1, blocks / N);
-  want = std::min<long long>(want, (n_c + min_rows - 1) / min_rows);
-  const int rows = (int)((n_c + want - 1) / want);
-  return {(n_c + rows - 1) / rows, rows};
+  want = std::min<long long>(want, ((long long)n_c + min_rows - 1) / min_rows);
+  const long long rows = (n_c + want - 1) / want;
+  return {(int)((n_c + rows - 1) / rows), (int)rows};
 }
 Slices grad_slices(int N, int n_c, int cols) {
   if (cols > kFusedCols) return slices_of(N, n_c, 256, 32);

@@ -322,3 +322,17 @@ def test_layer_norm_over_its_input_gives_what_the_gradient_takes(gc, dtype, cols
     a = gc.gc_layer_norm_backward(dy, want["h"], want["mean"], want["rstd"], None, 3, 4)
     b = gc.gc_layer_norm_backward(dy, f["h"], f["mean"], f["rstd"], None, 3, 4)
     assert torch.equal(a["dx"], b["dx"]) and torch.equal(a["G"], b["G"])
+
+
+def test_layer_norm_backward_of_as_many_rows_as_there_may_be(gc):
+    """A chunk of 2^31 - 1 rows of one column, whose last slice ends past 32 bits.  Every row adds 1 to the
+    gradient of beta and 2^-10 to gamma's.  Chains of fewer than 2^24 additions of ones are exact, the
+    sums of at most 2^12 slices round by 2^-24 each: 2^-12 of the total."""
+    rows = (1 << 31) - 1
+    one = torch.ones(rows, 1, dtype=torch.bfloat16, device="cuda")
+    stat = torch.full((rows,), 2.0 ** -5, device="cuda")
+    h = torch.full((rows, 1), 2.0 ** -4, dtype=torch.bfloat16, device="cuda")
+    G = gc.gc_layer_norm_backward(one, h, stat, stat, None, 1, rows, dx=False)["G"].double()
+    assert abs(G[0, 1].item() / rows - 1) <= 2.0 ** -12 and abs(G[0, 0].item() * 2.0 ** 10 / rows - 1) <= 2.0 ** -12
+    del one, stat, h
+    torch.cuda.empty_cache()
