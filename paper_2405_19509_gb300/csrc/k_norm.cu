@@ -274,10 +274,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? kGradThread
       ya[q] = xa[q];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        // past the row's end h is not the mean, but dy is zero, and gamma finite
-        const float2 y = two(d[q], j), x = __fmul2_rn(__fadd2_rn(two(n[q], j), both(-mu)), both(scale));
+        // h - mean; rstd is left to y and to the row's sum.  Past the row's end that is -mean, and dy zero:
+        // n, which need not be finite there, is not formed
+        const float2 y = two(d[q], j), x = __fadd2_rn(two(n[q], j), both(-mu));
         if (SUMS) {
-          put(sg[q], j, __ffma2_rn(y, x, two(sg[q], j)));
+          put(sg[q], j, __ffma2_rn(__fmul2_rn(y, both(scale)), x, two(sg[q], j)));
           put(sb[q], j, __fadd2_rn(y, two(sb[q], j)));
         }
         const float2 e = __fmul2_rn(y, two(g, j));
@@ -297,7 +298,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, TPR == 32 ? kGradThread
       c2 = lanes_sum<WPR>(p.y);
     }
     c1 *= inv;
-    c2 *= inv;
+    c2 = c2 * inv * scale * scale;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       const int col0 = (q * WPR + warp) * kSeg;

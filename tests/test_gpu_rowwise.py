@@ -336,3 +336,20 @@ def test_layer_norm_backward_of_as_many_rows_as_there_may_be(gc):
     assert abs(G[0, 1].item() / rows - 1) <= 2.0 ** -12 and abs(G[0, 0].item() * 2.0 ** 10 / rows - 1) <= 2.0 ** -12
     del one, stat, h
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [33, 40, 264, 1000, 1001, 8185, 8200])
+def test_gradient_of_constant_rows_of_large_values(gc, dtype, cols):
+    """Rows of 2^110 and a reciprocal deviation of 2^20, whose product is past fp32's range: n is zero, and
+    dx = rstd (a - mean a).  64 roundings a sum, as many in dx, and the store."""
+    rng = np.random.default_rng(cols)
+    dy = _mat(rng, 6, cols, dtype)
+    h = torch.full((6, cols), 2.0 ** 110, dtype=dy.dtype, device="cuda")
+    mean, rstd = torch.full((6,), 2.0 ** 110, device="cuda"), torch.full((6,), 2.0 ** 20, device="cuda")
+    got = gc.gc_layer_norm_backward(dy, h, mean, rstd, None, 2, 3)
+    a = _np(dy)
+    want = 2.0 ** 20 * (a - a.mean(1, keepdims=True))
+    assert (np.abs(_np(got["dx"]) - want) <= 2.0 ** 20 * 70 * U * np.abs(a).max() + V[dtype] * np.abs(want)).all()
+    G = _np(got["G"])
+    assert not G[:, :cols].any() and (np.abs(G[:, cols:] - a.reshape(2, 3, cols).sum(1)) <= 4 * U * 3 * np.abs(a).max()).all()
