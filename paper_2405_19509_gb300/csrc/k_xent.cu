@@ -54,6 +54,7 @@ constexpr long long kSpinX = 1LL << 32;
 // V = 32768, C = 256: 514, 483, 445, 400 us), though from 2^25 on they leave L2.
 constexpr long long kPieceElems = 1LL << 27;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kBf16Max = 0x1.fep+127f;
 
 constexpr int kNone = -1, kNoneBad = -2;  // labels that are none, the latter of a row that is not finite
 // K blocks of a product for a 32-bit result that are summed in tensor memory before the sum goes to
@@ -673,10 +674,10 @@ __global__ void __launch_bounds__(kThreadsX, 1)
   }
 }
 
-// bf16 parts [parts][rows][Cp] of a matrix: hi = bf16(x), lo = bf16(x - hi), zero from C to Cp.  A block
-// a row at a time, or a warp (WPR = 1: short rows).  With labels: lab = the label as an int, kNone where
-// there is none.  The products that follow multiply such a row by zeros, so what is not finite in it, or
-// would not be in bf16, enters as zero (kNoneBad).
+// bf16 parts [parts][rows][Cp] of a matrix: hi = bf16(x), lo = bf16(x - hi), zero from C to Cp; past bf16's
+// largest value, where fp32 goes on for another 2^-8 of it, that is hi.  A block a row at a time, or a warp
+// (WPR = 1: short rows).  With labels: lab = the label as an int, kNone where there is none.  The products that
+// follow multiply such a row by zeros, so what is not finite in it enters as zero (kNoneBad).
 template <typename T, bool VEC, int WPR>
 __global__ void __launch_bounds__(256)
     k_xent_parts(const T* __restrict__ x, long long ld, long long rows, int C, int Cp, int parts,
@@ -699,15 +700,19 @@ __global__ void __launch_bounds__(256)
       if (!live) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (!(fabsf(v[j]) < 3.38e38f)) {
+          if (!isfinite(v[j])) {
             v[j] = 0.f;
             bad = 1;
           }
       }
       for (int q = 0; q < parts; ++q) {
-        store_seg<VEC>(out + ((size_t)q * rows + row) * Cp, col0, lane, Cp, v);
+        float h[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+        for (int j = 0; j < 8; ++j)
+          h[j] = sizeof(T) == 4 && isfinite(v[j]) ? fminf(fmaxf(v[j], -kBf16Max), kBf16Max) : v[j];
+        store_seg<VEC>(out + ((size_t)q * rows + row) * Cp, col0, lane, Cp, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(h[j]));
       }
     }
     if (y) {

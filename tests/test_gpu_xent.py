@@ -433,3 +433,27 @@ def test_a_chunk_of_one_point_alone_gives_the_same_bits(gc, x, w, layout):
     for i in range(5):
         one = gc.gc_softmax_xent(X[i:i + 1], W, y[i:i + 1], 1, 1)
         assert torch.equal(one["G"][0], full["G"][i])
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("label", [-1, 7])
+def test_rows_at_the_end_of_the_range_are_finite(gc, x, label):
+    """The largest values of X's type are values: the row's logits are finite (W is small there), and so is
+    what comes of them, with a label or without, with the gradient or without it."""
+    X, W, y = _data(2, 20, 64, 200, x, "f32", 41, ignore=0)
+    X[3, 5], W[:, 5] = torch.finfo(X.dtype).max, 2.0 ** -122
+    W[9, 5] = 2.0 ** -121
+    y[3] = label
+    z = X.double() @ W.double().T
+    lse = torch.logsumexp(z, 1)
+    tz = (20 * 2.0 ** -23 + 2.0 ** -15) * (X.double().abs() @ W.double().abs().T)
+    tol = tz.amax(1) + 2.0 ** -20 * (1 + lse + z.abs().amax(1))
+    full, only = gc.gc_softmax_xent(X, W, y, 2, 20), gc.gc_softmax_xent(X, W, y, 2, 20, dX=False, G=False)
+    for got in (full, only):
+        assert ((got["lse"].double() - lse).abs() <= tol).all()
+        assert torch.isfinite(got["row_loss"]).all()
+    assert torch.equal(full["lse"], only["lse"]) and torch.equal(full["row_loss"], only["row_loss"])
+    assert torch.isfinite(full["dX"]).all()
+    if label < 0:
+        want = gc.gc_softmax_xent(torch.where(y[:, None] < 0, torch.zeros_like(X), X), W, y, 2, 20)
+        assert torch.equal(full["G"], want["G"]) and torch.equal(full["dX"], want["dX"])
