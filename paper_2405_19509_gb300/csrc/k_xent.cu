@@ -61,8 +61,11 @@ constexpr int kNone = -1, kNoneBad = -2;  // labels that are none, the latter of
 // registers: an addition there is cut off, not rounded, and all errors have one sign (5,569 points, C = 384,
 // fp32: G was 1.9e-5 off in one sum, 2e-8 a step).  Four blocks leave bf16's G as exact as fp32 products are:
 // 8,192 points in eight chunks, C = 2048, V = 65536 by 8, 4, 2 blocks: 1.2e-6, 6.7e-7, 4.5e-7 off in the 2-norm
-// (5.6e-7 in fp32) at 6.4, 6.7, 7.4 ms.  bf16 results and z, a few hundred steps long, do without.
+// (5.6e-7 in fp32) at 6.4, 6.7, 7.4 ms.  bf16 results do without.
 constexpr int kSegment = 4;
+// ... and the K blocks of z, times its products, likewise: 128 steps, C = 2048 in bf16.  Losses of bf16 rows of
+// 1024, 2048, 4096, 8192: 3.5, 7.3, 7.1, 7.0e-7 off; in one sum 3.4, 7.0, 15, 30e-7, at the same times.
+constexpr int kSegmentZ = 32;
 enum { STAT = 0, PROB = 1, GRAD = 2 };
 constexpr int kThreadsX = 64 + 32 * kEpi;
 // The ring of operand stages and the store boxes of each epilogue warp.
@@ -90,6 +93,7 @@ struct XentParams {
   long long T;
   int C, V, N, n_c;
   int nx, nw;          // bf16 parts of X and of W
+  int z_seg;           // K blocks of z that are summed in tensor memory at a time
   int v0, w;           // PROB, GRAD: the piece is columns [v0, v0 + w)
   int np, np_dx;       // parts of P: kept, and that enter dX
   int mt, nt, group;   // tiles of T and of the columns; row tiles that share a sweep of the columns
@@ -156,7 +160,7 @@ __device__ __forceinline__ TileAt tile_at(const XentParams& p, int unit, int k) 
     t.nkb = (p.C + BK - 1) / BK;
     t.na = p.nx;
     t.nb = p.nw;
-    t.seg = t.nkb;
+    t.seg = p.z_seg;
     return t;
   }
   const int ndx = (p.ndx - unit + p.units - 1) / p.units;
@@ -277,21 +281,19 @@ __device__ __forceinline__ void box_ready() {
   __syncwarp();
 }
 
-// The epilogue of STAT and PROB.  `release` hands the accumulator back: called once, when the last of it is
-// in registers.
-template <int MODE, typename Release>
-__device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, uint32_t taddr, long long row_in,
-                                         int half, int lab, float l2, uint8_t* box, const CUtensorMap* mOut,
-                                         Release release) {
+// The epilogue of STAT and PROB: `get` gives 64 (STAT) or 32 columns of a lane's row, in turn; U of those in a
+// loop's body.
+template <int MODE, int U, typename Get>
+__device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, long long row_in, int half, int lab,
+                                         float l2, uint8_t* box, const CUtensorMap* mOut, Get get) {
   const int lane = threadIdx.x & 31;
   if (MODE == STAT) {
     float m = -INFINITY, s = 0.f;
-#pragma unroll 1
+#pragma unroll(U)
     for (int c = 0; c < HALF / 64; ++c) {
       float v[64];
       __syncwarp();
-      tmem_ld64(taddr + (uint32_t)(c * 64), v);
-      if (c == HALF / 64 - 1) release();
+      get(c, v);
       const int col = t.n0 + half * HALF + c * 64;
       const int n = p.V - col;
       if (n < 64) {
@@ -316,11 +318,11 @@ __device__ __forceinline__ void epilogue(const XentParams& p, const TileAt& t, u
     }
     if (row_in < p.T && t.n0 < p.V) p.part[(long long)(t.n0 / HALF + half) * p.T + row_in] = make_float2(m, s);
   } else {
+#pragma unroll(U)
     for (int c = 0; c < HALF / 32; ++c) {
       float v[32];
       __syncwarp();
-      tmem_ld32(taddr + (uint32_t)(c * 32), v);
-      if (c == HALF / 32 - 1) release();
+      get(c, v);
       if (t.n0 >= p.w || row_in - lane >= p.T) continue;  // nothing of the warp's rows or columns exists
       const int at = lab - (p.v0 + t.n0 + half * HALF + c * 32);  // the label's place here
 #pragma unroll
@@ -635,7 +637,7 @@ __global__ void __launch_bounds__(kThreadsX, 1)
         if (MODE == PROB) l2 = __ldg(p.lse + row) * kLog2e;
       }
       uint8_t* box = store_box + (warp - 2) * boxes(MODE) * BOX;
-      if (MODE == GRAD && t.nkb > t.seg) {
+      if (t.nkb > t.seg) {
         float sum[HALF];
 #pragma unroll
         for (int j = 0; j < HALF; ++j) sum[j] = 0.f;
@@ -645,20 +647,30 @@ __global__ void __launch_bounds__(kThreadsX, 1)
           release();
         }
         if (!ok) break;
-        store_grad(p, t, row, half, box, &mOut, &mAcc, [&](int c, float(&v)[32]) {
+        auto get = [&](int c, auto& v) {
+          constexpr int n = sizeof(v) / sizeof(float);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = sum[c * 32 + j];
-        });
+          for (int j = 0; j < n; ++j) v[j] = sum[c * n + j];
+        };
+        if constexpr (MODE == GRAD)
+          store_grad(p, t, row, half, box, &mOut, &mAcc, get);
+        else
+          epilogue<MODE, HALF / 32>(p, t, row, half, lab, l2, box, &mOut, get);
         continue;
       }
       if (!filled()) break;
-      if (MODE == GRAD)
-        store_grad(p, t, row, half, box, &mOut, &mAcc, [&](int c, float(&v)[32]) {
-          tmem_ld32(at() + (uint32_t)(c * 32), v);
-          if (c == HALF / 32 - 1) release();
-        });
+      auto get = [&](int c, auto& v) {  // the accumulator is handed back when the last of it is in registers
+        constexpr int n = sizeof(v) / sizeof(float);
+        if constexpr (n == 64)
+          tmem_ld64(at() + (uint32_t)(c * n), v);
+        else
+          tmem_ld32(at() + (uint32_t)(c * n), v);
+        if (c == HALF / n - 1) release();
+      };
+      if constexpr (MODE == GRAD)
+        store_grad(p, t, row, half, box, &mOut, &mAcc, get);
       else
-        epilogue<MODE>(p, t, at(), row, half, lab, l2, box, &mOut, release);
+        epilogue<MODE, MODE == STAT ? 1 : HALF / 32>(p, t, row, half, lab, l2, box, &mOut, get);
       ++use;
     }
     if (boxes(MODE) && lane == 0) bulk_wait_all();
@@ -1250,6 +1262,9 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.n_c = s.n_c;
   p.nx = w.nx;
   p.nw = w.nw;
+  // z in as few sums as the limit allows, of one length
+  const int nkb = (s.C + BK - 1) / BK, z_most = kSegmentZ / (w.nx + w.nw - 1), z_sums = (nkb + z_most - 1) / z_most;
+  p.z_seg = (nkb + z_sums - 1) / z_sums;
   p.mt = tiles(T);
   p.group = std::min(p.mt, 16);
   p.a_both = T > HALF;

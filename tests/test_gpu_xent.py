@@ -457,3 +457,33 @@ def test_rows_at_the_end_of_the_range_are_finite(gc, x, label):
     if label < 0:
         want = gc.gc_softmax_xent(torch.where(y[:, None] < 0, torch.zeros_like(X), X), W, y, 2, 20)
         assert torch.equal(full["G"], want["G"]) and torch.equal(full["dX"], want["dX"])
+
+
+@pytest.mark.parametrize("x,w,C", [("bf16", "bf16", 32768), ("f32", "f32", 16384), ("bf16", "f32", 16384), ("bf16", "bf16", 4160)])
+def test_logits_of_long_rows_keep_their_digits(gc, x, w, C):
+    """Products of one sign, whose sum loses most where additions cut off.  At most 128 of them, and 16 products
+    each, are added in tensor memory in a row, each off by at most 2^-23 of the sum; the sums of those are
+    rounded (2^-24 each); operands in two parts are off by 2^-15 together.  lse adds 2^-20."""
+    T, V = 40, 300
+    g = torch.Generator(device="cuda").manual_seed(C)
+    X = torch.rand(T, C, generator=g, device="cuda").add_(0.5).to(TYPES[x])
+    W = torch.rand(V, C, generator=g, device="cuda").add_(0.5).mul_(30.0 / C).to(TYPES[w])
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    z = X.double() @ W.double().T
+    lse = torch.logsumexp(z, 1)
+    parts = 2.0 ** -15 if "f32" in (x, w) else 0.0
+    top = z.amax(1)
+    tz = (144 * 2.0 ** -23 + (C / 640 + 1) * 2.0 ** -24 + parts) * top
+    tl = tz + 2.0 ** -20 * (1 + lse.abs() + top)
+    loss = lse - z.gather(1, y[:, None])[:, 0]
+    ws = gc.Workspace()
+    for grad in (False, True):
+        got = gc.gc_softmax_xent(X, W, y, 1, T, dX=grad, G=grad, ws=ws)
+        gc.gc_status(ws)
+        assert ((got["lse"].double() - lse).abs() <= tl).all()
+        assert ((got["row_loss"].double() - loss).abs() <= tl + tz).all()
+    # the columns of P add to nothing in every row, as far as P and lse come from the same z
+    P = torch.softmax(z, 1).scatter_add(1, y[:, None], torch.full((T, 1), -1.0, dtype=torch.float64, device="cuda"))
+    tp = P.abs() * (tz + tl)[:, None] + 2.0 ** -16 * P.abs()
+    G = got["G"].view(V, C).double()
+    assert ((G - P.T @ X.double()).abs() <= (tp.T @ X.double()) + 2.0 ** -15 * (P.abs().T @ X.double())).all()
