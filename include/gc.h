@@ -322,17 +322,21 @@ int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t 
  *   G[i][v]     = sum_{t in chunk i} P[t][v] X[t]        (chunk i: points [i n_c, (i + 1) n_c)).
  * A point whose label is negative (padding) has row_loss 0 and enters no gradient, whatever its row
  * of X holds; its lse is formed all the same (not finite where the row is not).  A label
- * >= V is treated so too, and raises GC_ERR_DATA in the status header.  Neither z nor P is kept: both are formed for a piece of the vocabulary at a
- * time (a piece of P is at most about 2^27 values), the products on the tensor cores with fp32 sums.
+ * >= V is treated so too, and raises GC_ERR_DATA in the status header.  Neither z nor P is kept: both
+ * are formed for a piece of the vocabulary at a time, of a multiple of 256 columns: about 2^27 values of P,
+ * or 256 columns where the points are more than 2^19.  The products run on the tensor cores with fp32 sums.
  * bf16 operands are used as they are, fp32 ones as bf16 hi + lo (2^-17); P enters G as hi + lo, and
- * a bf16 dX in bf16.  In the 2-norm G is about 1e-6 off with bf16 rows and 4e-6 with fp32 ones.
+ * a bf16 dX in bf16.  In the 2-norm losses and lse are within 1e-6, G about 1e-6 off with bf16 rows and
+ * 4e-6 with fp32 ones.
  *   X    N n_c rows of C values of x_dtype, ldx elements apart.    W   V rows, ldw apart, w_dtype.
  *   y    N n_c labels, int64 (y64 != 0) or int32.
  *   loss one device double; row_loss, lse  N n_c fp32;  dX  N n_c rows of x_dtype, lddx apart;
  *   G    N rows of V * C fp32, ldg apart (a slice of the chunk gradients of a model): each nullable,
  *        not all of them.  dX must not overlap X.  Any alignment; the sums have a fixed order.
  *   Limits: C <= 2^20, V <= 2^28, N n_c < 2^31, and at most 2^29 tiles of 256 x 256.
- * Workspace: gc_softmax_xent_workspace bytes.  w_16: whether W and its rows lie on 16-byte boundaries
+ * Workspace: gc_softmax_xent_workspace bytes: the copies of X and W in bf16 parts, 16 bytes a point and 256
+ * columns of the vocabulary for partial sums (8 GB for 2^20 points and 2^17 columns), with a gradient 2 or 4
+ * bytes a value of a piece of P and fp32 sums of dX.  w_16: whether W and its rows lie on 16-byte boundaries
  * (bf16 rows that do are read in place; others are copied); want: 1 with dX, 2 with G, added up.  The size
  * depends on the current device's number of SMs.
  */
