@@ -181,8 +181,9 @@ int go_norm(const NormArgs& a, cudaStream_t s) {
   constexpr int threads = TPR == 32 ? 128 : TPR;
   const long long blocks = (a.rows + RPB - 1) / RPB;
   // bf16 rows without dropout leave the SMs idle half the time, and fewer rows at once suit the memory better:
-  // 16,384 rows of 4096 with residual 85 us by 768 threads an SM, 96 by 1024 (with dropout 96 and 92; fp32 113
-  // and 103).
+  // 2^26 values with residual by 768 and 1024 threads an SM, rows of 1024 columns 88 and 98 us, of 2048 84 and 96, of
+  // 4096 83 and 94; of 256 95 and 86, and without residual 60 and 57.  With dropout 95 and 91 (4096); fp32 with
+  // residual 177 and 169, without 112 and 102.
   const int per_sm = sizeof(T) == 2 && !a.m.t && threads <= 256 ? 768 : 1024;
   const long long grid = std::min<long long>(blocks, (long long)device_sm_count() * (per_sm / threads));
   k_norm<T, VEC, TPR, VPT><<<(unsigned)grid, threads, 0, s>>>(a);
@@ -223,7 +224,7 @@ struct NormGradArgs {
 // while one is worked on.  SUMS: the column sums for G as well.  512 threads an SM have registers for
 // all that.  (16,384 rows of 4096 bf16 with residual, 671 MB, with dropout and without it: no row ahead 168 us;
 // one segment a warp, 1024 threads 144 and 123; two 133 and 125; two, 768 threads, which spill, 179 and 165;
-// two with two-wide arithmetic 129 and 123.)
+// two with two-wide arithmetic 129 and 122.)
 constexpr int kGradSegs = 2;
 constexpr int kGradThreads = 512;  // an SM
 template <typename T, bool VEC, int TPR, bool SUMS>

@@ -28,8 +28,8 @@
 // and the fp32 dX leave by way of 32-row boxes in shared memory (1,540 points, C = 1000, V = 10007: 575 -> 371
 // us).  Every wait is bounded (GC_ERR_TIMEOUT).
 //
-// 8,192 points, C = 2048, V = 65536, bf16: losses alone 1.2 ms, 1810 TFLOP/s, 93% of the rate of the library's
-// bf16 product (the tensor pipe is active 90% of the clocks), 1.65 ms with MMAs issued from a branch; with the
+// 8,192 points, C = 2048, V = 65536, bf16: losses alone 1.11 ms, 1.97 PFLOP/s, the rate of the library's bf16
+// product (the tensor pipe is active 90% of the clocks), 1.65 ms with MMAs issued from a branch; with the
 // gradient in eight chunks 7.0 ms, 11.0 TFLOP issued at 1.57 PFLOP/s, near what the power limit allows (1.7).
 #include <cudaTypedefs.h>
 
@@ -50,8 +50,8 @@ constexpr int kEpi = 8;
 constexpr int BOX = 32 * 128;  // a store box: 32 rows of 128 bytes, 128-byte swizzle
 constexpr long long kSpinX = 1LL << 32;
 // Values of a piece of P: 512 MB as two bf16 parts.  Larger pieces mean fewer waves that are not full and fewer
-// sums of dX to add to (8,192 points, V = 65536, C = 2048, 2^24 to 2^27: 7.1, 6.6, 6.5, 6.3 ms; 4,096 points,
-// V = 32768, C = 256: 514, 483, 445, 400 us), though from 2^25 on they leave L2.
+// sums of dX to add to (8,192 points, V = 65536, C = 2048, 2^24 to 2^27: 7.9, 7.3, 7.1, 7.0 ms; 4,096 points,
+// V = 32768, C = 256: 743, 536, 422, 393 us), though from 2^25 on they leave L2.
 constexpr long long kPieceElems = 1LL << 27;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kBf16Max = 0x1.fep+127f;
@@ -60,8 +60,8 @@ constexpr int kNone = -1, kNoneBad = -2;  // labels that are none, the latter of
 // K blocks of a product for a 32-bit result that are summed in tensor memory before the sum goes to
 // registers: an addition there is cut off, not rounded, and all errors have one sign (5,569 points, C = 384,
 // fp32: G was 1.9e-5 off in one sum, 2e-8 a step).  Four blocks leave bf16's G as exact as fp32 products are:
-// 8,192 points in eight chunks, C = 2048, V = 65536 by 8, 4, 2 blocks: 1.2e-6, 6.7e-7, 4.5e-7 off in the 2-norm
-// (5.6e-7 in fp32) at 6.4, 6.7, 7.4 ms.  bf16 results do without.
+// 8,192 points in eight chunks, C = 2048, V = 65536 by 8, 4, 2 blocks: 1.2e-6, 6.9e-7, 4.7e-7 off in the 2-norm
+// (5.6e-7 in fp32) at 6.7, 7.0, 7.4 ms.  bf16 results do without.
 constexpr int kSegment = 4;
 // ... and the K blocks of z, times its products, likewise: 128 steps, C = 2048 in bf16.  Losses of bf16 rows of
 // 1024, 2048, 4096, 8192: 3.5, 7.3, 7.1, 7.0e-7 off; in one sum 3.4, 7.0, 15, 30e-7, at the same times.
