@@ -326,8 +326,9 @@ int gc_layer_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t 
  * are formed for a piece of the vocabulary at a time, of a multiple of 256 columns: about 2^27 values of P,
  * or 256 columns where the points are more than 2^19.  The products run on the tensor cores with fp32 sums.
  * bf16 operands are used as they are, fp32 ones as bf16 hi + lo (2^-17); P enters G as hi + lo, and
- * a bf16 dX in bf16.  Off in the 2-norm, at most, with bf16 rows and with fp32 ones: losses and lse 1.1e-6
- * and 1.4e-6, G 2e-6 and 4e-6, dX 1.9e-3 (rounded once it would be 1.7e-3) and 4e-6.
+ * a bf16 dX in bf16.  Off in the 2-norm for C >= 64, at most, with bf16 rows and with fp32 ones: losses and
+ * lse 1.1e-6 and 1.4e-6, G 2e-6 and 4e-6, dX 1.9e-3 (rounded once it would be 1.7e-3) and 4e-6.  With a few
+ * columns the roundings of fp32 operands do not average: 2e-5.
  *   X    N n_c rows of C values of x_dtype, ldx elements apart.    W   V rows, ldw apart, w_dtype.
  *   y    N n_c labels, int64 (y64 != 0) or int32.
  *   loss one device double; row_loss, lse  N n_c fp32;  dX  N n_c rows of x_dtype, lddx apart;
