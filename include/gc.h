@@ -61,6 +61,12 @@ extern "C" {
 #define GC_F32 0  /* X element type: float32                              */
 #define GC_BF16 1 /* X element type: bfloat16                             */
 
+#define GC_ACT_NONE 0      /* act(z) = z                                       */
+#define GC_ACT_RELU 1      /* max(z, 0), slope 0 at 0                          */
+#define GC_ACT_GELU 2      /* z (1 + erf(z / sqrt 2)) / 2                      */
+#define GC_ACT_GELU_TANH 3 /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+#define GC_ACT_SILU 4      /* z / (1 + exp(-z))                                */
+
 #define GC_LSQ 0      /* l = (x^T w - y)^2 / 2                             */
 #define GC_LOGISTIC 1 /* l = log(1 + exp(-y x^T w)), y in {-1, +1}          */
 
@@ -103,6 +109,8 @@ int gc_set_wait_limit(int64_t cycles);
                                   compute, see gc_set_decode_policy) */
 #define GC_STALL_BATCHED 4     /* the batched chunk-gradient GEMMs (first one) */
 #define GC_STALL_XENT 16       /* softmax cross entropy (its first pass)      */
+#define GC_STALL_LINEAR 32     /* the linear layer's product, forward or backward */
+#define GC_STALL_MUON 64       /* the first product of gc_orthogonalize, gc_muon_step */
 int gc_inject_stall(int kernels);
 
 /* Path of the batched decode (gc_decode_batch, gc_decode_apply,
@@ -346,6 +354,88 @@ int gc_softmax_xent(const void* X, int64_t ldx, int x_dtype, const void* W, int6
                     const void* y, int y64, int N, int n_c, int C, int V, double* loss, float* row_loss,
                     float* lse, void* dX, int64_t lddx, float* G, int64_t ldg, void* ws, size_t ws_bytes,
                     void* stream);
+
+/* ---- a linear layer with bias, activation and residual ------------------------
+ *   z = X W^T + bias,  y = residual + act(z)        (act: GC_ACT_*)
+ * for every row of X: the matrices of a feed-forward block.  Products run on the tensor cores with fp32 sums; bias,
+ * activation and residual are added in fp32 before y is rounded, and act takes z before it is rounded for its store.
+ *   X    rows of C values of x_dtype, ldx elements apart.   W   F rows of C, ldw apart, w_dtype.
+ *   bias F fp32, may be NULL.   residual   rows of F values of x_dtype, ldr apart, may be NULL.
+ *   y    rows of F values of x_dtype, ldy apart; may be residual itself (same pointer and stride).
+ *   z    NULL, or rows of F values of x_dtype, ldz apart: what gc_linear_backward takes where act is not GC_ACT_NONE.
+ * y and z must not overlap X, W or one another, nor z the residual.  Any alignment.  rows 0 .. 2^30 (0: nothing is
+ * launched), C, F 1 .. 2^20.
+ * bf16 operands are used as they are; an fp32 W beside bf16 rows as bf16 hi + lo (2^-17), and fp32 rows as three bf16
+ * parts (24 bits) in as many products as an fp32 result needs.  A row of X reaches its own row of y alone, whatever it
+ * holds; of an fp32 row or W an infinity gives infinities or NaN.
+ * Workspace: gc_linear_workspace bytes (copies of X and W in parts where they are fp32 or lie on no 16-byte boundary,
+ * which x_16 and w_16 say; sums of ranges of C where tiles are few).  The size depends on the current device's number of
+ * SMs.
+ */
+size_t gc_linear_workspace(int64_t rows, int C, int F, int x_dtype, int w_dtype, int x_16, int w_16);
+int gc_linear(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ldw, int w_dtype, const float* bias,
+              int act, const void* residual, int64_t ldr, int64_t rows, int C, int F, void* y, int64_t ldy, void* z,
+              int64_t ldz, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- gradient of gc_linear, the parameters' per chunk --------------------------
+ * With dy the gradient of y and d = dy act'(z) (relu' = 0 at 0), for T = N n_c rows
+ *   dX        = d W
+ * and for chunk i, rows [i n_c, (i + 1) n_c), un-normalised sums as in gc_chunk_grads
+ *   G[i]      = d_i^T X_i        (F x C, of W)
+ *   Gb[i]     = sum_t d_t        (F, of the bias).
+ * The gradient of the residual is dy itself.
+ *   dy, z  T rows of F values of x_dtype, lddy and ldz apart; z may be NULL where act is GC_ACT_NONE.
+ *   X, W   as in gc_linear; X may be NULL without G, W without dX.
+ *   dX     T rows of C values of x_dtype, lddx apart, overlapping no input.
+ *   G, Gb  N rows of F * C and of F fp32, ldg and ldgb apart: slices of the chunk gradients of a model.
+ * dX, G and Gb are each nullable, not all of them.  T <= 2^30.  Any alignment.  All sums have a fixed order; G and Gb of
+ * a chunk depend on its rows alone, bit for bit, whatever chunks the call has besides.
+ * With bf16 rows d enters G as bf16 hi + lo (2^-17; as it is without an activation) and dX in bf16; an fp32 W as hi + lo.
+ * fp32 rows enter as in gc_linear.
+ * Workspace: gc_linear_backward_workspace bytes; dy_16: whether dy lies on 16-byte boundaries; want: 1 with dX, 2 with
+ * G, 4 with Gb, added up.  The size depends on the current device's number of SMs.
+ */
+size_t gc_linear_backward_workspace(int N, int n_c, int C, int F, int x_dtype, int w_dtype, int act, int x_16,
+                                    int w_16, int dy_16, int want);
+int gc_linear_backward(const void* dy, int64_t lddy, const void* z, int64_t ldz, const void* X, int64_t ldx,
+                       int x_dtype, const void* W, int64_t ldw, int w_dtype, int act, int N, int n_c, int C, int F,
+                       void* dX, int64_t lddx, float* G, int64_t ldg, float* Gb, int64_t ldgb, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/* ---- orthogonalised matrices -----------------------------------------------
+ * From X = U / max(|U|_F, eps), `steps` times
+ *   A = X X^T,  X <- (a I + b A + c A^2) X
+ * (X^T X from the right where a matrix is higher than wide: the same polynomial of its singular values), which draws all
+ * singular values towards 1: Newton-Schulz.  For `batch` matrices of rows x cols values of dtype.
+ *   U, out   rows ldu, ldo elements apart, matrices stride_u, stride_o apart (not read for one matrix); out may be U.
+ *            Matrices of a batch may lie one after the other or side by side; they must not overlap.  Any alignment.
+ *   coeffs   a, b, c (host), or NULL: 3.4445, -4.7750, 2.0315, whose slope at 0 is so steep that five steps bring singular
+ *            values from 0.01 to between 0.7 and 1.2.  Refused where they take singular values of at most 1 past 4.
+ *   steps    1 .. 64.   eps >= 0: a matrix of zeros stays one if it is positive.
+ * batch 0 .. 2^20 (0: nothing is launched), rows and cols 1 .. 2^20, the smaller 1 .. 2^15.
+ * Products run on the tensor cores with fp32 sums, fp32 matrices in two 16-bit parts (22 bits; as near to 64 bits as a
+ * computation in fp32), bf16 ones in one or two, so that the result is within its own rounding of theirs.  A value that is
+ * not finite makes its own matrix NaN, no other.
+ * Workspace: gc_orthogonalize_workspace bytes (8 a value, and 8 m^2 a matrix, m the smaller side, and more for few and
+ * small ones).  The size depends on the current device's number of SMs.
+ */
+size_t gc_orthogonalize_workspace(int batch, int rows, int cols, int dtype);
+int gc_orthogonalize(const void* U, int64_t ldu, int64_t stride_u, int dtype, int batch, int rows, int cols,
+                     const float* coeffs, int steps, float eps, void* out, int64_t ldo, int64_t stride_o, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/* ---- update of matrices by orthogonalised momentum -----------------------------
+ * Beside gc_sgd_step, for the matrices of a model (vectors keep gc_sgd_step):
+ *   momentum <- mu momentum + g / Ntil
+ *   O         = gc_orthogonalize of momentum, or where nesterov != 0 of g / Ntil + mu momentum
+ *   w        <- (1 - lr weight_decay) w - lr scale O
+ * all fp32; g: a decoded gradient (the sum over Ntil points), say a slice of one.  w, momentum and g share no element.
+ * Layout, coeffs, steps and eps as above.  Workspace: gc_orthogonalize_workspace of GC_F32.
+ */
+int gc_muon_step(float* w, int64_t ldw, int64_t stride_w, float* momentum, int64_t ldm, int64_t stride_m, const float* g,
+                 int64_t ldg, int64_t stride_g, int batch, int rows, int cols, float lr, int64_t Ntil, float mu,
+                 int nesterov, float weight_decay, float scale, const float* coeffs, int steps, float eps, void* ws,
+                 size_t ws_bytes, void* stream);
 
 /* ---- Algorithm 1, Find-Encoding-Coeff, batched over patterns ----------
  * R      ell x m float64, the PS's Gaussian matrix (Sec. II).

@@ -1,9 +1,12 @@
-"""fp64 oracle of the language-model operators: dropout by counters, layer norm and its gradient, and
-softmax cross entropy over a vocabulary with its gradient, from their definitions.
+"""fp64 oracle of the language-model operators: dropout by counters, layer norm and its gradient,
+softmax cross entropy over a vocabulary with its gradient, linear layers with theirs, and the orthogonalised
+update of a matrix, from their definitions.
 
 Test infrastructure only; plain NumPy, no code shared with the CUDA path.
 """
 from __future__ import annotations
+
+import math
 
 import numpy as np
 
@@ -86,3 +89,73 @@ def softmax_xent(X, W, y, N):
     Xl = np.where(live[:, None], X, 0.0)
     G = np.stack([P[i * n_c:(i + 1) * n_c].T @ Xl[i * n_c:(i + 1) * n_c] for i in range(N)])
     return loss, lse, P @ W, G
+
+
+_erf = np.vectorize(math.erf, otypes=[np.float64])
+
+
+def activation(z, act):
+    """act(z) of "none", "relu", "gelu", "gelu_tanh" or "silu"."""
+    z = np.asarray(z, dtype=np.float64)
+    if act == "relu":
+        return np.maximum(z, 0)
+    if act == "gelu":
+        return 0.5 * z * (1 + _erf(z / math.sqrt(2)))
+    if act == "gelu_tanh":
+        return 0.5 * z * (1 + np.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)))
+    return z / (1 + np.exp(-z)) if act == "silu" else z
+
+
+def activation_grad(z, act):
+    """act'(z); of relu 0 at 0."""
+    z = np.asarray(z, dtype=np.float64)
+    if act == "relu":
+        return (z > 0).astype(np.float64)
+    if act == "gelu":
+        return 0.5 * (1 + _erf(z / math.sqrt(2))) + z * np.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    if act == "gelu_tanh":
+        k = math.sqrt(2 / math.pi)
+        t = np.tanh(k * (z + 0.044715 * z ** 3))
+        return 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * k * (1 + 3 * 0.044715 * z * z)
+    if act == "silu":
+        s = 1 / (1 + np.exp(-z))
+        return s * (1 + z * (1 - s))
+    return np.ones_like(z)
+
+
+def linear(x, W, bias=None, act="none", residual=None):
+    """(y, z): z = x W^T + bias, y = residual + act(z)."""
+    z = np.asarray(x, dtype=np.float64) @ np.asarray(W, dtype=np.float64).T
+    if bias is not None:
+        z = z + np.asarray(bias, dtype=np.float64)
+    y = activation(z, act)
+    return (y if residual is None else y + np.asarray(residual, dtype=np.float64)), z
+
+
+def linear_grad(dy, z, x, W, act, N):
+    """(dx, G: N x F C, Gb: N x F) for the gradient dy of y, chunks of equal rows."""
+    d = np.asarray(dy, dtype=np.float64) * (1 if act == "none" else activation_grad(z, act))
+    x = np.asarray(x, dtype=np.float64)
+    parts = list(zip(np.split(d, N), np.split(x, N)))
+    return (d @ np.asarray(W, dtype=np.float64), np.stack([(p.T @ q).ravel() for p, q in parts]),
+            np.stack([p.sum(0) for p, _ in parts]))
+
+
+def orthogonalize(u, coeffs=(3.4445, -4.7750, 2.0315), steps=5, eps=1e-7):
+    """X <- (a + b X X^T + c (X X^T)^2) X, `steps` times, from u / max(|u|, eps) (Frobenius)."""
+    u = np.asarray(u, dtype=np.float64)
+    a, b, c = coeffs
+    X = u / max(np.linalg.norm(u), eps)
+    for _ in range(steps):
+        A = X @ X.T
+        X = a * X + (b * A + c * A @ A) @ X
+    return X
+
+
+def muon_step(w, momentum, g, lr, points, mu=0.95, nesterov=True, weight_decay=0.0, scale=1.0, **ns):
+    """(w, momentum) after a step: momentum = mu momentum + g / points, and w = (1 - lr weight_decay) w
+    - lr scale O, O the orthogonalised momentum (nesterov: g / points + mu times the new one)."""
+    g = np.asarray(g, dtype=np.float64) / points
+    m = mu * np.asarray(momentum, dtype=np.float64) + g
+    o = orthogonalize(g + mu * m if nesterov else m, **ns)
+    return (1 - lr * weight_decay) * np.asarray(w, dtype=np.float64) - lr * scale * o, m

@@ -25,6 +25,7 @@ lib = ctypes.CDLL(library_path)
 GC_CYCLIC, GC_EXPLICIT = 0, 1
 GC_F32, GC_BF16 = 0, 1
 GC_LSQ, GC_LOGISTIC = 0, 1
+GC_ACT_NONE, GC_ACT_RELU, GC_ACT_GELU, GC_ACT_GELU_TANH, GC_ACT_SILU = range(5)
 
 _i, _sz, _p, _d, _f, _i64, _u64 = (ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_double,
                                    ctypes.c_float, ctypes.c_int64, ctypes.c_uint64)
@@ -88,6 +89,18 @@ _sig("gc_layer_norm_backward", _i, _p, _i64, _p, _i64, _p, _p, _p, _p, _i64, _i,
 _sig("gc_softmax_xent_workspace", _sz, _i, _i, _i, _i, _i, _i, _i, _i)
 _sig("gc_softmax_xent", _i, _p, _i64, _i, _p, _i64, _i, _p, _i, _i, _i, _i, _i, _p, _p, _p, _p, _i64, _p,
      _i64, _p, _sz, _p)
+
+_sig("gc_linear_workspace", _sz, _i64, _i, _i, _i, _i, _i, _i)
+_sig("gc_linear", _i, _p, _i64, _i, _p, _i64, _i, _p, _i, _p, _i64, _i64, _i, _i, _p, _i64, _p, _i64, _p, _sz,
+     _p)
+_sig("gc_linear_backward_workspace", _sz, *[_i] * 11)
+_sig("gc_linear_backward", _i, _p, _i64, _p, _i64, _p, _i64, _i, _p, _i64, _i, _i, _i, _i, _i, _i, _p, _i64, _p,
+     _i64, _p, _i64, _p, _sz, _p)
+
+_sig("gc_orthogonalize_workspace", _sz, _i, _i, _i, _i)
+_sig("gc_orthogonalize", _i, _p, _i64, _i64, _i, _i, _i, _i, _p, _i, _f, _p, _i64, _i64, _p, _sz, _p)
+_sig("gc_muon_step", _i, _p, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _i, _i, _i, _f, _i64, _f, _i, _f, _f, _p, _i,
+     _f, _p, _sz, _p)
 
 
 class GCError(RuntimeError):
@@ -428,6 +441,150 @@ def gc_softmax_xent(X, W, y, N: int, n_c: int, loss=True, row_loss=True, lse=Tru
     return {"loss": loss, "row_loss": row_loss, "lse": lse, "dX": dX, "G": G}
 
 
+# ---------------------------------------------------------------- linear layers
+def _out(t, shape, dtype, device):
+    """An output: the tensor given, one made for True, None for False."""
+    if isinstance(t, torch.Tensor):
+        return t
+    return torch.empty(shape, dtype=dtype, device=device) if t else None
+
+
+def _on_16(ptr, ld, rows, elt):
+    """Whether rows lie on 16-byte boundaries (a single one needs no stride)."""
+    return int(ptr is not None and ptr % 16 == 0 and (ld * elt % 16 == 0 or rows == 1))
+
+
+def _same_device(*tensors):
+    """Calls run on the current device's stream: its tensors alone."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != here:
+            raise ValueError(f"a tensor on {t.device}, but the current device is cuda:{here}")
+
+
+def gc_linear(x, W, bias=None, act: int = GC_ACT_NONE, residual=None, y=None, z=False,
+              ws: Workspace | None = None):
+    """y = residual + act(z), z = x W^T + bias (x rows x C, W F x C, float32 or bfloat16 each, bias F
+    float32).  Returns dict with y (x's type; a tensor given is written into, and may be the residual) and z
+    (None unless True or a tensor is given: what gc_linear_backward takes).  Rows may be strided."""
+    xt, wt = _elt(x, "x"), _elt(W, "W")
+    rows, C = x.shape
+    F = W.shape[0]
+    y = _out(True if y is None else y, (rows, F), x.dtype, x.device)
+    z = _out(z, (rows, F), x.dtype, x.device)
+    xp, ldx = _rows(x, x.dtype, "x", x.shape)
+    wp_, ldw = _rows(W, W.dtype, "W", (F, C))
+    rp, ldr = _rows(residual, x.dtype, "residual", (rows, F))
+    yp, ldy = _rows(y, x.dtype, "y", (rows, F))
+    zp, ldz = _rows(z, x.dtype, "z", (rows, F))
+    bp = _dev(bias, torch.float32, "bias", (F,))
+    _same_device(x, W, bias, residual, y, z)
+    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_linear_workspace", rows, C, F, xt, wt,
+                                        _on_16(xp, ldx, rows, x.element_size()),
+                                        _on_16(wp_, ldw, F, W.element_size())), x.device)
+    _check(lib.gc_linear(xp, ldx, xt, wp_, ldw, wt, bp, act, rp, ldr, rows, C, F, yp, ldy, zp, ldz, wp, wn,
+                         _stream()))
+    return {"y": y, "z": z}
+
+
+def gc_linear_backward(dy, x, W, N: int, n_c: int, z=None, act: int = GC_ACT_NONE, dx=True, G=True, Gb=True,
+                       ws: Workspace | None = None):
+    """Gradient of gc_linear from dy (N n_c x F, of y).  Returns dict with dx (x's type), G (N x F C float32:
+    per chunk the gradient of W, un-normalised) and Gb (N x F float32: of the bias); booleans ask for an
+    output, tensors are written into (G and Gb may be column slices of a larger matrix).  The gradient of the
+    residual is dy."""
+    xt, wt = _elt(x, "x"), _elt(W, "W")
+    T, C = x.shape
+    F = W.shape[0]
+    if T != N * n_c:
+        raise ValueError("x must have N * n_c rows")
+    dx, G = _out(dx, (T, C), x.dtype, x.device), _out(G, (N, F * C), torch.float32, x.device)
+    Gb = _out(Gb, (N, F), torch.float32, x.device)
+    yp, lddy = _rows(dy, x.dtype, "dy", (T, F))
+    zp, ldz = _rows(z, x.dtype, "z", (T, F))
+    xp, ldx = _rows(x, x.dtype, "x", (T, C))
+    wp_, ldw = _rows(W, W.dtype, "W", (F, C))
+    dp, lddx = _rows(dx, x.dtype, "dx", (T, C))
+    gp, ldg = _rows(G, torch.float32, "G", (N, F * C))
+    bp, ldgb = _rows(Gb, torch.float32, "Gb", (N, F))
+    _same_device(dy, x, W, z, dx, G, Gb)
+    e = x.element_size()
+    want = (dx is not None) + 2 * (G is not None) + 4 * (Gb is not None)
+    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_linear_backward_workspace", N, n_c, C, F,
+                                        xt, wt, act, _on_16(xp, ldx, T, e), _on_16(wp_, ldw, F, W.element_size()),
+                                        _on_16(yp, lddy, T, e), want), x.device)
+    _check(lib.gc_linear_backward(yp, lddy, zp, ldz, xp, ldx, xt, wp_, ldw, wt, act, N, n_c, C, F, dp, lddx, gp, ldg,
+                                  bp, ldgb, wp, wn, _stream()))
+    return {"dx": dx, "G": G, "Gb": Gb}
+
+
+# ---------------------------------------------------------------- orthogonalised updates
+def _mats(t, dtype, name, shape):
+    """(device pointer, row stride, matrix stride) of a CUDA matrix, or of a batch of them."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.stride(-1) != 1 and shape[-1] > 1:
+        raise ValueError(f"the elements of a row of {name} must lie next to each other")
+    ld = t.stride(-2) if shape[-2] > 1 else shape[-1]
+    return t.data_ptr(), ld, t.stride(0) if len(shape) == 3 else 0
+
+
+def _mats_of(t, name):
+    """(batch, rows, cols, element type) of a matrix or of a batch of them."""
+    if not isinstance(t, torch.Tensor) or t.dim() not in (2, 3):
+        raise TypeError(f"{name} must be a matrix or a batch of matrices")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    return (t.shape[0] if t.dim() == 3 else 1, t.shape[-2], t.shape[-1], GC_BF16 if t.dtype is torch.bfloat16 else GC_F32)
+
+
+def _coeffs(coeffs):
+    """Host array of the polynomial's three coefficients (None -> NULL)."""
+    if coeffs is None:
+        return None
+    if len(coeffs) != 3:
+        raise ValueError("coeffs must be three numbers")
+    return (ctypes.c_float * 3)(*coeffs)
+
+
+def gc_orthogonalize(u, coeffs=None, steps: int = 5, eps: float = 1e-7, out=None, ws: Workspace | None = None):
+    """u (rows x cols, or batch x rows x cols; float32 or bfloat16) with its singular values drawn towards 1 by
+    `steps` Newton-Schulz products, X <- (a + b X X^T + c (X X^T)^2) X from u / max(|u|, eps).  Returns
+    out, which may be u."""
+    batch, rows, cols, dt = _mats_of(u, "u")
+    if out is None:
+        out = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+    up, ldu, su = _mats(u, u.dtype, "u", u.shape)
+    op, ldo, so = _mats(out, u.dtype, "out", u.shape)
+    _same_device(u, out)
+    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_orthogonalize_workspace", batch, rows, cols, dt),
+                       u.device)
+    _check(lib.gc_orthogonalize(up, ldu, su, dt, batch, rows, cols, _coeffs(coeffs), steps, eps, op, ldo, so, wp, wn,
+                                _stream()))
+    return out
+
+
+def gc_muon_step(w, momentum, g, lr: float, Ntil: int, mu: float = 0.95, nesterov: bool = True,
+                 weight_decay: float = 0.0, scale: float = 1.0, coeffs=None, steps: int = 5, eps: float = 1e-7,
+                 ws: Workspace | None = None) -> None:
+    """momentum = mu momentum + g / Ntil; w = (1 - lr weight_decay) w - lr scale O, in place, with O the
+    orthogonalised momentum (of g / Ntil + mu momentum where nesterov).  w, momentum, g: float32, rows x cols or
+    batch x rows x cols, their rows strided as they may be."""
+    batch, rows, cols, _ = _mats_of(w, "w")
+    wp_, ldw, sw = _mats(w, torch.float32, "w", w.shape)
+    mp, ldm, sm = _mats(momentum, torch.float32, "momentum", w.shape)
+    gp, ldg, sg = _mats(g, torch.float32, "g", w.shape)
+    _same_device(w, momentum, g)
+    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_orthogonalize_workspace", batch, rows, cols,
+                                        GC_F32), w.device)
+    _check(lib.gc_muon_step(wp_, ldw, sw, mp, ldm, sm, gp, ldg, sg, batch, rows, cols, lr, Ntil, mu, int(nesterov),
+                            weight_decay, scale, _coeffs(coeffs), steps, eps, wp, wn, _stream()))
+
+
 # ---------------------------------------------------------------- Algorithm 1
 def gc_coeff_workspace(N, m, delta, ell, npat):
     return lib.gc_coeff_workspace(N, m, delta, ell, npat)
@@ -631,6 +788,8 @@ GC_STALL_CHUNK_GRADS = 1
 GC_STALL_COMBINE = 2
 GC_STALL_BATCHED = 4
 GC_STALL_XENT = 16
+GC_STALL_LINEAR = 32
+GC_STALL_MUON = 64
 
 
 def gc_inject_stall(kernels: int) -> None:

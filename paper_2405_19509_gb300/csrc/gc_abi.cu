@@ -114,7 +114,8 @@ int gc_version(void) { return 300; }
 uint64_t gc_kernel_launches(void) { return g_launches.load(); }
 
 int gc_inject_stall(int kernels) {
-  if (kernels & ~(GC_STALL_CHUNK_GRADS | GC_STALL_COMBINE | GC_STALL_BATCHED | GC_STALL_XENT))
+  if (kernels & ~(GC_STALL_CHUNK_GRADS | GC_STALL_COMBINE | GC_STALL_BATCHED | GC_STALL_XENT | GC_STALL_LINEAR |
+                  GC_STALL_MUON))
     return fail(GC_ERR_ARG, "kernels=0x%x has unknown bits", kernels);
   g_stall.store(kernels);
   return GC_OK;
@@ -416,6 +417,186 @@ int gc_softmax_xent(const void* X, int64_t ldx, int x_dtype, const void* W, int6
   Carve c(ws);
   const XentIO io{X, W, y, y64, loss, row_loss, lse, dX, G, ldx, ldw, lddx, ldg};
   return launch_xent(s, io, c, status_of(ws), as_stream(stream));
+}
+
+// ---------------------------------------------------------------- linear layers
+static int check_linear(int64_t T, int C, int F, int x_dtype, int w_dtype, int act) {
+  if (x_dtype != GC_F32 && x_dtype != GC_BF16) return fail(GC_ERR_ARG, "x_dtype=%d", x_dtype);
+  if (w_dtype != GC_F32 && w_dtype != GC_BF16) return fail(GC_ERR_ARG, "w_dtype=%d", w_dtype);
+  if (act < GC_ACT_NONE || act > GC_ACT_SILU) return fail(GC_ERR_ARG, "act=%d", act);
+  if (C < 1 || F < 1) return fail(GC_ERR_SHAPE, "C and F must be >= 1");
+  if (T > (1LL << 30)) return fail(GC_ERR_UNSUPPORTED, "%lld rows exceed 2^30", (long long)T);
+  if (C > (1 << 20) || F > (1 << 20)) return fail(GC_ERR_UNSUPPORTED, "C=%d or F=%d exceeds 2^20", C, F);
+  // tiles of 256 x 128 are counted in 32 bits
+  const long long mt = (T + 255) / 256;
+  if (mt * ((F + 127) / 128) > (1 << 30) || mt * ((C + 127) / 128) > (1 << 30))
+    return fail(GC_ERR_UNSUPPORTED, "too many tiles: %lld rows, C=%d, F=%d", (long long)T, C, F);
+  return GC_OK;
+}
+static bool on_16(const void* p, int64_t ld, int elt) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * elt % 16 == 0;
+}
+
+size_t gc_linear_workspace(int64_t rows, int C, int F, int x_dtype, int w_dtype, int x_16, int w_16) {
+  if (rows < 0 || check_linear(rows, C, F, x_dtype, w_dtype, GC_ACT_NONE)) return 0;
+  if (rows == 0) return kHeaderBytes;
+  return linear_ws_bytes(LinearShape{rows, C, F, x_dtype, w_dtype, GC_ACT_NONE, x_16, w_16});
+}
+
+int gc_linear(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ldw, int w_dtype, const float* bias,
+              int act, const void* residual, int64_t ldr, int64_t rows, int C, int F, void* y, int64_t ldy, void* z,
+              int64_t ldz, void* ws, size_t ws_bytes, void* stream) {
+  NvtxRange nvtx_("gc_linear");
+  if (rows < 0) return fail(GC_ERR_SHAPE, "rows must be >= 0");
+  int rc = check_linear(rows, C, F, x_dtype, w_dtype, act);
+  if (rc) return rc;
+  if (rows == 0) return GC_OK;
+  const int xe = x_dtype == GC_BF16 ? 2 : 4, we = w_dtype == GC_BF16 ? 2 : 4;
+  if ((rc = check_rows("X", X, ldx, rows, C, xe, true)) || (rc = check_rows("W", W, ldw, F, C, we, true)) ||
+      (rc = check_rows("bias", bias, F, 1, F, 4, false)) ||
+      (rc = check_rows("residual", residual, ldr, rows, F, xe, false)) ||
+      (rc = check_rows("y", y, ldy, rows, F, xe, true)) || (rc = check_rows("z", z, ldz, rows, F, xe, false)))
+    return rc;
+  if (y == X || z == X || y == z || (z && z == residual))
+    return fail(GC_ERR_ARG, "y and z must not be X or one another, nor z the residual");
+  // one row needs no stride, but the layout rules below read it
+  if (F == 1) ldw = (C + 7) / 8 * 8;
+  if (rows == 1) {
+    ldx = (C + 7) / 8 * 8;
+    ldr = ldy = ldz = (F + 7) / 8 * 8;
+  }
+  const LinearShape s{rows, C, F, x_dtype, w_dtype, act, on_16(X, ldx, xe), on_16(W, ldw, we)};
+  if ((rc = check_ws(ws, ws_bytes, linear_ws_bytes(s)))) return rc;
+  Carve c(ws);
+  const LinearIO io{X, W, bias, residual, y, z, ldx, ldw, ldr, ldy, ldz};
+  return launch_linear(s, io, c, status_of(ws), as_stream(stream));
+}
+
+static int check_linear_grad(int N, int n_c, int C, int F, int x_dtype, int w_dtype, int act) {
+  if (N < 1 || n_c < 1) return fail(GC_ERR_SHAPE, "N, n_c must be >= 1");
+  int rc = check_linear((int64_t)N * n_c, C, F, x_dtype, w_dtype, act);
+  if (rc) return rc;
+  if ((long long)N * ((F + 255) / 256) * ((C + 127) / 128) > (1 << 30) ||
+      (long long)N * ((n_c + 63) / 64) * ((F + 255) / 256) > (1 << 30) || (long long)N * ((F + 31) / 32) > (1 << 30))
+    return fail(GC_ERR_UNSUPPORTED, "too many tiles: N=%d, n_c=%d, C=%d, F=%d", N, n_c, C, F);
+  return GC_OK;
+}
+
+size_t gc_linear_backward_workspace(int N, int n_c, int C, int F, int x_dtype, int w_dtype, int act, int x_16,
+                                    int w_16, int dy_16, int want) {
+  if (check_linear_grad(N, n_c, C, F, x_dtype, w_dtype, act)) return 0;
+  return linear_grad_ws_bytes(LinearGradShape{N, n_c, C, F, x_dtype, w_dtype, act, x_16, w_16, dy_16, want});
+}
+
+int gc_linear_backward(const void* dy, int64_t lddy, const void* z, int64_t ldz, const void* X, int64_t ldx,
+                       int x_dtype, const void* W, int64_t ldw, int w_dtype, int act, int N, int n_c, int C, int F,
+                       void* dX, int64_t lddx, float* G, int64_t ldg, float* Gb, int64_t ldgb, void* ws,
+                       size_t ws_bytes, void* stream) {
+  NvtxRange nvtx_("gc_linear_backward");
+  int rc = check_linear_grad(N, n_c, C, F, x_dtype, w_dtype, act);
+  if (rc) return rc;
+  const int want = (dX ? LINEAR_DX : 0) | (G ? LINEAR_G : 0) | (Gb ? LINEAR_GB : 0);
+  if (!want) return fail(GC_ERR_ARG, "one of dX, G and Gb must be non-NULL");
+  const int64_t T = (int64_t)N * n_c;
+  const int xe = x_dtype == GC_BF16 ? 2 : 4, we = w_dtype == GC_BF16 ? 2 : 4;
+  if ((rc = check_rows("dy", dy, lddy, T, F, xe, true)) ||
+      (rc = check_rows("z", z, ldz, T, F, xe, act != GC_ACT_NONE)) ||
+      (rc = check_rows("X", X, ldx, T, C, xe, G != nullptr)) || (rc = check_rows("W", W, ldw, F, C, we, dX != nullptr)) ||
+      (rc = check_rows("dX", dX, lddx, T, C, xe, false)) ||
+      (rc = check_rows("G", G, ldg, N, (int64_t)F * C, 4, false)) || (rc = check_rows("Gb", Gb, ldgb, N, F, 4, false)))
+    return rc;
+  if (dX && (dX == dy || dX == X || dX == z || dX == W))
+    return fail(GC_ERR_ARG, "dX must not be one of the inputs");
+  // one row needs no stride, but the layout rules below read it
+  if (F == 1) ldw = (C + 7) / 8 * 8;
+  if (T == 1) {
+    ldx = lddx = (C + 7) / 8 * 8;
+    lddy = ldz = (F + 7) / 8 * 8;
+  }
+  if (N == 1) ldg = ((int64_t)F * C + 3) / 4 * 4;
+  const LinearGradShape s{N,   n_c, C, F, x_dtype, w_dtype, act, on_16(X, ldx, xe), on_16(W, ldw, we), on_16(dy, lddy, xe),
+                          want};
+  if ((rc = check_ws(ws, ws_bytes, linear_grad_ws_bytes(s)))) return rc;
+  Carve c(ws);
+  const LinearGradIO io{dy, z, X, W, dX, G, Gb, lddy, ldz, ldx, ldw, lddx, ldg, ldgb};
+  return launch_linear_grad(s, io, c, status_of(ws), as_stream(stream));
+}
+
+// ---------------------------------------------------------------- orthogonalised updates
+static int check_ns(int batch, int rows, int cols, int dtype) {
+  if (dtype != GC_F32 && dtype != GC_BF16) return fail(GC_ERR_ARG, "dtype=%d", dtype);
+  if (batch < 0 || rows < 1 || cols < 1) return fail(GC_ERR_SHAPE, "batch must be >= 0, rows and cols >= 1");
+  const int m = rows < cols ? rows : cols;
+  if (rows > (1 << 20) || cols > (1 << 20) || m > (1 << 15) || batch > (1 << 20))
+    return fail(GC_ERR_UNSUPPORTED, "%d matrices of %d x %d: more than 2^20 by 2^15, or more than 2^20 of them", batch, rows, cols);
+  // tiles of 256 x 128 and blocks of 32 x 32 are counted in 32 bits
+  if ((long long)batch * ((rows + 31) / 32) * ((cols + 31) / 32) > (1LL << 30))
+    return fail(GC_ERR_UNSUPPORTED, "too many tiles: %d matrices of %d x %d", batch, rows, cols);
+  return GC_OK;
+}
+// Matrices of rows ld apart that begin `stride` elements apart and share no element.
+static int check_mats(const char* name, const void* p, int64_t ld, int64_t stride, int batch, int rows, int cols, int elt) {
+  const int rc = check_rows(name, p, ld, rows, cols, elt, true);
+  if (rc || batch == 1) return rc;
+  const bool apart = stride >= (rows - 1) * ld + cols && stride <= (1LL << 40);  // one after the other
+  const bool beside = rows > 1 && stride >= cols && ld >= (batch - 1) * stride + cols;  // rows side by side
+  return apart || beside ? GC_OK : fail(GC_ERR_SHAPE, "%s: matrices %lld elements apart overlap", name, (long long)stride);
+}
+static int check_ns_args(const float* coeffs, int steps, float eps, NsShape* s) {
+  static const float kCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
+  if (steps < 1 || steps > 64) return fail(GC_ERR_ARG, "steps=%d outside [1, 64]", steps);
+  if (!(eps >= 0.f) || eps > 3.4e38f) return fail(GC_ERR_ARG, "eps=%g must be finite and >= 0", (double)eps);
+  for (int i = 0; i < 3; ++i) s->coeffs[i] = coeffs ? coeffs[i] : kCoeffs[i];
+  s->steps = steps;
+  if (!ns_coefficients_bounded(s->coeffs, steps))
+    return fail(GC_ERR_ARG, "coefficients (%g, %g, %g) take singular values of 1 past 4", (double)s->coeffs[0],
+                (double)s->coeffs[1], (double)s->coeffs[2]);
+  return GC_OK;
+}
+
+size_t gc_orthogonalize_workspace(int batch, int rows, int cols, int dtype) {
+  if (check_ns(batch, rows, cols, dtype)) return 0;
+  return batch == 0 ? kHeaderBytes : ns_ws_bytes(NsShape{batch, rows, cols, dtype, 0, {}});
+}
+
+int gc_orthogonalize(const void* U, int64_t ldu, int64_t stride_u, int dtype, int batch, int rows, int cols,
+                     const float* coeffs, int steps, float eps, void* out, int64_t ldo, int64_t stride_o, void* ws,
+                     size_t ws_bytes, void* stream) {
+  NvtxRange nvtx_("gc_orthogonalize");
+  NsShape s{batch, rows, cols, dtype, 0, {}};
+  int rc = check_ns(batch, rows, cols, dtype);
+  if (rc || (rc = check_ns_args(coeffs, steps, eps, &s))) return rc;
+  if (batch == 0) return GC_OK;
+  const int e = dtype == GC_BF16 ? 2 : 4;
+  if ((rc = check_mats("U", U, ldu, stride_u, batch, rows, cols, e)) ||
+      (rc = check_mats("out", out, ldo, stride_o, batch, rows, cols, e)))
+    return rc;
+  if ((rc = check_ws(ws, ws_bytes, ns_ws_bytes(s)))) return rc;
+  Carve c(ws);
+  const NsIO io{U, nullptr, out, ldu, stride_u, 0, 0, ldo, stride_o, eps, 0.f, 0.f, 0.f, 0.f, 0};
+  return launch_ns(s, io, c, status_of(ws), as_stream(stream));
+}
+
+int gc_muon_step(float* w, int64_t ldw, int64_t stride_w, float* momentum, int64_t ldm, int64_t stride_m, const float* g,
+                 int64_t ldg, int64_t stride_g, int batch, int rows, int cols, float lr, int64_t Ntil, float mu,
+                 int nesterov, float weight_decay, float scale, const float* coeffs, int steps, float eps, void* ws,
+                 size_t ws_bytes, void* stream) {
+  NvtxRange nvtx_("gc_muon_step");
+  NsShape s{batch, rows, cols, GC_F32, 0, {}};
+  int rc = check_ns(batch, rows, cols, GC_F32);
+  if (rc || (rc = check_ns_args(coeffs, steps, eps, &s))) return rc;
+  if (Ntil < 1) return fail(GC_ERR_ARG, "Ntil must be >= 1");
+  if (batch == 0) return GC_OK;
+  if ((rc = check_mats("w", w, ldw, stride_w, batch, rows, cols, 4)) ||
+      (rc = check_mats("momentum", momentum, ldm, stride_m, batch, rows, cols, 4)) ||
+      (rc = check_mats("g", g, ldg, stride_g, batch, rows, cols, 4)))
+    return rc;
+  if (w == momentum || w == g || momentum == g) return fail(GC_ERR_ARG, "w, momentum and g must be three matrices");
+  if ((rc = check_ws(ws, ws_bytes, ns_ws_bytes(s)))) return rc;
+  Carve c(ws);
+  const NsIO io{g, momentum, w, ldg, stride_g, ldm, stride_m, ldw, stride_w, eps, mu, (float)Ntil, 1.f - lr * weight_decay,
+                -lr * scale, nesterov != 0};
+  return launch_ns(s, io, c, status_of(ws), as_stream(stream));
 }
 
 // ---------------------------------------------------------------- Algorithm 1

@@ -207,6 +207,54 @@ struct XentIO {
 size_t xent_ws_bytes(const XentShape& s);
 int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* status, cudaStream_t st);
 
+// ---- linear layers (k_linear.cu, k_linear_grad.cu) ---------------------------
+struct LinearShape {
+  long long T;
+  int C, F, x_dtype, w_dtype, act;
+  int x_16, w_16;  // rows of X, W on 16-byte boundaries
+};
+struct LinearIO {
+  const void *X, *W;
+  const float* bias;
+  const void* res;
+  void *y, *z;
+  int64_t ldx, ldw, ldr, ldy, ldz;
+};
+size_t linear_ws_bytes(const LinearShape& s);
+int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t* status, cudaStream_t st);
+enum { LINEAR_DX = 1, LINEAR_G = 2, LINEAR_GB = 4 };
+struct LinearGradShape {
+  int N, n_c, C, F, x_dtype, w_dtype, act;
+  int x_16, w_16, dy_16;
+  int want;  // LINEAR_DX | LINEAR_G | LINEAR_GB
+};
+struct LinearGradIO {
+  const void *dy, *z, *X, *W;
+  void* dX;
+  float *G, *Gb;
+  int64_t lddy, ldz, ldx, ldw, lddx, ldg, ldgb;
+};
+size_t linear_grad_ws_bytes(const LinearGradShape& s);
+int launch_linear_grad(const LinearGradShape& s, const LinearGradIO& io, Carve& ws, uint32_t* status, cudaStream_t st);
+
+// ---- orthogonalised matrices and their momentum step (k_newton.cu) ------------
+struct NsShape {
+  int batch, rows, cols, dtype, steps;
+  float coeffs[3];
+};
+struct NsIO {
+  const void* u;    // the matrices; with m the gradients, `points` times what enters the momentum
+  float* m;         // momentum, or NULL
+  void* out;        // the result; with m: out = keep out + step result
+  int64_t ldu, su, ldm, sm, ldo, so;
+  float eps, mu, points, keep, step;
+  int nesterov;
+};
+// Whether the polynomial a s + b s^3 + c s^5 keeps singular values in the range of the kernels' operands.
+bool ns_coefficients_bounded(const float* coeffs, int steps);
+size_t ns_ws_bytes(const NsShape& s);
+int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cudaStream_t st);
+
 // ---- batched decode in residual form (k_decode_resid.cu) -----------------
 // Per pattern the ordered list of decode blocks that differ from I_ell (chunk
 // index and D = Pi - I).

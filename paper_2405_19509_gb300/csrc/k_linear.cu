@@ -1,0 +1,146 @@
+// A linear layer: z = x W^T + b, y = residual + act(z), for T rows of C values and F rows of W.
+//   k_parts         x and W as bf16 parts where they are fp32 or do not lie on 16-byte boundaries
+//   k_tiles<FwdOp>  z tile by tile in tensor memory; bias, activation and residual in the epilogue, z kept on request
+//   k_linear_join   the same epilogue where a tile's sum over C runs in ranges
+//
+// A bf16 x with a bf16 W is one product; an fp32 W enters it as hi + lo (2^-17), two products, so that a bf16 result
+// is rounded once.  An fp32 x enters as three parts, 24 bits: with an fp32 W six products (parts i + j < 3), which keep
+// what an fp32 product keeps.
+#include "linear_tiles.cuh"
+
+namespace gc {
+namespace {
+
+using namespace tiles;
+using namespace linear;
+
+struct FwdOp {
+  struct Params {
+    Common q;
+    Finish f;
+    long long T;
+    int mt, nt, tn, group;  // tiles of T and of F; row tiles that share a sweep of the columns
+    int nkb, ks, seg;       // K blocks, in ks ranges
+    int nx, nw, lim;
+    float* part;            // sums of the ranges [ks][T][ld_part]
+    int ld_part;
+  };
+  static __device__ __forceinline__ int jobs(const Params& p, int unit) {
+    return (int)(((long long)p.mt * p.nt * p.ks - unit + p.q.units - 1) / p.q.units);
+  }
+  static __device__ __forceinline__ Job job(const Params& p, int unit, int k) {
+    const int i = unit + k * p.q.units, at = i / p.ks;
+    const int per = p.group * p.nt, g = at / per, rem = at - g * per;
+    const int gm = min(p.group, p.mt - g * p.group);
+    const int n = rem / gm;
+    Job t;
+    t.kind = t.b = 0;
+    t.range = i - at * p.ks;
+    t.m0 = (g * p.group + rem - n * gm) * TM;
+    t.n0 = n * p.tn;
+    t.kb0 = (int)((long long)t.range * p.nkb / p.ks);
+    t.nkb = (int)((long long)(t.range + 1) * p.nkb / p.ks) - t.kb0;
+    t.na = p.nx;
+    t.nb = p.nw;
+    t.lim = p.lim;
+    t.seg = p.seg;
+    t.a_mn = t.b_mn = false;
+    return t;
+  }
+  template <int NC, int U, typename Get>
+  static __device__ __forceinline__ void store(const Params& p, const Job& t, int row0, int col0, uint8_t* box,
+                                               const CUtensorMap*, Get get) {
+    store_rows<NC, U>(p.f, p.T, p.ks > 1 ? p.part + (size_t)t.range * p.T * p.ld_part : nullptr, p.ld_part, row0, col0, box, get);
+  }
+};
+
+struct Scratch {
+  int Cp, nx, nw, lim, tn, ks, ld_part;
+  bool x_in_place, w_in_place;
+  __nv_bfloat16 *X, *W;
+  float* part;
+};
+
+Scratch carve_linear(Carve& c, const LinearShape& s) {
+  Scratch w{};
+  const bool xb = s.x_dtype == GC_BF16, wb = s.w_dtype == GC_BF16;
+  w.Cp = (s.C + 7) / 8 * 8;
+  w.nx = xb ? 1 : 3;
+  w.nw = wb ? 1 : xb ? 2 : 3;
+  w.lim = xb ? 2 : 3;
+  w.x_in_place = xb && s.x_16;
+  w.w_in_place = wb && s.w_16;
+  if (!w.x_in_place) w.X = c.take<__nv_bfloat16>((size_t)w.nx * s.T * w.Cp);
+  if (!w.w_in_place) w.W = c.take<__nv_bfloat16>((size_t)w.nw * s.F * w.Cp);
+  const int prod = products(w.nx, w.nw, w.lim);
+  const Split cut = split_of([&](int tn) { return (long long)tiles_of(s.T, TM) * tiles_of(s.F, tn); }, (double)s.T * s.F,
+                             (s.C + BK - 1) / BK, prod, device_sm_count() / 2);
+  w.tn = cut.tn;
+  w.ks = cut.ks;
+  w.ld_part = (s.F + 3) / 4 * 4;
+  if (w.ks > 1) w.part = c.take<float>((size_t)w.ks * s.T * w.ld_part);
+  return w;
+}
+
+}  // namespace
+
+size_t linear_ws_bytes(const LinearShape& s) {
+  Carve c(nullptr);
+  carve_linear(c, s);
+  return c.bytes();
+}
+
+int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t* status, cudaStream_t st) {
+  const Scratch w = carve_linear(ws, s);
+  const bool xb = s.x_dtype == GC_BF16;
+  int rc = GC_OK;
+  bool chained = false;
+  if (!w.x_in_place) {
+    if ((rc = launch_parts(io.X, s.x_dtype, io.ldx, s.T, s.C, w.Cp, w.nx, w.X, chained, st))) return rc;
+    chained = true;
+  }
+  if (!w.w_in_place) {
+    if ((rc = launch_parts(io.W, s.w_dtype, io.ldw, s.F, s.C, w.Cp, w.nw, w.W, chained, st))) return rc;
+    chained = true;
+  }
+  const void *X = w.x_in_place ? io.X : w.X, *W = w.w_in_place ? io.W : w.W;
+  const long long ldx = w.x_in_place ? io.ldx : w.Cp, ldw = w.w_in_place ? io.ldw : w.Cp;
+  FwdOp::Params p{};
+  const int e = xb ? 2 : 4;
+  auto fours = [&](const void* q, int64_t ld) {
+    return !q || (reinterpret_cast<uintptr_t>(q) % (4 * e) == 0 && ld % 4 == 0);
+  };
+  p.f = Finish{s.F, s.act, xb, io.bias, io.res, io.y, io.z, (long long)io.ldr, (long long)io.ldy, (long long)io.ldz,
+               fours(io.res, io.ldr) && fours(io.y, io.ldy) && fours(io.z, io.ldz)};
+  p.T = s.T;
+  p.tn = w.tn;
+  p.mt = tiles_of(s.T, TM);
+  p.nt = tiles_of(s.F, w.tn);
+  p.group = std::min(p.mt, 16);
+  p.nkb = (s.C + BK - 1) / BK;
+  p.ks = w.ks;
+  p.nx = w.nx;
+  p.nw = w.nw;
+  p.lim = w.lim;
+  p.seg = segment(xb, products(w.nx, w.nw, w.lim), p.nkb);
+  p.part = w.part;
+  p.ld_part = w.ld_part;
+  p.q.a_both = s.T > 128;
+  p.q.a_rows = s.T > 128 ? 128 : (int)(s.T + 7) / 8 * 8;
+  p.q.spin_limit = wait_limit(kSpin);
+  p.q.stall = take_stall(GC_STALL_LINEAR) ? 1 : 0;
+  p.q.status = status;
+  Maps m;
+  if ((rc = operand_map(&m.a[0], X, false, s.C, s.T, 1, w.nx, ldx, s.T * ldx, s.T * ldx, p.q.a_rows)) ||
+      (rc = operand_map(&m.b[0], W, false, s.C, s.F, 1, w.nw, ldw, s.F * ldw, s.F * ldw, w.tn / 2)))
+    return rc;
+  m.a[1] = m.out = m.a[0];
+  m.b[1] = m.b[0];
+  const long long jobs = (long long)p.mt * p.nt * p.ks;
+  rc = w.tn == 256 ? launch_tiles<FwdOp, 256>(m, p, jobs, w.nx, w.nw, "k_linear", chained, st)
+                   : launch_tiles<FwdOp, 128>(m, p, jobs, w.nx, w.nw, "k_linear", chained, st);
+  if (rc || w.ks == 1) return rc;
+  return launch_join(w.part, w.ks, s.T, w.ld_part, p.f, st);
+}
+
+}  // namespace gc

@@ -1,0 +1,360 @@
+// Gradient of a linear layer with its activation: d = dy act'(z), dx = d W, and per chunk of n_c points G_i = d_i^T x_i
+// (F x C) and Gb_i = sum_t d_t.
+//   k_linear_d       d as bf16 parts, and its column sums over 64 points at a time; k_linear_gb joins them
+//   k_tiles<GradOp>  dx and all chunks' G in one launch
+//   k_linear_join    dx where its tiles' sum over F runs in ranges
+//
+// G is a 32-bit result (what the encode takes): with bf16 rows d enters it as hi + lo (2^-17; exact where there is no
+// activation: d is dy, read in place), a bf16 dx, rounded to 2^-8, takes the hi alone.  fp32 rows enter as three parts, six
+// products.  The sums over a chunk depend on its points alone, bit for bit, whatever chunks a call has: the workers that
+// hold a chunk form one gradient.
+#include "linear_tiles.cuh"
+
+namespace gc {
+namespace {
+
+using namespace tiles;
+using namespace linear;
+using namespace rowwise;
+
+constexpr int kRowsD = 64;  // points of a block of k_linear_d
+
+// A block: 256 columns of 64 points of a chunk, a warp eight rows, four loads ahead.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256)
+    k_linear_d(const T* __restrict__ dy, long long lddy, const T* __restrict__ z, long long ldz, int act, int N, int n_c,
+               int F, int Fp, int np, __nv_bfloat16* __restrict__ d, float* __restrict__ sums, int R) {
+  __shared__ float red[8][kSeg];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int segs = (Fp + kSeg - 1) / kSeg;
+  const long long i = blockIdx.x, block = i / segs;
+  const int col0 = (int)(i - block * segs) * kSeg;
+  const int chunk = (int)(block / R), r0 = (int)(block - (long long)chunk * R) * kRowsD;
+  const int rows = min(kRowsD, n_c - r0);
+  const long long T_all = (long long)N * n_c, first = (long long)chunk * n_c + r0;
+  start_next();
+  wait_prior();
+  float sum[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+#pragma unroll 4
+  for (int r = warp; r < rows; r += 8) {
+    const long long row = first + r;
+    float v[8];
+    load_seg<VEC>(dy + row * lddy, col0, lane, F, v);
+    if (act != GC_ACT_NONE) {
+      float u[8];
+      load_seg<VEC>(z + row * ldz, col0, lane, F, u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= slope(act, u[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (!in_row<VEC>(col0, lane, j, F)) v[j] = 0.f;  // relu' of a zero that stands for nothing is one, NaN or not
+      sum[j] += v[j];
+    }
+    uint32_t far = 0;
+    for (int q = 0; q < np; ++q) {
+      float h[8];
+      next_part(v, far, h);
+      store_seg<VEC>(d + ((size_t)q * T_all + row) * Fp, col0, lane, Fp, h);
+    }
+  }
+  if (!sums) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) red[warp][j * 32 + lane] = sum[j];
+  __syncthreads();
+  const int c = VEC ? (int)(threadIdx.x & 31) * 8 + (int)(threadIdx.x >> 5) : (int)threadIdx.x;
+  float s = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) s += red[w][threadIdx.x];
+  if (col0 + c < F) sums[block * F + col0 + c] = s;
+}
+
+// Gb[chunk][c] from R partial sums: a block 32 columns, warp w the sums w, w + 8, ..., then the warps in order.
+__global__ void __launch_bounds__(256) k_linear_gb(const float* __restrict__ sums, int R, int F, float* __restrict__ Gb,
+                                                   long long ldgb) {
+  __shared__ float red[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int blocks = (F + 31) / 32, chunk = blockIdx.x / blocks, c = (blockIdx.x - chunk * blocks) * 32 + lane;
+  start_next();
+  wait_prior();
+  float s = 0.f;
+  if (c < F) {
+    const float* at = sums + (size_t)chunk * R * F + c;
+#pragma unroll 8
+    for (int r = warp; r < R; r += 8) s += __ldcg(at + (size_t)r * F);
+  }
+  red[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && c < F) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) s += red[w][lane];
+    Gb[chunk * ldgb + c] = s;
+  }
+}
+
+struct GradOp {
+  struct Params {
+    Common q;
+    Finish f;              // of dx
+    long long T;
+    int C, F, N;
+    int tn, mt, ct, ft;    // tiles of T, of C and of F
+    int ndx, ng, r, extra; // dx tiles, round robin; then G's, `extra` each for the units past the first r, which have
+                           // one dx tile less, and the rest round robin
+    int f_nkb, c_nkb, ks;  // K blocks of dx, in ks ranges, and of G
+    int np_dx, np, nx, nw, lim, seg_dx, seg_g;
+    float* part;
+    int ld_part;
+    float* G;
+    long long ldg;
+    int g_box;
+  };
+  static __device__ __forceinline__ int jobs(const Params& p, int unit) {
+    const int ndx = (p.ndx - unit + p.q.units - 1) / p.q.units;
+    const int rest = p.ng - p.extra * (p.q.units - p.r);
+    return ndx + (unit >= p.r ? p.extra : 0) + (rest - unit + p.q.units - 1) / p.q.units;
+  }
+  static __device__ __forceinline__ Job job(const Params& p, int unit, int k) {
+    Job t;
+    t.b_mn = true;
+    t.lim = p.lim;
+    const int ndx = (p.ndx - unit + p.q.units - 1) / p.q.units;
+    if (k < ndx) {
+      const int i = unit + k * p.q.units, at = i / p.ks;
+      t.kind = t.b = 0;
+      t.a_mn = false;
+      t.range = i - at * p.ks;
+      t.m0 = at / p.ct * TM;
+      t.n0 = at % p.ct * p.tn;
+      t.kb0 = (int)((long long)t.range * p.f_nkb / p.ks);
+      t.nkb = (int)((long long)(t.range + 1) * p.f_nkb / p.ks) - t.kb0;
+      t.na = p.np_dx;
+      t.nb = p.nw;
+      t.seg = p.seg_dx;
+      return t;
+    }
+    k -= ndx;
+    const int nb = p.q.units - p.r, mine = unit >= p.r ? p.extra : 0;
+    const int i = k < mine ? k * nb + unit - p.r : p.extra * nb + (k - mine) * p.q.units + unit;
+    const int per = p.ft * p.ct, c = i / per, rem = i - c * per;
+    t.kind = 1;
+    t.a_mn = true;
+    t.range = t.kb0 = 0;
+    t.b = c;
+    t.m0 = rem / p.ct * TM;
+    t.n0 = rem % p.ct * p.tn;
+    t.nkb = p.c_nkb;
+    t.na = p.np;
+    t.nb = p.nx;
+    t.seg = p.seg_g;
+    return t;
+  }
+  template <int NC, int U, typename Get>
+  static __device__ __forceinline__ void store(const Params& p, const Job& t, int row0, int col0, uint8_t* box,
+                                               const CUtensorMap* out, Get get) {
+    if (t.kind == 0) {
+      store_rows<NC, U>(p.f, p.T, p.ks > 1 ? p.part + (size_t)t.range * p.T * p.ld_part : nullptr, p.ld_part, row0, col0,
+                        box, get);
+      return;
+    }
+    const int lane = threadIdx.x & 31;
+    const int rows = min(p.F - row0, 32);
+#pragma unroll(U)
+    for (int c = 0; c < NC; ++c) {
+      float v[32];
+      __syncwarp();
+      get(c, v);
+      const int col = col0 + c * 32;
+      if (rows <= 0 || col >= p.C) continue;
+      if (p.g_box) {
+        if (lane == 0) bulk_wait_read<0>();  // the box's last store has read it
+        __syncwarp();
+        box_put(box, lane, v);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          store_3d(out, box, col, row0, t.b);
+          bulk_commit();
+        }
+      } else {
+        box_put(box, lane, v);
+        __syncwarp();
+        float* g = p.G + t.b * p.ldg + (long long)row0 * p.C + col + lane;
+        by_rows<8>(box, lane, col + lane < p.C ? rows : 0, [&](int r, float s) { g[(long long)r * p.C] = s; });
+      }
+    }
+    if (p.g_box) {  // a dx tile may use the box next
+      if (lane == 0) bulk_wait_read<0>();
+      __syncwarp();
+    }
+  }
+};
+
+struct Scratch {
+  int Cp, Fp, np, np_dx, nx, nw, lim, tn, ks, ld_part, R;
+  bool x_in_place, w_in_place, d_in_place, direct;  // direct: one partial sum a chunk, which is Gb
+  __nv_bfloat16 *X, *W, *D;
+  float *part, *sums;
+};
+
+Scratch carve_grad(Carve& c, const LinearGradShape& s) {
+  Scratch w{};
+  const long long T = (long long)s.N * s.n_c;
+  const bool xb = s.x_dtype == GC_BF16, wb = s.w_dtype == GC_BF16;
+  const bool dx = s.want & LINEAR_DX, g = s.want & LINEAR_G;
+  w.Cp = (s.C + 7) / 8 * 8;
+  w.Fp = (s.F + 7) / 8 * 8;
+  w.nx = xb ? 1 : 3;
+  w.nw = wb ? 1 : xb ? 2 : 3;
+  w.lim = xb ? 2 : 3;
+  w.np_dx = xb ? 1 : 3;
+  w.np = !dx && !g ? 0 : !xb ? 3 : g && s.act != GC_ACT_NONE ? 2 : 1;
+  w.d_in_place = xb && s.act == GC_ACT_NONE && s.dy_16;
+  w.x_in_place = xb && s.x_16;
+  w.w_in_place = wb && s.w_16;
+  if (w.np && !w.d_in_place) w.D = c.take<__nv_bfloat16>((size_t)w.np * T * w.Fp);
+  if (g && !w.x_in_place) w.X = c.take<__nv_bfloat16>((size_t)w.nx * T * w.Cp);
+  if (dx && !w.w_in_place) w.W = c.take<__nv_bfloat16>((size_t)w.nw * s.F * w.Cp);
+  w.R = (s.n_c + kRowsD - 1) / kRowsD;
+  if (s.want & LINEAR_GB) w.sums = c.take<float>((size_t)s.N * w.R * s.F);
+  // the cut whose estimated clocks are fewest, as split_of's, over both kinds of tiles
+  const int units = device_sm_count() / 2;
+  const int f_nkb = (s.F + BK - 1) / BK, c_nkb = (s.n_c + BK - 1) / BK;
+  const int p_dx = products(w.np_dx, w.nw, w.lim), p_g = products(w.np, w.nx, w.lim);
+  double least = 0;
+  w.tn = 256;
+  w.ks = 1;
+  for (int tn = 256; tn >= 128; tn /= 2) {
+    const double nd = dx ? (double)tiles_of(T, TM) * tiles_of(s.C, tn) : 0;
+    const double ng = g ? (double)s.N * tiles_of(s.F, TM) * tiles_of(s.C, tn) : 0;
+    const double one_g = ng > 0 ? c_nkb * p_g * 2.0 * tn + 600 : 0;
+    for (int ks = 1; ks <= (dx ? 32 : 1) && ks * 2 <= std::max(2, f_nkb); ++ks) {
+      if (ks > 1 && nd * (ks - 1) >= 2 * units) break;
+      const double one_d = nd > 0 ? (f_nkb + ks - 1) / ks * p_dx * 2.0 * tn + 600 : 0;
+      const double longest = std::max(one_d, one_g), share = (nd * ks * one_d + ng * one_g) / units;
+      double clk = std::max(longest, share + (nd * ks + ng > units ? std::min(longest, ng > 0 ? one_g : one_d) / 2 : 0));
+      if (ks > 1) clk += 5000 + (double)T * s.C * 8 * ks / 3500;
+      if (least == 0 || clk < least) {
+        least = clk;
+        w.tn = tn;
+        w.ks = ks;
+      }
+    }
+  }
+  w.ld_part = (s.C + 3) / 4 * 4;
+  if (w.ks > 1) w.part = c.take<float>((size_t)w.ks * T * w.ld_part);
+  return w;
+}
+
+template <typename T>
+int launch_d(const LinearGradShape& s, const LinearGradIO& io, const Scratch& w, int np, cudaStream_t st) {
+  const bool vec = s.F % 8 == 0 && rows_16(io.dy, io.lddy, sizeof(T)) && (s.act == GC_ACT_NONE || rows_16(io.z, io.ldz, sizeof(T)));
+  const long long grid = (long long)s.N * w.R * ((w.Fp + kSeg - 1) / kSeg);
+  return launch_chain(vec ? k_linear_d<T, true> : k_linear_d<T, false>, "k_linear_d", (unsigned)grid, 256, 0, 1, false, st,
+                      (const T*)io.dy, (long long)io.lddy, (const T*)io.z, (long long)io.ldz, s.act, s.N, s.n_c, s.F,
+                      w.Fp, np, w.D, w.sums, w.R);
+}
+
+}  // namespace
+
+size_t linear_grad_ws_bytes(const LinearGradShape& s) {
+  Carve c(nullptr);
+  carve_grad(c, s);
+  return c.bytes();
+}
+
+int launch_linear_grad(const LinearGradShape& s, const LinearGradIO& io, Carve& ws, uint32_t* status, cudaStream_t st) {
+  const Scratch w = carve_grad(ws, s);
+  const long long T = (long long)s.N * s.n_c;
+  const bool xb = s.x_dtype == GC_BF16;
+  const bool dx = s.want & LINEAR_DX, g = s.want & LINEAR_G;
+  int rc = GC_OK;
+  bool chained = false;
+  const int np = w.d_in_place ? 0 : w.np;
+  if (np || w.sums) {
+    rc = xb ? launch_d<__nv_bfloat16>(s, io, w, np, st) : launch_d<float>(s, io, w, np, st);
+    if (rc) return rc;
+    chained = true;
+  }
+  if (w.sums) {
+    if ((rc = launch_chain(k_linear_gb, "k_linear_gb", (unsigned)(s.N * ((s.F + 31) / 32)), 256, 0, 1, chained, st, w.sums,
+                           w.R, s.F, io.Gb, (long long)io.ldgb)))
+      return rc;
+  }
+  if (!dx && !g) return GC_OK;
+  if (g && !w.x_in_place) {
+    if ((rc = launch_parts(io.X, s.x_dtype, io.ldx, T, s.C, w.Cp, w.nx, w.X, chained, st))) return rc;
+    chained = true;
+  }
+  if (dx && !w.w_in_place) {
+    if ((rc = launch_parts(io.W, s.w_dtype, io.ldw, s.F, s.C, w.Cp, w.nw, w.W, chained, st))) return rc;
+    chained = true;
+  }
+  const void *X = w.x_in_place ? io.X : w.X, *W = w.w_in_place ? io.W : w.W, *D = w.d_in_place ? io.dy : w.D;
+  const long long ldx = w.x_in_place ? io.ldx : w.Cp, ldw = w.w_in_place ? io.ldw : w.Cp;
+  const long long ldd = w.d_in_place ? io.lddy : w.Fp;
+  GradOp::Params p{};
+  const int e = xb ? 2 : 4;
+  p.f = Finish{s.C, GC_ACT_NONE, xb, nullptr, nullptr, io.dX, nullptr, 0, (long long)io.lddx, 0,
+               reinterpret_cast<uintptr_t>(io.dX) % (4 * e) == 0 && io.lddx % 4 == 0};
+  p.T = T;
+  p.C = s.C;
+  p.F = s.F;
+  p.N = s.N;
+  p.tn = w.tn;
+  p.mt = tiles_of(T, TM);
+  p.ct = tiles_of(s.C, w.tn);
+  p.ft = tiles_of(s.F, TM);
+  p.f_nkb = (s.F + BK - 1) / BK;
+  p.c_nkb = (s.n_c + BK - 1) / BK;
+  p.ks = w.ks;
+  p.np_dx = w.np_dx;
+  p.np = w.np;
+  p.nx = w.nx;
+  p.nw = w.nw;
+  p.lim = w.lim;
+  const int prod_dx = products(w.np_dx, w.nw, w.lim), prod_g = products(w.np, w.nx, w.lim);
+  p.seg_dx = segment(xb, prod_dx, p.f_nkb);
+  p.seg_g = segment(false, prod_g, p.c_nkb);
+  p.part = w.part;
+  p.ld_part = w.ld_part;
+  p.G = io.G;
+  p.ldg = io.ldg;
+  p.ndx = dx ? p.mt * p.ct * p.ks : 0;
+  p.ng = g ? s.N * p.ft * p.ct : 0;
+  int units = 0;
+  if ((rc = w.tn == 256 ? resident<GradOp, 256>(&units) : resident<GradOp, 128>(&units))) return rc;
+  units = (int)std::min<long long>(units, (long long)p.ndx + p.ng);
+  p.r = p.ndx % units;
+  const double cost_dx = (double)p.f_nkb / p.ks * prod_dx, cost_g = (double)p.c_nkb * prod_g;
+  p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_g + 0.5), p.ng / (units - p.r));
+  p.q.a_both = T > 128;
+  p.q.a_rows = T > 128 ? 128 : (int)(T + 7) / 8 * 8;
+  p.q.spin_limit = wait_limit(kSpin);
+  p.q.stall = take_stall(GC_STALL_LINEAR) ? 1 : 0;
+  p.q.status = status;
+  Maps m;
+  if ((rc = operand_map(&m.a[0], D, false, s.F, T, 1, w.np, ldd, T * ldd, T * ldd, p.q.a_rows)) ||
+      (rc = operand_map(&m.a[1], D, false, s.F, s.n_c, s.N, w.np, ldd, s.n_c * ldd, T * ldd, BK)))
+    return rc;
+  m.b[0] = m.b[1] = m.out = m.a[0];
+  if (dx && (rc = operand_map(&m.b[0], W, false, s.C, s.F, 1, w.nw, ldw, s.F * ldw, s.F * ldw, BK))) return rc;
+  if (g) {
+    if ((rc = operand_map(&m.b[1], X, false, s.C, s.n_c, s.N, w.nx, ldx, s.n_c * ldx, T * ldx, BK))) return rc;
+    p.g_box = s.C % 4 == 0 && rows_16(io.G, io.ldg, 4);
+    if (p.g_box) {
+      const long long dg[3] = {s.C, s.F, s.N}, lg[2] = {s.C, io.ldg};
+      if ((rc = map_nd(&m.out, io.G, 3, dg, lg, 32, 1, MAP_F32))) return rc;
+    }
+  }
+  const long long jobs = (long long)p.ndx + p.ng;
+  const int most_a = std::max(dx ? w.np_dx : 0, g ? w.np : 0), most_b = std::max(dx ? w.nw : 0, g ? w.nx : 0);
+  rc = w.tn == 256 ? launch_tiles<GradOp, 256>(m, p, jobs, most_a, most_b, "k_linear_grad", chained, st)
+                   : launch_tiles<GradOp, 128>(m, p, jobs, most_a, most_b, "k_linear_grad", chained, st);
+  if (rc || !dx || w.ks == 1) return rc;
+  return launch_join(w.part, w.ks, T, w.ld_part, p.f, st);
+}
+
+}  // namespace gc

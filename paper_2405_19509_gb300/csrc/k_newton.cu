@@ -1,0 +1,623 @@
+// Newton-Schulz orthogonalisation of matrices, and the momentum step that uses it:
+//   X <- u / max(|u|_F, eps),  then `steps` times  A = X X^T,  P = a I + b A + c A^2,  X <- P X
+// an odd polynomial of the singular values, X X^T taken on the shorter side (m of m x n).
+//   k_ns_norm       momentum = mu momentum + g / Ntil (where there is one), and the sum of u's squares
+//   k_ns_scale      X as 16-bit parts
+//   k_tiles<NsOp>   the three products of a step, each with its epilogue: A, then P, then the next X; of the last step
+//                   the output, or w = keep w - step O
+//   k_ns_join       the same epilogues where a tile's sum runs in ranges
+//
+// X stays as u lies, wide or tall: of a tall u the products are X^T X and X P, whose operands are read MN-major, and
+// nothing is transposed.  A and P are symmetric: tiles above the diagonal are not formed but written as mirrors of those
+// below.
+//
+// Parts are fp16 of values times a power of two.  Singular values stay below kMost (the entry point checks the
+// polynomial), so entries of X, A and P fit, and the parts of an entry end at 2^-24 / scale, 2^-37 for X: what is lost is
+// absolute, beside singular values of 1.  An fp32 u takes two parts everywhere, 22 bits, three products each: the
+// iteration is as near to 64 bits as in fp32 (1 to 6e-6 in the 2-norm where fp32 has 2 to 11e-6; one part: 2e-3 to 2e-2).  A
+// bf16 u, whose result is rounded to 1.7e-3, takes X in one part in A, P in one part, and two where a part would show (A in
+// A^2, X in P X): 0.8 to 1.3e-3.
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "tc_tiles.cuh"
+
+namespace gc {
+namespace {
+
+using namespace tiles;
+using namespace rowwise;
+
+constexpr float kMost = 4.f;    // bound of the singular values
+constexpr float kTerms = 60.f;  // ... and of |a| + |b| s^2 + |c| s^4 over them
+constexpr float kSX = 8192.f, kSA = 2048.f, kSP = 1024.f;  // kSX kMost, kSA kMost^2 and kSP kTerms are below 65504
+
+// Parts [parts][batch][rows][ld] of matrices.
+struct Parts {
+  __half* p;
+  long long plane, mat;
+  int ld;
+};
+
+enum { NS_A, NS_P, NS_X, NS_OUT, NS_STEP };
+struct Epilogue {
+  int kind, rows, cols;
+  float s;             // scale of a sum
+  Parts out;
+  int np;              // parts of `out`
+  Parts A;             // NS_P: a I + b A + s sum
+  int na;
+  float a, b;
+  void* w;             // NS_OUT, NS_STEP: rows of results
+  long long ldw, sw;
+  int bf16, vec;       // vec: rows in groups of four
+  float keep;          // NS_STEP: w = keep w + s sum
+  const float* lam;    // [batch]: X is lam times what its parts hold
+
+  static __device__ __forceinline__ void get4(const __half* p, float (&v)[4]) {
+    const uint2 q = *reinterpret_cast<const uint2*>(p);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&q.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&q.y));
+    v[0] += a.x;
+    v[1] += a.y;
+    v[2] += b.x;
+    v[3] += b.y;
+  }
+  // Four neighbours as parts; rows of `out` end past a multiple of eight, so whole fours are stored.
+  __device__ __forceinline__ void put_parts(int mat, long long r, int c, float (&v)[4]) const {
+    __half* to = out.p + mat * out.mat + r * out.ld + c;
+    for (int q = 0; q < np; ++q, to += out.plane) {
+      const __half2 a = __floats2half2_rn(v[0], v[1]), b = __floats2half2_rn(v[2], v[3]);
+      *reinterpret_cast<uint2*>(to) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+      const float2 x = __half22float2(a), y = __half22float2(b);
+      v[0] -= x.x;
+      v[1] -= x.y;
+      v[2] -= y.x;
+      v[3] -= y.y;
+    }
+  }
+  __device__ __forceinline__ void one(int mat, float l, long long r, int c, float x) const {
+    x *= l;
+    if (bf16) {
+      reinterpret_cast<__nv_bfloat16*>(w)[mat * sw + r * ldw + c] = __float2bfloat16_rn(s * x);
+    } else {
+      float* to = reinterpret_cast<float*>(w) + mat * sw + r * ldw + c;
+      *to = kind == NS_STEP ? fmaf(s, x, keep * *to) : s * x;
+    }
+  }
+  __device__ __forceinline__ void four(int mat, float l, long long r, int c, float4 x) const {
+    x = make_float4(l * x.x, l * x.y, l * x.z, l * x.w);
+    if (bf16) {
+      const __nv_bfloat162 a = __floats2bfloat162_rn(s * x.x, s * x.y), b = __floats2bfloat162_rn(s * x.z, s * x.w);
+      *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(w) + mat * sw + r * ldw + c) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+      return;
+    }
+    float4* to = reinterpret_cast<float4*>(reinterpret_cast<float*>(w) + mat * sw + r * ldw + c);
+    if (kind == NS_STEP) {
+      const float4 o = *to;
+      *to = make_float4(fmaf(s, x.x, keep * o.x), fmaf(s, x.y, keep * o.y), fmaf(s, x.z, keep * o.z), fmaf(s, x.w, keep * o.w));
+    } else {
+      *to = make_float4(s * x.x, s * x.y, s * x.z, s * x.w);
+    }
+  }
+  // A box of 32 x 32 sums at (row0, col0); mirror: also at (col0, row0).
+  __device__ __forceinline__ void finish(uint8_t* box, int lane, int mat, int row0, int col0, bool mirror) const {
+    const int m = min(rows - row0, 32), n = cols - col0;
+    const float l = lam[mat], l2 = l * l;
+    if (kind >= NS_OUT) {
+      if (vec && n >= 32) {
+        by_fours(box, lane, [&](int r, int c, float4 x) {
+          if (r < m) four(mat, l, row0 + r, col0 + c, x);
+        });
+      } else {
+        by_rows<4>(box, lane, lane < n ? m : 0, [&](int r, float x) { one(mat, l, row0 + r, col0 + lane, x); });
+      }
+      return;
+    }
+    const float sum = kind == NS_P ? s * l2 * l2 : s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = i * 4 + (lane >> 3), c = (lane & 7) * 4;
+      float4* at = reinterpret_cast<float4*>(box + r * 128 + (((lane & 7) ^ (r & 7)) * 16));
+      const float4 x = *at;
+      float v[4] = {sum * x.x, sum * x.y, sum * x.z, sum * x.w};
+      if (r >= m || c >= n) continue;
+      if (kind == NS_P) {
+        float h[4] = {0.f, 0.f, 0.f, 0.f};
+        const __half* from = A.p + mat * A.mat + (long long)(row0 + r) * A.ld + col0 + c;
+        for (int q = 0; q < na; ++q, from += A.plane) get4(from, h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(b * l2, h[e], v[e]) + (row0 + r == col0 + c + e ? a : 0.f);
+      }
+      if (mirror) *at = make_float4(v[0], v[1], v[2], v[3]);
+      put_parts(mat, row0 + r, col0 + c, v);
+    }
+    if (!mirror) return;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = i * 4 + (lane >> 3), r = (lane & 7) * 4;
+      if (c >= n || r >= m) continue;
+      float v[4] = {box_at(box, r, c), box_at(box, r + 1, c), box_at(box, r + 2, c), box_at(box, r + 3, c)};
+      put_parts(mat, col0 + c, row0 + r, v);
+    }
+  }
+};
+
+// A tile's place: of a symmetric result the tiles of row tile i are those that begin at or before its last row.
+__host__ __device__ inline int sym_tiles(int rows, int tn) {
+  const int mt = (rows + TM - 1) / TM, nt = (rows + tn - 1) / tn, per = TM / tn;
+  return per * mt * (mt - 1) / 2 + nt;  // the last row tile has all of them
+}
+
+struct NsOp {
+  struct Params {
+    Common q;
+    Epilogue e;
+    int batch, mt, nt, per, tn, sym;  // tiles of rows, of columns, of a matrix
+    int nkb, ks, seg, na, nb, lim;
+    int a_mn, b_mn;
+    float* part;                      // sums of the ranges [ks][batch][rows][ld_part]
+    int ld_part;
+  };
+  static __device__ __forceinline__ int jobs(const Params& p, int unit) {
+    return (int)(((long long)p.batch * p.per * p.ks - unit + p.q.units - 1) / p.q.units);
+  }
+  static __device__ __forceinline__ Job job(const Params& p, int unit, int k) {
+    const int i = unit + k * p.q.units, at = i / p.ks;
+    Job t;
+    t.kind = 0;
+    t.range = i - at * p.ks;
+    t.b = at / p.per;
+    const int tile = at - t.b * p.per;
+    if (p.sym) {
+      const int w = TM / p.tn;  // row tile r begins at w r (r + 1) / 2
+      int r = (int)((sqrtf(8.f * (float)tile / (float)w + 1.f) - 1.f) * 0.5f);
+      while (w * r * (r + 1) / 2 > tile) --r;
+      while (r + 1 < p.mt && w * (r + 1) * (r + 2) / 2 <= tile) ++r;
+      t.m0 = r * TM;
+      t.n0 = (tile - w * r * (r + 1) / 2) * p.tn;
+    } else {
+      t.m0 = tile / p.nt * TM;
+      t.n0 = tile % p.nt * p.tn;
+    }
+    t.kb0 = (int)((long long)t.range * p.nkb / p.ks);
+    t.nkb = (int)((long long)(t.range + 1) * p.nkb / p.ks) - t.kb0;
+    t.na = p.na;
+    t.nb = p.nb;
+    t.lim = p.lim;
+    t.seg = p.seg;
+    t.a_mn = p.a_mn;
+    t.b_mn = p.b_mn;
+    return t;
+  }
+  template <int NC, int U, typename Get>
+  static __device__ __forceinline__ void store(const Params& p, const Job& t, int row0, int col0, uint8_t* box,
+                                               const CUtensorMap*, Get get) {
+    const int lane = threadIdx.x & 31;
+    const int rows = p.e.rows - row0;
+    const bool mirror = p.sym && t.n0 + p.tn <= t.m0;
+#pragma unroll(U)
+    for (int c = 0; c < NC; ++c) {
+      float v[32];
+      __syncwarp();
+      get(c, v);
+      const int col = col0 + c * 32;
+      if (rows <= 0 || col >= p.e.cols) continue;
+      box_put(box, lane, v);
+      __syncwarp();
+      if (p.ks > 1) {
+        float* to = p.part + (((size_t)t.range * p.batch + t.b) * p.e.rows + row0) * p.ld_part + col;
+        by_fours(box, lane, [&](int r, int j, float4 s) {
+          if (r < rows && col + j < p.e.cols) *reinterpret_cast<float4*>(to + (size_t)r * p.ld_part + j) = s;
+        });
+      } else {
+        p.e.finish(box, lane, t.b, row0, col, mirror);
+      }
+    }
+  }
+};
+
+// A warp a block of 32 x 32: the ranges' sums in their order, and the epilogue.
+__global__ void __launch_bounds__(128) k_ns_join(const float* __restrict__ part, int ks, int batch, int ld, int sym, int tn,
+                                                 const Epilogue e) {
+  __shared__ __align__(128) uint8_t boxes[4 * BOX];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint8_t* box = boxes + warp * BOX;
+  start_next();
+  wait_prior();
+  const int br = (e.rows + 31) / 32, bc = (e.cols + 31) / 32;
+  const long long i = (long long)blockIdx.x * 4 + warp;
+  if (i >= (long long)batch * br * bc) return;
+  const int mat = (int)(i / (br * bc)), at = (int)(i - (long long)mat * br * bc);
+  const int row0 = at / bc * 32, col0 = at % bc * 32;
+  const int m0 = row0 / TM * TM, n0 = col0 / tn * tn;
+  if (sym && n0 >= m0 + TM) return;
+  const size_t range = (size_t)batch * e.rows * ld;
+  const float* from = part + ((size_t)mat * e.rows + row0) * ld + col0;
+#pragma unroll
+  for (int g = 0; g < 8; ++g) {
+    const int r = g * 4 + (lane >> 3), j = lane & 7;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row0 + r < e.rows && col0 + 4 * j < e.cols) {
+      const float* p = from + (size_t)r * ld + 4 * j;
+      s = __ldcg(reinterpret_cast<const float4*>(p));
+      for (int k = 1; k < ks; ++k) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(p + k * range));
+        s.x += v.x;
+        s.y += v.y;
+        s.z += v.z;
+        s.w += v.w;
+      }
+    }
+    *reinterpret_cast<float4*>(box + r * 128 + ((j ^ (r & 7)) * 16)) = s;
+  }
+  __syncwarp();
+  e.finish(box, lane, mat, row0, col0, sym && n0 + tn <= m0);
+}
+
+// What u is: the matrix itself, or the momentum of a gradient (and, looking ahead, the gradient once more).
+struct Source {
+  const void* u;   // MOM: the gradient
+  float* m;        // MOM: the momentum
+  long long ldu, su, ldm, sm;
+  int rows, cols, batch, blocks, nesterov;
+  float mu, points;
+};
+
+template <typename T, bool VEC, bool MOM, bool UPDATE>
+__device__ __forceinline__ void load_u(const Source& s, int mat, int row, int col0, int lane, float (&v)[8]) {
+  const T* u = reinterpret_cast<const T*>(s.u) + mat * s.su + row * s.ldu;
+  if (!MOM) {
+    load_seg<VEC>(u, col0, lane, s.cols, v);
+    return;
+  }
+  float* m = s.m + mat * s.sm + row * s.ldm;
+  float g[8];
+  load_seg<VEC>(m, col0, lane, s.cols, v);
+  if (UPDATE || s.nesterov) {
+    load_seg<VEC>(u, col0, lane, s.cols, g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] = __fdiv_rn(g[j], s.points);
+  }
+  if (UPDATE) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __fmaf_rn(s.mu, v[j], g[j]);
+    store_seg<VEC>(m, col0, lane, s.cols, v);
+  }
+  if (s.nesterov) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __fmaf_rn(s.mu, v[j], g[j]);
+  }
+}
+
+// Sums of squares [batch][blocks], in 64 bits; eight values at a time in 32 where these hold them.
+template <typename T, bool VEC, bool MOM>
+__global__ void __launch_bounds__(256) k_ns_norm(const Source s, double* __restrict__ sums) {
+  __shared__ double red[8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int mat = blockIdx.x / s.blocks, block = blockIdx.x - mat * s.blocks;
+  const int segs = (s.cols + kSeg - 1) / kSeg;
+  start_next();
+  wait_prior();
+  double sum = 0;
+  const long long n = (long long)s.rows * segs;
+#pragma unroll 2
+  for (long long i = (long long)block * 8 + warp; i < n; i += (long long)s.blocks * 8) {
+    const int row = (int)(i / segs), col0 = (int)(i - (long long)row * segs) * kSeg;
+    float v[8];
+    load_u<T, VEC, MOM, MOM>(s, mat, row, col0, lane, v);
+    float q = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q = fmaf(v[j], v[j], q);
+    if (q > 1e-24f && q < 1e37f) {
+      sum += q;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += (double)v[j] * v[j];
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) red[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 8; ++w) sum += red[w];
+    sums[blockIdx.x] = sum;
+  }
+}
+
+// X / lam as parts, and lam: a power of two, 1 but where |u| is so far below eps that the steps, which enlarge nothing more
+// than `amp` times, leave X below that.  In its place the powers of A are taken times lam^2.
+template <typename T, bool VEC, bool MOM>
+__global__ void __launch_bounds__(256) k_ns_scale(const Source s, const double* __restrict__ sums, float eps, float amp, Parts X,
+                                                  int np, float* __restrict__ lam) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int mat = blockIdx.x / s.blocks, block = blockIdx.x - mat * s.blocks;
+  const int segs = (s.cols + kSeg - 1) / kSeg;
+  start_next();
+  wait_prior();
+  double sum = 0;
+  for (int i = lane; i < s.blocks; i += 32) sum += __ldcg(sums + (size_t)mat * s.blocks + i);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  // u / norm as three factors, none of which leaves fp32's range: norm = f 2^e
+  double norm = sqrt(sum);
+  int down = 0;  // lam = 2^-down
+  if (norm < (double)eps) {
+    const double t = norm / (double)eps * (double)amp;
+    if (t < 1) down = t > 0x1p-125 ? -ilogb(t) - 1 : 125;  // t <= lam < 2 t
+    norm = eps;
+  }
+  if (block == 0 && threadIdx.x == 0) lam[mat] = ldexpf(1.f, -down);
+  int e = 0;
+  const double f = frexp(norm, &e);
+  e -= down;
+  const float r = isinf(norm) ? 0.f : (float)((double)kSX / f);
+  const float p0 = isinf(norm) || isnan(norm) ? 1.f : ldexpf(1.f, -(e / 2)), p1 = isinf(norm) || isnan(norm) ? 1.f : ldexpf(1.f, -(e - e / 2));
+  const long long n = (long long)s.rows * segs;
+#pragma unroll 2
+  for (long long i = (long long)block * 8 + warp; i < n; i += (long long)s.blocks * 8) {
+    const int row = (int)(i / segs), col0 = (int)(i - (long long)row * segs) * kSeg;
+    float v[8];
+    load_u<T, VEC, MOM, false>(s, mat, row, col0, lane, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = v[j] * p0 * p1 * r;
+    __half* to = X.p + mat * X.mat + (long long)row * X.ld;
+    for (int q = 0; q < np; ++q, to += X.plane) {
+      float h[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const __half x = __float2half_rn(v[j]);
+        h[j] = __half2float(x);
+        v[j] -= h[j];
+      }
+      if (VEC) {
+        const int c = col0 + lane * 8;
+        if (c < X.ld) {
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const __half2 t = __floats2half2_rn(h[2 * j], h[2 * j + 1]);
+            w[j] = *reinterpret_cast<const uint32_t*>(&t);
+          }
+          *reinterpret_cast<uint4*>(to + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = col0 + j * 32 + lane;
+          if (c < s.cols) to[c] = __float2half_rn(h[j]);
+        }
+      }
+    }
+  }
+}
+
+// One of a step's products: result rows x cols over K.
+struct Product {
+  int rows, cols, K, sym;
+  int na, nb, a_mn, b_mn;
+  int lim() const { return std::max(na, nb); }
+  int prod() const { return products(na, nb, lim()); }
+};
+
+Split cut_of(const Product& g, int batch) {
+  return split_of([&](int tn) { return (long long)batch * (g.sym ? sym_tiles(g.rows, tn) : tiles_of(g.rows, TM) * tiles_of(g.cols, tn)); },
+                  (double)batch * g.rows * g.cols, (g.K + BK - 1) / BK, g.prod(), device_sm_count() / 2);
+}
+
+struct Scratch {
+  bool wide;
+  int m, n, xa, aa, pp, xx;  // parts: of X in A, of A in A^2, of P and of X in P X
+  int blocks;
+  Parts X[2], A, P;
+  double* sums;
+  float *lam, *part;
+  Product pa, pp2, px;
+  Split ca, cp, cx;
+};
+
+Parts take_parts(Carve& c, int np, int batch, int rows, int cols) {
+  Parts t;
+  t.ld = (cols + 7) / 8 * 8;
+  t.mat = (long long)rows * t.ld;
+  t.plane = batch * t.mat;
+  t.p = c.take<__half>((size_t)np * t.plane);
+  return t;
+}
+
+Scratch carve_ns(Carve& c, const NsShape& s) {
+  Scratch w{};
+  const bool bf = s.dtype == GC_BF16;
+  w.wide = s.rows <= s.cols;
+  w.m = std::min(s.rows, s.cols);
+  w.n = std::max(s.rows, s.cols);
+  w.xa = w.pp = bf ? 1 : 2;
+  w.aa = w.xx = 2;
+  const long long segs = (long long)s.rows * ((s.cols + kSeg - 1) / kSeg);
+  // some 16 warps of loads an SM, over all matrices
+  w.blocks = (int)std::max(1LL, std::min((segs + 15) / 16, 8LL * device_sm_count() / std::min(s.batch, 8 * device_sm_count())));
+  w.X[0] = take_parts(c, w.xx, s.batch, s.rows, s.cols);
+  w.X[1] = take_parts(c, w.xx, s.batch, s.rows, s.cols);
+  w.A = take_parts(c, w.aa, s.batch, w.m, w.m);
+  w.P = take_parts(c, w.pp, s.batch, w.m, w.m);
+  w.sums = c.take<double>((size_t)s.batch * w.blocks);
+  w.lam = c.take<float>(s.batch);
+  w.pa = Product{w.m, w.m, w.n, 1, w.xa, w.xa, !w.wide, !w.wide};
+  w.pp2 = Product{w.m, w.m, w.m, 1, w.aa, w.aa, 0, 0};
+  w.px = w.wide ? Product{w.m, w.n, w.m, 0, w.pp, w.xx, 0, 1} : Product{w.n, w.m, w.m, 0, w.xx, w.pp, 0, 0};
+  w.ca = cut_of(w.pa, s.batch);
+  w.cp = cut_of(w.pp2, s.batch);
+  w.cx = cut_of(w.px, s.batch);
+  size_t part = 0;
+  auto need = [&](const Product& g, const Split& t) {
+    if (t.ks > 1) part = std::max(part, (size_t)t.ks * s.batch * g.rows * ((g.cols + 3) / 4 * 4));
+  };
+  need(w.pa, w.ca);
+  need(w.pp2, w.cp);
+  need(w.px, w.cx);
+  if (part) w.part = c.take<float>(part);
+  return w;
+}
+
+int launch_product(const NsShape& s, const Product& g, const Split& cut, const Parts& A, const Parts& B, const Epilogue& e,
+                   bool bits16, float* part, uint32_t* status, bool stall, const char* name, cudaStream_t st) {
+  NsOp::Params p{};
+  p.e = e;
+  p.batch = s.batch;
+  p.tn = cut.tn;
+  p.sym = g.sym;
+  p.mt = tiles_of(g.rows, TM);
+  p.nt = tiles_of(g.cols, cut.tn);
+  p.per = g.sym ? sym_tiles(g.rows, cut.tn) : p.mt * p.nt;
+  p.nkb = (g.K + BK - 1) / BK;
+  p.ks = cut.ks;
+  p.na = g.na;
+  p.nb = g.nb;
+  p.lim = g.lim();
+  p.seg = segment(bits16, g.prod(), p.nkb);
+  p.a_mn = g.a_mn;
+  p.b_mn = g.b_mn;
+  p.part = part;
+  p.ld_part = (g.cols + 3) / 4 * 4;
+  p.q.f16 = 1;
+  p.q.a_both = g.rows > 128;
+  p.q.a_rows = g.rows > 128 ? 128 : (g.rows + 7) / 8 * 8;
+  p.q.spin_limit = wait_limit(kSpin);
+  p.q.stall = stall;
+  p.q.status = status;
+  Maps m;
+  int rc;
+  auto map = [&](CUtensorMap* t, const Parts& x, int np, int mn, int extent, int box) {
+    return mn ? operand_map(t, x.p, true, extent, g.K, s.batch, np, x.ld, x.mat, x.plane, BK)
+              : operand_map(t, x.p, true, g.K, extent, s.batch, np, x.ld, x.mat, x.plane, box);
+  };
+  if ((rc = map(&m.a[0], A, g.na, g.a_mn, g.rows, p.q.a_rows)) || (rc = map(&m.b[0], B, g.nb, g.b_mn, g.cols, cut.tn / 2)))
+    return rc;
+  m.a[1] = m.out = m.a[0];
+  m.b[1] = m.b[0];
+  const long long jobs = (long long)s.batch * p.per * p.ks;
+  rc = cut.tn == 256 ? launch_tiles<NsOp, 256>(m, p, jobs, g.na, g.nb, name, true, st)
+                     : launch_tiles<NsOp, 128>(m, p, jobs, g.na, g.nb, name, true, st);
+  if (rc || p.ks == 1) return rc;
+  const long long blocks = (long long)s.batch * ((g.rows + 31) / 32) * ((g.cols + 31) / 32);
+  return launch_chain(k_ns_join, "k_ns_join", (unsigned)((blocks + 3) / 4), 128, 0, 1, true, st, (const float*)part, p.ks, s.batch,
+                      p.ld_part, g.sym, cut.tn, e);
+}
+
+template <typename T, bool MOM>
+int launch_start(const Source& src, const Scratch& w, bool vec, float eps, float amp, cudaStream_t st) {
+  const unsigned grid = (unsigned)(src.batch * src.blocks);
+  int rc = launch_chain(vec ? k_ns_norm<T, true, MOM> : k_ns_norm<T, false, MOM>, "k_ns_norm", grid, 256, 0, 1, false, st, src,
+                        w.sums);
+  if (rc) return rc;
+  return launch_chain(vec ? k_ns_scale<T, true, MOM> : k_ns_scale<T, false, MOM>, "k_ns_scale", grid, 256, 0, 1, true, st, src,
+                      (const double*)w.sums, eps, amp, w.X[0], std::max(w.xa, w.xx), w.lam);
+}
+
+// f(largest singular value, largest factor it may have come by) after each step, from singular values of at most 1.  The
+// largest value of a s + b s^3 + c s^5 is at the end of the range, or where the slope a + 3 b q + 5 c q^2, q = s^2, is zero.
+template <typename F>
+void polynomial_bounds(const float* k, int steps, F f) {
+  const double a = k[0], b = k[1], c = k[2];
+  double most = 1;
+  auto value = [&](double x) { return fabs(x * (a + x * x * (b + x * x * c))); };
+  for (int i = 0; i < steps; ++i) {
+    const double terms = fabs(a) + most * most * (fabs(b) + most * most * fabs(c));
+    double next = value(most);
+    const double d = 9 * b * b - 20 * a * c;
+    double roots[2] = {-1, -1};
+    if (c != 0 && d >= 0) {
+      roots[0] = (-3 * b + sqrt(d)) / (10 * c);
+      roots[1] = (-3 * b - sqrt(d)) / (10 * c);
+    } else if (c == 0 && b != 0) {
+      roots[0] = -a / (3 * b);
+    }
+    for (double q : roots)
+      if (q > 0 && q < most * most) next = std::max(next, value(sqrt(q)));
+    f(next, terms);
+    most = std::max(next, 1e-30);
+  }
+}
+
+}  // namespace
+
+bool ns_coefficients_bounded(const float* k, int steps) {
+  bool ok = true;
+  polynomial_bounds(k, steps, [&](double most, double slope) { ok = ok && most <= kMost && slope <= kTerms; });
+  return ok;
+}
+
+size_t ns_ws_bytes(const NsShape& s) {
+  Carve c(nullptr);
+  carve_ns(c, s);
+  return c.bytes();
+}
+
+int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cudaStream_t st) {
+  const Scratch w = carve_ns(ws, s);
+  const bool bf = s.dtype == GC_BF16, mom = io.m != nullptr;
+  const int e = bf ? 2 : 4;
+  Source src{io.u, io.m, (long long)io.ldu, (long long)io.su, (long long)io.ldm, (long long)io.sm,
+             s.rows, s.cols, s.batch, w.blocks, io.nesterov, io.mu, io.points};
+  const bool vec = s.cols % 8 == 0 && rows_16(io.u, io.ldu, e) && (s.batch == 1 || io.su * e % 16 == 0) &&
+                   (!mom || (rows_16(io.m, io.ldm, 4) && (s.batch == 1 || io.sm % 4 == 0)));
+  double amp = 1, now = 1;
+  polynomial_bounds(s.coeffs, s.steps, [&](double, double slope) { amp = std::max(amp, now *= slope); });
+  const float most = (float)std::min(amp, 1e30);
+  int rc = mom  ? launch_start<float, true>(src, w, vec, io.eps, most, st)
+           : bf ? launch_start<__nv_bfloat16, false>(src, w, vec, io.eps, most, st)
+                : launch_start<float, false>(src, w, vec, io.eps, most, st);
+  if (rc) return rc;
+  bool stall = take_stall(GC_STALL_MUON);
+  for (int i = 0; i < s.steps; ++i) {
+    const Parts &X = w.X[i & 1], &Y = w.X[1 - (i & 1)];
+    Epilogue ea{};
+    ea.kind = NS_A;
+    ea.rows = ea.cols = w.m;
+    ea.s = kSA / (kSX * kSX);
+    ea.out = w.A;
+    ea.np = w.aa;
+    ea.lam = w.lam;
+    if ((rc = launch_product(s, w.pa, w.ca, X, X, ea, bf, w.part, status, stall, "k_ns_a", st))) return rc;
+    stall = false;
+    Epilogue ep = ea;
+    ep.kind = NS_P;
+    ep.s = s.coeffs[2] * (kSP / (kSA * kSA));
+    ep.out = w.P;
+    ep.np = w.pp;
+    ep.A = w.A;
+    ep.na = w.aa;
+    ep.a = s.coeffs[0] * kSP;
+    ep.b = s.coeffs[1] * (kSP / kSA);
+    if ((rc = launch_product(s, w.pp2, w.cp, w.A, w.A, ep, bf, w.part, status, false, "k_ns_p", st))) return rc;
+    Epilogue ex{};
+    ex.lam = w.lam;
+    ex.rows = s.rows;
+    ex.cols = s.cols;
+    if (i + 1 < s.steps) {
+      ex.kind = NS_X;
+      ex.s = 1.f / kSP;
+      ex.out = Y;
+      ex.np = w.xx;
+    } else {
+      ex.kind = mom ? NS_STEP : NS_OUT;
+      ex.s = (mom ? io.step : 1.f) / (kSP * kSX);
+      ex.keep = io.keep;
+      ex.w = io.out;
+      ex.ldw = io.ldo;
+      ex.sw = io.so;
+      ex.bf16 = bf;
+      ex.vec = reinterpret_cast<uintptr_t>(io.out) % (4 * e) == 0 && io.ldo % 4 == 0 &&
+               (s.batch == 1 || io.so % 4 == 0);
+    }
+    if ((rc = launch_product(s, w.px, w.cx, w.wide ? w.P : X, w.wide ? X : w.P, ex, bf, w.part, status, false, "k_ns_x", st)))
+      return rc;
+  }
+  return GC_OK;
+}
+
+}  // namespace gc

@@ -31,11 +31,10 @@
 // 8,192 points, C = 2048, V = 65536, bf16: losses alone 1.11 ms, 1.97 PFLOP/s, the rate of the library's bf16
 // product (the tensor pipe is active 90% of the clocks), 1.65 ms with MMAs issued from a branch; with the
 // gradient in eight chunks 7.0 ms, 11.0 TFLOP issued at 1.57 PFLOP/s, near what the power limit allows (1.7).
-#include <cudaTypedefs.h>
-
 #include <algorithm>
 
 #include "rowwise.cuh"
+#include "tc_host.cuh"
 #include "tc_pair.cuh"
 
 namespace gc {
@@ -980,62 +979,6 @@ __global__ void __launch_bounds__(1024) k_xent_loss(const float* __restrict__ ro
   }
 }
 
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn_x() {
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) ==
-            cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
-    return PFN_cuTensorMapEncodeTiled_v12000(nullptr);
-  }();
-  return fn;
-}
-
-// Map of `rank` dimensions, bf16 or fp32, innermost first; ld[i]: elements between neighbours of
-// dimension i + 1.  Box 128 bytes x box_rows x box_planes, 128-byte swizzle.
-int map_nd(CUtensorMap* map, const void* base, int rank, const long long* dims, const long long* ld,
-           int box_rows, int box_planes = 1, bool f32 = false) {
-  auto fn = encode_fn_x();
-  if (!fn) return fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
-  cuuint64_t d[4], st[3];
-  cuuint32_t box[4] = {f32 ? 32u : 64u, (cuuint32_t)box_rows, (cuuint32_t)box_planes, 1}, one[4] = {1, 1, 1, 1};
-  for (int i = 0; i < rank; ++i) d[i] = (cuuint64_t)dims[i];
-  for (int i = 0; i + 1 < rank; ++i) st[i] = (cuuint64_t)ld[i] * (f32 ? 4 : 2);
-  const CUresult r = fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st,
-                        box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? GC_OK : fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
-}
-
-// A launch with clusters of `cl` CTAs (1: none); `chained`: as a dependent of the call's kernel before it.
-template <typename... P, typename... A>
-int launch_chain(void (*kern)(P...), const char* name, unsigned grid, int block, size_t smem, int cl, bool chained,
-                 cudaStream_t s, A... args) {
-  cudaLaunchAttribute at[2];
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3((unsigned)block);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cfg.attrs = at;
-  if (cl > 1) {
-    at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-    at[cfg.numAttrs].val.clusterDim.x = (unsigned)cl;
-    at[cfg.numAttrs].val.clusterDim.y = at[cfg.numAttrs].val.clusterDim.z = 1;
-    ++cfg.numAttrs;
-  }
-  if (chained) {
-    at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-    ++cfg.numAttrs;
-  }
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
-  count_launches(1);
-  return cuda_check(e, name);
-}
-
 // Pairs that the current device holds at once.
 template <int MODE>
 int resident(int* units) {
@@ -1311,12 +1254,12 @@ int launch_xent(const XentShape& s, const XentIO& io, Carve& ws, uint32_t* statu
   p.g_box = io.G && s.C % 4 == 0 && rowwise::rows_16(io.G, io.ldg, 4);
   if (p.g_box) {
     const long long dg[3] = {s.C, s.V, s.N}, lg[2] = {s.C, io.ldg};
-    if ((rc = map_nd(&mG, io.G, 3, dg, lg, 32, 1, true))) return rc;
+    if ((rc = map_nd(&mG, io.G, 3, dg, lg, 32, 1, MAP_F32))) return rc;
   }
   p.acc_box = p.acc && (s.want & XENT_DX) && rowwise::rows_16(p.acc, p.ld_acc, 4);
   if (p.acc_box) {
     const long long da[3] = {s.C, T, std::max(1, w.ks)}, la[2] = {p.ld_acc, T * p.ld_acc};
-    if ((rc = map_nd(&mAcc, p.acc, 3, da, la, 32, 1, true))) return rc;
+    if ((rc = map_nd(&mAcc, p.acc, 3, da, la, 32, 1, MAP_F32))) return rc;
   }
   for (int v0 = 0; v0 < s.V; v0 += w.piece) {
     p.v0 = v0;
