@@ -47,10 +47,11 @@ struct FwdOp {
     t.a_mn = t.b_mn = false;
     return t;
   }
-  template <int NC, int U, typename Get>
+  template <int NC, typename Get>
   static __device__ __forceinline__ void store(const Params& p, const Job& t, int row0, int col0, uint8_t* box,
-                                               const CUtensorMap*, Get get) {
-    store_rows<NC, U>(p.f, p.T, p.ks > 1 ? p.part + (size_t)t.range * p.T * p.ld_part : nullptr, p.ld_part, row0, col0, box, get);
+                                               const CUtensorMap* out, Get get) {
+    store_rows<NC>(p.f, p.T, p.ks > 1 ? p.part + (size_t)t.range * p.T * p.ld_part : nullptr, p.ld_part, row0, col0, box, out,
+                   get);
   }
 };
 
@@ -111,7 +112,7 @@ int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t*
     return !q || (reinterpret_cast<uintptr_t>(q) % (4 * e) == 0 && ld % 4 == 0);
   };
   p.f = Finish{s.F, s.act, xb, io.bias, io.res, io.y, io.z, (long long)io.ldr, (long long)io.ldy, (long long)io.ldz,
-               fours(io.res, io.ldr) && fours(io.y, io.ldy) && fours(io.z, io.ldz)};
+               fours(io.res, io.ldr) && fours(io.y, io.ldy) && fours(io.z, io.ldz), 0};
   p.T = s.T;
   p.tn = w.tn;
   p.mt = tiles_of(s.T, TM);
@@ -134,8 +135,9 @@ int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t*
   if ((rc = operand_map(&m.a[0], X, false, s.C, s.T, 1, w.nx, ldx, s.T * ldx, s.T * ldx, p.q.a_rows)) ||
       (rc = operand_map(&m.b[0], W, false, s.C, s.F, 1, w.nw, ldw, s.F * ldw, s.F * ldw, w.tn / 2)))
     return rc;
-  m.a[1] = m.out = m.a[0];
+  m.a[1] = m.a[0];
   m.b[1] = m.b[0];
+  if ((rc = finish_maps(&p.f, s.T, &m))) return rc;
   const long long jobs = (long long)p.mt * p.nt * p.ks;
   rc = w.tn == 256 ? launch_tiles<FwdOp, 256>(m, p, jobs, w.nx, w.nw, "k_linear", chained, st)
                    : launch_tiles<FwdOp, 128>(m, p, jobs, w.nx, w.nw, "k_linear", chained, st);

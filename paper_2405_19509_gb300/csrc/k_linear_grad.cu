@@ -45,8 +45,7 @@ __global__ void __launch_bounds__(256)
     if (act != GC_ACT_NONE) {
       float u[8];
       load_seg<VEC>(z + row * ldz, col0, lane, F, u);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= slope(act, u[j]);
+      times_slope(act, u, v);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -55,9 +54,9 @@ __global__ void __launch_bounds__(256)
     }
     uint32_t far = 0;
     for (int q = 0; q < np; ++q) {
-      float h[8];
-      next_part(v, far, h);
-      store_seg<VEC>(d + ((size_t)q * T_all + row) * Fp, col0, lane, Fp, h);
+      uint32_t w[4];
+      next_part(v, far, w);
+      store_part<VEC>(d + ((size_t)q * T_all + row) * Fp, col0, lane, Fp, w);
     }
   }
   if (!sums) return;
@@ -151,17 +150,18 @@ struct GradOp {
     t.seg = p.seg_g;
     return t;
   }
-  template <int NC, int U, typename Get>
+  template <int NC, typename Get>
   static __device__ __forceinline__ void store(const Params& p, const Job& t, int row0, int col0, uint8_t* box,
                                                const CUtensorMap* out, Get get) {
+    const int lane = threadIdx.x & 31;
     if (t.kind == 0) {
-      store_rows<NC, U>(p.f, p.T, p.ks > 1 ? p.part + (size_t)t.range * p.T * p.ld_part : nullptr, p.ld_part, row0, col0,
-                        box, get);
+      store_rows<NC>(p.f, p.T, p.ks > 1 ? p.part + (size_t)t.range * p.T * p.ld_part : nullptr, p.ld_part, row0, col0, box, out,
+                     get);
+      box_free<0>(lane);  // a tile of G uses the box next
       return;
     }
-    const int lane = threadIdx.x & 31;
     const int rows = min(p.F - row0, 32);
-#pragma unroll(U)
+#pragma unroll 1
     for (int c = 0; c < NC; ++c) {
       float v[32];
       __syncwarp();
@@ -169,26 +169,21 @@ struct GradOp {
       const int col = col0 + c * 32;
       if (rows <= 0 || col >= p.C) continue;
       if (p.g_box) {
-        if (lane == 0) bulk_wait_read<0>();  // the box's last store has read it
-        __syncwarp();
+        box_free<0>(lane);
         box_put(box, lane, v);
-        fence_async_smem();
-        __syncwarp();
+        box_full();
         if (lane == 0) {
-          store_3d(out, box, col, row0, t.b);
+          store_3d(&out[1], box, col, row0, t.b);
           bulk_commit();
         }
       } else {
         box_put(box, lane, v);
         __syncwarp();
         float* g = p.G + t.b * p.ldg + (long long)row0 * p.C + col + lane;
-        by_rows<8>(box, lane, col + lane < p.C ? rows : 0, [&](int r, float s) { g[(long long)r * p.C] = s; });
+        by_rows<4>(box, lane, col + lane < p.C ? rows : 0, [&](int r, float s) { g[(long long)r * p.C] = s; });
       }
     }
-    if (p.g_box) {  // a dx tile may use the box next
-      if (lane == 0) bulk_wait_read<0>();
-      __syncwarp();
-    }
+    if (p.g_box) box_free<0>(lane);  // a tile of dx may use the box next
   }
 };
 
@@ -229,10 +224,10 @@ Scratch carve_grad(Carve& c, const LinearGradShape& s) {
   for (int tn = 256; tn >= 128; tn /= 2) {
     const double nd = dx ? (double)tiles_of(T, TM) * tiles_of(s.C, tn) : 0;
     const double ng = g ? (double)s.N * tiles_of(s.F, TM) * tiles_of(s.C, tn) : 0;
-    const double one_g = ng > 0 ? c_nkb * p_g * 2.0 * tn + 600 : 0;
+    const double one_g = ng > 0 ? c_nkb * block_clocks(tn, p_g) + 600 : 0;
     for (int ks = 1; ks <= (dx ? 32 : 1) && ks * 2 <= std::max(2, f_nkb); ++ks) {
       if (ks > 1 && nd * (ks - 1) >= 2 * units) break;
-      const double one_d = nd > 0 ? (f_nkb + ks - 1) / ks * p_dx * 2.0 * tn + 600 : 0;
+      const double one_d = nd > 0 ? (f_nkb + ks - 1) / ks * block_clocks(tn, p_dx) + 600 : 0;
       const double longest = std::max(one_d, one_g), share = (nd * ks * one_d + ng * one_g) / units;
       double clk = std::max(longest, share + (nd * ks + ng > units ? std::min(longest, ng > 0 ? one_g : one_d) / 2 : 0));
       if (ks > 1) clk += 5000 + (double)T * s.C * 8 * ks / 3500;
@@ -298,7 +293,7 @@ int launch_linear_grad(const LinearGradShape& s, const LinearGradIO& io, Carve& 
   GradOp::Params p{};
   const int e = xb ? 2 : 4;
   p.f = Finish{s.C, GC_ACT_NONE, xb, nullptr, nullptr, io.dX, nullptr, 0, (long long)io.lddx, 0,
-               reinterpret_cast<uintptr_t>(io.dX) % (4 * e) == 0 && io.lddx % 4 == 0};
+               reinterpret_cast<uintptr_t>(io.dX) % (4 * e) == 0 && io.lddx % 4 == 0, 0};
   p.T = T;
   p.C = s.C;
   p.F = s.F;
@@ -339,14 +334,17 @@ int launch_linear_grad(const LinearGradShape& s, const LinearGradIO& io, Carve& 
   if ((rc = operand_map(&m.a[0], D, false, s.F, T, 1, w.np, ldd, T * ldd, T * ldd, p.q.a_rows)) ||
       (rc = operand_map(&m.a[1], D, false, s.F, s.n_c, s.N, w.np, ldd, s.n_c * ldd, T * ldd, BK)))
     return rc;
-  m.b[0] = m.b[1] = m.out = m.a[0];
+  m.b[0] = m.b[1] = m.a[0];
+  if (dx) rc = finish_maps(&p.f, T, &m);
+  else m.out[0] = m.out[1] = m.a[0];
+  if (rc) return rc;
   if (dx && (rc = operand_map(&m.b[0], W, false, s.C, s.F, 1, w.nw, ldw, s.F * ldw, s.F * ldw, BK))) return rc;
   if (g) {
     if ((rc = operand_map(&m.b[1], X, false, s.C, s.n_c, s.N, w.nx, ldx, s.n_c * ldx, T * ldx, BK))) return rc;
     p.g_box = s.C % 4 == 0 && rows_16(io.G, io.ldg, 4);
     if (p.g_box) {
       const long long dg[3] = {s.C, s.F, s.N}, lg[2] = {s.C, io.ldg};
-      if ((rc = map_nd(&m.out, io.G, 3, dg, lg, 32, 1, MAP_F32))) return rc;
+      if ((rc = map_nd(&m.out[1], io.G, 3, dg, lg, 32, 1, MAP_F32))) return rc;
     }
   }
   const long long jobs = (long long)p.ndx + p.ng;

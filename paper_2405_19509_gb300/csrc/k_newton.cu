@@ -43,40 +43,19 @@ struct Parts {
 
 enum { NS_A, NS_P, NS_X, NS_OUT, NS_STEP };
 struct Epilogue {
-  int kind, rows, cols;
+  int kind, rows, cols, batch;
   float s;             // scale of a sum
   Parts out;
-  int np;              // parts of `out`
+  int np;              // parts of `out`, whose rows may be written past their ends up to 16 bytes
   Parts A;             // NS_P: a I + b A + s sum
   int na;
   float a, b;
   void* w;             // NS_OUT, NS_STEP: rows of results
   long long ldw, sw;
-  int bf16, vec;       // vec: rows in groups of four
+  int bf16, box;       // box: rows are whole 16-byte pieces
   float keep;          // NS_STEP: w = keep w + s sum
   const float* lam;    // [batch]: X is lam times what its parts hold
 
-  static __device__ __forceinline__ void get4(const __half* p, float (&v)[4]) {
-    const uint2 q = *reinterpret_cast<const uint2*>(p);
-    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&q.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&q.y));
-    v[0] += a.x;
-    v[1] += a.y;
-    v[2] += b.x;
-    v[3] += b.y;
-  }
-  // Four neighbours as parts; rows of `out` end past a multiple of eight, so whole fours are stored.
-  __device__ __forceinline__ void put_parts(int mat, long long r, int c, float (&v)[4]) const {
-    __half* to = out.p + mat * out.mat + r * out.ld + c;
-    for (int q = 0; q < np; ++q, to += out.plane) {
-      const __half2 a = __floats2half2_rn(v[0], v[1]), b = __floats2half2_rn(v[2], v[3]);
-      *reinterpret_cast<uint2*>(to) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-      const float2 x = __half22float2(a), y = __half22float2(b);
-      v[0] -= x.x;
-      v[1] -= x.y;
-      v[2] -= y.x;
-      v[3] -= y.y;
-    }
-  }
   __device__ __forceinline__ void one(int mat, float l, long long r, int c, float x) const {
     x *= l;
     if (bf16) {
@@ -86,63 +65,103 @@ struct Epilogue {
       *to = kind == NS_STEP ? fmaf(s, x, keep * *to) : s * x;
     }
   }
-  __device__ __forceinline__ void four(int mat, float l, long long r, int c, float4 x) const {
-    x = make_float4(l * x.x, l * x.y, l * x.z, l * x.w);
-    if (bf16) {
-      const __nv_bfloat162 a = __floats2bfloat162_rn(s * x.x, s * x.y), b = __floats2bfloat162_rn(s * x.z, s * x.w);
-      *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(w) + mat * sw + r * ldw + c) =
-          make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  // 32 x 32 sums at (row0, col0), a lane a row, to w.
+  __device__ __forceinline__ void finish_w(float (&v)[32], uint8_t* buf, const CUtensorMap* map, int mat, int row0, int col0,
+                                           int m, int n) const {
+    const int lane = threadIdx.x & 31;
+    const float l = lam[mat];
+    if (!box) {
+      box_put(buf, lane, v);
+      __syncwarp();
+      by_rows<1>(buf, lane, lane < n ? m : 0, [&](int r, float x) { one(mat, l, row0 + r, col0 + lane, x); });
       return;
     }
-    float4* to = reinterpret_cast<float4*>(reinterpret_cast<float*>(w) + mat * sw + r * ldw + c);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = s * (l * v[j]);
     if (kind == NS_STEP) {
-      const float4 o = *to;
-      *to = make_float4(fmaf(s, x.x, keep * o.x), fmaf(s, x.y, keep * o.y), fmaf(s, x.z, keep * o.z), fmaf(s, x.w, keep * o.w));
+      Rows32<8> old;
+      old.load(reinterpret_cast<const float*>(w) + mat * sw + (long long)row0 * ldw + col0, ldw * 4, m, n * 4, lane);
+      box_free<0>(lane);
+      old.turn(buf, lane);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[4 * j] = fmaf(keep, __uint_as_float(old.q[j].x), v[4 * j]);
+        v[4 * j + 1] = fmaf(keep, __uint_as_float(old.q[j].y), v[4 * j + 1]);
+        v[4 * j + 2] = fmaf(keep, __uint_as_float(old.q[j].z), v[4 * j + 2]);
+        v[4 * j + 3] = fmaf(keep, __uint_as_float(old.q[j].w), v[4 * j + 3]);
+      }
     } else {
-      *to = make_float4(s * x.x, s * x.y, s * x.z, s * x.w);
+      box_free<0>(lane);
+    }
+    if (bf16)
+      box_put_16(buf, lane, [&](int j) { return pack_bf16(v[j], v[j + 1]); });
+    else
+      box_put(buf, lane, v);
+    box_full();
+    if (lane == 0) {
+      store_3d(map, buf, col0, row0, mat);
+      bulk_commit();
     }
   }
-  // A box of 32 x 32 sums at (row0, col0); mirror: also at (col0, row0).
-  __device__ __forceinline__ void finish(uint8_t* box, int lane, int mat, int row0, int col0, bool mirror) const {
+  // ... or as parts; mirror: also at (col0, row0).
+  __device__ __forceinline__ void finish_parts(float (&v)[32], uint8_t* buf, const CUtensorMap* map, int mat, int row0, int col0,
+                                               int m, int n, bool mirror) const {
+    const int lane = threadIdx.x & 31;
+    box_free<0>(lane);
+    if (kind == NS_P) {
+      const float l2 = lam[mat] * lam[mat], sum = s * l2 * l2, b2 = b * l2;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = fmaf(sum, v[j], row0 + lane == col0 + j ? a : 0.f);
+      for (int q = 0; q < na; ++q) {
+        Rows32<4> part;  // rows of A end past a multiple of eight
+        part.load(A.p + q * A.plane + mat * A.mat + (long long)row0 * A.ld + col0, A.ld * 2LL, m, (n + 7) / 8 * 16, lane);
+        part.turn(buf, lane);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w4[4] = {part.q[j].x, part.q[j].y, part.q[j].z, part.q[j].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w4[e]));
+            v[8 * j + 2 * e] = fmaf(b2, t.x, v[8 * j + 2 * e]);
+            v[8 * j + 2 * e + 1] = fmaf(b2, t.y, v[8 * j + 2 * e + 1]);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] *= s;
+    }
+    for (int q = 0; q < np; ++q) {
+      uint32_t h[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const __half2 t = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+        const float2 f = __half22float2(t);
+        h[j] = *reinterpret_cast<const uint32_t*>(&t);
+        v[2 * j] -= f.x;
+        v[2 * j + 1] -= f.y;
+      }
+      box_put_16(buf + q * HALF_BOX, lane, [&](int j) { return h[j / 2]; });
+      box_full();
+      if (lane == 0) {
+        store_3d(map, buf + q * HALF_BOX, col0, row0, q * batch + mat);
+        bulk_commit();
+      }
+      if (mirror && lane < m) {
+        uint16_t* to = reinterpret_cast<uint16_t*>(out.p + q * out.plane + mat * out.mat + (long long)col0 * out.ld + row0 + lane);
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j < n) to[(long long)j * out.ld] = (uint16_t)(h[j / 2] >> (16 * (j & 1)));
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(float (&v)[32], uint8_t* buf, const CUtensorMap* map, int mat, int row0, int col0,
+                                         bool mirror) const {
     const int m = min(rows - row0, 32), n = cols - col0;
-    const float l = lam[mat], l2 = l * l;
-    if (kind >= NS_OUT) {
-      if (vec && n >= 32) {
-        by_fours(box, lane, [&](int r, int c, float4 x) {
-          if (r < m) four(mat, l, row0 + r, col0 + c, x);
-        });
-      } else {
-        by_rows<4>(box, lane, lane < n ? m : 0, [&](int r, float x) { one(mat, l, row0 + r, col0 + lane, x); });
-      }
-      return;
-    }
-    const float sum = kind == NS_P ? s * l2 * l2 : s;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = i * 4 + (lane >> 3), c = (lane & 7) * 4;
-      float4* at = reinterpret_cast<float4*>(box + r * 128 + (((lane & 7) ^ (r & 7)) * 16));
-      const float4 x = *at;
-      float v[4] = {sum * x.x, sum * x.y, sum * x.z, sum * x.w};
-      if (r >= m || c >= n) continue;
-      if (kind == NS_P) {
-        float h[4] = {0.f, 0.f, 0.f, 0.f};
-        const __half* from = A.p + mat * A.mat + (long long)(row0 + r) * A.ld + col0 + c;
-        for (int q = 0; q < na; ++q, from += A.plane) get4(from, h);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(b * l2, h[e], v[e]) + (row0 + r == col0 + c + e ? a : 0.f);
-      }
-      if (mirror) *at = make_float4(v[0], v[1], v[2], v[3]);
-      put_parts(mat, row0 + r, col0 + c, v);
-    }
-    if (!mirror) return;
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = i * 4 + (lane >> 3), r = (lane & 7) * 4;
-      if (c >= n || r >= m) continue;
-      float v[4] = {box_at(box, r, c), box_at(box, r + 1, c), box_at(box, r + 2, c), box_at(box, r + 3, c)};
-      put_parts(mat, col0 + c, row0 + r, v);
-    }
+    if (kind >= NS_OUT)
+      finish_w(v, buf, map, mat, row0, col0, m, n);
+    else
+      finish_parts(v, buf, map, mat, row0, col0, m, n, mirror);
   }
 };
 
@@ -193,69 +212,71 @@ struct NsOp {
     t.b_mn = p.b_mn;
     return t;
   }
-  template <int NC, int U, typename Get>
+  template <int NC, typename Get>
   static __device__ __forceinline__ void store(const Params& p, const Job& t, int row0, int col0, uint8_t* box,
-                                               const CUtensorMap*, Get get) {
+                                               const CUtensorMap* out, Get get) {
     const int lane = threadIdx.x & 31;
     const int rows = p.e.rows - row0;
     const bool mirror = p.sym && t.n0 + p.tn <= t.m0;
-#pragma unroll(U)
+#pragma unroll 1
     for (int c = 0; c < NC; ++c) {
       float v[32];
       __syncwarp();
       get(c, v);
       const int col = col0 + c * 32;
       if (rows <= 0 || col >= p.e.cols) continue;
-      box_put(box, lane, v);
-      __syncwarp();
       if (p.ks > 1) {
+        box_put(box, lane, v);
+        __syncwarp();
         float* to = p.part + (((size_t)t.range * p.batch + t.b) * p.e.rows + row0) * p.ld_part + col;
         by_fours(box, lane, [&](int r, int j, float4 s) {
           if (r < rows && col + j < p.e.cols) *reinterpret_cast<float4*>(to + (size_t)r * p.ld_part + j) = s;
         });
       } else {
-        p.e.finish(box, lane, t.b, row0, col, mirror);
+        p.e.finish(v, box, out, t.b, row0, col, mirror);
       }
     }
   }
 };
 
 // A warp a block of 32 x 32: the ranges' sums in their order, and the epilogue.
-__global__ void __launch_bounds__(128) k_ns_join(const float* __restrict__ part, int ks, int batch, int ld, int sym, int tn,
-                                                 const Epilogue e) {
-  __shared__ __align__(128) uint8_t boxes[4 * BOX];
+__global__ void __launch_bounds__(128) k_ns_join(const __grid_constant__ CUtensorMap out, const float* __restrict__ part,
+                                                 int ks, int ld, int sym, int tn, const __grid_constant__ Epilogue e) {
+  __shared__ __align__(1024) uint8_t boxes[4 * BOX];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint8_t* box = boxes + warp * BOX;
   start_next();
   wait_prior();
   const int br = (e.rows + 31) / 32, bc = (e.cols + 31) / 32;
   const long long i = (long long)blockIdx.x * 4 + warp;
-  if (i >= (long long)batch * br * bc) return;
+  if (i >= (long long)e.batch * br * bc) return;
   const int mat = (int)(i / (br * bc)), at = (int)(i - (long long)mat * br * bc);
   const int row0 = at / bc * 32, col0 = at % bc * 32;
   const int m0 = row0 / TM * TM, n0 = col0 / tn * tn;
   if (sym && n0 >= m0 + TM) return;
-  const size_t range = (size_t)batch * e.rows * ld;
-  const float* from = part + ((size_t)mat * e.rows + row0) * ld + col0;
+  const size_t range = (size_t)e.batch * e.rows * ld;
+  const float* from = part + ((size_t)mat * e.rows + row0 + lane) * ld + col0;
+  float v[32];
 #pragma unroll
-  for (int g = 0; g < 8; ++g) {
-    const int r = g * 4 + (lane >> 3), j = lane & 7;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row0 + r < e.rows && col0 + 4 * j < e.cols) {
-      const float* p = from + (size_t)r * ld + 4 * j;
-      s = __ldcg(reinterpret_cast<const float4*>(p));
+  for (int j = 0; j < 32; j += 4) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row0 + lane < e.rows && col0 + j < e.cols) {
+      x = __ldcg(reinterpret_cast<const float4*>(from + j));
       for (int k = 1; k < ks; ++k) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(p + k * range));
-        s.x += v.x;
-        s.y += v.y;
-        s.z += v.z;
-        s.w += v.w;
+        const float4 y = __ldcg(reinterpret_cast<const float4*>(from + j + k * range));
+        x.x += y.x;
+        x.y += y.y;
+        x.z += y.z;
+        x.w += y.w;
       }
     }
-    *reinterpret_cast<float4*>(box + r * 128 + ((j ^ (r & 7)) * 16)) = s;
+    v[j] = x.x;
+    v[j + 1] = x.y;
+    v[j + 2] = x.z;
+    v[j + 3] = x.w;
   }
-  __syncwarp();
-  e.finish(box, lane, mat, row0, col0, sym && n0 + tn <= m0);
+  e.finish(v, box, &out, mat, row0, col0, sym && n0 + tn <= m0);
+  if (lane == 0) bulk_wait_all();
 }
 
 // What u is: the matrix itself, or the momentum of a gradient (and, looking ahead, the gradient once more).
@@ -497,14 +518,19 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
   };
   if ((rc = map(&m.a[0], A, g.na, g.a_mn, g.rows, p.q.a_rows)) || (rc = map(&m.b[0], B, g.nb, g.b_mn, g.cols, cut.tn / 2)))
     return rc;
-  m.a[1] = m.out = m.a[0];
+  m.a[1] = m.out[0] = m.out[1] = m.a[0];
   m.b[1] = m.b[0];
+  if (e.kind < NS_OUT)
+    rc = box_map(&m.out[0], e.out.p, MAP_F16, g.cols, g.rows, (long long)e.np * s.batch, e.out.ld, e.out.mat);
+  else if (e.box)
+    rc = box_map(&m.out[0], e.w, e.bf16 ? MAP_BF16 : MAP_F32, g.cols, g.rows, s.batch, e.ldw, e.sw);
+  if (rc) return rc;
   const long long jobs = (long long)s.batch * p.per * p.ks;
   rc = cut.tn == 256 ? launch_tiles<NsOp, 256>(m, p, jobs, g.na, g.nb, name, true, st)
                      : launch_tiles<NsOp, 128>(m, p, jobs, g.na, g.nb, name, true, st);
   if (rc || p.ks == 1) return rc;
   const long long blocks = (long long)s.batch * ((g.rows + 31) / 32) * ((g.cols + 31) / 32);
-  return launch_chain(k_ns_join, "k_ns_join", (unsigned)((blocks + 3) / 4), 128, 0, 1, true, st, (const float*)part, p.ks, s.batch,
+  return launch_chain(k_ns_join, "k_ns_join", (unsigned)((blocks + 3) / 4), 128, 0, 1, true, st, m.out[0], (const float*)part, p.ks,
                       p.ld_part, g.sym, cut.tn, e);
 }
 
@@ -578,6 +604,7 @@ int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cud
     Epilogue ea{};
     ea.kind = NS_A;
     ea.rows = ea.cols = w.m;
+    ea.batch = s.batch;
     ea.s = kSA / (kSX * kSX);
     ea.out = w.A;
     ea.np = w.aa;
@@ -598,6 +625,7 @@ int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cud
     ex.lam = w.lam;
     ex.rows = s.rows;
     ex.cols = s.cols;
+    ex.batch = s.batch;
     if (i + 1 < s.steps) {
       ex.kind = NS_X;
       ex.s = 1.f / kSP;
@@ -611,8 +639,10 @@ int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cud
       ex.ldw = io.ldo;
       ex.sw = io.so;
       ex.bf16 = bf;
-      ex.vec = reinterpret_cast<uintptr_t>(io.out) % (4 * e) == 0 && io.ldo % 4 == 0 &&
-               (s.batch == 1 || io.so % 4 == 0);
+      // one row, or one matrix, needs no stride, but a map has one
+      if (s.rows == 1) ex.ldw = (s.cols + 7) / 8 * 8;
+      if (s.batch == 1) ex.sw = s.rows * ex.ldw;
+      ex.box = s.cols * e % 16 == 0 && rows_16(io.out, ex.ldw, e) && ex.sw * e % 16 == 0;
     }
     if ((rc = launch_product(s, w.px, w.cx, w.wide ? w.P : X, w.wide ? X : w.P, ex, bf, w.part, status, false, "k_ns_x", st)))
       return rc;

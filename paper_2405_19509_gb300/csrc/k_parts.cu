@@ -25,9 +25,9 @@ __global__ void __launch_bounds__(256) k_parts(const T* __restrict__ x, long lon
     load_seg<VEC>(x + row * ld, col0, lane, C, v);
     uint32_t far = 0;
     for (int q = 0; q < parts; ++q) {
-      float h[8];
-      linear::next_part(v, far, h);
-      store_seg<VEC>(out + ((size_t)q * rows + row) * Cp, col0, lane, Cp, h);
+      uint32_t w[4];
+      linear::next_part(v, far, w);
+      linear::store_part<VEC>(out + ((size_t)q * rows + row) * Cp, col0, lane, Cp, w);
     }
   }
 }

@@ -17,6 +17,7 @@ struct Finish {
   void *y, *z;
   long long ldr, ldy, ldz;
   int vec;  // rows of y, z and residual in groups of four
+  int box;  // ... and whole 16-byte pieces
 
   template <typename T>
   __device__ __forceinline__ void one(long long row, int c, float v) const {
@@ -73,38 +74,119 @@ struct Finish {
   }
 };
 
+__device__ __forceinline__ void activate32(int act, float (&v)[32]) {
+  switch (act) {  // outside the loop: one activation's code at a time
+#define GC_ALL(A)                                                  \
+  case A:                                                          \
+    _Pragma("unroll") for (int j = 0; j < 32; ++j) v[j] = linear::activate(A, v[j]); \
+    break;
+    GC_ALL(GC_ACT_RELU)
+    GC_ALL(GC_ACT_GELU)
+    GC_ALL(GC_ACT_GELU_TANH)
+    GC_ALL(GC_ACT_SILU)
+#undef GC_ALL
+  }
+}
+
+// 32 x 32 sums, a lane a row, through the epilogue and out by way of the box.  Rows of y, z and residual are whole 16-byte
+// pieces; what is past their ends is not stored.  first: nothing of this tile has left yet.  Values of 16 bits use the
+// halves of the box in turn (z and y, or y of every other block), so that a store is waited for one later.
+template <typename T, typename Get>
+__device__ __forceinline__ void store_box(const Finish& f, int rows, int row0, int col, int c, uint8_t* box,
+                                          const CUtensorMap* out, Get get) {
+  const int lane = threadIdx.x & 31;
+  const int n = f.F - col;
+  constexpr int N = sizeof(T) == 2 ? 4 : 8;
+  const float own = f.bias && lane < n ? __ldg(f.bias + col + lane) : 0.f;
+  Rows32<N> res;
+  if (f.res)
+    res.load(reinterpret_cast<const T*>(f.res) + (long long)row0 * f.ldr + col, f.ldr * (long long)sizeof(T), rows,
+             n * (int)sizeof(T), lane);
+  float v[32];
+  get(c, v);
+  if (f.bias) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, own, j);
+  }
+  auto put = [&](uint8_t* to) {
+    if (sizeof(T) == 2)
+      box_put_16(to, lane, [&](int j) { return pack_bf16(v[j], v[j + 1]); });
+    else
+      box_put(to, lane, v);
+  };
+  auto store = [&](const CUtensorMap* map, const uint8_t* from) {
+    box_full();
+    if (lane == 0) {
+      store_3d(map, from, col, row0, 0);
+      bulk_commit();
+    }
+  };
+  auto free = [&] {
+    if (sizeof(T) == 4 || c == 0)
+      box_free<0>(lane);
+    else
+      box_free<1>(lane);
+  };
+  if (f.z) {
+    free();
+    put(box);
+    store(&out[1], box);
+  }
+  activate32(f.act, v);
+  uint8_t* to = box + (sizeof(T) == 2 && (f.z || c % 2) ? HALF_BOX : 0);
+  if (!(f.z && sizeof(T) == 2 && c == 0)) free();  // the first tile's second half: the first wait was for it too
+  if (f.res) {
+    res.turn(to, lane);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const uint32_t w[4] = {res.q[j].x, res.q[j].y, res.q[j].z, res.q[j].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (sizeof(T) == 2) {
+          v[8 * j + 2 * e] += __uint_as_float(w[e] << 16);
+          v[8 * j + 2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
+        } else {
+          v[(4 * j + e) % 32] += __uint_as_float(w[e]);
+        }
+      }
+    }
+  }
+  put(to);
+  store(&out[0], to);
+}
+
 // A warp's part of a tile: rows row0 .. of T, columns col0 ..; to `part` (rows of fp32 sums, ld apart) where the sum
 // is one of several ranges, else through the epilogue.
-template <int NC, int U, typename Get>
+template <int NC, typename Get>
 __device__ __forceinline__ void store_rows(const Finish& f, long long T, float* part, int ld_part, int row0, int col0,
-                                           uint8_t* box, Get get) {
+                                           uint8_t* box, const CUtensorMap* out, Get get) {
   const int lane = threadIdx.x & 31;
   const int rows = (int)min(T - row0, 32LL);
-#pragma unroll(U)
+#pragma unroll 1
   for (int c = 0; c < NC; ++c) {
-    float v[32];
-    __syncwarp();
-    get(c, v);
     const int col = col0 + c * 32;
-    if (rows <= 0 || col >= f.F) continue;
-    box_put(box, lane, v);
     __syncwarp();
+    if (f.box && !part && rows > 0 && col < f.F) {
+      if (f.bf16)
+        store_box<__nv_bfloat16>(f, rows, row0, col, c, box, out, get);
+      else
+        store_box<float>(f, rows, row0, col, c, box, out, get);
+      continue;
+    }
+    float v[32];
+    get(c, v);
+    if (rows <= 0 || col >= f.F) continue;
     if (part) {
+      box_put(box, lane, v);
+      __syncwarp();
       float* to = part + (size_t)row0 * ld_part + col;
       by_fours(box, lane, [&](int r, int j, float4 s) {
         if (r < rows && col + j < f.F) *reinterpret_cast<float4*>(to + (size_t)r * ld_part + j) = s;
       });
-    } else if (f.vec) {
-      const float4 b = f.bias_of(col + (lane & 7) * 4);
-      by_fours(box, lane, [&](int r, int j, float4 s) {
-        if (r >= rows || col + j >= f.F) return;
-        if (f.bf16)
-          f.four<__nv_bfloat16>(row0 + r, col + j, s, b);
-        else
-          f.four<float>(row0 + r, col + j, s, b);
-      });
     } else {
-      by_rows<4>(box, lane, col + lane < f.F ? rows : 0, [&](int r, float s) {
+      box_put(box, lane, v);
+      __syncwarp();
+      by_rows<1>(box, lane, col + lane < f.F ? rows : 0, [&](int r, float s) {
         if (f.bf16)
           f.one<__nv_bfloat16>(row0 + r, col + lane, s);
         else
@@ -112,6 +194,18 @@ __device__ __forceinline__ void store_rows(const Finish& f, long long T, float* 
       });
     }
   }
+}
+
+// Maps of y and z, where their rows and the residual's are whole 16-byte pieces: a store by TMA writes no less.
+inline int finish_maps(Finish* f, long long T, Maps* m) {
+  const int e = f->bf16 ? 2 : 4;
+  f->box = f->F * e % 16 == 0 && rowwise::rows_16(f->y, f->ldy, e) && rowwise::rows_16(f->z, f->ldz, e) && rowwise::rows_16(f->res, f->ldr, e);
+  m->out[0] = m->out[1] = m->a[0];
+  if (!f->box) return GC_OK;
+  const MapType t = f->bf16 ? MAP_BF16 : MAP_F32;
+  int rc = box_map(&m->out[0], f->y, t, f->F, T, 1, f->ldy, T * f->ldy);
+  if (!rc && f->z) rc = box_map(&m->out[1], f->z, t, f->F, T, 1, f->ldz, T * f->ldz);
+  return rc;
 }
 
 // Four columns a thread: the ranges' sums in their order, and the epilogue.

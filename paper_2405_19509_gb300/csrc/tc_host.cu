@@ -20,12 +20,12 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
 }  // namespace
 
 int map_nd(CUtensorMap* map, const void* base, int rank, const long long* dims, const long long* ld, int box_rows,
-           int box_planes, MapType type) {
+           int box_planes, MapType type, bool narrow) {
   auto fn = encode_fn();
   if (!fn) return fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled entry point unavailable");
   const bool f32 = type == MAP_F32;
   cuuint64_t d[4], st[3];
-  cuuint32_t box[4] = {f32 ? 32u : 64u, (cuuint32_t)box_rows, (cuuint32_t)box_planes, 1}, one[4] = {1, 1, 1, 1};
+  cuuint32_t box[4] = {(f32 ? 32u : 64u) >> narrow, (cuuint32_t)box_rows, (cuuint32_t)box_planes, 1}, one[4] = {1, 1, 1, 1};
   for (int i = 0; i < rank; ++i) d[i] = (cuuint64_t)dims[i];
   for (int i = 0; i + 1 < rank; ++i) st[i] = (cuuint64_t)ld[i] * (f32 ? 4 : 2);
   const CUresult r = fn(map,
@@ -33,7 +33,7 @@ int map_nd(CUtensorMap* map, const void* base, int rank, const long long* dims, 
                         : type == MAP_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                           : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
                         (cuuint32_t)rank, const_cast<void*>(base), d, st, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        narrow ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? GC_OK : fail(GC_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }

@@ -10,9 +10,9 @@ namespace gc {
 enum MapType { MAP_BF16, MAP_F16, MAP_F32 };
 
 // Map of `rank` dimensions (up to 4), innermost first; ld[i]: elements between neighbours of dimension i + 1.  Box 128
-// bytes x box_rows x box_planes, 128-byte swizzle.
+// bytes x box_rows x box_planes, 128-byte swizzle; narrow: 64 bytes, 64-byte swizzle.
 int map_nd(CUtensorMap* map, const void* base, int rank, const long long* dims, const long long* ld, int box_rows,
-           int box_planes = 1, MapType type = MAP_BF16);
+           int box_planes = 1, MapType type = MAP_BF16, bool narrow = false);
 
 // A launch with clusters of `cl` CTAs (1: none); `chained`: as a dependent of the call's kernel before it.
 template <typename... P, typename... A>

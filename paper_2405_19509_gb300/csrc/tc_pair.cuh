@@ -109,6 +109,18 @@ __device__ __forceinline__ void tmem_add16(uint32_t taddr, float* sum) {
 #pragma unroll
   for (int j = 0; j < 16; ++j) sum[j] += __uint_as_float(r[j]);
 }
+// 16 consecutive columns of the warp's 32 lanes, to be waited for with tcgen05.wait::st (warp-collective).
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
+  uint32_t r[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(v[j]);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 "
+      "[%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
 // 64 consecutive columns of the warp's 32 lanes, both loads in flight at once (warp-collective).
 __device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&v)[64]) {
   uint32_t r[64];

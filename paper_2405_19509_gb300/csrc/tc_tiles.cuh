@@ -11,7 +11,7 @@
 // Sums: an addition in tensor memory is cut off, not rounded, about 2e-8 of the sum a step and always towards zero, so
 // 32-bit results leave it every `seg` K blocks and are added in registers.
 //
-// Bound: the tensor pipe (4 x 128 clocks a K block of one product at TN = 256) where tiles are many, else the
+// Bound: the tensor pipe (4 x 128 clocks a K block of one product at TN = 256; TN = 128 spreads few tiles) where tiles are many, else the
 // latency of a tile: barriers, the first loads and the epilogue, some 3 us.  Every wait is bounded (GC_ERR_TIMEOUT).
 #pragma once
 
@@ -57,7 +57,7 @@ struct Common {
 
 // Tensor maps of (inner, rows, batch, part) by kind, and the epilogue's.
 struct Maps {
-  CUtensorMap a[2], b[2], out;
+  CUtensorMap a[2], b[2], out[2];
 };
 
 __device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -90,10 +90,60 @@ __device__ __forceinline__ void by_fours(const uint8_t* box, int lane, F f) {
     f(r, 4 * j, *reinterpret_cast<const float4*>(box + r * 128 + ((j ^ (r & 7)) * 16)));
   }
 }
+// Boxes that leave by TMA.  32 x 32 values of 16 bits take half a box, rows of 64 bytes: piece j of row r at j ^ (r / 2 mod 4).
+constexpr int HALF_BOX = BOX / 2;
+template <typename Pack>
+__device__ __forceinline__ void box_put_16(uint8_t* half, int lane, Pack two) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *reinterpret_cast<uint4*>(half + lane * 64 + ((j ^ ((lane >> 1) & 3)) * 16)) =
+        make_uint4(two(8 * j), two(8 * j + 2), two(8 * j + 4), two(8 * j + 6));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+// Before a box is written: the stores that lane 0 issued from it, all but the newest N of the warp's, have read it.
+template <int N>
+__device__ __forceinline__ void box_free(int lane) {
+  if (lane == 0) bulk_wait_read<N>();
+  __syncwarp();
+}
+// After: what the warp wrote is seen by the store that lane 0 issues next.
+__device__ __forceinline__ void box_full() {
+  fence_async_smem();
+  __syncwarp();
+}
+// 32 rows of 4 N 32-bit words (N = 4: 64 bytes, N = 8: 128) from memory, neighbouring lanes a row; they reach a lane a row by
+// way of the box, in whose order of pieces they are put there.
+template <int N>
+struct Rows32 {
+  uint4 q[N];
+  static __device__ __forceinline__ int place(int r, int j) { return r * N * 16 + (N == 8 ? j ^ (r & 7) : j ^ ((r >> 1) & 3)) * 16; }
+  // the first `rows` rows, `ld` bytes apart, of which `bytes` exist, a multiple of 16
+  __device__ __forceinline__ void load(const void* from, long long ld, int rows, int bytes, int lane) {
+    const int j = lane % N;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = i * (32 / N) + lane / N;
+      q[i] = r < rows && j * 16 < bytes ? *reinterpret_cast<const uint4*>(static_cast<const char*>(from) + r * ld + j * 16)
+                                        : make_uint4(0, 0, 0, 0);
+    }
+  }
+  // ... as the lane's own row.  The box is free before; the lane may write its own row after.
+  __device__ __forceinline__ void turn(uint8_t* box, int lane) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(box + place(i * (32 / N) + lane / N, lane % N)) = q[i];
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < N; ++j) q[j] = *reinterpret_cast<const uint4*>(box + place(lane, j));
+    __syncwarp();
+  }
+};
 // f(r, value): rows r = 0 .. rows - 1, a lane a column, for rows on no boundary.
 template <int U, typename F>
 __device__ __forceinline__ void by_rows(const uint8_t* box, int lane, int rows, F f) {
-#pragma unroll U
+#pragma unroll(U)
   for (int r = 0; r < 32; ++r) {
     const float x = box_at(box, r, lane);
     if (r < rows) f(r, x);
@@ -101,7 +151,8 @@ __device__ __forceinline__ void by_rows(const uint8_t* box, int lane, int rows, 
 }
 
 template <class Op, int TN>
-__global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ Maps maps, const typename Op::Params p) {
+__global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ Maps maps,
+                                                        const __grid_constant__ typename Op::Params p) {
   constexpr int HN = TN / 2;             // columns of an epilogue warp, and B rows of a CTA
   constexpr int B_BYTES = HN * BK * 2;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -283,28 +334,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
       const Job t = Op::job(p, unit, k);
       const int row0 = t.m0 + side * 128 + quarter * 32, col0 = t.n0 + half * HN;  // the warp's
       if (t.nkb > t.seg) {
+        // the sum of the segments, back into the last one's place
         float sum[HN];
 #pragma unroll
         for (int j = 0; j < HN; ++j) sum[j] = 0.f;
-        for (int left = t.nkb; left > 0 && filled(); left -= t.seg, ++use) {
+        for (int left = t.nkb; filled(); left -= t.seg, ++use) {
 #pragma unroll
           for (int j = 0; j < HN; j += 16) tmem_add16(at() + (uint32_t)j, sum + j);
+          if (left <= t.seg) break;
           release();
         }
         if (!ok) break;
-        auto get = [&](int c, float (&v)[32]) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = sum[c * 32 + j];
-        };
-        Op::template store<HN / 32, HN / 32>(p, t, row0, col0, box, &maps.out, get);
-        continue;
+        for (int j = 0; j < HN; j += 16) tmem_st16(at() + (uint32_t)j, sum + j);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      } else if (!filled()) {
+        break;
       }
-      if (!filled()) break;
       auto get = [&](int c, float (&v)[32]) {  // the accumulator is handed back when the last of it is in registers
         tmem_ld32(at() + (uint32_t)(c * 32), v);
         if (c == HN / 32 - 1) release();
       };
-      Op::template store<HN / 32, 1>(p, t, row0, col0, box, &maps.out, get);
+      Op::template store<HN / 32>(p, t, row0, col0, box, maps.out, get);
       ++use;
     }
     if (lane == 0) bulk_wait_all();
@@ -334,8 +385,12 @@ inline int products(int na, int nb, int lim) {
 // bits 2,048, which lose 4e-5.
 inline int segment(bool bits16, int prod, int nkb) { return std::min(nkb, std::max(1, (bits16 ? 512 : 12) / prod)); }
 
+// Clocks of a K block.  A 256-wide tile keeps the tensor pipe busy (512 a product, 570 measured for one); a 128-wide one reads
+// its operands from shared memory for half the work and is bound by that: 633 for one product, 1,010 for three.
+inline double block_clocks(int tn, int prod) { return tn == 256 ? 60 + 512.0 * prod : 440 + 190.0 * prod; }
+
 // Width of the tiles and ranges of K for a product of `values` in tiles(width) tiles over nkb K blocks: the cut whose
-// estimated clocks are fewest.  A K block takes 2 tn clocks a product; a tile's first loads and its epilogue some 3,000 that
+// estimated clocks are fewest.  A tile's first loads and its epilogue some 3,000 that
 // nothing hides where a unit has one tile; ranges are joined by another launch that reads their sums.
 struct Split {
   int tn, ks;
@@ -349,7 +404,7 @@ Split split_of(Tiles tiles, double values, int nkb, int prod, int units) {
     for (int ks = 1; ks <= 32 && ks * 2 <= std::max(2, nkb); ++ks) {
       if (ks > 1 && n * (ks - 1) >= 2 * units) break;
       const double waves = (double)((n * ks + units - 1) / units);
-      double clk = 3000 + waves * ((nkb + ks - 1) / ks) * prod * 2.0 * tn + (waves - 1) * 300;
+      double clk = 3000 + waves * ((nkb + ks - 1) / ks) * block_clocks(tn, prod) + (waves - 1) * 300;
       if (ks > 1) clk += 5000 + values * 8 * ks / 3500;
       if (least == 0 || clk < least) {
         least = clk;
@@ -366,6 +421,13 @@ inline int operand_map(CUtensorMap* map, const void* base, bool f16, long long i
                        int parts, long long ld, long long ld_b, long long ld_p, int box_rows) {
   const long long d[4] = {inner, rows, batch, parts}, l[3] = {ld, ld_b, ld_p};
   return map_nd(map, base, 4, d, l, box_rows, 1, f16 ? MAP_F16 : MAP_BF16);
+}
+
+// Map of a result that leaves in boxes of 32 x 32: cols x rows x batch of 16- or 32-bit values.
+inline int box_map(CUtensorMap* map, const void* base, MapType type, long long cols, long long rows, long long batch, long long ld,
+                   long long ld_b) {
+  const long long d[3] = {cols, rows, batch}, l[2] = {ld, ld_b};
+  return map_nd(map, base, 3, d, l, 32, 1, type, type != MAP_F32);
 }
 
 // Pairs that the current device holds at once.
