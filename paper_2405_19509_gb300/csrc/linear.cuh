@@ -62,14 +62,27 @@ __device__ __forceinline__ void store_part(__nv_bfloat16* row, int col0, int lan
   }
 }
 
-// 1 / (1 + exp(-x)).  exp overflows to infinity, whose quotient is 0.
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + expf(-x)); }
+// 2^x and 1 / x by the special function unit, 2 and 1 units in the last place off; 2^x of x below -126 is 0.
+__device__ __forceinline__ float power2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 1 / (1 + exp(-x)), of x / log2(e).  2^-x overflows to infinity, whose reciprocal is 0.
+__device__ __forceinline__ float sigmoid2(float x) { return reciprocal(1.f + power2(-x)); }
 
 // The normal distribution's tail and density (times sqrt(2 pi)): Phi(-|z|) = exp(-z^2 / 2) t q(t), t = 1 / (1 + 0.35 |z|),
-// with q of degree 8 fitted to the least relative error, 3.2e-8, over |z| <= 14.5.  In fp32 it is 6e-7 off for |z| < 3 and 4e-6
+// with q of degree 8 fitted to the least relative error, 3.2e-8, over |z| <= 14.5.  In fp32 it is 1e-6 off for |z| < 3 and 1e-5
 // at 13, where 1 + erf has lost all digits.
 __device__ __forceinline__ float tail(float z, float* density) {
-  const float x = fabsf(z), t = __fdividef(1.f, fmaf(0.35f, x, 1.f));
+  const float t = reciprocal(fmaf(0.35f, fabsf(z), 1.f));
   float q = -0x1.ddba88p-6f;
   q = fmaf(q, t, 0x1.26fa9ap-3f);
   q = fmaf(q, t, -0x1.05fb9ep-2f);
@@ -79,24 +92,23 @@ __device__ __forceinline__ float tail(float z, float* density) {
   q = fmaf(q, t, 0x1.eac964p-4f);
   q = fmaf(q, t, 0x1.1e70cap-3f);
   q = fmaf(q, t, 0x1.1df1c6p-3f);
-  *density = expf(-0.5f * x * x);
+  *density = power2(-0.5f * kLog2e * z * z);
   return *density * (t * q);
 }
 
-// act(z).  gelu by the normal distribution, gelu_tanh by the tanh of a cubic u: (1 + tanh u) / 2 = sigmoid(2 u).
+// act(z).  gelu = max(z, 0) - |z| Phi(-|z|); gelu_tanh by the tanh of a cubic u: (1 + tanh u) / 2 = sigmoid(2 u).
 __device__ __forceinline__ float activate(int act, float z) {
   switch (act) {
     case GC_ACT_RELU:
       return z < 0.f ? 0.f : z;  // NaN stays
     case GC_ACT_GELU: {
       float e;
-      const float p = tail(z, &e);
-      return z * (z > 0.f ? 1.f - p : p);
+      return fmaf(-fabsf(z), tail(z, &e), fmaxf(z, 0.f));
     }
     case GC_ACT_GELU_TANH:
-      return z * sigmoid(2.f * kTanh0 * z * fmaf(kTanh1, z * z, 1.f));
+      return z * sigmoid2(z * fmaf(2.f * kLog2e * kTanh0 * kTanh1, z * z, 2.f * kLog2e * kTanh0));
     case GC_ACT_SILU:
-      return z * sigmoid(z);
+      return z * sigmoid2(kLog2e * z);
     default:
       return z;
   }
@@ -104,21 +116,20 @@ __device__ __forceinline__ float activate(int act, float z) {
 
 // act'(z): of relu 0 at 0.  Past 100 the others' slopes are 0 or 1, and a product of an infinity there would be none.
 __device__ __forceinline__ float slope(int act, float z) {
+  if (act == GC_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
   if (fabsf(z) > 100.f) z = copysignf(100.f, z);  // NaN stays
   switch (act) {
-    case GC_ACT_RELU:
-      return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
     case GC_ACT_GELU: {
       float e;
       const float p = tail(z, &e);
       return fmaf(z * kInvRoot2Pi, e, z > 0.f ? 1.f - p : p);
     }
     case GC_ACT_GELU_TANH: {
-      const float s = sigmoid(2.f * kTanh0 * z * fmaf(kTanh1, z * z, 1.f));
-      return fmaf(z * s * (1.f - s), 2.f * kTanh0 * fmaf(3.f * kTanh1, z * z, 1.f), s);
+      const float s = sigmoid2(z * fmaf(2.f * kLog2e * kTanh0 * kTanh1, z * z, 2.f * kLog2e * kTanh0));
+      return fmaf(z * s * (1.f - s), fmaf(6.f * kTanh0 * kTanh1, z * z, 2.f * kTanh0), s);
     }
     case GC_ACT_SILU: {
-      const float s = sigmoid(z);
+      const float s = sigmoid2(kLog2e * z);
       return s * fmaf(z, 1.f - s, 1.f);
     }
     default:
