@@ -458,7 +458,7 @@ def _same_device(*tensors):
     """Calls run on the current device's stream: its tensors alone."""
     here = torch.cuda.current_device()
     for t in tensors:
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != here:
+        if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor on {t.device}, but the current device is cuda:{here}")
 
 

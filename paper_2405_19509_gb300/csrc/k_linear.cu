@@ -87,11 +87,12 @@ Scratch carve_linear(Carve& c, const LinearShape& s) {
 
 size_t linear_ws_bytes(const LinearShape& s) {
   Carve c(nullptr);
-  carve_linear(c, s);
+  if (!linear_small(s)) carve_linear(c, s);
   return c.bytes();
 }
 
 int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t* status, cudaStream_t st) {
+  if (linear_small(s)) return launch_linear_small(s, io, finish_of(s, io), st);
   const Scratch w = carve_linear(ws, s);
   const bool xb = s.x_dtype == GC_BF16;
   int rc = GC_OK;
@@ -107,12 +108,7 @@ int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t*
   const void *X = w.x_in_place ? io.X : w.X, *W = w.w_in_place ? io.W : w.W;
   const long long ldx = w.x_in_place ? io.ldx : w.Cp, ldw = w.w_in_place ? io.ldw : w.Cp;
   FwdOp::Params p{};
-  const int e = xb ? 2 : 4;
-  auto fours = [&](const void* q, int64_t ld) {
-    return !q || (reinterpret_cast<uintptr_t>(q) % (4 * e) == 0 && ld % 4 == 0);
-  };
-  p.f = Finish{s.F, s.act, xb, io.bias, io.res, io.y, io.z, (long long)io.ldr, (long long)io.ldy, (long long)io.ldz,
-               fours(io.res, io.ldr) && fours(io.y, io.ldy) && fours(io.z, io.ldz), 0};
+  p.f = finish_of(s, io);
   p.T = s.T;
   p.tn = w.tn;
   p.mt = tiles_of(s.T, TM);

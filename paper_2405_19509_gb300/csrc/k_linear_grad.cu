@@ -252,15 +252,12 @@ int launch_d(const LinearGradShape& s, const LinearGradIO& io, const Scratch& w,
                       w.Fp, np, w.D, w.sums, w.R);
 }
 
-}  // namespace
-
-size_t linear_grad_ws_bytes(const LinearGradShape& s) {
-  Carve c(nullptr);
-  carve_grad(c, s);
-  return c.bytes();
+// The outputs that k_linear_small.cu forms.
+int small_part(const LinearGradShape& s) {
+  return s.want & ((linear_small_dx(s) ? LINEAR_DX : 0) | (linear_small_g(s) ? LINEAR_G | LINEAR_GB : 0));
 }
 
-int launch_linear_grad(const LinearGradShape& s, const LinearGradIO& io, Carve& ws, uint32_t* status, cudaStream_t st) {
+int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& ws, uint32_t* status, cudaStream_t st) {
   const Scratch w = carve_grad(ws, s);
   const long long T = (long long)s.N * s.n_c;
   const bool xb = s.x_dtype == GC_BF16;
@@ -291,9 +288,7 @@ int launch_linear_grad(const LinearGradShape& s, const LinearGradIO& io, Carve& 
   const long long ldx = w.x_in_place ? io.ldx : w.Cp, ldw = w.w_in_place ? io.ldw : w.Cp;
   const long long ldd = w.d_in_place ? io.lddy : w.Fp;
   GradOp::Params p{};
-  const int e = xb ? 2 : 4;
-  p.f = Finish{s.C, GC_ACT_NONE, xb, nullptr, nullptr, io.dX, nullptr, 0, (long long)io.lddx, 0,
-               reinterpret_cast<uintptr_t>(io.dX) % (4 * e) == 0 && io.lddx % 4 == 0, 0};
+  p.f = finish_of(s, io);
   p.T = T;
   p.C = s.C;
   p.F = s.F;
@@ -353,6 +348,31 @@ int launch_linear_grad(const LinearGradShape& s, const LinearGradIO& io, Carve& 
                    : launch_tiles<GradOp, 128>(m, p, jobs, most_a, most_b, "k_linear_grad", chained, st);
   if (rc || !dx || w.ks == 1) return rc;
   return launch_join(w.part, w.ks, T, w.ld_part, p.f, st);
+}
+
+}  // namespace
+
+size_t linear_grad_ws_bytes(const LinearGradShape& s) {
+  Carve c(nullptr);
+  LinearGradShape t = s;
+  t.want &= ~small_part(s);
+  if (t.want) carve_grad(c, t);
+  return c.bytes();
+}
+
+int launch_linear_grad(const LinearGradShape& s, const LinearGradIO& io, Carve& ws, uint32_t* status, cudaStream_t st) {
+  if (const int few = small_part(s)) {
+    LinearGradIO a = io, b = io;
+    (few & LINEAR_DX ? b : a).dX = nullptr;
+    (few & LINEAR_G ? b : a).G = nullptr;
+    (few & LINEAR_GB ? b : a).Gb = nullptr;
+    const int rc = launch_linear_grad_small(s, a, finish_of(s, a), st);
+    if (rc || few == s.want) return rc;
+    LinearGradShape t = s;
+    t.want &= ~few;
+    return launch_grad_tiles(t, b, ws, status, st);
+  }
+  return launch_grad_tiles(s, io, ws, status, st);
 }
 
 }  // namespace gc

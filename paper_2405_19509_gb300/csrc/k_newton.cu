@@ -22,6 +22,7 @@
 
 #include <algorithm>
 
+#include "newton.cuh"
 #include "tc_tiles.cuh"
 
 namespace gc {
@@ -255,25 +256,29 @@ __global__ void __launch_bounds__(128) k_ns_join(const __grid_constant__ CUtenso
   const int m0 = row0 / TM * TM, n0 = col0 / tn * tn;
   if (sym && n0 >= m0 + TM) return;
   const size_t range = (size_t)e.batch * e.rows * ld;
-  const float* from = part + ((size_t)mat * e.rows + row0 + lane) * ld + col0;
+  const float* from = part + ((size_t)mat * e.rows + row0) * ld + col0;
+  const int m = min(e.rows - row0, 32), n = min(ld - col0, 32);  // ld: a multiple of 4
+  Rows32<8> sum;
+  sum.load(from, ld * 4LL, m, n * 4, lane);
+  for (int k = 1; k < ks; ++k) {
+    Rows32<8> x;
+    x.load(from + k * range, ld * 4LL, m, n * 4, lane);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      sum.q[j].x = __float_as_uint(__uint_as_float(sum.q[j].x) + __uint_as_float(x.q[j].x));
+      sum.q[j].y = __float_as_uint(__uint_as_float(sum.q[j].y) + __uint_as_float(x.q[j].y));
+      sum.q[j].z = __float_as_uint(__uint_as_float(sum.q[j].z) + __uint_as_float(x.q[j].z));
+      sum.q[j].w = __float_as_uint(__uint_as_float(sum.q[j].w) + __uint_as_float(x.q[j].w));
+    }
+  }
+  sum.turn(box, lane);
   float v[32];
 #pragma unroll
-  for (int j = 0; j < 32; j += 4) {
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row0 + lane < e.rows && col0 + j < e.cols) {
-      x = __ldcg(reinterpret_cast<const float4*>(from + j));
-      for (int k = 1; k < ks; ++k) {
-        const float4 y = __ldcg(reinterpret_cast<const float4*>(from + j + k * range));
-        x.x += y.x;
-        x.y += y.y;
-        x.z += y.z;
-        x.w += y.w;
-      }
-    }
-    v[j] = x.x;
-    v[j + 1] = x.y;
-    v[j + 2] = x.z;
-    v[j + 3] = x.w;
+  for (int j = 0; j < 8; ++j) {
+    v[4 * j] = __uint_as_float(sum.q[j].x);
+    v[4 * j + 1] = __uint_as_float(sum.q[j].y);
+    v[4 * j + 2] = __uint_as_float(sum.q[j].z);
+    v[4 * j + 3] = __uint_as_float(sum.q[j].w);
   }
   e.finish(v, box, &out, mat, row0, col0, sym && n0 + tn <= m0);
   if (lane == 0) bulk_wait_all();
@@ -333,12 +338,7 @@ __global__ void __launch_bounds__(256) k_ns_norm(const Source s, double* __restr
     float q = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) q = fmaf(v[j], v[j], q);
-    if (q > 1e-24f && q < 1e37f) {
-      sum += q;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum += (double)v[j] * v[j];
-    }
+    add_squares(q, v, sum);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -360,24 +360,23 @@ __global__ void __launch_bounds__(256) k_ns_scale(const Source s, const double* 
   const int segs = (s.cols + kSeg - 1) / kSeg;
   start_next();
   wait_prior();
+  __shared__ double red[8];
+  __shared__ float factor[3];
   double sum = 0;
-  for (int i = lane; i < s.blocks; i += 32) sum += __ldcg(sums + (size_t)mat * s.blocks + i);
+#pragma unroll 4
+  for (int i = threadIdx.x; i < s.blocks; i += 256) sum += __ldcg(sums + (size_t)mat * s.blocks + i);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  // u / norm as three factors, none of which leaves fp32's range: norm = f 2^e
-  double norm = sqrt(sum);
-  int down = 0;  // lam = 2^-down
-  if (norm < (double)eps) {
-    const double t = norm / (double)eps * (double)amp;
-    if (t < 1) down = t > 0x1p-125 ? -ilogb(t) - 1 : 125;  // t <= lam < 2 t
-    norm = eps;
+  if (lane == 0) red[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 8; ++w) sum += red[w];
+    int down;
+    norm_factors(sum, eps, amp, kSX, factor, &down);
+    if (block == 0) lam[mat] = ldexpf(1.f, -down);
   }
-  if (block == 0 && threadIdx.x == 0) lam[mat] = ldexpf(1.f, -down);
-  int e = 0;
-  const double f = frexp(norm, &e);
-  e -= down;
-  const float r = isinf(norm) ? 0.f : (float)((double)kSX / f);
-  const float p0 = isinf(norm) || isnan(norm) ? 1.f : ldexpf(1.f, -(e / 2)), p1 = isinf(norm) || isnan(norm) ? 1.f : ldexpf(1.f, -(e - e / 2));
+  __syncthreads();
+  const float p0 = factor[0], p1 = factor[1], r = factor[2];
   const long long n = (long long)s.rows * segs;
 #pragma unroll 2
   for (long long i = (long long)block * 8 + warp; i < n; i += (long long)s.blocks * 8) {
@@ -579,11 +578,12 @@ bool ns_coefficients_bounded(const float* k, int steps) {
 
 size_t ns_ws_bytes(const NsShape& s) {
   Carve c(nullptr);
-  carve_ns(c, s);
+  if (!ns_small(s)) carve_ns(c, s);
   return c.bytes();
 }
 
 int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cudaStream_t st) {
+  if (ns_small(s)) return launch_ns_small(s, io, st);
   const Scratch w = carve_ns(ws, s);
   const bool bf = s.dtype == GC_BF16, mom = io.m != nullptr;
   const int e = bf ? 2 : 4;

@@ -238,6 +238,20 @@ static __global__ void __launch_bounds__(256) k_linear_join(const float* __restr
   }
 }
 
+inline bool fours(const void* q, int64_t ld, int elt) {
+  return !q || (reinterpret_cast<uintptr_t>(q) % (4 * elt) == 0 && ld % 4 == 0);
+}
+// The epilogue of a call; its box is for finish_maps to say.
+inline Finish finish_of(const LinearShape& s, const LinearIO& io) {
+  const int e = s.x_dtype == GC_BF16 ? 2 : 4;
+  return Finish{s.F, s.act, e == 2, io.bias, io.res, io.y, io.z, (long long)io.ldr, (long long)io.ldy, (long long)io.ldz,
+                fours(io.res, io.ldr, e) && fours(io.y, io.ldy, e) && fours(io.z, io.ldz, e), 0};
+}
+inline Finish finish_of(const LinearGradShape& s, const LinearGradIO& io) {
+  const int e = s.x_dtype == GC_BF16 ? 2 : 4;
+  return Finish{s.C, GC_ACT_NONE, e == 2, nullptr, nullptr, io.dX, nullptr, 0, (long long)io.lddx, 0, fours(io.dX, io.lddx, e), 0};
+}
+
 inline int launch_join(const float* part, int ks, long long rows, int ld, const Finish& f, cudaStream_t st) {
   const unsigned grid = (unsigned)((rows * (ld / 4) + 255) / 256);
   return f.bf16 ? launch_chain(k_linear_join<__nv_bfloat16>, "k_linear_join", grid, 256, 0, 1, true, st, part, ks, rows,
@@ -246,4 +260,22 @@ inline int launch_join(const float* part, int ks, long long rows, int ld, const 
 }
 
 }  // namespace linear
+
+// Small layers, in fp32 products (k_linear_small.cu).  G and Gb of a chunk have the same bits whatever chunks a call has, so
+// their choice looks at a chunk's work alone.
+// Measured as graph replays, kernels here against tiles (us): 2^24 products in bf16 6.2 against 11.6, 2^25 6.3 against 11.6, 2^26
+// 10.8 against 12.8, 2^27 15 against 13; fp32 2^27 18.5 against 13.5.  Rows of 2048 by 8192 in bf16: one 5.4, two 8.0, four 17, eight
+// 27, against 13.5; with an fp32 W, which tiles copy in parts, 9, 13, 21, 36 against 35.  dx of 2^23.6 8.8 against 14.9, of
+// 2^24.6 15.4 against 13.5; six chunks' G of 2^21 each 6.4 against 15.9, of 2^24 21 against 17.
+constexpr int kLinearRows = 8;
+constexpr double kLinearSmall = 1 << 25, kLinearSmallDx = 1 << 24, kLinearSmallChunk = 1 << 21;
+inline bool linear_small(const LinearShape& s) {
+  const bool copies = s.x_dtype != GC_BF16 || s.w_dtype != GC_BF16 || !s.x_16 || !s.w_16;
+  return s.T <= 2 || (double)s.T * s.C * s.F <= (s.T <= kLinearRows && copies ? 2 : 1) * kLinearSmall;
+}
+inline bool linear_small_dx(const LinearGradShape& s) { return (double)s.N * s.n_c * s.C * s.F <= kLinearSmallDx; }
+inline bool linear_small_g(const LinearGradShape& s) { return (double)s.n_c * s.C * s.F <= kLinearSmallChunk; }
+int launch_linear_small(const LinearShape& s, const LinearIO& io, const linear::Finish& f, cudaStream_t st);
+int launch_linear_grad_small(const LinearGradShape& s, const LinearGradIO& io, const linear::Finish& f, cudaStream_t st);
+
 }  // namespace gc

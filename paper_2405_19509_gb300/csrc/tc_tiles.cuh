@@ -126,7 +126,7 @@ struct Rows32 {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = i * (32 / N) + lane / N;
-      q[i] = r < rows && j * 16 < bytes ? *reinterpret_cast<const uint4*>(static_cast<const char*>(from) + r * ld + j * 16)
+      q[i] = r < rows && j * 16 < bytes ? __ldcg(reinterpret_cast<const uint4*>(static_cast<const char*>(from) + r * ld + j * 16))
                                         : make_uint4(0, 0, 0, 0);
     }
   }

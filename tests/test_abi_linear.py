@@ -24,7 +24,7 @@ def _fwd(X=Q, ldx=64, xt=1, W=P, ldw=64, wt=1, bias=None, act=0, res=None, ldr=1
     (dict(ldw=63), -2), (dict(ldy=99), -2), (dict(z=U, ldz=99), -2), (dict(res=U, ldr=99), -2), (dict(bias=BAD4), -1),
     (dict(X=BAD2), -1), (dict(y=BAD2), -1), (dict(X=BAD4, xt=0), -1), (dict(y=Q), -1), (dict(z=Q), -1), (dict(z=S), -1),
     (dict(z=U, res=U), -1), (dict(ws=None), -6), (dict(n=255), -6), (dict(ws=ctypes.c_void_p(4160)), -6),
-    (dict(wt=0, n=4096), -6)])
+    (dict(wt=0, rows=100000, n=4096), -6)])
 def test_forward_refusals(kw, code):
     assert _fwd(**kw) == code
 
@@ -46,7 +46,7 @@ def _bwd(dy=Q, lddy=100, z=U, ldz=100, X=Q, ldx=64, xt=1, W=P, ldw=64, wt=1, act
     (dict(N=1 << 20, n_c=1, C=1 << 17, F=1 << 17), -3), (dict(lddy=99), -2), (dict(ldz=99), -2), (dict(ldx=63), -2),
     (dict(ldw=63), -2), (dict(lddx=63), -2), (dict(ldg=6399), -2), (dict(ldgb=99), -2), (dict(G=BAD4), -1),
     (dict(Gb=BAD4), -1), (dict(dy=BAD2), -1), (dict(dX=Q), -1), (dict(dX=P), -1), (dict(dX=U), -1), (dict(ws=None), -6),
-    (dict(n=1000), -6), (dict(ws=ctypes.c_void_p(4160)), -6)])
+    (dict(n_c=100000, n=1000), -6), (dict(ws=ctypes.c_void_p(4160)), -6)])
 def test_backward_refusals(kw, code):
     assert _bwd(**kw) == code
 

@@ -33,7 +33,7 @@ COMMON = [
     (dict(batch=1 << 20, rows=1 << 11, cols=1 << 11), -3), (dict(steps=0), -1), (dict(steps=65), -1), (dict(eps=-1.0), -1),
     (dict(eps=float("nan")), -1), (dict(eps=float("inf")), -1), (dict(co=_c(3.4445, 4.775, 2.0315)), -1),
     (dict(co=_c(float("nan"), 0, 0)), -1), (dict(co=_c(1.5, -0.5, float("inf"))), -1), (dict(co=_c(100, -200, 100)), -1),
-    (dict(co=_c(4.5, 0, 0)), -1), (dict(ws=None), -6), (dict(n=4096), -6), (dict(ws=ctypes.c_void_p(4160)), -6),
+    (dict(co=_c(4.5, 0, 0)), -1), (dict(ws=None), -6), (dict(n=255), -6), (dict(ws=ctypes.c_void_p(4160)), -6),
 ]
 
 
@@ -67,7 +67,7 @@ def test_workspace():
     f = _lib().lib.gc_orthogonalize_workspace
     assert f(1, 100, 64, 2) == 0 and f(-1, 1, 1, 0) == 0 and f(1, 0, 1, 0) == 0 and f(0, 5, 5, 0) == 256
     m, n = 2048, 8192
-    assert 8 * m * n + 8 * m * m <= f(1, m, n, 0) < 1.1 * (8 * m * n + 8 * m * m)
+    assert 8 * m * n + 8 * m * m <= f(1, m, n, 0) < 1.5 * (8 * m * n + 8 * m * m)
     assert f(1, n, m, 0) == f(1, m, n, 0) and f(3, 100, 64, 1) <= f(3, 100, 64, 0)
 
 
