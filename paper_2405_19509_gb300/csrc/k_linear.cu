@@ -22,8 +22,6 @@ struct FwdOp {
     int mt, nt, tn, group;  // tiles of T and of F; row tiles that share a sweep of the columns
     int nkb, ks, seg;       // K blocks, in ks ranges
     int nx, nw, lim;
-    float* part;            // sums of the ranges [ks][T][ld_part]
-    int ld_part;
   };
   static __device__ __forceinline__ int jobs(const Params& p, int unit) {
     return (int)(((long long)p.mt * p.nt * p.ks - unit + p.q.units - 1) / p.q.units);
@@ -45,13 +43,13 @@ struct FwdOp {
     t.lim = p.lim;
     t.seg = p.seg;
     t.a_mn = t.b_mn = false;
+    t.a_turn = t.b_turn = kNever;
     return t;
   }
   template <int NC, typename Get>
   static __device__ __forceinline__ void store(const Params& p, const Job& t, int row0, int col0, uint8_t* box,
                                                const CUtensorMap* out, Get get) {
-    store_rows<NC>(p.f, p.T, p.ks > 1 ? p.part + (size_t)t.range * p.T * p.ld_part : nullptr, p.ld_part, row0, col0, box, out,
-                   get);
+    store_rows<NC>(p.f, p.T, p.ks > 1 ? t.range : -1, out, row0, col0, box, out, get);
   }
 };
 
@@ -120,8 +118,6 @@ int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t*
   p.nw = w.nw;
   p.lim = w.lim;
   p.seg = segment(xb, products(w.nx, w.nw, w.lim), p.nkb);
-  p.part = w.part;
-  p.ld_part = w.ld_part;
   p.q.a_both = s.T > 128;
   p.q.a_rows = s.T > 128 ? 128 : (int)(s.T + 7) / 8 * 8;
   p.q.spin_limit = wait_limit(kSpin);
@@ -133,7 +129,7 @@ int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t*
     return rc;
   m.a[1] = m.a[0];
   m.b[1] = m.b[0];
-  if ((rc = finish_maps(&p.f, s.T, &m))) return rc;
+  if ((rc = finish_maps(&p.f, s.T, w.part, w.ks, w.ld_part, &m))) return rc;
   const long long jobs = (long long)p.mt * p.nt * p.ks;
   rc = w.tn == 256 ? launch_tiles<FwdOp, 256>(m, p, jobs, w.nx, w.nw, "k_linear", chained, st)
                    : launch_tiles<FwdOp, 128>(m, p, jobs, w.nx, w.nw, "k_linear", chained, st);

@@ -104,8 +104,6 @@ struct GradOp {
                            // one dx tile less, and the rest round robin
     int f_nkb, c_nkb, ks;  // K blocks of dx, in ks ranges, and of G
     int np_dx, np, nx, nw, lim, seg_dx, seg_g;
-    float* part;
-    int ld_part;
     float* G;
     long long ldg;
     int g_box;
@@ -118,6 +116,7 @@ struct GradOp {
   static __device__ __forceinline__ Job job(const Params& p, int unit, int k) {
     Job t;
     t.b_mn = true;
+    t.a_turn = t.b_turn = kNever;
     t.lim = p.lim;
     const int ndx = (p.ndx - unit + p.q.units - 1) / p.q.units;
     if (k < ndx) {
@@ -155,9 +154,8 @@ struct GradOp {
                                                const CUtensorMap* out, Get get) {
     const int lane = threadIdx.x & 31;
     if (t.kind == 0) {
-      store_rows<NC>(p.f, p.T, p.ks > 1 ? p.part + (size_t)t.range * p.T * p.ld_part : nullptr, p.ld_part, row0, col0, box, out,
-                     get);
-      box_free<0>(lane);  // a tile of G uses the box next
+      store_rows<NC>(p.f, p.T, p.ks > 1 ? t.range : -1, out, row0, col0, box, out, get);
+      box_free(lane);  // a tile of G may write the box otherwise
       return;
     }
     const int rows = min(p.F - row0, 32);
@@ -169,27 +167,19 @@ struct GradOp {
       const int col = col0 + c * 32;
       if (rows <= 0 || col >= p.C) continue;
       if (p.g_box) {
-        box_free<0>(lane);
-        box_put(box, lane, v);
-        box_full();
-        if (lane == 0) {
-          store_3d(&out[1], box, col, row0, t.b);
-          bulk_commit();
-        }
+        store_32(&out[1], box, lane, v, p.C - col, col, row0, t.b);
       } else {
-        box_put(box, lane, v);
-        __syncwarp();
-        float* g = p.G + t.b * p.ldg + (long long)row0 * p.C + col + lane;
-        by_rows<4>(box, lane, col + lane < p.C ? rows : 0, [&](int r, float s) { g[(long long)r * p.C] = s; });
+        float* g = p.G + t.b * p.ldg + (long long)row0 * p.C + col;
+        by_rows(box, lane, v, rows, p.C - col, [&](int r, int j, float s) { g[(long long)r * p.C + j] = s; });
       }
     }
-    if (p.g_box) box_free<0>(lane);  // a tile of dx may use the box next
+    if (p.g_box) box_free(lane);  // and a tile of dx
   }
 };
 
 struct Scratch {
   int Cp, Fp, np, np_dx, nx, nw, lim, tn, ks, ld_part, R;
-  bool x_in_place, w_in_place, d_in_place, direct;  // direct: one partial sum a chunk, which is Gb
+  bool x_in_place, w_in_place, d_in_place;
   __nv_bfloat16 *X, *W, *D;
   float *part, *sums;
 };
@@ -308,8 +298,6 @@ int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& w
   const int prod_dx = products(w.np_dx, w.nw, w.lim), prod_g = products(w.np, w.nx, w.lim);
   p.seg_dx = segment(xb, prod_dx, p.f_nkb);
   p.seg_g = segment(false, prod_g, p.c_nkb);
-  p.part = w.part;
-  p.ld_part = w.ld_part;
   p.G = io.G;
   p.ldg = io.ldg;
   p.ndx = dx ? p.mt * p.ct * p.ks : 0;
@@ -330,16 +318,14 @@ int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& w
       (rc = operand_map(&m.a[1], D, false, s.F, s.n_c, s.N, w.np, ldd, s.n_c * ldd, T * ldd, BK)))
     return rc;
   m.b[0] = m.b[1] = m.a[0];
-  if (dx) rc = finish_maps(&p.f, T, &m);
-  else m.out[0] = m.out[1] = m.a[0];
-  if (rc) return rc;
+  m.out[0] = m.out[1] = m.a_turned = m.b_turned = m.a[0];
+  if (dx && (rc = finish_maps(&p.f, T, w.part, w.ks, w.ld_part, &m))) return rc;
   if (dx && (rc = operand_map(&m.b[0], W, false, s.C, s.F, 1, w.nw, ldw, s.F * ldw, s.F * ldw, BK))) return rc;
   if (g) {
     if ((rc = operand_map(&m.b[1], X, false, s.C, s.n_c, s.N, w.nx, ldx, s.n_c * ldx, T * ldx, BK))) return rc;
     p.g_box = s.C % 4 == 0 && rows_16(io.G, io.ldg, 4);
     if (p.g_box) {
-      const long long dg[3] = {s.C, s.F, s.N}, lg[2] = {s.C, io.ldg};
-      if ((rc = map_nd(&m.out[1], io.G, 3, dg, lg, 32, 1, MAP_F32))) return rc;
+      if ((rc = box_map(&m.out[1], io.G, MAP_F32, s.C, s.F, s.N, s.C, io.ldg))) return rc;
     }
   }
   const long long jobs = (long long)p.ndx + p.ng;

@@ -8,8 +8,8 @@
 //   k_ns_join       the same epilogues where a tile's sum runs in ranges
 //
 // X stays as u lies, wide or tall: of a tall u the products are X^T X and X P, whose operands are read MN-major, and
-// nothing is transposed.  A and P are symmetric: tiles above the diagonal are not formed but written as mirrors of those
-// below.
+// nothing is transposed.  A and P are symmetric: tiles above the diagonal are not formed, and where an operand's K blocks
+// would be theirs, those below are read in their place, MN-major for K-major.
 //
 // Parts are fp16 of values times a power of two.  Singular values stay below kMost (the entry point checks the
 // polynomial), so entries of X, A and P fit, and the parts of an entry end at 2^-24 / scale, 2^-37 for X: what is lost is
@@ -66,55 +66,56 @@ struct Epilogue {
       *to = kind == NS_STEP ? fmaf(s, x, keep * *to) : s * x;
     }
   }
-  // 32 x 32 sums at (row0, col0), a lane a row, to w.
+  // 32 x 32 sums at (row0, col0), a lane a row, of which m rows and n columns exist, to w.
   __device__ __forceinline__ void finish_w(float (&v)[32], uint8_t* buf, const CUtensorMap* map, int mat, int row0, int col0,
                                            int m, int n) const {
     const int lane = threadIdx.x & 31;
     const float l = lam[mat];
     if (!box) {
-      box_put(buf, lane, v);
-      __syncwarp();
-      by_rows<1>(buf, lane, lane < n ? m : 0, [&](int r, float x) { one(mat, l, row0 + r, col0 + lane, x); });
+      by_rows(buf, lane, v, m, n, [&](int r, int j, float x) { one(mat, l, row0 + r, col0 + j, x); });
       return;
+    }
+    Rows32 old[2];
+    if (kind == NS_STEP) {
+      const float* from = reinterpret_cast<const float*>(w) + mat * sw + (long long)row0 * ldw + col0;
+      old[0].load(from, ldw * 4, m, n * 4, lane);
+      old[1].load(from + 16, ldw * 4, m, n * 4 - 64, lane);
     }
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = s * (l * v[j]);
-    if (kind == NS_STEP) {
-      Rows32<8> old;
-      old.load(reinterpret_cast<const float*>(w) + mat * sw + (long long)row0 * ldw + col0, ldw * 4, m, n * 4, lane);
-      box_free<0>(lane);
-      old.turn(buf, lane);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[4 * j] = fmaf(keep, __uint_as_float(old.q[j].x), v[4 * j]);
-        v[4 * j + 1] = fmaf(keep, __uint_as_float(old.q[j].y), v[4 * j + 1]);
-        v[4 * j + 2] = fmaf(keep, __uint_as_float(old.q[j].z), v[4 * j + 2]);
-        v[4 * j + 3] = fmaf(keep, __uint_as_float(old.q[j].w), v[4 * j + 3]);
-      }
-    } else {
-      box_free<0>(lane);
-    }
-    if (bf16)
+    box_free(lane);
+    if (bf16) {
       box_put_16(buf, lane, [&](int j) { return pack_bf16(v[j], v[j + 1]); });
-    else
-      box_put(buf, lane, v);
-    box_full();
-    if (lane == 0) {
-      store_3d(map, buf, col0, row0, mat);
-      bulk_commit();
+      box_store(map, buf, lane, col0, row0, mat);
+      return;
     }
+    if (kind == NS_STEP) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        old[h].turn(buf, lane);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float* x = v + 16 * h + 4 * j;
+          x[0] = fmaf(keep, __uint_as_float(old[h].q[j].x), x[0]);
+          x[1] = fmaf(keep, __uint_as_float(old[h].q[j].y), x[1]);
+          x[2] = fmaf(keep, __uint_as_float(old[h].q[j].z), x[2]);
+          x[3] = fmaf(keep, __uint_as_float(old[h].q[j].w), x[3]);
+        }
+      }
+    }
+    store_32(map, buf, lane, v, n, col0, row0, mat);
   }
-  // ... or as parts; mirror: also at (col0, row0).
+  // ... or as parts.
   __device__ __forceinline__ void finish_parts(float (&v)[32], uint8_t* buf, const CUtensorMap* map, int mat, int row0, int col0,
-                                               int m, int n, bool mirror) const {
+                                               int m, int n) const {
     const int lane = threadIdx.x & 31;
-    box_free<0>(lane);
     if (kind == NS_P) {
       const float l2 = lam[mat] * lam[mat], sum = s * l2 * l2, b2 = b * l2;
+      box_free(lane);
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] = fmaf(sum, v[j], row0 + lane == col0 + j ? a : 0.f);
       for (int q = 0; q < na; ++q) {
-        Rows32<4> part;  // rows of A end past a multiple of eight
+        Rows32 part;  // rows of A end past a multiple of eight
         part.load(A.p + q * A.plane + mat * A.mat + (long long)row0 * A.ld + col0, A.ld * 2LL, m, (n + 7) / 8 * 16, lane);
         part.turn(buf, lane);
 #pragma unroll
@@ -142,27 +143,17 @@ struct Epilogue {
         v[2 * j] -= f.x;
         v[2 * j + 1] -= f.y;
       }
-      box_put_16(buf + q * HALF_BOX, lane, [&](int j) { return h[j / 2]; });
-      box_full();
-      if (lane == 0) {
-        store_3d(map, buf + q * HALF_BOX, col0, row0, q * batch + mat);
-        bulk_commit();
-      }
-      if (mirror && lane < m) {
-        uint16_t* to = reinterpret_cast<uint16_t*>(out.p + q * out.plane + mat * out.mat + (long long)col0 * out.ld + row0 + lane);
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (j < n) to[(long long)j * out.ld] = (uint16_t)(h[j / 2] >> (16 * (j & 1)));
-      }
+      box_free(lane);
+      box_put_16(buf, lane, [&](int j) { return h[j / 2]; });
+      box_store(map, buf, lane, col0, row0, q * batch + mat);
     }
   }
-  __device__ __forceinline__ void finish(float (&v)[32], uint8_t* buf, const CUtensorMap* map, int mat, int row0, int col0,
-                                         bool mirror) const {
+  __device__ __forceinline__ void finish(float (&v)[32], uint8_t* buf, const CUtensorMap* map, int mat, int row0, int col0) const {
     const int m = min(rows - row0, 32), n = cols - col0;
     if (kind >= NS_OUT)
       finish_w(v, buf, map, mat, row0, col0, m, n);
     else
-      finish_parts(v, buf, map, mat, row0, col0, m, n, mirror);
+      finish_parts(v, buf, map, mat, row0, col0, m, n);
   }
 };
 
@@ -179,8 +170,7 @@ struct NsOp {
     int batch, mt, nt, per, tn, sym;  // tiles of rows, of columns, of a matrix
     int nkb, ks, seg, na, nb, lim;
     int a_mn, b_mn;
-    float* part;                      // sums of the ranges [ks][batch][rows][ld_part]
-    int ld_part;
+    int a_sym, b_sym;                 // operands of which what is above the diagonal's blocks is not there
   };
   static __device__ __forceinline__ int jobs(const Params& p, int unit) {
     return (int)(((long long)p.batch * p.per * p.ks - unit + p.q.units - 1) / p.q.units);
@@ -211,31 +201,25 @@ struct NsOp {
     t.seg = p.seg;
     t.a_mn = p.a_mn;
     t.b_mn = p.b_mn;
+    t.a_turn = p.a_sym ? turn_of(t.m0) : kNever;
+    t.b_turn = p.b_sym ? turn_of(t.n0) : kNever;
     return t;
   }
   template <int NC, typename Get>
   static __device__ __forceinline__ void store(const Params& p, const Job& t, int row0, int col0, uint8_t* box,
                                                const CUtensorMap* out, Get get) {
     const int lane = threadIdx.x & 31;
-    const int rows = p.e.rows - row0;
-    const bool mirror = p.sym && t.n0 + p.tn <= t.m0;
 #pragma unroll 1
     for (int c = 0; c < NC; ++c) {
       float v[32];
       __syncwarp();
       get(c, v);
       const int col = col0 + c * 32;
-      if (rows <= 0 || col >= p.e.cols) continue;
-      if (p.ks > 1) {
-        box_put(box, lane, v);
-        __syncwarp();
-        float* to = p.part + (((size_t)t.range * p.batch + t.b) * p.e.rows + row0) * p.ld_part + col;
-        by_fours(box, lane, [&](int r, int j, float4 s) {
-          if (r < rows && col + j < p.e.cols) *reinterpret_cast<float4*>(to + (size_t)r * p.ld_part + j) = s;
-        });
-      } else {
-        p.e.finish(v, box, out, t.b, row0, col, mirror);
-      }
+      if (row0 >= p.e.rows || col >= p.e.cols) continue;
+      if (p.ks > 1)  // sums of the ranges [ks][batch][rows][cols, up to a multiple of four]
+        store_32(&out[1], box, lane, v, p.e.cols - col, col, row0, t.range * p.batch + t.b);
+      else
+        p.e.finish(v, box, out, t.b, row0, col);
     }
   }
 };
@@ -257,30 +241,33 @@ __global__ void __launch_bounds__(128) k_ns_join(const __grid_constant__ CUtenso
   if (sym && n0 >= m0 + TM) return;
   const size_t range = (size_t)e.batch * e.rows * ld;
   const float* from = part + ((size_t)mat * e.rows + row0) * ld + col0;
-  const int m = min(e.rows - row0, 32), n = min(ld - col0, 32);  // ld: a multiple of 4
-  Rows32<8> sum;
-  sum.load(from, ld * 4LL, m, n * 4, lane);
-  for (int k = 1; k < ks; ++k) {
-    Rows32<8> x;
-    x.load(from + k * range, ld * 4LL, m, n * 4, lane);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      sum.q[j].x = __float_as_uint(__uint_as_float(sum.q[j].x) + __uint_as_float(x.q[j].x));
-      sum.q[j].y = __float_as_uint(__uint_as_float(sum.q[j].y) + __uint_as_float(x.q[j].y));
-      sum.q[j].z = __float_as_uint(__uint_as_float(sum.q[j].z) + __uint_as_float(x.q[j].z));
-      sum.q[j].w = __float_as_uint(__uint_as_float(sum.q[j].w) + __uint_as_float(x.q[j].w));
-    }
-  }
-  sum.turn(box, lane);
+  const int m = min(e.rows - row0, 32), n = (ld - col0) * 4;  // ld: a multiple of 4
   float v[32];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    v[4 * j] = __uint_as_float(sum.q[j].x);
-    v[4 * j + 1] = __uint_as_float(sum.q[j].y);
-    v[4 * j + 2] = __uint_as_float(sum.q[j].z);
-    v[4 * j + 3] = __uint_as_float(sum.q[j].w);
+  for (int h = 0; h < 2; ++h) {
+    Rows32 sum;
+    sum.load(from + 16 * h, ld * 4LL, m, n - 64 * h, lane);
+    for (int k = 1; k < ks; ++k) {
+      Rows32 x;
+      x.load(from + 16 * h + k * range, ld * 4LL, m, n - 64 * h, lane);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sum.q[j].x = __float_as_uint(__uint_as_float(sum.q[j].x) + __uint_as_float(x.q[j].x));
+        sum.q[j].y = __float_as_uint(__uint_as_float(sum.q[j].y) + __uint_as_float(x.q[j].y));
+        sum.q[j].z = __float_as_uint(__uint_as_float(sum.q[j].z) + __uint_as_float(x.q[j].z));
+        sum.q[j].w = __float_as_uint(__uint_as_float(sum.q[j].w) + __uint_as_float(x.q[j].w));
+      }
+    }
+    sum.turn(box, lane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[16 * h + 4 * j] = __uint_as_float(sum.q[j].x);
+      v[16 * h + 4 * j + 1] = __uint_as_float(sum.q[j].y);
+      v[16 * h + 4 * j + 2] = __uint_as_float(sum.q[j].z);
+      v[16 * h + 4 * j + 3] = __uint_as_float(sum.q[j].w);
+    }
   }
-  e.finish(v, box, &out, mat, row0, col0, sym && n0 + tn <= m0);
+  e.finish(v, box, &out, mat, row0, col0);
   if (lane == 0) bulk_wait_all();
 }
 
@@ -420,6 +407,7 @@ __global__ void __launch_bounds__(256) k_ns_scale(const Source s, const double* 
 struct Product {
   int rows, cols, K, sym;
   int na, nb, a_mn, b_mn;
+  int a_sym, b_sym;
   int lim() const { return std::max(na, nb); }
   int prod() const { return products(na, nb, lim()); }
 };
@@ -466,9 +454,9 @@ Scratch carve_ns(Carve& c, const NsShape& s) {
   w.P = take_parts(c, w.pp, s.batch, w.m, w.m);
   w.sums = c.take<double>((size_t)s.batch * w.blocks);
   w.lam = c.take<float>(s.batch);
-  w.pa = Product{w.m, w.m, w.n, 1, w.xa, w.xa, !w.wide, !w.wide};
-  w.pp2 = Product{w.m, w.m, w.m, 1, w.aa, w.aa, 0, 0};
-  w.px = w.wide ? Product{w.m, w.n, w.m, 0, w.pp, w.xx, 0, 1} : Product{w.n, w.m, w.m, 0, w.xx, w.pp, 0, 0};
+  w.pa = Product{w.m, w.m, w.n, 1, w.xa, w.xa, !w.wide, !w.wide, 0, 0};
+  w.pp2 = Product{w.m, w.m, w.m, 1, w.aa, w.aa, 0, 0, 1, 1};
+  w.px = w.wide ? Product{w.m, w.n, w.m, 0, w.pp, w.xx, 0, 1, 1, 0} : Product{w.n, w.m, w.m, 0, w.xx, w.pp, 0, 0, 0, 1};
   w.ca = cut_of(w.pa, s.batch);
   w.cp = cut_of(w.pp2, s.batch);
   w.cx = cut_of(w.px, s.batch);
@@ -501,8 +489,9 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
   p.seg = segment(bits16, g.prod(), p.nkb);
   p.a_mn = g.a_mn;
   p.b_mn = g.b_mn;
-  p.part = part;
-  p.ld_part = (g.cols + 3) / 4 * 4;
+  p.a_sym = g.a_sym;
+  p.b_sym = g.b_sym;
+  const int ld_part = (g.cols + 3) / 4 * 4;
   p.q.f16 = 1;
   p.q.a_both = g.rows > 128;
   p.q.a_rows = g.rows > 128 ? 128 : (g.rows + 7) / 8 * 8;
@@ -517,8 +506,12 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
   };
   if ((rc = map(&m.a[0], A, g.na, g.a_mn, g.rows, p.q.a_rows)) || (rc = map(&m.b[0], B, g.nb, g.b_mn, g.cols, cut.tn / 2)))
     return rc;
-  m.a[1] = m.out[0] = m.out[1] = m.a[0];
-  m.b[1] = m.b[0];
+  m.a[1] = m.out[0] = m.out[1] = m.a_turned = m.a[0];
+  m.b[1] = m.b_turned = m.b[0];
+  if (g.a_sym && (rc = map(&m.a_turned, A, g.na, 1, g.rows, 0))) return rc;
+  if (g.b_sym && (rc = map(&m.b_turned, B, g.nb, 1, g.cols, 0))) return rc;
+  if (p.ks > 1 && (rc = box_map(&m.out[1], part, MAP_F32, ld_part, g.rows, (long long)p.ks * s.batch, ld_part, (long long)g.rows * ld_part)))
+    return rc;
   if (e.kind < NS_OUT)
     rc = box_map(&m.out[0], e.out.p, MAP_F16, g.cols, g.rows, (long long)e.np * s.batch, e.out.ld, e.out.mat);
   else if (e.box)
@@ -530,7 +523,7 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
   if (rc || p.ks == 1) return rc;
   const long long blocks = (long long)s.batch * ((g.rows + 31) / 32) * ((g.cols + 31) / 32);
   return launch_chain(k_ns_join, "k_ns_join", (unsigned)((blocks + 3) / 4), 128, 0, 1, true, st, m.out[0], (const float*)part, p.ks,
-                      p.ld_part, g.sym, cut.tn, e);
+                      ld_part, g.sym, cut.tn, e);
 }
 
 template <typename T, bool MOM>

@@ -89,76 +89,65 @@ __device__ __forceinline__ void activate32(int act, float (&v)[32]) {
 }
 
 // 32 x 32 sums, a lane a row, through the epilogue and out by way of the box.  Rows of y, z and residual are whole 16-byte
-// pieces; what is past their ends is not stored.  first: nothing of this tile has left yet.  Values of 16 bits use the
-// halves of the box in turn (z and y, or y of every other block), so that a store is waited for one later.
+// pieces; what is past their ends is not stored.
 template <typename T, typename Get>
 __device__ __forceinline__ void store_box(const Finish& f, int rows, int row0, int col, int c, uint8_t* box,
                                           const CUtensorMap* out, Get get) {
   const int lane = threadIdx.x & 31;
   const int n = f.F - col;
-  constexpr int N = sizeof(T) == 2 ? 4 : 8;
+  constexpr int N = sizeof(T) == 2 ? 1 : 2;  // boxes
   const float own = f.bias && lane < n ? __ldg(f.bias + col + lane) : 0.f;
-  Rows32<N> res;
-  if (f.res)
-    res.load(reinterpret_cast<const T*>(f.res) + (long long)row0 * f.ldr + col, f.ldr * (long long)sizeof(T), rows,
-             n * (int)sizeof(T), lane);
+  Rows32 res[N];
+  if (f.res) {
+    const char* from = reinterpret_cast<const char*>(reinterpret_cast<const T*>(f.res) + (long long)row0 * f.ldr + col);
+#pragma unroll
+    for (int h = 0; h < N; ++h)
+      res[h].load(from + 64 * h, f.ldr * (long long)sizeof(T), rows, n * (int)sizeof(T) - 64 * h, lane);
+  }
   float v[32];
   get(c, v);
   if (f.bias) {
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, own, j);
   }
-  auto put = [&](uint8_t* to) {
-    if (sizeof(T) == 2)
-      box_put_16(to, lane, [&](int j) { return pack_bf16(v[j], v[j + 1]); });
-    else
-      box_put(to, lane, v);
-  };
-  auto store = [&](const CUtensorMap* map, const uint8_t* from) {
-    box_full();
-    if (lane == 0) {
-      store_3d(map, from, col, row0, 0);
-      bulk_commit();
+  auto put = [&](const CUtensorMap* map) {
+    if (sizeof(T) == 4) {
+      store_32(map, box, lane, v, n, col, row0, 0);
+      return;
     }
+    box_free(lane);
+    box_put_16(box, lane, [&](int j) { return pack_bf16(v[j], v[j + 1]); });
+    box_store(map, box, lane, col, row0, 0);
   };
-  auto free = [&] {
-    if (sizeof(T) == 4 || c == 0)
-      box_free<0>(lane);
-    else
-      box_free<1>(lane);
-  };
-  if (f.z) {
-    free();
-    put(box);
-    store(&out[1], box);
-  }
+  if (f.z) put(&out[1]);
   activate32(f.act, v);
-  uint8_t* to = box + (sizeof(T) == 2 && (f.z || c % 2) ? HALF_BOX : 0);
-  if (!(f.z && sizeof(T) == 2 && c == 0)) free();  // the first tile's second half: the first wait was for it too
   if (f.res) {
-    res.turn(to, lane);
+    box_free(lane);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const uint32_t w[4] = {res.q[j].x, res.q[j].y, res.q[j].z, res.q[j].w};
+    for (int h = 0; h < N; ++h) {
+      res[h].turn(box, lane);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (sizeof(T) == 2) {
-          v[8 * j + 2 * e] += __uint_as_float(w[e] << 16);
-          v[8 * j + 2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
-        } else {
-          v[(4 * j + e) % 32] += __uint_as_float(w[e]);
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w[4] = {res[h].q[j].x, res[h].q[j].y, res[h].q[j].z, res[h].q[j].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (sizeof(T) == 2) {
+            v[8 * j + 2 * e] += __uint_as_float(w[e] << 16);
+            v[8 * j + 2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
+          } else {
+            v[16 * h + 4 * j + e] += __uint_as_float(w[e]);
+          }
         }
       }
     }
   }
-  put(to);
-  store(&out[0], to);
+  put(&out[0]);
 }
 
-// A warp's part of a tile: rows row0 .. of T, columns col0 ..; to `part` (rows of fp32 sums, ld apart) where the sum
-// is one of several ranges, else through the epilogue.
+// A warp's part of a tile: rows row0 .. of T, columns col0 ..; to plane `range` of the fp32 sums that `part` maps where the sum is
+// one of several ranges (range >= 0), else through the epilogue.
 template <int NC, typename Get>
-__device__ __forceinline__ void store_rows(const Finish& f, long long T, float* part, int ld_part, int row0, int col0,
+__device__ __forceinline__ void store_rows(const Finish& f, long long T, int range, const CUtensorMap* part, int row0, int col0,
                                            uint8_t* box, const CUtensorMap* out, Get get) {
   const int lane = threadIdx.x & 31;
   const int rows = (int)min(T - row0, 32LL);
@@ -166,7 +155,8 @@ __device__ __forceinline__ void store_rows(const Finish& f, long long T, float* 
   for (int c = 0; c < NC; ++c) {
     const int col = col0 + c * 32;
     __syncwarp();
-    if (f.box && !part && rows > 0 && col < f.F) {
+    const bool any = rows > 0 && col < f.F;
+    if (f.box && range < 0 && any) {
       if (f.bf16)
         store_box<__nv_bfloat16>(f, rows, row0, col, c, box, out, get);
       else
@@ -175,32 +165,27 @@ __device__ __forceinline__ void store_rows(const Finish& f, long long T, float* 
     }
     float v[32];
     get(c, v);
-    if (rows <= 0 || col >= f.F) continue;
-    if (part) {
-      box_put(box, lane, v);
-      __syncwarp();
-      float* to = part + (size_t)row0 * ld_part + col;
-      by_fours(box, lane, [&](int r, int j, float4 s) {
-        if (r < rows && col + j < f.F) *reinterpret_cast<float4*>(to + (size_t)r * ld_part + j) = s;
-      });
+    if (!any) continue;
+    if (range >= 0) {
+      store_32(part, box, lane, v, f.F - col, col, row0, range);
     } else {
-      box_put(box, lane, v);
-      __syncwarp();
-      by_rows<1>(box, lane, col + lane < f.F ? rows : 0, [&](int r, float s) {
+      by_rows(box, lane, v, rows, f.F - col, [&](int r, int j, float s) {
         if (f.bf16)
-          f.one<__nv_bfloat16>(row0 + r, col + lane, s);
+          f.one<__nv_bfloat16>(row0 + r, col + j, s);
         else
-          f.one<float>(row0 + r, col + lane, s);
+          f.one<float>(row0 + r, col + j, s);
       });
     }
   }
 }
 
-// Maps of y and z, where their rows and the residual's are whole 16-byte pieces: a store by TMA writes no less.
-inline int finish_maps(Finish* f, long long T, Maps* m) {
+// Maps of y and z, where their rows and the residual's are whole 16-byte pieces (a store by TMA writes no less), and in the
+// place of y's of `ks` ranges' sums.
+inline int finish_maps(Finish* f, long long T, float* part, int ks, int ld_part, Maps* m) {
   const int e = f->bf16 ? 2 : 4;
   f->box = f->F * e % 16 == 0 && rowwise::rows_16(f->y, f->ldy, e) && rowwise::rows_16(f->z, f->ldz, e) && rowwise::rows_16(f->res, f->ldr, e);
-  m->out[0] = m->out[1] = m->a[0];
+  m->out[0] = m->out[1] = m->a_turned = m->b_turned = m->a[0];
+  if (ks > 1) return box_map(&m->out[0], part, MAP_F32, ld_part, T, ks, ld_part, T * ld_part);
   if (!f->box) return GC_OK;
   const MapType t = f->bf16 ? MAP_BF16 : MAP_F32;
   int rc = box_map(&m->out[0], f->y, t, f->F, T, 1, f->ldy, T * f->ldy);

@@ -2,7 +2,7 @@
 // tiles that an operator `Op` lists (which operands, which range of K) and hands each finished tile to its epilogue.
 //
 // A pair of CTAs (cta_group::2) takes a 256 x TN tile, TN = 256 or 128, each CTA holding 128 rows of A and TN / 2
-// of B for a 64-wide K block: warp 0 loads them by TMA, the leader's warp 1 issues the MMAs, eight warps per CTA
+// of B for a 64-wide K block: warp 0 loads them by TMA, the leader's warp 1 issues the MMAs, sixteen warps per CTA
 // drain one of two accumulators while the other is filled.  Operands lie K-major (rows of K, K innermost) or MN-major (K
 // outermost: boxes of 64 columns x 64 K rows).  A value enters in up to three 16-bit parts (x = x0 + x1 + ..., each
 // the rounded rest of those before), and the products of parts i and j with i + j < lim are summed: bf16 parts of an
@@ -28,9 +28,9 @@ using namespace tcp;
 
 constexpr int TM = 256, BK = 64;
 constexpr int A_BYTES = 128 * BK * 2;  // a CTA's share of a part of A's K block
-constexpr int kEpi = 8;
+constexpr int kEpi = 16;               // a quarter of the rows and of the columns each
 constexpr int kThreads = 64 + 32 * kEpi;
-constexpr int BOX = 32 * 128;          // an epilogue warp's box: 32 rows of 128 bytes
+constexpr int BOX = 32 * 64;           // an epilogue warp's box: 32 rows of 64 bytes
 constexpr int RING = 12 * A_BYTES;
 constexpr int kMaxStages = 8;
 constexpr size_t kSmem = RING + kEpi * BOX + 1024 + 256;
@@ -43,7 +43,11 @@ struct Job {
   int na, nb, lim;      // parts of A and of B; products of parts i + j < lim
   int seg;              // K blocks that are summed in tensor memory at a time
   bool a_mn, b_mn;
+  int a_turn, b_turn;   // K blocks from which a symmetric operand's are read as their mirrors below the diagonal (kNever)
 };
+constexpr int kNever = 1 << 30;
+// ... where of rows `row` .. the blocks of 256 up to the diagonal exist.
+__device__ __forceinline__ int turn_of(int row) { return (row / TM + 1) * (TM / BK); }
 
 // What every operator's parameters hold.
 struct Common {
@@ -57,7 +61,7 @@ struct Common {
 
 // Tensor maps of (inner, rows, batch, part) by kind, and the epilogue's.
 struct Maps {
-  CUtensorMap a[2], b[2], out[2];
+  CUtensorMap a[2], b[2], out[2], a_turned, b_turned;
 };
 
 __device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -69,63 +73,61 @@ __device__ __forceinline__ uint32_t idesc_of(int tn, bool f16, bool a_mn, bool b
          ((uint32_t)(tn >> 3) << 17) | ((256u >> 4) << 24);
 }
 
-// An epilogue warp's 32 x 32 values go through a box: lane = row on the way in, 16-byte piece j of row r at j ^ (r mod
-// 8), so that rows, 4-column groups and columns are all read without many bank conflicts.
-__device__ __forceinline__ void box_put(uint8_t* box, int lane, const float (&v)[32]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    *reinterpret_cast<float4*>(box + lane * 128 + ((j ^ (lane & 7)) * 16)) =
-        make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+// An epilogue warp's 32 x 32 values go through its box, a lane a row: 32 columns of 16 bits or 16 of 32 bits at a time.  Piece j
+// (16 bytes) of row r lies at j ^ (r / 2 mod 4), TMA's 64-byte swizzle, so that rows and pieces are written and read without
+// bank conflicts.
+__device__ __forceinline__ int box_place(int r, int j) { return r * 64 + (j ^ ((r >> 1) & 3)) * 16; }
+
+// Before a box is written: the stores that lane 0 issued from it have read it.
+__device__ __forceinline__ void box_free(int lane) {
+  if (lane == 0) bulk_wait_read<0>();
+  __syncwarp();
 }
-__device__ __forceinline__ float box_at(const uint8_t* box, int r, int c) {
-  return *reinterpret_cast<const float*>(box + r * 128 + (((c / 4) ^ (r & 7)) * 16) + c % 4 * 4);
-}
-// f(r, c, four values): columns c .. c + 3 of row r, eight neighbouring lanes a row, four rows at a time.
-template <typename F>
-__device__ __forceinline__ void by_fours(const uint8_t* box, int lane, F f) {
-  const int j = lane & 7;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = i * 4 + (lane >> 3);
-    f(r, 4 * j, *reinterpret_cast<const float4*>(box + r * 128 + ((j ^ (r & 7)) * 16)));
-  }
-}
-// Boxes that leave by TMA.  32 x 32 values of 16 bits take half a box, rows of 64 bytes: piece j of row r at j ^ (r / 2 mod 4).
-constexpr int HALF_BOX = BOX / 2;
+// two(j): values j and j + 1 as a packed pair.
 template <typename Pack>
-__device__ __forceinline__ void box_put_16(uint8_t* half, int lane, Pack two) {
+__device__ __forceinline__ void box_put_16(uint8_t* box, int lane, Pack two) {
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    *reinterpret_cast<uint4*>(half + lane * 64 + ((j ^ ((lane >> 1) & 3)) * 16)) =
-        make_uint4(two(8 * j), two(8 * j + 2), two(8 * j + 4), two(8 * j + 6));
+    *reinterpret_cast<uint4*>(box + box_place(lane, j)) = make_uint4(two(8 * j), two(8 * j + 2), two(8 * j + 4), two(8 * j + 6));
+}
+__device__ __forceinline__ void box_put_32(uint8_t* box, int lane, const float* v) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *reinterpret_cast<float4*>(box + box_place(lane, j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&t);
 }
-// Before a box is written: the stores that lane 0 issued from it, all but the newest N of the warp's, have read it.
-template <int N>
-__device__ __forceinline__ void box_free(int lane) {
-  if (lane == 0) bulk_wait_read<N>();
-  __syncwarp();
-}
-// After: what the warp wrote is seen by the store that lane 0 issues next.
-__device__ __forceinline__ void box_full() {
+// The box leaves for (col, row, plane).
+__device__ __forceinline__ void box_store(const CUtensorMap* map, const uint8_t* box, int lane, int col, int row, int plane) {
   fence_async_smem();
   __syncwarp();
+  if (lane == 0) {
+    store_3d(map, box, col, row, plane);
+    bulk_commit();
+  }
 }
-// 32 rows of 4 N 32-bit words (N = 4: 64 bytes, N = 8: 128) from memory, neighbouring lanes a row; they reach a lane a row by
-// way of the box, in whose order of pieces they are put there.
-template <int N>
+// 32 x 32 values of 32 bits, of which the first n columns exist.
+__device__ __forceinline__ void store_32(const CUtensorMap* map, uint8_t* box, int lane, const float (&v)[32], int n, int col, int row,
+                                         int plane) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (16 * h >= n) break;
+    box_free(lane);
+    box_put_32(box, lane, v + 16 * h);
+    box_store(map, box, lane, col + 16 * h, row, plane);
+  }
+}
+// 32 rows of 64 bytes from memory, four neighbouring lanes a row; they reach a lane a row by way of the box.
 struct Rows32 {
-  uint4 q[N];
-  static __device__ __forceinline__ int place(int r, int j) { return r * N * 16 + (N == 8 ? j ^ (r & 7) : j ^ ((r >> 1) & 3)) * 16; }
+  uint4 q[4];
   // the first `rows` rows, `ld` bytes apart, of which `bytes` exist, a multiple of 16
   __device__ __forceinline__ void load(const void* from, long long ld, int rows, int bytes, int lane) {
-    const int j = lane % N;
+    const int j = lane % 4;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int r = i * (32 / N) + lane / N;
+    for (int i = 0; i < 4; ++i) {
+      const int r = i * 8 + lane / 4;
       q[i] = r < rows && j * 16 < bytes ? __ldcg(reinterpret_cast<const uint4*>(static_cast<const char*>(from) + r * ld + j * 16))
                                         : make_uint4(0, 0, 0, 0);
     }
@@ -133,27 +135,35 @@ struct Rows32 {
   // ... as the lane's own row.  The box is free before; the lane may write its own row after.
   __device__ __forceinline__ void turn(uint8_t* box, int lane) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(box + place(i * (32 / N) + lane / N, lane % N)) = q[i];
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(box + box_place(i * 8 + lane / 4, lane % 4)) = q[i];
     __syncwarp();
 #pragma unroll
-    for (int j = 0; j < N; ++j) q[j] = *reinterpret_cast<const uint4*>(box + place(lane, j));
+    for (int j = 0; j < 4; ++j) q[j] = *reinterpret_cast<const uint4*>(box + box_place(lane, j));
     __syncwarp();
   }
 };
-// f(r, value): rows r = 0 .. rows - 1, a lane a column, for rows on no boundary.
-template <int U, typename F>
-__device__ __forceinline__ void by_rows(const uint8_t* box, int lane, int rows, F f) {
-#pragma unroll(U)
-  for (int r = 0; r < 32; ++r) {
-    const float x = box_at(box, r, lane);
-    if (r < rows) f(r, x);
+// f(r, c, value) for the first `rows` rows and `n` columns, 16 neighbouring lanes a row: for rows on no boundary.
+template <typename F>
+__device__ __forceinline__ void by_rows(uint8_t* box, int lane, const float (&v)[32], int rows, int n, F f) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int c = 16 * h + lane % 16;
+    __syncwarp();
+    box_put_32(box, lane, v + 16 * h);
+    __syncwarp();
+#pragma unroll 2
+    for (int r = lane / 16; r < rows; r += 2) {
+      const float x = *reinterpret_cast<const float*>(box + box_place(r, c % 16 / 4) + c % 4 * 4);
+      if (c < n) f(r, c, x);
+    }
   }
 }
 
 template <class Op, int TN>
 __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ Maps maps,
                                                         const __grid_constant__ typename Op::Params p) {
-  constexpr int HN = TN / 2;             // columns of an epilogue warp, and B rows of a CTA
+  constexpr int HN = TN / 2;             // B rows of a CTA
+  constexpr int QN = TN / 4;             // columns of an epilogue warp
   constexpr int B_BYTES = HN * BK * 2;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -204,22 +214,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
     for (int k = 0; k < njobs && ok; ++k) {
       const Job t = Op::job(p, unit, k);
       const int ma = t.m0 + side * 128, nb = t.n0 + side * HN;
-      const bool skip_a = !t.a_mn && side == 1 && !q.a_both;
-      const uint32_t bytes = 2 * t.nb * B_BYTES +
-                             (t.a_mn ? 2 * t.na * A_BYTES : t.na * q.a_rows * BK * 2 * (q.a_both ? 2 : 1));
-      const CUtensorMap *mA = &maps.a[t.kind], *mB = &maps.b[t.kind];
       for (int kb = t.kb0; kb < t.kb0 + t.nkb; ++kb, ++it) {
         if (!mbar_wait(&empty[s], ph ^ 1, abort_flag, q.status, q.spin_limit)) ok = false;
         if (!__all_sync(0xffffffffu, ok)) {
           ok = false;
           break;
         }
+        const bool a_mn = t.a_mn || kb >= t.a_turn, b_mn = t.b_mn || kb >= t.b_turn;
+        const bool skip_a = !a_mn && side == 1 && !q.a_both;
+        const CUtensorMap* mA = kb >= t.a_turn ? &maps.a_turned : &maps.a[t.kind];
+        const CUtensorMap* mB = kb >= t.b_turn ? &maps.b_turned : &maps.b[t.kind];
         if (one) {
+          const uint32_t bytes = 2 * t.nb * B_BYTES +
+                                 (a_mn ? 2 * t.na * A_BYTES : t.na * q.a_rows * BK * 2 * (q.a_both ? 2 : 1));
           if (side == 0) mbar_expect_tx(&full[s], bytes);
           const uint32_t bar = at_rank(&full[s], 0);
           uint8_t* st = smem + (size_t)s * q.stage_bytes;
           for (int i = 0; i < t.na; ++i, st += A_BYTES) {
-            if (t.a_mn) {
+            if (a_mn) {
               load_4d(st, mA, ma, kb * BK, t.b, i, bar);
               load_4d(st + A_BYTES / 2, mA, ma + 64, kb * BK, t.b, i, bar);
             } else if (!skip_a) {
@@ -227,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
             }
           }
           for (int i = 0; i < t.nb; ++i, st += B_BYTES) {
-            if (t.b_mn) {
+            if (b_mn) {
               load_4d(st, mB, nb, kb * BK, t.b, i, bar);
               if (TN == 256) load_4d(st + B_BYTES / 2, mB, nb + 64, kb * BK, t.b, i, bar);
             } else {
@@ -258,10 +270,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
       bool ok = true;
       for (int k = 0; k < njobs && ok; ++k) {
         const Job t = Op::job(p, unit, k);
-        const uint32_t idesc = idesc_of(TN, q.f16, t.a_mn, t.b_mn);
-        const uint32_t a_step = (t.a_mn ? 2048 : 32) >> 4, b_step = (t.b_mn ? 2048 : 32) >> 4;
-        const uint64_t da0 = sdesc(smem_u32(smem), t.a_mn ? A_BYTES / 2 : 16, 1024);
-        const uint64_t db0 = sdesc(smem_u32(smem) + t.na * A_BYTES, t.b_mn ? (TN == 256 ? B_BYTES / 2 : B_BYTES) : 16, 1024);
         for (int kb = 0, left = 0; kb < t.nkb; ++kb) {
           const int ab = use & 1;
           if (left == 0) {
@@ -275,6 +283,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
           }
           const bool opens = left == t.seg, closes = --left == 0 || kb == t.nkb - 1;
           if (opens) fence_after();
+          const bool a_mn = t.a_mn || t.kb0 + kb >= t.a_turn, b_mn = t.b_mn || t.kb0 + kb >= t.b_turn;
+          const uint32_t idesc = idesc_of(TN, q.f16, a_mn, b_mn);
+          const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
+          const uint64_t da0 = sdesc(smem_u32(smem), a_mn ? A_BYTES / 2 : 16, 1024);
+          const uint64_t db0 = sdesc(smem_u32(smem) + t.na * A_BYTES, b_mn ? (TN == 256 ? B_BYTES / 2 : B_BYTES) : 16, 1024);
           if (one) {
             const uint32_t d = tmem_base + (uint32_t)(ab * TN);
             // the descriptors of the stage: only the address, in 16-byte units, differs
@@ -312,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
       __syncwarp();
     }
   } else {
-    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const int quarter = warp & 3, part = (warp - 2) >> 2;
     uint8_t* box = boxes + (warp - 2) * BOX;
     uint32_t use = 0;
     bool ok = true;
@@ -328,34 +341,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
       if (lane == 0) arrive_remote(at_rank(&tempty[use & 1], 0));
     };
     auto at = [&] {
-      return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((use & 1) * TN + half * HN);
+      return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((use & 1) * TN + part * QN);
     };
     for (int k = 0; k < njobs && ok; ++k) {
       const Job t = Op::job(p, unit, k);
-      const int row0 = t.m0 + side * 128 + quarter * 32, col0 = t.n0 + half * HN;  // the warp's
+      const int row0 = t.m0 + side * 128 + quarter * 32, col0 = t.n0 + part * QN;  // the warp's
       if (t.nkb > t.seg) {
         // the sum of the segments, back into the last one's place
-        float sum[HN];
+        float sum[QN];
 #pragma unroll
-        for (int j = 0; j < HN; ++j) sum[j] = 0.f;
+        for (int j = 0; j < QN; ++j) sum[j] = 0.f;
         for (int left = t.nkb; filled(); left -= t.seg, ++use) {
 #pragma unroll
-          for (int j = 0; j < HN; j += 16) tmem_add16(at() + (uint32_t)j, sum + j);
+          for (int j = 0; j < QN; j += 16) tmem_add16(at() + (uint32_t)j, sum + j);
           if (left <= t.seg) break;
           release();
         }
         if (!ok) break;
 #pragma unroll
-        for (int j = 0; j < HN; j += 16) tmem_st16(at() + (uint32_t)j, sum + j);
+        for (int j = 0; j < QN; j += 16) tmem_st16(at() + (uint32_t)j, sum + j);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       } else if (!filled()) {
         break;
       }
       auto get = [&](int c, float (&v)[32]) {  // the accumulator is handed back when the last of it is in registers
         tmem_ld32(at() + (uint32_t)(c * 32), v);
-        if (c == HN / 32 - 1) release();
+        if (c == QN / 32 - 1) release();
       };
-      Op::template store<HN / 32>(p, t, row0, col0, box, maps.out, get);
+      Op::template store<QN / 32>(p, t, row0, col0, box, maps.out, get);
       ++use;
     }
     if (lane == 0) bulk_wait_all();
@@ -423,11 +436,11 @@ inline int operand_map(CUtensorMap* map, const void* base, bool f16, long long i
   return map_nd(map, base, 4, d, l, box_rows, 1, f16 ? MAP_F16 : MAP_BF16);
 }
 
-// Map of a result that leaves in boxes of 32 x 32: cols x rows x batch of 16- or 32-bit values.
+// Map of a result that leaves in boxes: cols x rows x batch of 16- or 32-bit values.
 inline int box_map(CUtensorMap* map, const void* base, MapType type, long long cols, long long rows, long long batch, long long ld,
                    long long ld_b) {
   const long long d[3] = {cols, rows, batch}, l[2] = {ld, ld_b};
-  return map_nd(map, base, 3, d, l, 32, 1, type, type != MAP_F32);
+  return map_nd(map, base, 3, d, l, 32, 1, type, true);
 }
 
 // Pairs that the current device holds at once.
