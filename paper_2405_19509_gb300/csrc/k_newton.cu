@@ -164,6 +164,7 @@ __host__ __device__ inline int sym_tiles(int rows, int tn) {
 }
 
 struct NsOp {
+  static constexpr bool kTurns = true;
   struct Params {
     Common q;
     Epilogue e;

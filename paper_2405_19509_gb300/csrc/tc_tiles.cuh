@@ -159,6 +159,21 @@ __device__ __forceinline__ void by_rows(uint8_t* box, int lane, const float (&v)
   }
 }
 
+// How a K block's operands lie: descriptors of the first stage's, their steps of 16 K, and the instruction's.
+template <int TN>
+struct Way {
+  uint32_t idesc, a_step, b_step;
+  uint64_t a, b;
+  __device__ __forceinline__ Way(const Common& q, const Job& t, const uint8_t* smem, bool a_mn, bool b_mn) {
+    constexpr int B_BYTES = TN / 2 * BK * 2;
+    idesc = idesc_of(TN, q.f16, a_mn, b_mn);
+    a_step = (a_mn ? 2048 : 32) >> 4;
+    b_step = (b_mn ? 2048 : 32) >> 4;
+    a = sdesc(smem_u32(smem), a_mn ? A_BYTES / 2 : 16, 1024);
+    b = sdesc(smem_u32(smem) + t.na * A_BYTES, b_mn ? (TN == 256 ? B_BYTES / 2 : B_BYTES) : 16, 1024);
+  }
+};
+
 template <class Op, int TN>
 __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ Maps maps,
                                                         const __grid_constant__ typename Op::Params p) {
@@ -220,10 +235,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
           ok = false;
           break;
         }
-        const bool a_mn = t.a_mn || kb >= t.a_turn, b_mn = t.b_mn || kb >= t.b_turn;
+        const bool a_turned = Op::kTurns && kb >= t.a_turn, b_turned = Op::kTurns && kb >= t.b_turn;
+        const bool a_mn = t.a_mn || a_turned, b_mn = t.b_mn || b_turned;
         const bool skip_a = !a_mn && side == 1 && !q.a_both;
-        const CUtensorMap* mA = kb >= t.a_turn ? &maps.a_turned : &maps.a[t.kind];
-        const CUtensorMap* mB = kb >= t.b_turn ? &maps.b_turned : &maps.b[t.kind];
+        const CUtensorMap* mA = a_turned ? &maps.a_turned : &maps.a[t.kind];
+        const CUtensorMap* mB = b_turned ? &maps.b_turned : &maps.b[t.kind];
         if (one) {
           const uint32_t bytes = 2 * t.nb * B_BYTES +
                                  (a_mn ? 2 * t.na * A_BYTES : t.na * q.a_rows * BK * 2 * (q.a_both ? 2 : 1));
@@ -270,6 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
       bool ok = true;
       for (int k = 0; k < njobs && ok; ++k) {
         const Job t = Op::job(p, unit, k);
+        Way<TN> way(q, t, smem, t.a_mn, t.b_mn);
         for (int kb = 0, left = 0; kb < t.nkb; ++kb) {
           const int ab = use & 1;
           if (left == 0) {
@@ -283,23 +300,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
           }
           const bool opens = left == t.seg, closes = --left == 0 || kb == t.nkb - 1;
           if (opens) fence_after();
-          const bool a_mn = t.a_mn || t.kb0 + kb >= t.a_turn, b_mn = t.b_mn || t.kb0 + kb >= t.b_turn;
-          const uint32_t idesc = idesc_of(TN, q.f16, a_mn, b_mn);
-          const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
-          const uint64_t da0 = sdesc(smem_u32(smem), a_mn ? A_BYTES / 2 : 16, 1024);
-          const uint64_t db0 = sdesc(smem_u32(smem) + t.na * A_BYTES, b_mn ? (TN == 256 ? B_BYTES / 2 : B_BYTES) : 16, 1024);
+          if (Op::kTurns)
+            way = Way<TN>(q, t, smem, t.a_mn || t.kb0 + kb >= t.a_turn, t.b_mn || t.kb0 + kb >= t.b_turn);
           if (one) {
             const uint32_t d = tmem_base + (uint32_t)(ab * TN);
             // the descriptors of the stage: only the address, in 16-byte units, differs
             const uint64_t at = (uint64_t)((uint32_t)s * (uint32_t)q.stage_bytes >> 4);
-            uint64_t da = da0 + at;
+            uint64_t da = way.a + at;
             uint32_t more = opens ? 0u : 1u;
             for (int i = 0; i < t.na; ++i, da += A_BYTES >> 4) {
-              uint64_t db = db0 + at;
+              uint64_t db = way.b + at;
               for (int j = 0; j < t.nb && i + j < t.lim; ++j, db += B_BYTES >> 4) {
 #pragma unroll
                 for (int ks = 0; ks < BK / 16; ++ks) {
-                  mma(d, da + (uint64_t)(ks * a_step), db + (uint64_t)(ks * b_step), idesc, more);
+                  mma(d, da + (uint64_t)(ks * way.a_step), db + (uint64_t)(ks * way.b_step), way.idesc, more);
                   more = 1u;
                 }
               }
