@@ -1,6 +1,6 @@
 // Gradient of a linear layer with its activation: d = dy act'(z), dx = d W, and per chunk of n_c points G_i = d_i^T x_i
 // (F x C) and Gb_i = sum_t d_t.
-//   k_linear_d       d as bf16 parts, and its column sums over 64 points at a time; k_linear_gb joins them
+//   k_linear_d       d as bf16 parts, and its column sums over 128 points at a time; k_linear_gb joins them
 //   k_tiles<GradOp>  dx and all chunks' G in one launch
 //   k_linear_join    dx where its tiles' sum over F runs in ranges
 //
@@ -17,9 +17,9 @@ using namespace tiles;
 using namespace linear;
 using namespace rowwise;
 
-constexpr int kRowsD = 64;  // points of a block of k_linear_d
+constexpr int kRowsD = 128;  // points of a block of k_linear_d
 
-// A block: 256 columns of 64 points of a chunk, a warp eight rows, four loads ahead.
+// A block: 256 columns of 128 points of a chunk, a warp every eighth row, the next one's loads ahead.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256)
     k_linear_d(const T* __restrict__ dy, long long lddy, const T* __restrict__ z, long long ldz, int act, int N, int n_c,
@@ -37,16 +37,20 @@ __global__ void __launch_bounds__(256)
   float sum[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-#pragma unroll 4
+  RawSeg<VEC, T> next_d, next_z;  // of the warp's next row
+  auto take = [&](int r) {
+    next_d.load(dy + (first + r) * lddy, col0, lane, F);
+    if (act != GC_ACT_NONE) next_z.load(z + (first + r) * ldz, col0, lane, F);
+  };
+  if (warp < rows) take(warp);
+#pragma unroll 1
   for (int r = warp; r < rows; r += 8) {
     const long long row = first + r;
-    float v[8];
-    load_seg<VEC>(dy + row * lddy, col0, lane, F, v);
-    if (act != GC_ACT_NONE) {
-      float u[8];
-      load_seg<VEC>(z + row * ldz, col0, lane, F, u);
-      times_slope(act, u, v);
-    }
+    float v[8], u[8];
+    next_d.values(v);
+    if (act != GC_ACT_NONE) next_z.values(u);
+    if (r + 8 < rows) take(r + 8);
+    if (act != GC_ACT_NONE) times_slope(act, u, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (!in_row<VEC>(col0, lane, j, F)) v[j] = 0.f;  // relu' of a zero that stands for nothing is one, NaN or not
