@@ -21,24 +21,26 @@ struct FwdOp {
     Finish f;
     long long T;
     int mt, nt, tn, group;  // tiles of T and of F; row tiles that share a sweep of the columns
-    int nkb, ks, seg;       // K blocks, in ks ranges
+    Divisor per, full, rest;  // tiles of a group of rows; its row tiles, and those of the last group
+    Ranges k;
+    int seg;
     int nx, nw, lim;
   };
   static __device__ __forceinline__ int jobs(const Params& p, int unit) {
-    return (int)(((long long)p.mt * p.nt * p.ks - unit + p.q.units - 1) / p.q.units);
+    return (int)(((long long)p.mt * p.nt * p.k.ks - unit + p.q.units - 1) / p.q.units);
   }
   static __device__ __forceinline__ Job job(const Params& p, int unit, int k) {
-    const int i = unit + k * p.q.units, at = i / p.ks;
-    const int per = p.group * p.nt, g = at / per, rem = at - g * per;
-    const int gm = min(p.group, p.mt - g * p.group);
-    const int n = rem / gm;
+    const int i = unit + k * p.q.units, at = p.k.by.of(i);
+    const int g = p.per.of(at), rem = at - g * (int)p.per.d;
+    const bool last = (g + 1) * p.group > p.mt;
+    const int n = last ? p.rest.of(rem) : p.full.of(rem);
     Job t;
     t.kind = t.b = 0;
-    t.range = i - at * p.ks;
-    t.m0 = (g * p.group + rem - n * gm) * TM;
+    t.range = i - at * p.k.ks;
+    t.m0 = (g * p.group + rem - n * (int)(last ? p.rest.d : p.full.d)) * TM;
     t.n0 = n * p.tn;
-    t.kb0 = (int)((long long)t.range * p.nkb / p.ks);
-    t.nkb = (int)((long long)(t.range + 1) * p.nkb / p.ks) - t.kb0;
+    t.kb0 = p.k.first(t.range);
+    t.nkb = p.k.count(t.range);
     t.na = p.nx;
     t.nb = p.nw;
     t.lim = p.lim;
@@ -50,7 +52,7 @@ struct FwdOp {
   template <int NC, typename Get>
   static __device__ __forceinline__ void store(const Params& p, const Job& t, int row0, int col0, uint8_t* box,
                                                const CUtensorMap* out, Get get) {
-    store_rows<NC>(p.f, p.T, p.ks > 1 ? t.range : -1, out, row0, col0, box, out, get);
+    store_rows<NC>(p.f, p.T, p.k.ks > 1 ? t.range : -1, out, row0, col0, box, out, get);
   }
 };
 
@@ -113,12 +115,15 @@ int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t*
   p.mt = tiles_of(s.T, TM);
   p.nt = tiles_of(s.F, w.tn);
   p.group = std::min(p.mt, 16);
-  p.nkb = (s.C + BK - 1) / BK;
-  p.ks = w.ks;
+  p.per = Divisor((uint32_t)(p.group * p.nt));
+  p.full = Divisor((uint32_t)p.group);
+  p.rest = Divisor((uint32_t)(p.mt % p.group ? p.mt % p.group : p.group));
+  const int nkb = (s.C + BK - 1) / BK;
+  p.k = Ranges(nkb, w.ks);
   p.nx = w.nx;
   p.nw = w.nw;
   p.lim = w.lim;
-  p.seg = segment(xb, products(w.nx, w.nw, w.lim), p.nkb);
+  p.seg = segment(xb, products(w.nx, w.nw, w.lim), nkb);
   p.q.a_both = s.T > 128;
   p.q.a_rows = s.T > 128 ? 128 : (int)(s.T + 7) / 8 * 8;
   p.q.spin_limit = wait_limit(kSpin);
@@ -131,7 +136,7 @@ int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t*
   m.a[1] = m.a[0];
   m.b[1] = m.b[0];
   if ((rc = finish_maps(&p.f, s.T, w.part, w.ks, w.ld_part, &m))) return rc;
-  const long long jobs = (long long)p.mt * p.nt * p.ks;
+  const long long jobs = (long long)p.mt * p.nt * w.ks;
   rc = w.tn == 256 ? launch_tiles<FwdOp, 256>(m, p, jobs, w.nx, w.nw, "k_linear", chained, st)
                    : launch_tiles<FwdOp, 128>(m, p, jobs, w.nx, w.nw, "k_linear", chained, st);
   if (rc || w.ks == 1) return rc;

@@ -105,9 +105,11 @@ struct GradOp {
     long long T;
     int C, F, N;
     int tn, mt, ct, ft;    // tiles of T, of C and of F
-    int ndx, ng, r, extra; // dx tiles, round robin; then G's, `extra` each for the units past the first r, which have
+    int ndx, dx_each, ng, r, extra; // dx tiles, round robin; then G's, `extra` each for the units past the first r, which have
                            // one dx tile less, and the rest round robin
-    int f_nkb, c_nkb, ks;  // K blocks of dx, in ks ranges, and of G
+    Ranges dx_k;           // K blocks of dx
+    int c_nkb;             // ... and of G
+    Divisor by_ct, by_chunk;  // column tiles; tiles of a chunk's G
     int np_dx, np, nx, nw, lim, seg_dx, seg_g;
     float* G;
     long long ldg;
@@ -123,16 +125,16 @@ struct GradOp {
     t.b_mn = true;
     t.a_turn = t.b_turn = kNever;
     t.lim = p.lim;
-    const int ndx = (p.ndx - unit + p.q.units - 1) / p.q.units;
+    const int ndx = p.dx_each + (unit < p.r ? 1 : 0);
     if (k < ndx) {
-      const int i = unit + k * p.q.units, at = i / p.ks;
+      const int i = unit + k * p.q.units, at = p.dx_k.by.of(i), m = p.by_ct.of(at);
       t.kind = t.b = 0;
       t.a_mn = false;
-      t.range = i - at * p.ks;
-      t.m0 = at / p.ct * TM;
-      t.n0 = at % p.ct * p.tn;
-      t.kb0 = (int)((long long)t.range * p.f_nkb / p.ks);
-      t.nkb = (int)((long long)(t.range + 1) * p.f_nkb / p.ks) - t.kb0;
+      t.range = i - at * p.dx_k.ks;
+      t.m0 = m * TM;
+      t.n0 = (at - m * p.ct) * p.tn;
+      t.kb0 = p.dx_k.first(t.range);
+      t.nkb = p.dx_k.count(t.range);
       t.na = p.np_dx;
       t.nb = p.nw;
       t.seg = p.seg_dx;
@@ -141,13 +143,13 @@ struct GradOp {
     k -= ndx;
     const int nb = p.q.units - p.r, mine = unit >= p.r ? p.extra : 0;
     const int i = k < mine ? k * nb + unit - p.r : p.extra * nb + (k - mine) * p.q.units + unit;
-    const int per = p.ft * p.ct, c = i / per, rem = i - c * per;
+    const int c = p.by_chunk.of(i), rem = i - c * (int)p.by_chunk.d, m = p.by_ct.of(rem);
     t.kind = 1;
     t.a_mn = true;
     t.range = t.kb0 = 0;
     t.b = c;
-    t.m0 = rem / p.ct * TM;
-    t.n0 = rem % p.ct * p.tn;
+    t.m0 = m * TM;
+    t.n0 = (rem - m * p.ct) * p.tn;
     t.nkb = p.c_nkb;
     t.na = p.np;
     t.nb = p.nx;
@@ -159,7 +161,7 @@ struct GradOp {
                                                const CUtensorMap* out, Get get) {
     const int lane = threadIdx.x & 31;
     if (t.kind == 0) {
-      store_rows<NC>(p.f, p.T, p.ks > 1 ? t.range : -1, out, row0, col0, box, out, get);
+      store_rows<NC>(p.f, p.T, p.dx_k.ks > 1 ? t.range : -1, out, row0, col0, box, out, get);
       box_free(lane);  // a tile of G may write the box otherwise
       return;
     }
@@ -292,26 +294,29 @@ int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& w
   p.mt = tiles_of(T, TM);
   p.ct = tiles_of(s.C, w.tn);
   p.ft = tiles_of(s.F, TM);
-  p.f_nkb = (s.F + BK - 1) / BK;
+  const int f_nkb = (s.F + BK - 1) / BK;
+  p.dx_k = Ranges(f_nkb, w.ks);
   p.c_nkb = (s.n_c + BK - 1) / BK;
-  p.ks = w.ks;
+  p.by_ct = Divisor((uint32_t)p.ct);
+  p.by_chunk = Divisor((uint32_t)(p.ft * p.ct));
   p.np_dx = w.np_dx;
   p.np = w.np;
   p.nx = w.nx;
   p.nw = w.nw;
   p.lim = w.lim;
   const int prod_dx = products(w.np_dx, w.nw, w.lim), prod_g = products(w.np, w.nx, w.lim);
-  p.seg_dx = segment(xb, prod_dx, p.f_nkb);
+  p.seg_dx = segment(xb, prod_dx, f_nkb);
   p.seg_g = segment(false, prod_g, p.c_nkb);
   p.G = io.G;
   p.ldg = io.ldg;
-  p.ndx = dx ? p.mt * p.ct * p.ks : 0;
+  p.ndx = dx ? p.mt * p.ct * w.ks : 0;
   p.ng = g ? s.N * p.ft * p.ct : 0;
   int units = 0;
   if ((rc = w.tn == 256 ? resident<GradOp, 256>(&units) : resident<GradOp, 128>(&units))) return rc;
   units = (int)std::min<long long>(units, (long long)p.ndx + p.ng);
   p.r = p.ndx % units;
-  const double cost_dx = (double)p.f_nkb / p.ks * prod_dx, cost_g = (double)p.c_nkb * prod_g;
+  p.dx_each = p.ndx / units;
+  const double cost_dx = (double)f_nkb / w.ks * prod_dx, cost_g = (double)p.c_nkb * prod_g;
   p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_g + 0.5), p.ng / (units - p.r));
   p.q.a_both = T > 128;
   p.q.a_rows = T > 128 ? 128 : (int)(T + 7) / 8 * 8;

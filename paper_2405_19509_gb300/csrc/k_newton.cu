@@ -169,33 +169,36 @@ struct NsOp {
     Common q;
     Epilogue e;
     int batch, mt, nt, per, tn, sym;  // tiles of rows, of columns, of a matrix
-    int nkb, ks, seg, na, nb, lim;
+    Ranges k;
+    Divisor by_per, by_nt;
+    int seg, na, nb, lim;
     int a_mn, b_mn;
     int a_sym, b_sym;                 // operands of which what is above the diagonal's blocks is not there
   };
   static __device__ __forceinline__ int jobs(const Params& p, int unit) {
-    return (int)(((long long)p.batch * p.per * p.ks - unit + p.q.units - 1) / p.q.units);
+    return (int)(((long long)p.batch * p.per * p.k.ks - unit + p.q.units - 1) / p.q.units);
   }
   static __device__ __forceinline__ Job job(const Params& p, int unit, int k) {
-    const int i = unit + k * p.q.units, at = i / p.ks;
+    const int i = unit + k * p.q.units, at = p.k.by.of(i);
     Job t;
     t.kind = 0;
-    t.range = i - at * p.ks;
-    t.b = at / p.per;
+    t.range = i - at * p.k.ks;
+    t.b = p.by_per.of(at);
     const int tile = at - t.b * p.per;
     if (p.sym) {
       const int w = TM / p.tn;  // row tile r begins at w r (r + 1) / 2
-      int r = (int)((sqrtf(8.f * (float)tile / (float)w + 1.f) - 1.f) * 0.5f);
+      int r = (int)((sqrtf(8.f / (float)w * (float)tile + 1.f) - 1.f) * 0.5f);
       while (w * r * (r + 1) / 2 > tile) --r;
       while (r + 1 < p.mt && w * (r + 1) * (r + 2) / 2 <= tile) ++r;
       t.m0 = r * TM;
       t.n0 = (tile - w * r * (r + 1) / 2) * p.tn;
     } else {
-      t.m0 = tile / p.nt * TM;
-      t.n0 = tile % p.nt * p.tn;
+      const int m = p.by_nt.of(tile);
+      t.m0 = m * TM;
+      t.n0 = (tile - m * p.nt) * p.tn;
     }
-    t.kb0 = (int)((long long)t.range * p.nkb / p.ks);
-    t.nkb = (int)((long long)(t.range + 1) * p.nkb / p.ks) - t.kb0;
+    t.kb0 = p.k.first(t.range);
+    t.nkb = p.k.count(t.range);
     t.na = p.na;
     t.nb = p.nb;
     t.lim = p.lim;
@@ -217,7 +220,7 @@ struct NsOp {
       get(c, v);
       const int col = col0 + c * 32;
       if (row0 >= p.e.rows || col >= p.e.cols) continue;
-      if (p.ks > 1)  // sums of the ranges [ks][batch][rows][cols, up to a multiple of four]
+      if (p.k.ks > 1)  // sums of the ranges [ks][batch][rows][cols, up to a multiple of four]
         store_32(&out[1], box, lane, v, p.e.cols - col, col, row0, t.range * p.batch + t.b);
       else
         p.e.finish(v, box, out, t.b, row0, col);
@@ -482,12 +485,14 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
   p.mt = tiles_of(g.rows, TM);
   p.nt = tiles_of(g.cols, cut.tn);
   p.per = g.sym ? sym_tiles(g.rows, cut.tn) : p.mt * p.nt;
-  p.nkb = (g.K + BK - 1) / BK;
-  p.ks = cut.ks;
+  const int nkb = (g.K + BK - 1) / BK;
+  p.k = Ranges(nkb, cut.ks);
+  p.by_per = Divisor((uint32_t)p.per);
+  p.by_nt = Divisor((uint32_t)p.nt);
   p.na = g.na;
   p.nb = g.nb;
   p.lim = g.lim();
-  p.seg = segment(bits16, g.prod(), p.nkb);
+  p.seg = segment(bits16, g.prod(), nkb);
   p.a_mn = g.a_mn;
   p.b_mn = g.b_mn;
   p.a_sym = g.a_sym;
@@ -511,19 +516,19 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
   m.b[1] = m.b_turned = m.b[0];
   if (g.a_sym && (rc = map(&m.a_turned, A, g.na, 1, g.rows, 0))) return rc;
   if (g.b_sym && (rc = map(&m.b_turned, B, g.nb, 1, g.cols, 0))) return rc;
-  if (p.ks > 1 && (rc = box_map(&m.out[1], part, MAP_F32, ld_part, g.rows, (long long)p.ks * s.batch, ld_part, (long long)g.rows * ld_part)))
+  if (cut.ks > 1 && (rc = box_map(&m.out[1], part, MAP_F32, ld_part, g.rows, (long long)cut.ks * s.batch, ld_part, (long long)g.rows * ld_part)))
     return rc;
   if (e.kind < NS_OUT)
     rc = box_map(&m.out[0], e.out.p, MAP_F16, g.cols, g.rows, (long long)e.np * s.batch, e.out.ld, e.out.mat);
   else if (e.box)
     rc = box_map(&m.out[0], e.w, e.bf16 ? MAP_BF16 : MAP_F32, g.cols, g.rows, s.batch, e.ldw, e.sw);
   if (rc) return rc;
-  const long long jobs = (long long)s.batch * p.per * p.ks;
+  const long long jobs = (long long)s.batch * p.per * cut.ks;
   rc = cut.tn == 256 ? launch_tiles<NsOp, 256>(m, p, jobs, g.na, g.nb, name, true, st)
                      : launch_tiles<NsOp, 128>(m, p, jobs, g.na, g.nb, name, true, st);
-  if (rc || p.ks == 1) return rc;
+  if (rc || cut.ks == 1) return rc;
   const long long blocks = (long long)s.batch * ((g.rows + 31) / 32) * ((g.cols + 31) / 32);
-  return launch_chain(k_ns_join, "k_ns_join", (unsigned)((blocks + 3) / 4), 128, 0, 1, true, st, m.out[0], (const float*)part, p.ks,
+  return launch_chain(k_ns_join, "k_ns_join", (unsigned)((blocks + 3) / 4), 128, 0, 1, true, st, m.out[0], (const float*)part, cut.ks,
                       ld_part, g.sym, cut.tn, e);
 }
 

@@ -37,6 +37,30 @@ constexpr size_t kSmem = RING + kEpi * BOX + 1024 + 256;
 static_assert(kSmem <= kSmemMax, "shared memory");
 constexpr long long kSpin = 1LL << 32;
 
+// i / d for 0 <= i < 2^31, 1 <= d < 2^31, by a product (Granlund and Montgomery, "Division by invariant integers using
+// multiplication", PLDI 1994): tiles are many and short, and each is found by a few divisions in every role.
+struct Divisor {
+  uint32_t d, mul, shift;
+  Divisor() = default;
+  __host__ explicit Divisor(uint32_t n) : d(n) {
+    shift = 0;
+    while ((1ull << shift) < n) ++shift;
+    mul = (uint32_t)(((1ull << 31) * (1ull << shift) + n - 1) / n - (1ull << 31));  // ceil(2^(31 + shift) / n), less 2^31
+  }
+  __device__ __forceinline__ int of(int i) const {
+    return (int)(((unsigned long long)mul * (uint32_t)i + ((unsigned long long)(uint32_t)i << 31)) >> (31 + shift));
+  }
+};
+// nkb K blocks in ks ranges, the first `more` of them one longer.
+struct Ranges {
+  int ks, each, more;
+  Divisor by;
+  Ranges() = default;
+  __host__ Ranges(int nkb, int n) : ks(n), each(nkb / n), more(nkb % n), by((uint32_t)n) {}
+  __device__ __forceinline__ int first(int r) const { return r * each + min(r, more); }
+  __device__ __forceinline__ int count(int r) const { return each + (r < more ? 1 : 0); }
+};
+
 // One tile: rows [m0, m0 + 256) x columns [n0, n0 + TN) of batch b, K blocks [kb0, kb0 + nkb).
 struct Job {
   int kind, m0, n0, b, kb0, nkb, range;
