@@ -227,7 +227,7 @@ Scratch carve_grad(Carve& c, const LinearGradShape& s) {
       const double one_d = nd > 0 ? (f_nkb + ks - 1) / ks * block_clocks(tn, p_dx) + 600 : 0;
       const double longest = std::max(one_d, one_g), share = (nd * ks * one_d + ng * one_g) / units;
       double clk = std::max(longest, share + (nd * ks + ng > units ? std::min(longest, ng > 0 ? one_g : one_d) / 2 : 0));
-      if (ks > 1) clk += 5000 + (double)T * s.C * 8 * ks / 3500;
+      if (ks > 1) clk += 3000 + (double)T * s.C * 8 * ks / 3500;
       if (least == 0 || clk < least) {
         least = clk;
         w.tn = tn;

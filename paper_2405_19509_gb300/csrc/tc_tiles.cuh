@@ -441,8 +441,8 @@ inline int segment(bool bits16, int prod, int nkb) { return std::min(nkb, std::m
 inline double block_clocks(int tn, int prod) { return tn == 256 ? 60 + 512.0 * prod : 440 + 190.0 * prod; }
 
 // Width of the tiles and ranges of K for a product of `values` in tiles(width) tiles over nkb K blocks: the cut whose
-// estimated clocks are fewest.  A tile's first loads and its epilogue some 3,000 that
-// nothing hides where a unit has one tile; ranges are joined by another launch that reads their sums.
+// estimated clocks are fewest.  A tile's first loads and its epilogue are some 3,000 and 12 a column, which nothing hides where a
+// unit has one tile; ranges are joined by another launch that reads their sums.
 struct Split {
   int tn, ks;
 };
@@ -455,8 +455,8 @@ Split split_of(Tiles tiles, double values, int nkb, int prod, int units) {
     for (int ks = 1; ks <= 32 && ks * 2 <= std::max(2, nkb); ++ks) {
       if (ks > 1 && n * (ks - 1) >= 2 * units) break;
       const double waves = (double)((n * ks + units - 1) / units);
-      double clk = 3000 + waves * ((nkb + ks - 1) / ks) * block_clocks(tn, prod) + (waves - 1) * 300;
-      if (ks > 1) clk += 5000 + values * 8 * ks / 3500;
+      double clk = 3000 + 12.0 * tn + waves * ((nkb + ks - 1) / ks) * block_clocks(tn, prod) + (waves - 1) * 300;
+      if (ks > 1) clk += 3000 + values * 8 * ks / 3500;
       if (least == 0 || clk < least) {
         least = clk;
         best = Split{tn, ks};
