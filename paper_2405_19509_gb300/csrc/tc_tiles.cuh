@@ -9,7 +9,8 @@
 // fp32 value keep 8 bits each whatever its size, fp16 parts 11 each of values that are scaled to the middle of the range.
 //
 // Sums: an addition in tensor memory is cut off, not rounded, about 2e-8 of the sum a step and always towards zero, so
-// 32-bit results leave it every `seg` K blocks and are added in registers.
+// 32-bit results leave it every `seg` K blocks and are added in registers; an operator whose values have no short digits takes them
+// times given_back().
 //
 // Bound: the tensor pipe (4 x 128 clocks a K block of one product at TN = 256; TN = 128 spreads few tiles) where tiles are many, else the
 // latency of a tile: barriers, the first loads and the epilogue, some 3 us.  Every wait is bounded (GC_ERR_TIMEOUT).
@@ -70,6 +71,20 @@ struct Job {
   int a_turn, b_turn;   // K blocks from which a symmetric operand's are read as their mirrors below the diagonal (kNever)
 };
 constexpr int kNever = 1 << 30;
+// Products of parts i + j < lim.
+__host__ __device__ inline int products(int na, int nb, int lim) {
+  int n = 0;
+  for (int i = 0; i < na; ++i) n += max(0, min(nb, lim - i));
+  return n;
+}
+// What `nkb` K blocks of `prod` products cut off their sum S, as a factor that gives it back.  A step cuts half a unit in the last
+// place of the partial sum so far on average, 0.5 2^-23 / (2 ln 2) of it over significands as they fall, and the partial
+// sums, which grow with the first product's four steps of a block alone, add up to (2 prod (nkb + 1) - 3 / 2) S, also where
+// terms cancel: a partial sum is then so far from 0 on average too, given S.  Sums of few digits, of which nothing is cut off, are made
+// too large by it.
+__device__ __forceinline__ float given_back(int prod, int nkb) {
+  return fmaf(4.3e-8f, 2.f * (float)(prod * (nkb + 1)) - 1.5f, 1.f);
+}
 // ... where of rows `row` .. the blocks of 256 up to the diagonal exist.
 __device__ __forceinline__ int turn_of(int row) { return (row / TM + 1) * (TM / BK); }
 
@@ -384,6 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
     for (int k = 0; k < njobs && ok; ++k) {
       const Job t = Op::job(p, unit, k);
       const int row0 = t.m0 + side * 128 + quarter * 32, col0 = t.n0 + part * QN;  // the warp's
+      float back = Op::kGivesBack ? given_back(products(t.na, t.nb, t.lim), min(t.nkb, t.seg)) : 1.f;
       if (t.nkb > t.seg) {
         // the sum of the segments, back into the last one's place
         float sum[QN];
@@ -391,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
         for (int j = 0; j < QN; ++j) sum[j] = 0.f;
         for (int left = t.nkb; filled(); left -= t.seg, ++use) {
 #pragma unroll
-          for (int j = 0; j < QN; j += 16) tmem_add16(at() + (uint32_t)j, sum + j);
+          for (int j = 0; j < QN; j += 16) tmem_add16(at() + (uint32_t)j, sum + j, back);
           if (left <= t.seg) break;
           release();
         }
@@ -399,12 +415,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
 #pragma unroll
         for (int j = 0; j < QN; j += 16) tmem_st16(at() + (uint32_t)j, sum + j);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        back = 1.f;
       } else if (!filled()) {
         break;
       }
       auto get = [&](int c, float (&v)[32]) {  // the accumulator is handed back when the last of it is in registers
         tmem_ld32(at() + (uint32_t)(c * 32), v);
         if (c == QN / 32 - 1) release();
+        if (Op::kGivesBack) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] *= back;
+        }
       };
       Op::template store<QN / 32>(p, t, row0, col0, box, maps.out, get);
       ++use;
@@ -424,13 +445,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
 
 // ---- host ---------------------------------------------------------------------------------------
 inline int tiles_of(long long n, int tile) { return (int)((n + tile - 1) / tile); }
-
-// Products of parts i + j < lim.
-inline int products(int na, int nb, int lim) {
-  int n = 0;
-  for (int i = 0; i < na; ++i) n += std::max(0, std::min(nb, lim - i));
-  return n;
-}
 
 // K blocks that are summed in tensor memory at a time: 48 steps, whose additions lose less than 1e-6; for a result of 16
 // bits 2,048, which lose 4e-5.
