@@ -459,6 +459,8 @@ int gc_linear(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ld
     return rc;
   if (y == X || z == X || y == z || (z && z == residual))
     return fail(GC_ERR_ARG, "y and z must not be X or one another, nor z the residual");
+  if (y == residual && ldy != ldr && rows > 1)
+    return fail(GC_ERR_ARG, "y over the residual needs its stride, %lld and not %lld", (long long)ldr, (long long)ldy);
   // one row needs no stride, but the layout rules below read it
   if (F == 1) ldw = (C + 7) / 8 * 8;
   if (rows == 1) {

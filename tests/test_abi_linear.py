@@ -23,7 +23,7 @@ def _fwd(X=Q, ldx=64, xt=1, W=P, ldw=64, wt=1, bias=None, act=0, res=None, ldr=1
     (dict(C=(1 << 20) + 1), -3), (dict(F=(1 << 20) + 1), -3), (dict(rows=1 << 30, F=1 << 20), -3), (dict(ldx=63), -2),
     (dict(ldw=63), -2), (dict(ldy=99), -2), (dict(z=U, ldz=99), -2), (dict(res=U, ldr=99), -2), (dict(bias=BAD4), -1),
     (dict(X=BAD2), -1), (dict(y=BAD2), -1), (dict(X=BAD4, xt=0), -1), (dict(y=Q), -1), (dict(z=Q), -1), (dict(z=S), -1),
-    (dict(z=U, res=U), -1), (dict(ws=None), -6), (dict(n=255), -6), (dict(ws=ctypes.c_void_p(4160)), -6),
+    (dict(z=U, res=U), -1), (dict(res=S, ldr=104), -1), (dict(ws=None), -6), (dict(n=255), -6), (dict(ws=ctypes.c_void_p(4160)), -6),
     (dict(wt=0, rows=100000, n=4096), -6)])
 def test_forward_refusals(kw, code):
     assert _fwd(**kw) == code
