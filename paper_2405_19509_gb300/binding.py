@@ -130,10 +130,10 @@ def block_length(d: int, ell: int) -> int:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream() -> int:
+def _stream(device=None) -> int:
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(torch.cuda.current_device() if device is None else device)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -442,24 +442,28 @@ def gc_softmax_xent(X, W, y, N: int, n_c: int, loss=True, row_loss=True, lse=Tru
 
 
 # ---------------------------------------------------------------- linear layers
-def _out(t, shape, dtype, device):
-    """An output: the tensor given, one made for True, None for False."""
+def _out(t, rows, cols, dtype, device, name):
+    """(an output, its device pointer, its row stride): the tensor given, one made for True, None for False."""
     if isinstance(t, torch.Tensor):
-        return t
-    return torch.empty(shape, dtype=dtype, device=device) if t else None
+        return t, *_rows(t, dtype, name, (rows, cols))
+    if not t:
+        return None, None, 0
+    t = torch.empty((rows, cols), dtype=dtype, device=device)
+    return t, t.data_ptr(), cols
 
 
 def _on_16(ptr, ld, rows, elt):
     """Whether rows lie on 16-byte boundaries (a single one needs no stride)."""
-    return int(ptr is not None and ptr % 16 == 0 and (ld * elt % 16 == 0 or rows == 1))
+    return 1 if ptr is not None and not (ptr & 15) and (not (ld * elt & 15) or rows == 1) else 0
 
 
 def _same_device(*tensors):
-    """Calls run on the current device's stream: its tensors alone."""
+    """The current device: calls run on its stream, with its tensors alone."""
     here = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor on {t.device}, but the current device is cuda:{here}")
+    return here
 
 
 def gc_linear(x, W, bias=None, act: int = GC_ACT_NONE, residual=None, y=None, z=False,
@@ -468,22 +472,19 @@ def gc_linear(x, W, bias=None, act: int = GC_ACT_NONE, residual=None, y=None, z=
     float32).  Returns dict with y (x's type; a tensor given is written into, and may be the residual) and z
     (None unless True or a tensor is given: what gc_linear_backward takes).  Rows may be strided."""
     xt, wt = _elt(x, "x"), _elt(W, "W")
-    rows, C = x.shape
+    dt, (rows, C) = x.dtype, x.shape
     F = W.shape[0]
-    y = _out(True if y is None else y, (rows, F), x.dtype, x.device)
-    z = _out(z, (rows, F), x.dtype, x.device)
-    xp, ldx = _rows(x, x.dtype, "x", x.shape)
+    xp, ldx = _rows(x, dt, "x", (rows, C))
     wp_, ldw = _rows(W, W.dtype, "W", (F, C))
-    rp, ldr = _rows(residual, x.dtype, "residual", (rows, F))
-    yp, ldy = _rows(y, x.dtype, "y", (rows, F))
-    zp, ldz = _rows(z, x.dtype, "z", (rows, F))
+    rp, ldr = _rows(residual, dt, "residual", (rows, F))
     bp = _dev(bias, torch.float32, "bias", (F,))
-    _same_device(x, W, bias, residual, y, z)
-    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_linear_workspace", rows, C, F, xt, wt,
-                                        _on_16(xp, ldx, rows, x.element_size()),
-                                        _on_16(wp_, ldw, F, W.element_size())), x.device)
+    y, yp, ldy = _out(True if y is None else y, rows, F, dt, x.device, "y")
+    z, zp, ldz = _out(z, rows, F, dt, x.device, "z")
+    here = _same_device(x, W, bias, residual, y, z)
+    ws, (wp, wn) = _ws(ws, _device_bytes(here, "gc_linear_workspace", rows, C, F, xt, wt, _on_16(xp, ldx, rows, 4 - 2 * xt),
+                                        _on_16(wp_, ldw, F, 4 - 2 * wt)), x.device)
     _check(lib.gc_linear(xp, ldx, xt, wp_, ldw, wt, bp, act, rp, ldr, rows, C, F, yp, ldy, zp, ldz, wp, wn,
-                         _stream()))
+                         _stream(here)))
     return {"y": y, "z": z}
 
 
@@ -498,23 +499,22 @@ def gc_linear_backward(dy, x, W, N: int, n_c: int, z=None, act: int = GC_ACT_NON
     F = W.shape[0]
     if T != N * n_c:
         raise ValueError("x must have N * n_c rows")
-    dx, G = _out(dx, (T, C), x.dtype, x.device), _out(G, (N, F * C), torch.float32, x.device)
-    Gb = _out(Gb, (N, F), torch.float32, x.device)
-    yp, lddy = _rows(dy, x.dtype, "dy", (T, F))
-    zp, ldz = _rows(z, x.dtype, "z", (T, F))
-    xp, ldx = _rows(x, x.dtype, "x", (T, C))
+    dt, dev = x.dtype, x.device
+    yp, lddy = _rows(dy, dt, "dy", (T, F))
+    zp, ldz = _rows(z, dt, "z", (T, F))
+    xp, ldx = _rows(x, dt, "x", (T, C))
     wp_, ldw = _rows(W, W.dtype, "W", (F, C))
-    dp, lddx = _rows(dx, x.dtype, "dx", (T, C))
-    gp, ldg = _rows(G, torch.float32, "G", (N, F * C))
-    bp, ldgb = _rows(Gb, torch.float32, "Gb", (N, F))
-    _same_device(dy, x, W, z, dx, G, Gb)
-    e = x.element_size()
+    dx, dp, lddx = _out(dx, T, C, dt, dev, "dx")
+    G, gp, ldg = _out(G, N, F * C, torch.float32, dev, "G")
+    Gb, bp, ldgb = _out(Gb, N, F, torch.float32, dev, "Gb")
+    here = _same_device(dy, x, W, z, dx, G, Gb)
+    e = 4 - 2 * xt
     want = (dx is not None) + 2 * (G is not None) + 4 * (Gb is not None)
-    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_linear_backward_workspace", N, n_c, C, F,
-                                        xt, wt, act, _on_16(xp, ldx, T, e), _on_16(wp_, ldw, F, W.element_size()),
-                                        _on_16(yp, lddy, T, e), want), x.device)
+    ws, (wp, wn) = _ws(ws, _device_bytes(here, "gc_linear_backward_workspace", N, n_c, C, F, xt, wt, act,
+                                        _on_16(xp, ldx, T, e), _on_16(wp_, ldw, F, 4 - 2 * wt), _on_16(yp, lddy, T, e),
+                                        want), dev)
     _check(lib.gc_linear_backward(yp, lddy, zp, ldz, xp, ldx, xt, wp_, ldw, wt, act, N, n_c, C, F, dp, lddx, gp, ldg,
-                                  bp, ldgb, wp, wn, _stream()))
+                                  bp, ldgb, wp, wn, _stream(here)))
     return {"dx": dx, "G": G, "Gb": Gb}
 
 
@@ -560,11 +560,10 @@ def gc_orthogonalize(u, coeffs=None, steps: int = 5, eps: float = 1e-7, out=None
         out = torch.empty(u.shape, dtype=u.dtype, device=u.device)
     up, ldu, su = _mats(u, u.dtype, "u", u.shape)
     op, ldo, so = _mats(out, u.dtype, "out", u.shape)
-    _same_device(u, out)
-    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_orthogonalize_workspace", batch, rows, cols, dt),
-                       u.device)
+    here = _same_device(u, out)
+    ws, (wp, wn) = _ws(ws, _device_bytes(here, "gc_orthogonalize_workspace", batch, rows, cols, dt), u.device)
     _check(lib.gc_orthogonalize(up, ldu, su, dt, batch, rows, cols, _coeffs(coeffs), steps, eps, op, ldo, so, wp, wn,
-                                _stream()))
+                                _stream(here)))
     return out
 
 
@@ -578,11 +577,10 @@ def gc_muon_step(w, momentum, g, lr: float, Ntil: int, mu: float = 0.95, nestero
     wp_, ldw, sw = _mats(w, torch.float32, "w", w.shape)
     mp, ldm, sm = _mats(momentum, torch.float32, "momentum", w.shape)
     gp, ldg, sg = _mats(g, torch.float32, "g", w.shape)
-    _same_device(w, momentum, g)
-    ws, (wp, wn) = _ws(ws, _device_bytes(torch.cuda.current_device(), "gc_orthogonalize_workspace", batch, rows, cols,
-                                        GC_F32), w.device)
+    here = _same_device(w, momentum, g)
+    ws, (wp, wn) = _ws(ws, _device_bytes(here, "gc_orthogonalize_workspace", batch, rows, cols, GC_F32), w.device)
     _check(lib.gc_muon_step(wp_, ldw, sw, mp, ldm, sm, gp, ldg, sg, batch, rows, cols, lr, Ntil, mu, int(nesterov),
-                            weight_decay, scale, _coeffs(coeffs), steps, eps, wp, wn, _stream()))
+                            weight_decay, scale, _coeffs(coeffs), steps, eps, wp, wn, _stream(here)))
 
 
 # ---------------------------------------------------------------- Algorithm 1
