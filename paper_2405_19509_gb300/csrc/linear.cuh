@@ -96,6 +96,25 @@ __device__ __forceinline__ float tail(float z, float* density) {
   return *density * (t * q);
 }
 
+// ... of two values by the two-wide instructions, with the same bits.
+__device__ __forceinline__ float2 tail(float2 z, float2* density) {
+  using rowwise::both;
+  const float2 u = __ffma2_rn(both(0.35f), make_float2(fabsf(z.x), fabsf(z.y)), both(1.f));
+  const float2 t = make_float2(reciprocal(u.x), reciprocal(u.y));
+  float2 q = both(-0x1.ddba88p-6f);
+  q = __ffma2_rn(q, t, both(0x1.26fa9ap-3f));
+  q = __ffma2_rn(q, t, both(-0x1.05fb9ep-2f));
+  q = __ffma2_rn(q, t, both(0x1.464b9ap-3f));
+  q = __ffma2_rn(q, t, both(-0x1.7c5bdep-6f));
+  q = __ffma2_rn(q, t, both(0x1.b05920p-4f));
+  q = __ffma2_rn(q, t, both(0x1.eac964p-4f));
+  q = __ffma2_rn(q, t, both(0x1.1e70cap-3f));
+  q = __ffma2_rn(q, t, both(0x1.1df1c6p-3f));
+  const float2 e = __fmul2_rn(__fmul2_rn(both(-0.5f * kLog2e), z), z);
+  *density = make_float2(power2(e.x), power2(e.y));
+  return __fmul2_rn(*density, __fmul2_rn(t, q));
+}
+
 // act(z).  gelu = max(z, 0) - |z| Phi(-|z|); gelu_tanh by the tanh of a cubic u: (1 + tanh u) / 2 = sigmoid(2 u).
 __device__ __forceinline__ float activate(int act, float z) {
   switch (act) {
@@ -137,6 +156,26 @@ __device__ __forceinline__ float slope(int act, float z) {
   }
 }
 
+// gelu and v gelu' of two values.
+__device__ __forceinline__ void gelu(float& a, float& b) {
+  float2 e;
+  const float2 z = make_float2(a, b), p = tail(z, &e);
+  const float2 y = __ffma2_rn(make_float2(-fabsf(a), -fabsf(b)), p, make_float2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
+  a = y.x;
+  b = y.y;
+}
+__device__ __forceinline__ void times_gelu_slope(float2 z, float& a, float& b) {
+  if (fabsf(z.x) > 100.f) z.x = copysignf(100.f, z.x);
+  if (fabsf(z.y) > 100.f) z.y = copysignf(100.f, z.y);
+  float2 e;
+  const float2 p = tail(z, &e);
+  const float2 q = __fadd2_rn(rowwise::both(1.f), make_float2(-p.x, -p.y));
+  const float2 y = __fmul2_rn(make_float2(a, b), __ffma2_rn(__fmul2_rn(z, rowwise::both(kInvRoot2Pi)), e,
+                                                            make_float2(z.x > 0.f ? q.x : p.x, z.y > 0.f ? q.y : p.y)));
+  a = y.x;
+  b = y.y;
+}
+
 // v *= act'(z), the activation chosen once for eight values.
 __device__ __forceinline__ void times_slope(int act, const float (&z)[8], float (&v)[8]) {
 #define GC_ALL(A)                                                             \
@@ -144,8 +183,11 @@ __device__ __forceinline__ void times_slope(int act, const float (&z)[8], float 
     _Pragma("unroll") for (int j = 0; j < 8; ++j) v[j] *= slope(A, z[j]);     \
     break;
   switch (act) {
+    case GC_ACT_GELU:
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) times_gelu_slope(make_float2(z[j], z[j + 1]), v[j], v[j + 1]);
+      break;
     GC_ALL(GC_ACT_RELU)
-    GC_ALL(GC_ACT_GELU)
     GC_ALL(GC_ACT_GELU_TANH)
     GC_ALL(GC_ACT_SILU)
   }

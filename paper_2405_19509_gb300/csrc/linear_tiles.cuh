@@ -80,8 +80,11 @@ __device__ __forceinline__ void activate32(int act, float (&v)[32]) {
   case A:                                                          \
     _Pragma("unroll") for (int j = 0; j < 32; ++j) v[j] = linear::activate(A, v[j]); \
     break;
+    case GC_ACT_GELU:
+#pragma unroll
+      for (int j = 0; j < 32; j += 2) linear::gelu(v[j], v[j + 1]);
+      break;
     GC_ALL(GC_ACT_RELU)
-    GC_ALL(GC_ACT_GELU)
     GC_ALL(GC_ACT_GELU_TANH)
     GC_ALL(GC_ACT_SILU)
 #undef GC_ALL
