@@ -50,16 +50,15 @@ __global__ void __launch_bounds__(256)
     next_d.values(v);
     if (act != GC_ACT_NONE) next_z.values(u);
     if (r + 8 < rows) take(r + 8);
-    if (act != GC_ACT_NONE) times_slope(act, u, v);
+    if (act != GC_ACT_NONE) times_slope(act, u, v);  // past the row's end of two zeros
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (!in_row<VEC>(col0, lane, j, F)) v[j] = 0.f;  // relu' of a zero that stands for nothing is one, NaN or not
-      sum[j] += v[j];
-    }
+    for (int j = 0; j < 8; ++j) sum[j] += v[j];
     uint32_t far = 0;
-    for (int q = 0; q < np; ++q) {
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      if (q == np) break;
       uint32_t w[4];
-      next_part(v, far, w);
+      next_part(v, q == 0, q + 1 == np, far, w);
       store_part<VEC>(d + ((size_t)q * T_all + row) * Fp, col0, lane, Fp, w);
     }
   }

@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(256) k_parts(const T* __restrict__ x, long lon
     uint32_t far = 0;
     for (int q = 0; q < parts; ++q) {
       uint32_t w[4];
-      linear::next_part(v, far, w);
+      linear::next_part(v, q == 0, q + 1 == parts, far, w);
       linear::store_part<VEC>(out + ((size_t)q * rows + row) * Cp, col0, lane, Cp, w);
     }
   }

@@ -17,18 +17,19 @@ constexpr float kBf16Max = 0x1.fep+127f;
 constexpr float kInvRoot2Pi = 0.3989422804014327f;
 constexpr float kTanh0 = 0.7978845608028654f, kTanh1 = 0.044715f;  // sqrt(2 / pi); Hendrycks and Gimpel's cubic
 
-// The next bf16 part of eight values as packed pairs; the values keep their rest.  far: bits of those past bf16's largest
+// The next bf16 part of eight values as packed pairs; the values keep their rest (of no use after the last).  far: bits of those past bf16's largest
 // value, where fp32 goes on for another 2^-8 of it.  Their parts are cut off, not rounded, so that sums of them do not leave the
 // range either.  Of a value that is not finite the parts after the first are 0.
-__device__ __forceinline__ void next_part(float (&v)[8], uint32_t& far, uint32_t (&w)[4]) {
-  uint32_t ones = far;  // whether a part's exponent is all ones
+__device__ __forceinline__ void next_part(float (&v)[8], bool first, bool last, uint32_t& far, uint32_t (&w)[4]) {
+  uint32_t ones = far;  // whether the first part's exponent is all ones, or was where that is felt later
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
     w[j] = *reinterpret_cast<const uint32_t*>(&t);
-    ones |= ((w[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    if (first) ones |= ((w[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
   }
   if (ones == 0) {
+    if (last) return;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       v[2 * j] -= __uint_as_float(w[j] << 16);
@@ -96,10 +97,10 @@ __device__ __forceinline__ float tail(float z, float* density) {
   return *density * (t * q);
 }
 
-// ... of two values by the two-wide instructions, with the same bits.
+// ... of two |z| by the two-wide instructions, with the same bits.
 __device__ __forceinline__ float2 tail(float2 z, float2* density) {
   using rowwise::both;
-  const float2 u = __ffma2_rn(both(0.35f), make_float2(fabsf(z.x), fabsf(z.y)), both(1.f));
+  const float2 u = __ffma2_rn(both(0.35f), z, both(1.f));
   const float2 t = make_float2(reciprocal(u.x), reciprocal(u.y));
   float2 q = both(-0x1.ddba88p-6f);
   q = __ffma2_rn(q, t, both(0x1.26fa9ap-3f));
@@ -156,22 +157,27 @@ __device__ __forceinline__ float slope(int act, float z) {
   }
 }
 
+// min(|z|, 100), NaN of NaN.
+__device__ __forceinline__ float near(float z) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(z)), "f"(100.f));
+  return r;
+}
 // gelu and v gelu' of two values.
 __device__ __forceinline__ void gelu(float& a, float& b) {
   float2 e;
-  const float2 z = make_float2(a, b), p = tail(z, &e);
+  const float2 p = tail(make_float2(fabsf(a), fabsf(b)), &e);
   const float2 y = __ffma2_rn(make_float2(-fabsf(a), -fabsf(b)), p, make_float2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
   a = y.x;
   b = y.y;
 }
 __device__ __forceinline__ void times_gelu_slope(float2 z, float& a, float& b) {
-  if (fabsf(z.x) > 100.f) z.x = copysignf(100.f, z.x);
-  if (fabsf(z.y) > 100.f) z.y = copysignf(100.f, z.y);
+  const float2 m = make_float2(near(z.x), near(z.y));
   float2 e;
-  const float2 p = tail(z, &e);
+  const float2 p = tail(m, &e);
   const float2 q = __fadd2_rn(rowwise::both(1.f), make_float2(-p.x, -p.y));
-  const float2 y = __fmul2_rn(make_float2(a, b), __ffma2_rn(__fmul2_rn(z, rowwise::both(kInvRoot2Pi)), e,
-                                                            make_float2(z.x > 0.f ? q.x : p.x, z.y > 0.f ? q.y : p.y)));
+  const float2 zk = __fmul2_rn(make_float2(copysignf(m.x, z.x), copysignf(m.y, z.y)), rowwise::both(kInvRoot2Pi));
+  const float2 y = __fmul2_rn(make_float2(a, b), __ffma2_rn(zk, e, make_float2(z.x > 0.f ? q.x : p.x, z.y > 0.f ? q.y : p.y)));
   a = y.x;
   b = y.y;
 }
