@@ -26,6 +26,7 @@ struct FwdOp {
     int seg;
     int nx, nw, lim;
   };
+  static __device__ __forceinline__ void before(const Params&, int, int) {}
   static __device__ __forceinline__ int jobs(const Params& p, int unit) {
     return (int)(((long long)p.mt * p.nt * p.k.ks - unit + p.q.units - 1) / p.q.units);
   }
@@ -98,12 +99,11 @@ int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t*
   const bool xb = s.x_dtype == GC_BF16;
   int rc = GC_OK;
   bool chained = false;
-  if (!w.x_in_place) {
-    if ((rc = launch_parts(io.X, s.x_dtype, io.ldx, s.T, s.C, w.Cp, w.nx, w.X, chained, st))) return rc;
-    chained = true;
-  }
-  if (!w.w_in_place) {
-    if ((rc = launch_parts(io.W, s.w_dtype, io.ldw, s.F, s.C, w.Cp, w.nw, w.W, chained, st))) return rc;
+  if (!w.x_in_place || !w.w_in_place) {
+    const PartsJob none{};
+    if ((rc = launch_parts(w.x_in_place ? none : parts_job(io.X, s.x_dtype, io.ldx, s.T, s.C, w.Cp, w.nx, w.X),
+                           w.w_in_place ? none : parts_job(io.W, s.w_dtype, io.ldw, s.F, s.C, w.Cp, w.nw, w.W), false, st)))
+      return rc;
     chained = true;
   }
   const void *X = w.x_in_place ? io.X : w.X, *W = w.w_in_place ? io.W : w.W;

@@ -1,6 +1,7 @@
 // Gradient of a linear layer with its activation: d = dy act'(z), dx = d W, and per chunk of n_c points G_i = d_i^T x_i
 // (F x C) and Gb_i = sum_t d_t.
-//   k_linear_d       d as bf16 parts, and its column sums over 128 points at a time; k_linear_gb joins them
+//   k_linear_d       d as bf16 parts, and its column sums over 128 points at a time, which the tiles' warps join, or
+//                    k_linear_gb; and x and W as bf16 parts where they are fp32 or do not lie on 16-byte boundaries
 //   k_tiles<GradOp>  dx and all chunks' G in one launch
 //   k_linear_join    dx where its tiles' sum over F runs in ranges
 //
@@ -17,16 +18,26 @@ using namespace tiles;
 using namespace linear;
 using namespace rowwise;
 
-constexpr int kRowsD = 128;  // points of a block of k_linear_d
+constexpr int kRowsD = 128;    // points of a block of k_linear_d
+constexpr int kMostSums = 64;  // blocks of a chunk whose sums the tiles' warps join; more would hold up the first tile
 
-// A block: 256 columns of 128 points of a chunk, a warp every eighth row, the next one's loads ahead.
+// A block: 256 columns of 128 points of a chunk, a warp every eighth row, the next one's loads ahead.  The blocks past `blocks` form
+// the parts of x and of W.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256)
     k_linear_d(const T* __restrict__ dy, long long lddy, const T* __restrict__ z, long long ldz, int act, int N, int n_c,
-               int F, int Fp, int np, __nv_bfloat16* __restrict__ d, float* __restrict__ sums, int R) {
+               int F, int Fp, int np, __nv_bfloat16* __restrict__ d, float* __restrict__ sums, int R, int blocks,
+               const PartsJob x_parts, const PartsJob w_parts) {
   __shared__ float red[8][kSeg];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int segs = (Fp + kSeg - 1) / kSeg;
+  if ((int)blockIdx.x >= blocks) {
+    start_next();
+    wait_prior();
+    const int i = (int)blockIdx.x - blocks;
+    form_parts(i < x_parts.blocks ? x_parts : w_parts, i < x_parts.blocks ? i : i - x_parts.blocks);
+    return;
+  }
   const long long i = blockIdx.x, block = i / segs;
   const int col0 = (int)(i - block * segs) * kSeg;
   const int chunk = (int)(block / R), r0 = (int)(block - (long long)chunk * R) * kRowsD;
@@ -73,7 +84,8 @@ __global__ void __launch_bounds__(256)
   if (col0 + c < F) sums[block * F + col0 + c] = s;
 }
 
-// Gb[chunk][c] from R partial sums: a block 32 columns, warp w the sums w, w + 8, ..., then the warps in order.
+// Gb[chunk][c] from R partial sums: a block 32 columns, warp w the sums w, w + 8, ..., then the warps in order.  Where tiles
+// follow and R is small their warps do it (GradOp::before).
 __global__ void __launch_bounds__(256) k_linear_gb(const float* __restrict__ sums, int R, int F, float* __restrict__ Gb,
                                                    long long ldgb) {
   __shared__ float red[8][32];
@@ -113,7 +125,31 @@ struct GradOp {
     float* G;
     long long ldg;
     int g_box;
+    const float* sums;     // of d, `R` a chunk, and where their own sum goes; NULL: no place
+    int R, gb_blocks;      // blocks of 32 columns
+    float* Gb;
+    long long ldgb;
   };
+  // Before a unit's first tile is there, its epilogue warps sum Gb, a warp 32 columns, with k_linear_gb's bits.
+  static __device__ __forceinline__ void before(const Params& p, int warp, int warps) {
+    if (!p.sums) return;
+    const int lane = threadIdx.x & 31;
+    for (int i = warp; i < p.N * p.gb_blocks; i += warps) {
+      const int chunk = i / p.gb_blocks, c = (i - chunk * p.gb_blocks) * 32 + lane;
+      if (c >= p.F) continue;
+      const float* at = p.sums + (size_t)chunk * p.R * p.F + c;
+      float s[8];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) s[w] = 0.f;
+      for (int r = 0; r < p.R; r += 8)
+#pragma unroll
+        for (int w = 0; w < 8; ++w)
+          if (r + w < p.R) s[w] += __ldcg(at + (size_t)(r + w) * p.F);
+#pragma unroll
+      for (int w = 1; w < 8; ++w) s[0] += s[w];
+      p.Gb[chunk * p.ldgb + c] = s[0];
+    }
+  }
   static __device__ __forceinline__ int jobs(const Params& p, int unit) {
     const int ndx = (p.ndx - unit + p.q.units - 1) / p.q.units;
     const int rest = p.ng - p.extra * (p.q.units - p.r);
@@ -240,12 +276,13 @@ Scratch carve_grad(Carve& c, const LinearGradShape& s) {
 }
 
 template <typename T>
-int launch_d(const LinearGradShape& s, const LinearGradIO& io, const Scratch& w, int np, cudaStream_t st) {
+int launch_d(const LinearGradShape& s, const LinearGradIO& io, const Scratch& w, int np, const PartsJob& x, const PartsJob& W,
+             cudaStream_t st) {
   const bool vec = s.F % 8 == 0 && rows_16(io.dy, io.lddy, sizeof(T)) && (s.act == GC_ACT_NONE || rows_16(io.z, io.ldz, sizeof(T)));
   const long long grid = (long long)s.N * w.R * ((w.Fp + kSeg - 1) / kSeg);
-  return launch_chain(vec ? k_linear_d<T, true> : k_linear_d<T, false>, "k_linear_d", (unsigned)grid, 256, 0, 1, false, st,
-                      (const T*)io.dy, (long long)io.lddy, (const T*)io.z, (long long)io.ldz, s.act, s.N, s.n_c, s.F,
-                      w.Fp, np, w.D, w.sums, w.R);
+  return launch_chain(vec ? k_linear_d<T, true> : k_linear_d<T, false>, "k_linear_d", (unsigned)(grid + x.blocks + W.blocks), 256, 0,
+                      1, false, st, (const T*)io.dy, (long long)io.lddy, (const T*)io.z, (long long)io.ldz, s.act, s.N, s.n_c,
+                      s.F, w.Fp, np, w.D, w.sums, w.R, (int)grid, x, W);
 }
 
 // The outputs that k_linear_small.cu forms.
@@ -261,25 +298,24 @@ int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& w
   int rc = GC_OK;
   bool chained = false;
   const int np = w.d_in_place ? 0 : w.np;
+  PartsJob xp{}, wp{};
+  if (g && !w.x_in_place) xp = parts_job(io.X, s.x_dtype, io.ldx, T, s.C, w.Cp, w.nx, w.X);
+  if (dx && !w.w_in_place) wp = parts_job(io.W, s.w_dtype, io.ldw, s.F, s.C, w.Cp, w.nw, w.W);
   if (np || w.sums) {
-    rc = xb ? launch_d<__nv_bfloat16>(s, io, w, np, st) : launch_d<float>(s, io, w, np, st);
+    rc = xb ? launch_d<__nv_bfloat16>(s, io, w, np, xp, wp, st) : launch_d<float>(s, io, w, np, xp, wp, st);
     if (rc) return rc;
     chained = true;
+  } else if (xp.blocks + wp.blocks) {
+    if ((rc = launch_parts(xp, wp, false, st))) return rc;
+    chained = true;
   }
-  if (w.sums) {
+  const bool gb_in_tiles = w.sums && (dx || g) && w.R <= kMostSums;
+  if (w.sums && !gb_in_tiles) {
     if ((rc = launch_chain(k_linear_gb, "k_linear_gb", (unsigned)(s.N * ((s.F + 31) / 32)), 256, 0, 1, chained, st, w.sums,
                            w.R, s.F, io.Gb, (long long)io.ldgb)))
       return rc;
   }
   if (!dx && !g) return GC_OK;
-  if (g && !w.x_in_place) {
-    if ((rc = launch_parts(io.X, s.x_dtype, io.ldx, T, s.C, w.Cp, w.nx, w.X, chained, st))) return rc;
-    chained = true;
-  }
-  if (dx && !w.w_in_place) {
-    if ((rc = launch_parts(io.W, s.w_dtype, io.ldw, s.F, s.C, w.Cp, w.nw, w.W, chained, st))) return rc;
-    chained = true;
-  }
   const void *X = w.x_in_place ? io.X : w.X, *W = w.w_in_place ? io.W : w.W, *D = w.d_in_place ? io.dy : w.D;
   const long long ldx = w.x_in_place ? io.ldx : w.Cp, ldw = w.w_in_place ? io.ldw : w.Cp;
   const long long ldd = w.d_in_place ? io.lddy : w.Fp;
@@ -308,6 +344,11 @@ int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& w
   p.seg_g = segment(false, prod_g, p.c_nkb);
   p.G = io.G;
   p.ldg = io.ldg;
+  p.sums = gb_in_tiles ? w.sums : nullptr;
+  p.R = w.R;
+  p.gb_blocks = (s.F + 31) / 32;
+  p.Gb = io.Gb;
+  p.ldgb = io.ldgb;
   p.ndx = dx ? p.mt * p.ct * w.ks : 0;
   p.ng = g ? s.N * p.ft * p.ct : 0;
   int units = 0;

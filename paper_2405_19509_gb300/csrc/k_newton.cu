@@ -176,6 +176,7 @@ struct NsOp {
     int a_mn, b_mn;
     int a_sym, b_sym;                 // operands of which what is above the diagonal's blocks is not there
   };
+  static __device__ __forceinline__ void before(const Params&, int, int) {}
   static __device__ __forceinline__ int jobs(const Params& p, int unit) {
     return (int)(((long long)p.batch * p.per * p.k.ks - unit + p.q.units - 1) / p.q.units);
   }

@@ -7,9 +7,22 @@
 
 namespace gc {
 
-// 16-bit parts [parts][rows][Cp] of a matrix (k_parts.cu), zero from C to Cp, a multiple of 8.
-int launch_parts(const void* x, int dtype, int64_t ld, long long rows, int C, int Cp, int parts, __nv_bfloat16* out,
-                 bool chained, cudaStream_t s);
+// bf16 parts [parts][rows][Cp] of a matrix, zero from C to Cp, a multiple of 8: x = x0 + x1 + ..., part q the bf16 of what the
+// parts before left.  `blocks` blocks of 256 threads form them, none of an empty job.
+struct PartsJob {
+  const void* x;
+  long long ld, rows;
+  int C, Cp, parts, bf16, vec, blocks;
+  __nv_bfloat16* out;
+};
+inline PartsJob parts_job(const void* x, int dtype, int64_t ld, long long rows, int C, int Cp, int parts, __nv_bfloat16* out) {
+  const long long blocks = (rows * ((Cp + rowwise::kSeg - 1) / rowwise::kSeg) + 7) / 8;
+  const int bf = dtype == GC_BF16;
+  return PartsJob{x, (long long)ld, rows, C, Cp, parts, bf, C % 8 == 0 && rowwise::rows_16(x, ld, bf ? 2 : 4),
+                  (int)std::min<long long>(blocks, 16LL * device_sm_count()), out};
+}
+// Two matrices' in one launch (k_parts.cu).
+int launch_parts(const PartsJob& a, const PartsJob& b, bool chained, cudaStream_t s);
 
 namespace linear {
 
@@ -61,6 +74,32 @@ __device__ __forceinline__ void store_part(__nv_bfloat16* row, int col0, int lan
     const int c = col0 + j * 32 + lane;
     if (c < Cp) to[c] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
   }
+}
+
+// Block `block` of a job: a warp takes segments of 256 columns, several an SM in flight.
+template <typename T, bool VEC>
+__device__ __forceinline__ void form_parts(const PartsJob& p, int block) {
+  const int lane = threadIdx.x & 31;
+  const int segs = (p.Cp + rowwise::kSeg - 1) / rowwise::kSeg;
+  const long long n = p.rows * segs, step = (long long)p.blocks * 8;
+  for (long long i = (long long)block * 8 + (threadIdx.x >> 5); i < n; i += step) {
+    const long long row = i / segs;
+    const int col0 = (int)(i - row * segs) * rowwise::kSeg;
+    float v[8];
+    rowwise::load_seg<VEC>(reinterpret_cast<const T*>(p.x) + row * p.ld, col0, lane, p.C, v);
+    uint32_t far = 0;
+    for (int q = 0; q < p.parts; ++q) {
+      uint32_t w[4];
+      next_part(v, q == 0, q + 1 == p.parts, far, w);
+      store_part<VEC>(p.out + ((size_t)q * p.rows + row) * p.Cp, col0, lane, p.Cp, w);
+    }
+  }
+}
+__device__ __forceinline__ void form_parts(const PartsJob& p, int block) {
+  if (p.bf16)
+    p.vec ? form_parts<__nv_bfloat16, true>(p, block) : form_parts<__nv_bfloat16, false>(p, block);
+  else
+    p.vec ? form_parts<float, true>(p, block) : form_parts<float, false>(p, block);
 }
 
 // 2^x and 1 / x by the special function unit, 2 and 1 units in the last place off; 2^x of x below -126 is 0.

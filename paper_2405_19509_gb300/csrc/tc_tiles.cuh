@@ -380,6 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
   } else {
     const int quarter = warp & 3, part = (warp - 2) >> 2;
     uint8_t* box = boxes + (warp - 2) * BOX;
+    Op::before(p, (int)blockIdx.x * kEpi + warp - 2, (int)gridDim.x * kEpi);
     uint32_t use = 0;
     bool ok = true;
     auto filled = [&] {
