@@ -452,8 +452,9 @@ Scratch carve_ns(Carve& c, const NsShape& s) {
   w.xa = w.pp = bf ? 1 : 2;
   w.aa = w.xx = 2;
   const long long segs = (long long)s.rows * ((s.cols + kSeg - 1) / kSeg);
-  // some 16 warps of loads an SM, over all matrices
-  w.blocks = (int)std::max(1LL, std::min((segs + 15) / 16, 8LL * device_sm_count() / std::min(s.batch, 8 * device_sm_count())));
+  // at most four blocks an SM over all matrices, each of which adds up all blocks' sums: a step of 2048 x 2048 takes 117 us, with
+  // eight 123
+  w.blocks = (int)std::max(1LL, std::min((segs + 15) / 16, 4LL * device_sm_count() / std::min(s.batch, 4 * device_sm_count())));
   w.X[0] = take_parts(c, w.xx, s.batch, s.rows, s.cols);
   w.X[1] = take_parts(c, w.xx, s.batch, s.rows, s.cols);
   w.A = take_parts(c, w.aa, s.batch, w.m, w.m);
