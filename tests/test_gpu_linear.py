@@ -228,6 +228,17 @@ def test_outputs_alone_and_repeated(gc, x, w):
     assert b["z"] is None and torch.equal(a["y"], b["y"])
 
 
+@pytest.mark.parametrize("n_c", [8000, 9000])
+def test_bias_gradients_alone_have_the_same_bits(gc, n_c):
+    """Partial sums of few points are joined beside the products, of many in a launch of their own, alone always."""
+    m = Maker(n_c)
+    x, W, dy, z = (m.mat(*s, torch.bfloat16) for s in ((2 * n_c, 72), (130, 72), (2 * n_c, 130), (2 * n_c, 130)))
+    all_ = gc.gc_linear_backward(dy, x, W, 2, n_c, z=z, act=gc.GC_ACT_SILU)
+    alone = gc.gc_linear_backward(dy, x, W, 2, n_c, z=z, act=gc.GC_ACT_SILU, dx=False, G=False)["Gb"]
+    assert torch.equal(all_["Gb"], alone)
+    _close(alone, _ref_grad(dy, z, x, W, "silu", 2)["Gb"], "Gb")
+
+
 @pytest.mark.parametrize("T", [1, 5, 300])
 @pytest.mark.parametrize("x", ["bf16", "f32"])
 def test_y_over_the_residual(gc, x, T):

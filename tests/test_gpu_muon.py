@@ -103,6 +103,17 @@ def test_large(gc, b, r, n, x):
     assert _off(gc.gc_orthogonalize(u), _ref(u)) <= TOL[u.dtype]
 
 
+@pytest.mark.parametrize("b,r,n", [(3, 78, 78), (1, 200, 200), (1, 184, 1344), (1, 1000, 181), (2, 256, 256), (3, 886, 1304)])
+def test_five_steps_in_fp32_end_within_1e_5(gc, b, r, n):
+    """What additions cut off is given back on average, so the module's 1.9e-6 a product is left with its spread: the cut
+    is between 3/4 and 3/2 of its mean, by the significand, a fifth of 1.2e-6 in the 2-norm; with two operands and a result
+    rounded by 2^-22 (sqrt(1 / 3) of it in the 2-norm) sqrt(0.24^2 + 3 * 0.14^2) = 0.34e-6 a product, independent from
+    product to product: 0.34e-6 sqrt(15) = 1.3e-6, taken by slopes of up to 3.4 in each of the last two steps: below 1e-5, with
+    a term for X0, 0.14e-6 times 485 beside the share, below a hundredth, of the singular values that are so small."""
+    u = _gradient(b + r + n, b, r, n)
+    assert _off(gc.gc_orthogonalize(u), _ref(u)) <= 1e-5
+
+
 def test_reference_is_the_oracle():
     u = _gradient(1, 2, 9, 5)
     assert np.allclose(_ref(u)[1].cpu(), L.orthogonalize(u[1].double().cpu().numpy()))
