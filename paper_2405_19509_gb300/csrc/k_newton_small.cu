@@ -124,6 +124,8 @@ __global__ void __launch_bounds__(kThreads) k_ns_small(const NsShape s, const Ns
 
   const int side = mp / 4, tiles = side * side;
   const int each = ((mp + ctas - 1) / ctas + 3) / 4 * 4, row0 = min(rank * each, mp), rows = min(each, mp - row0);
+  int share = 1;  // threads of a tile of A, which split its sum; 16 x 2000 has 16 tiles
+  while (share < 32 && tiles * share * 2 <= kThreads) share *= 2;
   const int groups = (kn + 3) / 4;  // of the slice's columns, which are padded to a multiple of four
   const float a = s.coeffs[0], b = s.coeffs[1], c = s.coeffs[2];
   // f(k, i, sums): M S for columns k .. k + 3 of the slice S and rows i .. i + 3, a thread 4 x 4.  M is symmetric to the
@@ -154,12 +156,13 @@ __global__ void __launch_bounds__(kThreads) k_ns_small(const NsShape s, const Ns
   };
   for (int step = 0; step < s.steps; ++step) {
     __syncthreads();
-    // the slice's part of A, 4 x 4 a thread, to the CTA of its rows
-    for (int t = tid; t < tiles; t += kThreads) {
-      const int i = t / side * 4, j = t % side * 4, o = i / each;
+    // the slice's part of A, 4 x 4 a thread or `share` neighbouring ones, to the CTA of its rows
+    for (int t = tid; t - tid < tiles * share; t += kThreads) {
+      const int tile = min(t / share, tiles - 1), g = t % share;
+      const int i = tile / side * 4, j = tile % side * 4, o = i / each;
       float acc[4][4] = {};
 #pragma unroll 4
-      for (int k = 0; k < kn; ++k) {
+      for (int k = g; k < kn; k += share) {
         const float4 p = *reinterpret_cast<const float4*>(X + k * kLd + i), q = *reinterpret_cast<const float4*>(X + k * kLd + j);
         const float x[4] = {p.x, p.y, p.z, p.w}, y[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -167,10 +170,17 @@ __global__ void __launch_bounds__(kThreads) k_ns_small(const NsShape s, const Ns
 #pragma unroll
           for (int f = 0; f < 4; ++f) acc[e][f] = fmaf(x[e], y[f], acc[e][f]);
       }
+      for (int w = 1; w < share; w *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int f = 0; f < 4; ++f) acc[e][f] += __shfl_xor_sync(0xffffffffu, acc[e][f], w);
+      if (t >= tiles * share) break;
       float* to = ctas == 1 ? A + i * kLd : cluster.map_shared_rank(parts, o) + (rank * each + i - o * each) * kLd;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<float4*>(to + e * kLd + j) = make_float4(acc[e][0], acc[e][1], acc[e][2], acc[e][3]);
+        if ((e & (share - 1)) == g)
+          *reinterpret_cast<float4*>(to + e * kLd + j) = make_float4(acc[e][0], acc[e][1], acc[e][2], acc[e][3]);
     }
     sync();
     if (ctas > 1) {
