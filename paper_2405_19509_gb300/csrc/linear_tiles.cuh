@@ -255,14 +255,20 @@ inline int launch_join(const float* part, int ks, long long rows, int ld, const 
 // 10.8 against 12.8, 2^27 15 against 13; fp32 2^27 18.5 against 13.5.  Rows of 2048 by 8192 in bf16: one 5.4, two 8.0, four 17, eight
 // 27, against 13.5; with an fp32 W, which tiles copy in parts, 9, 13, 21, 36 against 35.  dx of 2^23.6 8.8 against 14.9, of
 // 2^24.6 15.4 against 13.5; six chunks' G of 2^21 each 6.4 against 15.9, of 2^24 21 against 17.
-constexpr int kLinearRows = 8;
+// A sum runs alone in a block there, some 2 us for 64 of its products: 16 x 5632 x 64 took 184 us.
+constexpr int kLinearRows = 8, kLinearSum = 256;
 constexpr double kLinearSmall = 1 << 25, kLinearSmallDx = 1 << 24, kLinearSmallChunk = 1 << 21;
 inline bool linear_small(const LinearShape& s) {
   const bool copies = s.x_dtype != GC_BF16 || s.w_dtype != GC_BF16 || !s.x_16 || !s.w_16;
+  if (s.T > kLinearRows && s.C > kLinearSum) return false;
   return s.T <= 2 || (double)s.T * s.C * s.F <= (s.T <= kLinearRows && copies ? 2 : 1) * kLinearSmall;
 }
-inline bool linear_small_dx(const LinearGradShape& s) { return (double)s.N * s.n_c * s.C * s.F <= kLinearSmallDx; }
-inline bool linear_small_g(const LinearGradShape& s) { return (double)s.n_c * s.C * s.F <= kLinearSmallChunk; }
+inline bool linear_small_dx(const LinearGradShape& s) {
+  return s.F <= kLinearSum && (double)s.N * s.n_c * s.C * s.F <= kLinearSmallDx;
+}
+inline bool linear_small_g(const LinearGradShape& s) {
+  return s.n_c <= kLinearSum && (double)s.n_c * s.C * s.F <= kLinearSmallChunk;
+}
 int launch_linear_small(const LinearShape& s, const LinearIO& io, const linear::Finish& f, cudaStream_t st);
 int launch_linear_grad_small(const LinearGradShape& s, const LinearGradIO& io, const linear::Finish& f, cudaStream_t st);
 
