@@ -227,6 +227,9 @@ struct Scratch {
   float *part, *sums;
 };
 
+// Clocks of a tile.
+double tile_clocks(int tn, int nkb, int prod) { return nkb * block_clocks(tn, prod) + 600; }
+
 Scratch carve_grad(Carve& c, const LinearGradShape& s) {
   Scratch w{};
   const long long T = (long long)s.N * s.n_c;
@@ -257,10 +260,10 @@ Scratch carve_grad(Carve& c, const LinearGradShape& s) {
   for (int tn = 256; tn >= 128; tn /= 2) {
     const double nd = dx ? (double)tiles_of(T, TM) * tiles_of(s.C, tn) : 0;
     const double ng = g ? (double)s.N * tiles_of(s.F, TM) * tiles_of(s.C, tn) : 0;
-    const double one_g = ng > 0 ? c_nkb * block_clocks(tn, p_g) + 600 : 0;
+    const double one_g = ng > 0 ? tile_clocks(tn, c_nkb, p_g) : 0;
     for (int ks = 1; ks <= (dx ? 32 : 1) && ks * 2 <= std::max(2, f_nkb); ++ks) {
       if (ks > 1 && nd * (ks - 1) >= 2 * units) break;
-      const double one_d = nd > 0 ? (f_nkb + ks - 1) / ks * block_clocks(tn, p_dx) + 600 : 0;
+      const double one_d = nd > 0 ? tile_clocks(tn, (f_nkb + ks - 1) / ks, p_dx) : 0;
       const double longest = std::max(one_d, one_g), share = (nd * ks * one_d + ng * one_g) / units;
       double clk = std::max(longest, share + (nd * ks + ng > units ? std::min(longest, ng > 0 ? one_g : one_d) / 2 : 0));
       if (ks > 1) clk += 3000 + (double)T * s.C * 8 * ks / 3500;
@@ -357,7 +360,10 @@ int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& w
   units = (int)std::min<long long>(units, (long long)p.ndx + p.ng);
   p.r = p.ndx % units;
   p.dx_each = p.ndx / units;
-  const double cost_dx = (double)f_nkb / w.ks * prod_dx, cost_g = (double)p.c_nkb * prod_g;
+  // of G with a short sum those of its store, 256 x tn values: at a pair's share of HBM in boxes, at a quarter of it by rows
+  p.g_box = g && s.C % 4 == 0 && rows_16(io.G, io.ldg, 4);
+  const double cost_dx = tile_clocks(w.tn, (f_nkb + w.ks - 1) / w.ks, prod_dx);
+  const double cost_g = std::max(tile_clocks(w.tn, p.c_nkb, prod_g), (p.g_box ? 25.0 : 90.0) * w.tn);
   p.extra = p.r == 0 ? 0 : std::min((int)(cost_dx / cost_g + 0.5), p.ng / (units - p.r));
   p.q.a_both = T > 128;
   p.q.a_rows = T > 128 ? 128 : (int)(T + 7) / 8 * 8;
@@ -374,7 +380,6 @@ int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& w
   if (dx && (rc = operand_map(&m.b[0], W, false, s.C, s.F, 1, w.nw, ldw, s.F * ldw, s.F * ldw, BK))) return rc;
   if (g) {
     if ((rc = operand_map(&m.b[1], X, false, s.C, s.n_c, s.N, w.nx, ldx, s.n_c * ldx, T * ldx, BK))) return rc;
-    p.g_box = s.C % 4 == 0 && rows_16(io.G, io.ldg, 4);
     if (p.g_box) {
       if ((rc = box_map(&m.out[1], io.G, MAP_F32, s.C, s.F, s.N, s.C, io.ldg))) return rc;
     }
