@@ -190,10 +190,14 @@ __device__ __forceinline__ void by_rows(uint8_t* box, int lane, const float (&v)
     __syncwarp();
     box_put_32(box, lane, v + 16 * h);
     __syncwarp();
-#pragma unroll 2
-    for (int r = lane / 16; r < rows; r += 2) {
-      const float x = *reinterpret_cast<const float*>(box + box_place(r, c % 16 / 4) + c % 4 * 4);
-      if (c < n) f(r, c, x);
+    if (c >= n) continue;
+    for (int r0 = lane / 16; r0 < rows; r0 += 16) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const float*>(box + box_place(r0 + 2 * i, c % 16 / 4) + c % 4 * 4);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + 2 * i < rows) f(r0 + 2 * i, c, x[i]);
     }
   }
 }
