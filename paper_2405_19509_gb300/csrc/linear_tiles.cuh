@@ -254,7 +254,8 @@ inline int launch_join(const float* part, int ks, long long rows, int ld, const 
 // Measured as graph replays, kernels here against tiles (us): 2^24 products in bf16 6.2 against 11.6, 2^25 6.3 against 11.6, 2^26
 // 10.8 against 12.8, 2^27 15 against 13; fp32 2^27 18.5 against 13.5.  Rows of 2048 by 8192 in bf16: one 5.4, two 8.0, four 17, eight
 // 27, against 13.5; with an fp32 W, which tiles copy in parts, 9, 13, 21, 36 against 35.  dx of 2^23.6 8.8 against 14.9, of
-// 2^24.6 15.4 against 13.5; six chunks' G of 2^21 each 6.4 against 15.9, of 2^24 21 against 17.
+// 2^24.6 15.4 against 13.5; six chunks' G of 2^21 each 6.4 against 15.9, of 2^24 21 against 17.  (A repeated call finds up to some 100 MB
+// of operands in L2.)
 // A sum runs alone in a block there, some 2 us for 64 of its products: 16 x 5632 x 64 took 184 us.
 constexpr int kLinearRows = 8, kLinearSum = 256;
 constexpr double kLinearSmall = 1 << 25, kLinearSmallDx = 1 << 24, kLinearSmallChunk = 1 << 21;
