@@ -5,8 +5,8 @@
 //   k_tiles<GradOp>  dx and all chunks' G in one launch
 //   k_linear_join    dx where its tiles' sum over F runs in ranges
 //
-// G is a 32-bit result (what the encode takes): with bf16 rows d enters it as hi + lo (2^-17; exact where there is no
-// activation: d is dy, read in place), a bf16 dx, rounded to 2^-8, takes the hi alone.  fp32 rows enter as three parts, six
+// With bf16 rows d enters G and dx as hi + lo (2^-17; exact where there is no activation: d is dy, read in place): a dx of the
+// hi alone was off by 2.35e-3 in the 2-norm, where its own rounding is 1.66e-3.  fp32 rows enter as three parts, six
 // products.  The sums over a chunk depend on its points alone, bit for bit, whatever chunks a call has: the workers that
 // hold a chunk form one gradient.
 #include "linear_tiles.cuh"
@@ -240,8 +240,8 @@ Scratch carve_grad(Carve& c, const LinearGradShape& s) {
   w.nx = xb ? 1 : 3;
   w.nw = wb ? 1 : xb ? 2 : 3;
   w.lim = xb ? 2 : 3;
-  w.np_dx = xb ? 1 : 3;
-  w.np = !dx && !g ? 0 : !xb ? 3 : g && s.act != GC_ACT_NONE ? 2 : 1;
+  w.np_dx = !xb ? 3 : s.act != GC_ACT_NONE ? 2 : 1;
+  w.np = dx || g ? w.np_dx : 0;
   w.d_in_place = xb && s.act == GC_ACT_NONE && s.dy_16;
   w.x_in_place = xb && s.x_16;
   w.w_in_place = wb && s.w_16;

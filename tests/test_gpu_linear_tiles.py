@@ -1,0 +1,50 @@
+"""gc_linear and gc_linear_backward where tiles on the tensor cores take the work: digits of their results, values that are
+not finite or at the end of the range, outputs over inputs, graphs.  Every test asserts that its sizes reach the tiles."""
+import pytest
+import torch
+
+from test_gpu_linear import PAIRS, TYPES, Maker, _act, _close, _code, _ref_grad, _ref_linear, _untouched, gc  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _t(dtype):
+    return 1 if dtype == torch.bfloat16 else 0
+
+
+def _by_tiles(gc, T, C, F, x, w, joined=None):
+    """Copies of rows on no boundary take a workspace on the tiles' path alone; of rows on one, ranges of a sum do."""
+    assert T > 8 and gc.lib.gc_linear_workspace(T, C, F, _t(TYPES[x]), _t(TYPES[w]), 0, 0) > 256
+    if joined is not None:
+        assert x == w == "bf16" and (gc.lib.gc_linear_workspace(T, C, F, 1, 1, 1, 1) > 256) == joined
+
+
+def _back_by_tiles(gc, N, n_c, C, F, x, w, want=3):
+    for k in (1, 2):
+        assert not want & k or gc.lib.gc_linear_backward_workspace(N, n_c, C, F, _t(TYPES[x]), _t(TYPES[w]), 2, 0, 0, 0, k) > 256
+
+
+def _norm_off(got, ref):
+    return ((got.double() - ref).norm() / ref.norm()).item()
+
+
+GRADS = [(2, 150, 520, 1000), (4, 77, 1000, 1031), (1, 700, 264, 4000), (8, 256, 512, 2048)]
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu", "relu", "none"])
+@pytest.mark.parametrize("w", ["bf16", "f32"])
+@pytest.mark.parametrize("N,n_c,C,F", GRADS)
+def test_dx_of_bf16_rows_is_rounded_once(gc, N, n_c, C, F, w, act):
+    """dx of bf16 rows is the fp32 product's, rounded: a value v off by e before it is rounded ends at most 2 e further from v
+    than v's own rounding.  e in the 2-norm, of terms of either sign: d and W as hi + lo, 2^-18 each and 2^-18 for lo lo, the
+    slope 2^-19; 2 F / 16 (with an fp32 W 3 F / 16) additions cut off by 2^-24 of a running sum of two thirds."""
+    _back_by_tiles(gc, N, n_c, C, F, "bf16", w, 1)
+    m = Maker(N + F)
+    T = N * n_c
+    X, W, z, dy = m.mat(T, C, torch.bfloat16), m.mat(F, C, TYPES[w], C ** -0.5), m.mat(T, F, torch.bfloat16, 1.5), m.mat(T, F, torch.bfloat16)
+    ref = _ref_grad(dy, z, X, W, act, N)["dx"][0]
+    e = 3 * 2.0 ** -18 + 2.0 ** -19 + (3 if w == "f32" else 2) * F / 16 * 2 / 3 * 2.0 ** -24
+    once = _norm_off(ref.to(torch.bfloat16), ref)
+    for G in (True, False):
+        got = gc.gc_linear_backward(dy, X, W, N, n_c, z=z, act=_code(gc, act), G=G, Gb=False)["dx"]
+        assert _norm_off(got, ref) <= once + 2 * e
