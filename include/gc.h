@@ -390,7 +390,8 @@ int gc_linear(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ld
  *   G, Gb  N rows of F * C and of F fp32, ldg and ldgb apart: slices of the chunk gradients of a model.
  * dX, G and Gb are each nullable, not all of them.  T <= 2^30.  Any alignment.  All sums have a fixed order; G and Gb of
  * a chunk depend on its rows alone, bit for bit, whatever chunks the call has besides.
- * With bf16 rows d enters G and dX as bf16 hi + lo (2^-17; as it is without an activation), an fp32 W as hi + lo.
+ * With bf16 rows d enters G as three bf16 parts (24 bits) and dX as bf16 hi + lo (2^-17), as it is without an activation, an
+ * fp32 W as hi + lo.
  * fp32 rows enter as in gc_linear.
  * Workspace: gc_linear_backward_workspace bytes; dy_16: whether dy lies on 16-byte boundaries; want: 1 with dX, 2 with
  * G, 4 with Gb, added up.  The size depends on the current device's number of SMs.

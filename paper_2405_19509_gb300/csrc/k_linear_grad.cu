@@ -5,9 +5,10 @@
 //   k_tiles<GradOp>  dx and all chunks' G in one launch
 //   k_linear_join    dx where its tiles' sum over F runs in ranges
 //
-// With bf16 rows d enters G and dx as hi + lo (2^-17; exact where there is no activation: d is dy, read in place): a dx of the
-// hi alone was off by 2.35e-3 in the 2-norm, where its own rounding is 1.66e-3.  fp32 rows enter as three parts, six
-// products.  The sums over a chunk depend on its points alone, bit for bit, whatever chunks a call has: the workers that
+// d has 24 bits and is an operand of 16.  With bf16 rows it enters G, an fp32 result (what the encode takes), as three parts, three
+// products: as hi + lo it left 2.5e-6 of G in the 2-norm where fp32 products leave 0.2 to 0.6e-6.  A bf16 dx takes hi + lo
+// (2^-17): of the hi alone it was off by 2.35e-3, where its own rounding is 1.66e-3.  Without an activation d is dy, one part,
+// read in place.  fp32 rows enter as three parts, six products.  The sums over a chunk depend on its points alone, bit for bit, whatever chunks a call has: the workers that
 // hold a chunk form one gradient.
 #include "linear_tiles.cuh"
 
@@ -122,7 +123,7 @@ struct GradOp {
     Ranges dx_k;           // K blocks of dx
     int c_nkb;             // ... and of G
     Divisor by_ct, by_chunk;  // column tiles; tiles of a chunk's G
-    int np_dx, np, nx, nw, lim, seg_dx, seg_g;
+    int np_dx, np, nx, nw, lim_dx, lim_g, seg_dx, seg_g;
     float* G;
     long long ldg;
     int g_box;
@@ -160,7 +161,6 @@ struct GradOp {
     Job t;
     t.b_mn = true;
     t.a_turn = t.b_turn = kNever;
-    t.lim = p.lim;
     const int ndx = p.dx_each + (unit < p.r ? 1 : 0);
     if (k < ndx) {
       const int i = unit + k * p.q.units, at = p.dx_k.by.of(i), m = p.by_ct.of(at);
@@ -173,6 +173,7 @@ struct GradOp {
       t.nkb = p.dx_k.count(t.range);
       t.na = p.np_dx;
       t.nb = p.nw;
+      t.lim = p.lim_dx;
       t.seg = p.seg_dx;
       return t;
     }
@@ -189,6 +190,7 @@ struct GradOp {
     t.nkb = p.c_nkb;
     t.na = p.np;
     t.nb = p.nx;
+    t.lim = p.lim_g;
     t.seg = p.seg_g;
     return t;
   }
@@ -221,7 +223,7 @@ struct GradOp {
 };
 
 struct Scratch {
-  int Cp, Fp, np, np_dx, nx, nw, lim, tn, ks, ld_part, R;
+  int Cp, Fp, np, np_dx, nx, nw, lim_dx, lim_g, tn, ks, ld_part, R;
   bool x_in_place, w_in_place, d_in_place;
   __nv_bfloat16 *X, *W, *D;
   float *part, *sums;
@@ -239,9 +241,10 @@ Scratch carve_grad(Carve& c, const LinearGradShape& s) {
   w.Fp = (s.F + 7) / 8 * 8;
   w.nx = xb ? 1 : 3;
   w.nw = wb ? 1 : xb ? 2 : 3;
-  w.lim = xb ? 2 : 3;
+  w.lim_dx = xb ? 2 : 3;
+  w.lim_g = 3;
   w.np_dx = !xb ? 3 : s.act != GC_ACT_NONE ? 2 : 1;
-  w.np = dx || g ? w.np_dx : 0;
+  w.np = !dx && !g ? 0 : g && s.act != GC_ACT_NONE ? 3 : w.np_dx;
   w.d_in_place = xb && s.act == GC_ACT_NONE && s.dy_16;
   w.x_in_place = xb && s.x_16;
   w.w_in_place = wb && s.w_16;
@@ -253,7 +256,7 @@ Scratch carve_grad(Carve& c, const LinearGradShape& s) {
   // the cut whose estimated clocks are fewest, as split_of's, over both kinds of tiles
   const int units = device_sm_count() / 2;
   const int f_nkb = (s.F + BK - 1) / BK, c_nkb = (s.n_c + BK - 1) / BK;
-  const int p_dx = products(w.np_dx, w.nw, w.lim), p_g = products(w.np, w.nx, w.lim);
+  const int p_dx = products(w.np_dx, w.nw, w.lim_dx), p_g = products(w.np, w.nx, w.lim_g);
   double least = 0;
   w.tn = 256;
   w.ks = 1;
@@ -342,8 +345,9 @@ int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& w
   p.np = w.np;
   p.nx = w.nx;
   p.nw = w.nw;
-  p.lim = w.lim;
-  const int prod_dx = products(w.np_dx, w.nw, w.lim), prod_g = products(w.np, w.nx, w.lim);
+  p.lim_dx = w.lim_dx;
+  p.lim_g = w.lim_g;
+  const int prod_dx = products(w.np_dx, w.nw, w.lim_dx), prod_g = products(w.np, w.nx, w.lim_g);
   p.seg_dx = segment(xb, prod_dx, f_nkb);
   p.seg_g = segment(false, prod_g, p.c_nkb);
   p.G = io.G;
