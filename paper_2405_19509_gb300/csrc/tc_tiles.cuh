@@ -8,9 +8,10 @@
 // the rounded rest of those before), and the products of parts i and j with i + j < lim are summed: bf16 parts of an
 // fp32 value keep 8 bits each whatever its size, fp16 parts 11 each of values that are scaled to the middle of the range.
 //
-// Sums: an addition in tensor memory is cut off, not rounded, about 2e-8 of the sum a step and always towards zero, so
-// 32-bit results leave it every `seg` K blocks and are added in registers; an operator whose values have no short digits takes them
-// times given_back().
+// Sums: an addition in tensor memory is cut off, not rounded, about 4e-8 of the sum so far a step and always towards zero.  So the
+// products of a K block are added from the smallest parts' to the largest's, which alone meet a sum of full size where a segment
+// begins (4,096 x 2048 -> 4096 in fp32: 1.2e-6 off in the 2-norm the other way round, 0.64e-6 so, at the same time), and 32-bit
+// results leave tensor memory every `seg` K blocks and are added in registers.
 //
 // Bound: the tensor pipe (4 x 128 clocks a K block of one product at TN = 256; TN = 128 spreads few tiles) where tiles are many, else the
 // latency of a tile: barriers, the first loads and the epilogue, some 3 us.  Every wait is bounded (GC_ERR_TIMEOUT).
@@ -349,14 +350,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
             const uint32_t d = tmem_base + (uint32_t)(ab * TN);
             // the descriptors of the stage: only the address, in 16-byte units, differs
             const uint64_t at = (uint64_t)((uint32_t)s * (uint32_t)q.stage_bytes >> 4);
-            uint64_t da = way.a + at;
+            const uint64_t da = way.a + at, db = way.b + at;
             uint32_t more = opens ? 0u : 1u;
-            for (int i = 0; i < t.na; ++i, da += A_BYTES >> 4) {
-              uint64_t db = way.b + at;
-              for (int j = 0; j < t.nb && i + j < t.lim; ++j, db += B_BYTES >> 4) {
+            for (int o = min(t.lim, t.na + t.nb - 1) - 1; o >= 0; --o) {
+              for (int i = max(0, o - t.nb + 1); i <= min(o, t.na - 1); ++i) {
+                const uint64_t pa = da + (uint64_t)(i * (A_BYTES >> 4)), pb = db + (uint64_t)((o - i) * (B_BYTES >> 4));
 #pragma unroll
                 for (int ks = 0; ks < BK / 16; ++ks) {
-                  mma(d, da + (uint64_t)(ks * way.a_step), db + (uint64_t)(ks * way.b_step), way.idesc, more);
+                  mma(d, pa + (uint64_t)(ks * way.a_step), pb + (uint64_t)(ks * way.b_step), way.idesc, more);
                   more = 1u;
                 }
               }
@@ -451,9 +452,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
 // ---- host ---------------------------------------------------------------------------------------
 inline int tiles_of(long long n, int tile) { return (int)((n + tile - 1) / tile); }
 
-// K blocks that are summed in tensor memory at a time: 48 steps, whose additions lose less than 1e-6; for a result of 16
-// bits 2,048, which lose 4e-5.
-inline int segment(bool bits16, int prod, int nkb) { return std::min(nkb, std::max(1, (bits16 ? 512 : 12) / prod)); }
+// K blocks that are summed in tensor memory at a time.  Of a 32-bit result so few that the additions that meet a sum of full size
+// stay below 28 (six products of two K blocks; three of two 16, one of six 24), off by 0.3 to 0.65e-6 in the 2-norm, as sums in
+// fp32 registers are.  Each such end of a segment costs some 700 clocks: 8 x 1024 x 2048 -> 8192 with G of three products takes 876 us
+// with two K blocks, 814 with four, off by 0.8e-6, and 1105 with one.  Of a result of 16 bits 2,048 steps, which lose 4e-5.
+inline int segment(bool bits16, int prod, int nkb) { return std::min(nkb, bits16 ? std::max(1, 512 / prod) : std::max(2, 6 / prod)); }
 
 // Clocks of a K block.  A 256-wide tile keeps the tensor pipe busy (512 a product, 570 measured for one); a 128-wide one reads
 // its operands from shared memory for half the work and is bound by that: 633 for one product, 1,010 for three.

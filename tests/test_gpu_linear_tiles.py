@@ -63,3 +63,30 @@ def test_G_of_bf16_rows_keeps_fp32_digits(gc, N, n_c, C, F, act):
     ref = _ref_grad(dy, z, X, W, act, N)
     for k in ("G", "Gb"):
         assert _norm_off(got[k], ref[k][0]) <= 2.1e-6, k
+
+
+@pytest.mark.parametrize("T,C,F", [(2048, 64, 1024), (1024, 128, 1031), (700, 520, 1000), (300, 4100, 520), (129, 8192, 136)])
+def test_fp32_rows_keep_fp32_digits(gc, T, C, F):
+    """fp32 rows enter as three parts, 24 bits.  At most 28 additions in a row meet a sum of its full size, each cut off by 2^-24 of
+    a running sum of two thirds, 1.1e-6, and the products left out 2^-24, the parts 2^-26: 1.2e-6, and of one K block of 64, where
+    four are of full size, 0.16e-6 + 0.07e-6.  Two parts would be 4.4e-6 off, 48 additions 1.9e-6."""
+    _by_tiles(gc, T, C, F, "f32", "f32")
+    m = Maker(C)
+    X, W = m.mat(T, C, torch.float32), m.mat(F, C, torch.float32, C ** -0.5)
+    got = gc.gc_linear(X, W)["y"]
+    assert _norm_off(got, X.double() @ W.double().T) <= (0.25e-6 if C == 64 else 0.8e-6)
+
+
+@pytest.mark.parametrize("x,act", [("f32", "gelu"), ("f32", "none"), ("bf16", "gelu"), ("bf16", "none")])
+@pytest.mark.parametrize("N,n_c,C,F", GRADS + [(3, 64, 520, 1000), (1, 5000, 136, 300)])
+def test_fp32_sums_of_chunks_keep_fp32_digits(gc, N, n_c, C, F, x, act):
+    """At most 28 additions of full size in a row (24 of bf16 products): 1.1e-6 at the most as above, all at their worst; a cut
+    is half of 2^-24 on average: 0.6e-6, and 0.2e-6 for d, the products left out and the joins."""
+    _back_by_tiles(gc, N, n_c, C, F, x, x)
+    m = Maker(N + F)
+    T = N * n_c
+    X, W, z, dy = m.mat(T, C, TYPES[x]), m.mat(F, C, TYPES[x], C ** -0.5), m.mat(T, F, TYPES[x]), m.mat(T, F, TYPES[x])
+    got = gc.gc_linear_backward(dy, X, W, N, n_c, z=z, act=_code(gc, act))
+    ref = _ref_grad(dy, z, X, W, act, N)
+    for k in ("dx", "G", "Gb") if x == "f32" else ("G", "Gb"):
+        assert _norm_off(got[k], ref[k][0]) <= 0.8e-6, k
