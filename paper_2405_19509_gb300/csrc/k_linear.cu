@@ -15,7 +15,7 @@ using namespace tiles;
 using namespace linear;
 
 struct FwdOp {
-  static constexpr bool kTurns = false, kGivesBack = false;
+  static constexpr bool kTurns = false;
   struct Params {
     Common q;
     Finish f;

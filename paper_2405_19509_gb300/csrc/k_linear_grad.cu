@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(256) k_linear_gb(const float* __restrict__ sum
 }
 
 struct GradOp {
-  static constexpr bool kTurns = false, kGivesBack = false;
+  static constexpr bool kTurns = false;
   struct Params {
     Common q;
     Finish f;              // of dx

@@ -13,9 +13,10 @@
 //
 // Parts are fp16 of values times a power of two.  Singular values stay below kMost (the entry point checks the
 // polynomial), so entries of X, A and P fit, and the parts of an entry end at 2^-24 / scale, 2^-37 for X: what is lost is
-// absolute, beside singular values of 1.  An fp32 u takes two parts everywhere, 22 bits, three products each: 0.7 to 7e-6 from
-// 64 bits in the 2-norm over 210 shapes up to 8192 x 2048, where fp32 has 0.6 to 4e-6 (one part: 2e-3 to 2e-2; without the
-// factor for what tensor memory cuts off, which costs no time: up to 1.3e-5).  A
+// absolute, beside singular values of 1.  An fp32 u takes two parts everywhere, 22 bits, three products each, whose sums leave
+// tensor memory every two K blocks: 0.5 to 7.8e-6 from 64 bits in the 2-norm over 130 shapes up to 4100 wide, dense and sparse ones,
+// where fp32 has up to 3.6e-6 (one part: 2e-3 to 2e-2).  Of rank 20 or less up to 1.4e-4, fp32 2.2e-4: what rounding leaves of
+// singular values of 0 is enlarged as any small one.  A
 // bf16 u, whose result is rounded to 1.7e-3, takes X in one part in A, P in one part, and two where a part would show (A in
 // A^2, X in P X): 0.8 to 1.3e-3.
 #include <cuda_fp16.h>
@@ -165,7 +166,7 @@ __host__ __device__ inline int sym_tiles(int rows, int tn) {
 }
 
 struct NsOp {
-  static constexpr bool kTurns = true, kGivesBack = true;
+  static constexpr bool kTurns = true;
   struct Params {
     Common q;
     Epilogue e;

@@ -96,8 +96,8 @@ __device__ __forceinline__ void commit_own(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
                : "memory");
 }
-// sum[0 .. 16) += f times 16 consecutive columns of the warp's 32 lanes (warp-collective).
-__device__ __forceinline__ void tmem_add16(uint32_t taddr, float* sum, float f = 1.f) {
+// sum[0 .. 16) += 16 consecutive columns of the warp's 32 lanes (warp-collective).
+__device__ __forceinline__ void tmem_add16(uint32_t taddr, float* sum) {
   uint32_t r[16];
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -107,7 +107,7 @@ __device__ __forceinline__ void tmem_add16(uint32_t taddr, float* sum, float f =
       : "r"(taddr));
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int j = 0; j < 16; ++j) sum[j] = fmaf(f, __uint_as_float(r[j]), sum[j]);
+  for (int j = 0; j < 16; ++j) sum[j] += __uint_as_float(r[j]);
 }
 // 16 consecutive columns of the warp's 32 lanes, to be waited for with tcgen05.wait::st (warp-collective).
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {

@@ -78,15 +78,7 @@ __host__ __device__ inline int products(int na, int nb, int lim) {
   for (int i = 0; i < na; ++i) n += max(0, min(nb, lim - i));
   return n;
 }
-// What `nkb` K blocks of `prod` products cut off their sum S, as a factor that gives it back.  A step cuts half a unit in the last
-// place of the partial sum so far on average, 0.5 2^-23 / (2 ln 2) of it over significands as they fall, and the partial
-// sums, which grow with the first product's four steps of a block alone, add up to (2 prod (nkb + 1) - 3 / 2) S, also where
-// terms cancel: a partial sum is then so far from 0 on average too, given S.  Sums of few digits, of which nothing is cut off, are made
-// too large by it.
-__device__ __forceinline__ float given_back(int prod, int nkb) {
-  return fmaf(4.3e-8f, 2.f * (float)(prod * (nkb + 1)) - 1.5f, 1.f);
-}
-// ... where of rows `row` .. the blocks of 256 up to the diagonal exist.
+// The K block from which on a symmetric operand's rows `row` .. are read as their mirrors: the blocks of 256 up to the diagonal exist.
 __device__ __forceinline__ int turn_of(int row) { return (row / TM + 1) * (TM / BK); }
 
 // What every operator's parameters hold.
@@ -405,7 +397,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
     for (int k = 0; k < njobs && ok; ++k) {
       const Job t = Op::job(p, unit, k);
       const int row0 = t.m0 + side * 128 + quarter * 32, col0 = t.n0 + part * QN;  // the warp's
-      float back = Op::kGivesBack ? given_back(products(t.na, t.nb, t.lim), min(t.nkb, t.seg)) : 1.f;
       if (t.nkb > t.seg) {
         // the sum of the segments, back into the last one's place
         float sum[QN];
@@ -413,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
         for (int j = 0; j < QN; ++j) sum[j] = 0.f;
         for (int left = t.nkb; filled(); left -= t.seg, ++use) {
 #pragma unroll
-          for (int j = 0; j < QN; j += 16) tmem_add16(at() + (uint32_t)j, sum + j, back);
+          for (int j = 0; j < QN; j += 16) tmem_add16(at() + (uint32_t)j, sum + j);
           if (left <= t.seg) break;
           release();
         }
@@ -421,17 +412,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
 #pragma unroll
         for (int j = 0; j < QN; j += 16) tmem_st16(at() + (uint32_t)j, sum + j);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-        back = 1.f;
       } else if (!filled()) {
         break;
       }
       auto get = [&](int c, float (&v)[32]) {  // the accumulator is handed back when the last of it is in registers
         tmem_ld32(at() + (uint32_t)(c * 32), v);
         if (c == QN / 32 - 1) release();
-        if (Op::kGivesBack) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] *= back;
-        }
       };
       Op::template store<QN / 32>(p, t, row0, col0, box, maps.out, get);
       ++use;
