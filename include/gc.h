@@ -417,7 +417,7 @@ int gc_linear_backward(const void* dy, int64_t lddy, const void* z, int64_t ldz,
  * Products run on the tensor cores with fp32 sums, fp32 matrices in two 16-bit parts (22 bits): five steps end within 1e-5 of
  * those in 64 bits in the 2-norm, where fp32 has up to 4e-6.  Singular values below some 1/500 of the norm are enlarged with what
  * rounding adds to them: of a matrix of low rank, whose other ones are 0 but not its entries, 1.4e-4 (fp32: 2.2e-4).  bf16
- * matrices take one or two parts, so that the result is within its own rounding of theirs.  A value that is not finite makes its own matrix NaN, no other.
+ * matrices take the same parts: the result is off by its own rounding.  A value that is not finite makes its own matrix NaN, no other.
  * Workspace: gc_orthogonalize_workspace bytes (8 a value, and 8 m^2 a matrix, m the smaller side, and more for few and
  * small ones).  The size depends on the current device's number of SMs.
  */

@@ -13,12 +13,11 @@
 //
 // Parts are fp16 of values times a power of two.  Singular values stay below kMost (the entry point checks the
 // polynomial), so entries of X, A and P fit, and the parts of an entry end at 2^-24 / scale, 2^-37 for X: what is lost is
-// absolute, beside singular values of 1.  An fp32 u takes two parts everywhere, 22 bits, three products each, whose sums leave
+// absolute, beside singular values of 1.  X, A and P take two parts everywhere, 22 bits, three products each, whose sums leave
 // tensor memory every two K blocks: 0.5 to 7.8e-6 from 64 bits in the 2-norm over 130 shapes up to 4100 wide, dense and sparse ones,
 // where fp32 has up to 3.6e-6 (one part: 2e-3 to 2e-2).  Of rank 20 or less up to 1.4e-4, fp32 2.2e-4: what rounding leaves of
-// singular values of 0 is enlarged as any small one.  A
-// bf16 u, whose result is rounded to 1.7e-3, takes X in one part in A, P in one part, and two where a part would show (A in
-// A^2, X in P X): 0.8 to 1.3e-3.
+// singular values of 0 is enlarged as any small one.  A bf16 u, whose result is rounded to 1.66e-3, takes the same parts, with sums
+// of up to 2,048 steps in tensor memory: of X in A and P in one part each the result was 1.75 to 1.95e-3 off.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -37,7 +36,9 @@ constexpr float kMost = 4.f;    // bound of the singular values
 constexpr float kTerms = 60.f;  // ... and of |a| + |b| s^2 + |c| s^4 over them
 constexpr float kSX = 8192.f, kSA = 2048.f, kSP = 1024.f;  // kSX kMost, kSA kMost^2 and kSP kTerms are below 65504
 
-// Parts [parts][batch][rows][ld] of matrices.
+constexpr int kParts = 2, kProd = 3;  // of a value; products of two values' parts i + j < 2
+
+// Parts [kParts][batch][rows][ld] of matrices.
 struct Parts {
   __half* p;
   long long plane, mat;
@@ -48,10 +49,8 @@ enum { NS_A, NS_P, NS_X, NS_OUT, NS_STEP };
 struct Epilogue {
   int kind, rows, cols, batch;
   float s;             // scale of a sum
-  Parts out;
-  int np;              // parts of `out`, whose rows may be written past their ends up to 16 bytes
+  Parts out;           // its rows may be written past their ends up to 16 bytes
   Parts A;             // NS_P: a I + b A + s sum
-  int na;
   float a, b;
   void* w;             // NS_OUT, NS_STEP: rows of results
   long long ldw, sw;
@@ -116,7 +115,7 @@ struct Epilogue {
       box_free(lane);
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] = fmaf(sum, v[j], row0 + lane == col0 + j ? a : 0.f);
-      for (int q = 0; q < na; ++q) {
+      for (int q = 0; q < kParts; ++q) {
         Rows32 part;  // rows of A end past a multiple of eight
         part.load(A.p + q * A.plane + mat * A.mat + (long long)row0 * A.ld + col0, A.ld * 2LL, m, (n + 7) / 8 * 16, lane);
         part.turn(buf, lane);
@@ -135,7 +134,7 @@ struct Epilogue {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] *= s;
     }
-    for (int q = 0; q < np; ++q) {
+    for (int q = 0; q < kParts; ++q) {
       uint32_t h[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
@@ -173,7 +172,7 @@ struct NsOp {
     int batch, mt, nt, per, tn, sym;  // tiles of rows, of columns, of a matrix
     Ranges k;
     Divisor by_per, by_nt;
-    int seg, na, nb, lim;
+    int seg;
     int a_mn, b_mn;
     int a_sym, b_sym;                 // operands of which what is above the diagonal's blocks is not there
   };
@@ -202,9 +201,7 @@ struct NsOp {
     }
     t.kb0 = p.k.first(t.range);
     t.nkb = p.k.count(t.range);
-    t.na = p.na;
-    t.nb = p.nb;
-    t.lim = p.lim;
+    t.na = t.nb = t.lim = kParts;
     t.seg = p.seg;
     t.a_mn = p.a_mn;
     t.b_mn = p.b_mn;
@@ -348,7 +345,7 @@ __global__ void __launch_bounds__(256) k_ns_norm(const Source s, double* __restr
 // than `amp` times, leave X below that.  In its place the powers of A are taken times lam^2.
 template <typename T, bool VEC, bool MOM>
 __global__ void __launch_bounds__(256) k_ns_scale(const Source s, const double* __restrict__ sums, float eps, float amp, Parts X,
-                                                  int np, float* __restrict__ lam) {
+                                                  float* __restrict__ lam) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int mat = blockIdx.x / s.blocks, block = blockIdx.x - mat * s.blocks;
   const int segs = (s.cols + kSeg - 1) / kSeg;
@@ -380,7 +377,7 @@ __global__ void __launch_bounds__(256) k_ns_scale(const Source s, const double* 
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = v[j] * p0 * p1 * r;
     __half* to = X.p + mat * X.mat + (long long)row * X.ld;
-    for (int q = 0; q < np; ++q, to += X.plane) {
+    for (int q = 0; q < kParts; ++q, to += X.plane) {
       float h[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -413,21 +410,18 @@ __global__ void __launch_bounds__(256) k_ns_scale(const Source s, const double* 
 // One of a step's products: result rows x cols over K.
 struct Product {
   int rows, cols, K, sym;
-  int na, nb, a_mn, b_mn;
+  int a_mn, b_mn;
   int a_sym, b_sym;
-  int lim() const { return std::max(na, nb); }
-  int prod() const { return products(na, nb, lim()); }
 };
 
 Split cut_of(const Product& g, int batch) {
   return split_of([&](int tn) { return (long long)batch * (g.sym ? sym_tiles(g.rows, tn) : tiles_of(g.rows, TM) * tiles_of(g.cols, tn)); },
-                  (double)batch * g.rows * g.cols, (g.K + BK - 1) / BK, g.prod(), device_sm_count() / 2);
+                  (double)batch * g.rows * g.cols, (g.K + BK - 1) / BK, kProd, device_sm_count() / 2);
 }
 
 struct Scratch {
   bool wide;
-  int m, n, xa, aa, pp, xx;  // parts: of X in A, of A in A^2, of P and of X in P X
-  int blocks;
+  int m, n, blocks;
   Parts X[2], A, P;
   double* sums;
   float *lam, *part;
@@ -435,36 +429,33 @@ struct Scratch {
   Split ca, cp, cx;
 };
 
-Parts take_parts(Carve& c, int np, int batch, int rows, int cols) {
+Parts take_parts(Carve& c, int batch, int rows, int cols) {
   Parts t;
   t.ld = (cols + 7) / 8 * 8;
   t.mat = (long long)rows * t.ld;
   t.plane = batch * t.mat;
-  t.p = c.take<__half>((size_t)np * t.plane);
+  t.p = c.take<__half>((size_t)kParts * t.plane);
   return t;
 }
 
 Scratch carve_ns(Carve& c, const NsShape& s) {
   Scratch w{};
-  const bool bf = s.dtype == GC_BF16;
   w.wide = s.rows <= s.cols;
   w.m = std::min(s.rows, s.cols);
   w.n = std::max(s.rows, s.cols);
-  w.xa = w.pp = bf ? 1 : 2;
-  w.aa = w.xx = 2;
   const long long segs = (long long)s.rows * ((s.cols + kSeg - 1) / kSeg);
   // at most four blocks an SM over all matrices, each of which adds up all blocks' sums: a step of 2048 x 2048 takes 117 us, with
   // eight 123
   w.blocks = (int)std::max(1LL, std::min((segs + 15) / 16, 4LL * device_sm_count() / std::min(s.batch, 4 * device_sm_count())));
-  w.X[0] = take_parts(c, w.xx, s.batch, s.rows, s.cols);
-  w.X[1] = take_parts(c, w.xx, s.batch, s.rows, s.cols);
-  w.A = take_parts(c, w.aa, s.batch, w.m, w.m);
-  w.P = take_parts(c, w.pp, s.batch, w.m, w.m);
+  w.X[0] = take_parts(c, s.batch, s.rows, s.cols);
+  w.X[1] = take_parts(c, s.batch, s.rows, s.cols);
+  w.A = take_parts(c, s.batch, w.m, w.m);
+  w.P = take_parts(c, s.batch, w.m, w.m);
   w.sums = c.take<double>((size_t)s.batch * w.blocks);
   w.lam = c.take<float>(s.batch);
-  w.pa = Product{w.m, w.m, w.n, 1, w.xa, w.xa, !w.wide, !w.wide, 0, 0};
-  w.pp2 = Product{w.m, w.m, w.m, 1, w.aa, w.aa, 0, 0, 1, 1};
-  w.px = w.wide ? Product{w.m, w.n, w.m, 0, w.pp, w.xx, 0, 1, 1, 0} : Product{w.n, w.m, w.m, 0, w.xx, w.pp, 0, 0, 0, 1};
+  w.pa = Product{w.m, w.m, w.n, 1, !w.wide, !w.wide, 0, 0};
+  w.pp2 = Product{w.m, w.m, w.m, 1, 0, 0, 1, 1};
+  w.px = w.wide ? Product{w.m, w.n, w.m, 0, 0, 1, 1, 0} : Product{w.n, w.m, w.m, 0, 0, 0, 0, 1};
   w.ca = cut_of(w.pa, s.batch);
   w.cp = cut_of(w.pp2, s.batch);
   w.cx = cut_of(w.px, s.batch);
@@ -493,10 +484,7 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
   p.k = Ranges(nkb, cut.ks);
   p.by_per = Divisor((uint32_t)p.per);
   p.by_nt = Divisor((uint32_t)p.nt);
-  p.na = g.na;
-  p.nb = g.nb;
-  p.lim = g.lim();
-  p.seg = segment(bits16, g.prod(), nkb);
+  p.seg = segment(bits16, kProd, nkb);
   p.a_mn = g.a_mn;
   p.b_mn = g.b_mn;
   p.a_sym = g.a_sym;
@@ -510,26 +498,26 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
   p.q.status = status;
   Maps m;
   int rc;
-  auto map = [&](CUtensorMap* t, const Parts& x, int np, int mn, int extent, int box) {
-    return mn ? operand_map(t, x.p, true, extent, g.K, s.batch, np, x.ld, x.mat, x.plane, BK)
-              : operand_map(t, x.p, true, g.K, extent, s.batch, np, x.ld, x.mat, x.plane, box);
+  auto map = [&](CUtensorMap* t, const Parts& x, int mn, int extent, int box) {
+    return mn ? operand_map(t, x.p, true, extent, g.K, s.batch, kParts, x.ld, x.mat, x.plane, BK)
+              : operand_map(t, x.p, true, g.K, extent, s.batch, kParts, x.ld, x.mat, x.plane, box);
   };
-  if ((rc = map(&m.a[0], A, g.na, g.a_mn, g.rows, p.q.a_rows)) || (rc = map(&m.b[0], B, g.nb, g.b_mn, g.cols, cut.tn / 2)))
+  if ((rc = map(&m.a[0], A, g.a_mn, g.rows, p.q.a_rows)) || (rc = map(&m.b[0], B, g.b_mn, g.cols, cut.tn / 2)))
     return rc;
   m.a[1] = m.out[0] = m.out[1] = m.a_turned = m.a[0];
   m.b[1] = m.b_turned = m.b[0];
-  if (g.a_sym && (rc = map(&m.a_turned, A, g.na, 1, g.rows, 0))) return rc;
-  if (g.b_sym && (rc = map(&m.b_turned, B, g.nb, 1, g.cols, 0))) return rc;
+  if (g.a_sym && (rc = map(&m.a_turned, A, 1, g.rows, 0))) return rc;
+  if (g.b_sym && (rc = map(&m.b_turned, B, 1, g.cols, 0))) return rc;
   if (cut.ks > 1 && (rc = box_map(&m.out[1], part, MAP_F32, ld_part, g.rows, (long long)cut.ks * s.batch, ld_part, (long long)g.rows * ld_part)))
     return rc;
   if (e.kind < NS_OUT)
-    rc = box_map(&m.out[0], e.out.p, MAP_F16, g.cols, g.rows, (long long)e.np * s.batch, e.out.ld, e.out.mat);
+    rc = box_map(&m.out[0], e.out.p, MAP_F16, g.cols, g.rows, (long long)kParts * s.batch, e.out.ld, e.out.mat);
   else if (e.box)
     rc = box_map(&m.out[0], e.w, e.bf16 ? MAP_BF16 : MAP_F32, g.cols, g.rows, s.batch, e.ldw, e.sw);
   if (rc) return rc;
   const long long jobs = (long long)s.batch * p.per * cut.ks;
-  rc = cut.tn == 256 ? launch_tiles<NsOp, 256>(m, p, jobs, g.na, g.nb, name, true, st)
-                     : launch_tiles<NsOp, 128>(m, p, jobs, g.na, g.nb, name, true, st);
+  rc = cut.tn == 256 ? launch_tiles<NsOp, 256>(m, p, jobs, kParts, kParts, name, true, st)
+                     : launch_tiles<NsOp, 128>(m, p, jobs, kParts, kParts, name, true, st);
   if (rc || cut.ks == 1) return rc;
   const long long blocks = (long long)s.batch * ((g.rows + 31) / 32) * ((g.cols + 31) / 32);
   return launch_chain(k_ns_join, "k_ns_join", (unsigned)((blocks + 3) / 4), 128, 0, 1, true, st, m.out[0], (const float*)part, cut.ks,
@@ -543,7 +531,7 @@ int launch_start(const Source& src, const Scratch& w, bool vec, float eps, float
                         w.sums);
   if (rc) return rc;
   return launch_chain(vec ? k_ns_scale<T, true, MOM> : k_ns_scale<T, false, MOM>, "k_ns_scale", grid, 256, 0, 1, true, st, src,
-                      (const double*)w.sums, eps, amp, w.X[0], std::max(w.xa, w.xx), w.lam);
+                      (const double*)w.sums, eps, amp, w.X[0], w.lam);
 }
 
 // f(largest singular value, largest factor it may have come by) after each step, from singular values of at most 1.  The
@@ -610,7 +598,6 @@ int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cud
     ea.batch = s.batch;
     ea.s = kSA / (kSX * kSX);
     ea.out = w.A;
-    ea.np = w.aa;
     ea.lam = w.lam;
     if ((rc = launch_product(s, w.pa, w.ca, X, X, ea, bf, w.part, status, stall, "k_ns_a", st))) return rc;
     stall = false;
@@ -618,9 +605,7 @@ int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cud
     ep.kind = NS_P;
     ep.s = s.coeffs[2] * (kSP / (kSA * kSA));
     ep.out = w.P;
-    ep.np = w.pp;
     ep.A = w.A;
-    ep.na = w.aa;
     ep.a = s.coeffs[0] * kSP;
     ep.b = s.coeffs[1] * (kSP / kSA);
     if ((rc = launch_product(s, w.pp2, w.cp, w.A, w.A, ep, bf, w.part, status, false, "k_ns_p", st))) return rc;
@@ -633,7 +618,6 @@ int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cud
       ex.kind = NS_X;
       ex.s = 1.f / kSP;
       ex.out = Y;
-      ex.np = w.xx;
     } else {
       ex.kind = mom ? NS_STEP : NS_OUT;
       ex.s = (mom ? io.step : 1.f) / (kSP * kSX);

@@ -67,3 +67,15 @@ def test_dense_matrices_keep_their_digits(gc, b, r, n):
     sign.  gc.h states 1e-5."""
     u = _by_tiles(gc, _gradient(b + r + n, b, r, n))
     assert _off(gc.gc_orthogonalize(u), _ref(u)) <= 1e-5
+
+
+@pytest.mark.parametrize("b,r,n", [(1, 200, 200), (1, 184, 1344), (2, 300, 256), (1, 1024, 4096), (1, 2048, 520)])
+def test_bf16_matrices_are_rounded_once(gc, b, r, n):
+    """The steps of a bf16 matrix keep an fp32 one's digits: a value v off by e before it is rounded ends at most 2 e further from v
+    than v's own rounding.  e: 3 K / 16 additions in each of 15 products, cut off by half of 2^-24 on average of a running sum of
+    two thirds, and 3 * 0.14e-6 for 22 bits of operands and results."""
+    u = _by_tiles(gc, _gradient(b + r + n, b, r, n).to(torch.bfloat16))
+    ref = _ref(u)
+    K = (max(r, n) + 2 * min(r, n)) / 3
+    e = 15 * (3 * K / 16 * 2.0 ** -25 * 2 / 3 + 0.42e-6)
+    assert _off(gc.gc_orthogonalize(u), ref) <= _off(ref.to(torch.bfloat16), ref) + 2 * e
