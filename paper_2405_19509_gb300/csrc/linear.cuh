@@ -155,14 +155,16 @@ __device__ __forceinline__ float2 tail(float2 z, float2* density) {
   return __fmul2_rn(*density, __fmul2_rn(t, q));
 }
 
-// act(z).  gelu = max(z, 0) - |z| Phi(-|z|); gelu_tanh by the tanh of a cubic u: (1 + tanh u) / 2 = sigmoid(2 u).
+// act(z).  gelu = z Phi(z), which keeps the tail's digits and of +inf is that; gelu_tanh by the tanh of a cubic u:
+// (1 + tanh u) / 2 = sigmoid(2 u).
 __device__ __forceinline__ float activate(int act, float z) {
   switch (act) {
     case GC_ACT_RELU:
       return z < 0.f ? 0.f : z;  // NaN stays
     case GC_ACT_GELU: {
       float e;
-      return fmaf(-fabsf(z), tail(z, &e), fmaxf(z, 0.f));
+      const float p = tail(z, &e);
+      return z * (z > 0.f ? 1.f - p : p);
     }
     case GC_ACT_GELU_TANH:
       return z * sigmoid2(z * fmaf(2.f * kLog2e * kTanh0 * kTanh1, z * z, 2.f * kLog2e * kTanh0));
@@ -206,7 +208,8 @@ __device__ __forceinline__ float near(float z) {
 __device__ __forceinline__ void gelu(float& a, float& b) {
   float2 e;
   const float2 p = tail(make_float2(fabsf(a), fabsf(b)), &e);
-  const float2 y = __ffma2_rn(make_float2(-fabsf(a), -fabsf(b)), p, make_float2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
+  const float2 q = __fadd2_rn(rowwise::both(1.f), make_float2(-p.x, -p.y));
+  const float2 y = __fmul2_rn(make_float2(a, b), make_float2(a > 0.f ? q.x : p.x, b > 0.f ? q.y : p.y));
   a = y.x;
   b = y.y;
 }

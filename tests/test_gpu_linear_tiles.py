@@ -90,3 +90,25 @@ def test_fp32_sums_of_chunks_keep_fp32_digits(gc, N, n_c, C, F, x, act):
     ref = _ref_grad(dy, z, X, W, act, N)
     for k in ("dx", "G", "Gb") if x == "f32" else ("G", "Gb"):
         assert _norm_off(got[k], ref[k][0]) <= 0.8e-6, k
+
+
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu", "relu"])
+@pytest.mark.parametrize("T,C,F,tiles", [(5, 64, 40, False), (40, 64, 40, False), (1024, 64, 1024, True), (1024, 64, 1021, True)])
+def test_activations_far_from_zero(gc, T, C, F, tiles, act):
+    """z is the row's first value alone.  act(+inf) is +inf, act(-inf) what its formula gives, far values are themselves or 0, and
+    a row's do not reach the next."""
+    if tiles:
+        _by_tiles(gc, T, C, F, "bf16", "bf16")
+    bf = torch.bfloat16
+    far = torch.tensor([float("inf"), float("-inf"), float("nan"), 3e38, -3e38, 1e19, -1e19, 200.0, -200.0, 0.0, 40.0, -40.0, 1.0], device="cuda").to(bf)
+    X, W = torch.zeros(T, C, device="cuda", dtype=bf), torch.zeros(F, C, device="cuda", dtype=bf)
+    X[:, 0] = far[torch.arange(T, device="cuda") % len(far)]
+    W[:, 0] = 1.0
+    got = gc.gc_linear(X, W, act=_code(gc, act), z=True)
+    v = X[:, :1].double()
+    want = _act(v, act).expand(T, F)
+    if act == "gelu":
+        want = torch.where(v == float("-inf"), float("nan"), want)       # -inf times 0, as the others'
+    assert torch.equal(got["z"].isnan(), v.isnan().expand(T, F)) and torch.equal(got["z"].isinf(), v.isinf().expand(T, F))
+    assert torch.equal(got["y"].isnan(), want.isnan().contiguous())
+    assert torch.allclose(got["y"].double(), want, rtol=2.0 ** -7, atol=1e-30, equal_nan=True)
