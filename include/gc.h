@@ -412,7 +412,7 @@ int gc_linear_backward(const void* dy, int64_t lddy, const void* z, int64_t ldz,
  *            Matrices of a batch may lie one after the other or side by side; they must not overlap.  Any alignment.
  *   coeffs   a, b, c (host), or NULL: 3.4445, -4.7750, 2.0315, whose slope at 0 is so steep that five steps bring singular
  *            values from 0.01 to between 0.7 and 1.2.  Refused where they take singular values of at most 1 past 4.
- *   steps    1 .. 64.   eps >= 0: a matrix of zeros stays one if it is positive.
+ *   steps    1 .. 64.   eps >= 0: a matrix of zeros stays one if it is positive; norms down to 2^-100 of it keep their digits.
  * batch 0 .. 2^20 (0: nothing is launched), rows and cols 1 .. 2^20, the smaller 1 .. 2^15.
  * Products run on the tensor cores with fp32 sums, fp32 matrices in two 16-bit parts (22 bits): five steps end within 1e-5 of
  * those in 64 bits in the 2-norm, where fp32 has up to 4e-6.  Singular values below some 1/500 of the norm are enlarged with what

@@ -13,7 +13,7 @@
 //
 // Parts are fp16 of values times a power of two.  Singular values stay below kMost (the entry point checks the
 // polynomial), so entries of X, A and P fit, and the parts of an entry end at 2^-24 / scale, 2^-37 for X: what is lost is
-// absolute, beside singular values of 1.  X, A and P take two parts everywhere, 22 bits, three products each, whose sums leave
+// absolute, beside singular values of 1, or of lam where a step's X has none above that (k_ns_scale).  X, A and P take two parts everywhere, 22 bits, three products each, whose sums leave
 // tensor memory every two K blocks: 0.5 to 7.8e-6 from 64 bits in the 2-norm over 130 shapes up to 4100 wide, dense and sparse ones,
 // where fp32 has up to 3.6e-6 (one part: 2e-3 to 2e-2).  Of rank 20 or less up to 1.4e-4, fp32 2.2e-4: what rounding leaves of
 // singular values of 0 is enlarged as any small one.  A bf16 u, whose result is rounded to 1.66e-3, takes the same parts, with sums
@@ -36,6 +36,7 @@ constexpr float kMost = 4.f;    // bound of the singular values
 constexpr float kTerms = 60.f;  // ... and of |a| + |b| s^2 + |c| s^4 over them
 constexpr float kSX = 8192.f, kSA = 2048.f, kSP = 1024.f;  // kSX kMost, kSA kMost^2 and kSP kTerms are below 65504
 
+constexpr int kMostSteps = 64;
 constexpr int kParts = 2, kProd = 3;  // of a value; products of two values' parts i + j < 2
 
 // Parts [kParts][batch][rows][ld] of matrices.
@@ -56,7 +57,7 @@ struct Epilogue {
   long long ldw, sw;
   int bf16, box;       // box: rows are whole 16-byte pieces
   float keep;          // NS_STEP: w = keep w + s sum
-  const float* lam;    // [batch]: X is lam times what its parts hold
+  const float* lam;    // [batch], and the next X's behind them: X is lam times what its parts hold
 
   __device__ __forceinline__ void one(int mat, float l, long long r, int c, float x) const {
     x *= l;
@@ -131,8 +132,9 @@ struct Epilogue {
         }
       }
     } else {
+      const float f = kind == NS_X ? s * (lam[mat] / lam[batch + mat]) : s;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] *= s;
+      for (int j = 0; j < 32; ++j) v[j] *= f;
     }
     for (int q = 0; q < kParts; ++q) {
       uint32_t h[16];
@@ -341,10 +343,27 @@ __global__ void __launch_bounds__(256) k_ns_norm(const Source s, double* __restr
   }
 }
 
-// X / lam as parts, and lam: a power of two, 1 but where |u| is so far below eps that the steps, which enlarge nothing more
-// than `amp` times, leave X below that.  In its place the powers of A are taken times lam^2.
+// The polynomial f(s) = a s + b s^3 + c s^5, and |f| at the s^2 > 0 where its slope is 0 (infinite where there is none).
+struct Poly {
+  float a, b, c;
+  float at[2], value[2];
+  int steps;
+  // The largest |f(s)| of s in [0, most], and what rounding may add.
+  __device__ __forceinline__ float bound(float most) const {
+    const float q = most * most;
+    float v = most * fabsf(fmaf(fmaf(c, q, b), q, a));
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (at[i] < q) v = fmaxf(v, value[i]);
+    return v * (1.f + 1e-5f);
+  }
+};
+
+// X / lam as parts, and lam of every step's X: the power of two above the bound of its singular values, at most 1, so that an X that
+// starts far below 1, from a |u| below eps, keeps its parts' digits wherever the steps take it.  The powers of A are taken
+// times lam^2.
 template <typename T, bool VEC, bool MOM>
-__global__ void __launch_bounds__(256) k_ns_scale(const Source s, const double* __restrict__ sums, float eps, float amp, Parts X,
+__global__ void __launch_bounds__(256) k_ns_scale(const Source s, const double* __restrict__ sums, float eps, Poly poly, Parts X,
                                                   float* __restrict__ lam) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int mat = blockIdx.x / s.blocks, block = blockIdx.x - mat * s.blocks;
@@ -362,9 +381,12 @@ __global__ void __launch_bounds__(256) k_ns_scale(const Source s, const double* 
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < 8; ++w) sum += red[w];
-    int down;
-    norm_factors(sum, eps, amp, kSX, factor, &down);
-    if (block == 0) lam[mat] = ldexpf(1.f, -down);
+    const float ratio = norm_ratio(sum, eps);
+    norm_factors(sum, eps, power_above(ratio), kSX, factor);
+    if (block == 0) {
+      float most = ratio;
+      for (int i = 0; i < poly.steps; ++i, most = poly.bound(most)) lam[(size_t)i * s.batch + mat] = power_above(most);
+    }
   }
   __syncthreads();
   const float p0 = factor[0], p1 = factor[1], r = factor[2];
@@ -452,7 +474,7 @@ Scratch carve_ns(Carve& c, const NsShape& s) {
   w.A = take_parts(c, s.batch, w.m, w.m);
   w.P = take_parts(c, s.batch, w.m, w.m);
   w.sums = c.take<double>((size_t)s.batch * w.blocks);
-  w.lam = c.take<float>(s.batch);
+  w.lam = c.take<float>((size_t)kMostSteps * s.batch);
   w.pa = Product{w.m, w.m, w.n, 1, !w.wide, !w.wide, 0, 0};
   w.pp2 = Product{w.m, w.m, w.m, 1, 0, 0, 1, 1};
   w.px = w.wide ? Product{w.m, w.n, w.m, 0, 0, 1, 1, 0} : Product{w.n, w.m, w.m, 0, 0, 0, 0, 1};
@@ -525,46 +547,57 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
 }
 
 template <typename T, bool MOM>
-int launch_start(const Source& src, const Scratch& w, bool vec, float eps, float amp, cudaStream_t st) {
+int launch_start(const Source& src, const Scratch& w, bool vec, float eps, const Poly& poly, cudaStream_t st) {
   const unsigned grid = (unsigned)(src.batch * src.blocks);
   int rc = launch_chain(vec ? k_ns_norm<T, true, MOM> : k_ns_norm<T, false, MOM>, "k_ns_norm", grid, 256, 0, 1, false, st, src,
                         w.sums);
   if (rc) return rc;
   return launch_chain(vec ? k_ns_scale<T, true, MOM> : k_ns_scale<T, false, MOM>, "k_ns_scale", grid, 256, 0, 1, true, st, src,
-                      (const double*)w.sums, eps, amp, w.X[0], w.lam);
+                      (const double*)w.sums, eps, poly, w.X[0], w.lam);
 }
 
-// f(largest singular value, largest factor it may have come by) after each step, from singular values of at most 1.  The
-// largest value of a s + b s^3 + c s^5 is at the end of the range, or where the slope a + 3 b q + 5 c q^2, q = s^2, is zero.
-template <typename F>
-void polynomial_bounds(const float* k, int steps, F f) {
-  const double a = k[0], b = k[1], c = k[2];
-  double most = 1;
-  auto value = [&](double x) { return fabs(x * (a + x * x * (b + x * x * c))); };
-  for (int i = 0; i < steps; ++i) {
-    const double terms = fabs(a) + most * most * (fabs(b) + most * most * fabs(c));
-    double next = value(most);
-    const double d = 9 * b * b - 20 * a * c;
-    double roots[2] = {-1, -1};
+// s^2 where the slope a + 3 b s^2 + 5 c s^4 of f(s) = a s + b s^3 + c s^5 is zero; what is not above 0 is none.
+struct Turns {
+  double at[2] = {-1, -1};
+  explicit Turns(const float* k) {
+    const double a = k[0], b = k[1], c = k[2], d = 9 * b * b - 20 * a * c;
     if (c != 0 && d >= 0) {
-      roots[0] = (-3 * b + sqrt(d)) / (10 * c);
-      roots[1] = (-3 * b - sqrt(d)) / (10 * c);
+      at[0] = (-3 * b + sqrt(d)) / (10 * c);
+      at[1] = (-3 * b - sqrt(d)) / (10 * c);
     } else if (c == 0 && b != 0) {
-      roots[0] = -a / (3 * b);
+      at[0] = -a / (3 * b);
     }
-    for (double q : roots)
-      if (q > 0 && q < most * most) next = std::max(next, value(sqrt(q)));
-    f(next, terms);
-    most = std::max(next, 1e-30);
   }
+};
+double value_of(const float* k, double s) { return fabs(s * (k[0] + s * s * (k[1] + s * s * (double)k[2]))); }
+
+Poly poly_of(const NsShape& s) {
+  const Turns t(s.coeffs);
+  Poly p{s.coeffs[0], s.coeffs[1], s.coeffs[2], {INFINITY, INFINITY}, {0.f, 0.f}, s.steps};
+  for (int i = 0; i < 2; ++i)
+    if (t.at[i] > 0) {
+      p.at[i] = (float)t.at[i];
+      p.value[i] = (float)value_of(s.coeffs, sqrt(t.at[i]));
+    }
+  return p;
 }
 
 }  // namespace
 
+// From singular values of at most 1, the largest after each step, at the end of the range or where the slope is zero, and the
+// largest factor |a| + |b| s^2 + |c| s^4 that one may have come by.
 bool ns_coefficients_bounded(const float* k, int steps) {
-  bool ok = true;
-  polynomial_bounds(k, steps, [&](double most, double slope) { ok = ok && most <= kMost && slope <= kTerms; });
-  return ok;
+  const Turns turns(k);
+  double most = 1;
+  for (int i = 0; i < steps; ++i) {
+    const double q = most * most, terms = fabs((double)k[0]) + q * (fabs((double)k[1]) + q * fabs((double)k[2]));
+    double next = value_of(k, most);
+    for (double t : turns.at)
+      if (t > 0 && t < q) next = std::max(next, value_of(k, sqrt(t)));
+    if (!(next <= kMost && terms <= kTerms)) return false;
+    most = std::max(next, 1e-30);
+  }
+  return true;
 }
 
 size_t ns_ws_bytes(const NsShape& s) {
@@ -582,12 +615,10 @@ int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cud
              s.rows, s.cols, s.batch, w.blocks, io.nesterov, io.mu, io.points};
   const bool vec = s.cols % 8 == 0 && rows_16(io.u, io.ldu, e) && (s.batch == 1 || io.su * e % 16 == 0) &&
                    (!mom || (rows_16(io.m, io.ldm, 4) && (s.batch == 1 || io.sm % 4 == 0)));
-  double amp = 1, now = 1;
-  polynomial_bounds(s.coeffs, s.steps, [&](double, double slope) { amp = std::max(amp, now *= slope); });
-  const float most = (float)std::min(amp, 1e30);
-  int rc = mom  ? launch_start<float, true>(src, w, vec, io.eps, most, st)
-           : bf ? launch_start<__nv_bfloat16, false>(src, w, vec, io.eps, most, st)
-                : launch_start<float, false>(src, w, vec, io.eps, most, st);
+  const Poly poly = poly_of(s);
+  int rc = mom  ? launch_start<float, true>(src, w, vec, io.eps, poly, st)
+           : bf ? launch_start<__nv_bfloat16, false>(src, w, vec, io.eps, poly, st)
+                : launch_start<float, false>(src, w, vec, io.eps, poly, st);
   if (rc) return rc;
   bool stall = take_stall(GC_STALL_MUON);
   for (int i = 0; i < s.steps; ++i) {
@@ -598,7 +629,7 @@ int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cud
     ea.batch = s.batch;
     ea.s = kSA / (kSX * kSX);
     ea.out = w.A;
-    ea.lam = w.lam;
+    ea.lam = w.lam + (size_t)i * s.batch;
     if ((rc = launch_product(s, w.pa, w.ca, X, X, ea, bf, w.part, status, stall, "k_ns_a", st))) return rc;
     stall = false;
     Epilogue ep = ea;
@@ -610,7 +641,7 @@ int launch_ns(const NsShape& s, const NsIO& io, Carve& ws, uint32_t* status, cud
     ep.b = s.coeffs[1] * (kSP / kSA);
     if ((rc = launch_product(s, w.pp2, w.cp, w.A, w.A, ep, bf, w.part, status, false, "k_ns_p", st))) return rc;
     Epilogue ex{};
-    ex.lam = w.lam;
+    ex.lam = ea.lam;
     ex.rows = s.rows;
     ex.cols = s.cols;
     ex.batch = s.batch;

@@ -115,8 +115,7 @@ __global__ void __launch_bounds__(kThreads) k_ns_small(const NsShape s, const Ns
   if (tid == 0) {
     sum = 0;
     for (int r = 0; r < ctas; ++r) sum += *cluster.map_shared_rank(&total, r);
-    int down;
-    norm_factors(sum, io.eps, INFINITY, 1.f, factor, &down);  // fp32 needs no other scale for a small norm
+    norm_factors(sum, io.eps, 1.f, 1.f, factor);  // fp32 needs no other scale for a small norm
   }
   __syncthreads();
   const float p0 = factor[0], p1 = factor[1], r1 = factor[2];

@@ -20,16 +20,22 @@ __device__ __forceinline__ void add_squares(float q, const float (&v)[K], double
   for (int j = 0; j < K; ++j) sum += (double)v[j] * v[j];
 }
 
-// scale / max(sqrt(sum), eps) as three factors, none of which leaves fp32's range: the norm is f 2^e.  down: a norm below eps
-// that the steps, which enlarge nothing more than `amp` times, leave below 2^-down is taken 2^down times as large.
-__device__ __forceinline__ void norm_factors(double sum, float eps, float amp, float scale, float* factor, int* down) {
+// |u| / max(|u|, eps) of a norm's square, 1 of one that is not finite.
+__device__ __forceinline__ float norm_ratio(double sum, float eps) {
+  const double norm = sqrt(sum);
+  return norm < (double)eps ? (float)(norm / (double)eps) : 1.f;
+}
+// The least power of two that is no less than x, between 2^-125 and 1.
+__device__ __forceinline__ float power_above(float x) {
+  int e = 0;
+  if (!(x < 1.f)) return 1.f;
+  frexpf(x, &e);
+  return x < 0x1p-125f ? 0x1p-125f : ldexpf(1.f, e);
+}
+// scale / (lam max(sqrt(sum), eps)), lam a power of two, as three factors, none of which leaves fp32's range: the norm is f 2^e.
+__device__ __forceinline__ void norm_factors(double sum, float eps, float lam, float scale, float* factor) {
   double norm = sqrt(sum);
-  *down = 0;
-  if (norm < (double)eps) {
-    const double t = norm / (double)eps * (double)amp;
-    if (t < 1) *down = t > 0x1p-125 ? -ilogb(t) - 1 : 125;  // t <= 2^-down < 2 t
-    norm = eps;
-  }
+  if (norm < (double)eps) norm = eps;
   if (isinf(norm) || isnan(norm)) {
     factor[0] = factor[1] = 1.f;
     factor[2] = isinf(norm) ? 0.f : (float)norm;
@@ -37,7 +43,7 @@ __device__ __forceinline__ void norm_factors(double sum, float eps, float amp, f
   }
   int e = 0;
   const double f = frexp(norm, &e);
-  e -= *down;
+  e += ilogbf(lam);
   factor[0] = ldexpf(1.f, -(e / 2));
   factor[1] = ldexpf(1.f, -(e - e / 2));
   factor[2] = (float)((double)scale / f);

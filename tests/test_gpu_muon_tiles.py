@@ -79,3 +79,33 @@ def test_bf16_matrices_are_rounded_once(gc, b, r, n):
     K = (max(r, n) + 2 * min(r, n)) / 3
     e = 15 * (3 * K / 16 * 2.0 ** -25 * 2 / 3 + 0.42e-6)
     assert _off(gc.gc_orthogonalize(u), ref) <= _off(ref.to(torch.bfloat16), ref) + 2 * e
+
+
+COEFFS = [((3.4445, -4.7750, 2.0315), 5), ((1.875, -1.25, 0.375), 20), ((1.5, -0.5, 0.0), 64), ((0.5, 0.0, 0.0), 40)]
+
+
+@pytest.mark.parametrize("coeffs,steps", COEFFS)
+@pytest.mark.parametrize("below", [1.0, 1e-1, 1e-3, 1e-5, 1.5e-6, 1e-9, 1e-20])
+@pytest.mark.parametrize("r,n", [(300, 400), (1000, 1000)])
+def test_norms_below_eps(gc, r, n, below, coeffs, steps):
+    """u far below eps starts the steps far below 1, and may reach 1 in many; it keeps the digits of any other.  Beyond five steps the
+    polynomials' slope near 1 is below 1, so that errors do not add up."""
+    u = _gradient(r, 1, r, n)
+    u = _by_tiles(gc, u / torch.linalg.matrix_norm(u)[:, None, None])
+    u, eps = u * 2.0 ** -10, 2.0 ** -10 / below
+    ref = _ref(u, coeffs, steps, eps)
+    assert _off(gc.gc_orthogonalize(u, coeffs=coeffs, steps=steps, eps=eps), ref) <= 1e-5
+
+
+def test_norms_of_a_batch_are_its_matrices(gc):
+    """Matrices of a batch with norms above, below and far below eps, and zeros."""
+    u = _by_tiles(gc, _gradient(3, 5, 130, 200))
+    u = u / torch.linalg.matrix_norm(u)[:, None, None] * torch.tensor([3.0, 0.5, 1e-4, 1e-12, 0.0], device="cuda")[:, None, None]
+    got, ref = gc.gc_orthogonalize(u, eps=1.0), _ref(u, eps=1.0)
+    for i in range(4):
+        assert _off(got[i:i + 1], ref[i:i + 1]) <= 1e-5
+    assert not got[4].any()
+    w, m = torch.zeros_like(u), torch.zeros_like(u)
+    gc.gc_muon_step(w, m, u, 1.0, 1, mu=0.5, nesterov=False, eps=1.0)
+    for i in range(4):
+        assert _off(-w[i:i + 1], ref[i:i + 1]) <= 1e-5
