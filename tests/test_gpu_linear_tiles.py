@@ -112,3 +112,125 @@ def test_activations_far_from_zero(gc, T, C, F, tiles, act):
     assert torch.equal(got["z"].isnan(), v.isnan().expand(T, F)) and torch.equal(got["z"].isinf(), v.isinf().expand(T, F))
     assert torch.equal(got["y"].isnan(), want.isnan().contiguous())
     assert torch.allclose(got["y"].double(), want, rtol=2.0 ** -7, atol=1e-30, equal_nan=True)
+
+
+@pytest.mark.parametrize("x,w", PAIRS)
+@pytest.mark.parametrize("layout", ["dense", "ragged"])
+def test_a_row_reaches_its_own_alone(gc, x, w, layout):
+    """Infinities and NaN in one row of x or of dy, with tiles and with ranges joined: the other rows keep their bits."""
+    for T, C, F, joined in ((300, 520, 1000, None), (300, 4096, 264, True)):
+        if joined is None or layout == "dense" and x == w == "bf16":
+            _by_tiles(gc, T, C, F, x, w, joined)
+        _back_by_tiles(gc, 2, T // 2, C, F, x, w)
+        m = Maker(T + C, layout)
+        t = TYPES[x]
+        X, W, z, dy = m.mat(T, C, t), m.mat(F, C, TYPES[w]), m.mat(T, F, t), m.mat(T, F, t)
+        want = gc.gc_linear(X, W, act=gc.GC_ACT_RELU, z=True)
+        back = gc.gc_linear_backward(dy, X, W, 2, T // 2, z=z, act=gc.GC_ACT_GELU)
+        rest = torch.arange(T, device="cuda") != 1
+        for bad in (float("inf"), float("-inf"), float("nan")):
+            X2, dy2 = X.clone(), dy.clone()
+            X2[1, 3] = bad
+            dy2[1, 7] = bad
+            got = gc.gc_linear(X2, W, act=gc.GC_ACT_RELU, z=True)
+            assert all(torch.equal(got[k][rest], want[k][rest]) for k in got) and not torch.isfinite(got["z"][1]).any()
+            got = gc.gc_linear_backward(dy2, X, W, 2, T // 2, z=z, act=gc.GC_ACT_GELU)
+            assert torch.equal(got["dx"][rest], back["dx"][rest]) and not torch.isfinite(got["dx"][1]).any()
+            assert torch.equal(got["G"][1], back["G"][1]) and torch.equal(got["Gb"][1], back["Gb"][1])
+            assert not torch.isfinite(got["G"][0].view(F, C)[7]).any() and torch.isfinite(got["G"][0].view(F, C)[8:]).all()
+            assert not torch.isfinite(got["Gb"][0, 7]) and torch.isfinite(got["Gb"][0, 8:]).all()
+
+
+@pytest.mark.parametrize("layout", ["dense", "ragged"])
+def test_values_at_the_end_of_the_range(gc, layout):
+    """fp32's largest values round past bf16's; alone in a row they are themselves in y, dx and G, to 2^-22: three parts that are
+    cut off keep 24 bits, their sums are cut off once or twice.  2^-100 times 2^-120 is below fp32's smallest, 2^-149."""
+    T, C, F = 300, 520, 1000
+    _by_tiles(gc, T, C, F, "f32", "f32")
+    _back_by_tiles(gc, 1, T, C, F, "f32", "f32")
+    m = Maker(1, layout)
+    big = 3.4028234e38
+    X, W = m.mat(T, C, torch.float32, 0.0), m.mat(F, C, torch.float32, 0.0)
+    X[0, 5], X[1, 6], X[2, 7], X[290, 519] = big, -big, 2.0 ** -120, big
+    W[:, 5], W[:, 6], W[:, 7], W[:, 519] = 1.0, 0.5, 1.0, -1.0
+    near = lambda got, want: bool(((got.double() - want).abs() <= 2.0 ** -22 * want.abs() + 2.0 ** -149).all())
+    assert near(gc.gc_linear(X, W)["y"], X.double() @ W.double().T)
+    assert near(gc.gc_linear(W, X)["y"], W.double() @ X.double().T)              # as the weights
+    dy = m.mat(T, F, torch.float32, 0.0)
+    dy[0, 3], dy[1, 4], dy[2, 5], dy[290, 999] = big, -big, 2.0 ** -100, 1.0
+    got = gc.gc_linear_backward(dy, X.clamp(-1, 1), W, 1, T)
+    assert near(got["dx"], dy.double() @ W.double())
+    assert near(got["G"][0].view(F, C), dy.double().T @ X.clamp(-1, 1).double())
+    assert near(gc.gc_linear_backward(dy.clamp(-1, 1), X, W, 1, T)["G"][0].view(F, C), dy.clamp(-1, 1).double().T @ X.double())
+
+
+def test_weights_at_the_end_of_the_range_beside_bf16_rows(gc):
+    T, C, F = 300, 520, 1000
+    _by_tiles(gc, T, C, F, "bf16", "f32")
+    X, W = torch.zeros(T, C, device="cuda", dtype=torch.bfloat16), torch.zeros(F, C, device="cuda")
+    X[0, 5], X[1, 6] = 1.0, 0.5
+    W[:, 5], W[:, 6] = 3.38e38, 3.4028234e38
+    got = gc.gc_linear(X, W)["y"].double()
+    want = X.double() @ W.double().T
+    assert bool(((got - want).abs() <= (2.0 ** -8 + 2.0 ** -15) * want.abs()).all())
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("T,C,F,joined", [(300, 520, 1000, None), (300, 520, 1001, None), (300, 4096, 264, True), (300, 4096, 261, None),
+                                          (2100, 520, 1032, False)])
+def test_y_over_the_residual(gc, x, T, C, F, joined):
+    """By boxes, by rows on no boundary, and by the join of ranges."""
+    _by_tiles(gc, T, C, F, x, x, joined if x == "bf16" else None)
+    m = Maker(4)
+    X, W, res = m.mat(T, C, TYPES[x]), m.mat(F, C, TYPES[x], C ** -0.5), m.mat(T, F, TYPES[x])
+    want = gc.gc_linear(X, W, act=gc.GC_ACT_GELU, residual=res, z=True)
+    _close(want["y"], _ref_linear(X, W, None, "gelu", res)["y"], "y")
+    got = gc.gc_linear(X, W, act=gc.GC_ACT_GELU, residual=res, y=res, z=True)
+    assert got["y"] is res and torch.equal(res, want["y"]) and torch.equal(got["z"], want["z"])
+
+
+@pytest.mark.parametrize("x,w", PAIRS)
+@pytest.mark.parametrize("T,C,F", [(300, 520, 1000), (300, 4096, 264)])
+def test_on_another_stream_and_in_a_graph(gc, T, C, F, x, w):
+    """Forward and backward by tiles, copies in parts and joins among them, on a stream of their own and replayed."""
+    _by_tiles(gc, T, C, F, x, w)
+    _back_by_tiles(gc, 2, T // 2, C, F, x, w)
+    m = Maker(12)
+    X, W, dy = m.mat(T, C, TYPES[x]), m.mat(F, C, TYPES[w]), m.mat(T, F, TYPES[x])
+    f = gc.gc_linear(X * 2, W, act=gc.GC_ACT_GELU, z=True)
+    want = gc.gc_linear_backward(dy * 2, X * 2, W, 2, T // 2, z=f["z"], act=gc.GC_ACT_GELU)
+    torch.cuda.synchronize()
+    s, ws = torch.cuda.Stream(), gc.Workspace()
+    with torch.cuda.stream(s):
+        X2, dy2 = X * 2, dy * 2
+        got = gc.gc_linear(X2, W, act=gc.GC_ACT_GELU, z=True, ws=ws)
+        back = gc.gc_linear_backward(dy2, X2, W, 2, T // 2, z=got["z"], act=gc.GC_ACT_GELU, ws=ws)
+    s.synchronize()
+    assert all(torch.equal(got[k], f[k]) for k in f) and all(torch.equal(back[k], want[k]) for k in want)
+    for t in (*got.values(), *back.values()):
+        t.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gc.gc_linear(X2, W, act=gc.GC_ACT_GELU, y=got["y"], z=got["z"], ws=ws)
+        gc.gc_linear_backward(dy2, X2, W, 2, T // 2, z=got["z"], act=gc.GC_ACT_GELU, ws=ws, **back)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[k], f[k]) for k in f) and all(torch.equal(back[k], want[k]) for k in want)
+    gc.gc_status(ws)
+
+
+def test_slices_of_a_gradient_matrix(gc):
+    """G and Gb as a program has them: columns of an N x d matrix of odd d, from an odd one on, which keep the rest."""
+    N, n_c, C, F = 3, 120, 264, 1000
+    _back_by_tiles(gc, N, n_c, C, F, "bf16", "bf16")
+    m = Maker(8)
+    X, W, z, dy = (m.mat(*s, torch.bfloat16) for s in ((N * n_c, C), (F, C), (N * n_c, F), (N * n_c, F)))
+    want = gc.gc_linear_backward(dy, X, W, N, n_c, z=z, act=gc.GC_ACT_GELU)
+    d = 7 + F * C + F + 4
+    d += 1 - d % 2
+    all_ = torch.full((N, d), -77.0, device="cuda")
+    G, Gb = all_[:, 7:7 + F * C], all_[:, 7 + F * C:7 + F * C + F]
+    got = gc.gc_linear_backward(dy, X, W, N, n_c, z=z, act=gc.GC_ACT_GELU, G=G, Gb=Gb)
+    assert torch.equal(G, want["G"]) and torch.equal(Gb, want["Gb"]) and torch.equal(got["dx"], want["dx"])
+    assert bool((all_[:, :7] == -77).all()) and bool((all_[:, 7 + F * C + F:] == -77).all())

@@ -109,3 +109,43 @@ def test_norms_of_a_batch_are_its_matrices(gc):
     gc.gc_muon_step(w, m, u, 1.0, 1, mu=0.5, nesterov=False, eps=1.0)
     for i in range(4):
         assert _off(-w[i:i + 1], ref[i:i + 1]) <= 1e-5
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_zeros_and_values_that_are_not_finite(gc, x):
+    """A matrix of zeros stays one, one with an infinity or NaN becomes NaN, and no other matrix of the batch changes."""
+    u = _by_tiles(gc, _gradient(7, 5, 130, 200).to(TYPES[x]))
+    want = gc.gc_orthogonalize(u)
+    u[0] = 0
+    u[1, 3, 4] = float("inf")
+    u[2, 129, 199] = float("nan")
+    u[3, 0, 0] = float("-inf")
+    got = gc.gc_orthogonalize(u)
+    assert not got[0].any() and all(torch.isnan(got[i]).all() for i in (1, 2, 3)) and torch.equal(got[4], want[4])
+    assert torch.isnan(gc.gc_orthogonalize(u[:1], eps=0.0)).all()
+
+
+def test_a_step_of_values_that_are_not_finite(gc):
+    w, m, g = (_by_tiles(gc, _randn(s, 3, 130, 200)) for s in (1, 2, 3))
+    W, M = w.clone(), m.clone()
+    gc.gc_muon_step(W, M, g, 0.02, 9)
+    g[1, 5, 6] = float("inf")
+    gc.gc_muon_step(w, m, g, 0.02, 9)
+    assert torch.isnan(w[1]).all() and all(torch.equal(w[i], W[i]) and torch.equal(m[i], M[i]) for i in (0, 2))
+
+
+@pytest.mark.parametrize("r,n", [(130, 200), (1000, 300)])
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1e-12, 1e12, 1e25, 3e37])
+def test_any_size_of_values(gc, r, n, scale):
+    """The norm's squares leave fp32's range.  The result is that of the values as they are stored: 1e-5 as for values near 1."""
+    u = _by_tiles(gc, _gradient(3, 1, r, n).clamp(-8, 8) * scale)
+    assert _off(gc.gc_orthogonalize(u, eps=0.0), _ref(u, eps=0.0)) <= 1e-5
+
+
+@pytest.mark.parametrize("r,n", [(96, 200), (520, 520), (1000, 300)])
+def test_low_rank(gc, r, n):
+    """Of rank 3 the other singular values are what rounding leaves of them, and the steps enlarge it by up to 3.4445^5 = 485: a
+    spread of 2^-22 sqrt(1 / 3) of X0's values, 1.4e-7, and 3 * 2^-22 sqrt(1 / 3) of each of the next X, by what steps are
+    left, 485, 141, 41, 12 and 3.4: 6.8e-5 + 8.3e-5, beside |O| of about |X| then."""
+    u = _by_tiles(gc, (_randn(3, r, 3) @ _randn(4, 3, n))[None])
+    assert _off(gc.gc_orthogonalize(u), _ref(u)) <= 1.6e-4
