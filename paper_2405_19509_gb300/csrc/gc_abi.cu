@@ -457,8 +457,8 @@ int gc_linear(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ld
       (rc = check_rows("residual", residual, ldr, rows, F, xe, false)) ||
       (rc = check_rows("y", y, ldy, rows, F, xe, true)) || (rc = check_rows("z", z, ldz, rows, F, xe, false)))
     return rc;
-  if (y == X || z == X || y == z || (z && z == residual))
-    return fail(GC_ERR_ARG, "y and z must not be X or one another, nor z the residual");
+  if (y == X || z == X || y == W || z == W || y == z || (z && z == residual))
+    return fail(GC_ERR_ARG, "y and z must not be X, W or one another, nor z the residual");
   if (y == residual && ldy != ldr && rows > 1)
     return fail(GC_ERR_ARG, "y over the residual needs its stride, %lld and not %lld", (long long)ldr, (long long)ldy);
   // one row needs no stride, but the layout rules below read it
