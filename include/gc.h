@@ -408,7 +408,8 @@ int gc_linear_backward(const void* dy, int64_t lddy, const void* z, int64_t ldz,
  *   A = X X^T,  X <- (a I + b A + c A^2) X
  * (X^T X from the right where a matrix is higher than wide: the same polynomial of its singular values), which draws all
  * singular values towards 1: Newton-Schulz.  For `batch` matrices of rows x cols values of dtype.
- *   U, out   rows ldu, ldo elements apart, matrices stride_u, stride_o apart (not read for one matrix); out may be U.
+ *   U, out   rows ldu, ldo elements apart, matrices stride_u, stride_o apart (not read for one matrix); out may be U, a batch's
+ *            with the same strides.
  *            Matrices of a batch may lie one after the other or side by side; they must not overlap.  Any alignment.
  *   coeffs   a, b, c (host), or NULL: 3.4445, -4.7750, 2.0315, whose slope at 0 is so steep that five steps bring singular
  *            values from 0.01 to between 0.7 and 1.2.  Refused where they take singular values of at most 1 past 4.

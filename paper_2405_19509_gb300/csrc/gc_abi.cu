@@ -573,6 +573,9 @@ int gc_orthogonalize(const void* U, int64_t ldu, int64_t stride_u, int dtype, in
   if ((rc = check_mats("U", U, ldu, stride_u, batch, rows, cols, e)) ||
       (rc = check_mats("out", out, ldo, stride_o, batch, rows, cols, e)))
     return rc;
+  // the matrices of a batch run at once: in another layout one's result would lie on another's values
+  if (out == U && batch > 1 && (stride_o != stride_u || (rows > 1 && ldo != ldu)))
+    return fail(GC_ERR_ARG, "a batch in place needs U's strides for out");
   if ((rc = check_ws(ws, ws_bytes, ns_ws_bytes(s)))) return rc;
   Carve c(ws);
   const NsIO io{U, nullptr, out, ldu, stride_u, 0, 0, ldo, stride_o, eps, 0.f, 0.f, 0.f, 0.f, 0};
