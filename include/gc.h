@@ -388,7 +388,8 @@ int gc_linear(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ld
  *   X, W   as in gc_linear; X may be NULL without G, W without dX.
  *   dX     T rows of C values of x_dtype, lddx apart, overlapping no input.
  *   G, Gb  N rows of F * C and of F fp32, ldg and ldgb apart: slices of the chunk gradients of a model.
- * dX, G and Gb are each nullable, not all of them.  T <= 2^30.  Any alignment.  All sums have a fixed order; G and Gb of
+ * dX, G and Gb are each nullable, not all of them.  T <= 2^30, and less than 2^31 blocks of 32 x 32 values of dX and G.  Any
+ * alignment.  All sums have a fixed order; G and Gb of
  * a chunk depend on its rows alone, bit for bit, whatever chunks the call has besides.
  * With bf16 rows d enters G as three bf16 parts (24 bits) and dX as bf16 hi + lo (2^-17), as it is without an activation, an
  * fp32 W as hi + lo.

@@ -474,19 +474,23 @@ int gc_linear(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ld
   return launch_linear(s, io, c, status_of(ws), as_stream(stream));
 }
 
-static int check_linear_grad(int N, int n_c, int C, int F, int x_dtype, int w_dtype, int act) {
+static int check_linear_grad(int N, int n_c, int C, int F, int x_dtype, int w_dtype, int act, int want) {
   if (N < 1 || n_c < 1) return fail(GC_ERR_SHAPE, "N, n_c must be >= 1");
   int rc = check_linear((int64_t)N * n_c, C, F, x_dtype, w_dtype, act);
   if (rc) return rc;
   if ((long long)N * ((F + 255) / 256) * ((C + 127) / 128) > (1 << 30) ||
       (long long)N * ((n_c + 63) / 64) * ((F + 255) / 256) > (1 << 30) || (long long)N * ((F + 31) / 32) > (1 << 30))
     return fail(GC_ERR_UNSUPPORTED, "too many tiles: N=%d, n_c=%d, C=%d, F=%d", N, n_c, C, F);
+  // chunks of a few values take blocks of 32 x 32 of dX and of G, in one launch
+  const long long ct = (C + 31) / 32, ft = (F + 31) / 32, T = (long long)N * n_c;
+  if ((want & LINEAR_G) && N * ft * ct + (want & LINEAR_DX ? (T + 31) / 32 * ct : 0) > INT32_MAX)
+    return fail(GC_ERR_UNSUPPORTED, "too many blocks: N=%d, C=%d, F=%d", N, C, F);
   return GC_OK;
 }
 
 size_t gc_linear_backward_workspace(int N, int n_c, int C, int F, int x_dtype, int w_dtype, int act, int x_16,
                                     int w_16, int dy_16, int want) {
-  if (check_linear_grad(N, n_c, C, F, x_dtype, w_dtype, act)) return 0;
+  if (check_linear_grad(N, n_c, C, F, x_dtype, w_dtype, act, want)) return 0;
   return linear_grad_ws_bytes(LinearGradShape{N, n_c, C, F, x_dtype, w_dtype, act, x_16, w_16, dy_16, want});
 }
 
@@ -495,9 +499,9 @@ int gc_linear_backward(const void* dy, int64_t lddy, const void* z, int64_t ldz,
                        void* dX, int64_t lddx, float* G, int64_t ldg, float* Gb, int64_t ldgb, void* ws,
                        size_t ws_bytes, void* stream) {
   NvtxRange nvtx_("gc_linear_backward");
-  int rc = check_linear_grad(N, n_c, C, F, x_dtype, w_dtype, act);
-  if (rc) return rc;
   const int want = (dX ? LINEAR_DX : 0) | (G ? LINEAR_G : 0) | (Gb ? LINEAR_GB : 0);
+  int rc = check_linear_grad(N, n_c, C, F, x_dtype, w_dtype, act, want);
+  if (rc) return rc;
   if (!want) return fail(GC_ERR_ARG, "one of dX, G and Gb must be non-NULL");
   const int64_t T = (int64_t)N * n_c;
   const int xe = x_dtype == GC_BF16 ? 2 : 4, we = w_dtype == GC_BF16 ? 2 : 4;
