@@ -102,7 +102,7 @@ int launch_linear(const LinearShape& s, const LinearIO& io, Carve& ws, uint32_t*
   if (!w.x_in_place || !w.w_in_place) {
     const PartsJob none{};
     if ((rc = launch_parts(w.x_in_place ? none : parts_job(io.X, s.x_dtype, io.ldx, s.T, s.C, w.Cp, w.nx, w.X),
-                           w.w_in_place ? none : parts_job(io.W, s.w_dtype, io.ldw, s.F, s.C, w.Cp, w.nw, w.W), false, st)))
+                           w.w_in_place ? none : parts_job(io.W, s.w_dtype, io.ldw, s.F, s.C, w.Cp, w.nw, w.W), st)))
       return rc;
     chained = true;
   }

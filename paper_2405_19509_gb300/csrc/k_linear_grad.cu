@@ -313,7 +313,7 @@ int launch_grad_tiles(const LinearGradShape& s, const LinearGradIO& io, Carve& w
     if (rc) return rc;
     chained = true;
   } else if (xp.blocks + wp.blocks) {
-    if ((rc = launch_parts(xp, wp, false, st))) return rc;
+    if ((rc = launch_parts(xp, wp, st))) return rc;
     chained = true;
   }
   const bool gb_in_tiles = w.sums && (dx || g) && w.R <= kMostSums;

@@ -305,14 +305,14 @@ int launch_typed(const LinearShape& s, const LinearIO& io, const Finish& f, cuda
 }
 
 template <typename TX, typename TW>
-int launch_grad_typed(const LinearGradShape& s, const LinearGradIO& io, const Finish& f, bool chained, cudaStream_t st) {
+int launch_grad_typed(const LinearGradShape& s, const LinearGradIO& io, const Finish& f, cudaStream_t st) {
   const bool vec = rowwise::rows_16(io.dy, io.lddy, sizeof(TX)) && rowwise::rows_16(s.act == GC_ACT_NONE ? nullptr : io.z, io.ldz, sizeof(TX));
   const int ct = (s.C + kT - 1) / kT, ft = (s.F + kT - 1) / kT;
   const long long T = (long long)s.N * s.n_c;
   const int ndx = io.dX ? (int)((T + kT - 1) / kT) * ct : 0;
   const int ng = io.G ? s.N * ft * ct : io.Gb ? s.N * ft : 0;
   return launch_chain(vec ? k_linear_grad_small<TX, TW, true> : k_linear_grad_small<TX, TW, false>, "k_linear_grad_small",
-                      (unsigned)(ndx + ng), 256, 0, 1, chained, st, (const TX*)io.dy, (long long)io.lddy, (const TX*)io.z,
+                      (unsigned)(ndx + ng), 256, 0, 1, false, st, (const TX*)io.dy, (long long)io.lddy, (const TX*)io.z,
                       (long long)io.ldz, (const TX*)io.X, (long long)io.ldx, (const TW*)io.W, (long long)io.ldw, s.act, s.n_c,
                       T, s.C, ndx, f, s.F, io.G, (long long)io.ldg, io.Gb, (long long)io.ldgb);
 }
@@ -329,10 +329,10 @@ int launch_linear_small(const LinearShape& s, const LinearIO& io, const linear::
 int launch_linear_grad_small(const LinearGradShape& s, const LinearGradIO& io, const linear::Finish& f, cudaStream_t st) {
   const bool wb = s.w_dtype == GC_BF16;
   if (s.x_dtype == GC_BF16)
-    return wb ? launch_grad_typed<__nv_bfloat16, __nv_bfloat16>(s, io, f, false, st)
-              : launch_grad_typed<__nv_bfloat16, float>(s, io, f, false, st);
-  return wb ? launch_grad_typed<float, __nv_bfloat16>(s, io, f, false, st)
-            : launch_grad_typed<float, float>(s, io, f, false, st);
+    return wb ? launch_grad_typed<__nv_bfloat16, __nv_bfloat16>(s, io, f, st)
+              : launch_grad_typed<__nv_bfloat16, float>(s, io, f, st);
+  return wb ? launch_grad_typed<float, __nv_bfloat16>(s, io, f, st)
+            : launch_grad_typed<float, float>(s, io, f, st);
 }
 
 }  // namespace gc

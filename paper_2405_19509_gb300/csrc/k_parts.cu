@@ -16,8 +16,8 @@ __global__ void __launch_bounds__(256) k_parts(const PartsJob a, const PartsJob 
 
 }  // namespace
 
-int launch_parts(const PartsJob& a, const PartsJob& b, bool chained, cudaStream_t s) {
-  return launch_chain(k_parts, "k_parts", (unsigned)(a.blocks + b.blocks), 256, 0, 1, chained, s, a, b);
+int launch_parts(const PartsJob& a, const PartsJob& b, cudaStream_t s) {
+  return launch_chain(k_parts, "k_parts", (unsigned)(a.blocks + b.blocks), 256, 0, 1, false, s, a, b);
 }
 
 }  // namespace gc

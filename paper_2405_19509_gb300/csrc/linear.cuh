@@ -22,7 +22,7 @@ inline PartsJob parts_job(const void* x, int dtype, int64_t ld, long long rows, 
                   (int)std::min<long long>(blocks, 16LL * device_sm_count()), out};
 }
 // Two matrices' in one launch (k_parts.cu).
-int launch_parts(const PartsJob& a, const PartsJob& b, bool chained, cudaStream_t s);
+int launch_parts(const PartsJob& a, const PartsJob& b, cudaStream_t s);
 
 namespace linear {
 
