@@ -31,3 +31,8 @@ def test_more_blocks_than_a_launch_has(kw):
 
 def test_as_many_blocks_as_a_launch_has():
     assert _bwd(N=(1 << 30) - (1 << 27), n_c=1, F=1, C=33, lddy=64, ldz=64, ldgb=64, n=0) == -6
+
+
+def test_version():
+    """0.4: the linear layers and the orthogonalised matrices."""
+    assert _lib().gc_version() >= 400
