@@ -9,7 +9,7 @@
 // fp32 value keep 8 bits each whatever its size, fp16 parts 11 each of values that are scaled to the middle of the range.
 //
 // Sums: an addition in tensor memory is cut off, not rounded, about 4e-8 of the sum so far a step and always towards zero.  So the
-// products of a K block are added from the smallest parts' to the largest's, which alone meet a sum of full size where a segment
+// products of a K block end with the largest parts', which alone meet a sum of full size where a segment
 // begins (4,096 x 2048 -> 4096 in fp32: 1.2e-6 off in the 2-norm the other way round, 0.64e-6 so, at the same time), and 32-bit
 // results leave tensor memory every `seg` K blocks and are added in registers.
 //
@@ -323,6 +323,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
       for (int k = 0; k < njobs && ok; ++k) {
         const Job t = Op::job(p, unit, k);
         Way<TN> way(q, t, smem, t.a_mn, t.b_mn);
+        // from A's smallest part, with those of B that are taken with it, to the largest; found here, since what the issuing
+        // warp does between two K blocks of one product shows (8192 x 2048 -> 8192: 3%)
+        const int b_parts = min(t.nb, t.lim + 1 - t.na);
+        const uint32_t a_end = (uint32_t)((t.na - 1) * (A_BYTES >> 4)), b_end = (uint32_t)((b_parts - 1) * (B_BYTES >> 4));
         for (int kb = 0, left = 0; kb < t.nkb; ++kb) {
           const int ab = use & 1;
           if (left == 0) {
@@ -342,18 +346,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
             const uint32_t d = tmem_base + (uint32_t)(ab * TN);
             // the descriptors of the stage: only the address, in 16-byte units, differs
             const uint64_t at = (uint64_t)((uint32_t)s * (uint32_t)q.stage_bytes >> 4);
-            const uint64_t da = way.a + at, db = way.b + at;
-            uint32_t more = opens ? 0u : 1u;
-            for (int o = min(t.lim, t.na + t.nb - 1) - 1; o >= 0; --o) {
-              for (int i = max(0, o - t.nb + 1); i <= min(o, t.na - 1); ++i) {
-                const uint64_t pa = da + (uint64_t)(i * (A_BYTES >> 4)), pb = db + (uint64_t)((o - i) * (B_BYTES >> 4));
+            uint64_t da = way.a + at + a_end;
+            uint32_t more = opens ? 0u : 1u, end = b_end;
+            int i = t.na, n = b_parts;
+            do {
+              uint64_t db = way.b + at + end;
+              int j = n;
+              do {
 #pragma unroll
                 for (int ks = 0; ks < BK / 16; ++ks) {
-                  mma(d, pa + (uint64_t)(ks * way.a_step), pb + (uint64_t)(ks * way.b_step), way.idesc, more);
+                  mma(d, da + (uint64_t)(ks * way.a_step), db + (uint64_t)(ks * way.b_step), way.idesc, more);
                   more = 1u;
                 }
+                db -= B_BYTES >> 4;
+              } while (--j > 0);
+              da -= A_BYTES >> 4;
+              if (n < t.nb) {
+                ++n;
+                end += B_BYTES >> 4;
               }
-            }
+            } while (--i > 0);
             commit_to(&empty[s], pair);
             if (closes) commit_to(&tfull[ab], pair);
           }
