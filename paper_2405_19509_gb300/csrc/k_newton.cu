@@ -17,7 +17,7 @@
 // tensor memory every two K blocks: 0.5 to 7.8e-6 from 64 bits in the 2-norm over 130 shapes up to 4100 wide, dense and sparse ones,
 // where fp32 has up to 3.6e-6 (one part: 2e-3 to 2e-2).  Of rank 20 or less up to 1.4e-4, fp32 2.2e-4: what rounding leaves of
 // singular values of 0 is enlarged as any small one.  A bf16 u, whose result is rounded to 1.66e-3, takes the same parts, with sums
-// of up to 2,048 steps in tensor memory: of X in A and P in one part each the result was 1.75 to 1.95e-3 off.
+// of four K blocks in tensor memory: of X in A and P in one part each the result was 1.75 to 1.95e-3 off.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -506,7 +506,7 @@ int launch_product(const NsShape& s, const Product& g, const Split& cut, const P
   p.k = Ranges(nkb, cut.ks);
   p.by_per = Divisor((uint32_t)p.per);
   p.by_nt = Divisor((uint32_t)p.nt);
-  p.seg = segment(bits16, kProd, nkb);
+  p.seg = bits16 ? std::min(nkb, 4) : segment(false, kProd, nkb);
   p.a_mn = g.a_mn;
   p.b_mn = g.b_mn;
   p.a_sym = g.a_sym;

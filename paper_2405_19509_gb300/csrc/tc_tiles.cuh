@@ -453,8 +453,8 @@ inline int tiles_of(long long n, int tile) { return (int)((n + tile - 1) / tile)
 // K blocks that are summed in tensor memory at a time.  Of a 32-bit result so few that the additions that meet a sum of full size
 // stay below 28 (six products of two K blocks; three of two 16, one of six 24), off by 0.3 to 0.65e-6 in the 2-norm, as sums in
 // fp32 registers are.  Each such end of a segment costs some 700 clocks: 8 x 1024 x 2048 -> 8192 with G of three products takes 876 us
-// with two K blocks, 814 with four, off by 0.8e-6, and 1105 with one.  Of a result of 16 bits 2,048 steps, which lose 4e-5.
-inline int segment(bool bits16, int prod, int nkb) { return std::min(nkb, bits16 ? std::max(1, 512 / prod) : std::max(2, 6 / prod)); }
+// with two K blocks, 814 with four, off by 0.8e-6, and 1105 with one.  Of a result of 16 bits 512 steps, which lose 1e-5.
+inline int segment(bool bits16, int prod, int nkb) { return std::min(nkb, bits16 ? 128 / prod : std::max(2, 6 / prod)); }
 
 // Clocks of a K block.  A 256-wide tile keeps the tensor pipe busy (512 a product, 570 measured for one); a 128-wide one reads
 // its operands from shared memory for half the work and is bound by that: 633 for one product, 1,010 for three.

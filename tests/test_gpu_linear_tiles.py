@@ -234,3 +234,19 @@ def test_slices_of_a_gradient_matrix(gc):
     got = gc.gc_linear_backward(dy, X, W, N, n_c, z=z, act=gc.GC_ACT_GELU, G=G, Gb=Gb)
     assert torch.equal(G, want["G"]) and torch.equal(Gb, want["Gb"]) and torch.equal(got["dx"], want["dx"])
     assert bool((all_[:, :7] == -77).all()) and bool((all_[:, 7 + F * C + F:] == -77).all())
+
+
+@pytest.mark.parametrize("w", ["bf16", "f32"])
+def test_long_sums_of_bf16_results_are_not_cut_off(gc, w):
+    """Rounding a result to bf16 leaves its size what it is on average, to 2^-9 over the root of 300,000 values: 4e-6.  512 additions in a row
+    in tensor memory are each cut off by up to 2^-24 of a running sum whose share grows evenly to all of it: 512 * 2^-24 / 2 = 1.5e-5."""
+    T, C, F = 300, 1 << 15, 1000
+    _by_tiles(gc, T, C, F, "bf16", w)
+    _back_by_tiles(gc, 1, T, F, C, "bf16", w, 1)
+    m = Maker(21)
+    X, W = m.mat(T, C, torch.bfloat16), m.mat(F, C, TYPES[w], C ** -0.5)
+    size = lambda got, ref: abs(((got.double() * ref).sum() / (ref * ref).sum()).item() - 1)
+    assert size(gc.gc_linear(X, W)["y"], X.double() @ W.double().T) <= 2e-5
+    V, z = m.mat(C, F, TYPES[w], C ** -0.5), m.mat(T, C, torch.bfloat16)
+    got = gc.gc_linear_backward(X, X[:, :F], V, 1, T, z=z, act=gc.GC_ACT_GELU, G=False, Gb=False)
+    assert size(got["dx"], _ref_grad(X, z, X[:, :F], V, "gelu", 1)["dx"][0]) <= 2e-5

@@ -149,3 +149,13 @@ def test_low_rank(gc, r, n):
     left, 485, 141, 41, 12 and 3.4: 6.8e-5 + 8.3e-5, beside |O| of about |X| then."""
     u = _by_tiles(gc, (_randn(3, r, 3) @ _randn(4, 3, n))[None])
     assert _off(gc.gc_orthogonalize(u), _ref(u)) <= 1.6e-4
+
+
+@pytest.mark.parametrize("x,off", [("bf16", 2e-5), ("f32", 1e-5)])
+@pytest.mark.parametrize("r,n", [(80, 40000), (2048, 2100)])
+def test_long_sums_are_not_cut_off(gc, r, n, x, off):
+    """Rounding leaves the size of the result what it is on average.  Four K blocks (two in fp32) of three products are cut off by
+    up to 40 (16) times 2^-24 of a running sum of a half, 1.2e-6 (0.5e-6) a product; fifteen products 1.8e-5 (0.75e-5)."""
+    u = _by_tiles(gc, _gradient(r, 1, r, n).to(TYPES[x]))
+    ref = _ref(u)
+    assert abs(((gc.gc_orthogonalize(u).double() * ref).sum() / (ref * ref).sum()).item() - 1) <= off
