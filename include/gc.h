@@ -111,6 +111,7 @@ int gc_set_wait_limit(int64_t cycles);
 #define GC_STALL_XENT 16       /* softmax cross entropy (its first pass)      */
 #define GC_STALL_LINEAR 32     /* the linear layer's product, forward or backward */
 #define GC_STALL_MUON 64       /* the first product of gc_orthogonalize, gc_muon_step */
+/* (of both the products on the tensor cores: small layers and matrices, in kernels that wait for no copy, leave the bit armed) */
 int gc_inject_stall(int kernels);
 
 /* Path of the batched decode (gc_decode_batch, gc_decode_apply,
@@ -366,8 +367,9 @@ int gc_softmax_xent(const void* X, int64_t ldx, int x_dtype, const void* W, int6
  * y and z must not overlap X, W or one another, nor z the residual.  Any alignment.  rows 0 .. 2^30 (0: nothing is
  * launched), C, F 1 .. 2^20.
  * bf16 operands are used as they are; an fp32 W beside bf16 rows as bf16 hi + lo (2^-17), and fp32 rows as three bf16
- * parts (24 bits) in as many products as an fp32 result needs.  A row of X reaches its own row of y alone, whatever it
- * holds; of an fp32 row or W an infinity gives infinities or NaN.
+ * parts (24 bits) in as many products as an fp32 result needs: off by up to 6.5e-7 in the 2-norm.  A row of X reaches its own row of y
+ * alone, whatever it holds; of an fp32 row or W an infinity gives infinities or NaN.  act of +infinity is that, of
+ * -infinity 0 for relu and NaN for the others, as their formulas are evaluated.
  * Workspace: gc_linear_workspace bytes (copies of X and W in parts where they are fp32 or lie on no 16-byte boundary,
  * which x_16 and w_16 say; sums of ranges of C where tiles are few).  The size depends on the current device's number of
  * SMs.
@@ -389,11 +391,11 @@ int gc_linear(const void* X, int64_t ldx, int x_dtype, const void* W, int64_t ld
  *   dX     T rows of C values of x_dtype, lddx apart, overlapping no input.
  *   G, Gb  N rows of F * C and of F fp32, ldg and ldgb apart: slices of the chunk gradients of a model.
  * dX, G and Gb are each nullable, not all of them.  T <= 2^30, and less than 2^31 blocks of 32 x 32 values of dX and G.  Any
- * alignment.  All sums have a fixed order; G and Gb of
- * a chunk depend on its rows alone, bit for bit, whatever chunks the call has besides.
+ * alignment.  All sums have a fixed order; G and Gb of a chunk depend on its rows alone, bit for bit, whatever chunks the call has
+ * besides.
  * With bf16 rows d enters G as three bf16 parts (24 bits) and dX as bf16 hi + lo (2^-17), as it is without an activation, an
- * fp32 W as hi + lo.
- * fp32 rows enter as in gc_linear.
+ * fp32 W as hi + lo.  fp32 rows enter as in gc_linear.  G, Gb and an fp32 dX are off by up to 6.5e-7 in the 2-norm, a bf16 dX by
+ * its own rounding.
  * Workspace: gc_linear_backward_workspace bytes; dy_16: whether dy lies on 16-byte boundaries; want: 1 with dX, 2 with
  * G, 4 with Gb, added up.  The size depends on the current device's number of SMs.
  */
@@ -420,8 +422,8 @@ int gc_linear_backward(const void* dy, int64_t lddy, const void* z, int64_t ldz,
  * those in 64 bits in the 2-norm, where fp32 has up to 4e-6.  Singular values below some 1/500 of the norm are enlarged with what
  * rounding adds to them: of a matrix of low rank, whose other ones are 0 but not its entries, 1.4e-4 (fp32: 2.2e-4).  bf16
  * matrices take the same parts: the result is off by its own rounding.  A value that is not finite makes its own matrix NaN, no other.
- * Workspace: gc_orthogonalize_workspace bytes (8 a value, and 8 m^2 a matrix, m the smaller side, and more for few and
- * small ones).  The size depends on the current device's number of SMs.
+ * Workspace: gc_orthogonalize_workspace bytes (8 a value, and 8 m^2 + 256 a matrix, m the smaller side, and more for few
+ * and small ones).  The size depends on the current device's number of SMs.
  */
 size_t gc_orthogonalize_workspace(int batch, int rows, int cols, int dtype);
 int gc_orthogonalize(const void* U, int64_t ldu, int64_t stride_u, int dtype, int batch, int rows, int cols,

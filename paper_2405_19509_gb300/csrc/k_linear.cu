@@ -4,8 +4,8 @@
 //   k_linear_join   the same epilogue where a tile's sum over C runs in ranges
 //
 // A bf16 x with a bf16 W is one product; an fp32 W enters it as hi + lo (2^-17), two products, so that a bf16 result
-// is rounded once.  An fp32 x enters as three parts, 24 bits: with an fp32 W six products (parts i + j < 3), which keep
-// what an fp32 product keeps.
+// is rounded once.  An fp32 x enters as three parts, 24 bits: with an fp32 W six products (parts i + j < 3), off in the 2-norm by 0.8e-7
+// for C = 64 and 6e-7 from 128 on, where fp32 products are off by 1.4e-7, 2e-7 and, for 8192, 1.6e-6.
 #include "linear_tiles.cuh"
 
 namespace gc {

@@ -24,7 +24,8 @@ constexpr int kMostSums = 64;  // blocks of a chunk whose sums the tiles' warps 
 
 // A block: 256 columns of 128 points of a chunk, a warp every eighth row, the next one's loads ahead.  The blocks past `blocks` form
 // the parts of x and of W.  Bound: HBM and instructions (34 a value with gelu'); four blocks an SM, for which whole rows' loads
-// have the registers, take 104 us for 8 x 1024 x 8192 in bf16 where three take 109, and 72 for 71 on rows of no alignment.
+// have the registers, take 104 us for 8 x 1024 x 8192 in bf16 and two parts where three take 109, and 72 for 71 on rows of no
+// alignment; 111 with three parts.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256, VEC ? 4 : 3)
     k_linear_d(const T* __restrict__ dy, long long lddy, const T* __restrict__ z, long long ldz, int act, int N, int n_c,

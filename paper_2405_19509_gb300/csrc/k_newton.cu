@@ -13,11 +13,12 @@
 //
 // Parts are fp16 of values times a power of two.  Singular values stay below kMost (the entry point checks the
 // polynomial), so entries of X, A and P fit, and the parts of an entry end at 2^-24 / scale, 2^-37 for X: what is lost is
-// absolute, beside singular values of 1, or of lam where a step's X has none above that (k_ns_scale).  X, A and P take two parts everywhere, 22 bits, three products each, whose sums leave
-// tensor memory every two K blocks: 0.5 to 7.8e-6 from 64 bits in the 2-norm over 130 shapes up to 4100 wide, dense and sparse ones,
-// where fp32 has up to 3.6e-6 (one part: 2e-3 to 2e-2).  Of rank 20 or less up to 1.4e-4, fp32 2.2e-4: what rounding leaves of
-// singular values of 0 is enlarged as any small one.  A bf16 u, whose result is rounded to 1.66e-3, takes the same parts, with sums
-// of four K blocks in tensor memory: of X in A and P in one part each the result was 1.75 to 1.95e-3 off.
+// absolute, beside singular values of 1, or of lam where a step's X has none above that (k_ns_scale).
+// X, A and P take two parts everywhere, 22 bits, three products each, whose sums leave tensor memory every two K blocks: 0.4 to
+// 7.8e-6 from 64 bits in the 2-norm over 130 shapes up to 4100 wide, dense and sparse ones, where torch's fp32 products have 0.3 to
+// 4.3e-6 (one part: 2e-3 to 2e-2).  Of rank 20 or less up to 1.4e-4, torch's 2.2e-4: what rounding leaves of singular values of 0 is
+// enlarged as any small one.  A bf16 u, whose result is rounded to 1.66e-3, takes the same parts, and sums of four K blocks, which take
+// 3% less than of two: with X in A and P in one part each the result was 1.75 to 1.95e-3 off.
 #include <cuda_fp16.h>
 #include <math.h>
 

@@ -251,11 +251,11 @@ inline int launch_join(const float* part, int ks, long long rows, int ld, const 
 
 // Small layers, in fp32 products (k_linear_small.cu).  G and Gb of a chunk have the same bits whatever chunks a call has, so
 // their choice looks at a chunk's work alone.
-// Measured as graph replays, kernels here against tiles (us): 2^24 products in bf16 6.2 against 11.6, 2^25 6.3 against 11.6, 2^26
-// 10.8 against 12.8, 2^27 15 against 13; fp32 2^27 18.5 against 13.5.  Rows of 2048 by 8192 in bf16: one 5.4, two 8.0, four 17, eight
-// 27, against 13.5; with an fp32 W, which tiles copy in parts, 9, 13, 21, 36 against 35.  dx of 2^23.6 8.8 against 14.9, of
-// 2^24.6 15.4 against 13.5; six chunks' G of 2^21 each 6.4 against 15.9, of 2^24 21 against 17.  (A repeated call finds up to some 100 MB
-// of operands in L2.)
+// Measured as graph replays, kernels here against tiles (us): 256 x 256 x 256 in bf16 6.1 against 8.5, x 512, 2^25 products, 6.4 against
+// 8.7, where 2^26 took 10.8 here and take 8.7 on tiles; in fp32 6.8 against 13.1 for 2^25, 18.5 against 13.4 for 2^27.  Rows of 2048
+// by 8192 in bf16: one 5.7, two 7.6, four 17, eight 27, against 12.7; with an fp32 W, which tiles copy in parts, 10, 14, 21, 36 against
+// 40.  dx of 256 x 256 x 160, 2^23.3, 6.7 against 16.8, of 2^24.6 15.4 against 16.8; six chunks' G of 2^21 each 5.4 against 11.9, of 2^24
+// 21 against 17.4.  (A repeated call finds up to some 100 MB of operands in L2.)
 // A sum runs alone in a block there, some 2 us for 64 of its products: 16 x 5632 x 64 took 184 us.
 constexpr int kLinearRows = 8, kLinearSum = 256;
 constexpr double kLinearSmall = 1 << 25, kLinearSmallDx = 1 << 24, kLinearSmallChunk = 1 << 21;

@@ -9,9 +9,9 @@
 // fp32 value keep 8 bits each whatever its size, fp16 parts 11 each of values that are scaled to the middle of the range.
 //
 // Sums: an addition in tensor memory is cut off, not rounded, about 4e-8 of the sum so far a step and always towards zero.  So the
-// products of a K block end with the largest parts', which alone meet a sum of full size where a segment
-// begins (4,096 x 2048 -> 4096 in fp32: 1.2e-6 off in the 2-norm the other way round, 0.64e-6 so, at the same time), and 32-bit
-// results leave tensor memory every `seg` K blocks and are added in registers.
+// products of a K block end with the largest parts', and those before meet no sum of full size where a segment begins (4096 x 2048 ->
+// 4096 in fp32: 1.2e-6 off in the 2-norm the other way round, 0.64e-6 so, at the same time), and 32-bit results leave tensor
+// memory every `seg` K blocks and are added in registers.
 //
 // Bound: the tensor pipe (4 x 128 clocks a K block of one product at TN = 256; TN = 128 spreads few tiles) where tiles are many, else the
 // latency of a tile: barriers, the first loads and the epilogue, some 3 us.  Every wait is bounded (GC_ERR_TIMEOUT).
@@ -451,13 +451,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_tiles(const __grid_constant__ M
 inline int tiles_of(long long n, int tile) { return (int)((n + tile - 1) / tile); }
 
 // K blocks that are summed in tensor memory at a time.  Of a 32-bit result so few that the additions that meet a sum of full size
-// stay below 28 (six products of two K blocks; three of two 16, one of six 24), off by 0.3 to 0.65e-6 in the 2-norm, as sums in
-// fp32 registers are.  Each such end of a segment costs some 700 clocks: 8 x 1024 x 2048 -> 8192 with G of three products takes 876 us
-// with two K blocks, 814 with four, off by 0.8e-6, and 1105 with one.  Of a result of 16 bits 512 steps, which lose 1e-5.
+// are at most 28 (six products of two K blocks; three of two 16, one of six 24): 0.1 to 0.65e-6 off in the 2-norm whatever K, where
+// torch's fp32 products are off by 0.15e-6 for K = 64 and 1.6e-6 for 8192.  Each end of a segment costs some 700 clocks:
+// 8 x 1024 x 2048 -> 8192 with G of three products takes 876 us with two K blocks, 814 with four, 0.8e-6 off, and 1105 with one; sums of
+// up to four K blocks would be 0.1e-6 off with one, for 13 to 30% of the time.  Of a result of 16 bits 512 steps, which lose 1e-5.
 inline int segment(bool bits16, int prod, int nkb) { return std::min(nkb, bits16 ? 128 / prod : std::max(2, 6 / prod)); }
 
-// Clocks of a K block.  A 256-wide tile keeps the tensor pipe busy (512 a product, 570 measured for one); a 128-wide one reads
-// its operands from shared memory for half the work and is bound by that: 633 for one product, 1,010 for three.
+// Clocks of a K block, as measured.  A 256-wide tile keeps the tensor pipe busy, 512 a product, 570 for one; a 128-wide one, whose
+// products are 256 each, takes 633 for one and 1,010 for three, for a reason that has not been found.
 inline double block_clocks(int tn, int prod) { return tn == 256 ? 60 + 512.0 * prod : 440 + 190.0 * prod; }
 
 // Width of the tiles and ranges of K for a product of `values` in tiles(width) tiles over nkb K blocks: the cut whose
